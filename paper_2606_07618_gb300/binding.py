@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libnvfp4ss.so (include/nvfp4ss.h).
+"""Thin ctypes binding of libnvfp4ss.so (include/nvfp4ss.h, include/nvfp4mm.h).
 
 Every function has the name of the C entry point it calls and only marshals
 arguments: torch CUDA tensors become device pointers, the current torch CUDA
@@ -20,6 +20,9 @@ NVFP4_OBJ_MSE, NVFP4_OBJ_WMSE = 0, 1
 NVFP4_SF_LINEAR, NVFP4_SF_SWIZZLED = 1, 2
 NVFP4_WINDOW_DEFAULT = -(2 ** 31)
 NVFP4_WINDOW_TIGHT = -(2 ** 31) + 1
+
+FP4_FMT_NVFP4, FP4_FMT_MXFP4 = 0, 1
+FP4_ACT_SILU, FP4_ACT_GELU_TANH = 0, 1
 
 STATUS = {0: "NVFP4_OK", 1: "NVFP4_ERR_INVALID_ARG", 2: "NVFP4_ERR_UNSUPPORTED", 3: "NVFP4_ERR_ALIGNMENT",
           4: "NVFP4_ERR_RANGE", 5: "NVFP4_ERR_CUDA"}
@@ -49,6 +52,11 @@ class GroupTensor(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("w", ctypes.c_void_p),
                 ("w_row_stride", ctypes.c_int64), ("codes", ctypes.c_void_p), ("sf_linear", ctypes.c_void_p),
                 ("sf_swizzled", ctypes.c_void_p)]
+
+
+class Fp4Operand(ctypes.Structure):
+    """fp4_operand: codes, 128x4-atom scales and global scale of a quantised matrix."""
+    _fields_ = [("codes", ctypes.c_void_p), ("sf", ctypes.c_void_p), ("S", ctypes.c_void_p)]
 
 
 def library_path() -> str:
@@ -88,6 +96,20 @@ def lib() -> ctypes.CDLL:
         L.nvfp4_ldlq_prepare.argtypes = [p, i64, f, p, p, p, p, p, sz, p]
         L.nvfp4_ldlq_workspace.argtypes, L.nvfp4_ldlq_workspace.restype = [i64, i64], sz
         L.ldlq_quantize.argtypes = [p, i, i64, i64, i, p, p, p, p, p, p, p, sz, p]
+        op = ctypes.POINTER(Fp4Operand)
+        L.mxfp4_quantize.argtypes = [p, i, i64, i64, i64, p, p, p, p, p]
+        L.mxfp4_dequantize.argtypes = [p, p, i, i64, i64, p, i, p]
+        L.fp4_matmul.argtypes = [i, op, op, i64, i64, i64, p, i, i64, p, p]
+        L.fp4_matmul_backward_workspace.argtypes, L.fp4_matmul_backward_workspace.restype = [i64, i64, i64], sz
+        L.fp4_matmul_backward.argtypes = [i, op, op, i64, i64, i64, p, i64, p, i64, p, i64, p, p, sz, p]
+        L.fp4_gated_ff.argtypes = [i, i, op, op, op, i64, i64, i64, p, i64, p, p, p, p]
+        L.fp4_gated_ff_backward_workspace.argtypes = [i64, i64, i64]
+        L.fp4_gated_ff_backward_workspace.restype = sz
+        L.fp4_gated_ff_backward.argtypes = [i, i, op, op, op, i64, i64, i64, p, i64, p, i64, p, p, i64, p, i64, p, p, sz,
+                                            p]
+        for fn in ("mxfp4_quantize", "mxfp4_dequantize", "fp4_matmul", "fp4_matmul_backward", "fp4_gated_ff",
+                   "fp4_gated_ff_backward"):
+            getattr(L, fn).restype = i
         for fn in ("nvfp4_global_scale", "nvfp4_global_scale_noalloc", "scalesweep_quantize", "absmax_quantize",
                    "four_over_six_quantize", "nvfp4_dequantize", "scalesweep_quantize_dynamic",
                    "absmax_quantize_dynamic", "nvfp4_optimal_scale", "nvfp4_ldlq_prepare", "ldlq_quantize",
@@ -335,3 +357,147 @@ def nvfp4_row_shard_layout(rows: int, cols: int, block: int, world: int, rank: i
     rc = lib().nvfp4_row_shard_layout(int(rows), int(cols), int(block), int(world), int(rank), ctypes.byref(out))
     _check("nvfp4_row_shard_layout", rc)
     return out
+
+
+# --------------------------------------------------------------------------- 4-bit matrices (nvfp4mm.h)
+def mx_swizzled_bytes(rows: int, cols: int) -> int:
+    """Bytes of the 128x4-atom scale layout of an MXFP4 matrix."""
+    return swizzled_bytes(rows, cols, 32)
+
+
+def _rows(t, what: str) -> int:
+    """Row stride of a 2-d tensor whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a 2-d tensor with contiguous rows is wanted")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _operand(m, what: str):
+    """(codes [rows, cols/2], 128x4-atom scales, S or None) as an fp4_operand, its rows and cols."""
+    codes, sf, S = m
+    if codes.dim() != 2 or not codes.is_contiguous():
+        raise ValueError(f"{what}: contiguous codes [rows, cols/2] are wanted")
+    rows, half = codes.shape
+    return Fp4Operand(codes.data_ptr(), sf.data_ptr(), S.data_ptr() if S is not None else None), rows, 2 * half
+
+
+def _sf_size(fmt: int, m, what: str):
+    codes, sf, _ = m
+    want = swizzled_bytes(codes.shape[0], 2 * codes.shape[1], 32 if fmt == FP4_FMT_MXFP4 else 16)
+    if sf.numel() * sf.element_size() < want:
+        raise ValueError(f"{what}: scales of {want} bytes in the 128x4-atom layout are wanted")
+
+
+def _shaped(t, shape, what: str):
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{what}: shape {shape} is wanted, not {tuple(t.shape)}")
+
+
+def _bf16(t, what: str):
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{what}: bfloat16 is wanted, not {t.dtype}")
+
+
+def mxfp4_quantize(x, codes, sf_linear=None, sf_swizzled=None, status=None, stream=None):
+    """MXFP4 codes and scales of x [rows, cols] (bf16 or fp32, rows contiguous, any row stride)."""
+    rows, cols = x.shape
+    rc = lib().mxfp4_quantize(_ptr(x), _dtype(x), rows, cols, _rows(x, "x"), _ptr(codes), _ptr(sf_linear),
+                              _ptr(sf_swizzled), _ptr(status), _stream(stream))
+    _check("mxfp4_quantize", rc)
+
+
+def mxfp4_dequantize(codes, sf, layout: int, rows: int, cols: int, out, stream=None):
+    rc = lib().mxfp4_dequantize(_ptr(codes), _ptr(sf), int(layout), int(rows), int(cols), _ptr(out), _dtype(out),
+                                _stream(stream))
+    _check("mxfp4_dequantize", rc)
+
+
+def fp4_matmul(fmt: int, a, b, out, status=None, stream=None):
+    """out [m, n] (bf16 or fp32) = A B^T; a = (codes [m, k/2], swizzled scales, S or None), b likewise [n, k/2]."""
+    oa, m, k = _operand(a, "a")
+    ob, n, kb = _operand(b, "b")
+    if k != kb:
+        raise ValueError(f"fp4_matmul: operands of {k} and {kb} columns")
+    _sf_size(fmt, a, "a")
+    _sf_size(fmt, b, "b")
+    _shaped(out, (m, n), "out")
+    rc = lib().fp4_matmul(int(fmt), oa, ob, m, n, k, _ptr(out), _dtype(out), _rows(out, "out"), _ptr(status),
+                          _stream(stream))
+    _check("fp4_matmul", rc)
+
+
+def fp4_matmul_backward_workspace(m: int, n: int, k: int) -> int:
+    return int(lib().fp4_matmul_backward_workspace(int(m), int(n), int(k)))
+
+
+def _grad(t, shape, what: str):
+    """Pointer and row stride of an optional bf16 output."""
+    if t is None:
+        return None, 0
+    _bf16(t, what)
+    _shaped(t, shape, what)
+    return t.data_ptr(), _rows(t, what)
+
+
+def fp4_matmul_backward(fmt: int, a, b, d_out, d_a=None, d_b=None, workspace=None, status=None, stream=None):
+    """Gradients of fp4_matmul's operands from d_out [m, n] (bf16): d_a [m, k], d_b [n, k] (bf16, either None)."""
+    oa, m, k = _operand(a, "a")
+    ob, n, kb = _operand(b, "b")
+    if k != kb:
+        raise ValueError(f"fp4_matmul_backward: operands of {k} and {kb} columns")
+    _sf_size(fmt, a, "a")
+    _sf_size(fmt, b, "b")
+    pd, ldd = _grad(d_out, (m, n), "d_out")
+    pa, lda = _grad(d_a, (m, k), "d_a")
+    pb, ldb = _grad(d_b, (n, k), "d_b")
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    rc = lib().fp4_matmul_backward(int(fmt), oa, ob, m, n, k, pd, ldd, pa, lda, pb, ldb, _ptr(status), _ptr(workspace),
+                                   ws_bytes, _stream(stream))
+    _check("fp4_matmul_backward", rc)
+
+
+def _gated_operands(fn: str, fmt: int, x, w_gate, w_up):
+    ox, t, d = _operand(x, "x")
+    og, f, dg = _operand(w_gate, "w_gate")
+    ou, fu, du = _operand(w_up, "w_up")
+    if dg != d or du != d or fu != f:
+        raise ValueError(f"{fn}: operands [{t}, {d}], [{f}, {dg}] and [{fu}, {du}]")
+    for m, what in ((x, "x"), (w_gate, "w_gate"), (w_up, "w_up")):
+        _sf_size(fmt, m, what)
+    return ox, og, ou, t, f, d
+
+
+def fp4_gated_ff(fmt: int, act: int, x, w_gate, w_up, h=None, h_codes=None, h_sf=None, status=None, stream=None):
+    """act(x Wg^T) * (x Wu^T) of quantised operands, as h [t, f] bf16 and/or as an MXFP4 operand (h_codes [t, f/2],
+    h_sf of mx_swizzled_bytes(t, f) bytes)."""
+    ox, og, ou, t, f, d = _gated_operands("fp4_gated_ff", fmt, x, w_gate, w_up)
+    ph, ldh = _grad(h, (t, f), "h")
+    if h_codes is not None:
+        _shaped(h_codes, (t, f // 2), "h_codes")
+        if h_sf is not None and h_sf.numel() < mx_swizzled_bytes(t, f):
+            raise ValueError(f"h_sf: {mx_swizzled_bytes(t, f)} bytes are wanted")
+    rc = lib().fp4_gated_ff(int(fmt), int(act), ox, og, ou, t, f, d, ph, ldh, _ptr(h_codes), _ptr(h_sf), _ptr(status),
+                            _stream(stream))
+    _check("fp4_gated_ff", rc)
+
+
+def fp4_gated_ff_backward_workspace(t: int, f: int, d: int) -> int:
+    return int(lib().fp4_gated_ff_backward_workspace(int(t), int(f), int(d)))
+
+
+def fp4_gated_ff_backward(fmt: int, act: int, x, w_gate, w_up, d_h, d_x=None, d_gate=None, d_up=None, h=None,
+                          workspace=None, status=None, stream=None):
+    """Gradients of fp4_gated_ff's operands from d_h [t, f] (bf16): d_x [t, d], d_gate and d_up [f, d] (bf16, d_x or the
+    pair may be None); h [t, f] optionally receives the forward result."""
+    ox, og, ou, t, f, d = _gated_operands("fp4_gated_ff_backward", fmt, x, w_gate, w_up)
+    pdh, lddh = _grad(d_h, (t, f), "d_h")
+    px, ldx = _grad(d_x, (t, d), "d_x")
+    pg, ldg = _grad(d_gate, (f, d), "d_gate")
+    pu, ldu = _grad(d_up, (f, d), "d_up")
+    if pg and pu and ldg != ldu:
+        raise ValueError("d_gate and d_up: one row stride is wanted")
+    ph, ldh = _grad(h, (t, f), "h")
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    rc = lib().fp4_gated_ff_backward(int(fmt), int(act), ox, og, ou, t, f, d, pdh, lddh, px, ldx, pg, pu, ldg, ph, ldh,
+                                     _ptr(status), _ptr(workspace), ws_bytes, _stream(stream))
+    _check("fp4_gated_ff_backward", rc)

@@ -11,6 +11,7 @@
 #include <cuda_runtime.h>
 
 #include "group_kernels.h"
+#include "host_checks.h"
 #include "ldlq_kernels.h"
 #include "nvfp4_kernels.h"
 #include "nvfp4ss.h"
@@ -18,50 +19,6 @@
 using namespace nvfp4;
 
 namespace {
-
-int sm_count() {
-    static std::atomic<int> cache[64];           // zero-initialised; 0 = not looked up yet
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 0;
-    if (dev < 64) {
-        const int c = cache[dev].load(std::memory_order_relaxed);
-        if (c > 0) return c;
-    }
-    int n = 0;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    if (dev < 64) cache[dev].store(n, std::memory_order_relaxed);
-    return n;
-}
-
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-bool mul_ok(int64_t a, int64_t b, int64_t* out) {
-    if (a < 0 || b < 0) return false;
-    if (a != 0 && b > INT64_MAX / a) return false;
-    *out = a * b;
-    return true;
-}
-
-// [p, p+n) and [q, q+m) overlap?
-bool overlap(const void* p, int64_t n, const void* q, int64_t m) {
-    if (!p || !q || n <= 0 || m <= 0) return false;
-    uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-    return a < b + (uintptr_t)m && b < a + (uintptr_t)n;
-}
-
-// The kernels dereference these pointers on the device: reject memory the GPU
-// cannot address (plain pageable host memory or garbage) before launching.
-bool device_accessible(const void* p) {
-    if (!p) return true;
-    cudaPointerAttributes at;
-    cudaError_t e = cudaPointerGetAttributes(&at, p);
-    if (e != cudaSuccess) {
-        (void)cudaGetLastError();
-        return false;
-    }
-    return at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeManaged ||
-           (at.type == cudaMemoryTypeHost && at.devicePointer != nullptr);
-}
 
 struct Shape {
     int64_t n, kb, kpad4, nblocks, nseg, sw_bytes;

@@ -1,0 +1,387 @@
+// Host side of include/nvfp4mm.h: argument, alignment and overlap checks (all before any
+// launch), then dispatch.  As in api.cu nothing allocates, frees or synchronises.
+#include <climits>
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "fp4_kernels.h"
+#include "host_checks.h"
+#include "nvfp4mm.h"
+
+using namespace nvfp4;
+
+namespace {
+
+// Grid limits: 128 rows or columns to a tile, 65535 tiles along a grid dimension.
+constexpr int64_t kMaxRows = 65535ll * 128;
+constexpr int64_t kMaxCols = 1ll << 30;                      // 32-bit tensor-map coordinates
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// Memory that a call reads and writes.
+struct Memory {
+    const void* r[16];
+    const void* w[16];
+    int64_t rn[16], wn[16];
+    int nr = 0, nw = 0;
+    void read(const void* p, int64_t n) { if (p && n > 0) { r[nr] = p; rn[nr++] = n; } }
+    void write(const void* p, int64_t n) { if (p && n > 0) { w[nw] = p; wn[nw++] = n; } }
+    // bytes from the first to the last element of [rows, cols] with row stride ld
+    static int64_t span(int64_t rows, int64_t cols, int64_t ld, int64_t esize) {
+        return rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * esize : 0;
+    }
+    nvfp4_status check() const {
+        for (int i = 0; i < nw; i++) {
+            for (int j = 0; j < nr; j++)
+                if (overlap(w[i], wn[i], r[j], rn[j])) return NVFP4_ERR_INVALID_ARG;
+            for (int j = i + 1; j < nw; j++)
+                if (overlap(w[i], wn[i], w[j], wn[j])) return NVFP4_ERR_INVALID_ARG;
+        }
+        for (int i = 0; i < nw; i++)
+            if (!device_accessible(w[i])) return NVFP4_ERR_INVALID_ARG;
+        for (int i = 0; i < nr; i++)
+            if (!device_accessible(r[i])) return NVFP4_ERR_INVALID_ARG;
+        return NVFP4_OK;
+    }
+};
+
+// Sizes of a dense tensor: rows and row stride that address arithmetic in bytes can hold.
+nvfp4_status check_dense(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t esize) {
+    if (!p) return NVFP4_ERR_INVALID_ARG;
+    if (ld < cols) return NVFP4_ERR_INVALID_ARG;
+    int64_t n;
+    if (!mul_ok(rows, ld, &n) || n > INT64_MAX / 8) return NVFP4_ERR_RANGE;
+    return aligned(p, (uintptr_t)esize) ? NVFP4_OK : NVFP4_ERR_ALIGNMENT;
+}
+
+nvfp4_status check_format(fp4_format fmt, int64_t k) {
+    if (fmt != FP4_FMT_NVFP4 && fmt != FP4_FMT_MXFP4) return NVFP4_ERR_INVALID_ARG;
+    if (k < 32 || k % 32 != 0) return NVFP4_ERR_UNSUPPORTED;
+    return k <= kMaxCols ? NVFP4_OK : NVFP4_ERR_RANGE;
+}
+
+nvfp4_status check_rows(int64_t rows) { return rows < 0 ? NVFP4_ERR_INVALID_ARG : rows > kMaxRows ? NVFP4_ERR_RANGE : NVFP4_OK; }
+
+int64_t sf_bytes(fp4_format fmt, int64_t rows, int64_t k) {
+    return up(rows, 128) * up(k / (fmt == FP4_FMT_MXFP4 ? 32 : 16), 4);
+}
+
+nvfp4_status check_operand(fp4_format fmt, const fp4_operand* o, int64_t rows, int64_t k, Memory* mem) {
+    if (!o || !o->codes || !o->sf) return NVFP4_ERR_INVALID_ARG;
+    if (fmt == FP4_FMT_MXFP4 && o->S) return NVFP4_ERR_INVALID_ARG;
+    if (!aligned(o->codes, 16) || !aligned(o->sf, 16) || !aligned(o->S, 4)) return NVFP4_ERR_ALIGNMENT;
+    mem->read(o->codes, rows * (k / 2));
+    mem->read(o->sf, sf_bytes(fmt, rows, k));
+    mem->read(o->S, 4);
+    return NVFP4_OK;
+}
+
+Operand operand(const fp4_operand* o, int64_t rows) { return Operand{o->codes, o->sf, o->S, rows, 0}; }
+Operand dense(const void* p, const float* S, int64_t rows, int64_t ld) { return Operand{p, nullptr, S, rows, ld}; }
+
+nvfp4_status result(cudaError_t e) {
+    return e == cudaSuccess ? NVFP4_OK : e == cudaErrorNotSupported ? NVFP4_ERR_UNSUPPORTED : NVFP4_ERR_CUDA;
+}
+
+// A bf16 product for a gradient: out[t][n] = S sum_k q[t][k] p[n][k].
+cudaError_t grad_product(const void* p, int64_t prows, int64_t ldp, const void* q, int64_t qrows, int64_t ldq,
+                         int64_t k, const float* S, void* out, int64_t ldo, int* status, int sms, cudaStream_t s) {
+    Product g = {};
+    g.kind = kBf16;
+    g.mode = kPlain;
+    g.p = dense(p, S, prows, ldp);
+    g.q = dense(q, nullptr, qrows, ldq);
+    g.k = k;
+    g.out = out;
+    g.ldo = ldo;
+    g.status = status;
+    return launch_product(g, sms, s);
+}
+
+// Parts of a workspace, each to a multiple of 256 bytes.
+struct Parts {
+    char* base;
+    int64_t used = 0;
+    explicit Parts(void* ws) : base(static_cast<char*>(ws)) {}
+    void* take(int64_t bytes) {
+        void* p = base + used;
+        used += up(bytes, 256);
+        return p;
+    }
+};
+
+// bf16 buffers of fp4_matmul_backward: B and A transposed, dD transposed and re-pitched.
+struct MatmulGrad {
+    int64_t ldm, ldn, bt, at, dt, dp;
+    MatmulGrad(int64_t m, int64_t n, int64_t k)
+        : ldm(up(m, 8)), ldn(up(n, 8)), bt(k * ldn * 2), at(k * ldm * 2), dt(n * ldm * 2), dp(m * ldn * 2) {}
+    size_t bytes() const { return (size_t)(up(bt, 256) + up(at, 256) + up(dt, 256) + up(dp, 256)); }
+};
+
+// and of fp4_gated_ff_backward: both weights side by side transposed, x transposed, dg and
+// du side by side and transposed.
+struct GatedGrad {
+    int64_t fp, ldt, wt, xt, dgu, dgut;
+    GatedGrad(int64_t t, int64_t f, int64_t d)
+        : fp(up(f, 128)), ldt(up(t, 8)), wt(d * 2 * fp * 2), xt(d * ldt * 2), dgu(t * 2 * fp * 2), dgut(2 * fp * ldt * 2) {}
+    size_t bytes() const { return (size_t)(up(wt, 256) + up(xt, 256) + up(dgu, 256) + up(dgut, 256)); }
+};
+
+}  // namespace
+
+extern "C" {
+
+nvfp4_status mxfp4_quantize(const void* x, nvfp4_dtype dt, int64_t rows, int64_t cols, int64_t ldx, uint8_t* codes,
+                            uint8_t* sf_linear, uint8_t* sf_swizzled, int* status_dev, void* stream) {
+    if ((dt != NVFP4_IN_BF16 && dt != NVFP4_IN_F32) || rows < 0 || cols < 0 || cols % 32 != 0) return NVFP4_ERR_INVALID_ARG;
+    if (cols > kMaxCols) return NVFP4_ERR_RANGE;
+    if (rows == 0 || cols == 0) return NVFP4_OK;
+    const int64_t esize = dt == NVFP4_IN_BF16 ? 2 : 4;
+    if (!codes || (!sf_linear && !sf_swizzled)) return NVFP4_ERR_INVALID_ARG;
+    const nvfp4_status st = check_dense(x, rows, cols, ldx, esize);
+    if (st != NVFP4_OK) return st;
+    if (!aligned(codes, 8) || !aligned(sf_swizzled, 4) || !aligned(status_dev, 4)) return NVFP4_ERR_ALIGNMENT;
+    Memory mem;
+    mem.read(x, Memory::span(rows, cols, ldx, esize));
+    mem.write(codes, rows * (cols / 2));
+    mem.write(sf_linear, rows * (cols / 32));
+    mem.write(sf_swizzled, sf_bytes(FP4_FMT_MXFP4, rows, cols));
+    mem.write(status_dev, 4);
+    const nvfp4_status ms = mem.check();
+    if (ms != NVFP4_OK) return ms;
+    const int sms = sm_count();
+    if (sms <= 0) return NVFP4_ERR_CUDA;
+    return result(launch_mxfp4_quantize(x, dt == NVFP4_IN_BF16 ? 0 : 1, rows, cols, ldx, codes, sf_linear, sf_swizzled,
+                                        status_dev, sms, static_cast<cudaStream_t>(stream)));
+}
+
+nvfp4_status mxfp4_dequantize(const uint8_t* codes, const uint8_t* sf, nvfp4_sf_layout layout, int64_t rows,
+                              int64_t cols, void* out, nvfp4_dtype out_dt, void* stream) {
+    if ((out_dt != NVFP4_IN_BF16 && out_dt != NVFP4_IN_F32) || (layout != NVFP4_SF_LINEAR && layout != NVFP4_SF_SWIZZLED) ||
+        rows < 0 || cols < 0 || cols % 32 != 0)
+        return NVFP4_ERR_INVALID_ARG;
+    if (cols > kMaxCols) return NVFP4_ERR_RANGE;
+    if (rows == 0 || cols == 0) return NVFP4_OK;
+    if (!codes || !sf) return NVFP4_ERR_INVALID_ARG;
+    const int64_t esize = out_dt == NVFP4_IN_BF16 ? 2 : 4;
+    const nvfp4_status st = check_dense(out, rows, cols, cols, esize);
+    if (st != NVFP4_OK) return st;
+    if (!aligned(codes, 4) || !aligned(out, 16)) return NVFP4_ERR_ALIGNMENT;
+    const int swizzled = layout == NVFP4_SF_SWIZZLED;
+    Memory mem;
+    mem.read(codes, rows * (cols / 2));
+    mem.read(sf, swizzled ? sf_bytes(FP4_FMT_MXFP4, rows, cols) : rows * (cols / 32));
+    mem.write(out, rows * cols * esize);
+    const nvfp4_status ms = mem.check();
+    if (ms != NVFP4_OK) return ms;
+    const int sms = sm_count();
+    if (sms <= 0) return NVFP4_ERR_CUDA;
+    return result(launch_mxfp4_dequantize(codes, sf, swizzled, rows, cols, out, out_dt == NVFP4_IN_BF16 ? 0 : 1, sms,
+                                          static_cast<cudaStream_t>(stream)));
+}
+
+nvfp4_status fp4_matmul(fp4_format fmt, const fp4_operand* a, const fp4_operand* b, int64_t m, int64_t n, int64_t k,
+                        void* D, nvfp4_dtype out_dt, int64_t ldd, int* status_dev, void* stream) {
+    nvfp4_status st;
+    if (out_dt != NVFP4_IN_BF16 && out_dt != NVFP4_IN_F32) return NVFP4_ERR_INVALID_ARG;
+    if ((st = check_format(fmt, k)) != NVFP4_OK || (st = check_rows(m)) != NVFP4_OK || (st = check_rows(n)) != NVFP4_OK)
+        return st;
+    if (m == 0 || n == 0) return NVFP4_OK;
+    const int64_t esize = out_dt == NVFP4_IN_BF16 ? 2 : 4;
+    Memory mem;
+    if ((st = check_operand(fmt, a, m, k, &mem)) != NVFP4_OK || (st = check_operand(fmt, b, n, k, &mem)) != NVFP4_OK ||
+        (st = check_dense(D, m, n, ldd, esize)) != NVFP4_OK)
+        return st;
+    if (!aligned(status_dev, 4)) return NVFP4_ERR_ALIGNMENT;
+    mem.write(D, Memory::span(m, n, ldd, esize));
+    mem.write(status_dev, 4);
+    if ((st = mem.check()) != NVFP4_OK) return st;
+    const int sms = sm_count();
+    if (sms <= 0) return NVFP4_ERR_CUDA;
+    Product p = {};
+    p.kind = fmt == FP4_FMT_MXFP4 ? kMxfp4 : kNvfp4;
+    p.mode = kPlain;
+    p.p = operand(b, n);
+    p.q = operand(a, m);
+    p.k = k;
+    p.out = D;
+    p.out_f32 = out_dt == NVFP4_IN_F32;
+    p.ldo = ldd;
+    p.status = status_dev;
+    return result(launch_product(p, sms, static_cast<cudaStream_t>(stream)));
+}
+
+size_t fp4_matmul_backward_workspace(int64_t m, int64_t n, int64_t k) {
+    if (m <= 0 || n <= 0 || k <= 0 || m > kMaxRows || n > kMaxRows || k > kMaxCols) return 0;
+    return MatmulGrad(m, n, k).bytes();
+}
+
+nvfp4_status fp4_matmul_backward(fp4_format fmt, const fp4_operand* a, const fp4_operand* b, int64_t m, int64_t n,
+                                 int64_t k, const void* dD, int64_t lddd, void* dA, int64_t ldda, void* dB,
+                                 int64_t lddb, int* status_dev, void* workspace, size_t ws_bytes, void* stream) {
+    nvfp4_status st;
+    if ((st = check_format(fmt, k)) != NVFP4_OK || (st = check_rows(m)) != NVFP4_OK || (st = check_rows(n)) != NVFP4_OK)
+        return st;
+    if (k > kMaxRows) return NVFP4_ERR_RANGE;
+    if (!dA && !dB) return NVFP4_ERR_INVALID_ARG;
+    if (m == 0 || n == 0) return NVFP4_OK;
+    const MatmulGrad g(m, n, k);
+    Memory mem;
+    if ((st = check_operand(fmt, a, m, k, &mem)) != NVFP4_OK || (st = check_operand(fmt, b, n, k, &mem)) != NVFP4_OK ||
+        (st = check_dense(dD, m, n, lddd, 2)) != NVFP4_OK || (dA && (st = check_dense(dA, m, k, ldda, 2)) != NVFP4_OK) ||
+        (dB && (st = check_dense(dB, n, k, lddb, 2)) != NVFP4_OK))
+        return st;
+    if (!workspace || ws_bytes < g.bytes()) return NVFP4_ERR_INVALID_ARG;
+    if (!aligned(workspace, 256) || !aligned(status_dev, 4)) return NVFP4_ERR_ALIGNMENT;
+    mem.read(dD, Memory::span(m, n, lddd, 2));
+    if (dA) mem.write(dA, Memory::span(m, k, ldda, 2));
+    if (dB) mem.write(dB, Memory::span(n, k, lddb, 2));
+    mem.write(workspace, (int64_t)g.bytes());
+    mem.write(status_dev, 4);
+    if ((st = mem.check()) != NVFP4_OK) return st;
+    const int sms = sm_count();
+    if (sms <= 0) return NVFP4_ERR_CUDA;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int mx = fmt == FP4_FMT_MXFP4;
+    Parts ws(workspace);
+    void *bt = ws.take(g.bt), *at = ws.take(g.at), *dt = ws.take(g.dt), *dp = ws.take(g.dp);
+    cudaError_t e = cudaSuccess;
+    if (dA) {
+        const void* q = dD;
+        int64_t ldq = lddd;
+        if (!aligned(dD, 16) || lddd % 8 != 0) {             // rows that TMA cannot read
+            e = launch_repitch_bf16(dD, m, n, lddd, dp, g.ldn, s);
+            q = dp;
+            ldq = g.ldn;
+        }
+        if (e == cudaSuccess) e = launch_expand_t(mx, b->codes, b->sf, n, k, g.ldn, bt, g.ldn, s);
+        if (e == cudaSuccess) e = grad_product(bt, k, g.ldn, q, m, ldq, n, b->S, dA, ldda, status_dev, sms, s);
+    }
+    if (dB && e == cudaSuccess) {
+        e = launch_transpose_bf16(dD, m, n, lddd, dt, g.ldm, s);
+        if (e == cudaSuccess) e = launch_expand_t(mx, a->codes, a->sf, m, k, g.ldm, at, g.ldm, s);
+        if (e == cudaSuccess) e = grad_product(at, k, g.ldm, dt, n, g.ldm, m, a->S, dB, lddb, status_dev, sms, s);
+    }
+    return result(e);
+}
+
+nvfp4_status fp4_gated_ff(fp4_format fmt, fp4_activation act, const fp4_operand* x, const fp4_operand* w_gate,
+                          const fp4_operand* w_up, int64_t t, int64_t f, int64_t d, void* h, int64_t ldh,
+                          uint8_t* h_codes, uint8_t* h_sf, int* status_dev, void* stream) {
+    nvfp4_status st;
+    if (act != FP4_ACT_SILU && act != FP4_ACT_GELU_TANH) return NVFP4_ERR_INVALID_ARG;
+    if ((st = check_format(fmt, d)) != NVFP4_OK || (st = check_rows(t)) != NVFP4_OK || (st = check_rows(f)) != NVFP4_OK)
+        return st;
+    if (!h_codes != !h_sf || (!h && !h_codes)) return NVFP4_ERR_INVALID_ARG;
+    if (h_codes && f % 32 != 0) return NVFP4_ERR_INVALID_ARG;
+    if (t == 0 || f == 0) return NVFP4_OK;
+    Memory mem;
+    if ((st = check_operand(fmt, x, t, d, &mem)) != NVFP4_OK || (st = check_operand(fmt, w_gate, f, d, &mem)) != NVFP4_OK ||
+        (st = check_operand(fmt, w_up, f, d, &mem)) != NVFP4_OK || (h && (st = check_dense(h, t, f, ldh, 2)) != NVFP4_OK))
+        return st;
+    if (!aligned(h_codes, 16) || !aligned(h_sf, 4) || !aligned(status_dev, 4)) return NVFP4_ERR_ALIGNMENT;
+    if (h) mem.write(h, Memory::span(t, f, ldh, 2));
+    mem.write(h_codes, t * (f / 2));
+    if (h_sf) mem.write(h_sf, sf_bytes(FP4_FMT_MXFP4, t, f));
+    mem.write(status_dev, 4);
+    if ((st = mem.check()) != NVFP4_OK) return st;
+    const int sms = sm_count();
+    if (sms <= 0) return NVFP4_ERR_CUDA;
+    Product p = {};
+    p.kind = fmt == FP4_FMT_MXFP4 ? kMxfp4 : kNvfp4;
+    p.mode = kGated;
+    p.act = act;
+    p.p = operand(w_gate, f);
+    p.p2 = operand(w_up, f);
+    p.q = operand(x, t);
+    p.k = d;
+    p.out = h;
+    p.ldo = ldh;
+    p.h_codes = h_codes;
+    p.h_sf = h_sf;
+    p.status = status_dev;
+    return result(launch_product(p, sms, static_cast<cudaStream_t>(stream)));
+}
+
+size_t fp4_gated_ff_backward_workspace(int64_t t, int64_t f, int64_t d) {
+    if (t <= 0 || f <= 0 || d <= 0 || t > kMaxRows || f > kMaxRows || d > kMaxCols) return 0;
+    return GatedGrad(t, f, d).bytes();
+}
+
+nvfp4_status fp4_gated_ff_backward(fp4_format fmt, fp4_activation act, const fp4_operand* x,
+                                   const fp4_operand* w_gate, const fp4_operand* w_up, int64_t t, int64_t f, int64_t d,
+                                   const void* dh, int64_t lddh, void* d_x, int64_t lddx, void* d_gate, void* d_up,
+                                   int64_t lddw, void* h, int64_t ldh, int* status_dev, void* workspace,
+                                   size_t ws_bytes, void* stream) {
+    nvfp4_status st;
+    if (act != FP4_ACT_SILU && act != FP4_ACT_GELU_TANH) return NVFP4_ERR_INVALID_ARG;
+    if ((st = check_format(fmt, d)) != NVFP4_OK || (st = check_rows(t)) != NVFP4_OK || (st = check_rows(f)) != NVFP4_OK)
+        return st;
+    if (d > kMaxRows) return NVFP4_ERR_RANGE;
+    if (!d_gate != !d_up || (!d_x && !d_gate)) return NVFP4_ERR_INVALID_ARG;
+    if (t == 0 || f == 0) return NVFP4_OK;
+    const GatedGrad g(t, f, d);
+    Memory mem;
+    if ((st = check_operand(fmt, x, t, d, &mem)) != NVFP4_OK || (st = check_operand(fmt, w_gate, f, d, &mem)) != NVFP4_OK ||
+        (st = check_operand(fmt, w_up, f, d, &mem)) != NVFP4_OK || (st = check_dense(dh, t, f, lddh, 2)) != NVFP4_OK ||
+        (d_x && (st = check_dense(d_x, t, d, lddx, 2)) != NVFP4_OK) ||
+        (d_gate && (st = check_dense(d_gate, f, d, lddw, 2)) != NVFP4_OK) ||
+        (d_up && (st = check_dense(d_up, f, d, lddw, 2)) != NVFP4_OK) ||
+        (h && (st = check_dense(h, t, f, ldh, 2)) != NVFP4_OK))
+        return st;
+    if (!workspace || ws_bytes < g.bytes()) return NVFP4_ERR_INVALID_ARG;
+    if (!aligned(workspace, 256) || !aligned(status_dev, 4)) return NVFP4_ERR_ALIGNMENT;
+    mem.read(dh, Memory::span(t, f, lddh, 2));
+    if (d_x) mem.write(d_x, Memory::span(t, d, lddx, 2));
+    if (d_gate) mem.write(d_gate, Memory::span(f, d, lddw, 2));
+    if (d_up) mem.write(d_up, Memory::span(f, d, lddw, 2));
+    if (h) mem.write(h, Memory::span(t, f, ldh, 2));
+    mem.write(workspace, (int64_t)g.bytes());
+    mem.write(status_dev, 4);
+    if ((st = mem.check()) != NVFP4_OK) return st;
+    const int sms = sm_count();
+    if (sms <= 0) return NVFP4_ERR_CUDA;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int mx = fmt == FP4_FMT_MXFP4;
+    Parts ws(workspace);
+    uint16_t* wt = static_cast<uint16_t*>(ws.take(g.wt));
+    void* xt = ws.take(g.xt);
+    void* dgu = ws.take(g.dgu);
+    uint16_t* dgut = static_cast<uint16_t*>(ws.take(g.dgut));
+
+    Product p = {};
+    p.kind = mx ? kMxfp4 : kNvfp4;
+    p.mode = kGatedGrad;
+    p.act = act;
+    p.p = operand(w_gate, f);
+    p.p2 = operand(w_up, f);
+    p.q = operand(x, t);
+    p.k = d;
+    p.out = h;
+    p.ldo = ldh;
+    p.dh = dh;
+    p.lddh = lddh;
+    p.dgu = d_x ? dgu : nullptr;
+    p.dgu_t = d_gate ? dgut : nullptr;
+    p.fp = g.fp;
+    p.ldt = g.ldt;
+    p.status = status_dev;
+    cudaError_t e = launch_product(p, sms, s);
+    if (d_x && e == cudaSuccess) {
+        e = launch_expand_t(mx, w_gate->codes, w_gate->sf, f, d, g.fp, wt, 2 * g.fp, s);
+        if (e == cudaSuccess) e = launch_expand_t(mx, w_up->codes, w_up->sf, f, d, g.fp, wt + g.fp, 2 * g.fp, s);
+        if (e == cudaSuccess)
+            e = grad_product(wt, d, 2 * g.fp, dgu, t, 2 * g.fp, 2 * g.fp, nullptr, d_x, lddx, status_dev, sms, s);
+    }
+    if (d_gate && e == cudaSuccess) {
+        e = launch_expand_t(mx, x->codes, x->sf, t, d, g.ldt, xt, g.ldt, s);
+        if (e == cudaSuccess)
+            e = grad_product(xt, d, g.ldt, dgut, f, g.ldt, t, x->S, d_gate, lddw, status_dev, sms, s);
+        if (e == cudaSuccess)
+            e = grad_product(xt, d, g.ldt, dgut + g.fp * g.ldt, f, g.ldt, t, x->S, d_up, lddw, status_dev, sms, s);
+    }
+    return result(e);
+}
+
+}  // extern "C"

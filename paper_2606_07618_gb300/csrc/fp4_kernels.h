@@ -1,0 +1,55 @@
+// Internal interface between the host layer of nvfp4mm.h (fp4_api.cu) and its kernels.
+// Not part of the public ABI.
+#pragma once
+#include <cstdint>
+#include <cuda_runtime.h>
+
+namespace nvfp4 {
+
+// ---- mxfp4.cu
+cudaError_t launch_mxfp4_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, uint8_t* codes,
+                                  uint8_t* sf_linear, uint8_t* sf_swizzled, int* status, int sms, cudaStream_t s);
+cudaError_t launch_mxfp4_dequantize(const uint8_t* codes, const uint8_t* sf, int swizzled, int64_t rows, int64_t cols,
+                                    void* out, int dtype, int sms, cudaStream_t s);
+// out[c][r] = bf16(q * s) of a quantised matrix (without S), exact; rows r in [rows,
+// rows_out) are written as zero.  out row stride ld (a multiple of 8), 16-byte aligned.
+cudaError_t launch_expand_t(int mx, const uint8_t* codes, const uint8_t* sf, int64_t rows, int64_t cols,
+                            int64_t rows_out, void* out, int64_t ld, cudaStream_t s);
+// out[c][r] = in[r][c], bf16; in row stride ldi, out row stride ldo (a multiple of 8).
+cudaError_t launch_transpose_bf16(const void* in, int64_t rows, int64_t cols, int64_t ldi, void* out, int64_t ldo,
+                                  cudaStream_t s);
+// out[r][c] = in[r][c], bf16, for an input that TMA cannot read.
+cudaError_t launch_repitch_bf16(const void* in, int64_t rows, int64_t cols, int64_t ldi, void* out, int64_t ldo,
+                                cudaStream_t s);
+
+// ---- fp4_gemm.cu
+enum { kNvfp4 = 0, kMxfp4 = 1, kBf16 = 2 };                  // operand kinds of a product
+enum { kPlain = 0, kGated = 1, kGatedGrad = 2 };             // what the epilogue makes of the accumulators
+
+// An operand of a product, rows along its K-major storage.
+struct Operand {
+    const void* data;      // packed codes [rows, k/2], or bf16 [rows, ld]
+    const uint8_t* sf;     // 128x4-atom scales; null for bf16
+    const float* S;        // global scale or null
+    int64_t rows, ld;      // ld: row stride in elements (bf16 only)
+};
+
+// One product: out[t][n] over t < q.rows, n < p.rows, from sums over k of q[t][k] p[n][k].
+struct Product {
+    int kind, mode, act;
+    Operand p, p2, q;      // p2: the up projection's weight (gated modes)
+    int64_t k;
+    void* out;             // plain: D; gated modes: h (bf16) or null
+    int out_f32;
+    int64_t ldo;
+    uint8_t *h_codes, *h_sf;   // gated: h in MXFP4, or null
+    const void* dh;        // gated grad: gradient of h, bf16
+    int64_t lddh;
+    void* dgu;             // gated grad: [t][2 fp] bf16: S_gate * dg, S_up * du (columns past f zero)
+    void* dgu_t;           // gated grad: [2 fp][ldt] bf16: dg, du transposed, or null
+    int64_t fp, ldt;
+    int* status;
+};
+cudaError_t launch_product(const Product& p, int sms, cudaStream_t s);
+
+}  // namespace nvfp4

@@ -1,0 +1,152 @@
+// Device parts that the products on quantised operands share: tensor-core
+// instructions past those of tc_gemm.cuh, operand formats, the activation, and what
+// the epilogues write.
+#pragma once
+#include <cuda_bf16.h>
+
+#include "fp4_kernels.h"
+#include "tc_gemm.cuh"
+
+namespace nvfp4 {
+namespace mm {
+
+using namespace tc;
+
+// An operand tile is staged as rows of 128 bytes (one swizzle row) along K: 256 codes or
+// 64 bf16, four MMAs of 32 bytes each.  Scales come as 512-byte atoms of 128 rows by
+// four scale columns, 64 (NVFP4) or 128 (MXFP4) elements of K.
+__host__ __device__ constexpr int stage_k(int kind) { return kind == kBf16 ? 64 : 256; }
+__host__ __device__ constexpr int mma_k(int kind) { return kind == kBf16 ? 16 : 64; }
+__host__ __device__ constexpr int atoms(int kind) { return kind == kNvfp4 ? 4 : kind == kMxfp4 ? 2 : 0; }
+constexpr int kAtom = 512;
+constexpr int kRow = 128;                                    // bytes of an operand row in a stage
+
+// Instruction descriptor.  kind::f16: D fp32 (bits 4-5 = 1), A and B bf16 (7-9, 10-12 =
+// 1), N >> 3 (17-22), M >> 4 (24-28).  kind::mxf4nvf4: A and B E2M1 (7-9, 10-12 = 1), N >> 3
+// (17-22), scales UE4M3 = 0 or UE8M0 = 1 (23), M >> 7 (27-28), which of a cell's scale
+// bytes the MMA takes for B (4-5) and A (29-30).  All operands K-major, K = 32 bytes.
+__host__ __device__ constexpr uint32_t idesc(int kind, int m, int n) {
+    return kind == kBf16 ? (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24)
+                         : (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (kind == kMxfp4 ? 1u << 23 : 0u) |
+                               ((uint32_t)(m >> 7) << 27);
+}
+__host__ __device__ constexpr uint32_t sf_id(uint32_t id) { return id << 4 | id << 29; }
+
+// Descriptor of a 512-byte scale atom for tcgen05.cp: no swizzle, 16-byte rows, 8-row
+// groups 128 bytes apart.
+__device__ __forceinline__ uint64_t atom_desc(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+
+template <int CG>
+__device__ __forceinline__ void cp_atom(uint32_t taddr, uint64_t desc) {
+    if (CG == 1)
+        asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    else
+        asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+#define MM_MMA(CG, KIND)                                                                                            \
+    "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::" CG ".kind::" KIND " [%0], %1, %2, %3, " \
+    "[%5], [%6], p;\n\t}"
+template <int KIND, int CG>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate, uint32_t sfa,
+                                    uint32_t sfb) {
+    if (KIND == kBf16) {
+        if (CG == 1)
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                         ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+        else
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                         ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+    } else if (KIND == kNvfp4) {
+        if (CG == 1)
+            asm volatile(MM_MMA("1", "mxf4nvf4.block_scale.scale_vec::4X")
+                         ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
+        else
+            asm volatile(MM_MMA("2", "mxf4nvf4.block_scale.scale_vec::4X")
+                         ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
+    } else {
+        if (CG == 1)
+            asm volatile(MM_MMA("1", "mxf4nvf4.block_scale.scale_vec::2X")
+                         ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
+        else
+            asm volatile(MM_MMA("2", "mxf4nvf4.block_scale.scale_vec::2X")
+                         ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
+    }
+}
+#undef MM_MMA
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_wait16(float (&a)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(a[0]), "+f"(a[1]), "+f"(a[2]), "+f"(a[3]), "+f"(a[4]), "+f"(a[5]), "+f"(a[6]), "+f"(a[7]),
+                   "+f"(a[8]), "+f"(a[9]), "+f"(a[10]), "+f"(a[11]), "+f"(a[12]), "+f"(a[13]), "+f"(a[14]), "+f"(a[15])
+                 :: "memory");
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// What the accumulators become.
+struct Epilogue {
+    int act;
+    int64_t T, N;                  // rows (tokens) and columns of the result
+    const float *s_p, *s_p2, *s_q; // global scales or null
+    void* out;                     // D, or h (bf16) or null
+    int out_f32;
+    int64_t ldo;
+    uint8_t *h_codes, *h_sf;
+    uint32_t h_kpad4;
+    const uint16_t* dh;
+    int64_t lddh;
+    uint16_t *dgu, *dgu_t;
+    int64_t fp, ldt;
+    int* status;
+};
+
+// act(g) and, where wanted, its derivative.  Both activations are g * p with p a sigmoid
+// (of g, or of 2 z for (1 + tanh z) / 2), which keeps its relative accuracy where p is
+// small.  exp and the quotient by their fast forms: a few ulps, of 2^-23, below a bf16
+// result's 2^-9.
+template <bool GRAD>
+__device__ __forceinline__ float activate(int act, float g, float& da) {
+    float z = g, dz = 1.0f;
+    if (act == 1) {
+        const float g2 = g * g;
+        z = 1.5957691216f * g * fmaf(0.044715f, g2, 1.0f);   // 2 sqrt(2/pi)
+        if (GRAD) dz = 1.5957691216f * fmaf(0.134145f, g2, 1.0f);
+    }
+    const float p = __fdividef(1.0f, 1.0f + __expf(-z));
+    if (GRAD) da = fmaf(g * p * (1.0f - p), dz, p);
+    return g * p;
+}
+
+__device__ __forceinline__ uint16_t bf16_bits(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
+__device__ __forceinline__ float bf16_value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+__device__ __forceinline__ float scale_or_1(const float* s) { return s ? ld_f32(s) : 1.0f; }
+
+}  // namespace mm
+}  // namespace nvfp4

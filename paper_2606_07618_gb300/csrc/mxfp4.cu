@@ -1,0 +1,359 @@
+// MXFP4 (E2M1 elements, one power-of-two E8M0 scale for each block of 32): quantisation
+// and dequantisation, and the layout kernels of the gradients, which multiply bf16 by
+// the values of a quantised matrix along its rows.
+//
+// All of them are bound by memory: a few instructions per element, each byte once.
+#include <cuda_bf16.h>
+
+#include "fp4_kernels.h"
+#include "nvfp4_device.cuh"
+#include "nvfp4_kernels.h"
+
+namespace nvfp4 {
+namespace {
+
+__device__ __forceinline__ uint32_t div_by(uint32_t n, const FastDiv& d) {
+    const uint32_t t = __umulhi(n, d.mul);
+    return (t + ((n - t) >> d.s1)) >> d.s2;
+}
+
+// value of an E8M0 code (0: 2^-127, a subnormal; 255: NaN)
+__device__ __forceinline__ float e8m0_value(uint32_t c) {
+    return c == 0 ? __uint_as_float(0x00400000u) : c == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(c << 23);
+}
+// two E2M1 codes of a byte as fp32
+__device__ __forceinline__ void e2m1_pair(uint32_t byte, float& lo, float& hi) {
+    uint32_t h2;
+    asm("{\n\t.reg .b8 b;\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tcvt.u8.u16 b, t;\n\tcvt.rn.f16x2.e2m1x2 %0, b;\n\t}"
+        : "=r"(h2) : "r"(byte & 0xFFu));
+    lo = f16bits_to_f32((uint16_t)(h2 & 0xFFFFu));
+    hi = f16bits_to_f32((uint16_t)(h2 >> 16));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// ---------------------------------------------------------------------------
+// Quantisation.  A lane holds 16 elements, two neighbours a block; the block's maximum is
+// the larger of two lanes' integer maxima of |x| as bits, its exponent field gives X,
+// and x / X is a multiplication by a power of two, so nothing rounds before the convert.
+// A lane's loads are one or two 32-byte sectors; its codes are 8 bytes, a warp's 256.
+struct MxParams {
+    const void* x;
+    int64_t rows, cols, ldx;
+    uint8_t *codes, *sf_linear, *sf_swizzled;
+    int* status;
+    uint32_t segs, row_segs;     // of 16 elements
+    uint32_t kb, kpad4;
+    FastDiv div;                 // by row_segs
+};
+
+enum { kWide = 0, kHalf = 1, kElement = 2 };   // loads of 32 bytes, 16 bytes, single elements
+
+template <int BF16, int LOAD>
+__device__ __forceinline__ void load_seg(const void* base, int64_t off, float (&y)[16]) {
+    if (LOAD == kElement) {
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+            y[i] = BF16 ? __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(base)[off + i] << 16)
+                        : reinterpret_cast<const float*>(base)[off + i];
+        return;
+    }
+    constexpr int kVec = BF16 ? 2 : 4;                       // 16-byte words
+    uint4 v[kVec];
+    const char* p = static_cast<const char*>(base) + off * (BF16 ? 2 : 4);
+#pragma unroll
+    for (int i = 0; i < kVec; i += 2) {
+        if (LOAD == kWide) {
+            ld_stream32<false>(p + 16 * i, v[i], v[i + 1]);
+        } else {
+            v[i] = ld_stream16<false>(p + 16 * i);
+            v[i + 1] = ld_stream16<false>(p + 16 * i + 16);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kVec; i++) {
+        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            if (BF16) {
+                y[8 * i + 2 * j] = bf16lo(w[j]);
+                y[8 * i + 2 * j + 1] = bf16hi(w[j]);
+            } else {
+                y[4 * i + j] = __uint_as_float(w[j]);
+            }
+        }
+    }
+}
+
+template <int BF16, int LOAD>
+__global__ void __launch_bounds__(256) mxfp4_quantize_kernel(MxParams p) {
+    grid_dependency_wait();
+    const uint32_t stride = gridDim.x * blockDim.x;
+    const uint32_t padded = (p.segs + 31) & ~31u;            // whole warps: the shuffles name all lanes
+    bool bad = false;
+    for (uint32_t seg = blockIdx.x * blockDim.x + threadIdx.x; seg < padded; seg += stride) {
+        const bool live = seg < p.segs;
+        const uint32_t row = div_by(live ? seg : 0, p.div), c16 = (live ? seg : 0) - row * p.row_segs;
+        float y[16];
+        if (live) {
+            load_seg<BF16, LOAD>(p.x, (int64_t)row * p.ldx + 16 * (int64_t)c16, y);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; i++) y[i] = 0.0f;
+        }
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 16; i++) m = max(m, __float_as_uint(y[i]) & 0x7FFFFFFFu);
+        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+        const uint32_t e = m >> 23;
+        const bool finite = e != 255;
+        bad |= !finite;
+        const uint32_t code = finite && e > 2 ? e - 2 : 0;
+        const float inv = __uint_as_float((254u - code) << 23);  // 2^(127 - code)
+        u64 t[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float a = finite ? __fmul_rn(y[2 * i], inv) : copysignf(0.0f, y[2 * i]);
+            const float b = finite ? __fmul_rn(y[2 * i + 1], inv) : copysignf(0.0f, y[2 * i + 1]);
+            t[i] = pack2(a, b);
+        }
+        if (!live) continue;
+        reinterpret_cast<uint2*>(p.codes)[seg] = make_uint2(e2m1x8(t[0], t[1], t[2], t[3]), e2m1x8(t[4], t[5], t[6], t[7]));
+        if ((seg & 1) == 0) {
+            const uint32_t k = c16 >> 1;
+            if (p.sf_linear) p.sf_linear[(int64_t)row * p.kb + k] = (uint8_t)code;
+            if (p.sf_swizzled) {
+                uint8_t* at = p.sf_swizzled + swizzle_offset(row, k, p.kpad4);
+                *at = (uint8_t)code;
+                if (k == p.kb - 1)                           // the row's last word: its padding
+                    for (uint32_t j = 1; j < 4 - (k & 3); j++) at[j] = 0;
+            }
+        }
+    }
+    if (p.sf_swizzled) {                                     // rows up to a multiple of 128
+        const uint32_t pad_rows = (uint32_t)(-p.rows & 127);
+        for (uint32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < pad_rows * p.kpad4; i += stride) {
+            const int64_t r = p.rows + i / p.kpad4;
+            *reinterpret_cast<uint32_t*>(p.sf_swizzled + swizzle_offset(r, 4 * (int64_t)(i % p.kpad4), p.kpad4)) = 0;
+        }
+    }
+    if (bad && p.status) atomicOr(p.status, 1);
+}
+
+// ---------------------------------------------------------------------------
+// Dequantisation: 8 codes (a word) to a lane, four words in flight.
+template <int OUT_BF16, int SWIZZLED>
+__global__ void __launch_bounds__(256)
+    mxfp4_dequantize_kernel(const uint8_t* codes, const uint8_t* sf, uint32_t words, uint32_t kb, uint32_t kpad4,
+                            FastDiv div, void* out) {
+    constexpr int kUnroll = 4;
+    grid_dependency_wait();
+    const uint32_t stride = gridDim.x * blockDim.x * kUnroll;
+    for (uint32_t w0 = (blockIdx.x * blockDim.x + (threadIdx.x & ~31u)) * kUnroll + (threadIdx.x & 31); w0 < words;
+         w0 += stride) {
+        uint32_t c[kUnroll], s[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; u++) {
+            const uint32_t w = w0 + 32 * u;
+            if (w < words) {
+                const uint32_t blk = w >> 2;
+                c[u] = ld_u32(reinterpret_cast<const uint32_t*>(codes) + w);
+                if (SWIZZLED) {
+                    const uint32_t row = div_by(blk, div);
+                    s[u] = sf[swizzle_offset32(row, blk - row * kb, kpad4)];
+                } else {
+                    s[u] = sf[blk];
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; u++) {
+            const uint32_t w = w0 + 32 * u;
+            if (w >= words) break;
+            const float v = e8m0_value(s[u]);
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                e2m1_pair(c[u] >> (8 * j), f[2 * j], f[2 * j + 1]);
+                f[2 * j] = __fmul_rn(f[2 * j], v);
+                f[2 * j + 1] = __fmul_rn(f[2 * j + 1], v);
+            }
+            if (OUT_BF16) {
+                reinterpret_cast<uint4*>(out)[w] = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]),
+                                                              pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+            } else {
+                reinterpret_cast<float4*>(out)[2 * (int64_t)w] = make_float4(f[0], f[1], f[2], f[3]);
+                reinterpret_cast<float4*>(out)[2 * (int64_t)w + 1] = make_float4(f[4], f[5], f[6], f[7]);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The values of a quantised matrix without S, transposed, in bf16: exact, as q has two
+// significant bits and an E4M3 scale four.  A tile of 64 rows by 128 columns goes
+// through shared memory; reads are 64 bytes a row, writes 128 bytes a column.
+template <int MX>
+__global__ void __launch_bounds__(256)
+    expand_t_kernel(const uint8_t* codes, const uint8_t* sf, int64_t rows, int64_t cols, int64_t rows_out, uint32_t kpad4,
+                    uint16_t* out, int64_t ld) {
+    __shared__ uint16_t tile[128][66];                       // [column][row]; 33 words to a column
+    grid_dependency_wait();
+    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 128;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int w = i * 256 + threadIdx.x, r = w >> 4, cw = w & 15;   // 16 words of 8 codes to a row
+        const int64_t row = r0 + r, col = c0 + 8 * cw;
+        uint32_t c = 0;
+        float v = 0.0f;
+        if (row < rows && col < cols) {
+            c = ld_u32(codes + row * (cols / 2) + col / 2);
+            const uint32_t s = sf[swizzle_offset(row, col / (MX ? 32 : 16), kpad4)];
+            v = MX ? e8m0_value(s) : f16bits_to_f32(e4m3_to_f16bits(s));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            float a, b;
+            e2m1_pair(c >> (8 * j), a, b);
+            const uint32_t two = pack_bf16(__fmul_rn(a, v), __fmul_rn(b, v));
+            tile[8 * cw + 2 * j][r] = (uint16_t)two;
+            tile[8 * cw + 2 * j + 1][r] = (uint16_t)(two >> 16);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int w = i * 256 + threadIdx.x, c = w >> 3, g = w & 7;     // 8 rows (16 bytes) of a column
+        const int64_t col = c0 + c, row = r0 + 8 * g;
+        if (col >= cols || row >= rows_out) continue;
+        const uint32_t* t = reinterpret_cast<const uint32_t*>(&tile[c][8 * g]);
+        // ld is a multiple of 8 and at least rows_out: the whole 16 bytes lie in the row
+        *reinterpret_cast<uint4*>(out + col * ld + row) = make_uint4(t[0], t[1], t[2], t[3]);
+    }
+}
+
+__global__ void __launch_bounds__(256)
+    transpose_bf16_kernel(const uint16_t* in, int64_t rows, int64_t cols, int64_t ldi, uint16_t* out, int64_t ldo) {
+    __shared__ uint16_t tile[64][66];                        // [column][row]
+    grid_dependency_wait();
+    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        const int w = i * 256 + threadIdx.x, r = w >> 6, c = w & 63;
+        tile[c][r] = r0 + r < rows && c0 + c < cols ? in[(r0 + r) * ldi + c0 + c] : (uint16_t)0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const int w = i * 256 + threadIdx.x, c = w >> 3, g = w & 7;
+        const int64_t col = c0 + c, row = r0 + 8 * g;
+        if (col >= cols || row >= ldo) continue;
+        const uint32_t* t = reinterpret_cast<const uint32_t*>(&tile[c][8 * g]);
+        *reinterpret_cast<uint4*>(out + col * ldo + row) = make_uint4(t[0], t[1], t[2], t[3]);
+    }
+}
+
+__global__ void __launch_bounds__(256)
+    repitch_bf16_kernel(const uint16_t* in, int64_t rows, int64_t cols, int64_t ldi, uint16_t* out, int64_t ldo) {
+    grid_dependency_wait();
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int64_t c = threadIdx.x; c < cols; c += blockDim.x) out[r * ldo + c] = in[r * ldi + c];
+}
+
+template <typename... P, typename... Args>
+cudaError_t launch_grid(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t s, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
+template <int BF16>
+cudaError_t launch_quantize_as(const MxParams& p, int load, int64_t grid, cudaStream_t s) {
+    return launch_dependent(load == kWide   ? mxfp4_quantize_kernel<BF16, kWide>
+                            : load == kHalf ? mxfp4_quantize_kernel<BF16, kHalf>
+                                            : mxfp4_quantize_kernel<BF16, kElement>,
+                            grid, 256, s, p);
+}
+
+}  // namespace
+
+cudaError_t launch_mxfp4_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, uint8_t* codes,
+                                  uint8_t* sf_linear, uint8_t* sf_swizzled, int* status, int sms, cudaStream_t s) {
+    const int64_t esize = dtype == 0 ? 2 : 4, kb = cols / 32, kpad4 = (kb + 3) / 4;
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(x) | (uintptr_t)(rows > 1 ? ldx * esize : 0);
+    const int load = (bits & 31) == 0 ? kWide : (bits & 15) == 0 ? kHalf : kElement;
+    // segments are counted in 32 bits: rows in groups of whole 128 (one group below 2^30 segments)
+    const int64_t most = ((int64_t)1 << 30) / (cols / 16) / 128 * 128, group = most > 0 ? most : 128;
+    for (int64_t r = 0; r < rows; r += group) {
+        MxParams p;
+        p.rows = rows - r < group ? rows - r : group;
+        p.cols = cols;
+        p.ldx = ldx;
+        p.x = static_cast<const char*>(x) + r * ldx * esize;
+        p.codes = codes + r * (cols / 2);
+        p.sf_linear = sf_linear ? sf_linear + r * kb : nullptr;
+        p.sf_swizzled = sf_swizzled ? sf_swizzled + r * kpad4 * 4 : nullptr;
+        p.status = status;
+        p.row_segs = (uint32_t)(cols / 16);
+        p.segs = (uint32_t)(p.rows * p.row_segs);
+        p.kb = (uint32_t)kb;
+        p.kpad4 = (uint32_t)kpad4;
+        p.div = make_fast_div(p.row_segs);
+        int64_t grid = ((int64_t)p.segs + 255) / 256;
+        if (grid > (int64_t)sms * 8) grid = (int64_t)sms * 8;
+        const cudaError_t e = dtype == 0 ? launch_quantize_as<1>(p, load, grid, s) : launch_quantize_as<0>(p, load, grid, s);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+cudaError_t launch_mxfp4_dequantize(const uint8_t* codes, const uint8_t* sf, int swizzled, int64_t rows, int64_t cols,
+                                    void* out, int dtype, int sms, cudaStream_t s) {
+    const int64_t kb = cols / 32, kpad4 = (kb + 3) / 4, esize = dtype == 0 ? 2 : 4;
+    const int64_t most = ((int64_t)1 << 30) / (cols / 8) / 128 * 128, group = most > 0 ? most : 128;
+    const FastDiv div = make_fast_div((uint32_t)kb);
+    for (int64_t r = 0; r < rows; r += group) {
+        const int64_t n = rows - r < group ? rows - r : group, words = n * (cols / 8);
+        int64_t grid = (words + 1023) / 1024;
+        if (grid > (int64_t)sms * 8) grid = (int64_t)sms * 8;
+        const auto k = dtype == 0 ? (swizzled ? mxfp4_dequantize_kernel<1, 1> : mxfp4_dequantize_kernel<1, 0>)
+                                  : (swizzled ? mxfp4_dequantize_kernel<0, 1> : mxfp4_dequantize_kernel<0, 0>);
+        const cudaError_t e = launch_dependent(k, grid, 256, s, codes + r * (cols / 2), sf + r * (swizzled ? kpad4 * 4 : kb),
+                                               (uint32_t)words, (uint32_t)kb, (uint32_t)kpad4, div,
+                                               static_cast<void*>(static_cast<char*>(out) + r * cols * esize));
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+cudaError_t launch_expand_t(int mx, const uint8_t* codes, const uint8_t* sf, int64_t rows, int64_t cols,
+                            int64_t rows_out, void* out, int64_t ld, cudaStream_t s) {
+    const dim3 grid((unsigned)((cols + 127) / 128), (unsigned)((rows_out + 63) / 64));
+    const uint32_t kpad4 = (uint32_t)((cols / (mx ? 32 : 16) + 3) / 4);
+    return launch_grid(mx ? expand_t_kernel<1> : expand_t_kernel<0>, grid, 256, s, codes, sf, rows, cols, rows_out, kpad4,
+                       static_cast<uint16_t*>(out), ld);
+}
+
+cudaError_t launch_transpose_bf16(const void* in, int64_t rows, int64_t cols, int64_t ldi, void* out, int64_t ldo,
+                                  cudaStream_t s) {
+    const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)((rows + 63) / 64));
+    return launch_grid(transpose_bf16_kernel, grid, 256, s, static_cast<const uint16_t*>(in), rows, cols, ldi,
+                       static_cast<uint16_t*>(out), ldo);
+}
+
+cudaError_t launch_repitch_bf16(const void* in, int64_t rows, int64_t cols, int64_t ldi, void* out, int64_t ldo,
+                                cudaStream_t s) {
+    return launch_grid(repitch_bf16_kernel, dim3((unsigned)(rows < 65535 ? rows : 65535)), 256, s,
+                       static_cast<const uint16_t*>(in), rows, cols, ldi, static_cast<uint16_t*>(out), ldo);
+}
+
+}  // namespace nvfp4
