@@ -17,8 +17,6 @@
 //
 // Every mbarrier wait is bounded (1 s); on a timeout the CTA sets bit 16 of the status
 // word, drains its copies, frees its tensor memory and returns without writing.
-#include <cstdio>
-
 #include "fp4_tile.cuh"
 
 namespace nvfp4 {
@@ -272,57 +270,6 @@ __global__ void __launch_bounds__(kThreadsTile, 1) tile_kernel(const __grid_cons
 }
 
 // ---------------------------------------------------------------------------
-bool make_operand_map(CUtensorMap* m, const Operand& o, int kind, int64_t k, uint32_t box_rows) {
-    const EncodeTiledFn enc = encode_fn();
-    if (!enc) return false;
-    const bool bf = kind == kBf16;
-    const cuuint64_t dims[2] = {(cuuint64_t)(bf ? k : k / 2), (cuuint64_t)o.rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)(bf ? 2 * o.ld : k / 2)};
-    const cuuint32_t box[2] = {bf ? 64u : 128u, box_rows};
-    const cuuint32_t es[2] = {1, 1};
-    return enc(m, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(o.data), dims,
-               strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// The scale atoms as [row block][atom along K][128 words].
-bool make_scale_map(CUtensorMap* m, const Operand& o, int kind, int64_t k) {
-    const EncodeTiledFn enc = encode_fn();
-    if (!enc) return false;
-    const int64_t kb = k / (kind == kMxfp4 ? 32 : 16), k4 = (kb + 3) / 4;
-    const cuuint64_t dims[3] = {128, (cuuint64_t)k4, (cuuint64_t)((o.rows + 127) / 128)};
-    const cuuint64_t strides[2] = {(cuuint64_t)kAtom, (cuuint64_t)(k4 * kAtom)};
-    const cuuint32_t box[3] = {128, (cuuint32_t)atoms(kind), 1};
-    const cuuint32_t es[3] = {1, 1, 1};
-    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<uint8_t*>(o.sf), dims, strides, box, es,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-Epilogue make_epilogue(const Product& p) {
-    Epilogue e = {};
-    e.act = p.act;
-    e.T = p.q.rows;
-    e.N = p.p.rows;
-    e.s_p = p.p.S;
-    e.s_p2 = p.p2.S;
-    e.s_q = p.q.S;
-    e.out = p.out;
-    e.out_f32 = p.out_f32;
-    e.ldo = p.ldo;
-    e.h_codes = p.h_codes;
-    e.h_sf = p.h_sf;
-    e.h_kpad4 = (uint32_t)((p.p.rows / 32 + 3) / 4);
-    e.dh = static_cast<const uint16_t*>(p.dh);
-    e.lddh = p.lddh;
-    e.dgu = static_cast<uint16_t*>(p.dgu);
-    e.dgu_t = static_cast<uint16_t*>(p.dgu_t);
-    e.fp = p.fp;
-    e.ldt = p.ldt;
-    e.status = p.status;
-    return e;
-}
-
 template <int KIND, int MODE, int TN>
 cudaError_t launch_tile(const Product& p, int sms, cudaStream_t s) {
     using C = Tile<KIND, MODE, TN>;
@@ -390,6 +337,7 @@ cudaError_t launch_by_mode(const Product& p, int sms, cudaStream_t s) {
 }  // namespace mm
 
 cudaError_t launch_product(const Product& p, int sms, cudaStream_t s) {
+    if (p.q.rows > 128) return launch_pair(p, sms, s);
     switch (p.kind) {
         case kNvfp4: return mm::launch_by_mode<kNvfp4>(p, sms, s);
         case kMxfp4: return mm::launch_by_mode<kMxfp4>(p, sms, s);

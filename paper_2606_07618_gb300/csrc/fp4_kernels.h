@@ -51,5 +51,7 @@ struct Product {
     int* status;
 };
 cudaError_t launch_product(const Product& p, int sms, cudaStream_t s);
+// ---- fp4_pair.cu: the same for many tokens
+cudaError_t launch_pair(const Product& p, int sms, cudaStream_t s);
 
 }  // namespace nvfp4

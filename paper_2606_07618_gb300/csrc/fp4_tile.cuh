@@ -91,6 +91,28 @@ __device__ __forceinline__ void tmem_wait16(float (&a)[16]) {
                  :: "memory");
 }
 
+// 32 consecutive accumulator columns; there after tmem_wait32, which names them.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+          "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+          "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+          "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait32(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+          "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+          "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+          "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+        :: "memory");
+}
+
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -147,6 +169,58 @@ __device__ __forceinline__ float activate(int act, float g, float& da) {
 __device__ __forceinline__ uint16_t bf16_bits(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
 __device__ __forceinline__ float bf16_value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
 __device__ __forceinline__ float scale_or_1(const float* s) { return s ? ld_f32(s) : 1.0f; }
+
+// ---- host side
+inline bool make_operand_map(CUtensorMap* m, const Operand& o, int kind, int64_t k, uint32_t box_rows) {
+    const EncodeTiledFn enc = encode_fn();
+    if (!enc) return false;
+    const bool bf = kind == kBf16;
+    const cuuint64_t dims[2] = {(cuuint64_t)(bf ? k : k / 2), (cuuint64_t)o.rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)(bf ? 2 * o.ld : k / 2)};
+    const cuuint32_t box[2] = {bf ? 64u : 128u, box_rows};
+    const cuuint32_t es[2] = {1, 1};
+    return enc(m, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(o.data), dims,
+               strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The scale atoms as [row block][atom along K][128 words].
+inline bool make_scale_map(CUtensorMap* m, const Operand& o, int kind, int64_t k) {
+    const EncodeTiledFn enc = encode_fn();
+    if (!enc) return false;
+    const int64_t kb = k / (kind == kMxfp4 ? 32 : 16), k4 = (kb + 3) / 4;
+    const cuuint64_t dims[3] = {128, (cuuint64_t)k4, (cuuint64_t)((o.rows + 127) / 128)};
+    const cuuint64_t strides[2] = {(cuuint64_t)kAtom, (cuuint64_t)(k4 * kAtom)};
+    const cuuint32_t box[3] = {128, (cuuint32_t)atoms(kind), 1};
+    const cuuint32_t es[3] = {1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<uint8_t*>(o.sf), dims, strides, box, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+inline Epilogue make_epilogue(const Product& p) {
+    Epilogue e = {};
+    e.act = p.act;
+    e.T = p.q.rows;
+    e.N = p.p.rows;
+    e.s_p = p.p.S;
+    e.s_p2 = p.p2.S;
+    e.s_q = p.q.S;
+    e.out = p.out;
+    e.out_f32 = p.out_f32;
+    e.ldo = p.ldo;
+    e.h_codes = p.h_codes;
+    e.h_sf = p.h_sf;
+    e.h_kpad4 = (uint32_t)((p.p.rows / 32 + 3) / 4);
+    e.dh = static_cast<const uint16_t*>(p.dh);
+    e.lddh = p.lddh;
+    e.dgu = static_cast<uint16_t*>(p.dgu);
+    e.dgu_t = static_cast<uint16_t*>(p.dgu_t);
+    e.fp = p.fp;
+    e.ldt = p.ldt;
+    e.status = p.status;
+    return e;
+}
 
 }  // namespace mm
 }  // namespace nvfp4
