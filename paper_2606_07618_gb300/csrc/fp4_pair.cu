@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
     __shared__ int s_abort;
     __shared__ uint32_t s_tmem;
     uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
     const uint32_t rank = cluster_rank();
     const int nst = (int)((P.k + stage_k(KIND) - 1) / stage_k(KIND));
     const int ntiles = P.tiles_t * P.tiles_n, step = (int)gridDim.x / 2, first = (int)blockIdx.x / 2;
@@ -181,81 +181,91 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
     grid_dependency_wait();
     const uint32_t tmem = s_tmem;
 
-    if (tid == kEpiWarps * 32) {
-        int s = 0;
+    if (warp == kEpiWarps) {
+        Ring ring;
+        const uint32_t leader_full = at_rank(full0, 0);
         bool ok = true;
+        int issued = 0;
         for (int i = first; ok && i < ntiles; i += step) {
             int tt, tn;
             tile_at(i, P.tiles_t, P.tiles_n, tt, tn);
             const int t0 = tt * 256 + (int)rank * 128;
-            for (int kc = 0; kc < nst; kc++, s++) {
-                const int r = s % C::kStages;
-                if (s >= C::kStages && !mbar_wait(empty0 + 8 * r, (s / C::kStages - 1) & 1)) {
-                    atomicOr(&s_abort, 1);
+            for (int kc = 0; kc < nst; kc++) {
+                const int r = ring.slot;
+                if (issued >= C::kStages && !mbar_wait_warp(empty0 + 8 * r, ring.parity ^ 1)) {
                     ok = false;
                     break;
                 }
-                const uint32_t st = smem_u32(base) + r * C::kStage, bar = at_rank(full0 + 8 * r, 0);
-                if (rank == 0) mbar_expect_tx(full0 + 8 * r, 2 * C::kStage);
-                const int x = kc * (KIND == kBf16 ? 64 : 128);
-                tma_load_2d_pair(st, &P.q, x, t0, bar);
-                if (MODE == kPlain)
-                    tma_load_2d_pair(st + C::kOp, &P.p, x, tn * 256 + (int)rank * 128, bar);
-                else
-                    tma_load_2d_pair(st + C::kOp, rank == 0 ? &P.p : &P.p2, x, tn * 128, bar);
-                if (KIND != kBf16) {
-                    const uint32_t sf = st + 2 * C::kOp;
-                    const int a = kc * atoms(KIND);
-                    tma_load_3d_pair(sf, &P.sq, 0, a, t0 >> 7, bar);
-                    tma_load_3d_pair(sf + C::kS, &P.sp, 0, a, MODE == kPlain ? 2 * tn : tn, bar);
+                if (elect_one()) {
+                    const uint32_t st = smem_u32(base) + r * C::kStage, bar = leader_full + 8 * r;
+                    if (rank == 0) mbar_expect_tx(full0 + 8 * r, 2 * C::kStage);
+                    const int x = kc * (KIND == kBf16 ? 64 : 128);
+                    tma_load_2d_pair(st, &P.q, x, t0, bar);
                     if (MODE == kPlain)
-                        tma_load_3d_pair(sf + 2 * C::kS, &P.sp, 0, a, 2 * tn + 1, bar);
+                        tma_load_2d_pair(st + C::kOp, &P.p, x, tn * 256 + (int)rank * 128, bar);
                     else
-                        tma_load_3d_pair(sf + 2 * C::kS, &P.sp2, 0, a, tn, bar);
+                        tma_load_2d_pair(st + C::kOp, rank == 0 ? &P.p : &P.p2, x, tn * 128, bar);
+                    if (KIND != kBf16) {
+                        const uint32_t sf = st + 2 * C::kOp;
+                        const int a = kc * atoms(KIND);
+                        tma_load_3d_pair(sf, &P.sq, 0, a, t0 >> 7, bar);
+                        tma_load_3d_pair(sf + C::kS, &P.sp, 0, a, MODE == kPlain ? 2 * tn : tn, bar);
+                        if (MODE == kPlain)
+                            tma_load_3d_pair(sf + 2 * C::kS, &P.sp, 0, a, 2 * tn + 1, bar);
+                        else
+                            tma_load_3d_pair(sf + 2 * C::kS, &P.sp2, 0, a, tn, bar);
+                    }
                 }
+                __syncwarp();
+                if (issued < C::kStages) issued++;
+                ring.next(C::kStages);
             }
         }
-        for (int j = s < C::kStages ? 0 : s - C::kStages; j < s; j++)      // read, hence landed (bounded)
-            if (!mbar_wait(empty0 + 8 * (j % C::kStages), (j / C::kStages) & 1)) {
-                atomicOr(&s_abort, 1);
-                break;
-            }
-    } else if (tid == (kEpiWarps + 1) * 32 && rank == 0) {
+        // every slot in use read, hence landed
+        if (issued < C::kStages) ring = Ring{0, 1};          // each used once
+        for (int j = 0; ok && j < issued; j++, ring.next(C::kStages)) ok = mbar_wait_warp(empty0 + 8 * ring.slot, ring.parity ^ 1);
+        if (!ok && lane == 0) atomicOr(&s_abort, 1);
+    } else if (warp == kEpiWarps + 1 && rank == 0) {
         constexpr uint32_t id = idesc(KIND, 256, 256);
-        int s = 0, it = 0;
+        Ring ring;
+        int it = 0;
         bool ok = true;
         for (int i = first; ok && i < ntiles; i += step, it++) {
-            if (it > 0 && !mbar_wait(drained0 + 8 * ((it - 1) & 1), ((it - 1) >> 1) & 1)) ok = false;
+            if (it > 0 && !mbar_wait_warp(drained0 + 8 * ((it - 1) & 1), ((it - 1) >> 1) & 1)) ok = false;
             tc_fence_after();
             const uint32_t acc = tmem + (it & 1) * C::kAcc1;
-            for (int kc = 0; ok && kc < nst; kc++, s++) {
-                const int r = s % C::kStages;
-                if (!mbar_wait(full0 + 8 * r, (s / C::kStages) & 1)) {
+            for (int kc = 0; ok && kc < nst; kc++) {
+                const int r = ring.slot;
+                if (!mbar_wait_warp(full0 + 8 * r, ring.parity)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                const uint32_t st = smem_u32(base) + r * C::kStage, sf = st + 2 * C::kOp;
+                if (elect_one()) {
+                    const uint32_t st = smem_u32(base) + r * C::kStage, sf = st + 2 * C::kOp;
 #pragma unroll
-                for (int a = 0; a < atoms(KIND); a++) {
-                    cp_atom<2>(tmem + C::kSf + 4 * a, atom_desc(sf + a * kAtom));
-                    cp_atom<2>(tmem + C::kSf + 16 + 8 * a, atom_desc(sf + C::kS + a * kAtom));
-                    cp_atom<2>(tmem + C::kSf + 16 + 8 * a + 4, atom_desc(sf + 2 * C::kS + a * kAtom));
-                }
-                const int left = (int)((P.k - (int64_t)kc * stage_k(KIND) + mma_k(KIND) - 1) / mma_k(KIND));
+                    for (int a = 0; a < atoms(KIND); a++) {
+                        cp_atom<2>(tmem + C::kSf + 4 * a, atom_desc(sf + a * kAtom));
+                        cp_atom<2>(tmem + C::kSf + 16 + 8 * a, atom_desc(sf + C::kS + a * kAtom));
+                        cp_atom<2>(tmem + C::kSf + 16 + 8 * a + 4, atom_desc(sf + 2 * C::kS + a * kAtom));
+                    }
+                    const int left = (int)((P.k - (int64_t)kc * stage_k(KIND) + mma_k(KIND) - 1) / mma_k(KIND));
 #pragma unroll
-                for (int kk = 0; kk < 4; kk++) {
-                    if (kk >= left) break;
-                    const int a = KIND == kNvfp4 ? kk : kk >> 1;
-                    mma<KIND, 2>(acc, smem_desc(st + kk * 32, 16, 1024), smem_desc(st + C::kOp + kk * 32, 16, 1024),
-                                 KIND == kMxfp4 ? id | sf_id(2 * (kk & 1)) : id, (uint32_t)(kc | kk), tmem + C::kSf + 4 * a,
-                                 tmem + C::kSf + 16 + 8 * a);
+                    for (int kk = 0; kk < 4; kk++) {
+                        if (kk >= left) break;
+                        const int a = KIND == kNvfp4 ? kk : kk >> 1;
+                        mma<KIND, 2>(acc, smem_desc(st + kk * 32, 16, 1024), smem_desc(st + C::kOp + kk * 32, 16, 1024),
+                                     KIND == kMxfp4 ? id | sf_id(2 * (kk & 1)) : id, (uint32_t)(kc | kk), tmem + C::kSf + 4 * a,
+                                     tmem + C::kSf + 16 + 8 * a);
+                    }
+                    commit_pair(empty0 + 8 * r);
+                    if (kc == nst - 1) commit_pair(accf0 + 8 * (it & 1));
                 }
-                commit_pair(empty0 + 8 * r);
+                __syncwarp();
+                ring.next(C::kStages);
             }
-            if (ok) commit_pair(accf0 + 8 * (it & 1));
         }
-        if (!ok) atomicOr(&s_abort, 1);
+        if (!ok && lane == 0) atomicOr(&s_abort, 1);
     } else if (warp < kEpiWarps) {
         const Epilogue& e = P.e;
         const float sp = scale_or_1(e.s_p), sp2 = MODE != kPlain ? scale_or_1(e.s_p2) : 1.0f, sq = scale_or_1(e.s_q);

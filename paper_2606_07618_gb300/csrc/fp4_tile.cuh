@@ -113,6 +113,35 @@ __device__ __forceinline__ void tmem_wait32(float (&v)[32]) {
         :: "memory");
 }
 
+// One thread of a converged warp.  A role's warp runs its loop with all lanes and elects
+// one to issue: the operands of TMA and tensor-core instructions then stay in uniform registers,
+// where a branch on the thread's number cost ~50 cycles an instruction to move them there
+// (a stage of 12 scale copies and 4 MMAs: 1500 cycles for 512 of MMA).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ int warp_index() { return __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0); }
+
+// mbar_wait by all lanes of a warp, with one answer for all of them.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
+    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
+    const unsigned long long t0 = now_ns();
+    while (!__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity)))
+        if (__any_sync(0xFFFFFFFFu, now_ns() - t0 > kWaitNs)) return false;
+    return true;
+}
+
+// A ring of K-stages: slot and the parity of its current use.
+struct Ring {
+    int slot = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void next(int stages) {
+        if (++slot == stages) slot = 0, parity ^= 1;
+    }
+};
+
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
