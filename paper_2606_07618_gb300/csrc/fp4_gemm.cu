@@ -7,9 +7,9 @@
 // side whatever the number of tokens, so that one token costs an MMA of N = 16 and the
 // weight is read once.  Lane i of tensor memory is then column n0 + i of the result and a
 // warp's stores are consecutive.  The gated forms keep two accumulators, gate and up.
-//   * one thread loads stages (128 bytes of each operand's rows along K, and their scale
+//   * one warp loads stages (128 bytes of each operand's rows along K, and their scale
 //     atoms) by TMA into a ring; out-of-range rows, columns and atoms arrive as zeros;
-//   * one thread copies each stage's scale atoms to tensor memory (tcgen05.cp) and issues its
+//   * one warp copies each stage's scale atoms to tensor memory (tcgen05.cp) and issues its
 //     MMAs; copies and MMAs run in the order they are issued;
 //   * four warps read the accumulators and write the result.
 // Where there are fewer tiles than SMs, a cluster of CTAs splits K; each leaves its sums in
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kThreadsTile, 1) tile_kernel(const __grid_cons
     __shared__ int s_abort;
     __shared__ uint32_t s_tmem;
     uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
     const int split = (int)gridDim.x, rank = (int)blockIdx.x;   // the cluster is grid dimension x
     const int64_t n0 = (int64_t)blockIdx.y * 128, t0 = (int64_t)blockIdx.z * TN;
     const int nst = (int)((P.k + stage_k(KIND) - 1) / stage_k(KIND));
@@ -155,56 +155,74 @@ __global__ void __launch_bounds__(kThreadsTile, 1) tile_kernel(const __grid_cons
     grid_dependency_wait();
     const uint32_t tmem = s_tmem;
 
-    if (tid == 128) {
-        int s = from;
-        for (; s < to; s++) {
-            const int i = s - from, r = i % P.stages;
-            if (i >= P.stages && !mbar_wait(empty0 + 8 * r, (i / P.stages - 1) & 1)) {
-                atomicOr(&s_abort, 1);
+    if (warp == 4) {
+        Ring ring;
+        bool ok = true;
+        int issued = 0;
+        for (int s = from; s < to; s++) {
+            const int r = ring.slot;
+            if (issued >= P.stages && !mbar_wait_warp(empty0 + 8 * r, ring.parity ^ 1)) {
+                ok = false;
                 break;
             }
-            const uint32_t bar = full0 + 8 * r, st = smem_u32(base) + r * C::kStage;
-            const int kc = s * (KIND == kBf16 ? 64 : 128);   // elements of the map: bf16 or bytes
-            mbar_expect_tx(bar, C::kStage);
-            tma_load_2d(st, &P.p, kc, (int)n0, bar);
-            if (C::kG == 2) tma_load_2d(st + C::kP, &P.p2, kc, (int)n0, bar);
-            tma_load_2d(st + C::kG * C::kP, &P.q, kc, (int)t0, bar);
-            if (KIND != kBf16) {
-                const uint32_t sf = st + C::kG * C::kP + C::kQ;
-                tma_load_3d(sf, &P.sp, 0, s * atoms(KIND), (int)(n0 >> 7), bar);
-                if (C::kG == 2) tma_load_3d(sf + C::kS, &P.sp2, 0, s * atoms(KIND), (int)(n0 >> 7), bar);
-                tma_load_3d(sf + C::kG * C::kS, &P.sq, 0, s * atoms(KIND), (int)(t0 >> 7), bar);
+            if (elect_one()) {
+                const uint32_t bar = full0 + 8 * r, st = smem_u32(base) + r * C::kStage;
+                const int kc = s * (KIND == kBf16 ? 64 : 128);   // elements of the map: bf16 or bytes
+                mbar_expect_tx(bar, C::kStage);
+                tma_load_2d(st, &P.p, kc, (int)n0, bar);
+                if (C::kG == 2) tma_load_2d(st + C::kP, &P.p2, kc, (int)n0, bar);
+                tma_load_2d(st + C::kG * C::kP, &P.q, kc, (int)t0, bar);
+                if (KIND != kBf16) {
+                    const uint32_t sf = st + C::kG * C::kP + C::kQ;
+                    tma_load_3d(sf, &P.sp, 0, s * atoms(KIND), (int)(n0 >> 7), bar);
+                    if (C::kG == 2) tma_load_3d(sf + C::kS, &P.sp2, 0, s * atoms(KIND), (int)(n0 >> 7), bar);
+                    tma_load_3d(sf + C::kG * C::kS, &P.sq, 0, s * atoms(KIND), (int)(t0 >> 7), bar);
+                }
             }
+            __syncwarp();
+            if (issued < P.stages) issued++;
+            ring.next(P.stages);
         }
-        for (int i = max(0, s - from - P.stages); i < s - from; i++)       // none in flight at the end
-            if (!mbar_wait(full0 + 8 * (i % P.stages), (i / P.stages) & 1)) atomicOr(&s_abort, 1);
-    } else if (tid == 160) {
+        // every slot in use landed
+        if (issued < P.stages) ring = Ring{0, 1};            // each used once
+        for (int j = 0; j < issued; j++, ring.next(P.stages))
+            if (!mbar_wait_warp(full0 + 8 * ring.slot, ring.parity ^ 1)) ok = false;
+        if (!ok && lane == 0) atomicOr(&s_abort, 1);
+    } else if (warp == 5) {
         constexpr uint32_t id = idesc(KIND, 128, TN);
+        Ring ring;
+        bool ok = true;
         for (int s = from; s < to; s++) {
-            const int i = s - from, r = i % P.stages;
-            if (!mbar_wait(full0 + 8 * r, (i / P.stages) & 1)) {
-                atomicOr(&s_abort, 1);
+            const int r = ring.slot;
+            if (!mbar_wait_warp(full0 + 8 * r, ring.parity)) {
+                ok = false;
                 break;
             }
             tc_fence_after();
-            const uint32_t st = smem_u32(base) + r * C::kStage, sf = st + C::kG * C::kP + C::kQ;
+            if (elect_one()) {
+                const uint32_t st = smem_u32(base) + r * C::kStage, sf = st + C::kG * C::kP + C::kQ;
 #pragma unroll
-            for (int a = 0; a < (C::kG + 1) * atoms(KIND); a++) cp_atom<1>(tmem + C::kSfCol + 4 * a, atom_desc(sf + a * kAtom));
-            const int left = (int)((P.k - (int64_t)s * stage_k(KIND) + mma_k(KIND) - 1) / mma_k(KIND));
+                for (int a = 0; a < (C::kG + 1) * atoms(KIND); a++) cp_atom<1>(tmem + C::kSfCol + 4 * a, atom_desc(sf + a * kAtom));
+                const int left = (int)((P.k - (int64_t)s * stage_k(KIND) + mma_k(KIND) - 1) / mma_k(KIND));
 #pragma unroll
-            for (int kk = 0; kk < 4; kk++) {
-                if (kk >= left) break;                       // K ends inside the stage
-                const uint64_t qd = smem_desc(st + C::kG * C::kP + kk * 32, 16, 1024);
-                const uint32_t w = KIND == kNvfp4 ? id : id | sf_id(2 * (kk & 1) * (KIND == kMxfp4));
-                const uint32_t col = tmem + C::kSfCol + 4 * (KIND == kNvfp4 ? kk : kk >> 1);
+                for (int kk = 0; kk < 4; kk++) {
+                    if (kk >= left) break;                   // K ends inside the stage
+                    const uint64_t qd = smem_desc(st + C::kG * C::kP + kk * 32, 16, 1024);
+                    const uint32_t w = KIND == kMxfp4 ? id | sf_id(2 * (kk & 1)) : id;
+                    const uint32_t col = tmem + C::kSfCol + 4 * (KIND == kNvfp4 ? kk : kk >> 1);
 #pragma unroll
-                for (int g = 0; g < C::kG; g++)
-                    mma<KIND, 1>(tmem + g * TN, smem_desc(st + g * C::kP + kk * 32, 16, 1024), qd, w, (uint32_t)(i | kk),
-                                 col + g * C::kSfW, col + C::kG * C::kSfW);
+                    for (int g = 0; g < C::kG; g++)
+                        mma<KIND, 1>(tmem + g * TN, smem_desc(st + g * C::kP + kk * 32, 16, 1024), qd, w,
+                                     (uint32_t)((s - from) | kk), col + g * C::kSfW, col + C::kG * C::kSfW);
+                }
+                mma_commit(empty0 + 8 * r);
             }
-            mma_commit(empty0 + 8 * r);
+            __syncwarp();
+            ring.next(P.stages);
         }
-        mma_commit(dbar);                                    // after every MMA issued, also on a timeout
+        if (elect_one()) mma_commit(dbar);                   // after every MMA issued, also on a timeout
+        __syncwarp();
+        if (!ok && lane == 0) atomicOr(&s_abort, 1);
     }
     __syncthreads();
     if (!mbar_wait(dbar, 0)) atomicOr(&s_abort, 1);
