@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -96,7 +97,7 @@ def lib() -> ctypes.CDLL:
         L.nvfp4_ldlq_prepare.argtypes = [p, i64, f, p, p, p, p, p, sz, p]
         L.nvfp4_ldlq_workspace.argtypes, L.nvfp4_ldlq_workspace.restype = [i64, i64], sz
         L.ldlq_quantize.argtypes = [p, i, i64, i64, i, p, p, p, p, p, p, p, sz, p]
-        op = ctypes.POINTER(Fp4Operand)
+        op = ctypes.c_void_p                     # fp4_operand*: a Fp4Operand by reference, or its bytes
         L.mxfp4_quantize.argtypes = [p, i, i64, i64, i64, p, p, p, p, p]
         L.mxfp4_dequantize.argtypes = [p, p, i, i64, i64, p, i, p]
         L.fp4_matmul.argtypes = [i, op, op, i64, i64, i64, p, i, i64, p, p]
@@ -137,13 +138,19 @@ def _stream(stream):
     return int(stream)
 
 
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _current_device() -> int:
-    return torch.cuda.current_device()
+    # torch.cuda.current_device() without its check for initialisation
+    return _raw_device() if _raw_device is not None else torch.cuda.current_device()
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _current_stream(device: int) -> int:
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 def _dtype(x) -> int:
@@ -367,62 +374,64 @@ def mx_swizzled_bytes(rows: int, cols: int) -> int:
 
 def _rows(t, what: str) -> int:
     """Row stride of a 2-d tensor whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    rows, cols = t.shape
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
         raise ValueError(f"{what}: a 2-d tensor with contiguous rows is wanted")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return ld if rows > 1 else max(ld, cols)
 
 
-def _operand(m, what: str):
-    """(codes [rows, cols/2], 128x4-atom scales, S or None) as an fp4_operand, its rows and cols."""
+_pack_operand = struct.Struct("3P").pack
+
+
+def _operand(m, fmt: int, what: str):
+    """(codes [rows, cols/2], 128x4-atom scales, S or None) as the bytes of an fp4_operand (a
+    ctypes.Structure takes three times as long to fill, on a path of a few microseconds), its rows and cols."""
     codes, sf, S = m
-    if codes.dim() != 2 or not codes.is_contiguous():
-        raise ValueError(f"{what}: contiguous codes [rows, cols/2] are wanted")
     rows, half = codes.shape
-    return Fp4Operand(codes.data_ptr(), sf.data_ptr(), S.data_ptr() if S is not None else None), rows, 2 * half
+    if not codes.is_contiguous():
+        raise ValueError(f"{what}: contiguous codes [rows, cols/2] are wanted")
+    atoms = -(-half // (64 if fmt == FP4_FMT_MXFP4 else 32))       # 512 bytes: 128 rows by 4 scale columns
+    if sf.nbytes < -(-rows // 128) * atoms * 512:
+        raise ValueError(f"{what}: scales of {-(-rows // 128) * atoms * 512} bytes in the 128x4-atom layout are wanted")
+    return _pack_operand(codes.data_ptr(), sf.data_ptr(), 0 if S is None else S.data_ptr()), rows, 2 * half
 
 
-def _sf_size(fmt: int, m, what: str):
-    codes, sf, _ = m
-    want = swizzled_bytes(codes.shape[0], 2 * codes.shape[1], 32 if fmt == FP4_FMT_MXFP4 else 16)
-    if sf.numel() * sf.element_size() < want:
-        raise ValueError(f"{what}: scales of {want} bytes in the 128x4-atom layout are wanted")
-
-
-def _shaped(t, shape, what: str):
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{what}: shape {shape} is wanted, not {tuple(t.shape)}")
-
-
-def _bf16(t, what: str):
+def _out(t, shape, what: str):
+    """Pointer and row stride of an optional bf16 tensor."""
+    if t is None:
+        return None, 0
     if t.dtype != torch.bfloat16:
         raise TypeError(f"{what}: bfloat16 is wanted, not {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{what}: shape {shape} is wanted, not {tuple(t.shape)}")
+    return t.data_ptr(), _rows(t, what)
 
 
 def mxfp4_quantize(x, codes, sf_linear=None, sf_swizzled=None, status=None, stream=None):
     """MXFP4 codes and scales of x [rows, cols] (bf16 or fp32, rows contiguous, any row stride)."""
     rows, cols = x.shape
-    rc = lib().mxfp4_quantize(_ptr(x), _dtype(x), rows, cols, _rows(x, "x"), _ptr(codes), _ptr(sf_linear),
-                              _ptr(sf_swizzled), _ptr(status), _stream(stream))
+    rc = (_lib or lib()).mxfp4_quantize(x.data_ptr(), _dtype(x), rows, cols, _rows(x, "x"), _ptr(codes),
+                                        _ptr(sf_linear), _ptr(sf_swizzled), _ptr(status), _stream(stream))
     _check("mxfp4_quantize", rc)
 
 
 def mxfp4_dequantize(codes, sf, layout: int, rows: int, cols: int, out, stream=None):
-    rc = lib().mxfp4_dequantize(_ptr(codes), _ptr(sf), int(layout), int(rows), int(cols), _ptr(out), _dtype(out),
-                                _stream(stream))
+    rc = (_lib or lib()).mxfp4_dequantize(_ptr(codes), _ptr(sf), layout, rows, cols, _ptr(out), _dtype(out),
+                                          _stream(stream))
     _check("mxfp4_dequantize", rc)
 
 
 def fp4_matmul(fmt: int, a, b, out, status=None, stream=None):
     """out [m, n] (bf16 or fp32) = A B^T; a = (codes [m, k/2], swizzled scales, S or None), b likewise [n, k/2]."""
-    oa, m, k = _operand(a, "a")
-    ob, n, kb = _operand(b, "b")
+    oa, m, k = _operand(a, fmt, "a")
+    ob, n, kb = _operand(b, fmt, "b")
     if k != kb:
         raise ValueError(f"fp4_matmul: operands of {k} and {kb} columns")
-    _sf_size(fmt, a, "a")
-    _sf_size(fmt, b, "b")
-    _shaped(out, (m, n), "out")
-    rc = lib().fp4_matmul(int(fmt), oa, ob, m, n, k, _ptr(out), _dtype(out), _rows(out, "out"), _ptr(status),
-                          _stream(stream))
+    if out.shape != (m, n):
+        raise ValueError(f"out: shape {(m, n)} is wanted, not {tuple(out.shape)}")
+    rc = (_lib or lib()).fp4_matmul(fmt, oa, ob, m, n, k, out.data_ptr(), _dtype(out), _rows(out, "out"), _ptr(status),
+                                    _stream(stream))
     _check("fp4_matmul", rc)
 
 
@@ -430,40 +439,27 @@ def fp4_matmul_backward_workspace(m: int, n: int, k: int) -> int:
     return int(lib().fp4_matmul_backward_workspace(int(m), int(n), int(k)))
 
 
-def _grad(t, shape, what: str):
-    """Pointer and row stride of an optional bf16 output."""
-    if t is None:
-        return None, 0
-    _bf16(t, what)
-    _shaped(t, shape, what)
-    return t.data_ptr(), _rows(t, what)
-
-
 def fp4_matmul_backward(fmt: int, a, b, d_out, d_a=None, d_b=None, workspace=None, status=None, stream=None):
     """Gradients of fp4_matmul's operands from d_out [m, n] (bf16): d_a [m, k], d_b [n, k] (bf16, either None)."""
-    oa, m, k = _operand(a, "a")
-    ob, n, kb = _operand(b, "b")
+    oa, m, k = _operand(a, fmt, "a")
+    ob, n, kb = _operand(b, fmt, "b")
     if k != kb:
         raise ValueError(f"fp4_matmul_backward: operands of {k} and {kb} columns")
-    _sf_size(fmt, a, "a")
-    _sf_size(fmt, b, "b")
-    pd, ldd = _grad(d_out, (m, n), "d_out")
-    pa, lda = _grad(d_a, (m, k), "d_a")
-    pb, ldb = _grad(d_b, (n, k), "d_b")
+    pd, ldd = _out(d_out, (m, n), "d_out")
+    pa, lda = _out(d_a, (m, k), "d_a")
+    pb, ldb = _out(d_b, (n, k), "d_b")
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    rc = lib().fp4_matmul_backward(int(fmt), oa, ob, m, n, k, pd, ldd, pa, lda, pb, ldb, _ptr(status), _ptr(workspace),
-                                   ws_bytes, _stream(stream))
+    rc = (_lib or lib()).fp4_matmul_backward(fmt, oa, ob, m, n, k, pd, ldd, pa, lda, pb, ldb, _ptr(status),
+                                             _ptr(workspace), ws_bytes, _stream(stream))
     _check("fp4_matmul_backward", rc)
 
 
 def _gated_operands(fn: str, fmt: int, x, w_gate, w_up):
-    ox, t, d = _operand(x, "x")
-    og, f, dg = _operand(w_gate, "w_gate")
-    ou, fu, du = _operand(w_up, "w_up")
+    ox, t, d = _operand(x, fmt, "x")
+    og, f, dg = _operand(w_gate, fmt, "w_gate")
+    ou, fu, du = _operand(w_up, fmt, "w_up")
     if dg != d or du != d or fu != f:
         raise ValueError(f"{fn}: operands [{t}, {d}], [{f}, {dg}] and [{fu}, {du}]")
-    for m, what in ((x, "x"), (w_gate, "w_gate"), (w_up, "w_up")):
-        _sf_size(fmt, m, what)
     return ox, og, ou, t, f, d
 
 
@@ -471,13 +467,14 @@ def fp4_gated_ff(fmt: int, act: int, x, w_gate, w_up, h=None, h_codes=None, h_sf
     """act(x Wg^T) * (x Wu^T) of quantised operands, as h [t, f] bf16 and/or as an MXFP4 operand (h_codes [t, f/2],
     h_sf of mx_swizzled_bytes(t, f) bytes)."""
     ox, og, ou, t, f, d = _gated_operands("fp4_gated_ff", fmt, x, w_gate, w_up)
-    ph, ldh = _grad(h, (t, f), "h")
+    ph, ldh = _out(h, (t, f), "h")
     if h_codes is not None:
-        _shaped(h_codes, (t, f // 2), "h_codes")
-        if h_sf is not None and h_sf.numel() < mx_swizzled_bytes(t, f):
+        if h_codes.shape != (t, f // 2) or not h_codes.is_contiguous():
+            raise ValueError(f"h_codes: contiguous, of shape {(t, f // 2)}, is wanted")
+        if h_sf is not None and h_sf.nbytes < mx_swizzled_bytes(t, f):
             raise ValueError(f"h_sf: {mx_swizzled_bytes(t, f)} bytes are wanted")
-    rc = lib().fp4_gated_ff(int(fmt), int(act), ox, og, ou, t, f, d, ph, ldh, _ptr(h_codes), _ptr(h_sf), _ptr(status),
-                            _stream(stream))
+    rc = (_lib or lib()).fp4_gated_ff(fmt, act, ox, og, ou, t, f, d, ph, ldh, _ptr(h_codes), _ptr(h_sf), _ptr(status),
+                                      _stream(stream))
     _check("fp4_gated_ff", rc)
 
 
@@ -490,14 +487,14 @@ def fp4_gated_ff_backward(fmt: int, act: int, x, w_gate, w_up, d_h, d_x=None, d_
     """Gradients of fp4_gated_ff's operands from d_h [t, f] (bf16): d_x [t, d], d_gate and d_up [f, d] (bf16, d_x or the
     pair may be None); h [t, f] optionally receives the forward result."""
     ox, og, ou, t, f, d = _gated_operands("fp4_gated_ff_backward", fmt, x, w_gate, w_up)
-    pdh, lddh = _grad(d_h, (t, f), "d_h")
-    px, ldx = _grad(d_x, (t, d), "d_x")
-    pg, ldg = _grad(d_gate, (f, d), "d_gate")
-    pu, ldu = _grad(d_up, (f, d), "d_up")
+    pdh, lddh = _out(d_h, (t, f), "d_h")
+    px, ldx = _out(d_x, (t, d), "d_x")
+    pg, ldg = _out(d_gate, (f, d), "d_gate")
+    pu, ldu = _out(d_up, (f, d), "d_up")
     if pg and pu and ldg != ldu:
         raise ValueError("d_gate and d_up: one row stride is wanted")
-    ph, ldh = _grad(h, (t, f), "h")
+    ph, ldh = _out(h, (t, f), "h")
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    rc = lib().fp4_gated_ff_backward(int(fmt), int(act), ox, og, ou, t, f, d, pdh, lddh, px, ldx, pg, pu, ldg, ph, ldh,
-                                     _ptr(status), _ptr(workspace), ws_bytes, _stream(stream))
+    rc = (_lib or lib()).fp4_gated_ff_backward(fmt, act, ox, og, ou, t, f, d, pdh, lddh, px, ldx, pg, pu, ldg, ph, ldh,
+                                               _ptr(status), _ptr(workspace), ws_bytes, _stream(stream))
     _check("fp4_gated_ff_backward", rc)
