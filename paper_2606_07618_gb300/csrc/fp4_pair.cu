@@ -4,15 +4,13 @@
 //   out[t][n] = epilogue( sum_k q[t][k] p[n][k] )
 //
 // Tokens are the MMA's M side, so a thread's accumulator columns are consecutive columns of
-// one row: a block of 32 for MXFP4 is one thread's, and stores go out as boxes.  Each CTA
+// one row: whole sectors to store, and a block of 32 for MXFP4.  Each CTA
 // loads its 128 token rows and half of the 256 weight rows; the leader's MMA reads both halves,
 // so a stage of K costs 64 KB of loads for 256 x 256 x 128 bytes of K.
 //   warp 8   loads: 128 bytes of K a stage, operands and scale atoms, by TMA; completion is
 //            counted on the leader's barrier
 //   warp 9   (leader) copies the scale atoms of both CTAs to tensor memory and issues the MMAs
-//   warps 0-7  accumulators to results, 32 columns at a time, through two 2 KB boxes of shared
-//            memory a warp, stored by TMA (rows of single elements where the result's
-//            stride does not allow that); beside the next tile's MMAs
+//   warps 0-7  accumulators to results, beside the next tile's MMAs
 //
 // Tensor memory holds two accumulators of 256 columns and 48 columns of scales in 512: with
 // scales the accumulators overlap in 48 columns, which the epilogue drains first.  An arrival
@@ -34,10 +32,9 @@ constexpr int kPairStages = 6;                               // at most
 
 struct PairParams {
     CUtensorMap p, p2, q, sp, sp2, sq;
-    CUtensorMap o, o2, o3;                                   // results: D or h; dg and du
     int64_t k;
     int tiles_t, tiles_n;
-    int64_t boxed;                                           // columns of D or h that go out by TMA
+    int wide_out, wide_dh, wide_codes;                       // bytes that rows of D or h, dh, codes are aligned to: 32, 16 or fewer
     Epilogue e;
 };
 
@@ -47,7 +44,7 @@ struct Pair {
     static constexpr int kS = atoms(KIND) * kAtom;
     static constexpr int kStage = 2 * kOp + 3 * kS;          // + scales of its tokens, of all columns
     static constexpr int kStages = KIND == kBf16 ? 6 : 5;
-    static constexpr int kSmem = kStages * kStage + kEpiWarps * 2 * kBox + 1024;
+    static constexpr int kSmem = kStages * kStage + kEpiWarps * kBox + 1024;
     static constexpr int kSf = 464;                          // scale columns: tokens, then columns
     static constexpr int kAcc1 = KIND == kBf16 ? 256 : 208;  // the second accumulator
 };
@@ -72,8 +69,6 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-__device__ __forceinline__ void store_wait_read1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
-
 // Tile number -> token and column tile.  Eight token tiles are walked for each column tile, so
 // that the tiles in flight at one time cover a near-square of the result.
 __device__ __forceinline__ void tile_at(int i, int tiles_t, int tiles_n, int& tt, int& tn) {
@@ -82,63 +77,62 @@ __device__ __forceinline__ void tile_at(int i, int tiles_t, int tiles_n, int& tt
     tn = j / rows;
 }
 
-// A warp's boxes: 32 rows (lanes) of 64 bytes, 64-byte swizzle.
-struct Boxes {
-    uint8_t* base;
-    int next = 0;
-    int lane;
-    __device__ __forceinline__ uint8_t* take() {             // the box of two stores ago has been read
-        if (lane == 0) store_wait_read1();
-        __syncwarp();
-        return base + (next++ & 1) * kBox;
-    }
-    __device__ __forceinline__ void put(uint8_t* box, int c, uint4 v) const {
-        *reinterpret_cast<uint4*>(box + lane * 64 + ((c ^ (lane >> 1 & 3)) << 4)) = v;
-    }
-    __device__ __forceinline__ void store(const uint8_t* box, const CUtensorMap* map, int64_t n, int64_t t) const {
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) {
-            tma_store_2d(map, (int)n, (int)t, smem_u32(box));
-            tma_store_commit();
-        }
-    }
-    // the same by single elements of ES bytes: rows t.. below T, columns n.. below N
-    template <int ES>
-    __device__ __forceinline__ void spill(const uint8_t* box, void* out, int64_t ld, int64_t n, int64_t t, int64_t N,
-                                          int64_t T) const {
-        __syncwarp();
-        for (int r = lane >> 4; r < 32; r += 2) {
-            const int w = lane & 15;
-            const uint32_t v = *reinterpret_cast<const uint32_t*>(box + r * 64 + (((w >> 2) ^ (r >> 1 & 3)) << 4) + (w & 3) * 4);
-            if (t + r >= T) continue;
-            if (ES == 4) {
-                if (n + w < N) static_cast<uint32_t*>(out)[(t + r) * ld + n + w] = v;
-            } else {
-                if (n + 2 * w < N) static_cast<uint16_t*>(out)[(t + r) * ld + n + 2 * w] = (uint16_t)v;
-                if (n + 2 * w + 1 < N) static_cast<uint16_t*>(out)[(t + r) * ld + n + 2 * w + 1] = (uint16_t)(v >> 16);
-            }
-        }
-        __syncwarp();
-    }
-};
+__device__ __forceinline__ void st32(void* p, uint4 a, uint4 b) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+}
+__device__ __forceinline__ uint4 word4(const uint32_t* w) { return make_uint4(w[0], w[1], w[2], w[3]); }
 
 __device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// 32 bf16 (16 words) of this lane's row to a box and out; columns from `boxed` on by elements.
-__device__ __forceinline__ void out_bf16(Boxes& bx, const uint32_t (&w)[16], int64_t boxed, const CUtensorMap* map, void* out,
-                                         int64_t ld, int64_t n, int64_t t, int64_t N, int64_t T) {
-    if (n >= N || t >= T) return;                            // uniform: t is the warp's first row
-    uint8_t* box = bx.take();
+// W words (64 or 128 bytes) of this lane's row t0 + lane, columns n.. of a result with N columns
+// and T rows.  Rows aligned to 32 bytes go out as whole sectors, a lane's own (no staging:
+// TMA stores of boxes waited behind the loads in the SM's TMA queue, 7.2 us a tile of K = 4096 where
+// this takes 5.9).  Other rows, and a ragged last chunk, pass through the warp's 2 KB of
+// shared memory and go out by elements, a row's consecutive ones to consecutive lanes.
+template <int ES, int W>
+__device__ __forceinline__ void put_row(const uint32_t (&w)[W], int wide, uint8_t* box, void* out, int64_t ld, int64_t n,
+                                        int64_t t0, int64_t N, int64_t T) {
+    const int lane = threadIdx.x & 31;
+    if (n >= N || t0 >= T) return;                           // the same for the warp
+    if (wide >= 16 && n + W * 4 / ES <= N) {
+        if (t0 + lane >= T) return;
+        char* at = static_cast<char*>(out) + ((t0 + lane) * ld + n) * ES;
 #pragma unroll
-    for (int c = 0; c < 4; c++) bx.put(box, c, make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]));
-    if (n < boxed)
-        bx.store(box, map, n, t);
-    else
-        bx.spill<2>(box, out, ld, n, t, N, T);
+        for (int i = 0; i < W; i += 8) {
+            if (wide == 32) {
+                st32(at + 4 * i, word4(w + i), word4(w + i + 4));
+            } else {
+                *reinterpret_cast<uint4*>(at + 4 * i) = word4(w + i);
+                *reinterpret_cast<uint4*>(at + 4 * i + 16) = word4(w + i + 4);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < W; i += 16) {                        // 32 rows of 64 bytes, 16-byte parts swapped against conflicts
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 4; c++) *reinterpret_cast<uint4*>(box + lane * 64 + ((c ^ (lane >> 1 & 3)) << 4)) = word4(w + i + 4 * c);
+        __syncwarp();
+        constexpr int kCols = 64 / ES;
+        const int c = lane % kCols;
+        const int64_t col = n + i * 4 / ES + c;
+        if (col < N)
+#pragma unroll 4
+            for (int r = lane / kCols; r < 32; r += 32 / kCols) {
+                if (t0 + r >= T) break;
+                const uint8_t* from = box + r * 64 + (((c * ES >> 4) ^ (r >> 1 & 3)) << 4) + (c * ES & 15);
+                if (ES == 4)
+                    static_cast<uint32_t*>(out)[(t0 + r) * ld + col] = *reinterpret_cast<const uint32_t*>(from);
+                else
+                    static_cast<uint16_t*>(out)[(t0 + r) * ld + col] = *reinterpret_cast<const uint16_t*>(from);
+            }
+        __syncwarp();
+    }
 }
 
 template <int KIND, int MODE>
@@ -270,7 +264,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
         const Epilogue& e = P.e;
         const float sp = scale_or_1(e.s_p), sp2 = MODE != kPlain ? scale_or_1(e.s_p2) : 1.0f, sq = scale_or_1(e.s_q);
         const int half = warp >> 2, q = warp & 3;
-        Boxes bx{base + C::kStages * C::kStage + warp * 2 * kBox, 0, lane};
+        uint8_t* box = base + C::kStages * C::kStage + warp * kBox;
         const uint32_t leader_drained = at_rank(drained0, 0);
         bool bad = false;
         int it = 0;
@@ -294,35 +288,30 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
             const uint32_t acc = tmem + b * C::kAcc1 + ((uint32_t)(32 * q) << 16);
             const int64_t tw = (int64_t)tt * 256 + rank * 128 + 32 * q, t = tw + lane;   // the warp's first row, this lane's
             if (MODE == kPlain) {
+                // two halves of 64 columns, the overlapping one first
 #pragma unroll 1
-                for (int c = 0; c < 4; c++) {
-                    const int col = 128 * half + 32 * (overlap && half == 1 ? 3 - c : c);   // overlapping columns first
-                    float v[32];
-                    tmem_ld32(acc + col, v);
-                    tmem_wait32(v);
-                    if (overlap && c == 1) release();
-                    const int64_t n = (int64_t)tn * 256 + col;
+                for (int c = 0; c < 2; c++) {
+                    const int col = 128 * half + 64 * (overlap && half == 1 ? 1 - c : c);
+                    float v[2][32];
+                    tmem_ld32(acc + col, v[0]);
+                    tmem_ld32(acc + col + 32, v[1]);
+                    tmem_wait32(v[0]);
+                    tmem_wait32(v[1]);
+                    if (overlap && c == 0) release();
 #pragma unroll
-                    for (int j = 0; j < 32; j++) v[j] = v[j] * sp * sq;
-                    if (e.out_f32) {
+                    for (int z = 0; z < 2; z++) {
+                        const int64_t n = (int64_t)tn * 256 + col + 32 * z;
+                        if (e.out_f32) {
+                            uint32_t w[32];
 #pragma unroll
-                        for (int g = 0; g < 2; g++) {
-                            if (n + 16 * g >= e.N || tw >= e.T) continue;
-                            uint8_t* box = bx.take();
+                            for (int j = 0; j < 32; j++) w[j] = __float_as_uint(v[z][j] * sp * sq);
+                            put_row<4, 32>(w, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
+                        } else {
+                            uint32_t w[16];
 #pragma unroll
-                            for (int j = 0; j < 4; j++)
-                                bx.put(box, j, make_uint4(__float_as_uint(v[16 * g + 4 * j]), __float_as_uint(v[16 * g + 4 * j + 1]),
-                                                          __float_as_uint(v[16 * g + 4 * j + 2]), __float_as_uint(v[16 * g + 4 * j + 3])));
-                            if (n + 16 * g < P.boxed)
-                                bx.store(box, &P.o, n + 16 * g, tw);
-                            else
-                                bx.spill<4>(box, e.out, e.ldo, n + 16 * g, tw, e.N, e.T);
+                            for (int j = 0; j < 16; j++) w[j] = pack2_bf16(v[z][2 * j] * sp * sq, v[z][2 * j + 1] * sp * sq);
+                            put_row<2, 16>(w, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
                         }
-                    } else {
-                        uint32_t w[16];
-#pragma unroll
-                        for (int j = 0; j < 16; j++) w[j] = pack2_bf16(v[2 * j], v[2 * j + 1]);
-                        out_bf16(bx, w, P.boxed, &P.o, e.out, e.ldo, n, tw, e.N, e.T);
                     }
                 }
             } else {
@@ -333,7 +322,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                 tmem_wait32(first_[0]);
                 tmem_wait32(first_[1]);
                 if (overlap) release();
-                uint32_t sf2 = 0;
+                uint32_t sf2 = 0, cw[8];
 #pragma unroll
                 for (int c = 0; c < 2; c++) {
                     float g[32], u[32], other[32];
@@ -343,12 +332,17 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                     uint32_t dhw[16];
                     if (MODE == kGatedGrad) {
                         const uint16_t* at = e.dh + t * e.lddh + n;
-                        if (row && n + 32 <= e.N && ((reinterpret_cast<uintptr_t>(at) & 15) == 0)) {
+                        if (row && n + 32 <= e.N && P.wide_dh >= 16) {
+                            uint4 d[4];
+                            if (P.wide_dh == 32) {
+                                ld_stream32<false>(at, d[0], d[1]);
+                                ld_stream32<false>(at + 16, d[2], d[3]);
+                            } else {
 #pragma unroll
-                            for (int j = 0; j < 4; j++) {
-                                const uint4 d = *reinterpret_cast<const uint4*>(at + 8 * j);
-                                dhw[4 * j] = d.x, dhw[4 * j + 1] = d.y, dhw[4 * j + 2] = d.z, dhw[4 * j + 3] = d.w;
+                                for (int j = 0; j < 4; j++) d[j] = ld_stream16<false>(at + 8 * j);
                             }
+#pragma unroll
+                            for (int j = 0; j < 4; j++) dhw[4 * j] = d[j].x, dhw[4 * j + 1] = d[j].y, dhw[4 * j + 2] = d[j].z, dhw[4 * j + 3] = d[j].w;
                         } else {
 #pragma unroll
                             for (int j = 0; j < 16; j++) {
@@ -393,8 +387,8 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                             us[j] = n + 2 * j < e.N ? pack2_bf16(du[0] * sp2, n + 2 * j + 1 < e.N ? du[1] * sp2 : 0.0f) : 0u;
                         }
                         if (e.dgu) {
-                            out_bf16(bx, gs, e.fp, &P.o2, nullptr, 0, n, tw, e.fp, e.T);
-                            out_bf16(bx, us, e.fp, &P.o3, nullptr, 0, n, tw, e.fp, e.T);
+                            put_row<2, 16>(gs, 32, box, e.dgu, 2 * e.fp, n, tw, e.fp, e.T);
+                            put_row<2, 16>(us, 32, box, e.dgu + e.fp, 2 * e.fp, n, tw, e.fp, e.T);
                         }
                         if (e.dgu_t) {
                             // two neighbouring tokens of a column in one word: lanes exchange halves
@@ -413,7 +407,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                             }
                         }
                     }
-                    if (e.out) out_bf16(bx, hw, P.boxed, &P.o, e.out, e.ldo, n, tw, e.N, e.T);
+                    if (e.out) put_row<2, 16>(hw, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
                     if (MODE == kGated && e.h_codes) {
                         const bool live = row && n < e.N;    // N is a multiple of 32
                         uint32_t m = 0;
@@ -427,7 +421,6 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                         bad |= !finite;
                         const uint32_t code = finite && ex > 2 ? ex - 2 : 0;
                         const float inv = __uint_as_float((254u - code) << 23);
-                        uint32_t w[4];
 #pragma unroll
                         for (int j = 0; j < 4; j++) {
                             u64 x[4];
@@ -437,9 +430,14 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                                 x[z] = finite ? pack2(bf16lo(two) * inv, bf16hi(two) * inv)
                                               : pack2(copysignf(0.0f, bf16lo(two)), copysignf(0.0f, bf16hi(two)));
                             }
-                            w[j] = e2m1x8(x[0], x[1], x[2], x[3]);
+                            cw[4 * c + j] = e2m1x8(x[0], x[1], x[2], x[3]);
                         }
-                        if (live) *reinterpret_cast<uint4*>(e.h_codes + t * (e.N / 2) + n / 2) = make_uint4(w[0], w[1], w[2], w[3]);
+                        uint8_t* at = e.h_codes + t * (e.N / 2) + n / 2;
+                        if (P.wide_codes == 32) {            // both blocks are there: N is a multiple of 64
+                            if (c == 1 && live) st32(at - 16, word4(cw), word4(cw + 4));
+                        } else if (live) {
+                            *reinterpret_cast<uint4*>(at) = word4(cw + 4 * c);
+                        }
                         sf2 |= code << (8 * c);
                     }
                 }
@@ -449,7 +447,6 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                 }
             }
         }
-        if (lane == 0) tma_store_wait();
         if (bad && e.status) atomicOr(e.status, 1);
     }
     tc_fence_before();
@@ -460,18 +457,10 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-// Boxes of 64 bytes by 32 rows of a result.
-bool make_box_map(CUtensorMap* m, void* ptr, bool f32, int64_t rows, int64_t cols, int64_t ld) {
-    const EncodeTiledFn enc = encode_fn();
-    const int es = f32 ? 4 : 2;
-    if (!enc || (reinterpret_cast<uintptr_t>(ptr) & 15) || (ld * es & 15)) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)(ld * es)};
-    const cuuint32_t box[2] = {(cuuint32_t)(64 / es), 32};
-    const cuuint32_t one[2] = {1, 1};
-    return enc(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ptr, dims, strides, box, one,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+// What a matrix's rows are aligned to: 32, 16 or fewer bytes (1).
+int row_alignment(const void* p, int64_t stride_bytes) {
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | (uintptr_t)stride_bytes;
+    return bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 1;
 }
 
 template <int KIND, int MODE>
@@ -485,15 +474,9 @@ cudaError_t launch_pair_as(const Product& p, int sms, cudaStream_t s) {
     if (!ok) return cudaErrorNotSupported;
     P.k = p.k;
     P.e = make_epilogue(p);
-    // A store's box is cut at the matrix's edge in whole 16 bytes, so a box that holds a
-    // ragged edge goes out by elements.
-    if (p.out && make_box_map(&P.o, p.out, p.out_f32, p.q.rows, p.p.rows, p.ldo)) {
-        const int64_t es = p.out_f32 ? 4 : 2;
-        P.boxed = p.p.rows * es % 16 == 0 ? p.p.rows : p.p.rows / (64 / es) * (64 / es);
-    }
-    if (p.dgu && (!make_box_map(&P.o2, p.dgu, false, p.q.rows, p.fp, 2 * p.fp) ||
-                  !make_box_map(&P.o3, static_cast<uint16_t*>(p.dgu) + p.fp, false, p.q.rows, p.fp, 2 * p.fp)))
-        return cudaErrorNotSupported;
+    P.wide_out = row_alignment(p.out, p.ldo * (p.out_f32 ? 4 : 2));
+    P.wide_dh = row_alignment(p.dh, p.lddh * 2);
+    P.wide_codes = row_alignment(p.h_codes, p.p.rows / 2);
     const int64_t width = MODE == kPlain ? 256 : 128;
     P.tiles_t = (int)((p.q.rows + 255) / 256);
     P.tiles_n = (int)((p.p.rows + width - 1) / width);
