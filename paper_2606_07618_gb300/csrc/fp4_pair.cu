@@ -271,6 +271,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
         for (int i = first; i < ntiles; i += step, it++) {
             int tt, tn;
             tile_at(i, P.tiles_t, P.tiles_n, tt, tn);
+            const int64_t tw = (int64_t)tt * 256 + rank * 128 + 32 * q, t = tw + lane;   // the warp's first row, this lane's
             const int b = it & 1;
             const bool overlap = KIND != kBf16 && half == 1 - b;     // this warp reads the overlapping columns
             auto release = [&]() {
@@ -279,6 +280,35 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                 if (lane == 0) arrive_at(leader_drained + 8 * b);
             };
             if (!overlap) release();                         // done with the tile before
+            // dh of this tile, asked for before its accumulators are waited for
+            uint32_t dhw[2][16];
+            if (MODE == kGatedGrad) {
+#pragma unroll
+                for (int c = 0; c < 2; c++) {
+                    const int64_t n = (int64_t)tn * 128 + 64 * half + 32 * c;
+                    const bool row = t < e.T;
+                    const uint16_t* at = e.dh + t * e.lddh + n;
+                    if (row && n + 32 <= e.N && P.wide_dh >= 16) {
+                        uint4 d[4];
+                        if (P.wide_dh == 32) {
+                            ld_stream32<false>(at, d[0], d[1]);
+                            ld_stream32<false>(at + 16, d[2], d[3]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 4; j++) d[j] = ld_stream16<false>(at + 8 * j);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; j++)
+                            dhw[c][4 * j] = d[j].x, dhw[c][4 * j + 1] = d[j].y, dhw[c][4 * j + 2] = d[j].z, dhw[c][4 * j + 3] = d[j].w;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; j++) {
+                            const uint32_t lo = row && n + 2 * j < e.N ? at[2 * j] : 0, hi = row && n + 2 * j + 1 < e.N ? at[2 * j + 1] : 0;
+                            dhw[c][j] = lo | hi << 16;
+                        }
+                    }
+                }
+            }
             if (!mbar_wait(accf0 + 8 * b, (it >> 1) & 1)) {
                 atomicOr(&s_abort, 1);
                 break;
@@ -286,7 +316,6 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
             tc_fence_after();
             __syncwarp();
             const uint32_t acc = tmem + b * C::kAcc1 + ((uint32_t)(32 * q) << 16);
-            const int64_t tw = (int64_t)tt * 256 + rank * 128 + 32 * q, t = tw + lane;   // the warp's first row, this lane's
             if (MODE == kPlain) {
                 // two halves of 64 columns, the overlapping one first
 #pragma unroll 1
@@ -329,28 +358,6 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                     tmem_ld32(acc + (128 - pre) + 64 * half + 32 * c, other);
                     const int64_t n = (int64_t)tn * 128 + 64 * half + 32 * c;
                     const bool row = t < e.T;
-                    uint32_t dhw[16];
-                    if (MODE == kGatedGrad) {
-                        const uint16_t* at = e.dh + t * e.lddh + n;
-                        if (row && n + 32 <= e.N && P.wide_dh >= 16) {
-                            uint4 d[4];
-                            if (P.wide_dh == 32) {
-                                ld_stream32<false>(at, d[0], d[1]);
-                                ld_stream32<false>(at + 16, d[2], d[3]);
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 4; j++) d[j] = ld_stream16<false>(at + 8 * j);
-                            }
-#pragma unroll
-                            for (int j = 0; j < 4; j++) dhw[4 * j] = d[j].x, dhw[4 * j + 1] = d[j].y, dhw[4 * j + 2] = d[j].z, dhw[4 * j + 3] = d[j].w;
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 16; j++) {
-                                const uint32_t lo = row && n + 2 * j < e.N ? at[2 * j] : 0, hi = row && n + 2 * j + 1 < e.N ? at[2 * j + 1] : 0;
-                                dhw[j] = lo | hi << 16;
-                            }
-                        }
-                    }
                     tmem_wait32(other);
 #pragma unroll
                     for (int j = 0; j < 32; j++) {
@@ -371,7 +378,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                             float dg[2], du[2], hv[2];
 #pragma unroll
                             for (int z = 0; z < 2; z++) {
-                                const float dh = z ? bf16hi(dhw[j]) : bf16lo(dhw[j]);
+                                const float dh = z ? bf16hi(dhw[c][j]) : bf16lo(dhw[c][j]);
                                 float da;
                                 const float ag = activate<true>(e.act, g[2 * j + z], da);
                                 const bool live = row && n + 2 * j + z < e.N;
