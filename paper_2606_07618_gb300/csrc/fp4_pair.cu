@@ -180,7 +180,8 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
         const uint32_t leader_full = at_rank(full0, 0);
         bool ok = true;
         int issued = 0;
-        for (int i = first; ok && i < ntiles; i += step) {
+        uint32_t swap = 0;                                   // gated: gate and up change places with the accumulators
+        for (int i = first; ok && i < ntiles; i += step, swap ^= 1) {
             int tt, tn;
             tile_at(i, P.tiles_t, P.tiles_n, tt, tn);
             const int t0 = tt * 256 + (int)rank * 128;
@@ -198,16 +199,18 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                     if (MODE == kPlain)
                         tma_load_2d_pair(st + C::kOp, &P.p, x, tn * 256 + (int)rank * 128, bar);
                     else
-                        tma_load_2d_pair(st + C::kOp, rank == 0 ? &P.p : &P.p2, x, tn * 128, bar);
+                        tma_load_2d_pair(st + C::kOp, rank == swap ? &P.p : &P.p2, x, tn * 128, bar);
                     if (KIND != kBf16) {
                         const uint32_t sf = st + 2 * C::kOp;
                         const int a = kc * atoms(KIND);
                         tma_load_3d_pair(sf, &P.sq, 0, a, t0 >> 7, bar);
-                        tma_load_3d_pair(sf + C::kS, &P.sp, 0, a, MODE == kPlain ? 2 * tn : tn, bar);
-                        if (MODE == kPlain)
+                        if (MODE == kPlain) {
+                            tma_load_3d_pair(sf + C::kS, &P.sp, 0, a, 2 * tn, bar);
                             tma_load_3d_pair(sf + 2 * C::kS, &P.sp, 0, a, 2 * tn + 1, bar);
-                        else
-                            tma_load_3d_pair(sf + 2 * C::kS, &P.sp2, 0, a, tn, bar);
+                        } else {
+                            tma_load_3d_pair(sf + C::kS, swap ? &P.sp2 : &P.sp, 0, a, tn, bar);
+                            tma_load_3d_pair(sf + 2 * C::kS, swap ? &P.sp : &P.sp2, 0, a, tn, bar);
+                        }
                     }
                 }
                 __syncwarp();
@@ -344,79 +347,82 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                     }
                 }
             } else {
-                float first_[2][32];                         // what overlaps: the up columns of the upper half, the gate's of the lower
-                const int pre = half == 1 ? 128 : 0;
-                tmem_ld32(acc + pre + 64 * half, first_[0]);
-                tmem_ld32(acc + pre + 64 * half + 32, first_[1]);
-                tmem_wait32(first_[0]);
-                tmem_wait32(first_[1]);
+                // The up columns (the overlapping ones are theirs in either accumulator) to registers, then 32
+                // gate columns at a time; rolled, for the instruction cache.
+                const uint32_t up = acc + (b == 0 ? 128 : 0) + 64 * half, gate = acc + (b == 0 ? 0 : 128) + 64 * half;
+                float u[2][32];
+                tmem_ld32(up, u[0]);
+                tmem_ld32(up + 32, u[1]);
+                tmem_wait32(u[0]);
+                tmem_wait32(u[1]);
                 if (overlap) release();
-                uint32_t sf2 = 0, cw[8];
-#pragma unroll
+                uint32_t codes0[4], code0 = 0;               // of the first 32 columns
+#pragma unroll 1
                 for (int c = 0; c < 2; c++) {
-                    float g[32], u[32], other[32];
-                    tmem_ld32(acc + (128 - pre) + 64 * half + 32 * c, other);
                     const int64_t n = (int64_t)tn * 128 + 64 * half + 32 * c;
-                    const bool row = t < e.T;
-                    tmem_wait32(other);
+                    float g[32];
+                    tmem_ld32(gate + 32 * c, g);
+                    tmem_wait32(g);
 #pragma unroll
                     for (int j = 0; j < 32; j++) {
-                        g[j] = (half == 1 ? other[j] : first_[c][j]) * sp * sq;
-                        u[j] = (half == 1 ? first_[c][j] : other[j]) * sp2 * sq;
+                        g[j] = g[j] * sp * sq;
+                        u[0][j] = u[0][j] * sp2 * sq;
                     }
                     uint32_t hw[16];
                     if (MODE == kGated) {
-                        float unused;
+                        activate32<false>(e.act, g, nullptr);
 #pragma unroll
-                        for (int j = 0; j < 16; j++)
-                            hw[j] = pack2_bf16(activate<false>(e.act, g[2 * j], unused) * u[2 * j],
-                                               activate<false>(e.act, g[2 * j + 1], unused) * u[2 * j + 1]);
+                        for (int j = 0; j < 16; j++) hw[j] = pack2_bf16(g[2 * j] * u[0][2 * j], g[2 * j + 1] * u[0][2 * j + 1]);
                     } else {
-                        uint32_t gs[16], us[16], gt[16], ut[16];
+                        // dh is zero where there is no token or no column, and with it dg and du
+                        float da[32];
+                        activate32<true>(e.act, g, da);
+                        uint32_t gt[16], ut[16];
 #pragma unroll
                         for (int j = 0; j < 16; j++) {
-                            float dg[2], du[2], hv[2];
-#pragma unroll
-                            for (int z = 0; z < 2; z++) {
-                                const float dh = z ? bf16hi(dhw[c][j]) : bf16lo(dhw[c][j]);
-                                float da;
-                                const float ag = activate<true>(e.act, g[2 * j + z], da);
-                                const bool live = row && n + 2 * j + z < e.N;
-                                dg[z] = live ? dh * u[2 * j + z] * da : 0.0f;
-                                du[z] = live ? dh * ag : 0.0f;
-                                hv[z] = ag * u[2 * j + z];
-                            }
-                            hw[j] = pack2_bf16(hv[0], hv[1]);
-                            gt[j] = pack2_bf16(dg[0], dg[1]);
-                            ut[j] = pack2_bf16(du[0], du[1]);
-                            // a scale that is no number belongs to the columns below N alone
-                            gs[j] = n + 2 * j < e.N ? pack2_bf16(dg[0] * sp, n + 2 * j + 1 < e.N ? dg[1] * sp : 0.0f) : 0u;
-                            us[j] = n + 2 * j < e.N ? pack2_bf16(du[0] * sp2, n + 2 * j + 1 < e.N ? du[1] * sp2 : 0.0f) : 0u;
-                        }
-                        if (e.dgu) {
-                            put_row<2, 16>(gs, 32, box, e.dgu, 2 * e.fp, n, tw, e.fp, e.T);
-                            put_row<2, 16>(us, 32, box, e.dgu + e.fp, 2 * e.fp, n, tw, e.fp, e.T);
+                            const float d0 = bf16lo(dhw[0][j]), d1 = bf16hi(dhw[0][j]);
+                            hw[j] = pack2_bf16(g[2 * j] * u[0][2 * j], g[2 * j + 1] * u[0][2 * j + 1]);
+                            g[2 * j] *= d0;
+                            g[2 * j + 1] *= d1;
+                            ut[j] = pack2_bf16(g[2 * j], g[2 * j + 1]);
+                            da[2 * j] *= d0 * u[0][2 * j];
+                            da[2 * j + 1] *= d1 * u[0][2 * j + 1];
+                            gt[j] = pack2_bf16(da[2 * j], da[2 * j + 1]);
                         }
                         if (e.dgu_t) {
                             // two neighbouring tokens of a column in one word: lanes exchange halves
                             const int64_t t2 = tw + (lane & ~1);
                             const bool in = t2 < e.ldt;
+                            const uint32_t sel = lane & 1 ? 0x3276 : 0x5410;
                             uint16_t* at = e.dgu_t + (n + (lane & 1)) * e.ldt + t2;
+                            uint16_t* at2 = at + e.fp * e.ldt;
 #pragma unroll
                             for (int j = 0; j < 16; j++) {
-                                const uint32_t pg = __shfl_xor_sync(0xFFFFFFFFu, gt[j], 1), pu = __shfl_xor_sync(0xFFFFFFFFu, ut[j], 1);
-                                const uint32_t wg = lane & 1 ? __byte_perm(pg, gt[j], 0x7632) : __byte_perm(gt[j], pg, 0x5410);
-                                const uint32_t wu = lane & 1 ? __byte_perm(pu, ut[j], 0x7632) : __byte_perm(ut[j], pu, 0x5410);
+                                const uint32_t wg = __byte_perm(gt[j], __shfl_xor_sync(0xFFFFFFFFu, gt[j], 1), sel);
+                                const uint32_t wu = __byte_perm(ut[j], __shfl_xor_sync(0xFFFFFFFFu, ut[j], 1), sel);
                                 if (in) {
-                                    *reinterpret_cast<uint32_t*>(at + 2 * j * e.ldt) = wg;
-                                    *reinterpret_cast<uint32_t*>(at + (e.fp + 2 * j) * e.ldt) = wu;
+                                    *reinterpret_cast<uint32_t*>(at) = wg;
+                                    *reinterpret_cast<uint32_t*>(at2) = wu;
+                                }
+                                at += 2 * e.ldt;
+                                at2 += 2 * e.ldt;
+                            }
+                        }
+                        if (e.dgu) {
+                            if (KIND == kNvfp4) {            // times the weights' global scales
+#pragma unroll
+                                for (int j = 0; j < 16; j++) {
+                                    gt[j] = pack2_bf16(da[2 * j] * sp, da[2 * j + 1] * sp);
+                                    ut[j] = pack2_bf16(g[2 * j] * sp2, g[2 * j + 1] * sp2);
                                 }
                             }
+                            put_row<2, 16>(gt, 32, box, e.dgu, 2 * e.fp, n, tw, e.fp, e.T);
+                            put_row<2, 16>(ut, 32, box, e.dgu + e.fp, 2 * e.fp, n, tw, e.fp, e.T);
                         }
                     }
                     if (e.out) put_row<2, 16>(hw, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
                     if (MODE == kGated && e.h_codes) {
-                        const bool live = row && n < e.N;    // N is a multiple of 32
+                        const bool live = t < e.T && n < e.N;    // N is a multiple of 32
                         uint32_t m = 0;
 #pragma unroll
                         for (int j = 0; j < 16; j++) {
@@ -428,29 +434,35 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                         bad |= !finite;
                         const uint32_t code = finite && ex > 2 ? ex - 2 : 0;
                         const float inv = __uint_as_float((254u - code) << 23);
+                        uint32_t w[4];
 #pragma unroll
                         for (int j = 0; j < 4; j++) {
                             u64 x[4];
 #pragma unroll
                             for (int z = 0; z < 4; z++) {
-                                const uint32_t two = hw[4 * j + z];
-                                x[z] = finite ? pack2(bf16lo(two) * inv, bf16hi(two) * inv)
-                                              : pack2(copysignf(0.0f, bf16lo(two)), copysignf(0.0f, bf16hi(two)));
+                                const uint32_t two = finite ? hw[4 * j + z] : hw[4 * j + z] & 0x80008000u;
+                                x[z] = pack2(bf16lo(two) * inv, bf16hi(two) * inv);
                             }
-                            cw[4 * c + j] = e2m1x8(x[0], x[1], x[2], x[3]);
+                            w[j] = e2m1x8(x[0], x[1], x[2], x[3]);
                         }
                         uint8_t* at = e.h_codes + t * (e.N / 2) + n / 2;
                         if (P.wide_codes == 32) {            // both blocks are there: N is a multiple of 64
-                            if (c == 1 && live) st32(at - 16, word4(cw), word4(cw + 4));
+                            if (c == 1 && live) st32(at - 16, word4(codes0), word4(w));
                         } else if (live) {
-                            *reinterpret_cast<uint4*>(at) = word4(cw + 4 * c);
+                            *reinterpret_cast<uint4*>(at) = word4(w);
                         }
-                        sf2 |= code << (8 * c);
+                        if (c == 1 && (tw & ~127ll) < e.T)   // rows of an atom that hold no token: zero
+                            *reinterpret_cast<uint16_t*>(e.h_sf + swizzle_offset(t, (n >> 5) - 1, e.h_kpad4)) =
+                                (uint16_t)(code0 | code << 8);
+#pragma unroll
+                        for (int j = 0; j < 4; j++) codes0[j] = w[j];
+                        code0 = code;
                     }
-                }
-                if (MODE == kGated && e.h_codes && (tw & ~127ll) < e.T) {    // rows of an atom that hold no token: zero
-                    const int64_t n = (int64_t)tn * 128 + 64 * half;
-                    *reinterpret_cast<uint16_t*>(e.h_sf + swizzle_offset(t, n >> 5, e.h_kpad4)) = (uint16_t)sf2;
+#pragma unroll
+                    for (int j = 0; j < 32; j++) u[0][j] = u[1][j];
+                    if (MODE == kGatedGrad)
+#pragma unroll
+                        for (int j = 0; j < 16; j++) dhw[0][j] = dhw[1][j];
                 }
             }
         }

@@ -180,19 +180,46 @@ struct Epilogue {
 
 // act(g) and, where wanted, its derivative.  Both activations are g * p with p a sigmoid
 // (of g, or of 2 z for (1 + tanh z) / 2), which keeps its relative accuracy where p is
-// small.  exp and the quotient by their fast forms: a few ulps, of 2^-23, below a bf16
-// result's 2^-9.
+// small.  exp and the reciprocal by their fast forms: a few ulps, of 2^-23, below a bf16
+// result's 2^-9.  z is the sigmoid's argument, dz its derivative.
+__device__ __forceinline__ float fast_rcp(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+template <bool GRAD>
+__device__ __forceinline__ float gate_by(float g, float z, float dz, float& da) {
+    const float p = fast_rcp(1.0f + __expf(-z)), a = g * p;
+    if (GRAD) da = fmaf(a * (1.0f - p), dz, p);
+    return a;
+}
+template <bool GRAD>
+__device__ __forceinline__ void gelu_argument(float g, float& z, float& dz) {
+    const float g2 = g * g;
+    z = 1.5957691216f * g * fmaf(0.044715f, g2, 1.0f);       // 2 sqrt(2/pi)
+    if (GRAD) dz = 1.5957691216f * fmaf(0.134145f, g2, 1.0f);
+}
 template <bool GRAD>
 __device__ __forceinline__ float activate(int act, float g, float& da) {
     float z = g, dz = 1.0f;
+    if (act == 1) gelu_argument<GRAD>(g, z, dz);
+    return gate_by<GRAD>(g, z, dz, da);
+}
+// The same for 32 values in place, the branch on the activation outside.
+template <bool GRAD>
+__device__ __forceinline__ void activate32(int act, float (&g)[32], float* da) {
+    float unused;
     if (act == 1) {
-        const float g2 = g * g;
-        z = 1.5957691216f * g * fmaf(0.044715f, g2, 1.0f);   // 2 sqrt(2/pi)
-        if (GRAD) dz = 1.5957691216f * fmaf(0.134145f, g2, 1.0f);
+#pragma unroll
+        for (int j = 0; j < 32; j++) {
+            float z, dz = 1.0f;
+            gelu_argument<GRAD>(g[j], z, dz);
+            g[j] = gate_by<GRAD>(g[j], z, dz, GRAD ? da[j] : unused);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; j++) g[j] = gate_by<GRAD>(g[j], g[j], 1.0f, GRAD ? da[j] : unused);
     }
-    const float p = __fdividef(1.0f, 1.0f + __expf(-z));
-    if (GRAD) da = fmaf(g * p * (1.0f - p), dz, p);
-    return g * p;
 }
 
 __device__ __forceinline__ uint16_t bf16_bits(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
