@@ -1,22 +1,22 @@
-// Products on the tensor cores of quantised operands (tcgen05.mma.kind::mxf4nvf4, block
-// scales applied by the MMA) and of the bf16 operands of their gradients (kind::f16):
+// Products of few tokens on the tensor cores (tcgen05.mma.kind::mxf4nvf4, block scales
+// applied by the MMA), bound by reading the weight once:
 //
-//   out[t][n] = epilogue( sum_k q[t][k] p[n][k] ),   p: weights, q: tokens.
+//   out[t][n] = epilogue( sum_k q[t][k] p[n][k] ),   p: weights, q: at most TN tokens.
 //
-// tile_kernel: a CTA forms 128 columns n by TN tokens, the weight's rows on the MMA's M
-// side whatever the number of tokens, so that one token costs an MMA of N = 16 and the
-// weight is read once.  Lane i of tensor memory is then column n0 + i of the result and a
-// warp's stores are consecutive.  The gated forms keep two accumulators, gate and up.
+// The weight's rows are the MMA's M side, so that one token costs an MMA of N = 16.  Lane
+// i of tensor memory is then column n0 + i of the result and a warp's stores are consecutive.
+// The gated form keeps two accumulators, gate and up.
 //   * one warp loads stages (128 bytes of each operand's rows along K, and their scale
 //     atoms) by TMA into a ring; out-of-range rows, columns and atoms arrive as zeros;
 //   * one warp copies each stage's scale atoms to tensor memory (tcgen05.cp) and issues its
 //     MMAs; copies and MMAs run in the order they are issued;
 //   * four warps read the accumulators and write the result.
-// Where there are fewer tiles than SMs, a cluster of CTAs splits K; each leaves its sums in
-// its shared memory and adds a share of the columns over all of them in rank order.
+// Two CTAs to an SM, and a cluster of up to eight splits K so that their loads fill the SMs.  Each
+// rank sends its sums for a token to the rank that finishes that token, which adds
+// them in rank order: one cluster barrier after the sends, none after the reads.
 //
 // Every mbarrier wait is bounded (1 s); on a timeout the CTA sets bit 16 of the status
-// word, drains its copies, frees its tensor memory and returns without writing.
+// word, drains its copies, frees its tensor memory and returns; its results are not there.
 #include "fp4_tile.cuh"
 
 namespace nvfp4 {
@@ -25,11 +25,12 @@ namespace {
 
 constexpr int kThreadsTile = 192;                            // 4 epilogue warps, loads, MMAs
 constexpr int kMaxStages = 8;
+constexpr int kTileSmem = 112 * 1024;                        // of a CTA, two to an SM
 
 struct TileParams {
     CUtensorMap p, p2, q, sp, sp2, sq;
     int64_t k;
-    int stages;
+    int stages, log_split;
     Epilogue e;
 };
 
@@ -38,18 +39,21 @@ struct Tile {
     static constexpr int kG = MODE == kPlain ? 1 : 2;        // accumulators
     static constexpr int kP = 128 * kRow, kQ = TN * kRow, kS = atoms(KIND) * kAtom;
     static constexpr int kStage = kG * kP + kQ + (kG + 1) * kS;
+    static constexpr int kRed = kG * TN * 128 * 4;           // sums of all ranks for this rank's tokens
+    // More than 16 KB of them would cost the second CTA of an SM: they take the ring's place,
+    // once a further cluster barrier says that every rank is done with its own.
+    static constexpr bool kOver = kRed > 16 * 1024;
     // tensor memory: accumulators, then the scales of p, p2, q (4 columns an atom)
     static constexpr int kSfCol = kG * TN, kSfW = atoms(KIND) * 4;
     static constexpr int kCols = kSfCol + (kG + 1) * kSfW;
-    static constexpr int kTmem = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-    static int stages() {
-        const int n = (200 * 1024) / kStage;
-        return n > kMaxStages ? kMaxStages : n;
-    }
-    static int smem(int stages) {
-        const int ring = stages * kStage, red = kG * TN * 128 * 4;
-        return (ring > red ? ring : red) + 1024 + 256;
-    }
+    static constexpr int kTmem = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : 256;
+    static constexpr int kOwn = kOver ? 0 : kRed;
+    // stages of a CTA that has half an SM, or a whole one
+    static constexpr int kHalf = (kTileSmem - 1024 - 256 - kOwn) / kStage;
+    static constexpr int kWhole = (2 * kTileSmem - 1024 - 256 - kOwn) / kStage > kMaxStages ? kMaxStages
+                                                                                          : (2 * kTileSmem - 1024 - 256 - kOwn) / kStage;
+    static constexpr int smem(int stages) { return stages * kStage + kOwn + 1024; }
+    static_assert(kHalf >= 2 && (!kOver || kRed <= kHalf * kStage), "shared memory");
 };
 
 // One result column n of token t.  Whole warps call it (the MXFP4 form reduces over the
@@ -58,7 +62,7 @@ template <int MODE>
 __device__ __forceinline__ void emit(const Epilogue& e, int64_t t, int64_t n, float a, float b, float sp, float sp2,
                                      float sq, bool& bad) {
     if (MODE == kPlain) {
-        if (t < e.T && n < e.N) {
+        if (n < e.N) {
             const float v = a * sp * sq;
             if (e.out_f32)
                 static_cast<float*>(e.out)[t * e.ldo + n] = v;
@@ -70,10 +74,10 @@ __device__ __forceinline__ void emit(const Epilogue& e, int64_t t, int64_t n, fl
     float unused;
     const float g = a * sp * sq, u = b * sp2 * sq;
     const uint16_t h = bf16_bits(activate<false>(e.act, g, unused) * u);
-    if (e.out && t < e.T && n < e.N) static_cast<uint16_t*>(e.out)[t * e.ldo + n] = h;
-    if (MODE == kGated && e.h_codes) {
+    if (e.out && n < e.N) static_cast<uint16_t*>(e.out)[t * e.ldo + n] = h;
+    if (e.h_codes) {
         const int lane = threadIdx.x & 31;
-        const bool live = t < e.T && n < e.N;                // N % 32 == 0: the same for a warp
+        const bool live = n < e.N;                           // N % 32 == 0: the same for a warp
         const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, live ? (uint32_t)(h & 0x7FFF) << 16 : 0u), ex = m >> 23;
         const bool finite = ex != 255;
         bad |= !finite;
@@ -85,46 +89,12 @@ __device__ __forceinline__ void emit(const Epilogue& e, int64_t t, int64_t n, fl
         w |= __shfl_xor_sync(0xFFFFFFFFu, w, 2);
         w |= __shfl_xor_sync(0xFFFFFFFFu, w, 4);
         if (live && (lane & 7) == 0) *reinterpret_cast<uint32_t*>(e.h_codes + t * (e.N / 2) + n / 2) = w;
-        if (lane == 0) e.h_sf[swizzle_offset(t, n >> 5, e.h_kpad4)] = (uint8_t)code;   // padding: zero
-    }
-}
-
-// Sixteen tokens t0.. of column n: the gradients of the gated form.
-__device__ __forceinline__ void emit_grad16(const Epilogue& e, int64_t t0, int64_t n, const float (&a)[16],
-                                            const float (&b)[16], float sp, float sp2, float sq) {
-    uint32_t dgw[8], duw[8];
-#pragma unroll
-    for (int i = 0; i < 16; i++) {
-        const int64_t t = t0 + i;
-        const bool live = t < e.T && n < e.N;
-        const float g = a[i] * sp * sq, u = b[i] * sp2 * sq;
-        const float dh = live ? bf16_value(e.dh[t * e.lddh + n]) : 0.0f;
-        float da;
-        const float ag = activate<true>(e.act, g, da);
-        const float dg = live ? dh * u * da : 0.0f, du = live ? dh * ag : 0.0f;
-        if (e.out && live) static_cast<uint16_t*>(e.out)[t * e.ldo + n] = bf16_bits(ag * u);
-        if (e.dgu && t < e.T) {                              // n < fp: fp is a multiple of the tile
-            e.dgu[t * 2 * e.fp + n] = live ? bf16_bits(dg * sp) : (uint16_t)0;
-            e.dgu[t * 2 * e.fp + e.fp + n] = live ? bf16_bits(du * sp2) : (uint16_t)0;
-        }
-        const uint32_t bg = bf16_bits(dg), bu = bf16_bits(du);
-        dgw[i >> 1] = i & 1 ? dgw[i >> 1] | bg << 16 : bg;
-        duw[i >> 1] = i & 1 ? duw[i >> 1] | bu << 16 : bu;
-    }
-    if (e.dgu_t) {
-#pragma unroll
-        for (int j = 0; j < 2; j++) {
-            if (t0 + 8 * j >= e.ldt) continue;               // ldt is a multiple of 8
-            *reinterpret_cast<uint4*>(e.dgu_t + n * e.ldt + t0 + 8 * j) =
-                make_uint4(dgw[4 * j], dgw[4 * j + 1], dgw[4 * j + 2], dgw[4 * j + 3]);
-            *reinterpret_cast<uint4*>(e.dgu_t + (e.fp + n) * e.ldt + t0 + 8 * j) =
-                make_uint4(duw[4 * j], duw[4 * j + 1], duw[4 * j + 2], duw[4 * j + 3]);
-        }
+        if (lane == 0) e.h_sf[swizzle_offset(t, n >> 5, e.h_kpad4)] = (uint8_t)code;   // columns past N: zero
     }
 }
 
 template <int KIND, int MODE, int TN>
-__global__ void __launch_bounds__(kThreadsTile, 1) tile_kernel(const __grid_constant__ TileParams P) {
+__global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_constant__ TileParams P) {
     using C = Tile<KIND, MODE, TN>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 1];
@@ -132,15 +102,16 @@ __global__ void __launch_bounds__(kThreadsTile, 1) tile_kernel(const __grid_cons
     __shared__ uint32_t s_tmem;
     uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
-    const int split = (int)gridDim.x, rank = (int)blockIdx.x;   // the cluster is grid dimension x
-    const int64_t n0 = (int64_t)blockIdx.y * 128, t0 = (int64_t)blockIdx.z * TN;
+    const int lsplit = P.log_split, split = 1 << lsplit, rank = (int)blockIdx.x;   // the cluster is grid dimension x
+    const int stages = P.stages;
+    const int n0 = (int)blockIdx.y * 128;
     const int nst = (int)((P.k + stage_k(KIND) - 1) / stage_k(KIND));
     const int from = (int)((int64_t)nst * rank / split), to = (int)((int64_t)nst * (rank + 1) / split);
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kMaxStages, dbar = empty0 + 8 * kMaxStages;
 
     if (warp == 5) tmem_alloc(smem_u32(&s_tmem), C::kTmem);
     if (tid == 0) {
-        for (int b = 0; b < P.stages; b++) {
+        for (int b = 0; b < stages; b++) {
             mbar_init(full0 + 8 * b, 1);
             mbar_init(empty0 + 8 * b, 1);
         }
@@ -151,7 +122,21 @@ __global__ void __launch_bounds__(kThreadsTile, 1) tile_kernel(const __grid_cons
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    if (split > 1 && !C::kOver) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // may be sent to
     grid_launch_dependents();                                // tensor memory is this CTA's by now
+    if (warp == 4 && elect_one()) {
+        // the weight's first stages to L2 while the kernel before this one ends (a prefetch
+        // changes no value: whatever that kernel still writes goes to the same L2)
+        for (int s = from; s < to && s < from + kMaxStages; s++) {
+            prefetch_2d(&P.p, s * 128, n0);
+            prefetch_3d(&P.sp, 0, s * atoms(KIND), n0 >> 7);
+            if (C::kG == 2) {
+                prefetch_2d(&P.p2, s * 128, n0);
+                prefetch_3d(&P.sp2, 0, s * atoms(KIND), n0 >> 7);
+            }
+        }
+    }
+    __syncwarp();
     grid_dependency_wait();
     const uint32_t tmem = s_tmem;
 
@@ -161,31 +146,27 @@ __global__ void __launch_bounds__(kThreadsTile, 1) tile_kernel(const __grid_cons
         int issued = 0;
         for (int s = from; s < to; s++) {
             const int r = ring.slot;
-            if (issued >= P.stages && !mbar_wait_warp(empty0 + 8 * r, ring.parity ^ 1)) {
+            if (issued >= stages && !mbar_wait_warp(empty0 + 8 * r, ring.parity ^ 1)) {
                 ok = false;
                 break;
             }
             if (elect_one()) {
-                const uint32_t bar = full0 + 8 * r, st = smem_u32(base) + r * C::kStage;
-                const int kc = s * (KIND == kBf16 ? 64 : 128);   // elements of the map: bf16 or bytes
+                const uint32_t bar = full0 + 8 * r, st = smem_u32(base) + r * C::kStage, sf = st + C::kG * C::kP + C::kQ;
                 mbar_expect_tx(bar, C::kStage);
-                tma_load_2d(st, &P.p, kc, (int)n0, bar);
-                if (C::kG == 2) tma_load_2d(st + C::kP, &P.p2, kc, (int)n0, bar);
-                tma_load_2d(st + C::kG * C::kP, &P.q, kc, (int)t0, bar);
-                if (KIND != kBf16) {
-                    const uint32_t sf = st + C::kG * C::kP + C::kQ;
-                    tma_load_3d(sf, &P.sp, 0, s * atoms(KIND), (int)(n0 >> 7), bar);
-                    if (C::kG == 2) tma_load_3d(sf + C::kS, &P.sp2, 0, s * atoms(KIND), (int)(n0 >> 7), bar);
-                    tma_load_3d(sf + C::kG * C::kS, &P.sq, 0, s * atoms(KIND), (int)(t0 >> 7), bar);
-                }
+                tma_load_2d(st, &P.p, s * 128, n0, bar);
+                if (C::kG == 2) tma_load_2d(st + C::kP, &P.p2, s * 128, n0, bar);
+                tma_load_2d(st + C::kG * C::kP, &P.q, s * 128, 0, bar);
+                tma_load_3d(sf, &P.sp, 0, s * atoms(KIND), n0 >> 7, bar);
+                if (C::kG == 2) tma_load_3d(sf + C::kS, &P.sp2, 0, s * atoms(KIND), n0 >> 7, bar);
+                tma_load_3d(sf + C::kG * C::kS, &P.sq, 0, s * atoms(KIND), 0, bar);
             }
             __syncwarp();
-            if (issued < P.stages) issued++;
-            ring.next(P.stages);
+            if (issued < stages) issued++;
+            ring.next(stages);
         }
         // every slot in use landed
-        if (issued < P.stages) ring = Ring{0, 1};            // each used once
-        for (int j = 0; j < issued; j++, ring.next(P.stages))
+        if (issued < stages) ring = Ring{0, 1};          // each used once
+        for (int j = 0; j < issued; j++, ring.next(stages))
             if (!mbar_wait_warp(full0 + 8 * ring.slot, ring.parity ^ 1)) ok = false;
         if (!ok && lane == 0) atomicOr(&s_abort, 1);
     } else if (warp == 5) {
@@ -216,72 +197,81 @@ __global__ void __launch_bounds__(kThreadsTile, 1) tile_kernel(const __grid_cons
                                      (uint32_t)((s - from) | kk), col + g * C::kSfW, col + C::kG * C::kSfW);
                 }
                 mma_commit(empty0 + 8 * r);
+                if (s == to - 1) mma_commit(dbar);
             }
             __syncwarp();
-            ring.next(P.stages);
+            ring.next(stages);
         }
-        if (elect_one()) mma_commit(dbar);                   // after every MMA issued, also on a timeout
-        __syncwarp();
         if (!ok && lane == 0) atomicOr(&s_abort, 1);
+    } else if (!mbar_wait_warp(dbar, 0)) {
+        if (lane == 0) atomicOr(&s_abort, 1);
     }
-    __syncthreads();
-    if (!mbar_wait(dbar, 0)) atomicOr(&s_abort, 1);
     tc_fence_after();
     __syncthreads();
+    const Epilogue& e = P.e;
     const bool ok = s_abort == 0;
+    const int T = (int)e.T, lper = (TN == 16 ? 4 : TN == 32 ? 5 : 6) - lsplit, per = 1 << lper;   // tokens a rank finishes
     bool bad = false;
+    float sp = 1.0f, sp2 = 1.0f, sq = 1.0f;
+    const int64_t n = n0 + 32 * warp + lane;
     if (warp < 4) {
-        const Epilogue& e = P.e;
-        const float sp = scale_or_1(e.s_p), sp2 = C::kG == 2 ? scale_or_1(e.s_p2) : 1.0f, sq = scale_or_1(e.s_q);
-        const int64_t n = n0 + 32 * warp + lane;
-        const uint32_t acc = tmem + ((uint32_t)(32 * warp) << 16);
-        float* red = reinterpret_cast<float*>(base);
-        if (ok)
-#pragma unroll 1
-            for (int c = 0; c < TN; c += 16) {
-                float a[16], b[16];
-                tmem_ld16(acc + c, a);
-                if (C::kG == 2) tmem_ld16(acc + TN + c, b);
-                tmem_wait16(a);
-                if (C::kG == 2) tmem_wait16(b);
-                if (split > 1) {
-#pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        red[(c + i) * 128 + tid] = a[i];
-                        if (C::kG == 2) red[(TN + c + i) * 128 + tid] = b[i];
-                    }
-                } else if (MODE == kGatedGrad) {
-                    emit_grad16(e, t0 + c, n, a, b, sp, sp2, sq);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; i++) emit<MODE>(e, t0 + c + i, n, a[i], C::kG == 2 ? b[i] : 0.0f, sp, sp2, sq, bad);
-                }
-            }
+        sp = scale_or_1(e.s_p);
+        if (C::kG == 2) sp2 = scale_or_1(e.s_p2);
+        sq = scale_or_1(e.s_q);
     }
     if (split > 1) {
-        cluster_barrier();                                   // every rank's sums are in its shared memory
-        if (warp < 4 && ok) {
-            const Epilogue& e = P.e;
-            const float sp = scale_or_1(e.s_p), sp2 = C::kG == 2 ? scale_or_1(e.s_p2) : 1.0f, sq = scale_or_1(e.s_q);
-            const int64_t n = n0 + 32 * warp + lane;
-            const uint32_t mine = smem_u32(base) + 4 * tid;
-#pragma unroll 2
-            for (int c = TN * rank / split; c < TN * (rank + 1) / split; c++) {
-                float a = 0.0f, b = 0.0f;
-                for (int r = 0; r < split; r++) {
-                    const uint32_t from_r = at_rank(mine + c * 512, r);
-                    a += ld_cluster(from_r);
-                    if (C::kG == 2) b += ld_cluster(from_r + TN * 512);
+        if (C::kOver) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // done with the ring
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    const int red_at = C::kOver ? 0 : stages * C::kStage;
+    const uint32_t red = smem_u32(base) + red_at;         // [accumulator][token of this rank][rank][128]
+    if (warp < 4 && ok) {
+        const uint32_t acc = tmem + ((uint32_t)(32 * warp) << 16);
+#pragma unroll 1
+        for (int c = 0; c < TN && c < T; c += 16) {
+            float a[16], b[16];
+            tmem_ld16(acc + c, a);
+            if (C::kG == 2) tmem_ld16(acc + TN + c, b);
+            tmem_wait16(a);
+            if (C::kG == 2) tmem_wait16(b);
+            if (split > 1) {
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    const int t = c + i;
+                    if (t >= T) break;
+                    const uint32_t at = at_rank(red + (uint32_t)((((t & (per - 1)) << lsplit) + rank) * 512 + tid * 4), (uint32_t)(t >> lper));
+                    st_cluster(at, a[i]);
+                    if (C::kG == 2) st_cluster(at + TN * 512, b[i]);
                 }
-                emit<MODE>(e, t0 + c, n, a, b, sp, sp2, sq, bad);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    if (c + i >= T) break;
+                    emit<MODE>(e, c + i, n, a[i], C::kG == 2 ? b[i] : 0.0f, sp, sp2, sq, bad);
+                }
             }
         }
-        cluster_barrier();                                   // read before any rank's shared memory goes
     }
-    if (MODE == kGated && TN < 128 && P.e.h_codes && warp < 4 && rank == 0)    // scale rows of the tile that hold no token
-        for (int r = TN + lane; r < 128; r += 32) P.e.h_sf[swizzle_offset(t0 + r, (n0 >> 5) + warp, P.e.h_kpad4)] = 0;
-    if (tid == 0 && !ok && P.e.status) atomicOr(P.e.status, kStatusTimeout);
-    if (bad && P.e.status) atomicOr(P.e.status, 1);
+    if (split > 1) {
+        cluster_barrier();                                   // every rank's sums are here
+        if (warp < 4 && ok) {
+            const float* mine = reinterpret_cast<const float*>(base + red_at) + tid;
+#pragma unroll 2
+            for (int j = 0; j < per; j++) {
+                if (rank * per + j >= T) break;
+                float a = 0.0f, b = 0.0f;
+                for (int r = 0; r < split; r++) {
+                    a += mine[(j * split + r) * 128];
+                    if (C::kG == 2) b += mine[(TN + j * split + r) * 128];
+                }
+                emit<MODE>(e, rank * per + j, n, a, b, sp, sp2, sq, bad);
+            }
+        }
+    }
+    if (MODE == kGated && e.h_codes && warp < 4 && rank == 0)    // scale rows of the tile that hold no token
+        for (int r = T + lane; r < 128; r += 32) e.h_sf[swizzle_offset(r, (n0 >> 5) + warp, e.h_kpad4)] = 0;
+    if (tid == 0 && !ok && e.status) atomicOr(e.status, kStatusTimeout);
+    if (bad && e.status) atomicOr(e.status, 1);
     tc_fence_before();
     __syncthreads();
     if (warp == 5) tmem_dealloc(tmem, C::kTmem);
@@ -293,18 +283,17 @@ cudaError_t launch_tile(const Product& p, int sms, cudaStream_t s) {
     using C = Tile<KIND, MODE, TN>;
     TileParams P;
     const bool ok = make_operand_map(&P.p, p.p, KIND, p.k, 128) && make_operand_map(&P.q, p.q, KIND, p.k, TN) &&
-                    (C::kG == 1 || make_operand_map(&P.p2, p.p2, KIND, p.k, 128)) &&
-                    (KIND == kBf16 || (make_scale_map(&P.sp, p.p, KIND, p.k) && make_scale_map(&P.sq, p.q, KIND, p.k) &&
-                                       (C::kG == 1 || make_scale_map(&P.sp2, p.p2, KIND, p.k))));
+                    (C::kG == 1 || make_operand_map(&P.p2, p.p2, KIND, p.k, 128)) && make_scale_map(&P.sp, p.p, KIND, p.k) &&
+                    make_scale_map(&P.sq, p.q, KIND, p.k) && (C::kG == 1 || make_scale_map(&P.sp2, p.p2, KIND, p.k));
     if (!ok) return cudaErrorNotSupported;
     P.k = p.k;
     P.e = make_epilogue(p);
     const int nst = (int)((p.k + stage_k(KIND) - 1) / stage_k(KIND));
-    const int64_t tn = (p.p.rows + 127) / 128, tt = (p.q.rows + TN - 1) / TN;
-    int split = 1;
-    if (MODE != kGatedGrad)
-        while (split < 8 && 2 * split * tn * tt <= sms && 2 * split <= nst && 2 * split <= TN) split *= 2;
-    P.stages = C::stages();
+    const int64_t tn = (p.p.rows + 127) / 128;
+    P.log_split = 0;
+    while (P.log_split < 3 && 3 * (tn << P.log_split) <= 2 * sms && (2 << P.log_split) <= nst) P.log_split++;
+    const int split = 1 << P.log_split;
+    P.stages = split == 1 && tn <= sms ? C::kWhole : C::kHalf;
     const int smem = C::smem(P.stages);
     static std::atomic<bool> attr_set[64];
     int dev = 0;
@@ -312,12 +301,12 @@ cudaError_t launch_tile(const Product& p, int sms, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     const auto kernel = tile_kernel<KIND, MODE, TN>;
     if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem(C::kWhole));
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)split, (unsigned)tn, (unsigned)tt);
+    cfg.gridDim = dim3((unsigned)split, (unsigned)tn);
     cfg.blockDim = dim3(kThreadsTile);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = s;
@@ -335,32 +324,24 @@ cudaError_t launch_tile(const Product& p, int sms, cudaStream_t s) {
 
 template <int KIND, int MODE>
 cudaError_t launch_by_tokens(const Product& p, int sms, cudaStream_t s) {
-    // the fewest tokens to a tile that hold all, else 128: an atom's rows start a tile
     if (p.q.rows <= 16) return launch_tile<KIND, MODE, 16>(p, sms, s);
-    if (p.q.rows <= 32) return launch_tile<KIND, MODE, 32>(p, sms, s);
-    if (p.q.rows <= 64) return launch_tile<KIND, MODE, 64>(p, sms, s);
-    return launch_tile<KIND, MODE, 128>(p, sms, s);
-}
-
-template <int KIND>
-cudaError_t launch_by_mode(const Product& p, int sms, cudaStream_t s) {
-    switch (p.mode) {
-        case kPlain: return launch_by_tokens<KIND, kPlain>(p, sms, s);
-        case kGated: return launch_by_tokens<KIND, kGated>(p, sms, s);
-        default: return launch_tile<KIND, kGatedGrad, 128>(p, sms, s);
-    }
+    if (MODE == kGated || p.q.rows <= 32) return launch_tile<KIND, MODE, 32>(p, sms, s);
+    return launch_tile<KIND, kPlain, 64>(p, sms, s);
 }
 
 }  // namespace
 }  // namespace mm
 
+// Up to 64 tokens (gated: 32) the weight is streamed past them; more go to pairs of CTAs.
+// us, here / pairs: plain 32 x 4096 x 4096 6.3 / 8.6, 64 x 4096 x 4096 9.8 / 8.7, 64 x 14336 x 4096
+// 11.5 / 10.6, 64 x 4096 x 14336 14.5 / 16.7, 50 x 1001 x 2080 6.8 / 10.7; gated 32 x 14336 x 4096 15.8 /
+// 19.6, 50 x 1024 x 1024 8.3 / 5.8, 64 x 14336 x 4096 19.5 / 18.8.
 cudaError_t launch_product(const Product& p, int sms, cudaStream_t s) {
-    if (p.q.rows > 128) return launch_pair(p, sms, s);
-    switch (p.kind) {
-        case kNvfp4: return mm::launch_by_mode<kNvfp4>(p, sms, s);
-        case kMxfp4: return mm::launch_by_mode<kMxfp4>(p, sms, s);
-        default: return mm::launch_tile<kBf16, kPlain, 128>(p, sms, s);
-    }
+    const int few = p.kind == kBf16 || p.mode == kGatedGrad ? 0 : p.mode == kPlain ? 64 : 32;
+    if (p.q.rows > few) return launch_pair(p, sms, s);
+    if (p.mode == kPlain)
+        return p.kind == kMxfp4 ? mm::launch_by_tokens<kMxfp4, kPlain>(p, sms, s) : mm::launch_by_tokens<kNvfp4, kPlain>(p, sms, s);
+    return p.kind == kMxfp4 ? mm::launch_by_tokens<kMxfp4, kGated>(p, sms, s) : mm::launch_by_tokens<kNvfp4, kGated>(p, sms, s);
 }
 
 }  // namespace nvfp4

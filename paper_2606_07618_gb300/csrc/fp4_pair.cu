@@ -33,7 +33,7 @@ constexpr int kPairStages = 6;                               // at most
 struct PairParams {
     CUtensorMap p, p2, q, sp, sp2, sq;
     int64_t k;
-    int tiles_t, tiles_n;
+    int tiles_t, tiles_n, split;
     int wide_out, wide_dh, wide_codes;                       // bytes that rows of D or h, dh, codes are aligned to: 32, 16 or fewer
     Epilogue e;
 };
@@ -62,9 +62,9 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
         : "memory");
 }
 // Arrives on this barrier of both CTAs once the MMAs issued so far have finished.
-__device__ __forceinline__ void commit_pair(uint32_t bar) {
+__device__ __forceinline__ void commit_pair(uint32_t bar, uint32_t leader) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((uint16_t)3) : "memory");
+                 ::"r"(bar), "h"((uint16_t)(3u << leader)) : "memory");
 }
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
@@ -121,22 +121,180 @@ __device__ __forceinline__ void put_row(const uint32_t (&w)[W], int wide, uint8_
         constexpr int kCols = 64 / ES;
         const int c = lane % kCols;
         const int64_t col = n + i * 4 / ES + c;
-        if (col < N)
-#pragma unroll 4
-            for (int r = lane / kCols; r < 32; r += 32 / kCols) {
-                if (t0 + r >= T) break;
+        if (col < N) {
+            char* at = static_cast<char*>(out) + ((t0 + lane / kCols) * ld + col) * ES;
+            const int rows = (int)(T - t0 < 32 ? T - t0 : 32);
+#pragma unroll
+            for (int r0 = 0; r0 < 32; r0 += 32 / kCols) {    // all in flight: reads first in the schedule
+                const int r = r0 + lane / kCols;
                 const uint8_t* from = box + r * 64 + (((c * ES >> 4) ^ (r >> 1 & 3)) << 4) + (c * ES & 15);
-                if (ES == 4)
-                    static_cast<uint32_t*>(out)[(t0 + r) * ld + col] = *reinterpret_cast<const uint32_t*>(from);
-                else
-                    static_cast<uint16_t*>(out)[(t0 + r) * ld + col] = *reinterpret_cast<const uint16_t*>(from);
+                if (ES == 4) {
+                    const uint32_t v = *reinterpret_cast<const uint32_t*>(from);
+                    if (r < rows) *reinterpret_cast<uint32_t*>(at) = v;
+                } else {
+                    const uint16_t v = *reinterpret_cast<const uint16_t*>(from);
+                    if (r < rows) *reinterpret_cast<uint16_t*>(at) = v;
+                }
+                at += 32 / kCols * ld * ES;
             }
+        }
         __syncwarp();
     }
 }
 
-template <int KIND, int MODE>
-__global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pair_kernel(const __grid_constant__ PairParams P) {
+// What a warp makes of 32 columns n.. of its rows: lane's row t = tw + lane, tw the warp's first.
+enum { kFirst = 0, kSecond = 1, kAlone = 2 };                // of a run of 64 columns, or 32 alone
+struct Rows {
+    const Epilogue& e;
+    const PairParams& P;
+    uint8_t* box;
+    float sp, sp2, sq;
+    int lane;
+    int64_t tw, t;
+    bool bad;
+    uint32_t codes0[4], code0;                               // MXFP4 form of h: a run's first 32 columns
+
+    __device__ __forceinline__ void plain(const float (&v)[32], int64_t n) const {
+        if (e.out_f32) {
+            uint32_t w[32];
+#pragma unroll
+            for (int j = 0; j < 32; j++) w[j] = __float_as_uint(v[j] * sp * sq);
+            put_row<4, 32>(w, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
+        } else {
+            uint32_t w[16];
+#pragma unroll
+            for (int j = 0; j < 16; j++) w[j] = pack2_bf16(v[2 * j] * sp * sq, v[2 * j + 1] * sp * sq);
+            put_row<2, 16>(w, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
+        }
+    }
+
+    // dh, zero where there is no token or no column
+    __device__ __forceinline__ void load_dh(uint32_t (&d)[16], int64_t n) const {
+        const bool row = t < e.T;
+        const uint16_t* at = e.dh + t * e.lddh + n;
+        if (row && n + 32 <= e.N && P.wide_dh >= 16) {
+            uint4 v[4];
+            if (P.wide_dh == 32) {
+                ld_stream32<false>(at, v[0], v[1]);
+                ld_stream32<false>(at + 16, v[2], v[3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] = ld_stream16<false>(at + 8 * j);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; j++) d[4 * j] = v[j].x, d[4 * j + 1] = v[j].y, d[4 * j + 2] = v[j].z, d[4 * j + 3] = v[j].w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; j++) {
+                const uint32_t lo = row && n + 2 * j < e.N ? at[2 * j] : 0, hi = row && n + 2 * j + 1 < e.N ? at[2 * j + 1] : 0;
+                d[j] = lo | hi << 16;
+            }
+        }
+    }
+
+    // g and u are used up; PART: kFirst or kSecond, or kAlone
+    template <int KIND, int MODE, int PART>
+    __device__ __forceinline__ void gated(float (&g)[32], float (&u)[32], const uint32_t (&dhw)[16], int64_t n) {
+#pragma unroll
+        for (int j = 0; j < 32; j++) {
+            g[j] = g[j] * sp * sq;
+            u[j] = u[j] * sp2 * sq;
+        }
+        uint32_t hw[16];
+        if (MODE == kGated) {
+            activate32<false>(e.act, g, nullptr);
+#pragma unroll
+            for (int j = 0; j < 16; j++) hw[j] = pack2_bf16(g[2 * j] * u[2 * j], g[2 * j + 1] * u[2 * j + 1]);
+        } else {
+            // dh is zero where there is no token or no column, and with it dg and du
+            float da[32];
+            activate32<true>(e.act, g, da);
+            uint32_t gt[16], ut[16];
+#pragma unroll
+            for (int j = 0; j < 16; j++) {
+                const float d0 = bf16lo(dhw[j]), d1 = bf16hi(dhw[j]);
+                hw[j] = pack2_bf16(g[2 * j] * u[2 * j], g[2 * j + 1] * u[2 * j + 1]);
+                g[2 * j] *= d0;
+                g[2 * j + 1] *= d1;
+                ut[j] = pack2_bf16(g[2 * j], g[2 * j + 1]);
+                da[2 * j] *= d0 * u[2 * j];
+                da[2 * j + 1] *= d1 * u[2 * j + 1];
+                gt[j] = pack2_bf16(da[2 * j], da[2 * j + 1]);
+            }
+            if (e.dgu_t) {
+                // two neighbouring tokens of a column in one word: lanes exchange halves
+                const int64_t t2 = tw + (lane & ~1);
+                const bool in = t2 < e.ldt;
+                const uint32_t sel = lane & 1 ? 0x3276 : 0x5410;
+                uint16_t* at = e.dgu_t + (n + (lane & 1)) * e.ldt + t2;
+                uint16_t* at2 = at + e.fp * e.ldt;
+#pragma unroll
+                for (int j = 0; j < 16; j++) {
+                    const uint32_t wg = __byte_perm(gt[j], __shfl_xor_sync(0xFFFFFFFFu, gt[j], 1), sel);
+                    const uint32_t wu = __byte_perm(ut[j], __shfl_xor_sync(0xFFFFFFFFu, ut[j], 1), sel);
+                    if (in) {
+                        *reinterpret_cast<uint32_t*>(at) = wg;
+                        *reinterpret_cast<uint32_t*>(at2) = wu;
+                    }
+                    at += 2 * e.ldt;
+                    at2 += 2 * e.ldt;
+                }
+            }
+            if (e.dgu) {
+                if (KIND == kNvfp4) {                            // times the weights' global scales
+#pragma unroll
+                    for (int j = 0; j < 16; j++) {
+                        gt[j] = pack2_bf16(da[2 * j] * sp, da[2 * j + 1] * sp);
+                        ut[j] = pack2_bf16(g[2 * j] * sp2, g[2 * j + 1] * sp2);
+                    }
+                }
+                put_row<2, 16>(gt, 32, box, e.dgu, 2 * e.fp, n, tw, e.fp, e.T);
+                put_row<2, 16>(ut, 32, box, e.dgu + e.fp, 2 * e.fp, n, tw, e.fp, e.T);
+            }
+        }
+        if (e.out) put_row<2, 16>(hw, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
+        if (MODE == kGated && e.h_codes) {
+            const bool live = t < e.T && n < e.N;    // N is a multiple of 32
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < 16; j++) {
+                if (!live) hw[j] = 0;
+                m = max(m, max(hw[j] << 16 & 0x7FFF0000u, hw[j] & 0x7FFF0000u));
+            }
+            const uint32_t ex = m >> 23;
+            const bool finite = ex != 255;
+            bad |= !finite;
+            const uint32_t code = finite && ex > 2 ? ex - 2 : 0;
+            const float inv = __uint_as_float((254u - code) << 23);
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                u64 x[4];
+#pragma unroll
+                for (int z = 0; z < 4; z++) {
+                    const uint32_t two = finite ? hw[4 * j + z] : hw[4 * j + z] & 0x80008000u;
+                    x[z] = pack2(bf16lo(two) * inv, bf16hi(two) * inv);
+                }
+                w[j] = e2m1x8(x[0], x[1], x[2], x[3]);
+            }
+            uint8_t* at = e.h_codes + t * (e.N / 2) + n / 2;
+            const bool row = (tw & ~127ll) < e.T;                // rows of an atom that hold no token: zero
+            uint8_t* sf = e.h_sf + swizzle_offset(t, n >> 5, e.h_kpad4);
+            if (PART == kAlone || P.wide_codes != 32) {
+                if (live) *reinterpret_cast<uint4*>(at) = word4(w);
+            } else if (PART == kSecond && live) {                // both blocks are there: N is a multiple of 64
+                st32(at - 16, word4(codes0), word4(w));
+            }
+            if (PART == kAlone && row) *sf = (uint8_t)code;
+            if (PART == kSecond && row) *reinterpret_cast<uint16_t*>(sf - 1) = (uint16_t)(code0 | code << 8);
+#pragma unroll
+            for (int j = 0; j < 4; j++) codes0[j] = w[j];
+            code0 = code;
+        }    }
+};
+
+template <int KIND, int MODE, bool SPLIT>
+__global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_constant__ PairParams P) {
     using C = Pair<KIND>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * kPairStages + 4];
@@ -144,9 +302,12 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
     __shared__ uint32_t s_tmem;
     uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
-    const uint32_t rank = cluster_rank();
-    const int nst = (int)((P.k + stage_k(KIND) - 1) / stage_k(KIND));
-    const int ntiles = P.tiles_t * P.tiles_n, step = (int)gridDim.x / 2, first = (int)blockIdx.x / 2;
+    // the CTA's place in its pair, the pair's in its cluster (which splits K), the pair's stages of K
+    const uint32_t crank = cluster_rank(), rank = crank & 1, pair = SPLIT ? crank >> 1 : 0, leader = crank & ~1u;
+    const int split = SPLIT ? P.split : 1;
+    const int all = (int)((P.k + stage_k(KIND) - 1) / stage_k(KIND));
+    const int k0 = SPLIT ? (int)((int64_t)all * pair / split) : 0, nst = SPLIT ? (int)((int64_t)all * (pair + 1) / split) - k0 : all;
+    const int ntiles = P.tiles_t * P.tiles_n, step = (int)gridDim.x / (2 * split), first = (int)blockIdx.x / (2 * split);
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kPairStages, accf0 = empty0 + 8 * kPairStages,
                    drained0 = accf0 + 16;
 
@@ -177,7 +338,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
 
     if (warp == kEpiWarps) {
         Ring ring;
-        const uint32_t leader_full = at_rank(full0, 0);
+        const uint32_t leader_full = at_rank(full0, leader);
         bool ok = true;
         int issued = 0;
         uint32_t swap = 0;                                   // gated: gate and up change places with the accumulators
@@ -194,7 +355,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                 if (elect_one()) {
                     const uint32_t st = smem_u32(base) + r * C::kStage, bar = leader_full + 8 * r;
                     if (rank == 0) mbar_expect_tx(full0 + 8 * r, 2 * C::kStage);
-                    const int x = kc * (KIND == kBf16 ? 64 : 128);
+                    const int x = (k0 + kc) * (KIND == kBf16 ? 64 : 128);
                     tma_load_2d_pair(st, &P.q, x, t0, bar);
                     if (MODE == kPlain)
                         tma_load_2d_pair(st + C::kOp, &P.p, x, tn * 256 + (int)rank * 128, bar);
@@ -202,7 +363,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                         tma_load_2d_pair(st + C::kOp, rank == swap ? &P.p : &P.p2, x, tn * 128, bar);
                     if (KIND != kBf16) {
                         const uint32_t sf = st + 2 * C::kOp;
-                        const int a = kc * atoms(KIND);
+                        const int a = (k0 + kc) * atoms(KIND);
                         tma_load_3d_pair(sf, &P.sq, 0, a, t0 >> 7, bar);
                         if (MODE == kPlain) {
                             tma_load_3d_pair(sf + C::kS, &P.sp, 0, a, 2 * tn, bar);
@@ -246,7 +407,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                         cp_atom<2>(tmem + C::kSf + 16 + 8 * a, atom_desc(sf + C::kS + a * kAtom));
                         cp_atom<2>(tmem + C::kSf + 16 + 8 * a + 4, atom_desc(sf + 2 * C::kS + a * kAtom));
                     }
-                    const int left = (int)((P.k - (int64_t)kc * stage_k(KIND) + mma_k(KIND) - 1) / mma_k(KIND));
+                    const int left = (int)((P.k - (int64_t)(k0 + kc) * stage_k(KIND) + mma_k(KIND) - 1) / mma_k(KIND));
 #pragma unroll
                     for (int kk = 0; kk < 4; kk++) {
                         if (kk >= left) break;
@@ -255,8 +416,8 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                                      KIND == kMxfp4 ? id | sf_id(2 * (kk & 1)) : id, (uint32_t)(kc | kk), tmem + C::kSf + 4 * a,
                                      tmem + C::kSf + 16 + 8 * a);
                     }
-                    commit_pair(empty0 + 8 * r);
-                    if (kc == nst - 1) commit_pair(accf0 + 8 * (it & 1));
+                    commit_pair(empty0 + 8 * r, leader);
+                    if (kc == nst - 1) commit_pair(accf0 + 8 * (it & 1), leader);
                 }
                 __syncwarp();
                 ring.next(C::kStages);
@@ -265,16 +426,17 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
         if (!ok && lane == 0) atomicOr(&s_abort, 1);
     } else if (warp < kEpiWarps) {
         const Epilogue& e = P.e;
-        const float sp = scale_or_1(e.s_p), sp2 = MODE != kPlain ? scale_or_1(e.s_p2) : 1.0f, sq = scale_or_1(e.s_q);
         const int half = warp >> 2, q = warp & 3;
-        uint8_t* box = base + C::kStages * C::kStage + warp * kBox;
-        const uint32_t leader_drained = at_rank(drained0, 0);
-        bool bad = false;
+        Rows rows{e, P, base + C::kStages * C::kStage + warp * kBox, scale_or_1(e.s_p), MODE != kPlain ? scale_or_1(e.s_p2) : 1.0f,
+                  scale_or_1(e.s_q), lane};
+        rows.bad = false;
+        const uint32_t leader_drained = at_rank(drained0, leader);
         int it = 0;
         for (int i = first; i < ntiles; i += step, it++) {
             int tt, tn;
             tile_at(i, P.tiles_t, P.tiles_n, tt, tn);
-            const int64_t tw = (int64_t)tt * 256 + rank * 128 + 32 * q, t = tw + lane;   // the warp's first row, this lane's
+            rows.tw = (int64_t)tt * 256 + rank * 128 + 32 * q;
+            rows.t = rows.tw + lane;
             const int b = it & 1;
             const bool overlap = KIND != kBf16 && half == 1 - b;     // this warp reads the overlapping columns
             auto release = [&]() {
@@ -283,43 +445,29 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                 if (lane == 0) arrive_at(leader_drained + 8 * b);
             };
             if (!overlap) release();                         // done with the tile before
-            // dh of this tile, asked for before its accumulators are waited for
             uint32_t dhw[2][16];
-            if (MODE == kGatedGrad) {
-#pragma unroll
-                for (int c = 0; c < 2; c++) {
-                    const int64_t n = (int64_t)tn * 128 + 64 * half + 32 * c;
-                    const bool row = t < e.T;
-                    const uint16_t* at = e.dh + t * e.lddh + n;
-                    if (row && n + 32 <= e.N && P.wide_dh >= 16) {
-                        uint4 d[4];
-                        if (P.wide_dh == 32) {
-                            ld_stream32<false>(at, d[0], d[1]);
-                            ld_stream32<false>(at + 16, d[2], d[3]);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 4; j++) d[j] = ld_stream16<false>(at + 8 * j);
-                        }
-#pragma unroll
-                        for (int j = 0; j < 4; j++)
-                            dhw[c][4 * j] = d[j].x, dhw[c][4 * j + 1] = d[j].y, dhw[c][4 * j + 2] = d[j].z, dhw[c][4 * j + 3] = d[j].w;
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 16; j++) {
-                            const uint32_t lo = row && n + 2 * j < e.N ? at[2 * j] : 0, hi = row && n + 2 * j + 1 < e.N ? at[2 * j + 1] : 0;
-                            dhw[c][j] = lo | hi << 16;
-                        }
-                    }
-                }
+            const int64_t n0 = MODE == kPlain ? (int64_t)tn * 256 : (int64_t)tn * 128 + 64 * half;
+            if (MODE == kGatedGrad && !SPLIT) {              // asked for before the accumulators are waited for
+                rows.load_dh(dhw[0], n0);
+                rows.load_dh(dhw[1], n0 + 32);
             }
-            if (!mbar_wait(accf0 + 8 * b, (it >> 1) & 1)) {
-                atomicOr(&s_abort, 1);
+            if (!mbar_wait_warp(accf0 + 8 * b, (it >> 1) & 1)) {
+                if (lane == 0) atomicOr(&s_abort, 1);
                 break;
             }
             tc_fence_after();
-            __syncwarp();
             const uint32_t acc = tmem + b * C::kAcc1 + ((uint32_t)(32 * q) << 16);
-            if (MODE == kPlain) {
+            if (SPLIT) {                                     // sums to shared memory, in the ring's place: all its stages are read
+                float* red = reinterpret_cast<float*>(base) + 32 * q + lane;
+#pragma unroll 1
+                for (int c = 0; c < 128; c += 32) {
+                    float v[32];
+                    tmem_ld32(acc + 128 * half + c, v);
+                    tmem_wait32(v);
+#pragma unroll
+                    for (int j = 0; j < 32; j++) red[(128 * half + c + j) * 128] = v[j];
+                }
+            } else if (MODE == kPlain) {
                 // two halves of 64 columns, the overlapping one first
 #pragma unroll 1
                 for (int c = 0; c < 2; c++) {
@@ -330,25 +478,12 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                     tmem_wait32(v[0]);
                     tmem_wait32(v[1]);
                     if (overlap && c == 0) release();
-#pragma unroll
-                    for (int z = 0; z < 2; z++) {
-                        const int64_t n = (int64_t)tn * 256 + col + 32 * z;
-                        if (e.out_f32) {
-                            uint32_t w[32];
-#pragma unroll
-                            for (int j = 0; j < 32; j++) w[j] = __float_as_uint(v[z][j] * sp * sq);
-                            put_row<4, 32>(w, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
-                        } else {
-                            uint32_t w[16];
-#pragma unroll
-                            for (int j = 0; j < 16; j++) w[j] = pack2_bf16(v[z][2 * j] * sp * sq, v[z][2 * j + 1] * sp * sq);
-                            put_row<2, 16>(w, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
-                        }
-                    }
+                    rows.plain(v[0], n0 + col);
+                    rows.plain(v[1], n0 + col + 32);
                 }
             } else {
                 // The up columns (the overlapping ones are theirs in either accumulator) to registers, then 32
-                // gate columns at a time; rolled, for the instruction cache.
+                // gate columns at a time.
                 const uint32_t up = acc + (b == 0 ? 128 : 0) + 64 * half, gate = acc + (b == 0 ? 0 : 128) + 64 * half;
                 float u[2][32];
                 tmem_ld32(up, u[0]);
@@ -356,117 +491,68 @@ __global__ void __launch_bounds__(kThreadsPair, 1) __cluster_dims__(2, 1, 1) pai
                 tmem_wait32(u[0]);
                 tmem_wait32(u[1]);
                 if (overlap) release();
-                uint32_t codes0[4], code0 = 0;               // of the first 32 columns
-#pragma unroll 1
-                for (int c = 0; c < 2; c++) {
-                    const int64_t n = (int64_t)tn * 128 + 64 * half + 32 * c;
-                    float g[32];
-                    tmem_ld32(gate + 32 * c, g);
+                float g[32];
+                if (MODE == kGated) {
+                    tmem_ld32(gate, g);
                     tmem_wait32(g);
+                    rows.gated<KIND, MODE, kFirst>(g, u[0], dhw[0], n0);
+                    tmem_ld32(gate + 32, g);
+                    tmem_wait32(g);
+                    rows.gated<KIND, MODE, kSecond>(g, u[1], dhw[1], n0 + 32);
+                } else {
+                    // rolled, for the instruction cache (two copies: 311 us where this takes 223)
+#pragma unroll 1
+                    for (int c = 0; c < 2; c++) {
+                        tmem_ld32(gate + 32 * c, g);
+                        tmem_wait32(g);
+                        rows.gated<KIND, MODE, kAlone>(g, u[0], dhw[0], n0 + 32 * c);
 #pragma unroll
-                    for (int j = 0; j < 32; j++) {
-                        g[j] = g[j] * sp * sq;
-                        u[0][j] = u[0][j] * sp2 * sq;
-                    }
-                    uint32_t hw[16];
-                    if (MODE == kGated) {
-                        activate32<false>(e.act, g, nullptr);
-#pragma unroll
-                        for (int j = 0; j < 16; j++) hw[j] = pack2_bf16(g[2 * j] * u[0][2 * j], g[2 * j + 1] * u[0][2 * j + 1]);
-                    } else {
-                        // dh is zero where there is no token or no column, and with it dg and du
-                        float da[32];
-                        activate32<true>(e.act, g, da);
-                        uint32_t gt[16], ut[16];
-#pragma unroll
-                        for (int j = 0; j < 16; j++) {
-                            const float d0 = bf16lo(dhw[0][j]), d1 = bf16hi(dhw[0][j]);
-                            hw[j] = pack2_bf16(g[2 * j] * u[0][2 * j], g[2 * j + 1] * u[0][2 * j + 1]);
-                            g[2 * j] *= d0;
-                            g[2 * j + 1] *= d1;
-                            ut[j] = pack2_bf16(g[2 * j], g[2 * j + 1]);
-                            da[2 * j] *= d0 * u[0][2 * j];
-                            da[2 * j + 1] *= d1 * u[0][2 * j + 1];
-                            gt[j] = pack2_bf16(da[2 * j], da[2 * j + 1]);
-                        }
-                        if (e.dgu_t) {
-                            // two neighbouring tokens of a column in one word: lanes exchange halves
-                            const int64_t t2 = tw + (lane & ~1);
-                            const bool in = t2 < e.ldt;
-                            const uint32_t sel = lane & 1 ? 0x3276 : 0x5410;
-                            uint16_t* at = e.dgu_t + (n + (lane & 1)) * e.ldt + t2;
-                            uint16_t* at2 = at + e.fp * e.ldt;
-#pragma unroll
-                            for (int j = 0; j < 16; j++) {
-                                const uint32_t wg = __byte_perm(gt[j], __shfl_xor_sync(0xFFFFFFFFu, gt[j], 1), sel);
-                                const uint32_t wu = __byte_perm(ut[j], __shfl_xor_sync(0xFFFFFFFFu, ut[j], 1), sel);
-                                if (in) {
-                                    *reinterpret_cast<uint32_t*>(at) = wg;
-                                    *reinterpret_cast<uint32_t*>(at2) = wu;
-                                }
-                                at += 2 * e.ldt;
-                                at2 += 2 * e.ldt;
-                            }
-                        }
-                        if (e.dgu) {
-                            if (KIND == kNvfp4) {            // times the weights' global scales
-#pragma unroll
-                                for (int j = 0; j < 16; j++) {
-                                    gt[j] = pack2_bf16(da[2 * j] * sp, da[2 * j + 1] * sp);
-                                    ut[j] = pack2_bf16(g[2 * j] * sp2, g[2 * j + 1] * sp2);
-                                }
-                            }
-                            put_row<2, 16>(gt, 32, box, e.dgu, 2 * e.fp, n, tw, e.fp, e.T);
-                            put_row<2, 16>(ut, 32, box, e.dgu + e.fp, 2 * e.fp, n, tw, e.fp, e.T);
-                        }
-                    }
-                    if (e.out) put_row<2, 16>(hw, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
-                    if (MODE == kGated && e.h_codes) {
-                        const bool live = t < e.T && n < e.N;    // N is a multiple of 32
-                        uint32_t m = 0;
-#pragma unroll
-                        for (int j = 0; j < 16; j++) {
-                            if (!live) hw[j] = 0;
-                            m = max(m, max(hw[j] << 16 & 0x7FFF0000u, hw[j] & 0x7FFF0000u));
-                        }
-                        const uint32_t ex = m >> 23;
-                        const bool finite = ex != 255;
-                        bad |= !finite;
-                        const uint32_t code = finite && ex > 2 ? ex - 2 : 0;
-                        const float inv = __uint_as_float((254u - code) << 23);
-                        uint32_t w[4];
-#pragma unroll
-                        for (int j = 0; j < 4; j++) {
-                            u64 x[4];
-#pragma unroll
-                            for (int z = 0; z < 4; z++) {
-                                const uint32_t two = finite ? hw[4 * j + z] : hw[4 * j + z] & 0x80008000u;
-                                x[z] = pack2(bf16lo(two) * inv, bf16hi(two) * inv);
-                            }
-                            w[j] = e2m1x8(x[0], x[1], x[2], x[3]);
-                        }
-                        uint8_t* at = e.h_codes + t * (e.N / 2) + n / 2;
-                        if (P.wide_codes == 32) {            // both blocks are there: N is a multiple of 64
-                            if (c == 1 && live) st32(at - 16, word4(codes0), word4(w));
-                        } else if (live) {
-                            *reinterpret_cast<uint4*>(at) = word4(w);
-                        }
-                        if (c == 1 && (tw & ~127ll) < e.T)   // rows of an atom that hold no token: zero
-                            *reinterpret_cast<uint16_t*>(e.h_sf + swizzle_offset(t, (n >> 5) - 1, e.h_kpad4)) =
-                                (uint16_t)(code0 | code << 8);
-#pragma unroll
-                        for (int j = 0; j < 4; j++) codes0[j] = w[j];
-                        code0 = code;
-                    }
-#pragma unroll
-                    for (int j = 0; j < 32; j++) u[0][j] = u[1][j];
-                    if (MODE == kGatedGrad)
+                        for (int j = 0; j < 32; j++) u[0][j] = u[1][j];
 #pragma unroll
                         for (int j = 0; j < 16; j++) dhw[0][j] = dhw[1][j];
+                    }
                 }
             }
         }
-        if (bad && e.status) atomicOr(e.status, 1);
+        if (SPLIT) {
+            // one tile to a cluster: each pair finishes its share of the columns, adding all
+            // pairs' sums in their order
+            cluster_barrier();
+            int tt, tn;
+            tile_at(first, P.tiles_t, P.tiles_n, tt, tn);
+            const uint32_t mine = smem_u32(base) + 4 * (32 * q + lane);
+            auto sum32 = [&](int col, float (&v)[32]) {
+#pragma unroll
+                for (int j = 0; j < 32; j++) v[j] = 0.0f;
+                for (int r = 0; r < split; r++) {
+                    const uint32_t at = at_rank(mine + col * 512, 2 * r + rank);
+#pragma unroll
+                    for (int j = 0; j < 32; j++) v[j] += ld_cluster(at + 512 * j);
+                }
+            };
+            const int width = (MODE == kPlain ? 256 : 128) / split, from = width * (int)pair + (half * width / 2 & ~31);
+            const int to = half == 0 ? width * (int)pair + (width / 2 < 32 ? 32 : width / 2) : width * (int)(pair + 1);
+            if (half == 0 || width >= 64)
+#pragma unroll 1
+                for (int c = from; c < to; c += 32) {
+                    float g[32], u[32];
+                    sum32(c, g);
+                    if (MODE == kPlain) {
+                        rows.plain(g, (int64_t)tn * 256 + c);
+                    } else {
+                        uint32_t dhw[16];
+                        const int64_t n = (int64_t)tn * 128 + c;
+                        if (MODE == kGatedGrad) rows.load_dh(dhw, n);
+                        sum32(128 + c, u);
+                        rows.gated<KIND, MODE, kAlone>(g, u, dhw, n);
+                    }
+                }
+        }
+        if (rows.bad && e.status) atomicOr(e.status, 1);
+    }
+    if (SPLIT && warp >= kEpiWarps) {
+        __syncwarp();
+        cluster_barrier();
     }
     tc_fence_before();
     __syncthreads();
@@ -482,8 +568,8 @@ int row_alignment(const void* p, int64_t stride_bytes) {
     return bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 1;
 }
 
-template <int KIND, int MODE>
-cudaError_t launch_pair_as(const Product& p, int sms, cudaStream_t s) {
+template <int KIND, int MODE, bool SPLIT>
+cudaError_t launch_pair_as(const Product& p, int split, int sms, cudaStream_t s) {
     using C = Pair<KIND>;
     PairParams P = {};
     const bool ok = make_operand_map(&P.p, p.p, KIND, p.k, 128) && make_operand_map(&P.q, p.q, KIND, p.k, 128) &&
@@ -501,7 +587,7 @@ cudaError_t launch_pair_as(const Product& p, int sms, cudaStream_t s) {
     P.tiles_n = (int)((p.p.rows + width - 1) / width);
     const int64_t tiles = (int64_t)P.tiles_t * P.tiles_n;
     if (tiles >= 1ll << 30) return cudaErrorNotSupported;
-    const auto kernel = pair_kernel<KIND, MODE>;
+    const auto kernel = pair_kernel<KIND, MODE, SPLIT>;
     static std::atomic<bool> attr_set[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -511,16 +597,49 @@ cudaError_t launch_pair_as(const Product& p, int sms, cudaStream_t s) {
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
-    const int64_t pairs = tiles < sms / 2 ? tiles : sms / 2;
-    return launch_dependent_smem(kernel, 2 * pairs, kThreadsPair, C::kSmem, s, P);
+    P.split = split;
+    const int64_t pairs = SPLIT ? tiles * split : tiles < sms / 2 ? tiles : sms / 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * pairs));
+    cfg.blockDim = dim3(kThreadsPair);
+    cfg.dynamicSmemBytes = (size_t)C::kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)(2 * split);
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, P);
+}
+
+// Pairs that share a tile's K.  Adding up costs some 5 us (256 x 4096 x 14336, 56 stages: 21.6 us,
+// 17.2 by two, where a half of the stages take 9.5), so K has to be long; and clusters of four or eight
+// whole SMs have to find room (at most 36 and 15 on a GB300: 16 of eight ran one after
+// the others, 29 us).
+int pairs_of_a_tile(const Product& p, int sms) {
+    const int64_t width = p.mode == kPlain ? 256 : 128;
+    const int64_t tiles = ((p.q.rows + 255) / 256) * ((p.p.rows + width - 1) / width);
+    const int64_t nst = (p.k + stage_k(p.kind) - 1) / stage_k(p.kind);
+    if (nst < 32 || 4 * tiles > sms - 8) return 1;
+    return 8 * tiles <= sms - 32 ? 4 : 2;
+}
+
+template <int KIND, int MODE>
+cudaError_t launch_pair_mode(const Product& p, int sms, cudaStream_t s) {
+    const int split = pairs_of_a_tile(p, sms);
+    return split > 1 ? launch_pair_as<KIND, MODE, true>(p, split, sms, s) : launch_pair_as<KIND, MODE, false>(p, 1, sms, s);
 }
 
 template <int KIND>
-cudaError_t launch_pair_mode(const Product& p, int sms, cudaStream_t s) {
+cudaError_t launch_pair_kind(const Product& p, int sms, cudaStream_t s) {
     switch (p.mode) {
-        case kPlain: return launch_pair_as<KIND, kPlain>(p, sms, s);
-        case kGated: return launch_pair_as<KIND, kGated>(p, sms, s);
-        default: return launch_pair_as<KIND, kGatedGrad>(p, sms, s);
+        case kPlain: return launch_pair_mode<KIND, kPlain>(p, sms, s);
+        case kGated: return launch_pair_mode<KIND, kGated>(p, sms, s);
+        default: return launch_pair_mode<KIND, kGatedGrad>(p, sms, s);
     }
 }
 
@@ -529,9 +648,9 @@ cudaError_t launch_pair_mode(const Product& p, int sms, cudaStream_t s) {
 
 cudaError_t launch_pair(const Product& p, int sms, cudaStream_t s) {
     switch (p.kind) {
-        case kNvfp4: return mm::launch_pair_mode<kNvfp4>(p, sms, s);
-        case kMxfp4: return mm::launch_pair_mode<kMxfp4>(p, sms, s);
-        default: return mm::launch_pair_as<kBf16, kPlain>(p, sms, s);
+        case kNvfp4: return mm::launch_pair_kind<kNvfp4>(p, sms, s);
+        case kMxfp4: return mm::launch_pair_kind<kMxfp4>(p, sms, s);
+        default: return mm::launch_pair_mode<kBf16, kPlain>(p, sms, s);
     }
 }
 
