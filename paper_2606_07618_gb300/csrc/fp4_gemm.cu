@@ -124,19 +124,6 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
     tc_fence_after();
     if (split > 1 && !C::kOver) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // may be sent to
     grid_launch_dependents();                                // tensor memory is this CTA's by now
-    if (warp == 4 && elect_one()) {
-        // the weight's first stages to L2 while the kernel before this one ends (a prefetch
-        // changes no value: whatever that kernel still writes goes to the same L2)
-        for (int s = from; s < to && s < from + kMaxStages; s++) {
-            prefetch_2d(&P.p, s * 128, n0);
-            prefetch_3d(&P.sp, 0, s * atoms(KIND), n0 >> 7);
-            if (C::kG == 2) {
-                prefetch_2d(&P.p2, s * 128, n0);
-                prefetch_3d(&P.sp2, 0, s * atoms(KIND), n0 >> 7);
-            }
-        }
-    }
-    __syncwarp();
     grid_dependency_wait();
     const uint32_t tmem = s_tmem;
 
@@ -290,10 +277,15 @@ cudaError_t launch_tile(const Product& p, int sms, cudaStream_t s) {
     P.e = make_epilogue(p);
     const int nst = (int)((p.k + stage_k(KIND) - 1) / stage_k(KIND));
     const int64_t tn = (p.p.rows + 127) / 128;
+    // Few tiles: up to eight CTAs to a tile, two to an SM, so that some 150 to 300 load (us with
+    // 8 / 4 / 2 at most: 1 x 4096 x 4096 4.2 / 4.3 / 5.1, 1 x 4096 x 14336 7.0 / 8.6 / 11.4, gated 1 x
+    // 4096 x 4096 4.9 / 5.6 / 7.3).  Past half the SMs a CTA to a tile with the whole SM's ring: gated
+    // 16 x 14336 x 4096 14.7, where two with half a ring take 15.5; 64 x 14336 x 4096 11.3 / 16.6.
     P.log_split = 0;
-    while (P.log_split < 3 && 3 * (tn << P.log_split) <= 2 * sms && (2 << P.log_split) <= nst) P.log_split++;
+    const bool share = 2 * tn <= sms;
+    while (share && P.log_split < 3 && 5 * (tn << P.log_split) < 6 * sms && (2 << P.log_split) <= nst) P.log_split++;
     const int split = 1 << P.log_split;
-    P.stages = split == 1 && tn <= sms ? C::kWhole : C::kHalf;
+    P.stages = share || tn > sms ? C::kHalf : C::kWhole;
     const int smem = C::smem(P.stages);
     static std::atomic<bool> attr_set[64];
     int dev = 0;
