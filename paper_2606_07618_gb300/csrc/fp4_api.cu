@@ -85,15 +85,20 @@ nvfp4_status result(cudaError_t e) {
 }
 
 // A bf16 product for a gradient: out[t][n] = S sum_k q[t][k] p[n][k].
+// With out2, q holds two matrices of qrows rows, the second from row2 on, and their products go to out and out2.
 cudaError_t grad_product(const void* p, int64_t prows, int64_t ldp, const void* q, int64_t qrows, int64_t ldq,
-                         int64_t k, const float* S, void* out, int64_t ldo, int* status, int sms, cudaStream_t s) {
+                         int64_t k, const float* S, void* out, int64_t ldo, int* status, int sms, cudaStream_t s,
+                         void* out2 = nullptr, int64_t row2 = 0) {
     Product g = {};
     g.kind = kBf16;
     g.mode = kPlain;
     g.p = dense(p, S, prows, ldp);
-    g.q = dense(q, nullptr, qrows, ldq);
+    g.q = dense(q, nullptr, out2 ? row2 + qrows : qrows, ldq);
     g.k = k;
     g.out = out;
+    g.out2 = out2;
+    g.row2 = row2;
+    g.rows1 = qrows;
     g.ldo = ldo;
     g.status = status;
     return launch_product(g, sms, s);
@@ -255,12 +260,12 @@ nvfp4_status fp4_matmul_backward(fp4_format fmt, const fp4_operand* a, const fp4
             q = dp;
             ldq = g.ldn;
         }
-        if (e == cudaSuccess) e = launch_expand_t(mx, b->codes, b->sf, n, k, g.ldn, bt, g.ldn, s);
+        if (e == cudaSuccess) e = launch_expand_t(mx, b->codes, b->sf, nullptr, nullptr, n, k, g.ldn, bt, g.ldn, s);
         if (e == cudaSuccess) e = grad_product(bt, k, g.ldn, q, m, ldq, n, b->S, dA, ldda, status_dev, sms, s);
     }
     if (dB && e == cudaSuccess) {
         e = launch_transpose_bf16(dD, m, n, lddd, dt, g.ldm, s);
-        if (e == cudaSuccess) e = launch_expand_t(mx, a->codes, a->sf, m, k, g.ldm, at, g.ldm, s);
+        if (e == cudaSuccess) e = launch_expand_t(mx, a->codes, a->sf, nullptr, nullptr, m, k, g.ldm, at, g.ldm, s);
         if (e == cudaSuccess) e = grad_product(at, k, g.ldm, dt, n, g.ldm, m, a->S, dB, lddb, status_dev, sms, s);
     }
     return result(e);
@@ -369,17 +374,14 @@ nvfp4_status fp4_gated_ff_backward(fp4_format fmt, fp4_activation act, const fp4
     p.status = status_dev;
     cudaError_t e = launch_product(p, sms, s);
     if (d_x && e == cudaSuccess) {
-        e = launch_expand_t(mx, w_gate->codes, w_gate->sf, f, d, g.fp, wt, 2 * g.fp, s);
-        if (e == cudaSuccess) e = launch_expand_t(mx, w_up->codes, w_up->sf, f, d, g.fp, wt + g.fp, 2 * g.fp, s);
+        e = launch_expand_t(mx, w_gate->codes, w_gate->sf, w_up->codes, w_up->sf, f, d, g.fp, wt, 2 * g.fp, s);
         if (e == cudaSuccess)
             e = grad_product(wt, d, 2 * g.fp, dgu, t, 2 * g.fp, 2 * g.fp, nullptr, d_x, lddx, status_dev, sms, s);
     }
     if (d_gate && e == cudaSuccess) {
-        e = launch_expand_t(mx, x->codes, x->sf, t, d, g.ldt, xt, g.ldt, s);
+        e = launch_expand_t(mx, x->codes, x->sf, nullptr, nullptr, t, d, g.ldt, xt, g.ldt, s);
         if (e == cudaSuccess)
-            e = grad_product(xt, d, g.ldt, dgut, f, g.ldt, t, x->S, d_gate, lddw, status_dev, sms, s);
-        if (e == cudaSuccess)
-            e = grad_product(xt, d, g.ldt, dgut + g.fp * g.ldt, f, g.ldt, t, x->S, d_up, lddw, status_dev, sms, s);
+            e = grad_product(xt, d, g.ldt, dgut, f, g.ldt, t, x->S, d_gate, lddw, status_dev, sms, s, d_up, g.fp);
     }
     return result(e);
 }

@@ -12,9 +12,10 @@ cudaError_t launch_mxfp4_quantize(const void* x, int dtype, int64_t rows, int64_
 cudaError_t launch_mxfp4_dequantize(const uint8_t* codes, const uint8_t* sf, int swizzled, int64_t rows, int64_t cols,
                                     void* out, int dtype, int sms, cudaStream_t s);
 // out[c][r] = bf16(q * s) of a quantised matrix (without S), exact; rows r in [rows,
-// rows_out) are written as zero.  out row stride ld (a multiple of 8), 16-byte aligned.
-cudaError_t launch_expand_t(int mx, const uint8_t* codes, const uint8_t* sf, int64_t rows, int64_t cols,
-                            int64_t rows_out, void* out, int64_t ld, cudaStream_t s);
+// rows_out) are written as zero.  A second matrix of the same size (or null) goes to
+// out[c][rows_out + r].  out row stride ld (a multiple of 8), 16-byte aligned.
+cudaError_t launch_expand_t(int mx, const uint8_t* codes, const uint8_t* sf, const uint8_t* codes2, const uint8_t* sf2,
+                            int64_t rows, int64_t cols, int64_t rows_out, void* out, int64_t ld, cudaStream_t s);
 // out[c][r] = in[r][c], bf16; in row stride ldi, out row stride ldo (a multiple of 8).
 cudaError_t launch_transpose_bf16(const void* in, int64_t rows, int64_t cols, int64_t ldi, void* out, int64_t ldo,
                                   cudaStream_t s);
@@ -40,6 +41,8 @@ struct Product {
     Operand p, p2, q;      // p2: the up projection's weight (gated modes)
     int64_t k;
     void* out;             // plain: D; gated modes: h (bf16) or null
+    void* out2;            // plain: rows from row2 on go here (their own matrix, the size of the first), or null
+    int64_t row2, rows1;   // the first one's rows; row2 is a multiple of 128
     int out_f32;
     int64_t ldo;
     uint8_t *h_codes, *h_sf;   // gated: h in MXFP4, or null

@@ -155,16 +155,20 @@ struct Rows {
     uint32_t codes0[4], code0;                               // MXFP4 form of h: a run's first 32 columns
 
     __device__ __forceinline__ void plain(const float (&v)[32], int64_t n) const {
+        // a warp's 32 rows are of one matrix: row2 is a multiple of 128
+        const bool other = e.out2 && tw >= e.row2;
+        void* out = other ? e.out2 : e.out;
+        const int64_t t0 = other ? tw - e.row2 : tw;
         if (e.out_f32) {
             uint32_t w[32];
 #pragma unroll
             for (int j = 0; j < 32; j++) w[j] = __float_as_uint(v[j] * sp * sq);
-            put_row<4, 32>(w, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
+            put_row<4, 32>(w, P.wide_out, box, out, e.ldo, n, t0, e.N, e.rows1);
         } else {
             uint32_t w[16];
 #pragma unroll
             for (int j = 0; j < 16; j++) w[j] = pack2_bf16(v[2 * j] * sp * sq, v[2 * j + 1] * sp * sq);
-            put_row<2, 16>(w, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
+            put_row<2, 16>(w, P.wide_out, box, out, e.ldo, n, t0, e.N, e.rows1);
         }
     }
 
@@ -580,6 +584,7 @@ cudaError_t launch_pair_as(const Product& p, int split, int sms, cudaStream_t s)
     P.k = p.k;
     P.e = make_epilogue(p);
     P.wide_out = row_alignment(p.out, p.ldo * (p.out_f32 ? 4 : 2));
+    if (p.out2 && row_alignment(p.out2, 0) < P.wide_out) P.wide_out = row_alignment(p.out2, 0);
     P.wide_dh = row_alignment(p.dh, p.lddh * 2);
     P.wide_codes = row_alignment(p.h_codes, p.p.rows / 2);
     const int64_t width = MODE == kPlain ? 256 : 128;

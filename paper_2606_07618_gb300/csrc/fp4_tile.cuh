@@ -170,6 +170,8 @@ struct Epilogue {
     int64_t T, N;                  // rows (tokens) and columns of the result
     const float *s_p, *s_p2, *s_q; // global scales or null
     void* out;                     // D, or h (bf16) or null
+    void* out2;                    // rows from row2 on (pairs of CTAs, plain) or null
+    int64_t row2, rows1;
     int out_f32;
     int64_t ldo;
     uint8_t *h_codes, *h_sf;
@@ -266,6 +268,9 @@ inline Epilogue make_epilogue(const Product& p) {
     e.s_p2 = p.p2.S;
     e.s_q = p.q.S;
     e.out = p.out;
+    e.out2 = p.out2;
+    e.row2 = p.row2;
+    e.rows1 = p.out2 ? p.rows1 : p.q.rows;
     e.out_f32 = p.out_f32;
     e.ldo = p.ldo;
     e.h_codes = p.h_codes;
