@@ -375,6 +375,8 @@ def mx_swizzled_bytes(rows: int, cols: int) -> int:
 def _rows(t, what: str) -> int:
     """Row stride of a 2-d tensor whose rows are contiguous."""
     rows, cols = t.shape
+    if t.is_contiguous():
+        return cols
     ld, one = t.stride()
     if one != 1 and cols > 1:
         raise ValueError(f"{what}: a 2-d tensor with contiguous rows is wanted")

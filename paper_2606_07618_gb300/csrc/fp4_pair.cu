@@ -66,8 +66,11 @@ __device__ __forceinline__ void commit_pair(uint32_t bar, uint32_t leader) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar), "h"((uint16_t)(3u << leader)) : "memory");
 }
+// Arrival at another CTA's barrier.  What it says is about tensor memory, ordered by the
+// tcgen05 fence before it; a release at cluster scope would wait for this thread's stores to
+// global memory too (1300 to 2400 cycles a tile, in which the next one's MMAs stood still).
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 // Tile number -> token and column tile.  Eight token tiles are walked for each column tile, so
 // that the tiles in flight at one time cover a near-square of the result.
