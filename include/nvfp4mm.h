@@ -83,6 +83,14 @@ nvfp4_status fp4_matmul(fp4_format fmt, const fp4_operand* a, const fp4_operand*
                         void* D, nvfp4_dtype out_dt, int64_t ldd, int* status_dev, void* stream);
 
 /*
+ * Self-test of the products' bounded waits (failure detection): fp4_matmul whose waits for its
+ * operands are made to give up after their limit, by barriers that expect one arrival too many.
+ * status_dev (required) gets bit 16, D is not written and the CUDA context stays usable.
+ */
+nvfp4_status fp4_selftest_wait_timeout(fp4_format fmt, const fp4_operand* a, const fp4_operand* b, int64_t m, int64_t n,
+                                       int64_t k, void* D, nvfp4_dtype out_dt, int64_t ldd, int* status_dev, void* stream);
+
+/*
  * Gradients of fp4_matmul with respect to the values of its operands, from dD:
  *   dA = dD B [m, k],  dB = dD^T A [n, k],
  * all bf16 with row strides lddd, ldda, lddb; either of dA and dB may be NULL.  The

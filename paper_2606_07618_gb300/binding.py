@@ -101,6 +101,7 @@ def lib() -> ctypes.CDLL:
         L.mxfp4_quantize.argtypes = [p, i, i64, i64, i64, p, p, p, p, p]
         L.mxfp4_dequantize.argtypes = [p, p, i, i64, i64, p, i, p]
         L.fp4_matmul.argtypes = [i, op, op, i64, i64, i64, p, i, i64, p, p]
+        L.fp4_selftest_wait_timeout.argtypes = L.fp4_matmul.argtypes
         L.fp4_matmul_backward_workspace.argtypes, L.fp4_matmul_backward_workspace.restype = [i64, i64, i64], sz
         L.fp4_matmul_backward.argtypes = [i, op, op, i64, i64, i64, p, i64, p, i64, p, i64, p, p, sz, p]
         L.fp4_gated_ff.argtypes = [i, i, op, op, op, i64, i64, i64, p, i64, p, p, p, p]
@@ -108,8 +109,8 @@ def lib() -> ctypes.CDLL:
         L.fp4_gated_ff_backward_workspace.restype = sz
         L.fp4_gated_ff_backward.argtypes = [i, i, op, op, op, i64, i64, i64, p, i64, p, i64, p, p, i64, p, i64, p, p, sz,
                                             p]
-        for fn in ("mxfp4_quantize", "mxfp4_dequantize", "fp4_matmul", "fp4_matmul_backward", "fp4_gated_ff",
-                   "fp4_gated_ff_backward"):
+        for fn in ("mxfp4_quantize", "mxfp4_dequantize", "fp4_matmul", "fp4_selftest_wait_timeout", "fp4_matmul_backward",
+                   "fp4_gated_ff", "fp4_gated_ff_backward"):
             getattr(L, fn).restype = i
         for fn in ("nvfp4_global_scale", "nvfp4_global_scale_noalloc", "scalesweep_quantize", "absmax_quantize",
                    "four_over_six_quantize", "nvfp4_dequantize", "scalesweep_quantize_dynamic",
@@ -424,17 +425,26 @@ def mxfp4_dequantize(codes, sf, layout: int, rows: int, cols: int, out, stream=N
     _check("mxfp4_dequantize", rc)
 
 
-def fp4_matmul(fmt: int, a, b, out, status=None, stream=None):
-    """out [m, n] (bf16 or fp32) = A B^T; a = (codes [m, k/2], swizzled scales, S or None), b likewise [n, k/2]."""
+def _matmul(fn: str, fmt: int, a, b, out, status, stream):
     oa, m, k = _operand(a, fmt, "a")
     ob, n, kb = _operand(b, fmt, "b")
     if k != kb:
-        raise ValueError(f"fp4_matmul: operands of {k} and {kb} columns")
+        raise ValueError(f"{fn}: operands of {k} and {kb} columns")
     if out.shape != (m, n):
         raise ValueError(f"out: shape {(m, n)} is wanted, not {tuple(out.shape)}")
-    rc = (_lib or lib()).fp4_matmul(fmt, oa, ob, m, n, k, out.data_ptr(), _dtype(out), _rows(out, "out"), _ptr(status),
+    rc = getattr(_lib or lib(), fn)(fmt, oa, ob, m, n, k, out.data_ptr(), _dtype(out), _rows(out, "out"), _ptr(status),
                                     _stream(stream))
-    _check("fp4_matmul", rc)
+    _check(fn, rc)
+
+
+def fp4_matmul(fmt: int, a, b, out, status=None, stream=None):
+    """out [m, n] (bf16 or fp32) = A B^T; a = (codes [m, k/2], swizzled scales, S or None), b likewise [n, k/2]."""
+    _matmul("fp4_matmul", fmt, a, b, out, status, stream)
+
+
+def fp4_selftest_wait_timeout(fmt: int, a, b, out, status, stream=None):
+    """fp4_matmul whose waits for its operands run out (status bit 16, out not written).  See nvfp4mm.h."""
+    _matmul("fp4_selftest_wait_timeout", fmt, a, b, out, status, stream)
 
 
 def fp4_matmul_backward_workspace(m: int, n: int, k: int) -> int:

@@ -186,8 +186,11 @@ nvfp4_status mxfp4_dequantize(const uint8_t* codes, const uint8_t* sf, nvfp4_sf_
                                           static_cast<cudaStream_t>(stream)));
 }
 
-nvfp4_status fp4_matmul(fp4_format fmt, const fp4_operand* a, const fp4_operand* b, int64_t m, int64_t n, int64_t k,
-                        void* D, nvfp4_dtype out_dt, int64_t ldd, int* status_dev, void* stream) {
+}  // extern "C"
+
+namespace {
+nvfp4_status matmul_common(fp4_format fmt, const fp4_operand* a, const fp4_operand* b, int64_t m, int64_t n, int64_t k,
+                           void* D, nvfp4_dtype out_dt, int64_t ldd, int* status_dev, int starve, void* stream) {
     nvfp4_status st;
     if (out_dt != NVFP4_IN_BF16 && out_dt != NVFP4_IN_F32) return NVFP4_ERR_INVALID_ARG;
     if ((st = check_format(fmt, k)) != NVFP4_OK || (st = check_rows(m)) != NVFP4_OK || (st = check_rows(n)) != NVFP4_OK)
@@ -214,7 +217,22 @@ nvfp4_status fp4_matmul(fp4_format fmt, const fp4_operand* a, const fp4_operand*
     p.out_f32 = out_dt == NVFP4_IN_F32;
     p.ldo = ldd;
     p.status = status_dev;
+    p.starve = starve;
     return result(launch_product(p, sms, static_cast<cudaStream_t>(stream)));
+}
+}  // namespace
+
+extern "C" {
+
+nvfp4_status fp4_matmul(fp4_format fmt, const fp4_operand* a, const fp4_operand* b, int64_t m, int64_t n, int64_t k,
+                        void* D, nvfp4_dtype out_dt, int64_t ldd, int* status_dev, void* stream) {
+    return matmul_common(fmt, a, b, m, n, k, D, out_dt, ldd, status_dev, 0, stream);
+}
+
+nvfp4_status fp4_selftest_wait_timeout(fp4_format fmt, const fp4_operand* a, const fp4_operand* b, int64_t m, int64_t n,
+                                       int64_t k, void* D, nvfp4_dtype out_dt, int64_t ldd, int* status_dev, void* stream) {
+    if (!status_dev) return NVFP4_ERR_INVALID_ARG;
+    return matmul_common(fmt, a, b, m, n, k, D, out_dt, ldd, status_dev, 1, stream);
 }
 
 size_t fp4_matmul_backward_workspace(int64_t m, int64_t n, int64_t k) {

@@ -30,7 +30,7 @@ constexpr int kTileSmem = 112 * 1024;                        // of a CTA, two to
 struct TileParams {
     CUtensorMap p, p2, q, sp, sp2, sq;
     int64_t k;
-    int stages, log_split;
+    int stages, log_split, starve;
     Epilogue e;
 };
 
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
     if (warp == 5) tmem_alloc(smem_u32(&s_tmem), C::kTmem);
     if (tid == 0) {
         for (int b = 0; b < stages; b++) {
-            mbar_init(full0 + 8 * b, 1);
+            mbar_init(full0 + 8 * b, 1 + P.starve);
             mbar_init(empty0 + 8 * b, 1);
         }
         mbar_init(dbar, 1);
@@ -154,7 +154,10 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
         // every slot in use landed
         if (issued < stages) ring = Ring{0, 1};          // each used once
         for (int j = 0; j < issued; j++, ring.next(stages))
-            if (!mbar_wait_warp(full0 + 8 * ring.slot, ring.parity ^ 1)) ok = false;
+            if (!mbar_wait_warp(full0 + 8 * ring.slot, ring.parity ^ 1)) {
+                ok = false;
+                break;
+            }
         if (!ok && lane == 0) atomicOr(&s_abort, 1);
     } else if (warp == 5) {
         constexpr uint32_t id = idesc(KIND, 128, TN);
@@ -196,7 +199,7 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
     tc_fence_after();
     __syncthreads();
     const Epilogue& e = P.e;
-    const bool ok = s_abort == 0;
+    bool ok = s_abort == 0;
     const int T = (int)e.T, lper = (TN == 16 ? 4 : TN == 32 ? 5 : 6) - lsplit, per = 1 << lper;   // tokens a rank finishes
     bool bad = false;
     float sp = 1.0f, sp2 = 1.0f, sq = 1.0f;
@@ -240,7 +243,11 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
         }
     }
     if (split > 1) {
-        cluster_barrier();                                   // every rank's sums are here
+        // every rank's sums are here, or the word that one has none
+        if (!ok && tid < split) st_cluster(at_rank(smem_u32(&s_abort), tid), 1);
+        __syncwarp();
+        cluster_barrier();
+        ok = *reinterpret_cast<volatile int*>(&s_abort) == 0;
         if (warp < 4 && ok) {
             const float* mine = reinterpret_cast<const float*>(base + red_at) + tid;
 #pragma unroll 2
@@ -274,6 +281,7 @@ cudaError_t launch_tile(const Product& p, int sms, cudaStream_t s) {
                     make_scale_map(&P.sq, p.q, KIND, p.k) && (C::kG == 1 || make_scale_map(&P.sp2, p.p2, KIND, p.k));
     if (!ok) return cudaErrorNotSupported;
     P.k = p.k;
+    P.starve = p.starve;
     P.e = make_epilogue(p);
     const int nst = (int)((p.k + stage_k(KIND) - 1) / stage_k(KIND));
     const int64_t tn = (p.p.rows + 127) / 128;

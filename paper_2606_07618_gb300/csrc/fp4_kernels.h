@@ -52,6 +52,7 @@ struct Product {
     void* dgu_t;           // gated grad: [2 fp][ldt] bf16: dg, du transposed, or null
     int64_t fp, ldt;
     int* status;
+    int starve;            // 1: the waits for the operands run out (self-test)
 };
 cudaError_t launch_product(const Product& p, int sms, cudaStream_t s);
 // ---- fp4_pair.cu: the same for many tokens

@@ -33,7 +33,7 @@ constexpr int kPairStages = 6;                               // at most
 struct PairParams {
     CUtensorMap p, p2, q, sp, sp2, sq;
     int64_t k;
-    int tiles_t, tiles_n, split;
+    int tiles_t, tiles_n, split, starve;
     int wide_out, wide_dh, wide_codes;                       // bytes that rows of D or h, dh, codes are aligned to: 32, 16 or fewer
     Epilogue e;
 };
@@ -297,7 +297,8 @@ struct Rows {
 #pragma unroll
             for (int j = 0; j < 4; j++) codes0[j] = w[j];
             code0 = code;
-        }    }
+        }
+    }
 };
 
 template <int KIND, int MODE, bool SPLIT>
@@ -320,7 +321,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
 
     if (tid == 0) {
         for (int b = 0; b < C::kStages; b++) {
-            mbar_init(full0 + 8 * b, 1);
+            mbar_init(full0 + 8 * b, 1 + P.starve);
             mbar_init(empty0 + 8 * b, 1);
         }
         mbar_init(accf0, 1);
@@ -386,9 +387,16 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                 ring.next(C::kStages);
             }
         }
-        // every slot in use read, hence landed
+        // Every slot in use read, hence landed.  After a timeout the leader, whose barriers count both
+        // CTAs' copies, waits for those instead (the other CTA stays for the last cluster barrier).
         if (issued < C::kStages) ring = Ring{0, 1};          // each used once
-        for (int j = 0; ok && j < issued; j++, ring.next(C::kStages)) ok = mbar_wait_warp(empty0 + 8 * ring.slot, ring.parity ^ 1);
+        const bool landed = !ok;
+        if (!landed || rank == 0)
+            for (int j = 0; j < issued; j++, ring.next(C::kStages))
+                if (!mbar_wait_warp((landed ? full0 : empty0) + 8 * ring.slot, ring.parity ^ 1)) {
+                    ok = false;
+                    break;
+                }
         if (!ok && lane == 0) atomicOr(&s_abort, 1);
     } else if (warp == kEpiWarps + 1 && rank == 0) {
         constexpr uint32_t id = idesc(KIND, 256, 256);
@@ -437,6 +445,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
         Rows rows{e, P, base + C::kStages * C::kStage + warp * kBox, scale_or_1(e.s_p), MODE != kPlain ? scale_or_1(e.s_p2) : 1.0f,
                   scale_or_1(e.s_q), lane};
         rows.bad = false;
+        bool lost = false;                                   // a wait ran out
         const uint32_t leader_drained = at_rank(drained0, leader);
         int it = 0;
         for (int i = first; i < ntiles; i += step, it++) {
@@ -460,6 +469,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
             }
             if (!mbar_wait_warp(accf0 + 8 * b, (it >> 1) & 1)) {
                 if (lane == 0) atomicOr(&s_abort, 1);
+                lost = true;
                 break;
             }
             tc_fence_after();
@@ -523,8 +533,11 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
         }
         if (SPLIT) {
             // one tile to a cluster: each pair finishes its share of the columns, adding all
-            // pairs' sums in their order
+            // pairs' sums in their order; none does after a timeout anywhere in the cluster
+            if (lost && lane < 2 * split) st_cluster(at_rank(smem_u32(&s_abort), lane), 1);
+            __syncwarp();
             cluster_barrier();
+            const bool whole = *reinterpret_cast<volatile int*>(&s_abort) == 0;
             int tt, tn;
             tile_at(first, P.tiles_t, P.tiles_n, tt, tn);
             const uint32_t mine = smem_u32(base) + 4 * (32 * q + lane);
@@ -539,7 +552,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
             };
             const int width = (MODE == kPlain ? 256 : 128) / split, from = width * (int)pair + (half * width / 2 & ~31);
             const int to = half == 0 ? width * (int)pair + (width / 2 < 32 ? 32 : width / 2) : width * (int)(pair + 1);
-            if (half == 0 || width >= 64)
+            if (whole && (half == 0 || width >= 64))
 #pragma unroll 1
                 for (int c = from; c < to; c += 32) {
                     float g[32], u[32];
@@ -606,6 +619,7 @@ cudaError_t launch_pair_as(const Product& p, int split, int sms, cudaStream_t s)
         if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
     P.split = split;
+    P.starve = p.starve;
     const int64_t pairs = SPLIT ? tiles * split : tiles < sms / 2 ? tiles : sms / 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * pairs));

@@ -27,7 +27,7 @@ def test_header_and_exports(B):
     names = re.findall(r"^(?:nvfp4_status|size_t)\s+([a-z0-9_]+)\s*\(", src, re.M)
     assert sorted(names) == sorted(["mxfp4_quantize", "mxfp4_dequantize", "fp4_matmul", "fp4_matmul_backward_workspace",
                                     "fp4_matmul_backward", "fp4_gated_ff", "fp4_gated_ff_backward_workspace",
-                                    "fp4_gated_ff_backward"])
+                                    "fp4_gated_ff_backward", "fp4_selftest_wait_timeout"])
     for n in names:
         assert hasattr(B.lib(), n), n
 
@@ -69,6 +69,8 @@ def test_matmul_refusals(B):
     assert mm(D=FAKE + 0x2000001) == ALIGNMENT and mm(dt=1, D=FAKE + 0x2000002) == ALIGNMENT
     assert mm(D=FAKE) == INVALID                                   # over A's codes
     assert mm(m=2 ** 40) == RANGE and mm(k=2 ** 31) == RANGE and mm(n=2 ** 20, ld=2 ** 62) == RANGE
+    assert L.fp4_selftest_wait_timeout(0, _op(B), _op(B, FAKE + 0x1000000, FAKE + 0x1800000), 4, 8, 64, FAKE + 0x2000000, 0, 8,
+                                       None, None) == INVALID           # its status word is required
     w = L.fp4_matmul_backward_workspace(4, 8, 64)
     assert w > 0 and L.fp4_matmul_backward_workspace(0, 8, 64) == 0 and L.fp4_matmul_backward_workspace(-1, 8, 64) == 0
     bw = lambda dD=FAKE + 0x2000000, dA=FAKE + 0x2100000, dB=FAKE + 0x2200000, ws=FAKE + 0x3000000, wsb=w, ldd=8, lda=64: \

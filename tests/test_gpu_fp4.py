@@ -480,3 +480,19 @@ def test_many_calls_back_to_back(B):
     torch.cuda.synchronize()
     for a, b, D in outs:
         near(D, a.v @ b.v.T, sum_bound(a.v, b.v, 512))
+
+
+# one CTA to a tile, a cluster of them, pairs over several tiles, pairs that split K
+@pytest.mark.parametrize("m,n,k", [(3, 10000, 512), (3, 256, 4096), (300, 600, 512), (200, 256, 8192)])
+def test_waits_that_run_out_are_reported(B, m, n, k):
+    """The status word says so, the output is untouched and the next call is right."""
+    a, b = Held(m, k, R.NV, 1), Held(n, k, R.NV, 2)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    D = torch.full((m, n), 7.0, device=DEV)
+    B.fp4_selftest_wait_timeout(R.NV, a.op, b.op, D, st)
+    torch.cuda.synchronize()
+    assert st.item() == 16 and bool((D == 7.0).all())
+    st.zero_()
+    B.fp4_matmul(R.NV, a.op, b.op, D, st)
+    near(D, a.v @ b.v.T, sum_bound(a.v, b.v, k))
+    assert st.item() == 0
