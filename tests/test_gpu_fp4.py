@@ -482,6 +482,94 @@ def test_many_calls_back_to_back(B):
         near(D, a.v @ b.v.T, sum_bound(a.v, b.v, 512))
 
 
+# ------------------------------------------------------------------ long contractions, split over pairs of CTAs
+@pytest.mark.parametrize("fmt", [R.NV, R.MX])
+@pytest.mark.parametrize("m,n,k", [(65, 129, 8224), (300, 1000, 8192), (257, 4100, 8960), (512, 4864, 8192)])
+def test_matmul_long_contraction(B, fmt, m, n, k):
+    a, b = Held(m, k, fmt, 5), Held(n, k, fmt, 6)
+    for out in (torch.float32, torch.bfloat16):
+        D, check = guarded(m, n, out)
+        B.fp4_matmul(fmt, a.op, b.op, D)
+        want = a.v @ b.v.T
+        near(D, want, sum_bound(a.v, b.v, k) + (H * np.abs(want) if out == torch.bfloat16 else 0))
+        check()
+
+
+@pytest.mark.parametrize("fmt", [R.NV, R.MX])
+@pytest.mark.parametrize("t,f,d", [(70, 192, 8224), (300, 416, 8192), (260, 2080, 8192)])
+def test_gated_long_contraction(B, fmt, t, f, d):
+    x, wg, wu = gated_operands(t, f, d, fmt)
+    h, check = guarded(t, f, torch.bfloat16)
+    codes = torch.full((t, f // 2), 0xAA, dtype=torch.uint8, device=DEV)
+    sf = torch.full((B.mx_swizzled_bytes(t, f),), 0xAA, dtype=torch.uint8, device=DEV)
+    B.fp4_gated_ff(fmt, 0, x.op, wg.op, wu.op, h, codes, sf)
+    want, bound, *_ = gated_bounds(0, x.v, wg.v, wu.v, d)
+    near(h, want, bound + H * (np.abs(want) + bound) + 2.0 ** -133)
+    check()
+    qc, _, qs, _ = quantised(B, h)
+    assert torch.equal(codes, qc) and torch.equal(sf, qs)
+
+
+@pytest.mark.parametrize("t,f,d", [(40, 1100, 8224), (2100, 72, 96)])
+def test_gated_backward_long_sums(B, t, f, d):
+    """Recomputed sums over d, sums over 2 f for d_x and over t for the weights, each past 32 stages of K."""
+    x, wg, wu = gated_operands(t, f, d, R.NV)
+    dh = bf16(np.random.default_rng(4).standard_normal((t, f)))
+    ws = torch.empty(B.fp4_gated_ff_backward_workspace(t, f, d), dtype=torch.uint8, device=DEV)
+    out = [guarded(r, d, torch.bfloat16) for r in (t, f, f)]
+    B.fp4_gated_ff_backward(R.NV, 0, x.op, wg.op, wu.op, dh.to(DEV), *(o[0] for o in out), None, ws)
+    for (got, check), (want, bound) in zip(out, grad_bounds(0, x.v, wg.v, wu.v, dh.double().numpy(), d)):
+        near(got, want, bound)
+        check()
+
+
+# ------------------------------------------------------------------ offsets past 32 bits
+def test_offsets_past_32_bits_in_the_result(B):
+    m = n = 66000                                                # 4.4e9 elements
+    a, b = Held(m, 32, R.MX, 1), Held(n, 32, R.MX, 2)
+    D = torch.empty(m, n, dtype=torch.bfloat16, device=DEV)
+    B.fp4_matmul(R.MX, a.op, b.op, D)
+    for r in (0, 1, 33000, 65279, 65280, m - 1):
+        want = a.v[r:r + 1] @ b.v.T
+        near(D[r:r + 1], want, 36 * U * (np.abs(a.v[r:r + 1]) @ np.abs(b.v).T) + H * np.abs(want))
+
+
+def test_offsets_past_32_bits_in_a_weight(B):
+    n, k = 4300000, 2048                                         # 4.4e9 bytes of codes
+    g = torch.Generator(device=DEV).manual_seed(1)
+    codes = torch.randint(0, 256, (n, k // 2), dtype=torch.uint8, device=DEV, generator=g)
+    sf = torch.randint(124, 131, (B.mx_swizzled_bytes(n, k),), dtype=torch.uint8, device=DEV, generator=g)
+    for m in (1, 130):
+        a = Held(m, k, R.MX, 3)
+        D = torch.empty(m, n, device=DEV)
+        B.fp4_matmul(R.MX, a.op, (codes, sf, None), D)
+        for r0 in (0, n // 2 // 128 * 128, (n - 1) // 128 * 128):
+            rows = min(128, n - r0)
+            kb = k // 32
+            r, c = np.meshgrid(np.arange(rows), np.arange(kb), indexing="ij")
+            at = (r0 // 128 * (kb // 4) + c // 4) * 512 + (r % 32) * 16 + r // 32 * 4 + c % 4
+            v = R.values(codes[r0:r0 + rows].cpu().numpy(), sf[torch.from_numpy(at).to(DEV)].cpu().numpy(), R.MX)
+            near(D[:, r0:r0 + rows], a.v @ v.T, sum_bound(a.v, v, k))
+
+
+def test_offsets_past_32_bits_in_quantisation(B):
+    rows, cols = 270000, 65536                                   # 1.8e10 elements: past a launch's 2^30 segments
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device=DEV)
+    at = [0, 1, 65535, 131071, 262143, 262144, 262145, rows - 1]
+    x[at] = torch.randn(len(at), cols, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV)
+    codes = torch.full((rows, cols // 2), 0xAA, dtype=torch.uint8, device=DEV)
+    sf = torch.full((rows, cols // 32), 0xAA, dtype=torch.uint8, device=DEV)
+    B.mxfp4_quantize(x, codes, sf)
+    wc, ws = R.mxfp4(host(x[at]))
+    assert np.array_equal(codes[at].cpu().numpy(), wc) and np.array_equal(sf[at].cpu().numpy(), ws)
+    others = [2, 100000, 262143 - 7, 262150]
+    assert not bool(codes[others].any()) and not bool(sf[others].any())
+    del x
+    out = torch.empty(rows, cols, dtype=torch.bfloat16, device=DEV)
+    B.mxfp4_dequantize(codes, sf, B.NVFP4_SF_LINEAR, rows, cols, out)
+    assert np.array_equal(host(out[at]), R.values(wc, ws, R.MX)) and not bool(out[others].any())
+
+
 # one CTA to a tile, a cluster of them, pairs over several tiles, pairs that split K
 @pytest.mark.parametrize("m,n,k", [(3, 10000, 512), (3, 256, 4096), (300, 600, 512), (200, 256, 8192)])
 def test_waits_that_run_out_are_reported(B, m, n, k):
