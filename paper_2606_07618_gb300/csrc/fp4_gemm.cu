@@ -332,12 +332,12 @@ cudaError_t launch_by_tokens(const Product& p, int sms, cudaStream_t s) {
 }  // namespace
 }  // namespace mm
 
-// Up to 64 tokens (gated: 32) the weight is streamed past them; more go to pairs of CTAs.
-// us, here / pairs: plain 32 x 4096 x 4096 6.3 / 8.6, 64 x 4096 x 4096 9.8 / 8.7, 64 x 14336 x 4096
-// 11.5 / 10.6, 64 x 4096 x 14336 14.5 / 16.7, 50 x 1001 x 2080 6.8 / 10.7; gated 32 x 14336 x 4096 15.8 /
-// 19.6, 50 x 1024 x 1024 8.3 / 5.8, 64 x 14336 x 4096 19.5 / 18.8.
+// Up to 32 tokens the weight is streamed past them, up to 64 where K is long; more go to pairs of
+// CTAs.  us, here / pairs: 32 x 4096 x 4096 6.2 / 8.4, gated 32 x 14336 x 4096 15.9 / 19.6; 64 x 1024 x
+// 1024 7.8 / 5.1, 64 x 4096 x 4096 9.4 / 8.4, 64 x 4096 x 14336 12.7 / 16.7, gated 64 x 2048 x 2048
+// 11.1 / 6.8.
 cudaError_t launch_product(const Product& p, int sms, cudaStream_t s) {
-    const int few = p.kind == kBf16 || p.mode == kGatedGrad ? 0 : p.mode == kPlain ? 64 : 32;
+    const int few = p.kind == kBf16 || p.mode == kGatedGrad ? 0 : p.mode == kPlain && p.k >= 8192 ? 64 : 32;
     if (p.q.rows > few) return launch_pair(p, sms, s);
     if (p.mode == kPlain)
         return p.kind == kMxfp4 ? mm::launch_by_tokens<kMxfp4, kPlain>(p, sms, s) : mm::launch_by_tokens<kNvfp4, kPlain>(p, sms, s);

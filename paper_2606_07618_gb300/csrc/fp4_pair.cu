@@ -91,13 +91,29 @@ __device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+__device__ __forceinline__ void st_shared16(uint32_t at, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+template <int ES>
+__device__ __forceinline__ uint32_t ld_shared(uint32_t at) {
+    uint32_t v;
+    if (ES == 4) {
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    } else {
+        uint16_t h;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at) : "memory");
+        v = h;
+    }
+    return v;
+}
+
 // W words (64 or 128 bytes) of this lane's row t0 + lane, columns n.. of a result with N columns
 // and T rows.  Rows aligned to 32 bytes go out as whole sectors, a lane's own (no staging:
 // TMA stores of boxes waited behind the loads in the SM's TMA queue, 7.2 us a tile of K = 4096 where
 // this takes 5.9).  Other rows, and a ragged last chunk, pass through the warp's 2 KB of
 // shared memory and go out by elements, a row's consecutive ones to consecutive lanes.
 template <int ES, int W>
-__device__ __forceinline__ void put_row(const uint32_t (&w)[W], int wide, uint8_t* box, void* out, int64_t ld, int64_t n,
+__device__ __forceinline__ void put_row(const uint32_t (&w)[W], int wide, uint32_t box, void* out, int64_t ld, int64_t n,
                                         int64_t t0, int64_t N, int64_t T) {
     const int lane = threadIdx.x & 31;
     if (n >= N || t0 >= T) return;                           // the same for the warp
@@ -119,29 +135,28 @@ __device__ __forceinline__ void put_row(const uint32_t (&w)[W], int wide, uint8_
     for (int i = 0; i < W; i += 16) {                        // 32 rows of 64 bytes, 16-byte parts swapped against conflicts
         __syncwarp();
 #pragma unroll
-        for (int c = 0; c < 4; c++) *reinterpret_cast<uint4*>(box + lane * 64 + ((c ^ (lane >> 1 & 3)) << 4)) = word4(w + i + 4 * c);
+        for (int c = 0; c < 4; c++) st_shared16(box + lane * 64 + ((c ^ (lane >> 1 & 3)) << 4), word4(w + i + 4 * c));
         __syncwarp();
-        constexpr int kCols = 64 / ES;
+        constexpr int kCols = 64 / ES, kSteps = kCols;       // rows at a time: 32 / kCols
         const int c = lane % kCols;
         const int64_t col = n + i * 4 / ES + c;
-        if (col < N) {
-            char* at = static_cast<char*>(out) + ((t0 + lane / kCols) * ld + col) * ES;
-            const int rows = (int)(T - t0 < 32 ? T - t0 : 32);
+        const int rows = (int)(T - t0 < 32 ? T - t0 : 32);
+        uint32_t v[kSteps];                                  // all read before the first is stored
 #pragma unroll
-            for (int r0 = 0; r0 < 32; r0 += 32 / kCols) {    // all in flight: reads first in the schedule
-                const int r = r0 + lane / kCols;
-                const uint8_t* from = box + r * 64 + (((c * ES >> 4) ^ (r >> 1 & 3)) << 4) + (c * ES & 15);
-                if (ES == 4) {
-                    const uint32_t v = *reinterpret_cast<const uint32_t*>(from);
-                    if (r < rows) *reinterpret_cast<uint32_t*>(at) = v;
-                } else {
-                    const uint16_t v = *reinterpret_cast<const uint16_t*>(from);
-                    if (r < rows) *reinterpret_cast<uint16_t*>(at) = v;
-                }
-                at += 32 / kCols * ld * ES;
-            }
+        for (int j = 0; j < kSteps; j++) {
+            const int r = j * (32 / kCols) + lane / kCols;
+            v[j] = ld_shared<ES>(box + r * 64 + (((c * ES >> 4) ^ (r >> 1 & 3)) << 4) + (c * ES & 15));
         }
-        __syncwarp();
+        char* at = static_cast<char*>(out) + ((t0 + lane / kCols) * ld + col) * ES;
+        if (col < N)
+#pragma unroll
+            for (int j = 0; j < kSteps; j++, at += 32 / kCols * ld * ES) {
+                if (j * (32 / kCols) + lane / kCols >= rows) continue;
+                if (ES == 4)
+                    *reinterpret_cast<uint32_t*>(at) = v[j];
+                else
+                    *reinterpret_cast<uint16_t*>(at) = (uint16_t)v[j];
+            }
     }
 }
 
@@ -150,7 +165,7 @@ enum { kFirst = 0, kSecond = 1, kAlone = 2 };                // of a run of 64 c
 struct Rows {
     const Epilogue& e;
     const PairParams& P;
-    uint8_t* box;
+    uint32_t box;                                            // the warp's 2 KB of shared memory
     float sp, sp2, sq;
     int lane;
     int64_t tw, t;
@@ -442,7 +457,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
     } else if (warp < kEpiWarps) {
         const Epilogue& e = P.e;
         const int half = warp >> 2, q = warp & 3;
-        Rows rows{e, P, base + C::kStages * C::kStage + warp * kBox, scale_or_1(e.s_p), MODE != kPlain ? scale_or_1(e.s_p2) : 1.0f,
+        Rows rows{e, P, smem_u32(base) + C::kStages * C::kStage + warp * kBox, scale_or_1(e.s_p), MODE != kPlain ? scale_or_1(e.s_p2) : 1.0f,
                   scale_or_1(e.s_q), lane};
         rows.bad = false;
         bool lost = false;                                   // a wait ran out
