@@ -27,7 +27,7 @@ namespace {
 
 constexpr int kEpiWarps = 8;
 constexpr int kThreadsPair = (kEpiWarps + 2) * 32;
-constexpr int kBox = 2048;                                   // 32 rows of 64 bytes
+constexpr int kBox = 4096;                                   // 32 rows of 32 fp32
 constexpr int kPairStages = 6;                               // at most
 
 struct PairParams {
@@ -45,6 +45,7 @@ struct Pair {
     static constexpr int kStage = 2 * kOp + 3 * kS;          // + scales of its tokens, of all columns
     static constexpr int kStages = KIND == kBf16 ? 6 : 5;
     static constexpr int kSmem = kStages * kStage + kEpiWarps * kBox + 1024;
+    static_assert(kSmem <= 227 * 1024 - 256, "shared memory");
     static constexpr int kSf = 464;                          // scale columns: tokens, then columns
     static constexpr int kAcc1 = KIND == kBf16 ? 256 : 208;  // the second accumulator
 };
@@ -110,19 +111,20 @@ __device__ __forceinline__ uint32_t ld_shared(uint32_t at) {
 // W words (64 or 128 bytes) of this lane's row t0 + lane, columns n.. of a result with N columns
 // and T rows.  Rows aligned to 32 bytes go out as whole sectors, a lane's own (no staging:
 // TMA stores of boxes waited behind the loads in the SM's TMA queue, 7.2 us a tile of K = 4096 where
-// this takes 5.9).  Other rows, and a ragged last chunk, pass through the warp's 2 KB of
+// this takes 5.9).  Other rows, and a ragged last chunk, pass through the warp's 4 KB of
 // shared memory and go out by elements, a row's consecutive ones to consecutive lanes.
-template <int ES, int W>
+// WHOLE: rows aligned to 32 bytes and no ragged chunk, whatever the sizes.
+template <int ES, int W, bool WHOLE = false>
 __device__ __forceinline__ void put_row(const uint32_t (&w)[W], int wide, uint32_t box, void* out, int64_t ld, int64_t n,
                                         int64_t t0, int64_t N, int64_t T) {
     const int lane = threadIdx.x & 31;
     if (n >= N || t0 >= T) return;                           // the same for the warp
-    if (wide >= 16 && n + W * 4 / ES <= N) {
+    if (WHOLE || (wide >= 16 && n + W * 4 / ES <= N)) {
         if (t0 + lane >= T) return;
         char* at = static_cast<char*>(out) + ((t0 + lane) * ld + n) * ES;
 #pragma unroll
         for (int i = 0; i < W; i += 8) {
-            if (wide == 32) {
+            if (WHOLE || wide == 32) {
                 st32(at + 4 * i, word4(w + i), word4(w + i + 4));
             } else {
                 *reinterpret_cast<uint4*>(at + 4 * i) = word4(w + i);
@@ -131,33 +133,29 @@ __device__ __forceinline__ void put_row(const uint32_t (&w)[W], int wide, uint32
         }
         return;
     }
+    // 32 rows of 4 W bytes, their 16-byte parts swapped against conflicts; a row's 32 elements
+    // go to the 32 lanes
+    static_assert(W * 4 == 32 * ES, "32 columns");
+    constexpr int kRowBytes = 4 * W, kMask = kRowBytes == 64 ? 3 : 7, kShift = kRowBytes == 64 ? 1 : 0;
+    __syncwarp();
 #pragma unroll
-    for (int i = 0; i < W; i += 16) {                        // 32 rows of 64 bytes, 16-byte parts swapped against conflicts
-        __syncwarp();
+    for (int c = 0; c < W / 4; c++) st_shared16(box + lane * kRowBytes + ((c ^ (lane >> kShift & kMask)) << 4), word4(w + 4 * c));
+    __syncwarp();
+    const int rows = (int)(T - t0 < 32 ? T - t0 : 32);
+    uint32_t v[32];                                          // all read before the first is stored
 #pragma unroll
-        for (int c = 0; c < 4; c++) st_shared16(box + lane * 64 + ((c ^ (lane >> 1 & 3)) << 4), word4(w + i + 4 * c));
-        __syncwarp();
-        constexpr int kCols = 64 / ES, kSteps = kCols;       // rows at a time: 32 / kCols
-        const int c = lane % kCols;
-        const int64_t col = n + i * 4 / ES + c;
-        const int rows = (int)(T - t0 < 32 ? T - t0 : 32);
-        uint32_t v[kSteps];                                  // all read before the first is stored
+    for (int r = 0; r < 32; r++)
+        v[r] = ld_shared<ES>(box + r * kRowBytes + (((lane * ES >> 4) ^ (r >> kShift & kMask)) << 4) + (lane * ES & 15));
+    char* at = static_cast<char*>(out) + (t0 * ld + n + lane) * ES;
+    if (n + lane < N)
 #pragma unroll
-        for (int j = 0; j < kSteps; j++) {
-            const int r = j * (32 / kCols) + lane / kCols;
-            v[j] = ld_shared<ES>(box + r * 64 + (((c * ES >> 4) ^ (r >> 1 & 3)) << 4) + (c * ES & 15));
+        for (int r = 0; r < 32; r++, at += ld * ES) {
+            if (r >= rows) continue;
+            if (ES == 4)
+                *reinterpret_cast<uint32_t*>(at) = v[r];
+            else
+                *reinterpret_cast<uint16_t*>(at) = (uint16_t)v[r];
         }
-        char* at = static_cast<char*>(out) + ((t0 + lane / kCols) * ld + col) * ES;
-        if (col < N)
-#pragma unroll
-            for (int j = 0; j < kSteps; j++, at += 32 / kCols * ld * ES) {
-                if (j * (32 / kCols) + lane / kCols >= rows) continue;
-                if (ES == 4)
-                    *reinterpret_cast<uint32_t*>(at) = v[j];
-                else
-                    *reinterpret_cast<uint16_t*>(at) = (uint16_t)v[j];
-            }
-    }
 }
 
 // What a warp makes of 32 columns n.. of its rows: lane's row t = tw + lane, tw the warp's first.
@@ -165,7 +163,7 @@ enum { kFirst = 0, kSecond = 1, kAlone = 2 };                // of a run of 64 c
 struct Rows {
     const Epilogue& e;
     const PairParams& P;
-    uint32_t box;                                            // the warp's 2 KB of shared memory
+    uint32_t box;                                            // the warp's 4 KB of shared memory
     float sp, sp2, sq;
     int lane;
     int64_t tw, t;
@@ -270,8 +268,8 @@ struct Rows {
                         ut[j] = pack2_bf16(g[2 * j] * sp2, g[2 * j + 1] * sp2);
                     }
                 }
-                put_row<2, 16>(gt, 32, box, e.dgu, 2 * e.fp, n, tw, e.fp, e.T);
-                put_row<2, 16>(ut, 32, box, e.dgu + e.fp, 2 * e.fp, n, tw, e.fp, e.T);
+                put_row<2, 16, true>(gt, 32, box, e.dgu, 2 * e.fp, n, tw, e.fp, e.T);
+                put_row<2, 16, true>(ut, 32, box, e.dgu + e.fp, 2 * e.fp, n, tw, e.fp, e.T);
             }
         }
         if (e.out) put_row<2, 16>(hw, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
