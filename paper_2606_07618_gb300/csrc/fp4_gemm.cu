@@ -56,40 +56,66 @@ struct Tile {
     static_assert(kHalf >= 2 && (!kOver || kRed <= kHalf * kStage), "shared memory");
 };
 
-// One result column n of token t.  Whole warps call it (the MXFP4 form reduces over the
-// 32 columns of a warp, one block).
-template <int MODE>
-__device__ __forceinline__ void emit(const Epilogue& e, int64_t t, int64_t n, float a, float b, float sp, float sp2,
-                                     float sq, bool& bad) {
-    if (MODE == kPlain) {
-        if (n < e.N) {
-            const float v = a * sp * sq;
-            if (e.out_f32)
-                static_cast<float*>(e.out)[t * e.ldo + n] = v;
-            else
-                static_cast<uint16_t*>(e.out)[t * e.ldo + n] = bf16_bits(v);
+// Column n of tokens t.. below T, K of them at most.  Whole warps call it (the MXFP4 form reduces
+// over the 32 columns of a warp, one block).  All values first, then all stores: with the branches
+// on what is wanted inside a token's work, tokens ran one after the other (240 cycles each).
+template <int MODE, int K>
+__device__ __forceinline__ void emit(const Epilogue& e, int t, int T, int64_t n, const float (&a)[K], const float (&b)[K],
+                                     float sp, float sp2, float sq, bool& bad) {
+    if constexpr (MODE == kPlain) {
+        if (n >= e.N) return;
+        if (e.out_f32) {
+            float* at = static_cast<float*>(e.out) + t * e.ldo + n;
+#pragma unroll
+            for (int i = 0; i < K; i++)
+                if (t + i < T) at[i * e.ldo] = a[i] * sp * sq;
+        } else {
+            uint16_t* at = static_cast<uint16_t*>(e.out) + t * e.ldo + n;
+#pragma unroll
+            for (int i = 0; i < K; i++)
+                if (t + i < T) at[i * e.ldo] = bf16_bits(a[i] * sp * sq);
         }
-        return;
-    }
-    float unused;
-    const float g = a * sp * sq, u = b * sp2 * sq;
-    const uint16_t h = bf16_bits(activate<false>(e.act, g, unused) * u);
-    if (e.out && n < e.N) static_cast<uint16_t*>(e.out)[t * e.ldo + n] = h;
-    if (e.h_codes) {
-        const int lane = threadIdx.x & 31;
-        const bool live = n < e.N;                           // N % 32 == 0: the same for a warp
-        const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, live ? (uint32_t)(h & 0x7FFF) << 16 : 0u), ex = m >> 23;
-        const bool finite = ex != 255;
-        bad |= !finite;
-        const uint32_t code = finite && ex > 2 ? ex - 2 : 0;
-        const float hv = bf16_value(h);
-        const float x = finite ? hv * __uint_as_float((254u - code) << 23) : copysignf(0.0f, hv);
-        uint32_t w = (e2m1x8(pack2(x, 0.0f), 0, 0, 0) & 0xFu) << (4 * (lane & 7));
-        w |= __shfl_xor_sync(0xFFFFFFFFu, w, 1);
-        w |= __shfl_xor_sync(0xFFFFFFFFu, w, 2);
-        w |= __shfl_xor_sync(0xFFFFFFFFu, w, 4);
-        if (live && (lane & 7) == 0) *reinterpret_cast<uint32_t*>(e.h_codes + t * (e.N / 2) + n / 2) = w;
-        if (lane == 0) e.h_sf[swizzle_offset(t, n >> 5, e.h_kpad4)] = (uint8_t)code;   // columns past N: zero
+    } else {
+        uint16_t h[K];
+        float g[K], unused;
+#pragma unroll
+        for (int i = 0; i < K; i++) g[i] = a[i] * sp * sq;
+        if (e.act == 1) {
+#pragma unroll
+            for (int i = 0; i < K; i++) g[i] = activate<false>(1, g[i], unused);
+        } else {
+#pragma unroll
+            for (int i = 0; i < K; i++) g[i] = activate<false>(0, g[i], unused);
+        }
+#pragma unroll
+        for (int i = 0; i < K; i++) h[i] = bf16_bits(g[i] * (b[i] * sp2 * sq));
+        if (e.out && n < e.N) {
+            uint16_t* at = static_cast<uint16_t*>(e.out) + t * e.ldo + n;
+#pragma unroll
+            for (int i = 0; i < K; i++)
+                if (t + i < T) at[i * e.ldo] = h[i];
+        }
+        if (e.h_codes) {
+            const int lane = threadIdx.x & 31;
+            const bool live = n < e.N;                           // N % 32 == 0: the same for a warp
+#pragma unroll
+            for (int i = 0; i < K; i++) {
+                const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, live ? (uint32_t)(h[i] & 0x7FFF) << 16 : 0u), ex = m >> 23;
+                const bool finite = ex != 255;
+                const uint32_t code = finite && ex > 2 ? ex - 2 : 0;
+                const float hv = bf16_value(h[i]);
+                const float x = finite ? hv * __uint_as_float((254u - code) << 23) : copysignf(0.0f, hv);
+                uint32_t w = (e2m1x8(pack2(x, 0.0f), 0, 0, 0) & 0xFu) << (4 * (lane & 7));
+                w |= __shfl_xor_sync(0xFFFFFFFFu, w, 1);
+                w |= __shfl_xor_sync(0xFFFFFFFFu, w, 2);
+                w |= __shfl_xor_sync(0xFFFFFFFFu, w, 4);
+                const int64_t r = t + i;
+                if (r >= T) continue;
+                bad |= !finite;
+                if (live && (lane & 7) == 0) *reinterpret_cast<uint32_t*>(e.h_codes + r * (e.N / 2) + n / 2) = w;
+                if (lane == 0) e.h_sf[swizzle_offset(r, n >> 5, e.h_kpad4)] = (uint8_t)code;   // columns past N: zero
+            }
+        }
     }
 }
 
@@ -228,16 +254,17 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
                     const int t = c + i;
-                    if (t >= T) break;
+                    if (t >= T) continue;
                     const uint32_t at = at_rank(red + (uint32_t)((((t & (per - 1)) << lsplit) + rank) * 512 + tid * 4), (uint32_t)(t >> lper));
                     st_cluster(at, a[i]);
                     if (C::kG == 2) st_cluster(at + TN * 512, b[i]);
                 }
             } else {
-#pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    if (c + i >= T) break;
-                    emit<MODE>(e, c + i, n, a[i], C::kG == 2 ? b[i] : 0.0f, sp, sp2, sq, bad);
+                if (T - c <= 2) {
+                    const float a2[2] = {a[0], a[1]}, b2[2] = {b[0], b[1]};
+                    emit<MODE, 2>(e, c, T, n, a2, b2, sp, sp2, sq, bad);
+                } else {
+                    emit<MODE, 16>(e, c, T, n, a, b, sp, sp2, sq, bad);
                 }
             }
         }
@@ -250,15 +277,18 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
         ok = *reinterpret_cast<volatile int*>(&s_abort) == 0;
         if (warp < 4 && ok) {
             const float* mine = reinterpret_cast<const float*>(base + red_at) + tid;
-#pragma unroll 2
-            for (int j = 0; j < per; j++) {
-                if (rank * per + j >= T) break;
-                float a = 0.0f, b = 0.0f;
+            // two tokens at a time: a rank has at least two
+#pragma unroll 1
+            for (int j = 0; j < per && rank * per + j < T; j += 2) {
+                float a[2] = {0.0f, 0.0f}, b[2] = {0.0f, 0.0f};
                 for (int r = 0; r < split; r++) {
-                    a += mine[(j * split + r) * 128];
-                    if (C::kG == 2) b += mine[(TN + j * split + r) * 128];
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        a[i] += mine[((j + i) * split + r) * 128];
+                        if (C::kG == 2) b[i] += mine[(TN + (j + i) * split + r) * 128];
+                    }
                 }
-                emit<MODE>(e, rank * per + j, n, a, b, sp, sp2, sq, bad);
+                emit<MODE, 2>(e, rank * per + j, T, n, a, b, sp, sp2, sq, bad);
             }
         }
     }
