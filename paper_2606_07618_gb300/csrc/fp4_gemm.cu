@@ -355,19 +355,21 @@ cudaError_t launch_tile(const Product& p, int sms, cudaStream_t s) {
 template <int KIND, int MODE>
 cudaError_t launch_by_tokens(const Product& p, int sms, cudaStream_t s) {
     if (p.q.rows <= 16) return launch_tile<KIND, MODE, 16>(p, sms, s);
-    if (MODE == kGated || p.q.rows <= 32) return launch_tile<KIND, MODE, 32>(p, sms, s);
-    return launch_tile<KIND, kPlain, 64>(p, sms, s);
+    if (p.q.rows <= 32) return launch_tile<KIND, MODE, 32>(p, sms, s);
+    return launch_tile<KIND, MODE, 64>(p, sms, s);
 }
 
 }  // namespace
 }  // namespace mm
 
-// Up to 32 tokens the weight is streamed past them, up to 64 where K is long; more go to pairs of
-// CTAs.  us, here / pairs: 32 x 4096 x 4096 6.2 / 8.4, gated 32 x 14336 x 4096 15.9 / 19.6; 64 x 1024 x
-// 1024 7.8 / 5.1, 64 x 4096 x 4096 9.4 / 8.4, 64 x 4096 x 14336 12.7 / 16.7, gated 64 x 2048 x 2048
-// 11.1 / 6.8.
+// Up to 32 tokens the weight is streamed past them, up to 64 where it is long or has a tile for
+// half the SMs; more go to pairs of CTAs.  us, here / pairs: 32 x 1024 x 1024 4.4 / 4.8, 32 x 2048 x 2048
+// 4.7 / 6.0, gated 32 x 14336 x 4096 14.1 / 19.0; 64 x 4096 x 14336 12.4 / 16.7, 64 x 14336 x 4096 9.7 /
+// 10.2, gated 15.7 / 18.0; 64 x 1024 x 1024 6.9 / 5.0, 64 x 4096 x 4096 9.1 / 8.3, gated 64 x 2048 x 2048
+// 11.0 / 6.8.
 cudaError_t launch_product(const Product& p, int sms, cudaStream_t s) {
-    const int few = p.kind == kBf16 || p.mode == kGatedGrad ? 0 : p.mode == kPlain && p.k >= 8192 ? 64 : 32;
+    const bool long_or_wide = p.k >= 8192 || 2 * ((p.p.rows + 127) / 128) > sms;
+    const int few = p.kind == kBf16 || p.mode == kGatedGrad ? 0 : long_or_wide ? 64 : 32;
     if (p.q.rows > few) return launch_pair(p, sms, s);
     if (p.mode == kPlain)
         return p.kind == kMxfp4 ? mm::launch_by_tokens<kMxfp4, kPlain>(p, sms, s) : mm::launch_by_tokens<kNvfp4, kPlain>(p, sms, s);
