@@ -112,13 +112,13 @@ __global__ void __launch_bounds__(256) mxfp4_quantize_kernel(MxParams p) {
         bad |= !finite;
         const uint32_t code = finite && e > 2 ? e - 2 : 0;
         const float inv = __uint_as_float((254u - code) << 23);  // 2^(127 - code)
+        if (!finite)
+#pragma unroll
+            for (int i = 0; i < 16; i++) y[i] = copysignf(0.0f, y[i]);
+        const u64 inv2 = pack2(inv, inv);
         u64 t[8];
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const float a = finite ? __fmul_rn(y[2 * i], inv) : copysignf(0.0f, y[2 * i]);
-            const float b = finite ? __fmul_rn(y[2 * i + 1], inv) : copysignf(0.0f, y[2 * i + 1]);
-            t[i] = pack2(a, b);
-        }
+        for (int i = 0; i < 8; i++) t[i] = mul2(pack2(y[2 * i], y[2 * i + 1]), inv2);
         if (!live) continue;
         reinterpret_cast<uint2*>(p.codes)[seg] = make_uint2(e2m1x8(t[0], t[1], t[2], t[3]), e2m1x8(t[4], t[5], t[6], t[7]));
         if ((seg & 1) == 0) {
