@@ -34,6 +34,7 @@ struct PairParams {
     CUtensorMap p, p2, q, sp, sp2, sq;
     int64_t k;
     int tiles_t, tiles_n, split, starve;
+    int width;                                               // columns of a tile: 256, for bf16 also fewer
     int wide_out, wide_dh, wide_codes;                       // bytes that rows of D or h, dh, codes are aligned to: 32, 16 or fewer
     Epilogue e;
 };
@@ -328,6 +329,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
     const int split = SPLIT ? P.split : 1;
     const int all = (int)((P.k + stage_k(KIND) - 1) / stage_k(KIND));
     const int k0 = SPLIT ? (int)((int64_t)all * pair / split) : 0, nst = SPLIT ? (int)((int64_t)all * (pair + 1) / split) - k0 : all;
+    const int width = KIND == kBf16 ? P.width : 256;
     const int ntiles = P.tiles_t * P.tiles_n, step = (int)gridDim.x / (2 * split), first = (int)blockIdx.x / (2 * split);
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kPairStages, accf0 = empty0 + 8 * kPairStages,
                    drained0 = accf0 + 16;
@@ -375,11 +377,11 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                 }
                 if (elect_one()) {
                     const uint32_t st = smem_u32(base) + r * C::kStage, bar = leader_full + 8 * r;
-                    if (rank == 0) mbar_expect_tx(full0 + 8 * r, 2 * C::kStage);
+                    if (rank == 0) mbar_expect_tx(full0 + 8 * r, KIND == kBf16 ? 2 * C::kOp + P.width * kRow : 2 * C::kStage);
                     const int x = (k0 + kc) * (KIND == kBf16 ? 64 : 128);
                     tma_load_2d_pair(st, &P.q, x, t0, bar);
                     if (MODE == kPlain)
-                        tma_load_2d_pair(st + C::kOp, &P.p, x, tn * 256 + (int)rank * 128, bar);
+                        tma_load_2d_pair(st + C::kOp, &P.p, x, tn * width + (int)rank * (width / 2), bar);
                     else
                         tma_load_2d_pair(st + C::kOp, rank == swap ? &P.p : &P.p2, x, tn * 128, bar);
                     if (KIND != kBf16) {
@@ -412,7 +414,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                 }
         if (!ok && lane == 0) atomicOr(&s_abort, 1);
     } else if (warp == kEpiWarps + 1 && rank == 0) {
-        constexpr uint32_t id = idesc(KIND, 256, 256);
+        const uint32_t id = idesc(KIND, 256, width);
         Ring ring;
         int it = 0;
         bool ok = true;
@@ -475,7 +477,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
             };
             if (!overlap) release();                         // done with the tile before
             uint32_t dhw[2][16];
-            const int64_t n0 = MODE == kPlain ? (int64_t)tn * 256 : (int64_t)tn * 128 + 64 * half;
+            const int64_t n0 = MODE == kPlain ? (int64_t)tn * width : (int64_t)tn * 128 + 64 * half;
             if (MODE == kGatedGrad && !SPLIT) {              // asked for before the accumulators are waited for
                 rows.load_dh(dhw[0], n0);
                 rows.load_dh(dhw[1], n0 + 32);
@@ -508,8 +510,8 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                     tmem_wait32(v[0]);
                     tmem_wait32(v[1]);
                     if (overlap && c == 0) release();
-                    rows.plain(v[0], n0 + col);
-                    rows.plain(v[1], n0 + col + 32);
+                    if (KIND != kBf16 || col < width) rows.plain(v[0], n0 + col);
+                    if (KIND != kBf16 || col + 32 < width) rows.plain(v[1], n0 + col + 32);
                 }
             } else {
                 // The up columns (the overlapping ones are theirs in either accumulator) to registers, then 32
@@ -571,7 +573,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                     float g[32], u[32];
                     sum32(c, g);
                     if (MODE == kPlain) {
-                        rows.plain(g, (int64_t)tn * 256 + c);
+                        rows.plain(g, (int64_t)tn * 256 + c);   // a split tile is 256 wide
                     } else {
                         uint32_t dhw[16];
                         const int64_t n = (int64_t)tn * 128 + c;
@@ -605,7 +607,18 @@ template <int KIND, int MODE, bool SPLIT>
 cudaError_t launch_pair_as(const Product& p, int split, int sms, cudaStream_t s) {
     using C = Pair<KIND>;
     PairParams P = {};
-    const bool ok = make_operand_map(&P.p, p.p, KIND, p.k, 128) && make_operand_map(&P.q, p.q, KIND, p.k, 128) &&
+    // bf16 tiles may be narrower, which fills the last wave better (scale atoms start at 128 rows, so
+    // others are not): the width of least waves times columns.
+    P.width = 256;
+    const int64_t tiles_t = (p.q.rows + 255) / 256;
+    if (KIND == kBf16 && !SPLIT) {
+        int64_t best = INT64_MAX;
+        for (int w = 256; w >= 128; w -= 32) {
+            const int64_t tiles = tiles_t * ((p.p.rows + w - 1) / w), cost = (tiles + sms / 2 - 1) / (sms / 2) * w;
+            if (cost < best) best = cost, P.width = w;
+        }
+    }
+    const bool ok = make_operand_map(&P.p, p.p, KIND, p.k, MODE == kPlain ? P.width / 2 : 128) && make_operand_map(&P.q, p.q, KIND, p.k, 128) &&
                     (MODE == kPlain || make_operand_map(&P.p2, p.p2, KIND, p.k, 128)) &&
                     (KIND == kBf16 || (make_scale_map(&P.sp, p.p, KIND, p.k) && make_scale_map(&P.sq, p.q, KIND, p.k) &&
                                        (MODE == kPlain || make_scale_map(&P.sp2, p.p2, KIND, p.k))));
@@ -616,8 +629,8 @@ cudaError_t launch_pair_as(const Product& p, int split, int sms, cudaStream_t s)
     if (p.out2 && row_alignment(p.out2, 0) < P.wide_out) P.wide_out = row_alignment(p.out2, 0);
     P.wide_dh = row_alignment(p.dh, p.lddh * 2);
     P.wide_codes = row_alignment(p.h_codes, p.p.rows / 2);
-    const int64_t width = MODE == kPlain ? 256 : 128;
-    P.tiles_t = (int)((p.q.rows + 255) / 256);
+    const int64_t width = MODE == kPlain ? P.width : 128;
+    P.tiles_t = (int)tiles_t;
     P.tiles_n = (int)((p.p.rows + width - 1) / width);
     const int64_t tiles = (int64_t)P.tiles_t * P.tiles_n;
     if (tiles >= 1ll << 30) return cudaErrorNotSupported;
