@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
     const uint32_t tmem = s_tmem;
 
     if (warp == 4) {
-        Ring ring;
+        Ring ring(smem_u32(base));
         bool ok = true;
         int issued = 0;
         for (int s = from; s < to; s++) {
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
                 break;
             }
             if (elect_one()) {
-                const uint32_t bar = full0 + 8 * r, st = smem_u32(base) + r * C::kStage, sf = st + C::kG * C::kP + C::kQ;
+                const uint32_t bar = full0 + 8 * r, st = ring.at, sf = st + C::kG * C::kP + C::kQ;
                 mbar_expect_tx(bar, C::kStage);
                 tma_load_2d(st, &P.p, s * 128, n0, bar);
                 if (C::kG == 2) tma_load_2d(st + C::kP, &P.p2, s * 128, n0, bar);
@@ -175,11 +175,11 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
             }
             __syncwarp();
             if (issued < stages) issued++;
-            ring.next(stages);
+            ring.next(stages, C::kStage);
         }
         // every slot in use landed
-        if (issued < stages) ring = Ring{0, 1};          // each used once
-        for (int j = 0; j < issued; j++, ring.next(stages))
+        if (issued < stages) ring = Ring(ring.first, 1);          // each used once
+        for (int j = 0; j < issued; j++, ring.next(stages, C::kStage))
             if (!mbar_wait_warp(full0 + 8 * ring.slot, ring.parity ^ 1)) {
                 ok = false;
                 break;
@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
         if (!ok && lane == 0) atomicOr(&s_abort, 1);
     } else if (warp == 5) {
         constexpr uint32_t id = idesc(KIND, 128, TN);
-        Ring ring;
+        Ring ring(smem_u32(base));
         bool ok = true;
         for (int s = from; s < to; s++) {
             const int r = ring.slot;
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
             }
             tc_fence_after();
             if (elect_one()) {
-                const uint32_t st = smem_u32(base) + r * C::kStage, sf = st + C::kG * C::kP + C::kQ;
+                const uint32_t st = ring.at, sf = st + C::kG * C::kP + C::kQ;
 #pragma unroll
                 for (int a = 0; a < (C::kG + 1) * atoms(KIND); a++) cp_atom<1>(tmem + C::kSfCol + 4 * a, atom_desc(sf + a * kAtom));
                 const int left = (int)((P.k - (int64_t)s * stage_k(KIND) + mma_k(KIND) - 1) / mma_k(KIND));
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kThreadsTile, 2) tile_kernel(const __grid_cons
                 if (s == to - 1) mma_commit(dbar);
             }
             __syncwarp();
-            ring.next(stages);
+            ring.next(stages, C::kStage);
         }
         if (!ok && lane == 0) atomicOr(&s_abort, 1);
     } else if (!mbar_wait_warp(dbar, 0)) {

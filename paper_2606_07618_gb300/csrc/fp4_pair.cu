@@ -27,14 +27,15 @@ namespace {
 
 constexpr int kEpiWarps = 8;
 constexpr int kThreadsPair = (kEpiWarps + 2) * 32;
-constexpr int kBox = 4096;                                   // 32 rows of 32 fp32
-constexpr int kPairStages = 6;                               // at most
+constexpr int kPairStages = 8;                               // at most
+constexpr int kPairSmem = 227 * 1024 - 256;                  // of a CTA, less its static part
 
 struct PairParams {
     CUtensorMap p, p2, q, sp, sp2, sq;
     int64_t k;
     int tiles_t, tiles_n, split, starve;
-    int width;                                               // columns of a tile: 256, for bf16 also fewer
+    int stages, stage, box;                                  // the ring: slots, bytes of one; bytes of a warp's box
+    int width;                                               // columns of a tile (gated: 256, half of them gate's)
     int wide_out, wide_dh, wide_codes;                       // bytes that rows of D or h, dh, codes are aligned to: 32, 16 or fewer
     Epilogue e;
 };
@@ -43,10 +44,6 @@ template <int KIND>
 struct Pair {
     static constexpr int kOp = 128 * kRow;                   // a CTA's part of an operand: 16 KB
     static constexpr int kS = atoms(KIND) * kAtom;
-    static constexpr int kStage = 2 * kOp + 3 * kS;          // + scales of its tokens, of all columns
-    static constexpr int kStages = KIND == kBf16 ? 6 : 5;
-    static constexpr int kSmem = kStages * kStage + kEpiWarps * kBox + 1024;
-    static_assert(kSmem <= 227 * 1024 - 256, "shared memory");
     static constexpr int kSf = 464;                          // scale columns: tokens, then columns
     static constexpr int kAcc1 = KIND == kBf16 ? 256 : 208;  // the second accumulator
 };
@@ -164,7 +161,7 @@ enum { kFirst = 0, kSecond = 1, kAlone = 2 };                // of a run of 64 c
 struct Rows {
     const Epilogue& e;
     const PairParams& P;
-    uint32_t box;                                            // the warp's 4 KB of shared memory
+    uint32_t box;                                            // the warp's box in shared memory
     float sp, sp2, sq;
     int lane;
     int64_t tw, t;
@@ -329,13 +326,14 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
     const int split = SPLIT ? P.split : 1;
     const int all = (int)((P.k + stage_k(KIND) - 1) / stage_k(KIND));
     const int k0 = SPLIT ? (int)((int64_t)all * pair / split) : 0, nst = SPLIT ? (int)((int64_t)all * (pair + 1) / split) - k0 : all;
-    const int width = KIND == kBf16 ? P.width : 256;
+    const int width = MODE == kPlain ? P.width : 256, stages = P.stages, stage = P.stage;
+    const int sf_at = C::kOp + width / 2 * kRow;             // a slot: tokens, columns, scales
     const int ntiles = P.tiles_t * P.tiles_n, step = (int)gridDim.x / (2 * split), first = (int)blockIdx.x / (2 * split);
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kPairStages, accf0 = empty0 + 8 * kPairStages,
                    drained0 = accf0 + 16;
 
     if (tid == 0) {
-        for (int b = 0; b < C::kStages; b++) {
+        for (int b = 0; b < stages; b++) {
             mbar_init(full0 + 8 * b, 1 + P.starve);
             mbar_init(empty0 + 8 * b, 1);
         }
@@ -360,7 +358,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
     const uint32_t tmem = s_tmem;
 
     if (warp == kEpiWarps) {
-        Ring ring;
+        Ring ring(smem_u32(base));
         const uint32_t leader_full = at_rank(full0, leader);
         bool ok = true;
         int issued = 0;
@@ -371,13 +369,13 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
             const int t0 = tt * 256 + (int)rank * 128;
             for (int kc = 0; kc < nst; kc++) {
                 const int r = ring.slot;
-                if (issued >= C::kStages && !mbar_wait_warp(empty0 + 8 * r, ring.parity ^ 1)) {
+                if (issued >= stages && !mbar_wait_warp(empty0 + 8 * r, ring.parity ^ 1)) {
                     ok = false;
                     break;
                 }
                 if (elect_one()) {
-                    const uint32_t st = smem_u32(base) + r * C::kStage, bar = leader_full + 8 * r;
-                    if (rank == 0) mbar_expect_tx(full0 + 8 * r, KIND == kBf16 ? 2 * C::kOp + P.width * kRow : 2 * C::kStage);
+                    const uint32_t st = ring.at, bar = leader_full + 8 * r;
+                    if (rank == 0) mbar_expect_tx(full0 + 8 * r, 2 * stage);
                     const int x = (k0 + kc) * (KIND == kBf16 ? 64 : 128);
                     tma_load_2d_pair(st, &P.q, x, t0, bar);
                     if (MODE == kPlain)
@@ -385,12 +383,12 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                     else
                         tma_load_2d_pair(st + C::kOp, rank == swap ? &P.p : &P.p2, x, tn * 128, bar);
                     if (KIND != kBf16) {
-                        const uint32_t sf = st + 2 * C::kOp;
+                        const uint32_t sf = st + sf_at;
                         const int a = (k0 + kc) * atoms(KIND);
                         tma_load_3d_pair(sf, &P.sq, 0, a, t0 >> 7, bar);
                         if (MODE == kPlain) {
-                            tma_load_3d_pair(sf + C::kS, &P.sp, 0, a, 2 * tn, bar);
-                            tma_load_3d_pair(sf + 2 * C::kS, &P.sp, 0, a, 2 * tn + 1, bar);
+                            tma_load_3d_pair(sf + C::kS, &P.sp, 0, a, tn * (width >> 7), bar);
+                            if (width > 128) tma_load_3d_pair(sf + 2 * C::kS, &P.sp, 0, a, 2 * tn + 1, bar);
                         } else {
                             tma_load_3d_pair(sf + C::kS, swap ? &P.sp2 : &P.sp, 0, a, tn, bar);
                             tma_load_3d_pair(sf + 2 * C::kS, swap ? &P.sp : &P.sp2, 0, a, tn, bar);
@@ -398,16 +396,16 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                     }
                 }
                 __syncwarp();
-                if (issued < C::kStages) issued++;
-                ring.next(C::kStages);
+                if (issued < stages) issued++;
+                ring.next(stages, stage);
             }
         }
         // Every slot in use read, hence landed.  After a timeout the leader, whose barriers count both
         // CTAs' copies, waits for those instead (the other CTA stays for the last cluster barrier).
-        if (issued < C::kStages) ring = Ring{0, 1};          // each used once
+        if (issued < stages) ring = Ring(ring.first, 1);          // each used once
         const bool landed = !ok;
         if (!landed || rank == 0)
-            for (int j = 0; j < issued; j++, ring.next(C::kStages))
+            for (int j = 0; j < issued; j++, ring.next(stages, stage))
                 if (!mbar_wait_warp((landed ? full0 : empty0) + 8 * ring.slot, ring.parity ^ 1)) {
                     ok = false;
                     break;
@@ -415,7 +413,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
         if (!ok && lane == 0) atomicOr(&s_abort, 1);
     } else if (warp == kEpiWarps + 1 && rank == 0) {
         const uint32_t id = idesc(KIND, 256, width);
-        Ring ring;
+        Ring ring(smem_u32(base));
         int it = 0;
         bool ok = true;
         for (int i = first; ok && i < ntiles; i += step, it++) {
@@ -430,12 +428,12 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                 }
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint32_t st = smem_u32(base) + r * C::kStage, sf = st + 2 * C::kOp;
+                    const uint32_t st = ring.at, sf = st + sf_at;
 #pragma unroll
                     for (int a = 0; a < atoms(KIND); a++) {
                         cp_atom<2>(tmem + C::kSf + 4 * a, atom_desc(sf + a * kAtom));
                         cp_atom<2>(tmem + C::kSf + 16 + 8 * a, atom_desc(sf + C::kS + a * kAtom));
-                        cp_atom<2>(tmem + C::kSf + 16 + 8 * a + 4, atom_desc(sf + 2 * C::kS + a * kAtom));
+                        if (width > 128) cp_atom<2>(tmem + C::kSf + 16 + 8 * a + 4, atom_desc(sf + 2 * C::kS + a * kAtom));
                     }
                     const int left = (int)((P.k - (int64_t)(k0 + kc) * stage_k(KIND) + mma_k(KIND) - 1) / mma_k(KIND));
 #pragma unroll
@@ -450,14 +448,14 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                     if (kc == nst - 1) commit_pair(accf0 + 8 * (it & 1), leader);
                 }
                 __syncwarp();
-                ring.next(C::kStages);
+                ring.next(stages, stage);
             }
         }
         if (!ok && lane == 0) atomicOr(&s_abort, 1);
     } else if (warp < kEpiWarps) {
         const Epilogue& e = P.e;
         const int half = warp >> 2, q = warp & 3;
-        Rows rows{e, P, smem_u32(base) + C::kStages * C::kStage + warp * kBox, scale_or_1(e.s_p), MODE != kPlain ? scale_or_1(e.s_p2) : 1.0f,
+        Rows rows{e, P, smem_u32(base) + (uint32_t)(stages * stage + warp * P.box), scale_or_1(e.s_p), MODE != kPlain ? scale_or_1(e.s_p2) : 1.0f,
                   scale_or_1(e.s_q), lane};
         rows.bad = false;
         bool lost = false;                                   // a wait ran out
@@ -469,7 +467,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
             rows.tw = (int64_t)tt * 256 + rank * 128 + 32 * q;
             rows.t = rows.tw + lane;
             const int b = it & 1;
-            const bool overlap = KIND != kBf16 && half == 1 - b;     // this warp reads the overlapping columns
+            const bool overlap = KIND != kBf16 && width == 256 && half == 1 - b;   // this warp reads the overlapping columns
             auto release = [&]() {
                 tc_fence_before();
                 __syncwarp();
@@ -492,7 +490,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
             if (SPLIT) {                                     // sums to shared memory, in the ring's place: all its stages are read
                 float* red = reinterpret_cast<float*>(base) + 32 * q + lane;
 #pragma unroll 1
-                for (int c = 0; c < 128; c += 32) {
+                for (int c = 0; c < 128 && 128 * half + c < width; c += 32) {
                     float v[32];
                     tmem_ld32(acc + 128 * half + c, v);
                     tmem_wait32(v);
@@ -500,18 +498,20 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                     for (int j = 0; j < 32; j++) red[(128 * half + c + j) * 128] = v[j];
                 }
             } else if (MODE == kPlain) {
-                // two halves of 64 columns, the overlapping one first
+                // the columns of this half of the warps, 64 at a time, the overlapping ones first
+                const int mid = (width + 32) / 64 * 32, end = half == 0 ? mid : width;
 #pragma unroll 1
                 for (int c = 0; c < 2; c++) {
-                    const int col = 128 * half + 64 * (overlap && half == 1 ? 1 - c : c);
+                    const int col = mid * half + 64 * (overlap && half == 1 ? 1 - c : c);
+                    if (col >= end) break;
                     float v[2][32];
                     tmem_ld32(acc + col, v[0]);
                     tmem_ld32(acc + col + 32, v[1]);
                     tmem_wait32(v[0]);
                     tmem_wait32(v[1]);
                     if (overlap && c == 0) release();
-                    if (KIND != kBf16 || col < width) rows.plain(v[0], n0 + col);
-                    if (KIND != kBf16 || col + 32 < width) rows.plain(v[1], n0 + col + 32);
+                    rows.plain(v[0], n0 + col);
+                    if (col + 32 < end) rows.plain(v[1], n0 + col + 32);
                 }
             } else {
                 // The up columns (the overlapping ones are theirs in either accumulator) to registers, then 32
@@ -565,15 +565,15 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                     for (int j = 0; j < 32; j++) v[j] += ld_cluster(at + 512 * j);
                 }
             };
-            const int width = (MODE == kPlain ? 256 : 128) / split, from = width * (int)pair + (half * width / 2 & ~31);
-            const int to = half == 0 ? width * (int)pair + (width / 2 < 32 ? 32 : width / 2) : width * (int)(pair + 1);
-            if (whole && (half == 0 || width >= 64))
+            const int share = (MODE == kPlain ? width : 128) / split, from = share * (int)pair + (half * share / 2 & ~31);
+            const int to = half == 0 ? share * (int)pair + (share / 2 < 32 ? 32 : share / 2) : share * (int)(pair + 1);
+            if (whole && (half == 0 || share >= 64))
 #pragma unroll 1
                 for (int c = from; c < to; c += 32) {
                     float g[32], u[32];
                     sum32(c, g);
                     if (MODE == kPlain) {
-                        rows.plain(g, (int64_t)tn * 256 + c);   // a split tile is 256 wide
+                        rows.plain(g, (int64_t)tn * width + c);
                     } else {
                         uint32_t dhw[16];
                         const int64_t n = (int64_t)tn * 128 + c;
@@ -603,21 +603,21 @@ int row_alignment(const void* p, int64_t stride_bytes) {
     return bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 1;
 }
 
+// A slot of the ring: 128 rows of tokens, half a tile's columns, their scales.  A multiple of 1024.
+int stage_bytes(int kind, int width) { return (128 + width / 2) * kRow + (width > 128 ? 3 : 2) * atoms(kind) * kAtom; }
+// A warp's box: 32 x 32 elements of a result whose rows allow no wide store.
+int box_bytes(const Product& p) { return p.out_f32 ? 4096 : 2048; }
+int ring_slots(const Product& p, int width) {
+    const int n = (kPairSmem - 1024 - kEpiWarps * box_bytes(p)) / stage_bytes(p.kind, width);
+    return n > kPairStages ? kPairStages : n;
+}
+
 template <int KIND, int MODE, bool SPLIT>
-cudaError_t launch_pair_as(const Product& p, int split, int sms, cudaStream_t s) {
+cudaError_t launch_pair_as(const Product& p, int width, int split, int sms, cudaStream_t s) {
     using C = Pair<KIND>;
     PairParams P = {};
-    // bf16 tiles may be narrower, which fills the last wave better (scale atoms start at 128 rows, so
-    // others are not): the width of least waves times columns.
-    P.width = 256;
+    P.width = width;
     const int64_t tiles_t = (p.q.rows + 255) / 256;
-    if (KIND == kBf16 && !SPLIT) {
-        int64_t best = INT64_MAX;
-        for (int w = 256; w >= 128; w -= 32) {
-            const int64_t tiles = tiles_t * ((p.p.rows + w - 1) / w), cost = (tiles + sms / 2 - 1) / (sms / 2) * w;
-            if (cost < best) best = cost, P.width = w;
-        }
-    }
     const bool ok = make_operand_map(&P.p, p.p, KIND, p.k, MODE == kPlain ? P.width / 2 : 128) && make_operand_map(&P.q, p.q, KIND, p.k, 128) &&
                     (MODE == kPlain || make_operand_map(&P.p2, p.p2, KIND, p.k, 128)) &&
                     (KIND == kBf16 || (make_scale_map(&P.sp, p.p, KIND, p.k) && make_scale_map(&P.sq, p.q, KIND, p.k) &&
@@ -629,9 +629,9 @@ cudaError_t launch_pair_as(const Product& p, int split, int sms, cudaStream_t s)
     if (p.out2 && row_alignment(p.out2, 0) < P.wide_out) P.wide_out = row_alignment(p.out2, 0);
     P.wide_dh = row_alignment(p.dh, p.lddh * 2);
     P.wide_codes = row_alignment(p.h_codes, p.p.rows / 2);
-    const int64_t width = MODE == kPlain ? P.width : 128;
+    const int64_t columns = MODE == kPlain ? width : 128;
     P.tiles_t = (int)tiles_t;
-    P.tiles_n = (int)((p.p.rows + width - 1) / width);
+    P.tiles_n = (int)((p.p.rows + columns - 1) / columns);
     const int64_t tiles = (int64_t)P.tiles_t * P.tiles_n;
     if (tiles >= 1ll << 30) return cudaErrorNotSupported;
     const auto kernel = pair_kernel<KIND, MODE, SPLIT>;
@@ -640,17 +640,20 @@ cudaError_t launch_pair_as(const Product& p, int split, int sms, cudaStream_t s)
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
     P.split = split;
+    P.stage = stage_bytes(KIND, width);
+    P.box = box_bytes(p);
+    P.stages = ring_slots(p, width);
     P.starve = p.starve;
     const int64_t pairs = SPLIT ? tiles * split : tiles < sms / 2 ? tiles : sms / 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * pairs));
     cfg.blockDim = dim3(kThreadsPair);
-    cfg.dynamicSmemBytes = (size_t)C::kSmem;
+    cfg.dynamicSmemBytes = (size_t)(P.stages * P.stage + kEpiWarps * P.box + 1024);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -664,22 +667,44 @@ cudaError_t launch_pair_as(const Product& p, int split, int sms, cudaStream_t s)
     return cudaLaunchKernelEx(&cfg, kernel, P);
 }
 
-// Pairs that share a tile's K.  Adding up costs some 5 us (256 x 4096 x 14336, 56 stages: 21.6 us,
-// 17.2 by two, where a half of the stages take 9.5), so K has to be long; and clusters of four or eight
-// whole SMs have to find room (at most 36 and 15 on a GB300: 16 of eight ran one after
-// the others, 29 us).
-int pairs_of_a_tile(const Product& p, int sms) {
-    const int64_t width = p.mode == kPlain ? 256 : 128;
-    const int64_t tiles = ((p.q.rows + 255) / 256) * ((p.p.rows + width - 1) / width);
-    const int64_t nst = (p.k + stage_k(p.kind) - 1) / stage_k(p.kind);
-    if (nst < 32 || 4 * tiles > sms - 8) return 1;
-    return 8 * tiles <= sms - 32 ? 4 : 2;
+// How wide a tile is and how many pairs share its K: the least of an estimate in cycles.
+//   A stage takes its MMAs (2 a column) or its loads, 62 bytes a cycle and CTA with most SMs loading,
+//   100 with few, or its share of the latency of HBM; a tile 1500 more, adding up a split K 8000.  Narrow tiles fill the last wave (bf16 in
+//   steps of 32 columns; scale atoms start at 128 rows, so 4-bit tiles are 256 or 128 wide and gated
+//   ones 256) and shorten what a few tiles take; clusters of four or eight whole SMs have to find
+//   room (at most 36 and 15 on a GB300: 16 of eight ran one after the others).
+struct Plan {
+    int width = 256, split = 1;
+};
+Plan plan(const Product& p, int sms) {
+    const int64_t pairs = sms / 2, tiles_t = (p.q.rows + 255) / 256, nst = (p.k + stage_k(p.kind) - 1) / stage_k(p.kind);
+    const int least = p.mode != kPlain ? 256 : p.kind == kBf16 ? 64 : 128, step = p.kind == kBf16 ? 32 : 128;
+    Plan best;
+    int64_t least_cost = INT64_MAX;
+    for (int w = 256; w >= least; w -= step) {
+        const int64_t columns = p.mode == kPlain ? w : 128, tiles = tiles_t * ((p.p.rows + columns - 1) / columns);
+        const int64_t bytes = stage_bytes(p.kind, w), latency = 2900 / ring_slots(p, w);
+        for (int split = 1; split <= 4; split *= 2) {
+            if (split > 1 && (w % 128 != 0 || nst < 8 * split || tiles > (split == 2 ? sms / 4 - 2 : sms / 8 - 4))) continue;
+            const int64_t rate = 2 * tiles * split > pairs ? 62 : 100;
+            const int64_t moved = bytes / rate > latency ? bytes / rate : latency, stage = moved > 2 * w ? moved : 2 * w;
+            const int64_t waves = split > 1 ? 1 : (tiles + pairs - 1) / pairs;
+            const int64_t cost = waves * ((nst + split - 1) / split * stage + 1500) + (split > 1 ? 8000 : 0);
+            if (cost < least_cost) {
+                least_cost = cost;
+                best.width = w;
+                best.split = split;
+            }
+        }
+    }
+    return best;
 }
 
 template <int KIND, int MODE>
 cudaError_t launch_pair_mode(const Product& p, int sms, cudaStream_t s) {
-    const int split = pairs_of_a_tile(p, sms);
-    return split > 1 ? launch_pair_as<KIND, MODE, true>(p, split, sms, s) : launch_pair_as<KIND, MODE, false>(p, 1, sms, s);
+    const Plan b = plan(p, sms);
+    return b.split > 1 ? launch_pair_as<KIND, MODE, true>(p, b.width, b.split, sms, s)
+                       : launch_pair_as<KIND, MODE, false>(p, b.width, 1, sms, s);
 }
 
 template <int KIND>

@@ -133,12 +133,15 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
     return true;
 }
 
-// A ring of K-stages: slot and the parity of its current use.
+// A ring of K-stages: slot, its address and the parity of its current use.
 struct Ring {
+    uint32_t first, at;
     int slot = 0;
     uint32_t parity = 0;
-    __device__ __forceinline__ void next(int stages) {
-        if (++slot == stages) slot = 0, parity ^= 1;
+    __device__ __forceinline__ explicit Ring(uint32_t base, uint32_t parity_ = 0) : first(base), at(base), parity(parity_) {}
+    __device__ __forceinline__ void next(int stages, int bytes) {
+        at += bytes;
+        if (++slot == stages) slot = 0, at = first, parity ^= 1;
     }
 };
 
