@@ -77,31 +77,25 @@ nvfp4_status check_operand(fp4_format fmt, const fp4_operand* o, int64_t rows, i
     return NVFP4_OK;
 }
 
-Operand operand(const fp4_operand* o, int64_t rows) { return Operand{o->codes, o->sf, o->S, rows, 0}; }
-Operand dense(const void* p, const float* S, int64_t rows, int64_t ld) { return Operand{p, nullptr, S, rows, ld}; }
+Operand operand(const fp4_operand* o, int64_t rows) { return Operand{o->codes, o->sf, o->S, rows, 0, 0}; }
 
 nvfp4_status result(cudaError_t e) {
     return e == cudaSuccess ? NVFP4_OK : e == cudaErrorNotSupported ? NVFP4_ERR_UNSUPPORTED : NVFP4_ERR_CUDA;
 }
 
-// A bf16 product for a gradient: out[t][n] = S sum_k q[t][k] p[n][k].
-// With out2, q holds two matrices of qrows rows, the second from row2 on, and their products go to out and out2.
-cudaError_t grad_product(const void* p, int64_t prows, int64_t ldp, const void* q, int64_t qrows, int64_t ldq,
-                         int64_t k, const float* S, void* out, int64_t ldo, int* status, int sms, cudaStream_t s,
-                         void* out2 = nullptr, int64_t row2 = 0) {
+// A bf16 product for a gradient: out[t][n] = S sum_k q[t][k] p[k][n].
+Product grad_product(const void* p, int64_t n, int64_t ldp, const float* S, const void* q, int64_t qrows, int64_t ldq,
+                     int along, int64_t k, void* out, int64_t ldo, int* status) {
     Product g = {};
     g.kind = kBf16;
     g.mode = kPlain;
-    g.p = dense(p, S, prows, ldp);
-    g.q = dense(q, nullptr, out2 ? row2 + qrows : qrows, ldq);
+    g.p = Operand{p, nullptr, S, n, ldp, 1};
+    g.q = Operand{q, nullptr, nullptr, qrows, ldq, along};
     g.k = k;
     g.out = out;
-    g.out2 = out2;
-    g.row2 = row2;
-    g.rows1 = qrows;
     g.ldo = ldo;
     g.status = status;
-    return launch_product(g, sms, s);
+    return g;
 }
 
 // Parts of a workspace, each to a multiple of 256 bytes.
@@ -116,21 +110,19 @@ struct Parts {
     }
 };
 
-// bf16 buffers of fp4_matmul_backward: B and A transposed, dD transposed and re-pitched.
+// bf16 buffers of fp4_matmul_backward: the values of B and A, and dD where TMA cannot read its rows.
 struct MatmulGrad {
-    int64_t ldm, ldn, bt, at, dt, dp;
-    MatmulGrad(int64_t m, int64_t n, int64_t k)
-        : ldm(up(m, 8)), ldn(up(n, 8)), bt(k * ldn * 2), at(k * ldm * 2), dt(n * ldm * 2), dp(m * ldn * 2) {}
-    size_t bytes() const { return (size_t)(up(bt, 256) + up(at, 256) + up(dt, 256) + up(dp, 256)); }
+    int64_t ldn, b, a, d;
+    MatmulGrad(int64_t m, int64_t n, int64_t k) : ldn(up(n, 8)), b(n * k * 2), a(m * k * 2), d(m * ldn * 2) {}
+    size_t bytes() const { return (size_t)(up(b, 256) + up(a, 256) + up(d, 256)); }
 };
 
-// and of fp4_gated_ff_backward: both weights side by side transposed, x transposed, dg and
-// du side by side and transposed.
+// and of fp4_gated_ff_backward: the values of both weights, one after the other (gate's rows up to a
+// multiple of 128), and of x; dg and du side by side.
 struct GatedGrad {
-    int64_t fp, ldt, wt, xt, dgu, dgut;
-    GatedGrad(int64_t t, int64_t f, int64_t d)
-        : fp(up(f, 128)), ldt(up(t, 8)), wt(d * 2 * fp * 2), xt(d * ldt * 2), dgu(t * 2 * fp * 2), dgut(2 * fp * ldt * 2) {}
-    size_t bytes() const { return (size_t)(up(wt, 256) + up(xt, 256) + up(dgu, 256) + up(dgut, 256)); }
+    int64_t fp, w, x, dgu;
+    GatedGrad(int64_t t, int64_t f, int64_t d) : fp(up(f, 128)), w(2 * fp * d * 2), x(t * d * 2), dgu(t * 2 * fp * 2) {}
+    size_t bytes() const { return (size_t)(up(w, 256) + up(x, 256) + up(dgu, 256)); }
 };
 
 }  // namespace
@@ -268,23 +260,22 @@ nvfp4_status fp4_matmul_backward(fp4_format fmt, const fp4_operand* a, const fp4
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int mx = fmt == FP4_FMT_MXFP4;
     Parts ws(workspace);
-    void *bt = ws.take(g.bt), *at = ws.take(g.at), *dt = ws.take(g.dt), *dp = ws.take(g.dp);
+    void *bv = ws.take(g.b), *av = ws.take(g.a), *dv = ws.take(g.d);
+    const void* d = dD;
+    int64_t ldd = lddd;
     cudaError_t e = cudaSuccess;
-    if (dA) {
-        const void* q = dD;
-        int64_t ldq = lddd;
-        if (!aligned(dD, 16) || lddd % 8 != 0) {             // rows that TMA cannot read
-            e = launch_repitch_bf16(dD, m, n, lddd, dp, g.ldn, s);
-            q = dp;
-            ldq = g.ldn;
-        }
-        if (e == cudaSuccess) e = launch_expand_t(mx, b->codes, b->sf, nullptr, nullptr, n, k, g.ldn, bt, g.ldn, s);
-        if (e == cudaSuccess) e = grad_product(bt, k, g.ldn, q, m, ldq, n, b->S, dA, ldda, status_dev, sms, s);
+    if (!aligned(dD, 16) || lddd % 8 != 0) {                 // rows that TMA cannot read
+        e = launch_repitch_bf16(dD, m, n, lddd, dv, g.ldn, s);
+        d = dv;
+        ldd = g.ldn;
+    }
+    if (dA && e == cudaSuccess) {
+        e = launch_expand(mx, b->codes, b->sf, nullptr, nullptr, n, k, n, bv, s);
+        if (e == cudaSuccess) e = launch_product(grad_product(bv, k, k, b->S, d, m, ldd, 0, n, dA, ldda, status_dev), sms, s);
     }
     if (dB && e == cudaSuccess) {
-        e = launch_transpose_bf16(dD, m, n, lddd, dt, g.ldm, s);
-        if (e == cudaSuccess) e = launch_expand_t(mx, a->codes, a->sf, nullptr, nullptr, m, k, g.ldm, at, g.ldm, s);
-        if (e == cudaSuccess) e = grad_product(at, k, g.ldm, dt, n, g.ldm, m, a->S, dB, lddb, status_dev, sms, s);
+        e = launch_expand(mx, a->codes, a->sf, nullptr, nullptr, m, k, m, av, s);
+        if (e == cudaSuccess) e = launch_product(grad_product(av, k, k, a->S, d, n, ldd, 1, m, dB, lddb, status_dev), sms, s);
     }
     return result(e);
 }
@@ -368,10 +359,7 @@ nvfp4_status fp4_gated_ff_backward(fp4_format fmt, fp4_activation act, const fp4
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int mx = fmt == FP4_FMT_MXFP4;
     Parts ws(workspace);
-    uint16_t* wt = static_cast<uint16_t*>(ws.take(g.wt));
-    void* xt = ws.take(g.xt);
-    void* dgu = ws.take(g.dgu);
-    uint16_t* dgut = static_cast<uint16_t*>(ws.take(g.dgut));
+    void *wv = ws.take(g.w), *xv = ws.take(g.x), *dgu = ws.take(g.dgu);
 
     Product p = {};
     p.kind = mx ? kMxfp4 : kNvfp4;
@@ -385,21 +373,26 @@ nvfp4_status fp4_gated_ff_backward(fp4_format fmt, fp4_activation act, const fp4
     p.ldo = ldh;
     p.dh = dh;
     p.lddh = lddh;
-    p.dgu = d_x ? dgu : nullptr;
-    p.dgu_t = d_gate ? dgut : nullptr;
+    p.dgu = dgu;
     p.fp = g.fp;
-    p.ldt = g.ldt;
     p.status = status_dev;
     cudaError_t e = launch_product(p, sms, s);
     if (d_x && e == cudaSuccess) {
-        e = launch_expand_t(mx, w_gate->codes, w_gate->sf, w_up->codes, w_up->sf, f, d, g.fp, wt, 2 * g.fp, s);
-        if (e == cudaSuccess)
-            e = grad_product(wt, d, 2 * g.fp, dgu, t, 2 * g.fp, 2 * g.fp, nullptr, d_x, lddx, status_dev, sms, s);
+        e = launch_expand(mx, w_gate->codes, w_gate->sf, w_up->codes, w_up->sf, f, d, g.fp, wv, s);
+        // gate's half of the contraction and up's have a global scale each
+        Product q = grad_product(wv, d, d, w_gate->S, dgu, t, 2 * g.fp, 0, 2 * g.fp, d_x, lddx, status_dev);
+        q.p2.S = w_up->S;
+        if (!mx) q.k_part = g.fp;
+        if (e == cudaSuccess) e = launch_product(q, sms, s);
     }
     if (d_gate && e == cudaSuccess) {
-        e = launch_expand_t(mx, x->codes, x->sf, nullptr, nullptr, t, d, g.ldt, xt, g.ldt, s);
-        if (e == cudaSuccess)
-            e = grad_product(xt, d, g.ldt, dgut, f, g.ldt, t, x->S, d_gate, lddw, status_dev, sms, s, d_up, g.fp);
+        e = launch_expand(mx, x->codes, x->sf, nullptr, nullptr, t, d, t, xv, s);
+        // one product for both: dg's columns of dgu are its rows 0.. , du's its rows fp..
+        Product q = grad_product(xv, d, d, x->S, dgu, g.fp + f, 2 * g.fp, 1, t, d_gate, lddw, status_dev);
+        q.out2 = d_up;
+        q.row2 = g.fp;
+        q.rows1 = f;
+        if (e == cudaSuccess) e = launch_product(q, sms, s);
     }
     return result(e);
 }

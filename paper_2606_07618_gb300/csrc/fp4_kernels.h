@@ -11,14 +11,11 @@ cudaError_t launch_mxfp4_quantize(const void* x, int dtype, int64_t rows, int64_
                                   uint8_t* sf_linear, uint8_t* sf_swizzled, int* status, int sms, cudaStream_t s);
 cudaError_t launch_mxfp4_dequantize(const uint8_t* codes, const uint8_t* sf, int swizzled, int64_t rows, int64_t cols,
                                     void* out, int dtype, int sms, cudaStream_t s);
-// out[c][r] = bf16(q * s) of a quantised matrix (without S), exact; rows r in [rows,
-// rows_out) are written as zero.  A second matrix of the same size (or null) goes to
-// out[c][rows_out + r].  out row stride ld (a multiple of 8), 16-byte aligned.
-cudaError_t launch_expand_t(int mx, const uint8_t* codes, const uint8_t* sf, const uint8_t* codes2, const uint8_t* sf2,
-                            int64_t rows, int64_t cols, int64_t rows_out, void* out, int64_t ld, cudaStream_t s);
-// out[c][r] = in[r][c], bf16; in row stride ldi, out row stride ldo (a multiple of 8).
-cudaError_t launch_transpose_bf16(const void* in, int64_t rows, int64_t cols, int64_t ldi, void* out, int64_t ldo,
-                                  cudaStream_t s);
+// out[r][c] = bf16(q * s) of a quantised matrix (without S), exact, 32-byte aligned; rows in
+// [rows, rows_out) are written as zero.  A second matrix of the same size (or null) goes to rows
+// rows_out and on.
+cudaError_t launch_expand(int mx, const uint8_t* codes, const uint8_t* sf, const uint8_t* codes2, const uint8_t* sf2,
+                          int64_t rows, int64_t cols, int64_t rows_out, void* out, cudaStream_t s);
 // out[r][c] = in[r][c], bf16, for an input that TMA cannot read.
 cudaError_t launch_repitch_bf16(const void* in, int64_t rows, int64_t cols, int64_t ldi, void* out, int64_t ldo,
                                 cudaStream_t s);
@@ -27,19 +24,20 @@ cudaError_t launch_repitch_bf16(const void* in, int64_t rows, int64_t cols, int6
 enum { kNvfp4 = 0, kMxfp4 = 1, kBf16 = 2 };                  // operand kinds of a product
 enum { kPlain = 0, kGated = 1, kGatedGrad = 2 };             // what the epilogue makes of the accumulators
 
-// An operand of a product, rows along its K-major storage.
+// An operand of a product.
 struct Operand {
-    const void* data;      // packed codes [rows, k/2], or bf16 [rows, ld]
+    const void* data;      // packed codes [rows, k/2]; bf16 [rows][ld], K along the row, or with `along` [k][ld]
     const uint8_t* sf;     // 128x4-atom scales; null for bf16
     const float* S;        // global scale or null
     int64_t rows, ld;      // ld: row stride in elements (bf16 only)
+    int along;             // bf16: rows are contiguous, K steps by ld (always for p)
 };
 
 // One product: out[t][n] over t < q.rows, n < p.rows, from sums over k of q[t][k] p[n][k].
 struct Product {
     int kind, mode, act;
-    Operand p, p2, q;      // p2: the up projection's weight (gated modes)
-    int64_t k;
+    Operand p, p2, q;      // p2: the up projection's weight (gated modes); bf16: p2.S scales the second part of K
+    int64_t k, k_part;     // bf16: where K's second part begins (a multiple of 64), or 0
     void* out;             // plain: D; gated modes: h (bf16) or null
     void* out2;            // plain: rows from row2 on go here (their own matrix, the size of the first), or null
     int64_t row2, rows1;   // the first one's rows; row2 is a multiple of 128
@@ -48,9 +46,8 @@ struct Product {
     uint8_t *h_codes, *h_sf;   // gated: h in MXFP4, or null
     const void* dh;        // gated grad: gradient of h, bf16
     int64_t lddh;
-    void* dgu;             // gated grad: [t][2 fp] bf16: S_gate * dg, S_up * du (columns past f zero)
-    void* dgu_t;           // gated grad: [2 fp][ldt] bf16: dg, du transposed, or null
-    int64_t fp, ldt;
+    void* dgu;             // gated grad: [t][2 fp] bf16: dg, du (columns past f zero)
+    int64_t fp;
     int* status;
     int starve;            // 1: the waits for the operands run out (self-test)
 };

@@ -28,6 +28,7 @@ namespace {
 constexpr int kEpiWarps = 8;
 constexpr int kThreadsPair = (kEpiWarps + 2) * 32;
 constexpr int kPairStages = 8;                               // at most
+constexpr int kBlock = 64 * kRow;                            // 64 contiguous rows by 64 steps of K, bf16
 constexpr int kPairSmem = 227 * 1024 - 256;                  // of a CTA, less its static part
 
 struct PairParams {
@@ -35,6 +36,7 @@ struct PairParams {
     int64_t k;
     int tiles_t, tiles_n, split, starve;
     int stages, stage, box;                                  // the ring: slots, bytes of one; bytes of a warp's box
+    int along, part;                                         // bf16: q's rows are contiguous; stages of K's first part, or 0
     int width;                                               // columns of a tile (gated: 256, half of them gate's)
     int wide_out, wide_dh, wide_codes;                       // bytes that rows of D or h, dh, codes are aligned to: 32, 16 or fewer
     Epilogue e;
@@ -239,36 +241,8 @@ struct Rows {
                 da[2 * j + 1] *= d1 * u[2 * j + 1];
                 gt[j] = pack2_bf16(da[2 * j], da[2 * j + 1]);
             }
-            if (e.dgu_t) {
-                // two neighbouring tokens of a column in one word: lanes exchange halves
-                const int64_t t2 = tw + (lane & ~1);
-                const bool in = t2 < e.ldt;
-                const uint32_t sel = lane & 1 ? 0x3276 : 0x5410;
-                uint16_t* at = e.dgu_t + (n + (lane & 1)) * e.ldt + t2;
-                uint16_t* at2 = at + e.fp * e.ldt;
-#pragma unroll
-                for (int j = 0; j < 16; j++) {
-                    const uint32_t wg = __byte_perm(gt[j], __shfl_xor_sync(0xFFFFFFFFu, gt[j], 1), sel);
-                    const uint32_t wu = __byte_perm(ut[j], __shfl_xor_sync(0xFFFFFFFFu, ut[j], 1), sel);
-                    if (in) {
-                        *reinterpret_cast<uint32_t*>(at) = wg;
-                        *reinterpret_cast<uint32_t*>(at2) = wu;
-                    }
-                    at += 2 * e.ldt;
-                    at2 += 2 * e.ldt;
-                }
-            }
-            if (e.dgu) {
-                if (KIND == kNvfp4) {                            // times the weights' global scales
-#pragma unroll
-                    for (int j = 0; j < 16; j++) {
-                        gt[j] = pack2_bf16(da[2 * j] * sp, da[2 * j + 1] * sp);
-                        ut[j] = pack2_bf16(g[2 * j] * sp2, g[2 * j + 1] * sp2);
-                    }
-                }
-                put_row<2, 16, true>(gt, 32, box, e.dgu, 2 * e.fp, n, tw, e.fp, e.T);
-                put_row<2, 16, true>(ut, 32, box, e.dgu + e.fp, 2 * e.fp, n, tw, e.fp, e.T);
-            }
+            put_row<2, 16, true>(gt, 32, box, e.dgu, 2 * e.fp, n, tw, e.fp, e.T);
+            put_row<2, 16, true>(ut, 32, box, e.dgu + e.fp, 2 * e.fp, n, tw, e.fp, e.T);
         }
         if (e.out) put_row<2, 16>(hw, P.wide_out, box, e.out, e.ldo, n, tw, e.N, e.T);
         if (MODE == kGated && e.h_codes) {
@@ -377,9 +351,18 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                     const uint32_t st = ring.at, bar = leader_full + 8 * r;
                     if (rank == 0) mbar_expect_tx(full0 + 8 * r, 2 * stage);
                     const int x = (k0 + kc) * (KIND == kBf16 ? 64 : 128);
-                    tma_load_2d_pair(st, &P.q, x, t0, bar);
-                    if (MODE == kPlain)
-                        tma_load_2d_pair(st + C::kOp, &P.p, x, tn * width + (int)rank * (width / 2), bar);
+                    const int n = tn * width + (int)rank * (width / 2);
+                    if (KIND == kBf16 && P.along) {          // 64 rows by 64 steps of K, twice
+                        tma_load_2d_pair(st, &P.q, t0, x, bar);
+                        tma_load_2d_pair(st + kBlock, &P.q, t0 + 64, x, bar);
+                    } else {
+                        tma_load_2d_pair(st, &P.q, x, t0, bar);
+                    }
+                    if (KIND == kBf16) {
+                        tma_load_2d_pair(st + C::kOp, &P.p, n, x, bar);
+                        if (width > 128) tma_load_2d_pair(st + C::kOp + kBlock, &P.p, n + 64, x, bar);
+                    } else if (MODE == kPlain)
+                        tma_load_2d_pair(st + C::kOp, &P.p, x, n, bar);
                     else
                         tma_load_2d_pair(st + C::kOp, rank == swap ? &P.p : &P.p2, x, tn * 128, bar);
                     if (KIND != kBf16) {
@@ -412,14 +395,15 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                 }
         if (!ok && lane == 0) atomicOr(&s_abort, 1);
     } else if (warp == kEpiWarps + 1 && rank == 0) {
-        const uint32_t id = idesc(KIND, 256, width);
+        const uint32_t id = idesc(KIND, 256, width) | (KIND == kBf16 ? kAlongB | (P.along ? kAlongA : 0u) : 0u);
+        const int second = KIND == kBf16 && P.part ? P.part - k0 : 1 << 30;    // the first stage of K's second part
         Ring ring(smem_u32(base));
         int it = 0;
         bool ok = true;
         for (int i = first; ok && i < ntiles; i += step, it++) {
             if (it > 0 && !mbar_wait_warp(drained0 + 8 * ((it - 1) & 1), ((it - 1) >> 1) & 1)) ok = false;
             tc_fence_after();
-            const uint32_t acc = tmem + (it & 1) * C::kAcc1;
+            const uint32_t acc0 = KIND == kBf16 && P.part ? tmem : tmem + (it & 1) * C::kAcc1;
             for (int kc = 0; ok && kc < nst; kc++) {
                 const int r = ring.slot;
                 if (!mbar_wait_warp(full0 + 8 * r, ring.parity)) {
@@ -440,9 +424,16 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                     for (int kk = 0; kk < 4; kk++) {
                         if (kk >= left) break;
                         const int a = KIND == kNvfp4 ? kk : kk >> 1;
-                        mma<KIND, 2>(acc, smem_desc(st + kk * 32, 16, 1024), smem_desc(st + C::kOp + kk * 32, 16, 1024),
-                                     KIND == kMxfp4 ? id | sf_id(2 * (kk & 1)) : id, (uint32_t)(kc | kk), tmem + C::kSf + 4 * a,
-                                     tmem + C::kSf + 16 + 8 * a);
+                        if (KIND == kBf16) {
+                            // contiguous rows: 16 steps of K are 16 rows of 128 bytes, 64 rows a block
+                            const uint64_t ad = P.along ? smem_desc(st + kk * 16 * kRow, kBlock, 1024) : smem_desc(st + kk * 32, 16, 1024);
+                            mma<KIND, 2>(kc >= second ? acc0 + 256 : acc0, ad, smem_desc(st + C::kOp + kk * 16 * kRow, kBlock, 1024), id,
+                                         (uint32_t)((kc != 0 && kc != second) | kk), 0, 0);
+                        } else {
+                            mma<KIND, 2>(acc0, smem_desc(st + kk * 32, 16, 1024), smem_desc(st + C::kOp + kk * 32, 16, 1024),
+                                         KIND == kMxfp4 ? id | sf_id(2 * (kk & 1)) : id, (uint32_t)(kc | kk), tmem + C::kSf + 4 * a,
+                                         tmem + C::kSf + 16 + 8 * a);
+                        }
                     }
                     commit_pair(empty0 + 8 * r, leader);
                     if (kc == nst - 1) commit_pair(accf0 + 8 * (it & 1), leader);
@@ -455,10 +446,24 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
     } else if (warp < kEpiWarps) {
         const Epilogue& e = P.e;
         const int half = warp >> 2, q = warp & 3;
-        Rows rows{e, P, smem_u32(base) + (uint32_t)(stages * stage + warp * P.box), scale_or_1(e.s_p), MODE != kPlain ? scale_or_1(e.s_p2) : 1.0f,
+        Rows rows{e, P, smem_u32(base) + (uint32_t)(stages * stage + warp * P.box), scale_or_1(e.s_p), scale_or_1(e.s_p2),
                   scale_or_1(e.s_q), lane};
         rows.bad = false;
         bool lost = false;                                   // a wait ran out
+        // two parts of K, an accumulator and a scale each: added here, 32 columns at a time
+        const bool parts = KIND == kBf16 && P.part;
+        const float part0 = rows.sp, part1 = rows.sp2;
+        if (parts) rows.sp = 1.0f;
+        auto add_parts = [&](uint32_t at, float (&v)[32]) {
+            float w[32];
+            const bool a = !SPLIT || k0 < P.part, b = !SPLIT || k0 + nst > P.part;   // those this pair has
+            if (a) tmem_ld32(at, v);
+            if (b) tmem_ld32(at + 256, w);
+            if (a) tmem_wait32(v);
+            if (b) tmem_wait32(w);
+#pragma unroll
+            for (int j = 0; j < 32; j++) v[j] = (a ? v[j] * part0 : 0.0f) + (b ? w[j] * part1 : 0.0f);
+        };
         const uint32_t leader_drained = at_rank(drained0, leader);
         int it = 0;
         for (int i = first; i < ntiles; i += step, it++) {
@@ -473,7 +478,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                 __syncwarp();
                 if (lane == 0) arrive_at(leader_drained + 8 * b);
             };
-            if (!overlap) release();                         // done with the tile before
+            if (!overlap && !parts) release();               // done with the tile before
             uint32_t dhw[2][16];
             const int64_t n0 = MODE == kPlain ? (int64_t)tn * width : (int64_t)tn * 128 + 64 * half;
             if (MODE == kGatedGrad && !SPLIT) {              // asked for before the accumulators are waited for
@@ -486,16 +491,29 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                 break;
             }
             tc_fence_after();
-            const uint32_t acc = tmem + b * C::kAcc1 + ((uint32_t)(32 * q) << 16);
+            const uint32_t acc = tmem + (parts ? 0 : b * C::kAcc1) + ((uint32_t)(32 * q) << 16);
             if (SPLIT) {                                     // sums to shared memory, in the ring's place: all its stages are read
                 float* red = reinterpret_cast<float*>(base) + 32 * q + lane;
 #pragma unroll 1
                 for (int c = 0; c < 128 && 128 * half + c < width; c += 32) {
                     float v[32];
-                    tmem_ld32(acc + 128 * half + c, v);
-                    tmem_wait32(v);
+                    if (parts) {
+                        add_parts(acc + 128 * half + c, v);
+                    } else {
+                        tmem_ld32(acc + 128 * half + c, v);
+                        tmem_wait32(v);
+                    }
 #pragma unroll
                     for (int j = 0; j < 32; j++) red[(128 * half + c + j) * 128] = v[j];
+                }
+            } else if (MODE == kPlain && KIND == kBf16 && parts) {
+                const int mid = (width + 32) / 64 * 32, end = half == 0 ? mid : width;
+#pragma unroll 1
+                for (int col = mid * half; col < end; col += 32) {
+                    float v[32];
+                    add_parts(acc + col, v);
+                    if (col + 32 >= end) release();          // both accumulators are this tile's
+                    rows.plain(v, n0 + col);
                 }
             } else if (MODE == kPlain) {
                 // the columns of this half of the warps, 64 at a time, the overlapping ones first
@@ -603,8 +621,12 @@ int row_alignment(const void* p, int64_t stride_bytes) {
     return bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 1;
 }
 
-// A slot of the ring: 128 rows of tokens, half a tile's columns, their scales.  A multiple of 1024.
-int stage_bytes(int kind, int width) { return (128 + width / 2) * kRow + (width > 128 ? 3 : 2) * atoms(kind) * kAtom; }
+// A slot of the ring: 128 rows of tokens, half a tile's columns (bf16: in blocks of 64), their
+// scales.  A multiple of 1024.
+int stage_bytes(int kind, int width) {
+    if (kind == kBf16) return (width > 128 ? 4 : 3) * kBlock;
+    return (128 + width / 2) * kRow + (width > 128 ? 3 : 2) * atoms(kind) * kAtom;
+}
 // A warp's box: 32 x 32 elements of a result whose rows allow no wide store.
 int box_bytes(const Product& p) { return p.out_f32 ? 4096 : 2048; }
 int ring_slots(const Product& p, int width) {
@@ -624,6 +646,8 @@ cudaError_t launch_pair_as(const Product& p, int width, int split, int sms, cuda
                                        (MODE == kPlain || make_scale_map(&P.sp2, p.p2, KIND, p.k))));
     if (!ok) return cudaErrorNotSupported;
     P.k = p.k;
+    P.along = p.q.along;
+    P.part = (int)(p.k_part / stage_k(KIND));
     P.e = make_epilogue(p);
     P.wide_out = row_alignment(p.out, p.ldo * (p.out_f32 ? 4 : 2));
     if (p.out2 && row_alignment(p.out2, 0) < P.wide_out) P.wide_out = row_alignment(p.out2, 0);
@@ -678,7 +702,7 @@ struct Plan {
 };
 Plan plan(const Product& p, int sms) {
     const int64_t pairs = sms / 2, tiles_t = (p.q.rows + 255) / 256, nst = (p.k + stage_k(p.kind) - 1) / stage_k(p.kind);
-    const int least = p.mode != kPlain ? 256 : p.kind == kBf16 ? 64 : 128, step = p.kind == kBf16 ? 32 : 128;
+    const int least = p.mode != kPlain ? 256 : 128, step = p.kind == kBf16 ? 32 : 128;
     Plan best;
     int64_t least_cost = INT64_MAX;
     for (int w = 256; w >= least; w -= step) {

@@ -24,12 +24,14 @@ constexpr int kRow = 128;                                    // bytes of an oper
 // Instruction descriptor.  kind::f16: D fp32 (bits 4-5 = 1), A and B bf16 (7-9, 10-12 =
 // 1), N >> 3 (17-22), M >> 4 (24-28).  kind::mxf4nvf4: A and B E2M1 (7-9, 10-12 = 1), N >> 3
 // (17-22), scales UE4M3 = 0 or UE8M0 = 1 (23), M >> 7 (27-28), which of a cell's scale
-// bytes the MMA takes for B (4-5) and A (29-30).  All operands K-major, K = 32 bytes.
+// bytes the MMA takes for B (4-5) and A (29-30).  Operands K-major but where bits 15 (A) and 16 (B)
+// say otherwise, K = 32 bytes.
 __host__ __device__ constexpr uint32_t idesc(int kind, int m, int n) {
     return kind == kBf16 ? (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24)
                          : (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (kind == kMxfp4 ? 1u << 23 : 0u) |
                                ((uint32_t)(m >> 7) << 27);
 }
+constexpr uint32_t kAlongA = 1u << 15, kAlongB = 1u << 16;
 __host__ __device__ constexpr uint32_t sf_id(uint32_t id) { return id << 4 | id << 29; }
 
 // Descriptor of a 512-byte scale atom for tcgen05.cp: no swizzle, 16-byte rows, 8-row
@@ -184,8 +186,8 @@ struct Epilogue {
     uint32_t h_kpad4;
     const uint16_t* dh;
     int64_t lddh;
-    uint16_t *dgu, *dgu_t;
-    int64_t fp, ldt;
+    uint16_t* dgu;
+    int64_t fp;
     int* status;
 };
 
@@ -242,9 +244,10 @@ inline bool make_operand_map(CUtensorMap* m, const Operand& o, int kind, int64_t
     const EncodeTiledFn enc = encode_fn();
     if (!enc) return false;
     const bool bf = kind == kBf16;
-    const cuuint64_t dims[2] = {(cuuint64_t)(bf ? k : k / 2), (cuuint64_t)o.rows};
+    // K along the row: boxes of 128 bytes of K by box_rows; else 64 rows by 64 steps of K
+    const cuuint64_t dims[2] = {(cuuint64_t)(!bf ? k / 2 : o.along ? o.rows : k), (cuuint64_t)(o.along ? k : o.rows)};
     const cuuint64_t strides[1] = {(cuuint64_t)(bf ? 2 * o.ld : k / 2)};
-    const cuuint32_t box[2] = {bf ? 64u : 128u, box_rows};
+    const cuuint32_t box[2] = {bf ? 64u : 128u, o.along ? 64u : box_rows};
     const cuuint32_t es[2] = {1, 1};
     return enc(m, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(o.data), dims,
                strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -285,9 +288,7 @@ inline Epilogue make_epilogue(const Product& p) {
     e.dh = static_cast<const uint16_t*>(p.dh);
     e.lddh = p.lddh;
     e.dgu = static_cast<uint16_t*>(p.dgu);
-    e.dgu_t = static_cast<uint16_t*>(p.dgu_t);
     e.fp = p.fp;
-    e.ldt = p.ldt;
     e.status = p.status;
     return e;
 }

@@ -1,6 +1,5 @@
 // MXFP4 (E2M1 elements, one power-of-two E8M0 scale for each block of 32): quantisation
-// and dequantisation, and the layout kernels of the gradients, which multiply bf16 by
-// the values of a quantised matrix along its rows.
+// and dequantisation, and the expansion to bf16 of the operands that gradients are formed with.
 //
 // All of them are bound by memory: a few instructions per element, each byte once.
 #include <cuda_bf16.h>
@@ -192,95 +191,49 @@ __global__ void __launch_bounds__(256)
 }
 
 // ---------------------------------------------------------------------------
-// The values of a quantised matrix without S, transposed, in bf16: exact, as q has two
-// significant bits and an E4M3 scale four.  A tile of 64 rows by 128 columns goes through
-// shared memory: a thread reads 32 codes of a row and writes them down the columns, so that a
-// warp's 32 rows are neighbours there (with a row's words to neighbouring lanes the writes
-// met in four banks, 40 us for 14336 x 4096 now 26); then 128 bytes a column go out.
-// blockIdx.z: one of two matrices of the same size, the second's rows `rows_out` further on.
+// The values of a quantised matrix without S in bf16: exact, as q has two significant bits and
+// an E4M3 scale four.  16 codes to a lane, 32 bytes out; four in flight (blockIdx.y: one of two
+// matrices of the same size, the second's rows further on).
 template <int MX>
 __global__ void __launch_bounds__(256)
-    expand_t_kernel(const uint8_t* codes, const uint8_t* sf, const uint8_t* codes2, const uint8_t* sf2, int64_t rows, int64_t cols,
-                    int64_t rows_out, uint32_t kpad4, uint16_t* out, int64_t ld) {
-    __shared__ uint16_t tile[128][66];                       // [column][row]; 33 words to a column
+    expand_kernel(const uint8_t* codes, const uint8_t* sf, const uint8_t* codes2, const uint8_t* sf2, uint32_t segs,
+                  uint32_t segs_out, uint32_t row_segs, uint32_t kpad4, FastDiv div, uint4* out) {
+    constexpr int kUnroll = 4;
     grid_dependency_wait();
-    if (blockIdx.z == 1) {
+    if (blockIdx.y == 1) {
         codes = codes2;
         sf = sf2;
-        out += rows_out;
+        out += 2 * (int64_t)segs_out;
     }
-    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 128;
-    const int r = threadIdx.x & 63, q = threadIdx.x >> 6;
-    const int64_t row = r0 + r, col = c0 + 32 * q;
-    uint4 c = make_uint4(0, 0, 0, 0);
-    float v[2] = {0.0f, 0.0f};
-    if (row < rows && col < cols) {                          // cols is a multiple of 32
-        c = *reinterpret_cast<const uint4*>(codes + row * (cols / 2) + col / 2);
-        if (MX) {
-            v[0] = v[1] = e8m0_value(sf[swizzle_offset(row, col / 32, kpad4)]);
-        } else {                                             // an even scale column and the next: one word's halves
-            const uint32_t two = *reinterpret_cast<const uint16_t*>(sf + swizzle_offset(row, col / 16, kpad4));
-            v[0] = f16bits_to_f32(e4m3_to_f16bits(two & 0xFF));
-            v[1] = f16bits_to_f32(e4m3_to_f16bits(two >> 8));
+    const uint32_t s0 = (blockIdx.x * blockDim.x + (threadIdx.x & ~31u)) * kUnroll + (threadIdx.x & 31);
+    uint2 c[kUnroll];
+    uint32_t s[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; u++) {
+        const uint32_t seg = s0 + 32 * u;
+        c[u] = make_uint2(0, 0);
+        s[u] = MX ? 127 : 0;                                 // rows past the matrix: zero codes
+        if (seg < segs) {
+            const uint32_t row = div_by(seg, div), k = seg - row * row_segs;
+            c[u] = reinterpret_cast<const uint2*>(codes)[seg];
+            s[u] = sf[swizzle_offset(row, MX ? k >> 1 : k, kpad4)];
         }
     }
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
-    for (int j = 0; j < 16; j++) {
-        float a, b;
-        e2m1_pair(w[j >> 2] >> (8 * (j & 3)), a, b);
-        const uint32_t two = pack_bf16(__fmul_rn(a, v[j >> 3]), __fmul_rn(b, v[j >> 3]));
-        tile[32 * q + 2 * j][r] = (uint16_t)two;
-        tile[32 * q + 2 * j + 1][r] = (uint16_t)(two >> 16);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const int x = i * 256 + threadIdx.x, cc = x >> 3, g = x & 7;    // 8 rows (16 bytes) of a column
-        const int64_t ocol = c0 + cc, orow = r0 + 8 * g;
-        if (ocol >= cols || orow >= rows_out) continue;
-        const uint32_t* t = reinterpret_cast<const uint32_t*>(&tile[cc][8 * g]);
-        // ld is a multiple of 8 and at least rows_out: the whole 16 bytes lie in the row
-        *reinterpret_cast<uint4*>(out + ocol * ld + orow) = make_uint4(t[0], t[1], t[2], t[3]);
-    }
-}
-
-// A transpose of 64 x 64 tiles, laid out as above: a thread has 16 elements of a row.
-template <int LOAD>
-__global__ void __launch_bounds__(256)
-    transpose_bf16_kernel(const uint16_t* in, int64_t rows, int64_t cols, int64_t ldi, uint16_t* out, int64_t ldo) {
-    __shared__ uint16_t tile[64][66];                        // [column][row]
-    grid_dependency_wait();
-    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
-    const int r = threadIdx.x & 63, q = threadIdx.x >> 6;
-    const int64_t row = r0 + r, col = c0 + 16 * q;
-    const uint16_t* at = in + row * ldi + col;
-    if (LOAD != kElement && row < rows && col + 16 <= cols) {
-        uint4 v[2];
-        if (LOAD == kWide) {
-            ld_stream32<false>(at, v[0], v[1]);
-        } else {
-            v[0] = ld_stream16<false>(at);
-            v[1] = ld_stream16<false>(at + 8);
-        }
-        const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+    for (int u = 0; u < kUnroll; u++) {
+        const uint32_t seg = s0 + 32 * u;
+        if (seg >= segs_out) break;
+        const float v = MX ? e8m0_value(s[u]) : f16bits_to_f32(e4m3_to_f16bits(s[u]));
+        uint32_t w[8];
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-            tile[16 * q + 2 * j][r] = (uint16_t)w[j];
-            tile[16 * q + 2 * j + 1][r] = (uint16_t)(w[j] >> 16);
+            float a, b;
+            e2m1_pair((j < 4 ? c[u].x : c[u].y) >> (8 * (j & 3)), a, b);
+            w[j] = pack_bf16(__fmul_rn(a, v), __fmul_rn(b, v));
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 16; j++) tile[16 * q + j][r] = row < rows && col + j < cols ? at[j] : (uint16_t)0;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const int w = i * 256 + threadIdx.x, c = w >> 3, g = w & 7;
-        const int64_t ocol = c0 + c, orow = r0 + 8 * g;
-        if (ocol >= cols || orow >= ldo) continue;
-        const uint32_t* t = reinterpret_cast<const uint32_t*>(&tile[c][8 * g]);
-        *reinterpret_cast<uint4*>(out + ocol * ldo + orow) = make_uint4(t[0], t[1], t[2], t[3]);
+        uint4* at = out + 2 * (int64_t)seg;
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
     }
 }
 
@@ -363,23 +316,29 @@ cudaError_t launch_mxfp4_dequantize(const uint8_t* codes, const uint8_t* sf, int
     return cudaSuccess;
 }
 
-cudaError_t launch_expand_t(int mx, const uint8_t* codes, const uint8_t* sf, const uint8_t* codes2, const uint8_t* sf2,
-                            int64_t rows, int64_t cols, int64_t rows_out, void* out, int64_t ld, cudaStream_t s) {
-    const dim3 grid((unsigned)((cols + 127) / 128), (unsigned)((rows_out + 63) / 64), codes2 ? 2u : 1u);
-    const uint32_t kpad4 = (uint32_t)((cols / (mx ? 32 : 16) + 3) / 4);
-    return launch_grid(mx ? expand_t_kernel<1> : expand_t_kernel<0>, grid, 256, s, codes, sf, codes2, sf2, rows, cols, rows_out,
-                       kpad4, static_cast<uint16_t*>(out), ld);
-}
-
-cudaError_t launch_transpose_bf16(const void* in, int64_t rows, int64_t cols, int64_t ldi, void* out, int64_t ldo,
-                                  cudaStream_t s) {
-    const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)((rows + 63) / 64));
-    const uintptr_t bits = reinterpret_cast<uintptr_t>(in) | (uintptr_t)(ldi * 2);
-    return launch_grid((bits & 31) == 0   ? transpose_bf16_kernel<kWide>
-                       : (bits & 15) == 0 ? transpose_bf16_kernel<kHalf>
-                                          : transpose_bf16_kernel<kElement>,
-                       grid, 256, s, static_cast<const uint16_t*>(in), rows, cols, ldi,
-                       static_cast<uint16_t*>(out), ldo);
+cudaError_t launch_expand(int mx, const uint8_t* codes, const uint8_t* sf, const uint8_t* codes2, const uint8_t* sf2,
+                          int64_t rows, int64_t cols, int64_t rows_out, void* out, cudaStream_t s) {
+    const uint32_t row_segs = (uint32_t)(cols / 16), kpad4 = (uint32_t)((cols / (mx ? 32 : 16) + 3) / 4);
+    const FastDiv div = make_fast_div(row_segs);
+    // segments are counted in 32 bits: rows in groups of whole 128, as in quantisation (never with a second matrix
+    // past one group: its place follows from the first's size)
+    const int64_t most = ((int64_t)1 << 30) / row_segs / 128 * 128, group = most > 0 ? most : 128;
+    const int pair = codes2 && rows_out <= group;
+    for (int m = 0; m < (codes2 && !pair ? 2 : 1); m++) {
+        char* to = static_cast<char*>(out) + m * rows_out * cols * 2;
+        for (int64_t r = 0; r < rows_out; r += group) {
+            const int64_t n_out = rows_out - r < group ? rows_out - r : group, left = rows - r, n = left < 0 ? 0 : left < n_out ? left : n_out;
+            const int64_t segs_out = n_out * row_segs;
+            const dim3 grid((unsigned)((segs_out + 1023) / 1024), pair ? 2u : 1u);
+            const int64_t co = r * (cols / 2), so = r * kpad4 * 4;
+            const cudaError_t e = launch_grid(mx ? expand_kernel<1> : expand_kernel<0>, grid, 256, s, (m ? codes2 : codes) + co,
+                                              (m ? sf2 : sf) + so, pair ? codes2 + co : nullptr, pair ? sf2 + so : nullptr,
+                                              (uint32_t)(n * row_segs), (uint32_t)segs_out, row_segs, kpad4, div,
+                                              reinterpret_cast<uint4*>(to + r * cols * 2));
+            if (e != cudaSuccess) return e;
+        }
+    }
+    return cudaSuccess;
 }
 
 cudaError_t launch_repitch_bf16(const void* in, int64_t rows, int64_t cols, int64_t ldi, void* out, int64_t ldo,
