@@ -692,8 +692,8 @@ cudaError_t launch_pair_as(const Product& p, int width, int split, int sms, cuda
 }
 
 // How wide a tile is and how many pairs share its K: the least of an estimate in cycles.
-//   A stage takes its MMAs (2 a column) or its loads, 62 bytes a cycle and CTA with most SMs loading,
-//   100 with few, or its share of the latency of HBM; a tile 1500 more, adding up a split K 8000.  Narrow tiles fill the last wave (bf16 in
+//   A stage takes its MMAs (2 a column) or its loads, 55 to 70 bytes a cycle and CTA with most SMs
+//   loading, 100 with few, or its share of the latency of HBM; a tile 1500 more, adding up a split K 8000.  Narrow tiles fill the last wave (bf16 in
 //   steps of 32 columns; scale atoms start at 128 rows, so 4-bit tiles are 256 or 128 wide and gated
 //   ones 256) and shorten what a few tiles take; clusters of four or eight whole SMs have to find
 //   room (at most 36 and 15 on a GB300: 16 of eight ran one after the others).
@@ -703,6 +703,8 @@ struct Plan {
 Plan plan(const Product& p, int sms) {
     const int64_t pairs = sms / 2, tiles_t = (p.q.rows + 255) / 256, nst = (p.k + stage_k(p.kind) - 1) / stage_k(p.kind);
     const int least = p.mode != kPlain ? 256 : 128, step = p.kind == kBf16 ? 32 : 128;
+    // bf16 rows that start inside a 128-byte line take two of L2's
+    const int64_t full_rate = p.kind != kBf16 ? 62 : p.q.ld % 64 == 0 ? 70 : 55;
     Plan best;
     int64_t least_cost = INT64_MAX;
     for (int w = 256; w >= least; w -= step) {
@@ -710,11 +712,11 @@ Plan plan(const Product& p, int sms) {
         const int64_t bytes = stage_bytes(p.kind, w), latency = 2900 / ring_slots(p, w);
         for (int split = 1; split <= 4; split *= 2) {
             if (split > 1 && (w % 128 != 0 || nst < 8 * split || tiles > (split == 2 ? sms / 4 - 2 : sms / 8 - 4))) continue;
-            const int64_t rate = 2 * tiles * split > pairs ? 62 : 100;
+            const int64_t rate = 2 * tiles * split > pairs ? full_rate : 100;
             const int64_t moved = bytes / rate > latency ? bytes / rate : latency, stage = moved > 2 * w ? moved : 2 * w;
             const int64_t waves = split > 1 ? 1 : (tiles + pairs - 1) / pairs;
             const int64_t cost = waves * ((nst + split - 1) / split * stage + 1500) + (split > 1 ? 8000 : 0);
-            if (cost < least_cost) {
+            if (least_cost == INT64_MAX || 32 * cost < 31 * least_cost) {   // not for a difference the estimate cannot see
                 least_cost = cost;
                 best.width = w;
                 best.split = split;

@@ -419,6 +419,26 @@ def test_matmul_backward_against_differences(B):
         assert abs((host(grad) * u).sum() - diff) <= (bound * np.abs(u)).sum() + 1e-9 * abs(diff)
 
 
+@pytest.mark.parametrize("t", [3, 130])
+def test_gated_with_a_zero_weight(B, t):
+    """A gate of zeros, whose global scale is 0 as nvfp4_global_scale gives it: h and d_x are zero, and the
+    gate's own gradient is not lost."""
+    f, d = 160, 96
+    x, wg, wu = gated_operands(t, f, d, R.NV)
+    S = torch.zeros(1, device=DEV)
+    zero = (torch.zeros_like(wg.op[0]), torch.zeros_like(wg.op[1]), S)
+    h = torch.empty(t, f, dtype=torch.bfloat16, device=DEV)
+    B.fp4_gated_ff(R.NV, 0, x.op, zero, wu.op, h)
+    assert not bool(h.any())
+    dh = bf16(np.random.default_rng(4).standard_normal((t, f)))
+    ws = torch.empty(B.fp4_gated_ff_backward_workspace(t, f, d), dtype=torch.uint8, device=DEV)
+    dx, dg, du = (torch.empty(r, d, dtype=torch.bfloat16, device=DEV) for r in (t, f, f))
+    B.fp4_gated_ff_backward(R.NV, 0, x.op, zero, wu.op, dh.to(DEV), dx, dg, du, None, ws)
+    for got, (want, bound) in zip((dx, dg, du), grad_bounds(0, x.v, 0 * wg.v, wu.v, dh.double().numpy(), d)):
+        near(got, want, bound)
+    assert bool(dg.any()) and not bool(dx.any()) and not bool(du.any())
+
+
 # ------------------------------------------------------------------ use
 def test_results_do_not_change_from_run_to_run(B):
     """Split sums are added in a fixed order: the same bits every time."""
