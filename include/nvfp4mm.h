@@ -111,7 +111,8 @@ nvfp4_status fp4_matmul_backward(fp4_format fmt, const fp4_operand* a, const fp4
  *   h        optional [t, f] bf16, row stride ldh.
  *   h_codes, h_sf  optional (both or neither; f % 32 == 0): h in MXFP4, the codes and
  *            128x4-atom scales that mxfp4_quantize gives for the bf16 h, ready to be the
- *            next product's operand.  h_codes 16-byte, h_sf 4-byte aligned.
+ *            next product's operand; status_dev bit 0 as there (a block of h that is not finite).
+ *            h_codes 16-byte, h_sf 4-byte aligned.
  * At least one of the two forms.
  */
 nvfp4_status fp4_gated_ff(fp4_format fmt, fp4_activation act, const fp4_operand* x, const fp4_operand* w_gate,

@@ -54,13 +54,10 @@ __device__ __forceinline__ void cp_atom(uint32_t taddr, uint64_t desc) {
 template <int KIND, int CG>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate, uint32_t sfa,
                                     uint32_t sfb) {
+    static_assert(KIND != kBf16 || CG == 2, "bf16 products are pairs'");
     if (KIND == kBf16) {
-        if (CG == 1)
-            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                         ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
-        else
-            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                         ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
     } else if (KIND == kNvfp4) {
         if (CG == 1)
             asm volatile(MM_MMA("1", "mxf4nvf4.block_scale.scale_vec::4X")
