@@ -8,8 +8,9 @@
 // one row: whole sectors to store, and a block of 32 for MXFP4.  Each CTA
 // loads its 128 token rows and half of the tile's columns; the leader's MMA reads both halves,
 // so a stage of K costs 64 KB of loads for 256 x 256 x 128 bytes of K.  An MMA takes 128 cycles for
-// 32 bytes of K of any type: a stage at least 512, and shared memory, through which its 76 KB come and
-// go, 550 a CTA.  NVFP4, 8192 x 4096 x 14336: 131 us, 7.3 PFLOP/s, 620 cycles a stage; bf16: 515.
+// 32 bytes of K of any type, a stage at least 512.  Shared memory is the bound of 4-bit products: 38
+// KB in, 38 out (operands and scales) at 128 bytes a cycle are 601 cycles a stage for NVFP4, 555 for MXFP4;
+// 8192 x 4096 x 14336 takes 606 and 570 (129 and 122 us, 7.5 and 7.9 PFLOP/s).  bf16: 515, MMAs.
 //
 // bf16 operands come as they lie: K along the rows (dg and du for d_x), or down the rows (values of
 // weights and activations; dg, du for the weights' gradients), then in blocks of 64 contiguous rows by 64
@@ -379,8 +380,7 @@ __global__ void __launch_bounds__(kThreadsPair, 1) pair_kernel(const __grid_cons
                         const int a = (k0 + kc) * atoms(KIND);
                         tma_load_3d_pair(sf, &P.sq, 0, a, t0 >> 7, bar);
                         if (MODE == kPlain) {
-                            tma_load_3d_pair(sf + C::kS, &P.sp, 0, a, tn * (width >> 7), bar);
-                            if (width > 128) tma_load_3d_pair(sf + 2 * C::kS, &P.sp, 0, a, 2 * tn + 1, bar);
+                            tma_load_3d_pair(sf + C::kS, &P.sp, 0, a, tn * (width >> 7), bar);   // one or two atom rows
                         } else {
                             tma_load_3d_pair(sf + C::kS, swap ? &P.sp2 : &P.sp, 0, a, tn, bar);
                             tma_load_3d_pair(sf + 2 * C::kS, swap ? &P.sp : &P.sp2, 0, a, tn, bar);
@@ -651,7 +651,7 @@ cudaError_t launch_pair_as(const Product& p, int width, int split, int sms, cuda
     const int64_t tiles_t = (p.q.rows + 255) / 256;
     const bool ok = make_operand_map(&P.p, p.p, KIND, p.k, MODE == kPlain ? P.width / 2 : 128) && make_operand_map(&P.q, p.q, KIND, p.k, 128) &&
                     (MODE == kPlain || make_operand_map(&P.p2, p.p2, KIND, p.k, 128)) &&
-                    (KIND == kBf16 || (make_scale_map(&P.sp, p.p, KIND, p.k) && make_scale_map(&P.sq, p.q, KIND, p.k) &&
+                    (KIND == kBf16 || (make_scale_map(&P.sp, p.p, KIND, p.k, MODE == kPlain && width > 128 ? 2 : 1) && make_scale_map(&P.sq, p.q, KIND, p.k) &&
                                        (MODE == kPlain || make_scale_map(&P.sp2, p.p2, KIND, p.k))));
     if (!ok) return cudaErrorNotSupported;
     P.k = p.k;
@@ -710,7 +710,7 @@ struct Plan {
     int width = 256, split = 1;
 };
 Plan plan(const Product& p, int sms) {
-    const int64_t pairs = sms / 2, tiles_t = (p.q.rows + 255) / 256, nst = (p.k + stage_k(p.kind) - 1) / stage_k(p.kind);
+    const int64_t pairs = sms > 1 ? sms / 2 : 1, tiles_t = (p.q.rows + 255) / 256, nst = (p.k + stage_k(p.kind) - 1) / stage_k(p.kind);
     const int least = p.mode != kPlain ? 256 : 128, step = p.kind == kBf16 ? 32 : 128;
     // bf16 rows that start inside a 128-byte line take two of L2's
     const int64_t full_rate = p.kind != kBf16 ? 62 : p.q.ld % 64 == 0 ? 70 : 55;

@@ -251,14 +251,14 @@ inline bool make_operand_map(CUtensorMap* m, const Operand& o, int kind, int64_t
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The scale atoms as [row block][atom along K][128 words].
-inline bool make_scale_map(CUtensorMap* m, const Operand& o, int kind, int64_t k) {
+// The scale atoms as [row block][atom along K][128 words], `blocks` of the first to a box.
+inline bool make_scale_map(CUtensorMap* m, const Operand& o, int kind, int64_t k, int blocks = 1) {
     const EncodeTiledFn enc = encode_fn();
     if (!enc) return false;
     const int64_t kb = k / (kind == kMxfp4 ? 32 : 16), k4 = (kb + 3) / 4;
     const cuuint64_t dims[3] = {128, (cuuint64_t)k4, (cuuint64_t)((o.rows + 127) / 128)};
     const cuuint64_t strides[2] = {(cuuint64_t)kAtom, (cuuint64_t)(k4 * kAtom)};
-    const cuuint32_t box[3] = {128, (cuuint32_t)atoms(kind), 1};
+    const cuuint32_t box[3] = {128, (cuuint32_t)atoms(kind), (cuuint32_t)blocks};
     const cuuint32_t es[3] = {1, 1, 1};
     return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<uint8_t*>(o.sf), dims, strides, box, es,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
