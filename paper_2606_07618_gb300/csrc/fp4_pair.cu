@@ -702,10 +702,14 @@ cudaError_t launch_pair_as(const Product& p, int width, int split, int sms, cuda
 
 // How wide a tile is and how many pairs share its K: the least of an estimate in cycles.
 //   A stage takes its MMAs (2 a column) or its loads, 55 to 70 bytes a cycle and CTA with most SMs
-//   loading, 100 with few, or its share of the latency of HBM; a tile 1500 more, adding up a split K 8000.  Narrow tiles fill the last wave (bf16 in
-//   steps of 32 columns; scale atoms start at 128 rows, so 4-bit tiles are 256 or 128 wide and gated
-//   ones 256) and shorten what a few tiles take; clusters of four or eight whole SMs have to find
-//   room (at most 36 and 15 on a GB300: 16 of eight ran one after the others).
+//   loading, 100 with few, or its share of the latency of HBM; a tile 1500 more, adding up a split K
+//   8000.  Narrow tiles fill the last wave (bf16 in steps of 32 columns; scale atoms start at 128 rows,
+//   so 4-bit tiles are 256 or 128 wide and gated ones 256) and shorten what a few tiles take; clusters of
+//   four or eight whole SMs have to find room (at most 36 and 15 on a GB300: 16 of eight ran one
+//   after the others).
+// us, always 256 wide and split from 32 stages on / as estimated: 77 x 1001 x 2080 (fp32) 7.9 / 6.4, 512 x
+// 1024 x 1024 6.0 / 5.1, 256 x 4096 x 14336 17.8 / 15.7, 200 x 512 x 14336 13.4 / 10.8; with gradients 2048
+// x 4096 x 4096 111 / 106.
 struct Plan {
     int width = 256, split = 1;
 };
