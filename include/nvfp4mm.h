@@ -26,6 +26,8 @@
  *     alignment, and run faster with 16-byte aligned bases and row strides.
  *   - Row strides (ld*) are in elements and at least the row's length.
  *   - A call with no rows or no columns of output launches nothing and returns NVFP4_OK.
+ *     A gradient that sums over no rows or columns (no tokens: the weights') is zeros; such
+ *     a call needs no workspace, and tensors without elements may be NULL.
  *   - status_dev: optional device int; bit 16 is OR-ed in when a bounded wait inside a
  *     kernel ran out (about a second; the outputs are then incomplete).
  *   - Outputs must not overlap inputs or each other.

@@ -98,6 +98,30 @@ Product grad_product(const void* p, int64_t n, int64_t ldp, const float* S, cons
     return g;
 }
 
+// Gradients that sum over no rows or no columns: zeros.  A tensor without elements may be null.
+struct ZeroGrad {
+    void* p;
+    int64_t rows, cols, ld;
+};
+template <int N>
+nvfp4_status zero_grads(const ZeroGrad (&g)[N], cudaStream_t s) {
+    Memory mem;
+    for (const ZeroGrad& z : g) {
+        if (!z.p || z.rows == 0) continue;
+        const nvfp4_status st = check_dense(z.p, z.rows, z.cols, z.ld, 2);
+        if (st != NVFP4_OK) return st;
+        mem.write(z.p, Memory::span(z.rows, z.cols, z.ld, 2));
+    }
+    const nvfp4_status st = mem.check();
+    if (st != NVFP4_OK) return st;
+    for (const ZeroGrad& z : g)
+        if (z.p && z.rows > 0) {
+            const cudaError_t e = launch_zero_bf16(z.rows, z.cols, z.p, z.ld, s);
+            if (e != cudaSuccess) return result(e);
+        }
+    return NVFP4_OK;
+}
+
 // Parts of a workspace, each to a multiple of 256 bytes.
 struct Parts {
     char* base;
@@ -239,8 +263,11 @@ nvfp4_status fp4_matmul_backward(fp4_format fmt, const fp4_operand* a, const fp4
     if ((st = check_format(fmt, k)) != NVFP4_OK || (st = check_rows(m)) != NVFP4_OK || (st = check_rows(n)) != NVFP4_OK)
         return st;
     if (k > kMaxRows) return NVFP4_ERR_RANGE;
+    if (m == 0 || n == 0) {
+        const ZeroGrad z[] = {{dA, m, k, ldda}, {dB, n, k, lddb}};
+        return zero_grads(z, static_cast<cudaStream_t>(stream));
+    }
     if (!dA && !dB) return NVFP4_ERR_INVALID_ARG;
-    if (m == 0 || n == 0) return NVFP4_OK;
     const MatmulGrad g(m, n, k);
     Memory mem;
     if ((st = check_operand(fmt, a, m, k, &mem)) != NVFP4_OK || (st = check_operand(fmt, b, n, k, &mem)) != NVFP4_OK ||
@@ -287,9 +314,9 @@ nvfp4_status fp4_gated_ff(fp4_format fmt, fp4_activation act, const fp4_operand*
     if (act != FP4_ACT_SILU && act != FP4_ACT_GELU_TANH) return NVFP4_ERR_INVALID_ARG;
     if ((st = check_format(fmt, d)) != NVFP4_OK || (st = check_rows(t)) != NVFP4_OK || (st = check_rows(f)) != NVFP4_OK)
         return st;
-    if (!h_codes != !h_sf || (!h && !h_codes)) return NVFP4_ERR_INVALID_ARG;
-    if (h_codes && f % 32 != 0) return NVFP4_ERR_INVALID_ARG;
+    if (!h_codes != !h_sf || (h_codes && f % 32 != 0)) return NVFP4_ERR_INVALID_ARG;
     if (t == 0 || f == 0) return NVFP4_OK;
+    if (!h && !h_codes) return NVFP4_ERR_INVALID_ARG;
     Memory mem;
     if ((st = check_operand(fmt, x, t, d, &mem)) != NVFP4_OK || (st = check_operand(fmt, w_gate, f, d, &mem)) != NVFP4_OK ||
         (st = check_operand(fmt, w_up, f, d, &mem)) != NVFP4_OK || (h && (st = check_dense(h, t, f, ldh, 2)) != NVFP4_OK))
@@ -333,8 +360,12 @@ nvfp4_status fp4_gated_ff_backward(fp4_format fmt, fp4_activation act, const fp4
     if ((st = check_format(fmt, d)) != NVFP4_OK || (st = check_rows(t)) != NVFP4_OK || (st = check_rows(f)) != NVFP4_OK)
         return st;
     if (d > kMaxRows) return NVFP4_ERR_RANGE;
-    if (!d_gate != !d_up || (!d_x && !d_gate)) return NVFP4_ERR_INVALID_ARG;
-    if (t == 0 || f == 0) return NVFP4_OK;
+    if (!d_gate != !d_up) return NVFP4_ERR_INVALID_ARG;
+    if (t == 0 || f == 0) {
+        const ZeroGrad z[] = {{d_x, t, d, lddx}, {d_gate, f, d, lddw}, {d_up, f, d, lddw}};
+        return zero_grads(z, static_cast<cudaStream_t>(stream));
+    }
+    if (!d_x && !d_gate) return NVFP4_ERR_INVALID_ARG;
     const GatedGrad g(t, f, d);
     Memory mem;
     if ((st = check_operand(fmt, x, t, d, &mem)) != NVFP4_OK || (st = check_operand(fmt, w_gate, f, d, &mem)) != NVFP4_OK ||

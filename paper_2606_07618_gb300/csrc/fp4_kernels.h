@@ -19,6 +19,7 @@ cudaError_t launch_expand(int mx, const uint8_t* codes, const uint8_t* sf, const
 // out[r][c] = in[r][c], bf16, for an input that TMA cannot read.
 cudaError_t launch_repitch_bf16(const void* in, int64_t rows, int64_t cols, int64_t ldi, void* out, int64_t ldo,
                                 cudaStream_t s);
+cudaError_t launch_zero_bf16(int64_t rows, int64_t cols, void* out, int64_t ldo, cudaStream_t s);
 
 // ---- fp4_gemm.cu
 enum { kNvfp4 = 0, kMxfp4 = 1, kBf16 = 2 };                  // operand kinds of a product

@@ -244,6 +244,12 @@ __global__ void __launch_bounds__(256)
         for (int64_t c = threadIdx.x; c < cols; c += blockDim.x) out[r * ldo + c] = in[r * ldi + c];
 }
 
+__global__ void __launch_bounds__(256) zero_bf16_kernel(int64_t rows, int64_t cols, uint16_t* out, int64_t ldo) {
+    grid_dependency_wait();
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int64_t c = threadIdx.x; c < cols; c += blockDim.x) out[r * ldo + c] = 0;
+}
+
 template <typename... P, typename... Args>
 cudaError_t launch_grid(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t s, Args... args) {
     cudaLaunchConfig_t cfg = {};
@@ -345,6 +351,11 @@ cudaError_t launch_repitch_bf16(const void* in, int64_t rows, int64_t cols, int6
                                 cudaStream_t s) {
     return launch_grid(repitch_bf16_kernel, dim3((unsigned)(rows < 65535 ? rows : 65535)), 256, s,
                        static_cast<const uint16_t*>(in), rows, cols, ldi, static_cast<uint16_t*>(out), ldo);
+}
+
+cudaError_t launch_zero_bf16(int64_t rows, int64_t cols, void* out, int64_t ldo, cudaStream_t s) {
+    return launch_grid(zero_bf16_kernel, dim3((unsigned)(rows < 65535 ? rows : 65535)), 256, s, rows, cols,
+                       static_cast<uint16_t*>(out), ldo);
 }
 
 }  // namespace nvfp4

@@ -103,6 +103,25 @@ def test_gated_refusals(B):
     assert gb(dx=FAKE + 0x3000000) == INVALID and gb(h=FAKE + 0x3100000) == INVALID
 
 
+def test_gradients_without_rows_check_what_they_zero(B):
+    """Zeros are written only where the output's own arguments hold; nothing to write is no error."""
+    L = B.lib()
+    mb = lambda m, n, dA, lda, dB, ldb: L.fp4_matmul_backward(0, None, None, m, n, 64, None, n, dA, lda, dB, ldb, None, None, 0, None)
+    assert mb(0, 8, None, 64, None, 64) == OK and mb(8, 0, None, 64, None, 64) == OK and mb(0, 0, FAKE, 64, FAKE, 64) == OK
+    assert mb(0, 8, None, 64, FAKE, 63) == INVALID and mb(0, 8, None, 64, FAKE + 1, 64) == ALIGNMENT
+    assert mb(8, 0, FAKE, 63, None, 64) == INVALID
+    gb = lambda t, f, dx, dg, du, ldw: L.fp4_gated_ff_backward(0, 0, None, None, None, t, f, 64, None, f, dx, 64, dg, du, ldw,
+                                                                 None, f, None, None, 0, None)
+    assert gb(0, 8, None, None, None, 64) == OK and gb(8, 0, None, None, None, 64) == OK
+    assert gb(0, 8, None, FAKE, None, 64) == INVALID and gb(0, 8, None, FAKE, FAKE + 64, 64) == INVALID     # overlap
+    assert gb(0, 8, None, FAKE, FAKE + 0x10000, 60) == INVALID and gb(8, 0, FAKE + 1, None, None, 64) == ALIGNMENT
+
+
+def test_gated_without_rows_takes_null_outputs(B):
+    gf = lambda t, f, hc=None, hs=None: B.lib().fp4_gated_ff(0, 0, None, None, None, t, f, 64, None, f, hc, hs, None, None)
+    assert gf(0, 64) == OK and gf(4, 0) == OK and gf(0, 64, FAKE, None) == INVALID
+
+
 def test_binding_refuses_shapes_and_types(B):
     z = lambda *s, dt=torch.uint8: torch.zeros(*s, dtype=dt)
     op = lambda rows, cols: (z(rows, cols // 2), z(B.swizzled_bytes(rows, cols)), None)

@@ -71,6 +71,17 @@ def test_block(F, fmt, act, t, f, d):
     assert list(only) == ["x"] and torch.equal(only["x"], g["x"])
 
 
+@pytest.mark.parametrize("fmt", [R.NV, R.MX])
+def test_no_tokens(F, fmt):
+    """An empty batch: an empty result, and gradients of zeros for the weights."""
+    ff, _ = block(F, fmt, 96, 64)
+    none = torch.empty(0, 64, dtype=torch.bfloat16, device=DEV)
+    assert ff(none).shape == (0, 64)
+    g = ff.backward(none)
+    assert g["x"].shape == (0, 64) and all(not bool(g[n].any()) for n in ("gate", "up", "down"))
+    assert list(ff.backward(none, weights=False)) == ["x"] and int(ff.status) == 0
+
+
 def test_nvfp4_weights_are_scalesweeps(F):
     """The block's NVFP4 weights are the grouped ScaleSweep's, bit for bit."""
     from paper_2606_07618_gb300 import binding as B

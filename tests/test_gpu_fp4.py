@@ -439,6 +439,35 @@ def test_gated_with_a_zero_weight(B, t):
     assert bool(dg.any()) and not bool(dx.any()) and not bool(du.any())
 
 
+@pytest.mark.parametrize("fmt", [R.NV, R.MX])
+def test_gradients_over_nothing_are_zero(B, fmt):
+    """No tokens: the weights' gradients are sums over no rows; no columns: the tokens' are.  No workspace, the
+    tensors without elements null or None."""
+    none = lambda cols: (torch.empty(0, cols // 2, dtype=torch.uint8, device=DEV), torch.empty(0, dtype=torch.uint8, device=DEV), None)
+    empty = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device=DEV)
+    w, up = Held(45, 96, fmt, 1), Held(45, 96, fmt, 2)
+    for rows, a, b, dA_first in ((45, none(96), w.op, False), (45, w.op, none(96), True)):
+        got, check = guarded(rows, 96, torch.bfloat16, 101, 1)
+        grads = (got, empty(0, 96)) if dA_first else (empty(0, 96), got)
+        d = empty(rows, 0) if dA_first else empty(0, rows)
+        for other in (grads, tuple(g if g is got else None for g in grads)):
+            got.fill_(3.0)
+            B.fp4_matmul_backward(fmt, a, b, d, *other)
+            assert not bool(got.any())
+            check()
+    (dg, cg), (du, cu) = (guarded(45, 96, torch.bfloat16, 104) for _ in range(2))
+    for dx in (empty(0, 96), None):
+        dg.fill_(3.0), du.fill_(3.0)
+        B.fp4_gated_ff_backward(fmt, 0, none(96), w.op, up.op, empty(0, 45), dx, dg, du)
+        assert not bool(dg.any()) and not bool(du.any())
+        cg(), cu()
+    B.fp4_gated_ff_backward(fmt, 0, none(96), w.op, up.op, empty(0, 45), empty(0, 96))      # frozen weights: nothing to write
+    dx, check = guarded(45, 96, torch.bfloat16, 97)
+    B.fp4_gated_ff_backward(fmt, 1, w.op, none(96), none(96), empty(45, 0), dx, empty(0, 96), empty(0, 96))
+    assert not bool(dx.any())
+    check()
+
+
 # ------------------------------------------------------------------ use
 def test_results_do_not_change_from_run_to_run(B):
     """Split sums are added in a fixed order: the same bits every time."""
