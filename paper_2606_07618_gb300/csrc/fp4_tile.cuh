@@ -205,7 +205,8 @@ __device__ __forceinline__ float gate_by(float g, float z, float dz, float& da) 
 }
 template <bool GRAD>
 __device__ __forceinline__ void gelu_argument(float g, float& z, float& dz) {
-    const float g2 = g * g;
+    // dz is a factor of a (1 - p), which is 0 long before |g| = 2^10, so g^2 need not overflow there
+    const float g2 = GRAD ? fminf(g * g, 1048576.0f) : g * g;
     z = 1.5957691216f * g * fmaf(0.044715f, g2, 1.0f);       // 2 sqrt(2/pi)
     if (GRAD) dz = 1.5957691216f * fmaf(0.134145f, g2, 1.0f);
 }

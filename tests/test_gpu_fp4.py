@@ -419,6 +419,35 @@ def test_matmul_backward_against_differences(B):
         assert abs((host(grad) * u).sum() - diff) <= (bound * np.abs(u)).sum() + 1e-9 * abs(diff)
 
 
+@pytest.mark.parametrize("power", [0, 60, 100])
+def test_gated_backward_far_from_zero(B, power):
+    """Gates of +-64 * 36 * 2^power, whose square overflows fp32 for the larger two: act' is 1 or 0 there.
+    g is exact in fp32 and act adds nothing to it, so each gradient is the sum of exact terms after one
+    rounding of dg or du to bf16 (u's own error is within the few U beside it)."""
+    t, f, d = 5, 40, 64
+    wu = Held(f, d, R.MX, 3, 0)
+    wg = np.full((f, d // 2), 0x77, np.uint8)                    # 6 in every place
+    wg[20:] = 0xFF                                               # -6
+    sx, sg = np.full((t, d // 32), 127, np.uint8), np.full((f, d // 32), 127 + power, np.uint8)
+    x, gate = ((torch.from_numpy(c).to(DEV), torch.from_numpy(R.swizzle(s)).to(DEV), None)
+               for c, s in ((np.full((t, d // 2), 0x77, np.uint8), sx), (wg, sg)))
+    vx, vg = np.full((t, d), 6.0), R.values(wg, sg, R.MX)
+    g, u = vx @ vg.T, vx @ wu.v.T
+    on = (g > 0).astype(np.float64)
+    dh = bf16(np.random.default_rng(4).standard_normal((t, f)))
+    D = dh.double().numpy()
+    dg, du = D * u * on, D * g * on
+    ws = torch.empty(B.fp4_gated_ff_backward_workspace(t, f, d), dtype=torch.uint8, device=DEV)
+    for act in (0, 1):
+        got = [torch.empty(r, d, dtype=torch.bfloat16, device=DEV) for r in (t, f, f)]
+        B.fp4_gated_ff_backward(R.MX, act, x, gate, wu.op, dh.to(DEV), *got, None, ws)
+        su = np.abs(vx) @ np.abs(wu.v).T                         # what u's rounding is relative to
+        for out, want, s, n in zip(got, (dg @ vg + du @ wu.v, dg.T @ vx, du.T @ vx),
+                                   ((np.abs(D) * su * on) @ np.abs(vg) + np.abs(du) @ np.abs(wu.v),
+                                    (np.abs(D) * su * on).T @ vx, np.abs(du).T @ vx), (2 * f, t, t)):
+            near(out, want, (1 + 2 * H) * (H + (n + d + 16) * U) * s + H * np.abs(want) + 1e-30)
+
+
 @pytest.mark.parametrize("t", [3, 130])
 def test_gated_with_a_zero_weight(B, t):
     """A gate of zeros, whose global scale is 0 as nvfp4_global_scale gives it: h and d_x are zero, and the
