@@ -58,8 +58,9 @@ typedef struct {
  * Every step is exact but the rounding to E2M1.  A block of zeros, and one that holds a
  * NaN or an infinity, gets scale code 0 and nibbles that carry only the signs (the zero rule of
  * nvfp4ss.h); the latter also sets bit 0 of status_dev.
- *   x            [rows, cols] of type dt, row stride ldx; cols % 32 == 0.  Bases and
- *                strides of whole 32 bytes are read fastest.
+ *   x            [rows, cols] of type dt, row stride ldx; cols % 32 == 0, at most 2^30, and 128
+ *                rows (or all, if fewer) hold at most 2^34 elements.  Bases and strides of whole
+ *                32 bytes are read fastest.
  *   codes        [rows, cols/2], 8-byte aligned.
  *   sf_linear    optional [rows, cols/32] codes.
  *   sf_swizzled  optional, 128x4-atom layout: ceil(rows/128)*128 x ceil(cols/128)*4 bytes,
@@ -71,7 +72,7 @@ nvfp4_status mxfp4_quantize(const void* x, nvfp4_dtype dt, int64_t rows, int64_t
 /*
  * x_hat = fl32(q * 2^(code - 127)) of a matrix in MXFP4, written as fp32 or its RNE bf16.
  *   codes [rows, cols/2] (4-byte aligned), sf in `layout`, out [rows, cols] of out_dt,
- *   16-byte aligned.
+ *   16-byte aligned; the limits on rows and cols are mxfp4_quantize's.
  */
 nvfp4_status mxfp4_dequantize(const uint8_t* codes, const uint8_t* sf, nvfp4_sf_layout layout, int64_t rows,
                               int64_t cols, void* out, nvfp4_dtype out_dt, void* stream);

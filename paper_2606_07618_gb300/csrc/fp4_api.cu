@@ -17,6 +17,9 @@ namespace {
 constexpr int64_t kMaxRows = 65535ll * 128;
 constexpr int64_t kMaxCols = 1ll << 30;                      // 32-bit tensor-map coordinates
 
+// Conversions count a launch's parts in 32 bits, and a launch covers whole groups of 128 rows.
+constexpr int64_t kMaxGroup = 1ll << 34;                     // elements
+
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // Memory that a call reads and writes.
@@ -156,7 +159,7 @@ extern "C" {
 nvfp4_status mxfp4_quantize(const void* x, nvfp4_dtype dt, int64_t rows, int64_t cols, int64_t ldx, uint8_t* codes,
                             uint8_t* sf_linear, uint8_t* sf_swizzled, int* status_dev, void* stream) {
     if ((dt != NVFP4_IN_BF16 && dt != NVFP4_IN_F32) || rows < 0 || cols < 0 || cols % 32 != 0) return NVFP4_ERR_INVALID_ARG;
-    if (cols > kMaxCols) return NVFP4_ERR_RANGE;
+    if (cols > kMaxCols || (rows < 128 ? rows : 128) * cols > kMaxGroup) return NVFP4_ERR_RANGE;
     if (rows == 0 || cols == 0) return NVFP4_OK;
     const int64_t esize = dt == NVFP4_IN_BF16 ? 2 : 4;
     if (!codes || (!sf_linear && !sf_swizzled)) return NVFP4_ERR_INVALID_ARG;
@@ -182,7 +185,7 @@ nvfp4_status mxfp4_dequantize(const uint8_t* codes, const uint8_t* sf, nvfp4_sf_
     if ((out_dt != NVFP4_IN_BF16 && out_dt != NVFP4_IN_F32) || (layout != NVFP4_SF_LINEAR && layout != NVFP4_SF_SWIZZLED) ||
         rows < 0 || cols < 0 || cols % 32 != 0)
         return NVFP4_ERR_INVALID_ARG;
-    if (cols > kMaxCols) return NVFP4_ERR_RANGE;
+    if (cols > kMaxCols || (rows < 128 ? rows : 128) * cols > kMaxGroup) return NVFP4_ERR_RANGE;
     if (rows == 0 || cols == 0) return NVFP4_OK;
     if (!codes || !sf) return NVFP4_ERR_INVALID_ARG;
     const int64_t esize = out_dt == NVFP4_IN_BF16 ? 2 : 4;

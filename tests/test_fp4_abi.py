@@ -54,6 +54,16 @@ def test_quantise_refusals(B):
     assert d(codes=None) == INVALID and d(out=FAKE + 0x200008) == ALIGNMENT and d(out=FAKE) == INVALID
 
 
+@pytest.mark.parametrize("rows,cols", [(17, 2 ** 30), (64, 2 ** 30), (2 ** 20, 2 ** 27 + 32)])
+def test_conversions_refuse_what_their_counts_cannot_hold(B, rows, cols):
+    """128 rows (or all) of more than 2^34 elements; at that size the call goes on to its other arguments."""
+    L = B.lib()
+    q = lambda r, c: L.mxfp4_quantize(FAKE, 0, r, c, c, None, None, None, None, None)
+    d = lambda r, c: L.mxfp4_dequantize(None, FAKE, 2, r, c, FAKE, 0, None)
+    assert q(rows, cols) == RANGE and d(rows, cols) == RANGE
+    assert q(16, 2 ** 30) == INVALID and d(128, 2 ** 27) == INVALID and q(2 ** 20, 2 ** 27) == INVALID
+
+
 def test_matmul_refusals(B):
     L = B.lib()
     mm = lambda fmt=0, a=None, b=None, m=4, n=8, k=64, D=FAKE + 0x2000000, dt=0, ld=8, st=None: \
