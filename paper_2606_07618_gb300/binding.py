@@ -384,6 +384,15 @@ def _rows(t, what: str) -> int:
     return ld if rows > 1 else max(ld, cols)
 
 
+def _buffer(t, nbytes: int, what: str):
+    """Pointer of an optional buffer; a tensor's has to hold nbytes in a row."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.nbytes < nbytes or not t.is_contiguous():
+        raise ValueError(f"{what}: {nbytes} contiguous bytes are wanted")
+    return t.data_ptr()
+
+
 _pack_operand = struct.Struct("3P").pack
 
 
@@ -395,7 +404,7 @@ def _operand(m, fmt: int, what: str):
     if not codes.is_contiguous():
         raise ValueError(f"{what}: contiguous codes [rows, cols/2] are wanted")
     atoms = -(-half // (64 if fmt == FP4_FMT_MXFP4 else 32))       # 512 bytes: 128 rows by 4 scale columns
-    if sf.nbytes < -(-rows // 128) * atoms * 512:
+    if sf.nbytes < -(-rows // 128) * atoms * 512 or not sf.is_contiguous():
         raise ValueError(f"{what}: scales of {-(-rows // 128) * atoms * 512} bytes in the 128x4-atom layout are wanted")
     return _pack_operand(codes.data_ptr(), sf.data_ptr(), 0 if S is None else S.data_ptr()), rows, 2 * half
 
@@ -414,13 +423,18 @@ def _out(t, shape, what: str):
 def mxfp4_quantize(x, codes, sf_linear=None, sf_swizzled=None, status=None, stream=None):
     """MXFP4 codes and scales of x [rows, cols] (bf16 or fp32, rows contiguous, any row stride)."""
     rows, cols = x.shape
-    rc = (_lib or lib()).mxfp4_quantize(x.data_ptr(), _dtype(x), rows, cols, _rows(x, "x"), _ptr(codes),
-                                        _ptr(sf_linear), _ptr(sf_swizzled), _ptr(status), _stream(stream))
+    rc = (_lib or lib()).mxfp4_quantize(x.data_ptr(), _dtype(x), rows, cols, _rows(x, "x"),
+                                        _buffer(codes, rows * (cols // 2), "codes"),
+                                        _buffer(sf_linear, rows * (cols // 32), "sf_linear"),
+                                        _buffer(sf_swizzled, mx_swizzled_bytes(rows, cols), "sf_swizzled"), _ptr(status),
+                                        _stream(stream))
     _check("mxfp4_quantize", rc)
 
 
 def mxfp4_dequantize(codes, sf, layout: int, rows: int, cols: int, out, stream=None):
-    rc = (_lib or lib()).mxfp4_dequantize(_ptr(codes), _ptr(sf), layout, rows, cols, _ptr(out), _dtype(out),
+    sf_bytes = mx_swizzled_bytes(rows, cols) if layout == NVFP4_SF_SWIZZLED else rows * (cols // 32)
+    rc = (_lib or lib()).mxfp4_dequantize(_buffer(codes, rows * (cols // 2), "codes"), _buffer(sf, sf_bytes, "sf"), layout,
+                                          rows, cols, _buffer(out, rows * cols * out.element_size(), "out"), _dtype(out),
                                           _stream(stream))
     _check("mxfp4_dequantize", rc)
 
@@ -460,9 +474,9 @@ def fp4_matmul_backward(fmt: int, a, b, d_out, d_a=None, d_b=None, workspace=Non
     pd, ldd = _out(d_out, (m, n), "d_out")
     pa, lda = _out(d_a, (m, k), "d_a")
     pb, ldb = _out(d_b, (n, k), "d_b")
-    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    ws_bytes = workspace.nbytes if workspace is not None else 0
     rc = (_lib or lib()).fp4_matmul_backward(fmt, oa, ob, m, n, k, pd, ldd, pa, lda, pb, ldb, _ptr(status),
-                                             _ptr(workspace), ws_bytes, _stream(stream))
+                                             _buffer(workspace, 0, "workspace"), ws_bytes, _stream(stream))
     _check("fp4_matmul_backward", rc)
 
 
@@ -483,10 +497,8 @@ def fp4_gated_ff(fmt: int, act: int, x, w_gate, w_up, h=None, h_codes=None, h_sf
     if h_codes is not None:
         if h_codes.shape != (t, f // 2) or not h_codes.is_contiguous():
             raise ValueError(f"h_codes: contiguous, of shape {(t, f // 2)}, is wanted")
-        if h_sf is not None and h_sf.nbytes < mx_swizzled_bytes(t, f):
-            raise ValueError(f"h_sf: {mx_swizzled_bytes(t, f)} bytes are wanted")
-    rc = (_lib or lib()).fp4_gated_ff(fmt, act, ox, og, ou, t, f, d, ph, ldh, _ptr(h_codes), _ptr(h_sf), _ptr(status),
-                                      _stream(stream))
+    rc = (_lib or lib()).fp4_gated_ff(fmt, act, ox, og, ou, t, f, d, ph, ldh, _ptr(h_codes),
+                                      _buffer(h_sf, mx_swizzled_bytes(t, f), "h_sf"), _ptr(status), _stream(stream))
     _check("fp4_gated_ff", rc)
 
 
@@ -506,7 +518,8 @@ def fp4_gated_ff_backward(fmt: int, act: int, x, w_gate, w_up, d_h, d_x=None, d_
     if pg and pu and ldg != ldu:
         raise ValueError("d_gate and d_up: one row stride is wanted")
     ph, ldh = _out(h, (t, f), "h")
-    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    ws_bytes = workspace.nbytes if workspace is not None else 0
     rc = (_lib or lib()).fp4_gated_ff_backward(fmt, act, ox, og, ou, t, f, d, pdh, lddh, px, ldx, pg, pu, ldg, ph, ldh,
-                                               _ptr(status), _ptr(workspace), ws_bytes, _stream(stream))
+                                               _ptr(status), _buffer(workspace, 0, "workspace"), ws_bytes,
+                                               _stream(stream))
     _check("fp4_gated_ff_backward", rc)

@@ -153,6 +153,29 @@ def test_binding_refuses_shapes_and_types(B):
         B.mxfp4_quantize(z(64, 4, dt=torch.float32).t(), z(4, 32), z(4, 2))
 
 
+def test_binding_refuses_buffers_that_are_too_small(B):
+    """Buffers that a kernel would run past: short ones, and views whose elements are not in a row."""
+    z = lambda *s, dt=torch.uint8: torch.zeros(*s, dtype=dt)
+    x, codes, lin, swz = z(4, 64, dt=torch.float32), z(4, 32), z(4, 2), z(B.mx_swizzled_bytes(4, 64))
+    for bad in ((codes[:3], lin, None), (codes, lin[:3], None), (codes, None, swz[:-1]), (z(4, 64)[:, ::2], lin, None),
+                (codes, None, z(1).expand(swz.numel()))):
+        with pytest.raises(ValueError):
+            B.mxfp4_quantize(x, *bad)
+    for bad in ((codes[:3], lin, 1), (codes, lin[:3], 1), (codes, lin, 2)):
+        with pytest.raises(ValueError):
+            B.mxfp4_dequantize(*bad, 4, 64, x)
+    with pytest.raises(ValueError):
+        B.mxfp4_dequantize(codes, lin, 1, 4, 64, x[:3])
+    op = lambda rows, cols: (z(rows, cols // 2), z(B.swizzled_bytes(rows, cols)), None)
+    with pytest.raises(ValueError):
+        B.fp4_matmul(0, (z(4, 32), z(1).expand(512), None), op(4, 64), z(4, 4, dt=torch.float32))
+    with pytest.raises(ValueError):
+        B.fp4_gated_ff(0, 0, op(4, 64), op(32, 64), op(32, 64), None, z(4, 16), z(1).expand(512))
+    with pytest.raises(ValueError):
+        B.fp4_matmul_backward(0, op(4, 64), op(8, 64), z(4, 8, dt=torch.bfloat16), z(4, 64, dt=torch.bfloat16), None,
+                              z(1).expand(2 ** 20))
+
+
 # ------------------------------------------------------------------ the reference itself
 def test_reference_rounds_as_the_definition():
     x = np.zeros((1, 32))
