@@ -299,14 +299,13 @@ nvfp4_status fp4_matmul_backward(fp4_format fmt, const fp4_operand* a, const fp4
         d = dv;
         ldd = g.ldn;
     }
-    if (dA && e == cudaSuccess) {
-        e = launch_expand(mx, b->codes, b->sf, nullptr, nullptr, n, k, n, bv, s);
-        if (e == cudaSuccess) e = launch_product(grad_product(bv, k, k, b->S, d, m, ldd, 0, n, dA, ldda, status_dev), sms, s);
-    }
-    if (dB && e == cudaSuccess) {
-        e = launch_expand(mx, a->codes, a->sf, nullptr, nullptr, m, k, m, av, s);
-        if (e == cudaSuccess) e = launch_product(grad_product(av, k, k, a->S, d, n, ldd, 1, m, dB, lddb, status_dev), sms, s);
-    }
+    Expansion x[2];
+    int nx = 0;
+    if (dA) x[nx++] = Expansion{b->codes, b->sf, n, n, bv};
+    if (dB) x[nx++] = Expansion{a->codes, a->sf, m, m, av};
+    if (e == cudaSuccess) e = launch_expand(mx, x, nx, k, s);
+    if (dA && e == cudaSuccess) e = launch_product(grad_product(bv, k, k, b->S, d, m, ldd, 0, n, dA, ldda, status_dev), sms, s);
+    if (dB && e == cudaSuccess) e = launch_product(grad_product(av, k, k, a->S, d, n, ldd, 1, m, dB, lddb, status_dev), sms, s);
     return result(e);
 }
 
@@ -411,22 +410,28 @@ nvfp4_status fp4_gated_ff_backward(fp4_format fmt, fp4_activation act, const fp4
     p.fp = g.fp;
     p.status = status_dev;
     cudaError_t e = launch_product(p, sms, s);
+    Expansion v[3];
+    int nv = 0;
+    if (d_x) {
+        v[nv++] = Expansion{w_gate->codes, w_gate->sf, f, g.fp, wv};
+        v[nv++] = Expansion{w_up->codes, w_up->sf, f, g.fp, static_cast<char*>(wv) + g.fp * d * 2};
+    }
+    if (d_gate) v[nv++] = Expansion{x->codes, x->sf, t, t, xv};
+    if (e == cudaSuccess) e = launch_expand(mx, v, nv, d, s);
     if (d_x && e == cudaSuccess) {
-        e = launch_expand(mx, w_gate->codes, w_gate->sf, w_up->codes, w_up->sf, f, d, g.fp, wv, s);
         // gate's half of the contraction and up's have a global scale each
         Product q = grad_product(wv, d, d, w_gate->S, dgu, t, 2 * g.fp, 0, 2 * g.fp, d_x, lddx, status_dev);
         q.p2.S = w_up->S;
         if (!mx) q.k_part = g.fp;
-        if (e == cudaSuccess) e = launch_product(q, sms, s);
+        e = launch_product(q, sms, s);
     }
     if (d_gate && e == cudaSuccess) {
-        e = launch_expand(mx, x->codes, x->sf, nullptr, nullptr, t, d, t, xv, s);
         // one product for both: dg's columns of dgu are its rows 0.. , du's its rows fp..
         Product q = grad_product(xv, d, d, x->S, dgu, g.fp + f, 2 * g.fp, 1, t, d_gate, lddw, status_dev);
         q.out2 = d_up;
         q.row2 = g.fp;
         q.rows1 = f;
-        if (e == cudaSuccess) e = launch_product(q, sms, s);
+        e = launch_product(q, sms, s);
     }
     return result(e);
 }

@@ -11,11 +11,14 @@ cudaError_t launch_mxfp4_quantize(const void* x, int dtype, int64_t rows, int64_
                                   uint8_t* sf_linear, uint8_t* sf_swizzled, int* status, int sms, cudaStream_t s);
 cudaError_t launch_mxfp4_dequantize(const uint8_t* codes, const uint8_t* sf, int swizzled, int64_t rows, int64_t cols,
                                     void* out, int dtype, int sms, cudaStream_t s);
-// out[r][c] = bf16(q * s) of a quantised matrix (without S), exact, 32-byte aligned; rows in
-// [rows, rows_out) are written as zero.  A second matrix of the same size (or null) goes to rows
-// rows_out and on.
-cudaError_t launch_expand(int mx, const uint8_t* codes, const uint8_t* sf, const uint8_t* codes2, const uint8_t* sf2,
-                          int64_t rows, int64_t cols, int64_t rows_out, void* out, cudaStream_t s);
+// out[r][c] = bf16(q * s) of quantised matrices of one width (without S), exact, 32-byte aligned; rows in
+// [rows, rows_out) are written as zero.
+struct Expansion {
+    const uint8_t *codes, *sf;
+    int64_t rows, rows_out;
+    void* out;
+};
+cudaError_t launch_expand(int mx, const Expansion* m, int count, int64_t cols, cudaStream_t s);
 // out[r][c] = in[r][c], bf16, for an input that TMA cannot read.
 cudaError_t launch_repitch_bf16(const void* in, int64_t rows, int64_t cols, int64_t ldi, void* out, int64_t ldo,
                                 cudaStream_t s);

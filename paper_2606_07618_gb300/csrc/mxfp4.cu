@@ -193,22 +193,29 @@ __global__ void __launch_bounds__(256)
 }
 
 // ---------------------------------------------------------------------------
-// The values of a quantised matrix without S in bf16: exact, as q has two significant bits and
-// an E4M3 scale four.  16 codes to a lane, 32 bytes out; four in flight (blockIdx.y: one of two
-// matrices of the same size, the second's rows further on).
+// The values of quantised matrices without S in bf16: exact, as q has two significant bits and
+// an E4M3 scale four.  16 codes to a lane, 32 bytes out; four in flight.  Up to three matrices of one width to a
+// launch, their tiles of 1024 segments one after the other (a gradient call's all: training, 100 x 501 x 608, 17.1 us,
+// 18.7 with a launch for each operand; 2048 x 4096 x 4096 101.4, 105.5).
+struct ExpandPart {
+    const uint8_t *codes, *sf;
+    uint4* out;
+    uint32_t segs, segs_out;     // of 16 elements: those there are, those to write
+};
+struct ExpandParams {
+    ExpandPart part[3];
+    uint32_t first[3];           // the tile that each starts with
+    uint32_t row_segs, kpad4;
+    FastDiv div;                 // by row_segs
+};
 template <int MX>
-__global__ void __launch_bounds__(256)
-    expand_kernel(const uint8_t* codes, const uint8_t* sf, const uint8_t* codes2, const uint8_t* sf2, uint32_t segs,
-                  uint32_t segs_out, uint32_t row_segs, uint32_t kpad4, FastDiv div, uint4* out) {
+__global__ void __launch_bounds__(256) expand_kernel(const __grid_constant__ ExpandParams P) {
     constexpr int kUnroll = 4;
     grid_dependency_wait();
-    grid_launch_dependents();                                // the product: training, 100 x 501 x 608, 18.6 us, 20.2 without
-    if (blockIdx.y == 1) {
-        codes = codes2;
-        sf = sf2;
-        out += 2 * (int64_t)segs_out;
-    }
-    const uint32_t s0 = (blockIdx.x * blockDim.x + (threadIdx.x & ~31u)) * kUnroll + (threadIdx.x & 31);
+    grid_launch_dependents();                                // the product: 1.6 us of a small training step
+    const int which = blockIdx.x >= P.first[2] ? 2 : blockIdx.x >= P.first[1] ? 1 : 0;
+    const ExpandPart& m = P.part[which];
+    const uint32_t s0 = ((blockIdx.x - P.first[which]) * blockDim.x + (threadIdx.x & ~31u)) * kUnroll + (threadIdx.x & 31);
     uint2 c[kUnroll];
     uint32_t s[kUnroll];
 #pragma unroll
@@ -216,16 +223,16 @@ __global__ void __launch_bounds__(256)
         const uint32_t seg = s0 + 32 * u;
         c[u] = make_uint2(0, 0);
         s[u] = MX ? 127 : 0;                                 // rows past the matrix: zero codes
-        if (seg < segs) {
-            const uint32_t row = div_by(seg, div), k = seg - row * row_segs;
-            c[u] = reinterpret_cast<const uint2*>(codes)[seg];
-            s[u] = sf[swizzle_offset(row, MX ? k >> 1 : k, kpad4)];
+        if (seg < m.segs) {
+            const uint32_t row = div_by(seg, P.div), k = seg - row * P.row_segs;
+            c[u] = reinterpret_cast<const uint2*>(m.codes)[seg];
+            s[u] = m.sf[swizzle_offset(row, MX ? k >> 1 : k, P.kpad4)];
         }
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; u++) {
         const uint32_t seg = s0 + 32 * u;
-        if (seg >= segs_out) break;
+        if (seg >= m.segs_out) break;
         const float v = MX ? e8m0_value(s[u]) : f16bits_to_f32(e4m3_to_f16bits(s[u]));
         uint32_t w[8];
 #pragma unroll
@@ -234,7 +241,7 @@ __global__ void __launch_bounds__(256)
             e2m1_pair((j < 4 ? c[u].x : c[u].y) >> (8 * (j & 3)), a, b);
             w[j] = pack_bf16(__fmul_rn(a, v), __fmul_rn(b, v));
         }
-        uint4* at = out + 2 * (int64_t)seg;
+        uint4* at = m.out + 2 * (int64_t)seg;
         asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                      ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
     }
@@ -330,28 +337,31 @@ cudaError_t launch_mxfp4_dequantize(const uint8_t* codes, const uint8_t* sf, int
     return cudaSuccess;
 }
 
-cudaError_t launch_expand(int mx, const uint8_t* codes, const uint8_t* sf, const uint8_t* codes2, const uint8_t* sf2,
-                          int64_t rows, int64_t cols, int64_t rows_out, void* out, cudaStream_t s) {
-    const uint32_t row_segs = (uint32_t)(cols / 16), kpad4 = (uint32_t)((cols / (mx ? 32 : 16) + 3) / 4);
-    const FastDiv div = make_fast_div(row_segs);
-    // segments are counted in 32 bits: rows in groups of whole 128, as in quantisation (never with a second matrix
-    // past one group: its place follows from the first's size)
-    const int64_t most = ((int64_t)1 << 30) / row_segs / 128 * 128, group = most > 0 ? most : 128;
-    const int pair = codes2 && rows_out <= group;
-    for (int m = 0; m < (codes2 && !pair ? 2 : 1); m++) {
-        char* to = static_cast<char*>(out) + m * rows_out * cols * 2;
-        for (int64_t r = 0; r < rows_out; r += group) {
-            const int64_t n_out = rows_out - r < group ? rows_out - r : group, left = rows - r, n = left < 0 ? 0 : left < n_out ? left : n_out;
-            const int64_t segs_out = n_out * row_segs;
-            const dim3 grid((unsigned)((segs_out + 1023) / 1024), pair ? 2u : 1u);
-            const int64_t co = r * (cols / 2), so = r * kpad4 * 4;
-            const cudaError_t e = launch_grid(mx ? expand_kernel<1> : expand_kernel<0>, grid, 256, s, (m ? codes2 : codes) + co,
-                                              (m ? sf2 : sf) + so, pair ? codes2 + co : nullptr, pair ? sf2 + so : nullptr,
-                                              (uint32_t)(n * row_segs), (uint32_t)segs_out, row_segs, kpad4, div,
-                                              reinterpret_cast<uint4*>(to + r * cols * 2));
+cudaError_t launch_expand(int mx, const Expansion* m, int count, int64_t cols, cudaStream_t s) {
+    ExpandParams P = {};
+    P.row_segs = (uint32_t)(cols / 16);
+    P.kpad4 = (uint32_t)((cols / (mx ? 32 : 16) + 3) / 4);
+    P.div = make_fast_div(P.row_segs);
+    // segments are counted in 32 bits: rows in groups of whole 128, as in quantisation
+    const int64_t most = ((int64_t)1 << 30) / P.row_segs / 128 * 128, group = most > 0 ? most : 128;
+    uint32_t tiles = 0;
+    int parts = 0;
+    for (int i = 0; i < count; i++)
+        for (int64_t r = 0; r < m[i].rows_out; r += group) {
+            const int64_t n_out = m[i].rows_out - r < group ? m[i].rows_out - r : group, left = m[i].rows - r;
+            const int64_t n = left < 0 ? 0 : left < n_out ? left : n_out;
+            P.part[parts] = ExpandPart{m[i].codes + r * (cols / 2), m[i].sf + r * P.kpad4 * 4,
+                                       reinterpret_cast<uint4*>(static_cast<char*>(m[i].out) + r * cols * 2),
+                                       (uint32_t)(n * P.row_segs), (uint32_t)(n_out * P.row_segs)};
+            P.first[parts++] = tiles;
+            tiles += (P.part[parts - 1].segs_out + 1023) / 1024;
+            if (parts < 3 && !(i == count - 1 && r + group >= m[i].rows_out)) continue;
+            for (int j = parts; j < 3; j++) P.first[j] = tiles;  // no tile
+            const cudaError_t e = launch_grid(mx ? expand_kernel<1> : expand_kernel<0>, dim3(tiles), 256, s, P);
             if (e != cudaSuccess) return e;
+            tiles = 0;
+            parts = 0;
         }
-    }
     return cudaSuccess;
 }
 
