@@ -386,7 +386,7 @@ def _rows(t, what: str) -> int:
 
 def _buffer(t, nbytes: int, what: str):
     """Pointer of an optional buffer; a tensor's has to hold nbytes in a row."""
-    if t is None or isinstance(t, int):
+    if t is None or type(t) is int:
         return t
     if t.nbytes < nbytes or not t.is_contiguous():
         raise ValueError(f"{what}: {nbytes} contiguous bytes are wanted")
@@ -426,7 +426,7 @@ def mxfp4_quantize(x, codes, sf_linear=None, sf_swizzled=None, status=None, stre
     rc = (_lib or lib()).mxfp4_quantize(x.data_ptr(), _dtype(x), rows, cols, _rows(x, "x"),
                                         _buffer(codes, rows * (cols // 2), "codes"),
                                         _buffer(sf_linear, rows * (cols // 32), "sf_linear"),
-                                        _buffer(sf_swizzled, mx_swizzled_bytes(rows, cols), "sf_swizzled"), _ptr(status),
+                                        _buffer(sf_swizzled, (rows + 127 >> 7) * (cols + 127 >> 7) * 512, "sf_swizzled"), _ptr(status),
                                         _stream(stream))
     _check("mxfp4_quantize", rc)
 
