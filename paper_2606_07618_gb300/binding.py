@@ -394,6 +394,7 @@ def _buffer(t, nbytes: int, what: str):
 
 
 _pack_operand = struct.Struct("3P").pack
+_BF16 = torch.bfloat16
 
 
 def _operand(m, fmt: int, what: str):
@@ -403,21 +404,22 @@ def _operand(m, fmt: int, what: str):
     rows, half = codes.shape
     if not codes.is_contiguous():
         raise ValueError(f"{what}: contiguous codes [rows, cols/2] are wanted")
-    atoms = -(-half // (64 if fmt == FP4_FMT_MXFP4 else 32))       # 512 bytes: 128 rows by 4 scale columns
-    if sf.nbytes < -(-rows // 128) * atoms * 512 or not sf.is_contiguous():
-        raise ValueError(f"{what}: scales of {-(-rows // 128) * atoms * 512} bytes in the 128x4-atom layout are wanted")
+    # atoms of 512 bytes: 128 rows by 4 scale columns
+    need = (rows + 127 >> 7) * (half + 63 >> 6 if fmt == FP4_FMT_MXFP4 else half + 31 >> 5) * 512
+    if sf.nbytes < need or not sf.is_contiguous():
+        raise ValueError(f"{what}: scales of {need} bytes in the 128x4-atom layout are wanted")
     return _pack_operand(codes.data_ptr(), sf.data_ptr(), 0 if S is None else S.data_ptr()), rows, 2 * half
 
 
-def _out(t, shape, what: str):
+def _out(t, rows: int, cols: int, what: str):
     """Pointer and row stride of an optional bf16 tensor."""
     if t is None:
         return None, 0
-    if t.dtype != torch.bfloat16:
+    if t.dtype is not _BF16:
         raise TypeError(f"{what}: bfloat16 is wanted, not {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{what}: shape {shape} is wanted, not {tuple(t.shape)}")
-    return t.data_ptr(), _rows(t, what)
+    if t.shape != (rows, cols):
+        raise ValueError(f"{what}: shape {(rows, cols)} is wanted, not {tuple(t.shape)}")
+    return t.data_ptr(), cols if t.is_contiguous() else _rows(t, what)
 
 
 def mxfp4_quantize(x, codes, sf_linear=None, sf_swizzled=None, status=None, stream=None):
@@ -446,8 +448,8 @@ def _matmul(fn: str, fmt: int, a, b, out, status, stream):
         raise ValueError(f"{fn}: operands of {k} and {kb} columns")
     if out.shape != (m, n):
         raise ValueError(f"out: shape {(m, n)} is wanted, not {tuple(out.shape)}")
-    rc = getattr(_lib or lib(), fn)(fmt, oa, ob, m, n, k, out.data_ptr(), _dtype(out), _rows(out, "out"), _ptr(status),
-                                    _stream(stream))
+    rc = getattr(_lib or lib(), fn)(fmt, oa, ob, m, n, k, out.data_ptr(), _dtype(out),
+                                    n if out.is_contiguous() else _rows(out, "out"), _ptr(status), _stream(stream))
     _check(fn, rc)
 
 
@@ -471,9 +473,9 @@ def fp4_matmul_backward(fmt: int, a, b, d_out, d_a=None, d_b=None, workspace=Non
     ob, n, kb = _operand(b, fmt, "b")
     if k != kb:
         raise ValueError(f"fp4_matmul_backward: operands of {k} and {kb} columns")
-    pd, ldd = _out(d_out, (m, n), "d_out")
-    pa, lda = _out(d_a, (m, k), "d_a")
-    pb, ldb = _out(d_b, (n, k), "d_b")
+    pd, ldd = _out(d_out, m, n, "d_out")
+    pa, lda = _out(d_a, m, k, "d_a")
+    pb, ldb = _out(d_b, n, k, "d_b")
     ws_bytes = workspace.nbytes if workspace is not None else 0
     rc = (_lib or lib()).fp4_matmul_backward(fmt, oa, ob, m, n, k, pd, ldd, pa, lda, pb, ldb, _ptr(status),
                                              _buffer(workspace, 0, "workspace"), ws_bytes, _stream(stream))
@@ -493,7 +495,7 @@ def fp4_gated_ff(fmt: int, act: int, x, w_gate, w_up, h=None, h_codes=None, h_sf
     """act(x Wg^T) * (x Wu^T) of quantised operands, as h [t, f] bf16 and/or as an MXFP4 operand (h_codes [t, f/2],
     h_sf of mx_swizzled_bytes(t, f) bytes)."""
     ox, og, ou, t, f, d = _gated_operands("fp4_gated_ff", fmt, x, w_gate, w_up)
-    ph, ldh = _out(h, (t, f), "h")
+    ph, ldh = _out(h, t, f, "h")
     if h_codes is not None:
         if h_codes.shape != (t, f // 2) or not h_codes.is_contiguous():
             raise ValueError(f"h_codes: contiguous, of shape {(t, f // 2)}, is wanted")
@@ -511,13 +513,13 @@ def fp4_gated_ff_backward(fmt: int, act: int, x, w_gate, w_up, d_h, d_x=None, d_
     """Gradients of fp4_gated_ff's operands from d_h [t, f] (bf16): d_x [t, d], d_gate and d_up [f, d] (bf16, d_x or the
     pair may be None); h [t, f] optionally receives the forward result."""
     ox, og, ou, t, f, d = _gated_operands("fp4_gated_ff_backward", fmt, x, w_gate, w_up)
-    pdh, lddh = _out(d_h, (t, f), "d_h")
-    px, ldx = _out(d_x, (t, d), "d_x")
-    pg, ldg = _out(d_gate, (f, d), "d_gate")
-    pu, ldu = _out(d_up, (f, d), "d_up")
+    pdh, lddh = _out(d_h, t, f, "d_h")
+    px, ldx = _out(d_x, t, d, "d_x")
+    pg, ldg = _out(d_gate, f, d, "d_gate")
+    pu, ldu = _out(d_up, f, d, "d_up")
     if pg and pu and ldg != ldu:
         raise ValueError("d_gate and d_up: one row stride is wanted")
-    ph, ldh = _out(h, (t, f), "h")
+    ph, ldh = _out(h, t, f, "h")
     ws_bytes = workspace.nbytes if workspace is not None else 0
     rc = (_lib or lib()).fp4_gated_ff_backward(fmt, act, ox, og, ou, t, f, d, pdh, lddh, px, ldx, pg, pu, ldg, ph, ldh,
                                                _ptr(status), _buffer(workspace, 0, "workspace"), ws_bytes,
