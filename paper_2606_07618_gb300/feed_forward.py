@@ -50,7 +50,6 @@ class GatedFeedForward:
             q = QuantizeStep(ws, importance, objective=B.NVFP4_OBJ_MSE if importance is None else B.NVFP4_OBJ_WMSE)
             q()
             self.gate, self.up, self.down = ((o["codes"], o["sf_swizzled"], q.S[i:i + 1]) for i, o in enumerate(q.outs))
-            self._dynamic = torch.empty(B.nvfp4_dynamic_workspace(), dtype=torch.uint8, device=self.device)
         self._x = self._h = None
 
     def _quantise(self, x):
@@ -63,9 +62,11 @@ class GatedFeedForward:
             return codes, sf, None
         sf = torch.empty(B.swizzled_bytes(rows, cols), dtype=torch.uint8, device=self.device)
         S = torch.empty(1, device=self.device)
+        # a workspace for each call: the global scale is reduced in it, and calls on two streams run at one time
+        ws = torch.empty(B.nvfp4_dynamic_workspace(), dtype=torch.uint8, device=self.device)
         win = (B.NVFP4_WINDOW_DEFAULT, B.NVFP4_WINDOW_DEFAULT)
-        B.scalesweep_quantize_dynamic(x.contiguous(), 16, 256.0, B.NVFP4_OBJ_MSE, None, 0, *win, S, self.status,
-                                      self._dynamic, codes, None, sf)
+        B.scalesweep_quantize_dynamic(x.contiguous(), 16, 256.0, B.NVFP4_OBJ_MSE, None, 0, *win, S, self.status, ws,
+                                      codes, None, sf)
         return codes, sf, S
 
     def __call__(self, x):

@@ -1,0 +1,32 @@
+"""feed_forward.py without a GPU: what it hands to the library's calls, which are replaced by ones that record."""
+import pytest
+import torch
+
+from paper_2606_07618_gb300 import binding as B
+from paper_2606_07618_gb300 import feed_forward as F
+
+CALLS = ("mxfp4_quantize", "scalesweep_quantize_dynamic", "scalesweep_quantize_group", "fp4_gated_ff", "fp4_matmul",
+         "fp4_matmul_backward", "fp4_gated_ff_backward")
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """(name, arguments) of each call; the arguments stay alive, so that their addresses stay apart."""
+    seen = []
+    for name in CALLS:
+        monkeypatch.setattr(B, name, lambda *a, _name=name, **k: seen.append((_name, a)))
+    return seen
+
+
+def block(fmt, f=64, d=32, dtype=torch.bfloat16, **kw):
+    return F.GatedFeedForward(*(torch.randn(*s).to(dtype) for s in ((f, d), (f, d), (d, f))), fmt=fmt, **kw)
+
+
+def test_calls_of_one_block_share_no_workspace(calls):
+    """Two calls may run at one time on two streams: each has a workspace of its own for the global scale."""
+    ff = block(B.FP4_FMT_NVFP4)
+    for _ in range(2):
+        ff(torch.randn(4, 32).to(torch.bfloat16))
+    ws = [a[10] for n, a in calls if n == "scalesweep_quantize_dynamic"]
+    assert len(ws) == 4 and len({w.data_ptr() for w in ws}) == 4
+    assert all(w.numel() == B.nvfp4_dynamic_workspace() for w in ws)
