@@ -16,7 +16,9 @@ quantisers).
     in bf16 and quantised the same way.
 
 All work runs in the library's kernels on the current stream; this module only arranges
-buffers.
+buffers.  A thread may call a block from several streams, each ordered after the block's
+construction; what a call keeps for its gradients is ``saved`` (the last call's), which a program
+that makes more calls before the ``backward`` of one takes and passes to it.
 """
 from __future__ import annotations
 
@@ -50,7 +52,16 @@ class GatedFeedForward:
             q = QuantizeStep(ws, importance, objective=B.NVFP4_OBJ_MSE if importance is None else B.NVFP4_OBJ_WMSE)
             q()
             self.gate, self.up, self.down = ((o["codes"], o["sf_swizzled"], q.S[i:i + 1]) for i, o in enumerate(q.outs))
-        self._x = self._h = None
+        self.saved = None
+
+    # the quantised x and h of the last call
+    @property
+    def _x(self):
+        return self.saved[0]
+
+    @property
+    def _h(self):
+        return self.saved[1]
 
     def _quantise(self, x):
         """x as an operand in this block's format."""
@@ -70,30 +81,38 @@ class GatedFeedForward:
         return codes, sf, S
 
     def __call__(self, x):
-        """y [t, d] bf16 of x [t, d] (bf16 or fp32).  The quantised x and h stay for ``backward``."""
+        """y [t, d] bf16 of x [t, d] (bf16 or fp32).  The quantised x and h stay for ``backward``, as ``saved``."""
         t = x.shape[0]
         if x.dim() != 2 or x.shape[1] != self.d:
             raise ValueError(f"x of shape {tuple(x.shape)}, [t, {self.d}] is wanted")
-        self._x = self._quantise(x)
+        qx = self._quantise(x)
         if self.fmt == B.FP4_FMT_MXFP4:
             codes = torch.empty(t, self.f // 2, dtype=torch.uint8, device=self.device)
             sf = torch.empty(B.mx_swizzled_bytes(t, self.f), dtype=torch.uint8, device=self.device)
-            B.fp4_gated_ff(self.fmt, self.act, self._x, self.gate, self.up, None, codes, sf, self.status)
-            self._h = (codes, sf, None)
+            B.fp4_gated_ff(self.fmt, self.act, qx, self.gate, self.up, None, codes, sf, self.status)
+            qh = (codes, sf, None)
         else:
             h = torch.empty(t, self.f, dtype=torch.bfloat16, device=self.device)
-            B.fp4_gated_ff(self.fmt, self.act, self._x, self.gate, self.up, h, status=self.status)
-            self._h = self._quantise(h)
+            B.fp4_gated_ff(self.fmt, self.act, qx, self.gate, self.up, h, status=self.status)
+            qh = self._quantise(h)
         y = torch.empty(t, self.d, dtype=torch.bfloat16, device=self.device)
-        B.fp4_matmul(self.fmt, self._h, self.down, y, self.status)
+        B.fp4_matmul(self.fmt, qh, self.down, y, self.status)
+        self.saved = qx, qh
         return y
 
-    def backward(self, dy, weights: bool = True) -> dict:
-        """Gradients (bf16) of sum(dy * y) for the last call: {"x", "gate", "up", "down"}, or {"x"} alone for frozen
-        weights."""
-        if self._x is None:
+    def backward(self, dy, weights: bool = True, saved=None) -> dict:
+        """Gradients (bf16) of sum(dy * y) for the call that ``saved`` is of (None: the last one): {"x", "gate", "up",
+        "down"}, or {"x"} alone for frozen weights."""
+        saved = saved or self.saved
+        if saved is None:
             raise RuntimeError("backward before a call")
-        t = self._x[0].shape[0]
+        qx, qh = saved
+        if self.device.type == "cuda":
+            # they may be another stream's, and dropped by its next call before this one's kernels have read them
+            for v in (*qx, *qh):
+                if v is not None:
+                    v.record_stream(torch.cuda.current_stream(self.device))
+        t = qx[0].shape[0]
         if dy.shape != (t, self.d):
             raise ValueError(f"dy of shape {tuple(dy.shape)}, {(t, self.d)} is wanted")
         new = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device=self.device)  # noqa: E731
@@ -103,8 +122,8 @@ class GatedFeedForward:
         dh = new(t, self.f)
         if weights:
             g.update(gate=new(self.f, self.d), up=new(self.f, self.d), down=new(self.d, self.f))
-        B.fp4_matmul_backward(self.fmt, self._h, self.down, dy, dh, g.get("down"), ws, self.status)
-        B.fp4_gated_ff_backward(self.fmt, self.act, self._x, self.gate, self.up, dh, g["x"], g.get("gate"), g.get("up"),
+        B.fp4_matmul_backward(self.fmt, qh, self.down, dy, dh, g.get("down"), ws, self.status)
+        B.fp4_gated_ff_backward(self.fmt, self.act, qx, self.gate, self.up, dh, g["x"], g.get("gate"), g.get("up"),
                                 None, ws, self.status)
         return g
 

@@ -30,3 +30,22 @@ def test_calls_of_one_block_share_no_workspace(calls):
     ws = [a[10] for n, a in calls if n == "scalesweep_quantize_dynamic"]
     assert len(ws) == 4 and len({w.data_ptr() for w in ws}) == 4
     assert all(w.numel() == B.nvfp4_dynamic_workspace() for w in ws)
+
+
+@pytest.mark.parametrize("fmt", [B.FP4_FMT_NVFP4, B.FP4_FMT_MXFP4])
+def test_backward_of_an_earlier_call(calls, fmt):
+    """The operands of the call that is asked for, not those of the one made since."""
+    ff = block(fmt)
+    saved = []
+    for t in (4, 4):
+        ff(torch.randn(t, 32).to(torch.bfloat16))
+        saved.append(ff.saved)
+    dy = torch.zeros(4, 32, dtype=torch.bfloat16)
+    for of in saved:
+        del calls[:]
+        ff.backward(dy, saved=of)
+        got = {n: a for n, a in calls}
+        assert got["fp4_matmul_backward"][1] is of[1] and got["fp4_gated_ff_backward"][2] is of[0]
+    del calls[:]
+    ff.backward(dy)                                              # the last call's
+    assert dict(calls)["fp4_matmul_backward"][1] is saved[1][1]

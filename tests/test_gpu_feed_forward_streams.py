@@ -41,3 +41,29 @@ def test_two_streams_through_one_block(F, fmt):
             got.append(ff(xs[i % 4]))
     torch.cuda.synchronize()
     assert all(torch.equal(y, want[i % 4]) for i, y in enumerate(got)) and ff.status.item() == 0
+
+
+@pytest.mark.parametrize("fmt", [R.NV, R.MX])
+def test_gradients_of_calls_made_on_two_streams(F, fmt):
+    """Each stream's gradients are of its own call, though both were made before either gradient."""
+    t, f, d = 130, 160, 128
+    ff, xs = block(F, fmt, f, d), inputs(t, d, 2)
+    dy = torch.randn(t, d, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).to(DEV)
+    want = []
+    for x in xs:
+        ff(x)
+        want.append(ff.backward(dy))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(10):
+        saved, got = [], []
+        for s, x in zip(streams, xs):
+            with torch.cuda.stream(s):
+                ff(x)
+                saved.append(ff.saved)
+        for s, of in zip(streams, saved):
+            with torch.cuda.stream(s):
+                got.append(ff.backward(dy, saved=of))
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert all(torch.equal(g[k], w[k]) for k in w)
