@@ -22,6 +22,25 @@ import torch
 from . import binding as B
 
 
+def _check(xs, ws, strides):
+    """One type for all tensors, rows of consecutive elements, and importance weights that reach as far."""
+    dtypes = {x.dtype for x in xs}
+    if len(dtypes) != 1 or not dtypes <= {torch.bfloat16, torch.float32}:
+        raise TypeError(f"tensors of one type are wanted, bfloat16 or float32, not {sorted(map(str, dtypes))}")
+    for x, w, stride in zip(xs, ws, strides):
+        if x.dim() != 2 or not x.is_contiguous():
+            raise ValueError(f"a contiguous 2-d tensor is wanted, not {tuple(x.shape)} with strides {x.stride()}")
+        if w is None or x.numel() == 0:
+            continue
+        if w.dtype != torch.float32:
+            raise TypeError(f"importance weights in float32 are wanted, not {w.dtype}")
+        rows, cols = x.shape
+        have = w.untyped_storage().nbytes() // 4 - w.storage_offset()
+        if w.shape[-1] < cols or w.stride(-1) != 1 or have < (rows - 1) * stride + cols:
+            raise ValueError(f"importance weights of shape {tuple(w.shape)} and row stride {stride} for a tensor of "
+                             f"{tuple(x.shape)}")
+
+
 class QuantizeStep:
     def __init__(self, xs, ws=None, block: int = 16, objective: int = B.NVFP4_OBJ_MSE, fp8_div: float = 256.0,
                  activation: bool = False, swizzled: bool | None = None, w_row_strides=None, outs=None,
@@ -50,6 +69,7 @@ class QuantizeStep:
         self.dtype = B.NVFP4_IN_BF16 if self.xs[0].dtype == torch.bfloat16 else B.NVFP4_IN_F32
         strides = list(w_row_strides) if w_row_strides is not None else [0] * len(self.xs)
         self.strides = strides
+        _check(self.xs, self.ws, strides)
         if self.fused:
             self.workspace = torch.empty(B.nvfp4_dynamic_workspace(), dtype=torch.uint8, device=dev)
         else:
