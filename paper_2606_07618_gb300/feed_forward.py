@@ -31,7 +31,7 @@ from .step import QuantizeStep
 class GatedFeedForward:
     def __init__(self, w_gate, w_up, w_down, fmt: int = B.FP4_FMT_MXFP4, act: int = B.FP4_ACT_SILU,
                  importance=None):
-        """w_gate, w_up [f, d] and w_down [d, f]: bf16 or fp32 weights on the GPU (f and d multiples of 32; not kept).
+        """w_gate, w_up [f, d] and w_down [d, f]: bf16 or fp32 weights on the GPU, of any strides (f and d multiples of 32; not kept).
         importance: optional per-input-channel WMSE weights of the three (fp32, NVFP4 only)."""
         if fmt not in (B.FP4_FMT_NVFP4, B.FP4_FMT_MXFP4):
             raise ValueError(f"unknown format {fmt}")
@@ -49,7 +49,7 @@ class GatedFeedForward:
         if fmt == B.FP4_FMT_MXFP4:
             self.gate, self.up, self.down = (self._quantise(w) for w in ws)
         else:
-            q = QuantizeStep(ws, importance, objective=B.NVFP4_OBJ_MSE if importance is None else B.NVFP4_OBJ_WMSE)
+            q = QuantizeStep([w.contiguous() for w in ws], importance, objective=B.NVFP4_OBJ_MSE if importance is None else B.NVFP4_OBJ_WMSE)
             q()
             self.gate, self.up, self.down = ((o["codes"], o["sf_swizzled"], q.S[i:i + 1]) for i, o in enumerate(q.outs))
         self.saved = None
@@ -68,6 +68,8 @@ class GatedFeedForward:
         rows, cols = x.shape
         codes = torch.empty(rows, cols // 2, dtype=torch.uint8, device=self.device)
         if self.fmt == B.FP4_FMT_MXFP4:
+            if x.stride(1) != 1:                                 # rows may lie apart, their elements not
+                x = x.contiguous()
             sf = torch.empty(B.mx_swizzled_bytes(rows, cols), dtype=torch.uint8, device=self.device)
             B.mxfp4_quantize(x, codes, None, sf, self.status)
             return codes, sf, None

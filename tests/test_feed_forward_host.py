@@ -1,4 +1,6 @@
 """feed_forward.py without a GPU: what it hands to the library's calls, which are replaced by ones that record."""
+import ctypes
+
 import pytest
 import torch
 
@@ -49,3 +51,22 @@ def test_backward_of_an_earlier_call(calls, fmt):
     del calls[:]
     ff.backward(dy)                                              # the last call's
     assert dict(calls)["fp4_matmul_backward"][1] is saved[1][1]
+
+
+@pytest.mark.parametrize("fmt", [B.FP4_FMT_NVFP4, B.FP4_FMT_MXFP4])
+def test_weights_and_tokens_of_any_strides(calls, monkeypatch, fmt):
+    """Transposed weights, and columns of a wider tensor, reach the quantisers as rows of consecutive elements."""
+    read = []
+
+    def group(desc, *a, **k):                                    # the copies are gone after the call
+        for t in desc:
+            at = (ctypes.c_uint8 * (2 * t.rows * t.cols)).from_address(t.x)
+            read.append(torch.frombuffer(at, dtype=torch.bfloat16).view(t.rows, t.cols).clone())
+    monkeypatch.setattr(B, "scalesweep_quantize_group", group)
+    wide, x = torch.randn(64, 80).to(torch.bfloat16), torch.randn(32, 6).to(torch.bfloat16).t()
+    ws = wide[:, 8:40], wide[:, 40:72], torch.randn(64, 32).to(torch.bfloat16).t()
+    F.GatedFeedForward(*ws, fmt=fmt)(x)
+    if fmt == B.FP4_FMT_MXFP4:
+        read = [a[0] for n, a in calls if n == "mxfp4_quantize"]
+        assert all(s.stride(1) == 1 for s in read)
+    assert all(torch.equal(a, b) for a, b in zip(read, ws)) and len(read) >= 3
