@@ -15,6 +15,14 @@ quantisers).
     ``scalesweep_quantize_dynamic`` (global scale and sweep in one call), the gated result
     in bf16 and quantised the same way.
 
+``status`` is the calls' status word on the device, which nothing here reads: the kernels set bit 0
+where a weight, x or h held a NaN or an infinity (MXFP4: zeros for its block; NVFP4: a global scale
+that leaves NaNs out and is infinite for an infinity) and bits 1 and 16 where a wait ran out.  A
+program reads and clears it where it can wait for the GPU.
+
+The gradients are a program's own to apply: a block does not keep the weights it was made of, takes
+part in no autograd graph, and a step of tuning makes a new block of the new weights.
+
 All work runs in the library's kernels on the current stream; this module only arranges
 buffers.  A thread may call a block from several streams, each ordered after the block's
 construction; what a call keeps for its gradients is ``saved`` (the last call's), which a program
@@ -50,6 +58,7 @@ class GatedFeedForward:
             self.gate, self.up, self.down = (self._quantise(w) for w in ws)
         else:
             q = QuantizeStep([w.contiguous() for w in ws], importance, objective=B.NVFP4_OBJ_MSE if importance is None else B.NVFP4_OBJ_WMSE)
+            q.status = self.status
             q()
             self.gate, self.up, self.down = ((o["codes"], o["sf_swizzled"], q.S[i:i + 1]) for i, o in enumerate(q.outs))
         self.saved = None

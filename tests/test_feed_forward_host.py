@@ -70,3 +70,15 @@ def test_weights_and_tokens_of_any_strides(calls, monkeypatch, fmt):
         read = [a[0] for n, a in calls if n == "mxfp4_quantize"]
         assert all(s.stride(1) == 1 for s in read)
     assert all(torch.equal(a, b) for a, b in zip(read, ws)) and len(read) >= 3
+
+
+@pytest.mark.parametrize("fmt", [B.FP4_FMT_NVFP4, B.FP4_FMT_MXFP4])
+def test_one_status_word(calls, fmt):
+    """Every call of a block, the quantisation of its weights among them, reports in the same word."""
+    at = {"mxfp4_quantize": 4, "scalesweep_quantize_dynamic": 9, "scalesweep_quantize_group": 5, "fp4_matmul": 4,
+          "fp4_matmul_backward": 7, "fp4_gated_ff_backward": 11}
+    ff = block(fmt)
+    ff(torch.randn(4, 32).to(torch.bfloat16))
+    ff.backward(torch.zeros(4, 32, dtype=torch.bfloat16))
+    words = [a[at[n]] for n, a in calls if n in at]
+    assert len(words) >= 6 and all(w is ff.status for w in words)
