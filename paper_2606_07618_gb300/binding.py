@@ -394,7 +394,16 @@ def _buffer(t, nbytes: int, what: str):
 
 
 _pack_operand = struct.Struct("3P").pack
-_BF16 = torch.bfloat16
+_BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+
+
+def _status(t):
+    """Pointer of an optional status word, which the kernels take for an int."""
+    if t is None or type(t) is int:
+        return t
+    if t.dtype is not _I32 or t.numel() < 1:
+        raise TypeError(f"status: an int32 element is wanted, not {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr()
 
 
 def _operand(m, fmt: int, what: str):
@@ -404,6 +413,10 @@ def _operand(m, fmt: int, what: str):
     rows, half = codes.shape
     if not codes.is_contiguous():
         raise ValueError(f"{what}: contiguous codes [rows, cols/2] are wanted")
+    if not (codes.dtype is sf.dtype is _U8 or codes.itemsize == sf.itemsize == 1):
+        raise TypeError(f"{what}: codes and scales in bytes are wanted, not {codes.dtype} and {sf.dtype}")
+    if S is not None and (S.dtype is not _F32 or S.numel() != 1):
+        raise TypeError(f"{what}: one float32 as S is wanted, not {tuple(S.shape)} of {S.dtype}")
     # atoms of 512 bytes: 128 rows by 4 scale columns
     need = (rows + 127 >> 7) * (half + 63 >> 6 if fmt == FP4_FMT_MXFP4 else half + 31 >> 5) * 512
     if sf.nbytes < need or not sf.is_contiguous():
@@ -428,7 +441,7 @@ def mxfp4_quantize(x, codes, sf_linear=None, sf_swizzled=None, status=None, stre
     rc = (_lib or lib()).mxfp4_quantize(x.data_ptr(), _dtype(x), rows, cols, _rows(x, "x"),
                                         _buffer(codes, rows * (cols // 2), "codes"),
                                         _buffer(sf_linear, rows * (cols // 32), "sf_linear"),
-                                        _buffer(sf_swizzled, (rows + 127 >> 7) * (cols + 127 >> 7) * 512, "sf_swizzled"), _ptr(status),
+                                        _buffer(sf_swizzled, (rows + 127 >> 7) * (cols + 127 >> 7) * 512, "sf_swizzled"), _status(status),
                                         _stream(stream))
     _check("mxfp4_quantize", rc)
 
@@ -449,7 +462,7 @@ def _matmul(fn: str, fmt: int, a, b, out, status, stream):
     if out.shape != (m, n):
         raise ValueError(f"out: shape {(m, n)} is wanted, not {tuple(out.shape)}")
     rc = getattr(_lib or lib(), fn)(fmt, oa, ob, m, n, k, out.data_ptr(), _dtype(out),
-                                    n if out.is_contiguous() else _rows(out, "out"), _ptr(status), _stream(stream))
+                                    n if out.is_contiguous() else _rows(out, "out"), _status(status), _stream(stream))
     _check(fn, rc)
 
 
@@ -477,7 +490,7 @@ def fp4_matmul_backward(fmt: int, a, b, d_out, d_a=None, d_b=None, workspace=Non
     pa, lda = _out(d_a, m, k, "d_a")
     pb, ldb = _out(d_b, n, k, "d_b")
     ws_bytes = workspace.nbytes if workspace is not None else 0
-    rc = (_lib or lib()).fp4_matmul_backward(fmt, oa, ob, m, n, k, pd, ldd, pa, lda, pb, ldb, _ptr(status),
+    rc = (_lib or lib()).fp4_matmul_backward(fmt, oa, ob, m, n, k, pd, ldd, pa, lda, pb, ldb, _status(status),
                                              _buffer(workspace, 0, "workspace"), ws_bytes, _stream(stream))
     _check("fp4_matmul_backward", rc)
 
@@ -499,8 +512,10 @@ def fp4_gated_ff(fmt: int, act: int, x, w_gate, w_up, h=None, h_codes=None, h_sf
     if h_codes is not None:
         if h_codes.shape != (t, f // 2) or not h_codes.is_contiguous():
             raise ValueError(f"h_codes: contiguous, of shape {(t, f // 2)}, is wanted")
+        if h_codes.itemsize != 1:
+            raise TypeError(f"h_codes: bytes are wanted, not {h_codes.dtype}")
     rc = (_lib or lib()).fp4_gated_ff(fmt, act, ox, og, ou, t, f, d, ph, ldh, _ptr(h_codes),
-                                      _buffer(h_sf, mx_swizzled_bytes(t, f), "h_sf"), _ptr(status), _stream(stream))
+                                      _buffer(h_sf, mx_swizzled_bytes(t, f), "h_sf"), _status(status), _stream(stream))
     _check("fp4_gated_ff", rc)
 
 
@@ -522,6 +537,6 @@ def fp4_gated_ff_backward(fmt: int, act: int, x, w_gate, w_up, d_h, d_x=None, d_
     ph, ldh = _out(h, t, f, "h")
     ws_bytes = workspace.nbytes if workspace is not None else 0
     rc = (_lib or lib()).fp4_gated_ff_backward(fmt, act, ox, og, ou, t, f, d, pdh, lddh, px, ldx, pg, pu, ldg, ph, ldh,
-                                               _ptr(status), _buffer(workspace, 0, "workspace"), ws_bytes,
+                                               _status(status), _buffer(workspace, 0, "workspace"), ws_bytes,
                                                _stream(stream))
     _check("fp4_gated_ff_backward", rc)
