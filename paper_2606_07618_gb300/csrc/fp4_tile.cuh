@@ -189,9 +189,11 @@ struct Epilogue {
 };
 
 // act(g) and, where wanted, its derivative.  Both activations are g * p with p a sigmoid
-// (of g, or of 2 z for (1 + tanh z) / 2), which keeps its relative accuracy where p is
-// small.  exp and the reciprocal by their fast forms: a few ulps, of 2^-23, below a bf16
-// result's 2^-9.  z is the sigmoid's argument, dz its derivative.
+// (of g, or of 2 z for (1 + tanh z) / 2).  z is the sigmoid's argument, dz its derivative.  p and 1 - p are
+// 1 / (1 + e) and e / (1 + e), e = exp(-|z|): neither is a difference, and the quotient's divisor is at most 2, so
+// both keep their relative accuracy down to fp32's smallest numbers.  exp and the reciprocal by their fast forms:
+// CUDA documents 2 + |1.173 z| units of 2^-23 for the first, which with what rounding z makes of it is below 2^-14
+// wherever e is not zero; bf16 results are rounded by up to 2^-8.
 __device__ __forceinline__ float fast_rcp(float x) {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -199,8 +201,9 @@ __device__ __forceinline__ float fast_rcp(float x) {
 }
 template <bool GRAD>
 __device__ __forceinline__ float gate_by(float g, float z, float dz, float& da) {
-    const float p = fast_rcp(1.0f + __expf(-z)), a = g * p;
-    if (GRAD) da = fmaf(a * (1.0f - p), dz, p);
+    const float e = __expf(-fabsf(z)), r = fast_rcp(1.0f + e), s = r * e;
+    const float p = z < 0.0f ? s : r, a = g * p;
+    if (GRAD) da = fmaf(a * (z < 0.0f ? r : s), dz, p);
     return a;
 }
 template <bool GRAD>
