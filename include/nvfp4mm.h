@@ -30,7 +30,8 @@
  *     a call needs no workspace, and tensors without elements may be NULL.
  *   - status_dev: optional device int; bit 16 is OR-ed in when a bounded wait inside a
  *     kernel ran out (about a second; the outputs are then incomplete).
- *   - Outputs must not overlap inputs or each other.
+ *   - Outputs must not overlap inputs or each other.  Dense tensors may be columns of one buffer, their
+ *     rows interleaved, where they have the same row stride.
  */
 #ifndef NVFP4MM_H
 #define NVFP4MM_H

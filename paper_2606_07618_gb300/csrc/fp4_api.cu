@@ -22,29 +22,48 @@ constexpr int64_t kMaxGroup = 1ll << 34;                     // elements
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
+// Rows of `width` bytes, `stride` bytes apart (one row: any run of bytes).
+struct Span {
+    const void* p;
+    int64_t rows, width, stride;
+    int64_t bytes() const { return (rows - 1) * stride + width; }
+};
+
+// Whether two spans have a byte in common.  Rows of one stride, the columns of one buffer, may
+// interleave: one's columns then lie beside the other's modulo the stride.
+bool overlap(const Span& a, const Span& b) {
+    if (!nvfp4::overlap(a.p, a.bytes(), b.p, b.bytes())) return false;
+    const int64_t stride = a.rows == 1 ? b.stride : a.stride;
+    if ((a.rows == 1 && b.rows == 1) || (b.rows > 1 && b.stride != stride)) return true;
+    int64_t at = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) % stride;
+    if (at < 0) at += stride;
+    return at < a.width || at + b.width > stride;
+}
+
 // Memory that a call reads and writes.
 struct Memory {
-    const void* r[16];
-    const void* w[16];
-    int64_t rn[16], wn[16];
+    Span r[16], w[16];
     int nr = 0, nw = 0;
-    void read(const void* p, int64_t n) { if (p && n > 0) { r[nr] = p; rn[nr++] = n; } }
-    void write(const void* p, int64_t n) { if (p && n > 0) { w[nw] = p; wn[nw++] = n; } }
-    // bytes from the first to the last element of [rows, cols] with row stride ld
-    static int64_t span(int64_t rows, int64_t cols, int64_t ld, int64_t esize) {
-        return rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * esize : 0;
+    void read(const void* p, int64_t n) { read(p, 1, n, 0, 1); }
+    void write(const void* p, int64_t n) { write(p, 1, n, 0, 1); }
+    // [rows, cols] of elements of `esize` bytes with row stride ld
+    void read(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t esize) {
+        if (p && rows > 0 && cols > 0) r[nr++] = Span{p, rows, cols * esize, ld * esize};
+    }
+    void write(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t esize) {
+        if (p && rows > 0 && cols > 0) w[nw++] = Span{p, rows, cols * esize, ld * esize};
     }
     nvfp4_status check() const {
         for (int i = 0; i < nw; i++) {
             for (int j = 0; j < nr; j++)
-                if (overlap(w[i], wn[i], r[j], rn[j])) return NVFP4_ERR_INVALID_ARG;
+                if (overlap(w[i], r[j])) return NVFP4_ERR_INVALID_ARG;
             for (int j = i + 1; j < nw; j++)
-                if (overlap(w[i], wn[i], w[j], wn[j])) return NVFP4_ERR_INVALID_ARG;
+                if (overlap(w[i], w[j])) return NVFP4_ERR_INVALID_ARG;
         }
         for (int i = 0; i < nw; i++)
-            if (!device_accessible(w[i])) return NVFP4_ERR_INVALID_ARG;
+            if (!device_accessible(w[i].p)) return NVFP4_ERR_INVALID_ARG;
         for (int i = 0; i < nr; i++)
-            if (!device_accessible(r[i])) return NVFP4_ERR_INVALID_ARG;
+            if (!device_accessible(r[i].p)) return NVFP4_ERR_INVALID_ARG;
         return NVFP4_OK;
     }
 };
@@ -113,7 +132,7 @@ nvfp4_status zero_grads(const ZeroGrad (&g)[N], cudaStream_t s) {
         if (!z.p || z.rows == 0) continue;
         const nvfp4_status st = check_dense(z.p, z.rows, z.cols, z.ld, 2);
         if (st != NVFP4_OK) return st;
-        mem.write(z.p, Memory::span(z.rows, z.cols, z.ld, 2));
+        mem.write(z.p, z.rows, z.cols, z.ld, 2);
     }
     const nvfp4_status st = mem.check();
     if (st != NVFP4_OK) return st;
@@ -167,7 +186,7 @@ nvfp4_status mxfp4_quantize(const void* x, nvfp4_dtype dt, int64_t rows, int64_t
     if (st != NVFP4_OK) return st;
     if (!aligned(codes, 8) || !aligned(sf_swizzled, 4) || !aligned(status_dev, 4)) return NVFP4_ERR_ALIGNMENT;
     Memory mem;
-    mem.read(x, Memory::span(rows, cols, ldx, esize));
+    mem.read(x, rows, cols, ldx, esize);
     mem.write(codes, rows * (cols / 2));
     mem.write(sf_linear, rows * (cols / 32));
     mem.write(sf_swizzled, sf_bytes(FP4_FMT_MXFP4, rows, cols));
@@ -221,7 +240,7 @@ nvfp4_status matmul_common(fp4_format fmt, const fp4_operand* a, const fp4_opera
         (st = check_dense(D, m, n, ldd, esize)) != NVFP4_OK)
         return st;
     if (!aligned(status_dev, 4)) return NVFP4_ERR_ALIGNMENT;
-    mem.write(D, Memory::span(m, n, ldd, esize));
+    mem.write(D, m, n, ldd, esize);
     mem.write(status_dev, 4);
     if ((st = mem.check()) != NVFP4_OK) return st;
     const int sms = sm_count();
@@ -279,9 +298,9 @@ nvfp4_status fp4_matmul_backward(fp4_format fmt, const fp4_operand* a, const fp4
         return st;
     if (!workspace || ws_bytes < g.bytes()) return NVFP4_ERR_INVALID_ARG;
     if (!aligned(workspace, 256) || !aligned(status_dev, 4)) return NVFP4_ERR_ALIGNMENT;
-    mem.read(dD, Memory::span(m, n, lddd, 2));
-    if (dA) mem.write(dA, Memory::span(m, k, ldda, 2));
-    if (dB) mem.write(dB, Memory::span(n, k, lddb, 2));
+    mem.read(dD, m, n, lddd, 2);
+    mem.write(dA, m, k, ldda, 2);
+    mem.write(dB, n, k, lddb, 2);
     mem.write(workspace, (int64_t)g.bytes());
     mem.write(status_dev, 4);
     if ((st = mem.check()) != NVFP4_OK) return st;
@@ -324,7 +343,7 @@ nvfp4_status fp4_gated_ff(fp4_format fmt, fp4_activation act, const fp4_operand*
         (st = check_operand(fmt, w_up, f, d, &mem)) != NVFP4_OK || (h && (st = check_dense(h, t, f, ldh, 2)) != NVFP4_OK))
         return st;
     if (!aligned(h_codes, 16) || !aligned(h_sf, 4) || !aligned(status_dev, 4)) return NVFP4_ERR_ALIGNMENT;
-    if (h) mem.write(h, Memory::span(t, f, ldh, 2));
+    mem.write(h, t, f, ldh, 2);
     mem.write(h_codes, t * (f / 2));
     if (h_sf) mem.write(h_sf, sf_bytes(FP4_FMT_MXFP4, t, f));
     mem.write(status_dev, 4);
@@ -379,11 +398,11 @@ nvfp4_status fp4_gated_ff_backward(fp4_format fmt, fp4_activation act, const fp4
         return st;
     if (!workspace || ws_bytes < g.bytes()) return NVFP4_ERR_INVALID_ARG;
     if (!aligned(workspace, 256) || !aligned(status_dev, 4)) return NVFP4_ERR_ALIGNMENT;
-    mem.read(dh, Memory::span(t, f, lddh, 2));
-    if (d_x) mem.write(d_x, Memory::span(t, d, lddx, 2));
-    if (d_gate) mem.write(d_gate, Memory::span(f, d, lddw, 2));
-    if (d_up) mem.write(d_up, Memory::span(f, d, lddw, 2));
-    if (h) mem.write(h, Memory::span(t, f, ldh, 2));
+    mem.read(dh, t, f, lddh, 2);
+    mem.write(d_x, t, d, lddx, 2);
+    mem.write(d_gate, f, d, lddw, 2);
+    mem.write(d_up, f, d, lddw, 2);
+    mem.write(h, t, f, ldh, 2);
     mem.write(workspace, (int64_t)g.bytes());
     mem.write(status_dev, 4);
     if ((st = mem.check()) != NVFP4_OK) return st;
