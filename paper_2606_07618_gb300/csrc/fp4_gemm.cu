@@ -313,17 +313,11 @@ cudaError_t launch_tile(const Product& p, int sms, cudaStream_t s) {
     P.k = p.k;
     P.starve = p.starve;
     P.e = make_epilogue(p);
-    const int nst = (int)((p.k + stage_k(KIND) - 1) / stage_k(KIND));
     const int64_t tn = (p.p.rows + 127) / 128;
-    // Few tiles: up to eight CTAs to a tile, two to an SM, so that some 150 to 300 load (us with
-    // 8 / 4 / 2 at most: 1 x 4096 x 4096 4.2 / 4.3 / 5.1, 1 x 4096 x 14336 7.0 / 8.6 / 11.4, gated 1 x
-    // 4096 x 4096 4.9 / 5.6 / 7.3).  Past half the SMs a CTA to a tile with the whole SM's ring: gated
-    // 16 x 14336 x 4096 14.7, where two with half a ring take 15.5; 64 x 14336 x 4096 11.3 / 16.6.
-    P.log_split = 0;
-    const bool share = 2 * tn <= sms;
-    while (share && P.log_split < 3 && 5 * (tn << P.log_split) < 6 * sms && (2 << P.log_split) <= nst) P.log_split++;
-    const int split = 1 << P.log_split;
-    P.stages = share || tn > sms ? C::kHalf : C::kWhole;
+    const TilePlan b = tile_plan(p.sizes(), sms);
+    P.log_split = b.log_split;
+    const int split = 1 << b.log_split;
+    P.stages = b.whole ? C::kWhole : C::kHalf;
     const int smem = C::smem(P.stages);
     static std::atomic<bool> attr_set[64];
     int dev = 0;
@@ -362,15 +356,8 @@ cudaError_t launch_by_tokens(const Product& p, int sms, cudaStream_t s) {
 }  // namespace
 }  // namespace mm
 
-// Up to 32 tokens the weight is streamed past them, up to 64 where it is long or has a tile for
-// half the SMs; more go to pairs of CTAs.  us, here / pairs: 32 x 1024 x 1024 4.4 / 4.8, 32 x 2048 x 2048
-// 4.7 / 6.0, gated 32 x 14336 x 4096 14.1 / 19.0; 64 x 4096 x 14336 12.4 / 16.7, 64 x 14336 x 4096 9.7 /
-// 10.2, gated 15.7 / 18.0; 64 x 1024 x 1024 6.9 / 5.0, 64 x 4096 x 4096 9.1 / 8.3, gated 64 x 2048 x 2048
-// 11.0 / 6.8.
 cudaError_t launch_product(const Product& p, int sms, cudaStream_t s) {
-    const bool long_or_wide = p.k >= 8192 || 2 * ((p.p.rows + 127) / 128) > sms;
-    const int few = p.kind == kBf16 || p.mode == kGatedGrad ? 0 : long_or_wide ? 64 : 32;
-    if (p.q.rows > few) return launch_pair(p, sms, s);
+    if (!mm::few_tokens(p.sizes(), sms)) return launch_pair(p, sms, s);
     if (p.mode == kPlain)
         return p.kind == kMxfp4 ? mm::launch_by_tokens<kMxfp4, kPlain>(p, sms, s) : mm::launch_by_tokens<kNvfp4, kPlain>(p, sms, s);
     return p.kind == kMxfp4 ? mm::launch_by_tokens<kMxfp4, kGated>(p, sms, s) : mm::launch_by_tokens<kNvfp4, kGated>(p, sms, s);

@@ -4,6 +4,8 @@
 #include <cstdint>
 #include <cuda_runtime.h>
 
+#include "fp4_plan.h"
+
 namespace nvfp4 {
 
 // ---- mxfp4.cu
@@ -25,9 +27,6 @@ cudaError_t launch_repitch_bf16(const void* in, int64_t rows, int64_t cols, int6
 cudaError_t launch_zero_bf16(int64_t rows, int64_t cols, void* out, int64_t ldo, cudaStream_t s);
 
 // ---- fp4_gemm.cu
-enum { kNvfp4 = 0, kMxfp4 = 1, kBf16 = 2 };                  // operand kinds of a product
-enum { kPlain = 0, kGated = 1, kGatedGrad = 2 };             // what the epilogue makes of the accumulators
-
 // An operand of a product.
 struct Operand {
     const void* data;      // packed codes [rows, k/2]; bf16 [rows][ld], K along the row, or with `along` [k][ld]
@@ -54,6 +53,8 @@ struct Product {
     int64_t fp;
     int* status;
     int starve;            // 1: the waits for the operands run out (self-test)
+
+    mm::Sizes sizes() const { return mm::Sizes{kind, mode, out_f32, q.rows, p.rows, k, q.ld}; }
 };
 cudaError_t launch_product(const Product& p, int sms, cudaStream_t s);
 // ---- fp4_pair.cu: the same for many tokens

@@ -35,11 +35,7 @@ namespace nvfp4 {
 namespace mm {
 namespace {
 
-constexpr int kEpiWarps = 8;
 constexpr int kThreadsPair = (kEpiWarps + 2) * 32;
-constexpr int kPairStages = 8;                               // at most
-constexpr int kBlock = 64 * kRow;                            // 64 contiguous rows by 64 steps of K, bf16
-constexpr int kPairSmem = 227 * 1024 - 256;                  // of a CTA, less its static part
 
 struct PairParams {
     CUtensorMap p, p2, q, sp, sp2, sq;
@@ -630,19 +626,6 @@ int row_alignment(const void* p, int64_t stride_bytes) {
     return bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 1;
 }
 
-// A slot of the ring: 128 rows of tokens, half a tile's columns (bf16: in blocks of 64), their
-// scales.  A multiple of 1024.
-int stage_bytes(int kind, int width) {
-    if (kind == kBf16) return (width > 128 ? 4 : 3) * kBlock;
-    return (128 + width / 2) * kRow + (width > 128 ? 3 : 2) * atoms(kind) * kAtom;
-}
-// A warp's box: 32 x 32 elements of a result whose rows allow no wide store.
-int box_bytes(const Product& p) { return p.out_f32 ? 4096 : 2048; }
-int ring_slots(const Product& p, int width) {
-    const int n = (kPairSmem - 1024 - kEpiWarps * box_bytes(p)) / stage_bytes(p.kind, width);
-    return n > kPairStages ? kPairStages : n;
-}
-
 template <int KIND, int MODE, bool SPLIT>
 cudaError_t launch_pair_as(const Product& p, int width, int split, int sms, cudaStream_t s) {
     using C = Pair<KIND>;
@@ -679,8 +662,8 @@ cudaError_t launch_pair_as(const Product& p, int width, int split, int sms, cuda
     }
     P.split = split;
     P.stage = stage_bytes(KIND, width);
-    P.box = box_bytes(p);
-    P.stages = ring_slots(p, width);
+    P.box = box_bytes(p.out_f32);
+    P.stages = ring_slots(p.sizes(), width);
     P.starve = p.starve;
     const int64_t pairs = SPLIT ? tiles * split : tiles < sms / 2 ? tiles : sms / 2;
     cudaLaunchConfig_t cfg = {};
@@ -700,48 +683,9 @@ cudaError_t launch_pair_as(const Product& p, int width, int split, int sms, cuda
     return cudaLaunchKernelEx(&cfg, kernel, P);
 }
 
-// How wide a tile is and how many pairs share its K: the least of an estimate in cycles.
-//   A stage takes its MMAs (2 a column) or its loads, 55 to 70 bytes a cycle and CTA with most SMs
-//   loading, 100 with few, or its share of the latency of HBM; a tile 1500 more, adding up a split K
-//   8000.  Narrow tiles fill the last wave (bf16 in steps of 32 columns; scale atoms start at 128 rows,
-//   so 4-bit tiles are 256 or 128 wide and gated ones 256) and shorten what a few tiles take; clusters of
-//   four or eight whole SMs have to find room (at most 36 and 15 on a GB300: 16 of eight ran one
-//   after the others).
-// us, always 256 wide and split from 32 stages on / as estimated: 77 x 1001 x 2080 (fp32) 7.9 / 6.4, 512 x
-// 1024 x 1024 6.0 / 5.1, 256 x 4096 x 14336 17.8 / 15.7, 200 x 512 x 14336 13.4 / 10.8; with gradients 2048
-// x 4096 x 4096 111 / 106.
-struct Plan {
-    int width = 256, split = 1;
-};
-Plan plan(const Product& p, int sms) {
-    const int64_t pairs = sms > 1 ? sms / 2 : 1, tiles_t = (p.q.rows + 255) / 256, nst = (p.k + stage_k(p.kind) - 1) / stage_k(p.kind);
-    const int least = p.mode != kPlain ? 256 : 128, step = p.kind == kBf16 ? 32 : 128;
-    // bf16 rows that start inside a 128-byte line take two of L2's
-    const int64_t full_rate = p.kind != kBf16 ? 62 : p.q.ld % 64 == 0 ? 70 : 55;
-    Plan best;
-    int64_t least_cost = INT64_MAX;
-    for (int w = 256; w >= least; w -= step) {
-        const int64_t columns = p.mode == kPlain ? w : 128, tiles = tiles_t * ((p.p.rows + columns - 1) / columns);
-        const int64_t bytes = stage_bytes(p.kind, w), latency = 2900 / ring_slots(p, w);
-        for (int split = 1; split <= 4; split *= 2) {
-            if (split > 1 && (w % 128 != 0 || nst < 8 * split || tiles > (split == 2 ? sms / 4 - 2 : sms / 8 - 4))) continue;
-            const int64_t rate = 2 * tiles * split > pairs ? full_rate : 100;
-            const int64_t moved = bytes / rate > latency ? bytes / rate : latency, stage = moved > 2 * w ? moved : 2 * w;
-            const int64_t waves = split > 1 ? 1 : (tiles + pairs - 1) / pairs;
-            const int64_t cost = waves * ((nst + split - 1) / split * stage + 1500) + (split > 1 ? 8000 : 0);
-            if (least_cost == INT64_MAX || 32 * cost < 31 * least_cost) {   // not for a difference the estimate cannot see
-                least_cost = cost;
-                best.width = w;
-                best.split = split;
-            }
-        }
-    }
-    return best;
-}
-
 template <int KIND, int MODE>
 cudaError_t launch_pair_mode(const Product& p, int sms, cudaStream_t s) {
-    const Plan b = plan(p, sms);
+    const PairPlan b = pair_plan(p.sizes(), sms);
     return b.split > 1 ? launch_pair_as<KIND, MODE, true>(p, b.width, b.split, sms, s)
                        : launch_pair_as<KIND, MODE, false>(p, b.width, 1, sms, s);
 }

@@ -12,15 +12,6 @@ namespace mm {
 
 using namespace tc;
 
-// An operand tile is staged as rows of 128 bytes (one swizzle row) along K: 256 codes or
-// 64 bf16, four MMAs of 32 bytes each.  Scales come as 512-byte atoms of 128 rows by
-// four scale columns, 64 (NVFP4) or 128 (MXFP4) elements of K.
-__host__ __device__ constexpr int stage_k(int kind) { return kind == kBf16 ? 64 : 256; }
-__host__ __device__ constexpr int mma_k(int kind) { return kind == kBf16 ? 16 : 64; }
-__host__ __device__ constexpr int atoms(int kind) { return kind == kNvfp4 ? 4 : kind == kMxfp4 ? 2 : 0; }
-constexpr int kAtom = 512;
-constexpr int kRow = 128;                                    // bytes of an operand row in a stage
-
 // Instruction descriptor.  kind::f16: D fp32 (bits 4-5 = 1), A and B bf16 (7-9, 10-12 =
 // 1), N >> 3 (17-22), M >> 4 (24-28).  kind::mxf4nvf4: A and B E2M1 (7-9, 10-12 = 1), N >> 3
 // (17-22), scales UE4M3 = 0 or UE8M0 = 1 (23), M >> 7 (27-28), which of a cell's scale
