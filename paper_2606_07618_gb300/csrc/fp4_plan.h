@@ -2,6 +2,7 @@
 // pairs share its K.  Host code without CUDA, so that the choices can be checked without a GPU.
 #pragma once
 #include <cstdint>
+#include <initializer_list>
 
 #ifdef __CUDACC__
 #define NVFP4_BOTH __host__ __device__
@@ -83,10 +84,10 @@ inline int ring_slots(const Sizes& p, int width) {
 // How wide a tile is and how many pairs share its K: the least of an estimate in cycles.
 //   A stage takes its MMAs (2 a column) or its loads, 55 to 70 bytes a cycle and CTA with most SMs
 //   loading, 100 with few, or its share of the latency of HBM; a tile 1500 more, adding up a split K
-//   8000.  Narrow tiles fill the last wave (bf16 in steps of 32 columns; scale atoms start at 128 rows,
-//   so 4-bit tiles are 256 or 128 wide and gated ones 256) and shorten what a few tiles take; clusters of
-//   four or eight whole SMs have to find room (at most 36 and 15 on a GB300: 16 of eight ran one
-//   after the others).
+//   8000.  Narrow tiles fill the last wave (bf16 224 too; 192 and 160 load as much as that, for fewer
+//   columns; a 4-bit tile takes whole scale atoms of 128 rows, so it is 256 or 128 wide and a gated one
+//   256) and shorten what a few tiles take; clusters of four or eight whole SMs have to find room (at
+//   most 36 and 15 on a GB300: 16 of eight ran one after the others).
 // us, always 256 wide and split from 32 stages on / as estimated: 77 x 1001 x 2080 (fp32) 7.9 / 6.4, 512 x
 // 1024 x 1024 6.0 / 5.1, 256 x 4096 x 14336 17.8 / 15.7, 200 x 512 x 14336 13.4 / 10.8; with gradients 2048
 // x 4096 x 4096 111 / 106.
@@ -95,12 +96,12 @@ struct PairPlan {
 };
 inline PairPlan pair_plan(const Sizes& p, int sms) {
     const int64_t pairs = sms > 1 ? sms / 2 : 1, tiles_t = (p.t + 255) / 256, nst = p.stages();
-    const int least = p.mode != kPlain ? 256 : 128, step = p.kind == kBf16 ? 32 : 128;
     // bf16 rows that start inside a 128-byte line take two of L2's
     const int64_t full_rate = p.kind != kBf16 ? 62 : p.ldq % 64 == 0 ? 70 : 55;
     PairPlan best;
     int64_t least_cost = INT64_MAX;
-    for (int w = 256; w >= least; w -= step) {
+    for (const int w : {256, 224, 128}) {
+        if (w != 256 && (p.mode != kPlain || (w == 224 && p.kind != kBf16))) continue;
         const int64_t columns = p.mode == kPlain ? w : 128, tiles = tiles_t * ((p.n + columns - 1) / columns);
         const int64_t bytes = stage_bytes(p.kind, w), latency = 2900 / ring_slots(p, w);
         for (int split = 1; split <= 4; split *= 2) {

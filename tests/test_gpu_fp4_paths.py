@@ -14,15 +14,15 @@ from test_gpu_fp4 import (DEV, B, H, U, Held, bf16, gated_bounds, gated_operands
 pytestmark = pytest.mark.gpu
 
 MATMUL = [((9, 300, 800), (16, 4, False)), ((3, 9800, 64), (16, 1, True)), ((20, 9800, 160), (32, 1, True)),
-          ((20, 19500, 64), (32, 1, False)),  ((25, 200, 288), (32, 2, False)), ((31, 300, 1056), (32, 4, False)), ((40, 19500, 96), (64, 1, False)),
-          ((50, 9900, 288), (64, 1, True)), ((64, 5900, 8192), (64, 4, False)), ((37, 200, 8224), (64, 8, False)),
+          ((20, 19500, 64), (32, 1, False)), ((25, 200, 288), (32, 2, False)), ((31, 300, 1056), (32, 4, False)),
+          ((40, 19500, 96), (64, 1, False)), ((50, 9900, 288), (64, 1, True)), ((64, 5900, 8192), (64, 4, False)), ((37, 200, 8224), (64, 8, False)),
           ((1700, 2561, 64), (128, 1, True)), ((100, 3900, 16384), (128, 2, False)), ((1300, 1111, 16384), (256, 2, False)),
           ((1300, 3300, 608), (256, 1, True))]
 
 GATED = [((9, 320, 800), (16, 4, False)), ((3, 9824, 64), (16, 1, True)), ((20, 9824, 160), (32, 1, True)),
          ((20, 19488, 64), (32, 1, False)), ((25, 192, 288), (32, 2, False)), ((31, 320, 1056), (32, 4, False)),
-         ((32, 96, 2080), (32, 8, False)), ((40, 19488, 96), (64, 1, False)), ((50, 9920, 288), (64, 1, True)), ((64, 5920, 8192), (64, 4, False)),
-         ((37, 192, 8224), (64, 8, False)), ((1300, 2080, 96), (256, 1, True)), ((1300, 2112, 352), (256, 1, True)),
+         ((32, 96, 2080), (32, 8, False)), ((40, 19488, 96), (64, 1, False)), ((50, 9920, 288), (64, 1, True)),
+         ((64, 5920, 8192), (64, 4, False)), ((37, 192, 8224), (64, 8, False)), ((1300, 2080, 96), (256, 1, True)), ((1300, 2112, 352), (256, 1, True)),
          ((1300, 2049, 352), (256, 1, True)), ((700, 4000, 608), (256, 1, True)), ((300, 2080, 12320), (256, 2, False))]
 
 MATMUL_GRADS = [((64, 4096, 256), (128, 4, False), (128, 1, False)), ((77, 4096, 4096), (128, 2, False), (256, 1, True)),
