@@ -18,10 +18,14 @@
  * Conventions are those of nvfp4ss.h: row-major tensors, device-accessible pointers that
  * the caller owns, no allocation and no synchronisation, every call asynchronous on
  * `stream`, argument errors returned before any launch.  Products are exact, sums are
- * held in fp32 and rounded once to the output's type; no result depends on timing: sums
- * split over several thread blocks are added in a fixed order.
+ * held in fp32, multiplied by the global scales in fp32 and rounded once to the output's type;
+ * no result depends on timing: sums split over several thread blocks are added in a fixed
+ * order.  That order follows from the sizes, so the same rows in calls of other sizes may differ in
+ * fp32's last places.
  *   - cols (the contraction) of a product's operands is a multiple of 32 and at least 32,
  *     for either format: the tensor core's loads need rows of whole 16 bytes.
+ *   - A product's operands have at most 8388480 rows (65535 * 128) and 2^30 columns, 8388480 where
+ *     gradients are formed; larger ones return NVFP4_ERR_RANGE, and their workspace queries 0.
  *   - codes and sf of an operand are 16-byte aligned; dense tensors need their element's
  *     alignment, and run faster with 16-byte aligned bases and row strides.
  *   - Row strides (ld*) are in elements and at least the row's length.
@@ -98,8 +102,8 @@ nvfp4_status fp4_selftest_wait_timeout(fp4_format fmt, const fp4_operand* a, con
  * Gradients of fp4_matmul with respect to the values of its operands, from dD:
  *   dA = dD B [m, k],  dB = dD^T A [n, k],
  * all bf16 with row strides lddd, ldda, lddb; either of dA and dB may be NULL.  The
- * operands' values without S are exact in bf16, so the sums' only rounding is fp32's,
- * then the results' to bf16.
+ * operands' values without S are exact in bf16 (those past fp32's range, of E8M0 codes 253 and
+ * 254, are infinite), so the sums' only rounding is fp32's, then the results' to bf16.
  *   workspace  fp4_matmul_backward_workspace(m, n, k) bytes, 256-byte aligned.
  */
 size_t fp4_matmul_backward_workspace(int64_t m, int64_t n, int64_t k);
@@ -127,11 +131,13 @@ nvfp4_status fp4_gated_ff(fp4_format fmt, fp4_activation act, const fp4_operand*
  * Gradients of the gated feed-forward with respect to the values of its operands, from
  * dh [t, f] bf16 (row stride lddh).  g and u are computed again (nothing is kept from the
  * forward call), then
- *   dg = dh * u * act'(g),  du = dh * act(g)      (fp32, rounded once to bf16)
+ *   dg = dh * u * act'(g),  du = dh * act(g)      (fp32, rounded once to bf16: by up to 2^-8,
+ *                                                  the operands of the two lines that follow)
  *   dx = dg Wg + du Wu [t, d],  dWg = dg^T x,  dWu = du^T x [f, d]   (bf16, row strides)
  *   d_x      optional, row stride lddx.
  *   d_gate, d_up  optional (both or neither: frozen weights), row stride lddw.
- *   h        optional: the forward result too, as fp4_gated_ff writes it (row stride ldh).
+ *   h        optional: the forward result too (row stride ldh).  fp4_gated_ff adds up fewer than 65
+ *            tokens' sums in another order, so a few of its last bits may differ there.
  *   workspace  fp4_gated_ff_backward_workspace(t, f, d) bytes, 256-byte aligned.
  */
 size_t fp4_gated_ff_backward_workspace(int64_t t, int64_t f, int64_t d);

@@ -274,7 +274,7 @@ nvfp4_status fp4_selftest_wait_timeout(fp4_format fmt, const fp4_operand* a, con
 }
 
 size_t fp4_matmul_backward_workspace(int64_t m, int64_t n, int64_t k) {
-    if (m <= 0 || n <= 0 || k <= 0 || m > kMaxRows || n > kMaxRows || k > kMaxCols) return 0;
+    if (m <= 0 || n <= 0 || k <= 0 || m > kMaxRows || n > kMaxRows || k > kMaxRows) return 0;
     return MatmulGrad(m, n, k).bytes();
 }
 
@@ -367,7 +367,7 @@ nvfp4_status fp4_gated_ff(fp4_format fmt, fp4_activation act, const fp4_operand*
 }
 
 size_t fp4_gated_ff_backward_workspace(int64_t t, int64_t f, int64_t d) {
-    if (t <= 0 || f <= 0 || d <= 0 || t > kMaxRows || f > kMaxRows || d > kMaxCols) return 0;
+    if (t <= 0 || f <= 0 || d <= 0 || t > kMaxRows || f > kMaxRows || d > kMaxRows) return 0;
     return GatedGrad(t, f, d).bytes();
 }
 
