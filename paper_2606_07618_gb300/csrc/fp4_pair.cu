@@ -1,5 +1,5 @@
 // Products of many tokens, and the bf16 ones of gradients: a pair of CTAs (cta_group::2) forms
-// 256 tokens by 256 columns or fewer (gated: 128 gate and the same 128 up columns) and walks
+// 256 tokens by 256, 224 or 128 columns (gated: 128 gate and the same 128 up columns) and walks
 // several such tiles.
 //
 //   out[t][n] = epilogue( sum_k q[t][k] p[n][k] )
@@ -8,9 +8,10 @@
 // one row: whole sectors to store, and a block of 32 for MXFP4.  Each CTA
 // loads its 128 token rows and half of the tile's columns; the leader's MMA reads both halves,
 // so a stage of K costs 64 KB of loads for 256 x 256 x 128 bytes of K.  An MMA takes 128 cycles for
-// 32 bytes of K of any type, a stage at least 512.  Shared memory is the bound of 4-bit products: 38
-// KB in, 38 out (operands and scales) at 128 bytes a cycle are 601 cycles a stage for NVFP4, 555 for MXFP4;
-// 8192 x 4096 x 14336 takes 606 and 570 (129 and 122 us, 7.5 and 7.9 PFLOP/s).  bf16: 515, MMAs.
+// 32 bytes of K of any type, a stage at least 512.  4-bit products take 606 cycles a stage in NVFP4 and 570
+// in MXFP4 (8192 x 4096 x 14336 in short loops: 129 and 122 us, 7.5 and 7.9 PFLOP/s), which is what
+// shared memory needs for 38 KB in and 38 out (operands and scales) at 128 bytes a cycle, 601 and 555; the
+// loads alone take 530, so what L2 delivers is not far behind.  bf16: 515, MMAs.
 //
 // bf16 operands come as they lie: K along the rows (dg and du for d_x), or down the rows (values of
 // weights and activations; dg, du for the weights' gradients), then in blocks of 64 contiguous rows by 64
@@ -232,7 +233,11 @@ struct Rows {
 #pragma unroll
             for (int j = 0; j < 16; j++) hw[j] = pack2_bf16(g[2 * j] * u[2 * j], g[2 * j + 1] * u[2 * j + 1]);
         } else {
-            // dh is zero where there is no token or no column, and with it dg and du
+            // dh is zero where there is no token or no column, and with it dg and du.  They are rounded to bf16, by up
+            // to 2^-8 each, as the operands of the products that follow: the gradients are then 0.0023 off (relative,
+            // of a training step of 4096 tokens), 0.0017 of it the rounding of their own bf16.  fp16 has no room for
+            // gradients' exponents nor for E8M0's; two bf16 terms would double products that are three quarters of
+            // the step.
             float da[32];
             activate32<true>(e.act, g, da);
             uint32_t gt[16], ut[16];
