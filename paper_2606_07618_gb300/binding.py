@@ -408,7 +408,8 @@ def _status(t):
 
 def _operand(m, fmt: int, what: str):
     """(codes [rows, cols/2], 128x4-atom scales, S or None) as the bytes of an fp4_operand (a
-    ctypes.Structure takes three times as long to fill, on a path of a few microseconds), its rows and cols."""
+    ctypes.Structure takes three times as long to fill, on a path of a few microseconds), its rows and cols.
+    Which format the scales are in is the caller's word: both are bytes, in as many atoms where cols are few."""
     codes, sf, S = m
     rows, half = codes.shape
     if not codes.is_contiguous():
