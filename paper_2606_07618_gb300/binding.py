@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libnvfp4ss.so (include/nvfp4ss.h, include/nvfp4mm.h).
+"""Thin ctypes binding of libnvfp4ss.so (include/nvfp4ss.h, include/nvfp4mm.h, include/nvfp4kv.h).
 
 Every function has the name of the C entry point it calls and only marshals
 arguments: torch CUDA tensors become device pointers, the current torch CUDA
@@ -24,6 +24,9 @@ NVFP4_WINDOW_TIGHT = -(2 ** 31) + 1
 
 FP4_FMT_NVFP4, FP4_FMT_MXFP4 = 0, 1
 FP4_ACT_SILU, FP4_ACT_GELU_TANH = 0, 1
+NVFP4_ROPE_NEIGHBOURS, NVFP4_ROPE_HALVES = 0, 1
+NVFP4_ROPE_PLAIN, NVFP4_ROPE_LINEAR, NVFP4_ROPE_BASE, NVFP4_ROPE_BANDS = 0, 1, 2, 3
+NVFP4_KV_ABSMAX, NVFP4_KV_SWEEP = 0, 1
 
 STATUS = {0: "NVFP4_OK", 1: "NVFP4_ERR_INVALID_ARG", 2: "NVFP4_ERR_UNSUPPORTED", 3: "NVFP4_ERR_ALIGNMENT",
           4: "NVFP4_ERR_RANGE", 5: "NVFP4_ERR_CUDA"}
@@ -58,6 +61,12 @@ class GroupTensor(ctypes.Structure):
 class Fp4Operand(ctypes.Structure):
     """fp4_operand: codes, 128x4-atom scales and global scale of a quantised matrix."""
     _fields_ = [("codes", ctypes.c_void_p), ("sf", ctypes.c_void_p), ("S", ctypes.c_void_p)]
+
+
+class KvCache(ctypes.Structure):
+    """nvfp4_kv_cache: the pool of pages, its scales and sizes."""
+    _fields_ = [("codes", ctypes.c_void_p), ("sf", ctypes.c_void_p), ("S_k", ctypes.c_void_p), ("S_v", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("page", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32)]
 
 
 def library_path() -> str:
@@ -109,6 +118,19 @@ def lib() -> ctypes.CDLL:
         L.fp4_gated_ff_backward_workspace.restype = sz
         L.fp4_gated_ff_backward.argtypes = [i, i, op, op, op, i64, i64, i64, p, i64, p, i64, p, p, i64, p, i64, p, p, sz,
                                             p]
+        d, i32 = ctypes.c_double, ctypes.c_int32
+        L.nvfp4_rope_turns.argtypes = [i, d, i, d, d, d, d, p]
+        L.nvfp4_rope.argtypes = [p, i64, i64, p, i64, i64, i, i64, i32, i32, i32, p, p, f, i, i, p]
+        L.nvfp4_kv_write.argtypes = [p, p, i64, i64, p, i64, i64, i, i64, p, i, p, p]
+        L.nvfp4_kv_read.argtypes = [p, p, i64, i64, p, p, i64, p, i64, i64, p, i64, i64, i, i64, p, p]
+        L.nvfp4_kv_attention_workspace.argtypes = [p, i64, i32, i64, i64, i64, i64]
+        L.nvfp4_kv_attention_workspace.restype = sz
+        L.nvfp4_kv_attention.argtypes = [p, p, i64, i64, i64, i32, p, i64, i64, p, p, i64, i64, f, i, p, i64, i64, p, p, p, sz, p]
+        L.nvfp4_kv_attention_prefix.argtypes = [p, p, i64, i64, i64, i32, p, i64, p, p, i64, i64, p, p, i64, i64, f, i, p, i64, i64,
+                                                p, p, p, sz, p]
+        for fn in ("nvfp4_rope_turns", "nvfp4_rope", "nvfp4_kv_write", "nvfp4_kv_read", "nvfp4_kv_attention",
+                   "nvfp4_kv_attention_prefix"):
+            getattr(L, fn).restype = i
         for fn in ("mxfp4_quantize", "mxfp4_dequantize", "fp4_matmul", "fp4_selftest_wait_timeout", "fp4_matmul_backward",
                    "fp4_gated_ff", "fp4_gated_ff_backward"):
             getattr(L, fn).restype = i
@@ -541,3 +563,177 @@ def fp4_gated_ff_backward(fmt: int, act: int, x, w_gate, w_up, d_h, d_x=None, d_
                                                _status(status), _buffer(workspace, 0, "workspace"), ws_bytes,
                                                _stream(stream))
     _check("fp4_gated_ff_backward", rc)
+
+
+# --------------------------------------------------------------------------- the key/value cache (nvfp4kv.h)
+_I64 = torch.int64
+_pack_cache = struct.Struct("4PqiiiP").pack                      # the last word pads the structure's end
+
+
+def _cache(c):
+    """(codes [pages, heads, 2, page, dim/2], sf [pages, heads, 2, dim/16, page], S_k, S_v) as the bytes of an
+    nvfp4_kv_cache, its heads, dim and page."""
+    codes, sf, S_k, S_v = c
+    pages, heads, two, page, half = codes.shape
+    dim = 2 * half
+    if two != 2 or sf.shape != (pages, heads, 2, dim // 16, page):
+        raise ValueError(f"cache: codes {tuple(codes.shape)} and scales {tuple(sf.shape)} do not belong together")
+    if not (codes.itemsize == sf.itemsize == 1):
+        raise TypeError(f"cache: codes and scales in bytes are wanted, not {codes.dtype} and {sf.dtype}")
+    if not (codes.is_contiguous() and sf.is_contiguous()):
+        raise ValueError("cache: contiguous codes and scales are wanted")
+    for S in (S_k, S_v):
+        if S.dtype is not _F32 or S.numel() != 1:
+            raise TypeError(f"cache: one float32 as S is wanted, not {tuple(S.shape)} of {S.dtype}")
+    return _pack_cache(codes.data_ptr(), sf.data_ptr(), S_k.data_ptr(), S_v.data_ptr(), pages, page, heads, dim, 0), heads, dim, page
+
+
+def _heads3(t, what: str):
+    """Pointer, token and head stride of a [tokens, heads, dim] tensor whose innermost dimension is contiguous."""
+    if t.dim() != 3:
+        raise ValueError(f"{what}: [tokens, heads, dim] is wanted, not {tuple(t.shape)}")
+    token, head, one = t.stride()
+    tokens, heads, dim = t.shape
+    if one != 1 and dim > 1:
+        raise ValueError(f"{what}: a contiguous innermost dimension is wanted")
+    if tokens <= 1:
+        token = max(token, heads * head, dim)
+    if heads <= 1:
+        head = max(head, dim)
+    return t.data_ptr(), token, head
+
+
+def _list(t, n: int, dtype, what: str):
+    """Pointer of n contiguous numbers of a type, on the device."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{what}: {dtype} is wanted, not {t.dtype}")
+    if t.dim() != 1 or t.numel() < n or (t.numel() > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what}: {n} contiguous numbers are wanted, not {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _pages(t, what: str):
+    """Pointer, row stride, rows and width of a page table."""
+    if t.dtype is not _I32:
+        raise TypeError(f"{what}: {_I32} is wanted, not {t.dtype}")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: [sequences, pages] with contiguous rows is wanted, not {tuple(t.shape)}")
+    rows, width = t.shape
+    return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), width), rows, width
+
+
+def nvfp4_rope_turns(rot: int, base: float = 10000.0, scaling: int = NVFP4_ROPE_PLAIN, factor: float = 1.0,
+                     original_len: float = 0.0, slow: float = 1.0, fast: float = 4.0, device="cuda"):
+    """The frequency table [rot/2] int64 (the bits of 64-bit fractions of a turn) of nvfp4_rope, on `device`."""
+    turns = torch.empty(max(int(rot) // 2, 0), dtype=_I64)
+    rc = (_lib or lib()).nvfp4_rope_turns(int(rot), float(base), int(scaling), float(factor), float(original_len), float(slow),
+                                          float(fast), turns.data_ptr())
+    _check("nvfp4_rope_turns", rc)
+    return turns.to(device)
+
+
+def nvfp4_rope(x, positions, turns, out=None, magnitude: float = 1.0, layout: int = NVFP4_ROPE_HALVES, inverse: bool = False,
+               stream=None):
+    """Rotary positions of x [tokens, heads, dim] (bf16 or fp32): the first 2 * len(turns) elements of each head; inverse: the
+    gradient of x from that of out.  out None: in place."""
+    if out is None:
+        out = x
+    if out.dtype is not x.dtype:
+        raise TypeError(f"out: {x.dtype} is wanted, not {out.dtype}")
+    if out.shape != x.shape:
+        raise ValueError(f"out: shape {tuple(x.shape)} is wanted, not {tuple(out.shape)}")
+    px, xt, xh = _heads3(x, "x")
+    po, ot, oh = _heads3(out, "out")
+    tokens, heads, dim = x.shape
+    rot = 2 * turns.numel()
+    rc = (_lib or lib()).nvfp4_rope(px, xt, xh, po, ot, oh, _dtype(x), tokens, heads, dim, rot,
+                                    _list(positions, tokens, _I64, "positions"), _list(turns, rot // 2, _I64, "turns"),
+                                    magnitude, layout, 1 if inverse else 0, _stream(stream))
+    _check("nvfp4_rope", rc)
+    return out
+
+
+def _kv_pair(k, v, tokens, heads: int, dim: int, what: str):
+    """Pointers and strides of k and v (either None), their dtype code and rows."""
+    args, dt = [], None
+    for t, name in ((k, "k"), (v, "v")):
+        if t is None:
+            args += (None, 0, 0)
+            continue
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+            raise ValueError(f"{name}: [tokens, {heads}, {dim}] is wanted, not {tuple(t.shape)}")
+        if tokens is None:
+            tokens, dt = t.shape[0], t.dtype
+        if t.shape[0] != tokens or t.dtype is not dt:
+            raise ValueError(f"{what}: k and v of one type and as many tokens are wanted")
+        args += _heads3(t, name)
+    if dt is None:
+        raise ValueError(f"{what}: k or v is wanted")
+    return args, NVFP4_IN_BF16 if dt is _BF16 else _dtype(k if k is not None else v), tokens
+
+
+def nvfp4_kv_write(cache, k, v, slots, method: int = NVFP4_KV_SWEEP, status=None, stream=None):
+    """Quantises k and v [tokens, heads, dim] (bf16 or fp32, either None) into the cache at slots [tokens] (page * size +
+    offset; negative: skipped)."""
+    c, heads, dim, _ = _cache(cache)
+    args, dt, tokens = _kv_pair(k, v, None, heads, dim, "nvfp4_kv_write")
+    rc = (_lib or lib()).nvfp4_kv_write(c, *args, dt, tokens, _list(slots, tokens, _I64, "slots"), method, _status(status),
+                                        _stream(stream))
+    _check("nvfp4_kv_write", rc)
+
+
+def nvfp4_kv_read(cache, table, starts, offsets, k=None, v=None, status=None, stream=None):
+    """Rows offsets[b] .. offsets[b+1] of k and v [tokens, heads, dim] (bf16 or fp32, either None) = tokens starts[b] .. of
+    sequence b (starts None: from 0)."""
+    c, heads, dim, _ = _cache(cache)
+    args, dt, tokens = _kv_pair(k, v, None, heads, dim, "nvfp4_kv_read")
+    pt, ld, batch, width = _pages(table, "table")
+    rc = (_lib or lib()).nvfp4_kv_read(c, pt, ld, width, None if starts is None else _list(starts, batch, _I32, "starts"),
+                                       _list(offsets, batch + 1, _I32, "offsets"), batch, *args, dt, tokens, _status(status),
+                                       _stream(stream))
+    _check("nvfp4_kv_read", rc)
+
+
+def nvfp4_kv_attention_workspace(cache, q, batch: int, width: int, max_q: int, prefix_width: int = 0) -> int:
+    """Bytes of workspace of attention for queries q [tokens, q_heads, dim] and page tables of these widths."""
+    return (_lib or lib()).nvfp4_kv_attention_workspace(_cache(cache)[0], q.shape[0], q.shape[1], batch, width, max_q,
+                                                        prefix_width)
+
+
+def _attention(fn: str, q, cache, prefix, table, lens, offsets, max_q, scale, out, causal, lse, workspace, status, stream):
+    c, heads, dim, _ = _cache(cache)
+    if q.dtype is not _BF16 or out.dtype is not _BF16:
+        raise TypeError(f"{fn}: queries and results in bfloat16 are wanted, not {q.dtype} and {out.dtype}")
+    if q.dim() != 3 or q.shape[2] != dim or q.shape != out.shape:
+        raise ValueError(f"{fn}: q and out of [tokens, heads, {dim}] are wanted, not {tuple(q.shape)} and {tuple(out.shape)}")
+    tokens, q_heads, _ = q.shape
+    if q_heads < 1 or q_heads % heads:
+        raise ValueError(f"{fn}: a multiple of {heads} query heads is wanted, not {q_heads}")
+    if lse is not None:
+        if lse.dtype is not _F32:
+            raise TypeError(f"lse: {_F32} is wanted, not {lse.dtype}")
+        if lse.shape != (tokens, q_heads) or not lse.is_contiguous():
+            raise ValueError(f"lse: contiguous, of shape {(tokens, q_heads)}, is wanted")
+    pt, ld, batch, width = _pages(table, "table")
+    rc = getattr(_lib or lib(), fn)(c, *_heads3(q, "q"), tokens, q_heads, *prefix, pt, ld, width, _list(lens, batch, _I32, "lens"),
+                                    _list(offsets, batch + 1, _I32, "offsets"), batch, max_q, scale, 1 if causal else 0,
+                                    *_heads3(out, "out"), None if lse is None else lse.data_ptr(), _status(status),
+                                    _buffer(workspace, 0, "workspace"), workspace.nbytes if workspace is not None else 0,
+                                    _stream(stream))
+    _check(fn, rc)
+
+
+def nvfp4_kv_attention(q, cache, table, lens, offsets, max_q: int, scale: float, out, causal: bool = True, lse=None,
+                       workspace=None, status=None, stream=None):
+    """out = softmax(scale q K^T) V for q, out [tokens, q_heads, dim] (bf16): rows offsets[b] .. of sequence b over its
+    lens[b] cached tokens.  lse [tokens, q_heads] (fp32) optional."""
+    _attention("nvfp4_kv_attention", q, cache, (), table, lens, offsets, max_q, scale, out, causal, lse, workspace, status,
+               stream)
+
+
+def nvfp4_kv_attention_prefix(q, cache, prefix, prefix_len, table, lens, offsets, max_q: int, scale: float, out,
+                              causal: bool = True, lse=None, workspace=None, status=None, stream=None):
+    """The same where every query also sees the first prefix_len (int32, one element) tokens of the pages prefix [pages]."""
+    pre = (_list(prefix, 0, _I32, "prefix"), prefix.numel(), _list(prefix_len.reshape(-1), 1, _I32, "prefix_len"))
+    _attention("nvfp4_kv_attention_prefix", q, cache, pre, table, lens, offsets, max_q, scale, out, causal, lse, workspace,
+               status, stream)

@@ -18,7 +18,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libnvfp4ss.so")
 SOURCES = ["api.cu", "quantize.cu", "quantize_dynamic.cu", "scale_dequant.cu", "global_scale_noalloc.cu",
-           "optimal_scale.cu", "ldlq.cu", "quantize_group.cu", "mxfp4.cu", "fp4_gemm.cu", "fp4_pair.cu", "fp4_api.cu"]
+           "optimal_scale.cu", "ldlq.cu", "quantize_group.cu", "mxfp4.cu", "fp4_gemm.cu", "fp4_pair.cu", "fp4_api.cu",
+           "kv_api.cu", "rope.cu", "kv_cache.cu", "kv_attention.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -40,7 +41,7 @@ def _flags(verbose: bool) -> list[str]:
 def _inputs() -> list[str]:
     files = [os.path.join(CSRC, s) for s in SOURCES]
     files += [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
-    files += [os.path.join(ROOT, "include", f) for f in ("nvfp4ss.h", "nvfp4mm.h")]
+    files += [os.path.join(ROOT, "include", f) for f in ("nvfp4ss.h", "nvfp4mm.h", "nvfp4kv.h")]
     return files
 
 

@@ -1,0 +1,565 @@
+// Attention over the NVFP4 key/value cache for few rows a key head (nvfp4_kv_attention,
+// nvfp4_kv_attention_prefix).
+//
+// A value q s (without S) has at most 5 significant bits and lies in 2^-10 .. 2688, so fp16 holds
+// it exactly; a query's row is scaled by a power of two to below 2 and is exact in fp16 too
+// but for elements below 2^-14 of the row's largest.  Both products run on mma.sync
+// m16n8k16 (fp16 operands, fp32 sums): with 8 or 16 rows they take a fifth of the time that the
+// conversion of the cache's codes takes, and that goes straight from global memory to
+// registers, in the layout that the MMA's operands want.
+//
+// Transposed products, so that the rows of queries are the MMA's narrow dimension:
+//   S^T [tokens 16, rows 8] = K Q^T,   O^T [dim 16, rows 8] += V^T P^T.
+// The order of the contracted index is free, as long as both operands share it.  A warp
+// takes 64 tokens; lane (g, t) = (lane / 4, lane % 4) reads
+//   keys:   of tokens 16 (g/2) + (g&1) + 2i, i = 0..7, the dim/4 elements from t dim/4 on,
+//           and their scales of 16 tokens with one load a block;
+//   values: of tokens 16 t .. 16 t + 15, the dim/8 elements from g dim/8 on.
+// Rows r and r + 8 of m-tile i of S^T are then tokens 16 (r/2) + 4i + (r&1) and two further, whose
+// weights, transposed by movmatrix, are the operand for the values of tokens 16 t + 4i .. + 3.
+// Two tokens' codes of one dim are brought side by side as nibbles, so that one conversion gives the
+// pair of fp16 that the MMA wants.
+//
+// Softmax runs over the tiles of a warp with the running maximum and sum, weights scaled by 2^15 (the
+// smallest then keep fp16's full precision down to 2^-29 of the largest); warps, and the parts that a
+// long cache is split into, are joined by their maxima, in a fixed order.
+#include "kv_kernels.h"
+#include "nvfp4_device.cuh"
+
+namespace nvfp4 {
+namespace kv {
+namespace {
+
+constexpr int kThreads = 128;
+constexpr float kWeightBits = 15.0f;
+
+__device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
+// The larger one; NaN if either is, so that a query with NaN gives NaN.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// Four bytes of E2M1 pairs -> four fp16 pairs.
+__device__ __forceinline__ void e2m1x8_to_f16(uint32_t w, uint32_t (&h)[4]) {
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+// Two E4M3 codes (16 bits) -> an fp16 pair.
+__device__ __forceinline__ uint32_t e4m3x2_to_f16(uint32_t codes) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
+    return h;
+}
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// What a block works on: the keys [begin, end) of one sequence or of the prefix, for one tile of rows.
+struct Job {
+    const int32_t* table;
+    int64_t width, begin, end;           // page numbers; tokens
+    int64_t row0, n, past;               // first row of q, queries; tokens that the first query sees, less one
+    int64_t first;                       // first row (query, head of the group) of the tile
+};
+
+template <int D, int NT>
+struct Tile {
+    static constexpr int R = 8 * NT;
+    static constexpr int KW = D / 32;    // words of codes of a token that a lane reads: keys
+    static constexpr int VW = D / 64;    // and values
+    static constexpr int KB = D / 64;    // key blocks of a lane
+};
+
+template <int W>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[W]) {
+    if constexpr (W == 4) {
+        const uint4 v = ld_stream16<false>(p);
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else if constexpr (W == 2) {
+        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    } else {
+        asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+    }
+}
+
+// PART: the result goes to the workspace as one of several parts (else to out).
+template <int D, int NT, bool PREFIX, bool PART>
+__global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, int64_t part0) {
+    using T = Tile<D, NT>;
+    __shared__ float s_o[4][T::R][D];
+    __shared__ float s_m[4][T::R], s_l[4][T::R];
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int head = blockIdx.y;
+    const int64_t tile = blockIdx.x % pass.tiles, rest = blockIdx.x / pass.tiles;
+    const int64_t part = rest % pass.parts, b = rest / pass.parts;
+
+    int64_t row0 = 0, n, len;
+    const int32_t* table;
+    int64_t width;
+    bool outside = false;
+    if (PREFIX) {
+        n = p.tokens;
+        len = *p.prefix_len;
+        table = p.prefix;
+        width = p.prefix_width;
+    } else {
+        row0 = p.offsets[b];
+        n = p.offsets[b + 1] - row0;
+        len = p.lens[b];
+        table = p.table + b * p.table_ld;
+        width = p.width;
+        if (row0 < 0 || n < 0 || row0 + n > p.tokens) {
+            outside = true;
+            n = 0;
+        }
+    }
+    if (len < 0 || len > (width << p.c.page_log2)) {
+        outside = true;
+        len = len < 0 ? 0 : width << p.c.page_log2;
+    }
+    const bool causal = !PREFIX && p.causal;
+    const int64_t computed = PREFIX || n < p.max_q ? n : p.max_q;
+    const int64_t first = tile * T::R, rows = computed * p.group;
+    if (p.status && outside && threadIdx.x == 0 && head == 0) atomicOr(p.status, kStatusBounds);
+    if (first >= rows) return;
+    // keys that the tile's last row sees
+    const int64_t last = (first + T::R < rows ? first + T::R : rows) - 1;
+    int64_t sees = causal ? len - n + last / p.group + 1 : len;
+    const int64_t begin = part * pass.chunk;
+    const int64_t end = begin + pass.chunk < sees ? begin + pass.chunk : sees;
+    if (PART && begin >= end) return;
+
+    // queries, scaled by a power of two, as the narrow operand: row 8 nt + g, elements from t D/4 on
+    uint32_t qf[NT][2 * T::KW][2];
+    float fac[NT][2], m[NT][2], l[NT][2];
+    int64_t lim[NT][2];
+    const float S = ld_f32(p.c.S_k) * p.scale * 1.4426950408889634f;
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        const int64_t r = first + 8 * nt + g;
+        uint32_t w[D / 8];
+#pragma unroll
+        for (int i = 0; i < D / 8; i++) w[i] = 0;
+        if (r < rows) {
+            const int64_t e = (row0 + r / p.group) * p.q.token + (head * (int64_t)p.group + r % p.group) * p.q.head + t * (D / 4);
+            const uint16_t* q = static_cast<const uint16_t*>(p.q.p) + e;
+            if (p.q.vec) {
+#pragma unroll
+                for (int i = 0; i < D / 32; i++) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(q + 8 * i);
+                    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 8; i++) w[i] = q[2 * i] | (uint32_t)q[2 * i + 1] << 16;
+            }
+        }
+        uint32_t top = 0;                                        // bf16 bits of the row's largest magnitude
+#pragma unroll
+        for (int i = 0; i < D / 8; i++) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^-e of the largest's exponent e, within fp32's normal powers; none for infinities and NaN
+        int e = (int)(top >> 7) - 127;
+        if (e == 128) e = 0;
+        e = e < -126 ? -126 : e > 126 ? 126 : e;
+        const float down = __int_as_float((127 - e) << 23), up = __int_as_float((127 + e) << 23);
+#pragma unroll
+        for (int i = 0; i < D / 8; i++)
+            qf[nt][i / 2][i & 1] = f16x2(bf16lo(w[i]) * down, bf16hi(w[i]) * down);
+#pragma unroll
+        for (int c = 0; c < 2; c++) {                            // columns 2t, 2t + 1 of the MMA's result
+            const int64_t rc = first + 8 * nt + 2 * t + c;
+            fac[nt][c] = S * __shfl_sync(0xffffffffu, up, (2 * t + c) * 4);
+            lim[nt][c] = rc < rows ? (causal ? len - n + rc / p.group + 1 : len) : 0;
+            m[nt][c] = neg_inf();
+            l[nt][c] = 0.0f;
+        }
+    }
+    float o[NT][D / 16][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int i = 0; i < D / 16; i++)
+#pragma unroll
+            for (int c = 0; c < 4; c++) o[nt][i][c] = 0.0f;
+    int64_t least = end;                                         // keys that every row sees
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int c = 0; c < 2; c++)
+            if (first + 8 * nt + 2 * t + c < rows && lim[nt][c] < least) least = lim[nt][c];
+#pragma unroll
+    for (int i = 1; i < 4; i *= 2) {
+        const int64_t other = __shfl_xor_sync(0xffffffffu, least, i);
+        least = other < least ? other : least;
+    }
+
+    const int page_mask = (1 << p.c.page_log2) - 1;
+    const int64_t head_codes = (int64_t)D << p.c.page_log2, part_codes = head_codes / 2;   // bytes of a page: a head's, K's
+    const int64_t part_sf = (int64_t)(D / 16) << p.c.page_log2;
+    for (int64_t k0 = begin + warp * kWarpTokens; k0 < end; k0 += 4 * kWarpTokens) {
+        // pages of this lane's keys (16-token group g / 2) and values (group t); -1: hidden
+        int64_t pages[2];
+        int at[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int64_t j = k0 + 16 * (i ? t : g >> 1);
+            int64_t pg = -1;
+            if (j < end) {
+                pg = table[j >> p.c.page_log2];
+                if (pg < 0 || pg >= p.c.pages) {
+                    outside = true;
+                    pg = -1;
+                }
+            }
+            pages[i] = pg;
+            at[i] = (int)(j & page_mask);
+        }
+        uint32_t kc[8][T::KW], ks[T::KB][4], vc[16][T::VW], vs[4];
+        const bool kv_ok = pages[0] >= 0, vv_ok = pages[1] >= 0;
+        const uint8_t* kp = p.c.codes + (pages[0] * p.c.heads + head) * head_codes + (at[0] + (g & 1)) * (D / 2) + t * (D / 8);
+        const uint8_t* kq = p.c.sf + (pages[0] * p.c.heads + head) * 2 * part_sf + ((int64_t)(t * T::KB) << p.c.page_log2) + at[0];
+        const uint8_t* vp = p.c.codes + (pages[1] * p.c.heads + head) * head_codes + part_codes + at[1] * (D / 2) + g * (D / 16);
+        const uint8_t* vq = p.c.sf + ((pages[1] * p.c.heads + head) * 2 + 1) * part_sf + ((int64_t)(g * D / 128) << p.c.page_log2) + at[1];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+#pragma unroll
+            for (int j = 0; j < T::KW; j++) kc[i][j] = 0;
+            if (kv_ok) load_words<T::KW>(kp + i * D, kc[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < T::KB; i++) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) ks[i][j] = 0;
+            if (kv_ok) load_words<4>(kq + ((int64_t)i << p.c.page_log2), ks[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+#pragma unroll
+            for (int j = 0; j < T::VW; j++) vc[i][j] = 0;
+            if (vv_ok) load_words<T::VW>(vp + i * (D / 2), vc[i]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++) vs[j] = 0;
+        if (vv_ok) load_words<4>(vq, vs);
+
+        float sc[NT][4][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int c = 0; c < 4; c++) sc[nt][i][c] = 0.0f;
+        const uint32_t pick = g & 1 ? 0x3232u : 0x1010u;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            uint32_t s0[T::KB], s1[T::KB];
+#pragma unroll
+            for (int k = 0; k < T::KB; k++) {
+                s0[k] = __byte_perm(e4m3x2_to_f16(ks[k][i] & 0xFFFF), 0, pick);
+                s1[k] = __byte_perm(e4m3x2_to_f16(ks[k][i] >> 16), 0, pick);
+            }
+#pragma unroll
+            for (int w = 0; w < T::KW; w++) {
+                uint32_t x[4], y[4];
+                e2m1x8_to_f16(kc[2 * i][w], x);
+                e2m1x8_to_f16(kc[2 * i + 1][w], y);
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const uint32_t a[4] = {mul_h2(x[2 * h], s0[w / 2]), mul_h2(y[2 * h], s1[w / 2]),
+                                           mul_h2(x[2 * h + 1], s0[w / 2]), mul_h2(y[2 * h + 1], s1[w / 2])};
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++) mma16(sc[nt][i], a, qf[nt][2 * w + h][0], qf[nt][2 * w + h][1]);
+                }
+            }
+        }
+        // weights
+        const bool whole = __all_sync(0xffffffffu, k0 + kWarpTokens <= least && kv_ok);
+        uint32_t pt[NT][4][2];
+        bool moved = false;
+        float alpha[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+            float top[2] = {neg_inf(), neg_inf()};
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    float v = sc[nt][i][c] * fac[nt][c & 1];
+                    if (!whole) {
+                        const int64_t j = k0 + 16 * (g >> 1) + 4 * i + (g & 1) + (c & 2);
+                        v = kv_ok && j < lim[nt][c & 1] && j < end ? v : neg_inf();
+                    }
+                    sc[nt][i][c] = v;
+                    top[c & 1] = max_nan(top[c & 1], v);
+                }
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+#pragma unroll
+                for (int i = 4; i < 32; i *= 2) top[c] = max_nan(top[c], __shfl_xor_sync(0xffffffffu, top[c], i));
+                const float next = max_nan(m[nt][c], top[c]);
+                const float base = next == neg_inf() ? 0.0f : next - kWeightBits;
+                alpha[nt][c] = m[nt][c] == neg_inf() ? 0.0f : ex2(m[nt][c] - next);
+                moved |= next != m[nt][c];
+                m[nt][c] = next;
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int h = 0; h < 4; h += 2) {
+                        const float w = ex2(sc[nt][i][h + c] - base);
+                        sc[nt][i][h + c] = w;
+                        sum += w;
+                    }
+                l[nt][c] = l[nt][c] * alpha[nt][c] + sum;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                pt[nt][i][0] = transpose8x8(f16x2(sc[nt][i][0], sc[nt][i][1]));
+                pt[nt][i][1] = transpose8x8(f16x2(sc[nt][i][2], sc[nt][i][3]));
+            }
+        }
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                for (int i = 0; i < D / 16; i++)
+#pragma unroll
+                    for (int c = 0; c < 4; c++) o[nt][i][c] *= alpha[nt][c & 1];
+        }
+        // scale bytes behind the last token may be anything, NaN among it, and 0 NaN is no 0
+        if (k0 + 16 * t + 16 > end) {
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int c = 0; c < 4; c++)
+                    if (k0 + 16 * t + 4 * j + c >= end) vs[j] &= ~(0xFFu << (8 * c));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint32_t s01 = e4m3x2_to_f16(vs[i] & 0xFFFF), s23 = e4m3x2_to_f16(vs[i] >> 16);
+#pragma unroll
+            for (int w = 0; w < T::VW; w++) {
+                constexpr uint32_t kLow = 0x0F0F0F0Fu;
+                const uint32_t a = vc[4 * i][w], b2 = vc[4 * i + 1][w], c = vc[4 * i + 2][w], d = vc[4 * i + 3][w];
+                uint32_t lo01[4], hi01[4], lo23[4], hi23[4];
+                e2m1x8_to_f16((a & kLow) | ((b2 << 4) & ~kLow), lo01);
+                e2m1x8_to_f16(((a >> 4) & kLow) | (b2 & ~kLow), hi01);
+                e2m1x8_to_f16((c & kLow) | ((d << 4) & ~kLow), lo23);
+                e2m1x8_to_f16(((c >> 4) & kLow) | (d & ~kLow), hi23);
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    const uint32_t v[4] = {mul_h2(lo01[r], s01), mul_h2(hi01[r], s01), mul_h2(lo23[r], s23), mul_h2(hi23[r], s23)};
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++) mma16(o[nt][4 * w + r], v, pt[nt][i][0], pt[nt][i][1]);
+                }
+            }
+        }
+    }
+    if (p.status && __any_sync(0xffffffffu, outside) && lane == 0) atomicOr(p.status, kStatusBounds);
+
+    // join the four warps
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int c = 0; c < 2; c++) {
+#pragma unroll
+            for (int i = 4; i < 32; i *= 2) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], i);
+            if (g == 0) {
+                s_m[warp][8 * nt + 2 * t + c] = m[nt][c];
+                s_l[warp][8 * nt + 2 * t + c] = l[nt][c];
+            }
+        }
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int c = 0; c < 2; c++) {
+            const int r = 8 * nt + 2 * t + c;
+            const float top = max_nan(max_nan(s_m[0][r], s_m[1][r]), max_nan(s_m[2][r], s_m[3][r]));
+            const float w = m[nt][c] == neg_inf() ? 0.0f : ex2(m[nt][c] - top);
+            // the lane's dims of this row: g D/8 + 0, 1, ..
+#pragma unroll
+            for (int i = 0; i < D / 16; i++)
+#pragma unroll
+                for (int h = 0; h < 2; h++) s_o[warp][r][g * (D / 8) + 2 * i + h] = o[nt][i][2 * h + c] * w;
+        }
+    __syncthreads();
+    const float Sv = ld_f32(p.c.S_v);
+    for (int x = threadIdx.x; x < T::R * D; x += kThreads) {
+        const int r = x / D, d = x % D;
+        const int64_t row = first + r;
+        if (row >= rows) break;
+        float top = neg_inf(), sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; w++) top = max_nan(top, s_m[w][r]);
+#pragma unroll
+        for (int w = 0; w < 4; w++) sum += s_m[w][r] == neg_inf() ? 0.0f : s_l[w][r] * ex2(s_m[w][r] - top);
+        const float v = (s_o[0][r][d] + s_o[1][r][d]) + (s_o[2][r][d] + s_o[3][r][d]);
+        const int64_t token = row0 + row / p.group, h = head * (int64_t)p.group + row % p.group;
+        if (PART) {
+            const int64_t at = ((part0 + part) * p.tokens + token) * p.q_heads + h;
+            static_cast<float*>(p.workspace)[at * D + d] = v;
+            if (d == 0)
+                reinterpret_cast<float2*>(static_cast<char*>(p.workspace) + p.plan.values)[at] = make_float2(top, sum);
+        } else {
+            const float out = top == neg_inf() ? 0.0f : v * (Sv / sum);
+            uint32_t bits;
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(bits) : "f"(0.0f), "f"(out));
+            static_cast<uint16_t*>(p.out.p)[token * p.out.token + h * p.out.head + d] = (uint16_t)bits;
+            if (p.lse && d == 0)
+                p.lse[token * p.q_heads + h] =
+                    top == neg_inf() ? neg_inf() : (top + log2f(sum) - kWeightBits) * 0.6931471805599453f;
+        }
+    }
+}
+
+// A row's parts joined: a warp for each row.
+template <int D>
+__global__ void __launch_bounds__(256) join_kernel(Attention p) {
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int64_t token = at / p.q_heads, h = at - token * p.q_heads;
+    if (token >= p.tokens) return;
+    int64_t lo = 0, hi = p.batch + 1;
+    while (hi > lo) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (p.offsets[mid] > token) hi = mid;
+        else lo = mid + 1;
+    }
+    const int64_t b = lo - 1;
+    if (b < 0 || b >= p.batch) return;
+    const int64_t n = p.offsets[b + 1] - p.offsets[b], i = token - p.offsets[b];
+    if (i >= p.max_q || n < 0 || p.offsets[b] < 0 || p.offsets[b] + n > p.tokens) return;
+    int64_t len = p.lens[b], most = p.width << p.c.page_log2;
+    len = len < 0 ? 0 : len > most ? most : len;
+    const int64_t sees = p.causal ? len - n + i + 1 : len;
+    const int64_t own = sees <= 0 ? 0 : (sees + p.plan.own.chunk - 1) / p.plan.own.chunk;
+    int64_t shared = 0;
+    if (p.prefix_len) {
+        int64_t len2 = *p.prefix_len;
+        most = p.prefix_width << p.c.page_log2;
+        len2 = len2 < 0 ? 0 : len2 > most ? most : len2;
+        shared = p.plan.prefix.parts ? (len2 + p.plan.prefix.chunk - 1) / p.plan.prefix.chunk : 0;
+    }
+    // parts 0 .. own - 1 and those of the prefix, behind the most that a sequence has
+    const float2* ml = reinterpret_cast<const float2*>(static_cast<const char*>(p.workspace) + p.plan.values);
+    const float* vals = static_cast<const float*>(p.workspace);
+    const int64_t stride = p.tokens * p.q_heads, parts = own + shared;
+    float top = neg_inf();
+    for (int64_t k = lane; k < parts; k += 32) {
+        const float2 v = ml[(k < own ? k : p.plan.own.parts + k - own) * stride + at];
+        top = max_nan(top, v.x);
+    }
+#pragma unroll
+    for (int k = 16; k; k /= 2) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, k));
+    constexpr int N = D / 32;
+    float sum = 0.0f, o[N];
+#pragma unroll
+    for (int k = 0; k < N; k++) o[k] = 0.0f;
+#pragma unroll 4
+    for (int64_t k = 0; k < parts; k++) {
+        const int64_t x = (k < own ? k : p.plan.own.parts + k - own) * stride + at;
+        const float2 v = ml[x];
+        const float w = v.x == neg_inf() ? 0.0f : ex2(v.x - top);
+        sum += v.y * w;
+        float q[N];
+        if constexpr (N == 4) {
+            const float4 f = *reinterpret_cast<const float4*>(vals + x * D + lane * 4);
+            q[0] = f.x, q[1] = f.y, q[2] = f.z, q[3] = f.w;
+        } else {
+            const float2 f = *reinterpret_cast<const float2*>(vals + x * D + lane * 2);
+            q[0] = f.x, q[1] = f.y;
+        }
+#pragma unroll
+        for (int c = 0; c < N; c++) o[c] += q[c] * w;
+    }
+    const float f = top == neg_inf() ? 0.0f : ld_f32(p.c.S_v) / sum;
+    uint16_t* out = static_cast<uint16_t*>(p.out.p) + token * p.out.token + h * p.out.head + lane * N;
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int c = 0; c < N / 2; c++) {
+        const float a = top == neg_inf() ? 0.0f : o[2 * c] * f, b2 = top == neg_inf() ? 0.0f : o[2 * c + 1] * f;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[c]) : "f"(b2), "f"(a));
+    }
+    if (p.out.vec) {
+        if constexpr (N == 4) *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t*>(out) = w[0];
+    } else {
+#pragma unroll
+        for (int c = 0; c < N; c++) out[c] = (uint16_t)(w[c / 2] >> (16 * (c & 1)));
+    }
+    if (p.lse && lane == 0)
+        p.lse[at] = top == neg_inf() ? neg_inf() : (top + log2f(sum) - kWeightBits) * 0.6931471805599453f;
+}
+
+cudaError_t launch_2d(void (*kernel)(Attention, Pass, int64_t), int64_t x, int y, cudaStream_t s, const Attention& p,
+                      const Pass& pass, int64_t part0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)x, (unsigned)y);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p, pass, part0);
+}
+
+template <int D, bool PREFIX>
+cudaError_t launch_rows(const Attention& p, const Pass& pass, int64_t part0, cudaStream_t s) {
+    const int64_t x = (PREFIX ? 1 : p.batch) * pass.parts * pass.tiles;
+    const bool part = p.plan.parts() > 1;
+    if (pass.rows == 8)
+        return launch_2d(part ? rows_kernel<D, 1, PREFIX, true> : rows_kernel<D, 1, PREFIX, false>, x, p.c.heads, s, p, pass, part0);
+    return launch_2d(part ? rows_kernel<D, 2, PREFIX, true> : rows_kernel<D, 2, PREFIX, false>, x, p.c.heads, s, p, pass, part0);
+}
+
+template <int D>
+cudaError_t launch(const Attention& p, cudaStream_t s) {
+    cudaError_t e = launch_rows<D, false>(p, p.plan.own, 0, s);
+    if (e == cudaSuccess && p.plan.prefix.parts) e = launch_rows<D, true>(p, p.plan.prefix, p.plan.own.parts, s);
+    if (e == cudaSuccess && p.plan.parts() > 1)
+        e = launch_dependent(join_kernel<D>, (p.tokens * p.q_heads + 7) / 8, 256, s, p);
+    return e;
+}
+
+}  // namespace
+
+cudaError_t launch_attention(const Attention& p, cudaStream_t s) {
+    return p.c.dim == 64 ? launch<64>(p, s) : launch<128>(p, s);
+}
+
+}  // namespace kv
+}  // namespace nvfp4

@@ -1,0 +1,78 @@
+// Internal interface between the host layer of nvfp4kv.h (kv_api.cu) and its kernels.
+// Not part of the public ABI.
+#pragma once
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "kv_plan.h"
+
+namespace nvfp4 {
+namespace kv {
+
+constexpr int kStatusNonFinite = 1;      // a token's x / S is not finite
+constexpr int kStatusBounds = 4;         // a length, slot or page number outside its bounds
+
+struct Cache {
+    uint8_t *codes, *sf;                 // [pages][heads][2][page][dim/2], [pages][heads][2][dim/16][page]
+    const float *S_k, *S_v;
+    int64_t pages;
+    int page_log2, heads, dim;
+};
+
+// Strided tensor [tokens, heads, dim]; vec: base and strides are multiples of 16 bytes.
+struct Tensor {
+    void* p;
+    int64_t token, head;
+    int vec;
+};
+
+struct Rope {
+    Tensor x, out;
+    int dtype, heads, dim, rot, halves, inverse;
+    int64_t tokens;
+    const int64_t* positions;
+    const uint64_t* turns;
+    float magnitude;
+};
+
+struct Write {
+    Cache c;
+    Tensor in[2];                        // k, v; null pointers are not written
+    int dtype, method;                   // method: 0 sweep, 1 block maximum
+    int64_t tokens;
+    const int64_t* slots;
+    int* status;
+};
+
+struct Read {
+    Cache c;
+    Tensor out[2];
+    int dtype;
+    const int32_t *table, *starts, *offsets;
+    int64_t table_ld, width, batch, tokens;
+    int* status;
+};
+
+struct Attention {
+    Cache c;
+    Tensor q, out;
+    int q_heads, group, causal;
+    int64_t tokens, batch, max_q;
+    const int32_t *table, *lens, *offsets;
+    int64_t table_ld, width;
+    const int32_t *prefix, *prefix_len;  // null without a prefix
+    int64_t prefix_width;
+    float scale;
+    float* lse;
+    int* status;
+    void* workspace;
+    Plan plan;
+};
+
+cudaError_t launch_rope(const Rope& p, int sms, cudaStream_t s);
+cudaError_t launch_write(const Write& p, int sms, cudaStream_t s);
+cudaError_t launch_read(const Read& p, int sms, cudaStream_t s);
+cudaError_t launch_attention(const Attention& p, cudaStream_t s);
+
+}  // namespace kv
+}  // namespace nvfp4
