@@ -19,7 +19,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libnvfp4ss.so")
 SOURCES = ["api.cu", "quantize.cu", "quantize_dynamic.cu", "scale_dequant.cu", "global_scale_noalloc.cu",
            "optimal_scale.cu", "ldlq.cu", "quantize_group.cu", "mxfp4.cu", "fp4_gemm.cu", "fp4_pair.cu", "fp4_api.cu",
-           "kv_api.cu", "rope.cu", "kv_cache.cu", "kv_attention.cu"]
+           "kv_api.cu", "rope.cu", "kv_cache.cu", "kv_attention.cu",
+           "kv_attention_tile.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -539,6 +539,7 @@ cudaError_t launch_2d(void (*kernel)(Attention, Pass, int64_t), int64_t x, int y
 
 template <int D, bool PREFIX>
 cudaError_t launch_rows(const Attention& p, const Pass& pass, int64_t part0, cudaStream_t s) {
+    if (pass.rows > 16) return launch_tiles(p, pass, PREFIX, part0, s);
     const int64_t x = (PREFIX ? 1 : p.batch) * pass.parts * pass.tiles;
     const bool part = p.plan.parts() > 1;
     if (pass.rows == 8)

@@ -1,0 +1,560 @@
+// Attention over the NVFP4 key/value cache for many rows a key head: prompts, and batches that
+// share a prefix (nvfp4_kv_attention, nvfp4_kv_attention_prefix), on tcgen05.
+//
+// A block takes 256 rows (query, head of the group) of one key head, as two tiles of 128, and
+// walks the keys of its part 128 at a time.  Codes become fp16 once for all 256 rows: q s (without S)
+// is exact in fp16, as are queries scaled by a power of two a row (kv_attention.cu), so both
+// products are kind::f16 MMAs with fp32 sums.
+//
+//   warps 8-11  a thread a token: its codes and scales from global memory (the next tile's are
+//               in flight while this one's wait for room), converted, into 128-byte-swizzled shared
+//               memory: keys read by the MMA along their rows, values across theirs
+//   warp 12     issues S = Q K^T of both tiles, then, as soon as a tile's weights are there, its
+//               O += P V and its next S: while one tile's softmax runs, the tensor cores do the other's
+//               products
+//   warps 0-7   softmax, a thread a row: maximum, weights to fp16 over the scores' own columns of
+//               tensor memory (P is the MMA's operand from there), the sum; O stays in tensor memory.
+//               O is scaled only when a row's maximum has grown by more than 2^8 (weights are held
+//               2^7-fold, so that they stay below fp16's largest).
+//
+// Tensor memory: scores of both tiles 2 x 128 columns, O 2 x dim.  Shared memory: Q 64 KB, two stages each
+// of keys and values of 32 KB (dim 128).
+//
+// Every mbarrier wait is bounded (1 s): a role that gives up stops, the others do after it,
+// bit 4 (16) of the status word is set and what is missing is not written.
+#include "fp4_tile.cuh"
+#include "kv_kernels.h"
+
+namespace nvfp4 {
+namespace kv {
+namespace {
+
+using namespace mm;
+
+constexpr int kSoftmaxWarps = 8, kLoadWarps = 4;
+constexpr int kTileThreads = 32 * (kSoftmaxWarps + kLoadWarps + 1);
+constexpr int kKeys = 128, kRows = 128;
+constexpr float kBits = 7.0f, kGrowth = 8.0f, kJoinBits = 15.0f;
+
+__device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t scale_pair(uint32_t code) {     // E4M3 code -> its fp16 value twice
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(code | code << 8)));
+    return h;
+}
+__device__ __forceinline__ uint4 e2m1x8_scaled(uint32_t w, uint32_t s) {
+    uint4 h;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h.x), "=r"(h.y), "=r"(h.z), "=r"(h.w) : "r"(w));
+    return make_uint4(mul_h2(h.x, s), mul_h2(h.y, s), mul_h2(h.z, s), mul_h2(h.w, s));
+}
+__device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// 32 columns of this thread's lane of tensor memory; the values are there after wait_ld32.
+__device__ __forceinline__ void tmem_ld32(uint32_t a, float (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, "
+        "%24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+          "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]),
+          "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]),
+          "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+        : "r"(a)
+        : "memory");
+}
+__device__ __forceinline__ void wait_ld32(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]),
+                   "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]),
+                   "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), "+f"(v[24]),
+                   "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+                 :: "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(a),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+}
+
+// kind::f16 with fp16 operands: D fp32 (bits 4-5 = 1), A and B fp16 (0), B's K along its rows or (bit 16) across them.
+__host__ __device__ constexpr uint32_t idesc_f16(int n, bool across) {
+    return (1u << 4) | (across ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+}
+
+template <int D>
+struct Shape {
+    static constexpr int kPanels = D / 64;                       // of 64 elements (128 bytes) a row
+    static constexpr int kPanel = 128 * 128;                     // 128 rows
+    static constexpr int kOp = kPanels * kPanel;                 // an operand: 128 rows of D fp16
+    static constexpr int kSmem = 6 * kOp + 1024;                 // Q twice, two stages of K and V
+    static constexpr int kScores = 0, kOut = 256;                // columns of tensor memory
+};
+
+struct Bars {
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full;
+};
+
+// A token's codes and scales of K or V on their way.
+template <int D>
+struct Held {
+    uint4 w[D / 32];
+    uint32_t s[D / 64];                                          // four scale codes each
+    __device__ __forceinline__ void load(const Cache& c, int64_t page, int at, int head, int part) {
+        if (page < 0) {
+#pragma unroll
+            for (int i = 0; i < D / 32; i++) w[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < D / 64; i++) s[i] = 0;
+            return;
+        }
+        const int64_t row = (page * c.heads + head) * 2 + part;
+        const uint8_t* p = c.codes + ((row << c.page_log2) + at) * (D / 2);
+#pragma unroll
+        for (int i = 0; i < D / 32; i++) w[i] = *reinterpret_cast<const uint4*>(p + 16 * i);
+        const uint8_t* q = c.sf + ((row * (D / 16)) << c.page_log2) + at;
+#pragma unroll
+        for (int i = 0; i < D / 64; i++) {
+            s[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; j++) s[i] |= (uint32_t)q[(int64_t)(4 * i + j) << c.page_log2] << (8 * j);
+        }
+    }
+    // into row `row` of an operand
+    __device__ __forceinline__ void store(uint32_t op, int row) const {
+#pragma unroll
+        for (int b = 0; b < D / 16; b++) {
+            const uint32_t sc = scale_pair((s[b / 4] >> (8 * (b & 3))) & 0xFF);
+            const uint4& v = w[b / 2];
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int chunk = 2 * b + h;                     // of 8 elements
+                const uint32_t code = b & 1 ? (h ? v.w : v.z) : (h ? v.y : v.x);
+                st_shared16(op + (chunk >> 3) * Shape<D>::kPanel + row * 128 + (((chunk & 7) ^ (row & 7)) << 4),
+                            e2m1x8_scaled(code, sc));
+            }
+        }
+    }
+};
+
+template <int D, bool PREFIX, bool PART>
+__global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass pass, int64_t part0) {
+    using H = Shape<D>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Bars s_bars;
+    __shared__ uint32_t s_tmem, s_hidden[4][4];
+    __shared__ int s_abort;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int head = blockIdx.y;
+    // tiles from the last one on: with a causal mask it has the most keys
+    const int64_t per = PREFIX ? pass.parts : pass.parts * p.batch;
+    const int64_t tile = pass.tiles - 1 - blockIdx.x / per, rest = blockIdx.x % per;
+    const int64_t part = PREFIX ? rest : rest % pass.parts, b = PREFIX ? 0 : rest / pass.parts;
+
+    int64_t row0 = 0, n, len, width;
+    const int32_t* table;
+    bool outside = false;
+    if (PREFIX) {
+        n = p.tokens;
+        len = *p.prefix_len;
+        table = p.prefix;
+        width = p.prefix_width;
+    } else {
+        row0 = p.offsets[b];
+        n = p.offsets[b + 1] - row0;
+        len = p.lens[b];
+        table = p.table + b * p.table_ld;
+        width = p.width;
+        if (row0 < 0 || n < 0 || row0 + n > p.tokens) {
+            outside = true;
+            n = 0;
+        }
+    }
+    if (len < 0 || len > (width << p.c.page_log2)) {
+        outside = true;
+        len = len < 0 ? 0 : width << p.c.page_log2;
+    }
+    if (p.status && outside && tid == 0 && head == 0) atomicOr(p.status, kStatusBounds);
+    const bool causal = !PREFIX && p.causal;
+    const int64_t rows = (PREFIX || n < p.max_q ? n : p.max_q) * p.group, first = tile * 2 * kRows;
+    if (first >= rows) return;
+    const int64_t last = (first + 2 * kRows < rows ? first + 2 * kRows : rows) - 1;
+    const int64_t sees = causal ? len - n + last / p.group + 1 : len;
+    const int64_t begin = part * pass.chunk;
+    const int64_t end = begin + pass.chunk < sees ? begin + pass.chunk : sees;
+    if (PART && begin >= end) return;
+    const int tiles = end > begin ? (int)((end - begin + kKeys - 1) / kKeys) : 0;      // a part is less than 2^31 tokens
+    const int both = rows - first > kRows;                       // the second tile has rows
+
+    const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;
+    const uint32_t sq = base, sk = base + 2 * H::kOp, sv = base + 4 * H::kOp;
+    if (warp == kSoftmaxWarps + kLoadWarps) tmem_alloc(smem_u32(&s_tmem), 512);
+    if (tid == 0) {
+        for (int i = 0; i < 2; i++) {
+            mbar_init(smem_u32(&s_bars.k_full[i]), kLoadWarps);
+            mbar_init(smem_u32(&s_bars.v_full[i]), kLoadWarps);
+            mbar_init(smem_u32(&s_bars.k_empty[i]), 1);
+            mbar_init(smem_u32(&s_bars.v_empty[i]), 1);
+            mbar_init(smem_u32(&s_bars.s_full[i]), 1);
+            mbar_init(smem_u32(&s_bars.p_full[i]), 4);
+        }
+        mbar_init(smem_u32(&s_bars.o_full), 1);
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+
+    // queries to fp16, scaled by a power of two a row
+    float fac = 0.0f;
+    int lim = 1 << 30;                                           // keys that the row sees of this part
+    const int half = warp >> 2;                                  // tile of this warp's rows (softmax warps)
+    const int64_t row = first + tid;
+    if (warp < kSoftmaxWarps) {
+        uint32_t w[D / 2];
+#pragma unroll
+        for (int i = 0; i < D / 2; i++) w[i] = 0;
+        if (row < rows) {
+            const uint16_t* q = static_cast<const uint16_t*>(p.q.p) + (row0 + row / p.group) * p.q.token +
+                                (head * (int64_t)p.group + row % p.group) * p.q.head;
+            if (p.q.vec) {
+#pragma unroll
+                for (int i = 0; i < D / 8; i++) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(q + 8 * i);
+                    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 2; i++) w[i] = q[2 * i] | (uint32_t)q[2 * i + 1] << 16;
+            }
+            const int64_t all = causal ? len - n + row / p.group + 1 : len;
+            const int64_t seen = (all < end ? all : end) - begin;
+            lim = seen < 0 ? 0 : (int)seen;
+        }
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < D / 2; i++) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+        int e = (int)(top >> 7) - 127;
+        if (e == 128) e = 0;                                     // infinities and NaN stay what they are
+        e = e < -126 ? -126 : e > 126 ? 126 : e;
+        const float down = __int_as_float((127 - e) << 23), up = __int_as_float((127 + e) << 23);
+        fac = ld_f32(p.c.S_k) * p.scale * 1.4426950408889634f * up;
+#pragma unroll
+        for (int i = 0; i < D / 8; i++) {
+            uint32_t h[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) h[j] = f16x2(bf16lo(w[4 * i + j]) * down, bf16hi(w[4 * i + j]) * down);
+            const int r = tid & 127;
+            st_shared16(sq + half * H::kOp + (i >> 3) * H::kPanel + r * 128 + (((i & 7) ^ (r & 7)) << 4),
+                        make_uint4(h[0], h[1], h[2], h[3]));
+        }
+        fence_proxy_async();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+
+    bool ok = true;
+    if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kLoadWarps) {
+        const int t = tid - 32 * kSoftmaxWarps;                  // token of the tile
+        Held<D> hk, hv;
+        int64_t page;
+        int at;
+        auto find = [&](int j) {
+            const int64_t x = begin + (int64_t)j * kKeys + t;
+            page = -1;
+            if (j < tiles && x < end) {
+                page = table[x >> p.c.page_log2];
+                if (page < 0 || page >= p.c.pages) {
+                    page = -1;
+                    outside = true;
+                }
+            }
+            at = (int)(x & ((1 << p.c.page_log2) - 1));
+            return x < end && page < 0;
+        };
+        bool hidden = find(0);
+        hk.load(p.c, page, at, head, 0);
+        hv.load(p.c, page, at, head, 1);
+        for (int j = 0; j < tiles; j++) {
+            const int st = j & 1;
+            const uint32_t parity = ((j >> 1) & 1) ^ 1;
+            if (j >= 2 && !mbar_wait_warp(smem_u32(&s_bars.k_empty[st]), parity)) { ok = false; break; }
+            const uint32_t mask = __ballot_sync(0xffffffffu, hidden);
+            if (lane == 0) s_hidden[j & 3][warp - kSoftmaxWarps] = mask;
+            hk.store(sk + st * H::kOp, t);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s_bars.k_full[st]));
+            hidden = find(j + 1);
+            hk.load(p.c, page, at, head, 0);
+            if (j >= 2 && !mbar_wait_warp(smem_u32(&s_bars.v_empty[st]), parity)) { ok = false; break; }
+            hv.store(sv + st * H::kOp, t);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s_bars.v_full[st]));
+            hv.load(p.c, page, at, head, 1);
+        }
+        if (p.status && __any_sync(0xffffffffu, outside) && lane == 0) atomicOr(p.status, kStatusBounds);
+    } else if (warp == kSoftmaxWarps + kLoadWarps && lane == 0) {
+        constexpr uint32_t id_s = idesc_f16(kKeys, false), id_o = idesc_f16(D, true);
+        auto scores = [&](int x, int st) {
+#pragma unroll
+            for (int kk = 0; kk < D / 16; kk++) {
+                const uint32_t at = (kk >> 2) * H::kPanel + (kk & 3) * 32;
+                mma_ss(tmem + H::kScores + x * 128, smem_desc(sq + x * H::kOp + at, 16, 1024),
+                       smem_desc(sk + st * H::kOp + at, 16, 1024), id_s, kk != 0);
+            }
+            mma_commit(smem_u32(&s_bars.s_full[x]));
+        };
+        if (tiles > 0) {
+            if (!mbar_wait(smem_u32(&s_bars.k_full[0]), 0)) ok = false;
+            tc_fence_after();
+            if (ok) {
+                scores(0, 0);
+                if (both) scores(1, 0);
+                mma_commit(smem_u32(&s_bars.k_empty[0]));
+            }
+        }
+        for (int j = 0; ok && j < tiles; j++) {
+            const int st = j & 1, nx = (j + 1) & 1;
+            if (!mbar_wait(smem_u32(&s_bars.v_full[st]), (j >> 1) & 1)) { ok = false; break; }
+            for (int x = 0; x <= both; x++) {
+                if (!mbar_wait(smem_u32(&s_bars.p_full[x]), j & 1)) { ok = false; break; }
+                tc_fence_after();
+#pragma unroll
+                for (int kk = 0; kk < kKeys / 16; kk++)
+                    mma_ts(tmem + H::kOut + x * D, tmem + H::kScores + x * 128 + kk * 8,
+                           smem_desc(sv + st * H::kOp + kk * 16 * 128, H::kPanel, 1024), id_o, (uint32_t)(j | kk));
+                if (j + 1 < tiles) {
+                    if (x == 0 && !mbar_wait(smem_u32(&s_bars.k_full[nx]), ((j + 1) >> 1) & 1)) { ok = false; break; }
+                    tc_fence_after();
+                    scores(x, nx);
+                }
+            }
+            if (!ok) break;
+            mma_commit(smem_u32(&s_bars.v_empty[st]));
+            if (j + 1 < tiles) mma_commit(smem_u32(&s_bars.k_empty[nx]));
+        }
+        mma_commit(smem_u32(&s_bars.o_full));                    // after every MMA issued, also on a timeout
+        if (!mbar_wait(smem_u32(&s_bars.o_full), 0)) ok = false;
+    } else if (warp < kSoftmaxWarps && (half == 0 || both)) {
+        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);      // this warp's lanes
+        const uint32_t ts = lanes + H::kScores + half * 128, to = lanes + H::kOut + half * D;
+        float m = neg_inf(), l = 0.0f;
+        for (int j = 0; j < tiles; j++) {
+            if (!mbar_wait_warp(smem_u32(&s_bars.s_full[half]), j & 1)) { ok = false; break; }
+            tc_fence_after();
+            const int left = lim - j * kKeys;                    // visible keys from this tile on
+            uint32_t hid[4];
+#pragma unroll
+            for (int c = 0; c < 4; c++) hid[c] = s_hidden[j & 3][c];
+            const bool whole = __all_sync(0xffffffffu, left >= kKeys && !(hid[0] | hid[1] | hid[2] | hid[3]));
+            float v[2][32];
+            float top = neg_inf();
+            tmem_ld32(ts, v[0]);
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                float(&x)[32] = v[c & 1];
+                wait_ld32(x);
+                if (c < 3) tmem_ld32(ts + 32 * (c + 1), v[(c + 1) & 1]);
+                if (!whole) {
+#pragma unroll
+                    for (int i = 0; i < 32; i++)
+                        if (32 * c + i >= left || (hid[c] >> i & 1)) x[i] = neg_inf();
+                }
+                float t2 = neg_inf();
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    top = max3_nan(top, x[i], x[i + 1]);
+                    t2 = max3_nan(t2, x[i + 2], x[i + 3]);
+                }
+                top = max3_nan(top, t2, t2);
+            }
+            tmem_ld32(ts, v[0]);
+            // -inf 0 is NaN: a row that sees nothing of the tile has no maximum to scale
+            top = top == neg_inf() ? top : top * fac;
+            const bool grown = top > m + kGrowth;
+            if (__any_sync(0xffffffffu, grown)) {
+                const float alpha = !grown ? 1.0f : m == neg_inf() ? 0.0f : ex2(m - top);
+                if (grown) m = top;
+                l *= alpha;
+                if (j > 0) {
+#pragma unroll
+                    for (int c = 0; c < D; c += 16) {
+                        float o[16], z[16];
+                        tmem_ld16(to + c, o);
+                        tmem_wait_ld(o, z);
+                        uint32_t u[16];
+#pragma unroll
+                        for (int i = 0; i < 16; i++) u[i] = __float_as_uint(o[i] * alpha);
+                        tmem_st16(to + c, u);
+                    }
+                }
+            }
+            const float shift = m == neg_inf() ? 0.0f : kBits - m;
+            const u64 f2 = pack2(fac, fac), s2 = pack2(shift, shift);
+            u64 sum0 = 0ull, sum1 = 0ull;
+            const u64 one2 = pack2(1.0f, 1.0f);
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                float(&x)[32] = v[c & 1];
+                wait_ld32(x);
+                if (c < 3) tmem_ld32(ts + 32 * (c + 1), v[(c + 1) & 1]);
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    float a, bb;
+                    unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), f2, s2), a, bb);
+                    a = ex2(a);
+                    bb = ex2(bb);
+                    if (!whole) {
+                        if (32 * c + 2 * i >= left || (hid[c] >> (2 * i) & 1)) a = 0.0f;
+                        if (32 * c + 2 * i + 1 >= left || (hid[c] >> (2 * i + 1) & 1)) bb = 0.0f;
+                    }
+                    if (i & 1) sum1 = fma2(pack2(a, bb), one2, sum1);
+                    else sum0 = fma2(pack2(a, bb), one2, sum0);
+                    w[i] = f16x2(a, bb);
+                }
+                tmem_st16(ts + 16 * c, w);
+            }
+            float a, bb, c2, d2;
+            unpack2(sum0, a, bb);
+            unpack2(sum1, c2, d2);
+            l += (a + bb) + (c2 + d2);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s_bars.p_full[half]));
+        }
+        if (ok && !mbar_wait_warp(smem_u32(&s_bars.o_full), 0)) ok = false;
+        tc_fence_after();
+        if (ok) {
+            const int64_t token = row0 + row / p.group, h = head * (int64_t)p.group + row % p.group;
+            const int64_t at = PART ? ((part0 + part) * p.tokens + token) * p.q_heads + h : token * p.q_heads + h;
+            const float f = PART ? 1.0f : ld_f32(p.c.S_v) / l;
+            const bool empty = l == 0.0f;                        // saw nothing
+            const bool valid = row < rows;
+#pragma unroll
+            for (int c = 0; c < D; c += 16) {
+                float o[16], z[16];
+                if (tiles > 0) {
+                    tmem_ld16(to + c, o);
+                    tmem_wait_ld(o, z);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; i++) o[i] = empty ? 0.0f : o[i] * f;
+                if (!valid) continue;
+                if (PART) {
+                    float4* d = reinterpret_cast<float4*>(static_cast<float*>(p.workspace) + at * D + c);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) d[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                } else {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; i++)
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(o[2 * i + 1]), "f"(o[2 * i]));
+                    uint16_t* d = static_cast<uint16_t*>(p.out.p) + token * p.out.token + h * p.out.head + c;
+                    if (p.out.vec) {
+                        reinterpret_cast<uint4*>(d)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                        reinterpret_cast<uint4*>(d)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; i++) d[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+                    }
+                }
+            }
+            if (valid) {
+                // weights here are 2^kBits-fold of 2^m, those of the join 2^kJoinBits-fold; a NaN sum shows in both
+                if (PART)
+                    reinterpret_cast<float2*>(static_cast<char*>(p.workspace) + p.plan.values)[at] =
+                        make_float2(l != l ? l : empty ? neg_inf() : m + (kJoinBits - kBits), l);
+                else if (p.lse)
+                    p.lse[at] = empty ? neg_inf() : (m + log2f(l) - kBits) * 0.6931471805599453f;
+            }
+        }
+    }
+    if (!ok) atomicOr(&s_abort, 1);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kSoftmaxWarps + kLoadWarps) tmem_dealloc(tmem, 512);
+    if (tid == 0 && s_abort && p.status) atomicOr(p.status, kStatusTimeout);
+}
+
+template <int D, bool PREFIX, bool PART>
+cudaError_t launch(const Attention& p, const Pass& pass, int64_t part0, cudaStream_t s) {
+    static std::atomic<uint64_t> opted;                          // devices whose shared memory limit is raised
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (!(opted.load(std::memory_order_relaxed) & bit) || !bit) {
+        e = cudaFuncSetAttribute(tile_kernel<D, PREFIX, PART>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem);
+        if (e != cudaSuccess) return e;
+        opted.fetch_or(bit, std::memory_order_relaxed);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(pass.tiles * pass.parts * (PREFIX ? 1 : p.batch)), (unsigned)p.c.heads);
+    cfg.blockDim = dim3(kTileThreads);
+    cfg.dynamicSmemBytes = Shape<D>::kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, tile_kernel<D, PREFIX, PART>, p, pass, part0);
+}
+
+template <int D>
+cudaError_t dispatch(const Attention& p, const Pass& pass, bool prefix, int64_t part0, cudaStream_t s) {
+    if (prefix) return p.plan.parts() > 1 ? launch<D, true, true>(p, pass, part0, s) : launch<D, true, false>(p, pass, part0, s);
+    return p.plan.parts() > 1 ? launch<D, false, true>(p, pass, part0, s) : launch<D, false, false>(p, pass, part0, s);
+}
+
+}  // namespace
+
+cudaError_t launch_tiles(const Attention& p, const Pass& pass, bool prefix, int64_t part0, cudaStream_t s) {
+    return p.c.dim == 64 ? dispatch<64>(p, pass, prefix, part0, s) : dispatch<128>(p, pass, prefix, part0, s);
+}
+
+}  // namespace kv
+}  // namespace nvfp4

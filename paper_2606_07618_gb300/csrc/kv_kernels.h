@@ -73,6 +73,8 @@ cudaError_t launch_rope(const Rope& p, int sms, cudaStream_t s);
 cudaError_t launch_write(const Write& p, int sms, cudaStream_t s);
 cudaError_t launch_read(const Read& p, int sms, cudaStream_t s);
 cudaError_t launch_attention(const Attention& p, cudaStream_t s);
+// A pass of attention for many rows (kv_attention_tile.cu).
+cudaError_t launch_tiles(const Attention& p, const Pass& pass, bool prefix, int64_t part0, cudaStream_t s);
 
 }  // namespace kv
 }  // namespace nvfp4

@@ -10,6 +10,9 @@ namespace kv {
 constexpr int kWarpTokens = 64, kBlockTokens = 256;
 // Blocks that fill the GPU about twice: 152 SMs with four of them each.
 constexpr int64_t kBlocks = 152 * 4 * 2;
+// Rows of a block on tcgen05 (one block an SM), keys that it takes at a time.
+constexpr int kTileRows = 256, kTileKeys = 128;
+constexpr int64_t kTileBlocks = 152;
 
 struct Sizes {
     int64_t tokens, batch, max_q;        // rows of q, sequences, the most queries of one
@@ -37,12 +40,14 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 inline Pass plan_pass(int64_t sequences, int64_t heads, int64_t rows, int64_t length) {
     Pass p;
-    p.rows = rows <= 8 ? 8 : 16;
+    p.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kTileRows;
     p.tiles = ceil_div(rows, p.rows);
-    const int64_t most = length > kBlockTokens ? ceil_div(length, kBlockTokens) : 1;
-    int64_t parts = kBlocks / sequences / heads / p.tiles;
+    const bool tile = p.rows == kTileRows;
+    const int64_t step = tile ? kTileKeys : kBlockTokens;
+    const int64_t most = length > step ? ceil_div(length, step) : 1;
+    int64_t parts = (tile ? kTileBlocks : kBlocks) / sequences / heads / p.tiles;
     parts = parts < 1 ? 1 : parts > most ? most : parts;
-    p.chunk = ceil_div(length > 0 ? length : 1, parts * kBlockTokens) * kBlockTokens;
+    p.chunk = ceil_div(length > 0 ? length : 1, parts * step) * step;
     p.parts = length > 0 ? ceil_div(length, p.chunk) : 1;
     return p;
 }

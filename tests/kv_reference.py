@@ -58,11 +58,11 @@ def attention(q, k, v, scale, past):
 def check(got, want, lse=None):
     """got (bf16) and lse (fp32) of attention() against its results: a weight is off by 2^-11 (fp16), by its logit's error, which
     the sum of weights has too, and by a few roundings of fp32; the result by half a step of bf16.  fp16's last bit is
-    2^-24, and weights are held 2^15-fold: however small, each is off by up to 2^-25 2^-15 = 2^-40 of the largest, which is at
-    most the sum that divides (an element whose larger weights all meet zeros shows it)."""
+    2^-24, and weights are held so that the largest is at least 2^7: however small, each is off by up to 2^-25 2^-7 = 2^-32 of the
+    largest, which is at most the sum that divides (an element whose larger weights all meet zeros shows it)."""
     out, ref_lse, mag, off, total = want
     got = got.double().cpu().view(out.shape)
-    tol = 2.0 ** -8 * out.abs() + (2.0 ** -11 + 2 * off + 2.0 ** -18)[..., None] * mag * 1.01 + 2.0 ** -40 * total
+    tol = 2.0 ** -8 * out.abs() + (2.0 ** -11 + 2 * off + 2.0 ** -18)[..., None] * mag * 1.01 + 2.0 ** -32 * total
     bad = ~((got - out).abs() <= tol)
     assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, most {((got - out).abs() / tol.clamp(min=1e-300)).max():.3g} of the tolerance"
     if lse is not None:
