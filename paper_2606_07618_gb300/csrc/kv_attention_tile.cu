@@ -32,7 +32,10 @@ namespace {
 using namespace mm;
 
 constexpr int kSoftmaxWarps = 8, kLoadWarps = 4;
-constexpr int kTileThreads = 32 * (kSoftmaxWarps + kLoadWarps + 1);
+// Four warps each of an SM's quarter, three of the last four idle: a quarter of the register file then goes 2 x 192 + 80 + 48
+// (of 4 x 128 launched) to softmax, loads and MMAs.
+constexpr int kTileThreads = 32 * (kSoftmaxWarps + kLoadWarps + 4);
+constexpr int kSoftmaxRegs = 192, kLoadRegs = 80, kMmaRegs = 48;
 constexpr int kKeys = 128, kRows = 128;
 constexpr float kBits = 7.0f, kGrowth = 8.0f, kJoinBits = 15.0f;
 
@@ -94,6 +97,11 @@ __device__ __forceinline__ void wait_ld32(float (&v)[32]) {
                    "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
                  :: "memory");
 }
+// Values of a load that another wait covers: no use of them moves above this.
+__device__ __forceinline__ void hold32(float (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; i++) asm volatile("" : "+f"(v[i]));
+}
 __device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t (&v)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -103,6 +111,10 @@ __device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t (&v)[16]) {
         : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
@@ -274,6 +286,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
         e = e < -126 ? -126 : e > 126 ? 126 : e;
         const float down = __int_as_float((127 - e) << 23), up = __int_as_float((127 + e) << 23);
         fac = ld_f32(p.c.S_k) * p.scale * 1.4426950408889634f * up;
+        if (fac == 0.0f) fac = 1e-37f;                           // hidden scores, -inf, stay that
 #pragma unroll
         for (int i = 0; i < D / 8; i++) {
             uint32_t h[4];
@@ -292,89 +305,108 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
 
     bool ok = true;
     if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kLoadWarps) {
+        regs_down<kLoadRegs>();
         const int t = tid - 32 * kSoftmaxWarps;                  // token of the tile
-        Held<D> hk, hv;
-        int64_t page;
-        int at;
-        auto find = [&](int j) {
+        // items: keys of a tile, then its values; the next two items' bytes are on their way, and the page after them
+        Held<D> now, next;
+        auto page_of = [&](int j) -> int64_t {
             const int64_t x = begin + (int64_t)j * kKeys + t;
-            page = -1;
-            if (j < tiles && x < end) {
-                page = table[x >> p.c.page_log2];
-                if (page < 0 || page >= p.c.pages) {
-                    page = -1;
-                    outside = true;
-                }
-            }
-            at = (int)(x & ((1 << p.c.page_log2) - 1));
-            return x < end && page < 0;
+            if (j >= tiles || x >= end) return -1;
+            const int64_t page = table[x >> p.c.page_log2];
+            if (page >= 0 && page < p.c.pages) return page;
+            outside = true;
+            return -2;
         };
-        bool hidden = find(0);
-        hk.load(p.c, page, at, head, 0);
-        hv.load(p.c, page, at, head, 1);
-        for (int j = 0; j < tiles; j++) {
-            const int st = j & 1;
-            const uint32_t parity = ((j >> 1) & 1) ^ 1;
-            if (j >= 2 && !mbar_wait_warp(smem_u32(&s_bars.k_empty[st]), parity)) { ok = false; break; }
-            const uint32_t mask = __ballot_sync(0xffffffffu, hidden);
-            if (lane == 0) s_hidden[j & 3][warp - kSoftmaxWarps] = mask;
-            hk.store(sk + st * H::kOp, t);
+        const auto at = [&](int j) { return (int)((begin + (int64_t)j * kKeys + t) & ((1 << p.c.page_log2) - 1)); };
+        int64_t page = page_of(0), page1 = page_of(1);
+        bool hidden = page == -2;
+        now.load(p.c, page, at(0), head, 0);
+        next.load(p.c, page, at(0), head, 1);
+#pragma unroll 1
+        for (int i = 0; i < 2 * tiles; i++) {
+            const int j = i >> 1, part = i & 1, st = j & 1;
+            Bars& bars = s_bars;
+            uint64_t *empty = part ? &bars.v_empty[st] : &bars.k_empty[st], *full = part ? &bars.v_full[st] : &bars.k_full[st];
+            if (j >= 2 && !mbar_wait_warp(smem_u32(empty), ((j >> 1) & 1) ^ 1)) { ok = false; break; }
+            if (part == 0) {
+                const uint32_t mask = __ballot_sync(0xffffffffu, hidden);
+                if (lane == 0) s_hidden[j & 3][warp - kSoftmaxWarps] = mask;
+            }
+            now.store((part ? sv : sk) + st * H::kOp, t);
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&s_bars.k_full[st]));
-            hidden = find(j + 1);
-            hk.load(p.c, page, at, head, 0);
-            if (j >= 2 && !mbar_wait_warp(smem_u32(&s_bars.v_empty[st]), parity)) { ok = false; break; }
-            hv.store(sv + st * H::kOp, t);
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&s_bars.v_full[st]));
-            hv.load(p.c, page, at, head, 1);
+            if (lane == 0) mbar_arrive(smem_u32(full));
+            now = next;
+            if (part == 0) {
+                page = page1;
+                page1 = page_of(j + 2);
+                hidden = page == -2;
+            }
+            next.load(p.c, page, at(j + 1), head, part);
         }
         if (p.status && __any_sync(0xffffffffu, outside) && lane == 0) atomicOr(p.status, kStatusBounds);
-    } else if (warp == kSoftmaxWarps + kLoadWarps && lane == 0) {
+    } else if (warp >= kSoftmaxWarps + kLoadWarps) {
+        regs_down<kMmaRegs>();
+        if (warp == kSoftmaxWarps + kLoadWarps) {
+        // all lanes run the loop and one is elected to issue, so that descriptors stay in uniform registers
         constexpr uint32_t id_s = idesc_f16(kKeys, false), id_o = idesc_f16(D, true);
         auto scores = [&](int x, int st) {
+            if (elect_one()) {
+                const uint64_t a = smem_desc(sq + x * H::kOp, 16, 1024), bd = smem_desc(sk + st * H::kOp, 16, 1024);
 #pragma unroll
-            for (int kk = 0; kk < D / 16; kk++) {
-                const uint32_t at = (kk >> 2) * H::kPanel + (kk & 3) * 32;
-                mma_ss(tmem + H::kScores + x * 128, smem_desc(sq + x * H::kOp + at, 16, 1024),
-                       smem_desc(sk + st * H::kOp + at, 16, 1024), id_s, kk != 0);
+                for (int kk = 0; kk < D / 16; kk++) {
+                    const uint32_t at = ((kk >> 2) * H::kPanel + (kk & 3) * 32) >> 4;
+                    mma_ss(tmem + H::kScores + x * 128, a + at, bd + at, id_s, kk != 0);
+                }
+                mma_commit(smem_u32(&s_bars.s_full[x]));
             }
-            mma_commit(smem_u32(&s_bars.s_full[x]));
+            __syncwarp();
+        };
+        auto commit = [&](uint64_t* bar) {
+            if (elect_one()) mma_commit(smem_u32(bar));
+            __syncwarp();
         };
         if (tiles > 0) {
-            if (!mbar_wait(smem_u32(&s_bars.k_full[0]), 0)) ok = false;
+            ok = mbar_wait_warp(smem_u32(&s_bars.k_full[0]), 0);
             tc_fence_after();
             if (ok) {
                 scores(0, 0);
                 if (both) scores(1, 0);
-                mma_commit(smem_u32(&s_bars.k_empty[0]));
+                commit(&s_bars.k_empty[0]);
             }
         }
         for (int j = 0; ok && j < tiles; j++) {
             const int st = j & 1, nx = (j + 1) & 1;
-            if (!mbar_wait(smem_u32(&s_bars.v_full[st]), (j >> 1) & 1)) { ok = false; break; }
-            for (int x = 0; x <= both; x++) {
-                if (!mbar_wait(smem_u32(&s_bars.p_full[x]), j & 1)) { ok = false; break; }
+            ok = mbar_wait_warp(smem_u32(&s_bars.v_full[st]), (j >> 1) & 1);
+            for (int x = 0; ok && x <= both; x++) {
+                ok = mbar_wait_warp(smem_u32(&s_bars.p_full[x]), j & 1);
+                if (!ok) break;
                 tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t bd = smem_desc(sv + st * H::kOp, H::kPanel, 1024);
 #pragma unroll
-                for (int kk = 0; kk < kKeys / 16; kk++)
-                    mma_ts(tmem + H::kOut + x * D, tmem + H::kScores + x * 128 + kk * 8,
-                           smem_desc(sv + st * H::kOp + kk * 16 * 128, H::kPanel, 1024), id_o, (uint32_t)(j | kk));
+                    for (int kk = 0; kk < kKeys / 16; kk++)
+                        mma_ts(tmem + H::kOut + x * D, tmem + H::kScores + x * 128 + kk * 8, bd + (kk * 16 * 128 >> 4), id_o,
+                               (uint32_t)(j | kk));
+                }
+                __syncwarp();
                 if (j + 1 < tiles) {
-                    if (x == 0 && !mbar_wait(smem_u32(&s_bars.k_full[nx]), ((j + 1) >> 1) & 1)) { ok = false; break; }
+                    if (x == 0) ok = mbar_wait_warp(smem_u32(&s_bars.k_full[nx]), ((j + 1) >> 1) & 1);
+                    if (!ok) break;
                     tc_fence_after();
                     scores(x, nx);
                 }
             }
             if (!ok) break;
-            mma_commit(smem_u32(&s_bars.v_empty[st]));
-            if (j + 1 < tiles) mma_commit(smem_u32(&s_bars.k_empty[nx]));
+            commit(&s_bars.v_empty[st]);
+            if (j + 1 < tiles) commit(&s_bars.k_empty[nx]);
         }
-        mma_commit(smem_u32(&s_bars.o_full));                    // after every MMA issued, also on a timeout
-        if (!mbar_wait(smem_u32(&s_bars.o_full), 0)) ok = false;
-    } else if (warp < kSoftmaxWarps && (half == 0 || both)) {
+        commit(&s_bars.o_full);                                  // after every MMA issued, also on a timeout
+        if (!mbar_wait_warp(smem_u32(&s_bars.o_full), 0)) ok = false;
+        }
+    } else {
+        regs_up<kSoftmaxRegs>();
+        if (half == 0 || both) {
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);      // this warp's lanes
         const uint32_t ts = lanes + H::kScores + half * 128, to = lanes + H::kOut + half * D;
         float m = neg_inf(), l = 0.0f;
@@ -386,37 +418,36 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
 #pragma unroll
             for (int c = 0; c < 4; c++) hid[c] = s_hidden[j & 3][c];
             const bool whole = __all_sync(0xffffffffu, left >= kKeys && !(hid[0] | hid[1] | hid[2] | hid[3]));
-            float v[2][32];
-            float top = neg_inf();
-            tmem_ld32(ts, v[0]);
+            float v[4][32];
 #pragma unroll
-            for (int c = 0; c < 4; c++) {
-                float(&x)[32] = v[c & 1];
-                wait_ld32(x);
-                if (c < 3) tmem_ld32(ts + 32 * (c + 1), v[(c + 1) & 1]);
-                if (!whole) {
+            for (int c = 0; c < 4; c++) tmem_ld32(ts + 32 * c, v[c]);
+            wait_ld32(v[0]);
+#pragma unroll
+            for (int c = 1; c < 4; c++) hold32(v[c]);
+            if (!whole) {
+#pragma unroll
+                for (int c = 0; c < 4; c++)
 #pragma unroll
                     for (int i = 0; i < 32; i++)
-                        if (32 * c + i >= left || (hid[c] >> i & 1)) x[i] = neg_inf();
-                }
-                float t2 = neg_inf();
-#pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    top = max3_nan(top, x[i], x[i + 1]);
-                    t2 = max3_nan(t2, x[i + 2], x[i + 3]);
-                }
-                top = max3_nan(top, t2, t2);
+                        if (32 * c + i >= left || (hid[c] >> i & 1)) v[c][i] = neg_inf();
             }
-            tmem_ld32(ts, v[0]);
-            // -inf 0 is NaN: a row that sees nothing of the tile has no maximum to scale
-            top = top == neg_inf() ? top : top * fac;
+            float t4[4];
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                t4[c] = max3_nan(v[c][0], v[c][1], v[c][2]);
+#pragma unroll
+                for (int i = 3; i < 31; i += 2) t4[c] = max3_nan(t4[c], v[c][i], v[c][i + 1]);
+                t4[c] = max3_nan(t4[c], v[c][31], v[c][31]);
+            }
+            float top = max3_nan(max3_nan(t4[0], t4[1], t4[2]), t4[3], t4[3]);
+            top *= fac;
             const bool grown = top > m + kGrowth;
             if (__any_sync(0xffffffffu, grown)) {
                 const float alpha = !grown ? 1.0f : m == neg_inf() ? 0.0f : ex2(m - top);
                 if (grown) m = top;
                 l *= alpha;
                 if (j > 0) {
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < D; c += 16) {
                         float o[16], z[16];
                         tmem_ld16(to + c, o);
@@ -430,33 +461,25 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
             }
             const float shift = m == neg_inf() ? 0.0f : kBits - m;
             const u64 f2 = pack2(fac, fac), s2 = pack2(shift, shift);
-            u64 sum0 = 0ull, sum1 = 0ull;
             const u64 one2 = pack2(1.0f, 1.0f);
+            u64 sum[2] = {0ull, 0ull};
 #pragma unroll
             for (int c = 0; c < 4; c++) {
-                float(&x)[32] = v[c & 1];
-                wait_ld32(x);
-                if (c < 3) tmem_ld32(ts + 32 * (c + 1), v[(c + 1) & 1]);
                 uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
                     float a, bb;
-                    unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), f2, s2), a, bb);
+                    unpack2(fma2(pack2(v[c][2 * i], v[c][2 * i + 1]), f2, s2), a, bb);
                     a = ex2(a);
                     bb = ex2(bb);
-                    if (!whole) {
-                        if (32 * c + 2 * i >= left || (hid[c] >> (2 * i) & 1)) a = 0.0f;
-                        if (32 * c + 2 * i + 1 >= left || (hid[c] >> (2 * i + 1) & 1)) bb = 0.0f;
-                    }
-                    if (i & 1) sum1 = fma2(pack2(a, bb), one2, sum1);
-                    else sum0 = fma2(pack2(a, bb), one2, sum0);
+                    sum[i & 1] = fma2(pack2(a, bb), one2, sum[i & 1]);
                     w[i] = f16x2(a, bb);
                 }
                 tmem_st16(ts + 16 * c, w);
             }
             float a, bb, c2, d2;
-            unpack2(sum0, a, bb);
-            unpack2(sum1, c2, d2);
+            unpack2(sum[0], a, bb);
+            unpack2(sum[1], c2, d2);
             l += (a + bb) + (c2 + d2);
             tmem_wait_st();
             tc_fence_before();
@@ -509,6 +532,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                     p.lse[at] = empty ? neg_inf() : (m + log2f(l) - kBits) * 0.6931471805599453f;
             }
         }
+    }
     }
     if (!ok) atomicOr(&s_abort, 1);
     __syncwarp();
