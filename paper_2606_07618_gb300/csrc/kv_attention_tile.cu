@@ -31,11 +31,10 @@ namespace {
 
 using namespace mm;
 
-constexpr int kSoftmaxWarps = 8, kLoadWarps = 4;
-// Four warps each of an SM's quarter, three of the last four idle: a quarter of the register file then goes 2 x 192 + 80 + 48
-// (of 4 x 128 launched) to softmax, loads and MMAs.
-constexpr int kTileThreads = 32 * (kSoftmaxWarps + kLoadWarps + 4);
-constexpr int kSoftmaxRegs = 192, kLoadRegs = 80, kMmaRegs = 48;
+constexpr int kSoftmaxWarps = 8, kLoadWarps = 8, kMmaWarp = kSoftmaxWarps + kLoadWarps;
+// Five warps to a quarter of the SM, three of the last four idle: of its 5 x 96 registers a thread, softmax takes 2 x 144, loads 2 x 72, MMAs 48.
+constexpr int kTileThreads = 32 * (kMmaWarp + 4);
+constexpr int kSoftmaxRegs = 144, kLoadRegs = 72, kMmaRegs = 48;
 constexpr int kKeys = 128, kRows = 128;
 constexpr float kBits = 7.0f, kGrowth = 8.0f, kJoinBits = 15.0f;
 
@@ -60,9 +59,9 @@ __device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
-__device__ __forceinline__ uint32_t scale_pair(uint32_t code) {     // E4M3 code -> its fp16 value twice
+__device__ __forceinline__ uint32_t scale_pair(uint32_t code2) {    // an E4M3 code twice -> its fp16 value twice
     uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(code | code << 8)));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)code2));
     return h;
 }
 __device__ __forceinline__ uint4 e2m1x8_scaled(uint32_t w, uint32_t s) {
@@ -167,19 +166,15 @@ struct Held {
             for (int j = 0; j < 4; j++) s[i] |= (uint32_t)q[(int64_t)(4 * i + j) << c.page_log2] << (8 * j);
         }
     }
-    // into row `row` of an operand
-    __device__ __forceinline__ void store(uint32_t op, int row) const {
+    // into a row of an operand, whose address has the row's swizzle in its chunk bits (16 bytes: 8 elements)
+    __device__ __forceinline__ void store(uint32_t row) const {
 #pragma unroll
         for (int b = 0; b < D / 16; b++) {
-            const uint32_t sc = scale_pair((s[b / 4] >> (8 * (b & 3))) & 0xFF);
+            const uint32_t sc = scale_pair(__byte_perm(s[b / 4], 0, 0x1111 * (b & 3)));
             const uint4& v = w[b / 2];
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const int chunk = 2 * b + h;                     // of 8 elements
-                const uint32_t code = b & 1 ? (h ? v.w : v.z) : (h ? v.y : v.x);
-                st_shared16(op + (chunk >> 3) * Shape<D>::kPanel + row * 128 + (((chunk & 7) ^ (row & 7)) << 4),
-                            e2m1x8_scaled(code, sc));
-            }
+            const uint32_t at = (row ^ ((2 * b & 7) << 4)) + (b >> 2) * Shape<D>::kPanel;
+            st_shared16(at, e2m1x8_scaled(b & 1 ? v.z : v.x, sc));
+            st_shared16(at ^ 16, e2m1x8_scaled(b & 1 ? v.w : v.y, sc));
         }
     }
 };
@@ -237,11 +232,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
 
     const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;
     const uint32_t sq = base, sk = base + 2 * H::kOp, sv = base + 4 * H::kOp;
-    if (warp == kSoftmaxWarps + kLoadWarps) tmem_alloc(smem_u32(&s_tmem), 512);
+    if (warp == kMmaWarp) tmem_alloc(smem_u32(&s_tmem), 512);
     if (tid == 0) {
         for (int i = 0; i < 2; i++) {
-            mbar_init(smem_u32(&s_bars.k_full[i]), kLoadWarps);
-            mbar_init(smem_u32(&s_bars.v_full[i]), kLoadWarps);
+            mbar_init(smem_u32(&s_bars.k_full[i]), 4);
+            mbar_init(smem_u32(&s_bars.v_full[i]), 4);
             mbar_init(smem_u32(&s_bars.k_empty[i]), 1);
             mbar_init(smem_u32(&s_bars.v_empty[i]), 1);
             mbar_init(smem_u32(&s_bars.s_full[i]), 1);
@@ -304,11 +299,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     const uint32_t tmem = s_tmem;
 
     bool ok = true;
-    if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kLoadWarps) {
+    if (warp >= kSoftmaxWarps && warp < kMmaWarp) {
         regs_down<kLoadRegs>();
-        const int t = tid - 32 * kSoftmaxWarps;                  // token of the tile
-        // items: keys of a tile, then its values; the next two items' bytes are on their way, and the page after them
-        Held<D> now, next;
+        // four warps the keys, four the values; the next tile's bytes are on their way, and the page after it
+        const int t = tid & 127, part_kv = (warp - kSoftmaxWarps) >> 2;
         auto page_of = [&](int j) -> int64_t {
             const int64_t x = begin + (int64_t)j * kKeys + t;
             if (j >= tiles || x >= end) return -1;
@@ -318,36 +312,31 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
             return -2;
         };
         const auto at = [&](int j) { return (int)((begin + (int64_t)j * kKeys + t) & ((1 << p.c.page_log2) - 1)); };
+        uint64_t *empty = part_kv ? s_bars.v_empty : s_bars.k_empty, *full = part_kv ? s_bars.v_full : s_bars.k_full;
+        const uint32_t row = (part_kv ? sv : sk) + t * 128 + ((t & 7) << 4);
+        Held<D> now;
         int64_t page = page_of(0), page1 = page_of(1);
-        bool hidden = page == -2;
-        now.load(p.c, page, at(0), head, 0);
-        next.load(p.c, page, at(0), head, 1);
+        now.load(p.c, page, at(0), head, part_kv);
 #pragma unroll 1
-        for (int i = 0; i < 2 * tiles; i++) {
-            const int j = i >> 1, part = i & 1, st = j & 1;
-            Bars& bars = s_bars;
-            uint64_t *empty = part ? &bars.v_empty[st] : &bars.k_empty[st], *full = part ? &bars.v_full[st] : &bars.k_full[st];
-            if (j >= 2 && !mbar_wait_warp(smem_u32(empty), ((j >> 1) & 1) ^ 1)) { ok = false; break; }
-            if (part == 0) {
-                const uint32_t mask = __ballot_sync(0xffffffffu, hidden);
+        for (int j = 0; j < tiles; j++) {
+            const int st = j & 1;
+            if (j >= 2 && !mbar_wait_warp(smem_u32(empty + st), ((j >> 1) & 1) ^ 1)) { ok = false; break; }
+            if (part_kv == 0) {
+                const uint32_t mask = __ballot_sync(0xffffffffu, page == -2);
                 if (lane == 0) s_hidden[j & 3][warp - kSoftmaxWarps] = mask;
             }
-            now.store((part ? sv : sk) + st * H::kOp, t);
+            now.store(row + st * H::kOp);
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(full));
-            now = next;
-            if (part == 0) {
-                page = page1;
-                page1 = page_of(j + 2);
-                hidden = page == -2;
-            }
-            next.load(p.c, page, at(j + 1), head, part);
+            if (lane == 0) mbar_arrive(smem_u32(full + st));
+            page = page1;
+            page1 = page_of(j + 2);
+            now.load(p.c, page, at(j + 1), head, part_kv);
         }
         if (p.status && __any_sync(0xffffffffu, outside) && lane == 0) atomicOr(p.status, kStatusBounds);
-    } else if (warp >= kSoftmaxWarps + kLoadWarps) {
+    } else if (warp >= kMmaWarp) {
         regs_down<kMmaRegs>();
-        if (warp == kSoftmaxWarps + kLoadWarps) {
+        if (warp == kMmaWarp) {
         // all lanes run the loop and one is elected to issue, so that descriptors stay in uniform registers
         constexpr uint32_t id_s = idesc_f16(kKeys, false), id_o = idesc_f16(D, true);
         auto scores = [&](int x, int st) {
@@ -418,26 +407,31 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
 #pragma unroll
             for (int c = 0; c < 4; c++) hid[c] = s_hidden[j & 3][c];
             const bool whole = __all_sync(0xffffffffu, left >= kKeys && !(hid[0] | hid[1] | hid[2] | hid[3]));
-            float v[4][32];
+            // the maximum over both halves of the scores; the first half stays in registers
+            float v[2][32], t4[4];
 #pragma unroll
-            for (int c = 0; c < 4; c++) tmem_ld32(ts + 32 * c, v[c]);
-            wait_ld32(v[0]);
+            for (int h = 1; h >= 0; h--) {
+                tmem_ld32(ts + 64 * h, v[0]);
+                tmem_ld32(ts + 64 * h + 32, v[1]);
+                wait_ld32(v[0]);
+                hold32(v[1]);
+                if (!whole) {
 #pragma unroll
-            for (int c = 1; c < 4; c++) hold32(v[c]);
-            if (!whole) {
+                    for (int c = 0; c < 2; c++)
 #pragma unroll
-                for (int c = 0; c < 4; c++)
+                        for (int i = 0; i < 32; i++)
+                            if (64 * h + 32 * c + i >= left || (hid[2 * h + c] >> i & 1)) v[c][i] = neg_inf();
+                }
 #pragma unroll
-                    for (int i = 0; i < 32; i++)
-                        if (32 * c + i >= left || (hid[c] >> i & 1)) v[c][i] = neg_inf();
-            }
-            float t4[4];
+                for (int c = 0; c < 2; c++) {
+                    float x = max3_nan(v[c][0], v[c][1], v[c][2]), y = max3_nan(v[c][3], v[c][4], v[c][5]);
 #pragma unroll
-            for (int c = 0; c < 4; c++) {
-                t4[c] = max3_nan(v[c][0], v[c][1], v[c][2]);
-#pragma unroll
-                for (int i = 3; i < 31; i += 2) t4[c] = max3_nan(t4[c], v[c][i], v[c][i + 1]);
-                t4[c] = max3_nan(t4[c], v[c][31], v[c][31]);
+                    for (int i = 6; i < 30; i += 4) {
+                        x = max3_nan(x, v[c][i], v[c][i + 1]);
+                        y = max3_nan(y, v[c][i + 2], v[c][i + 3]);
+                    }
+                    t4[2 * h + c] = max3_nan(max3_nan(x, v[c][30], v[c][31]), y, y);
+                }
             }
             float top = max3_nan(max3_nan(t4[0], t4[1], t4[2]), t4[3], t4[3]);
             top *= fac;
@@ -464,18 +458,34 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
             const u64 one2 = pack2(1.0f, 1.0f);
             u64 sum[2] = {0ull, 0ull};
 #pragma unroll
-            for (int c = 0; c < 4; c++) {
-                uint32_t w[16];
+            for (int h = 0; h < 2; h++) {
+                if (h == 1) {
+                    tmem_ld32(ts + 64, v[0]);
+                    tmem_ld32(ts + 96, v[1]);
+                    wait_ld32(v[0]);
+                    hold32(v[1]);
+                    if (!whole) {
 #pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    float a, bb;
-                    unpack2(fma2(pack2(v[c][2 * i], v[c][2 * i + 1]), f2, s2), a, bb);
-                    a = ex2(a);
-                    bb = ex2(bb);
-                    sum[i & 1] = fma2(pack2(a, bb), one2, sum[i & 1]);
-                    w[i] = f16x2(a, bb);
+                        for (int c = 0; c < 2; c++)
+#pragma unroll
+                            for (int i = 0; i < 32; i++)
+                                if (64 + 32 * c + i >= left || (hid[2 + c] >> i & 1)) v[c][i] = neg_inf();
+                    }
                 }
-                tmem_st16(ts + 16 * c, w);
+#pragma unroll
+                for (int c = 0; c < 2; c++) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        float a, bb;
+                        unpack2(fma2(pack2(v[c][2 * i], v[c][2 * i + 1]), f2, s2), a, bb);
+                        a = ex2(a);
+                        bb = ex2(bb);
+                        sum[i & 1] = fma2(pack2(a, bb), one2, sum[i & 1]);
+                        w[i] = f16x2(a, bb);
+                    }
+                    tmem_st16(ts + 32 * h + 16 * c, w);
+                }
             }
             float a, bb, c2, d2;
             unpack2(sum[0], a, bb);
@@ -539,7 +549,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == kSoftmaxWarps + kLoadWarps) tmem_dealloc(tmem, 512);
+    if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
     if (tid == 0 && s_abort && p.status) atomicOr(p.status, kStatusTimeout);
 }
 
