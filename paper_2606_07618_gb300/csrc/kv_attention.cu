@@ -79,14 +79,6 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
     return r;
 }
 
-// What a block works on: the keys [begin, end) of one sequence or of the prefix, for one tile of rows.
-struct Job {
-    const int32_t* table;
-    int64_t width, begin, end;           // page numbers; tokens
-    int64_t row0, n, past;               // first row of q, queries; tokens that the first query sees, less one
-    int64_t first;                       // first row (query, head of the group) of the tile
-};
-
 template <int D, int NT>
 struct Tile {
     static constexpr int R = 8 * NT;
@@ -107,18 +99,73 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[W]) {
     }
 }
 
-// PART: the result goes to the workspace as one of several parts (else to out).
-template <int D, int NT, bool PREFIX, bool PART>
+// Where a block's result goes: to out; to out together with the other blocks of its cluster, the parts of the
+// same rows; to the workspace, for join_kernel.
+enum Join { kAlone, kCluster, kWorkspace };
+
+__device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t a) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// Four elements of a row's result: top its largest logit (base 2), sum that of its weights, v weights times values.
+template <int D, bool PART>
+__device__ __forceinline__ void write_row(const Attention& p, int64_t part, int64_t row0, int head, int64_t row, int d,
+                                          const float4& v, float top, float sum) {
+    const int64_t token = row0 + row / p.group, h = head * (int64_t)p.group + row % p.group;
+    if (PART) {
+        const int64_t at = (part * p.tokens + token) * p.q_heads + h;
+        *reinterpret_cast<float4*>(static_cast<float*>(p.workspace) + at * D + d) = v;
+        if (d == 0) reinterpret_cast<float2*>(static_cast<char*>(p.workspace) + p.plan.values)[at] = make_float2(top, sum);
+        return;
+    }
+    const bool empty = top == neg_inf();
+    const float f = empty ? 0.0f : ld_f32(p.c.S_v) / sum;
+    const float o[4] = {empty ? 0.0f : v.x * f, empty ? 0.0f : v.y * f, empty ? 0.0f : v.z * f, empty ? 0.0f : v.w * f};
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; i++) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(o[2 * i + 1]), "f"(o[2 * i]));
+    uint16_t* out = static_cast<uint16_t*>(p.out.p) + token * p.out.token + h * p.out.head + d;
+    if (p.out.vec) {
+        *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) out[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+    }
+    if (p.lse && d == 0) p.lse[token * p.q_heads + h] = empty ? neg_inf() : (top + log2f(sum) - kWeightBits) * 0.6931471805599453f;
+}
+
+template <int D, int NT, bool PREFIX, int JOIN>
 __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, int64_t part0) {
+    constexpr bool PART = JOIN == kWorkspace;
     using T = Tile<D, NT>;
-    __shared__ float s_o[4][T::R][D];
-    __shared__ float s_m[4][T::R], s_l[4][T::R];
-    grid_launch_dependents();
-    grid_dependency_wait();
+    __shared__ alignas(16) float s_o[4][T::R][D];
+    __shared__ float s_m[4][T::R], s_l[4][T::R], s_top[T::R], s_sum[T::R];
+    if (!p.second) grid_dependency_wait();
+    grid_launch_dependents();                                    // behind the wait: the next pass counts on it
+    struct AtEnd {
+        int wait;
+        __device__ ~AtEnd() {
+            if (wait) grid_dependency_wait();
+        }
+    } at_end{p.second};
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int head = blockIdx.y;
-    const int64_t tile = blockIdx.x % pass.tiles, rest = blockIdx.x / pass.tiles;
-    const int64_t part = rest % pass.parts, b = rest / pass.parts;
+    const uint32_t parts = (uint32_t)pass.parts, x = blockIdx.x / parts, part = blockIdx.x - x * parts;
+    const int64_t b = x / (uint32_t)pass.tiles, tile = x - b * pass.tiles;
 
     int64_t row0 = 0, n, len;
     const int32_t* table;
@@ -151,15 +198,16 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
     if (first >= rows) return;
     // keys that the tile's last row sees
     const int64_t last = (first + T::R < rows ? first + T::R : rows) - 1;
-    int64_t sees = causal ? len - n + last / p.group + 1 : len;
-    const int64_t begin = part * pass.chunk;
-    const int64_t end = begin + pass.chunk < sees ? begin + pass.chunk : sees;
+    const int64_t sees = causal ? len - n + last / p.group + 1 : len;
+    const int64_t chunk = part_tokens(len, pass.parts, kWarpTokens), from = part * chunk;
+    // tokens fit 31 bits from here on
+    const int begin = (int)from, end = (int)(from + chunk < sees ? from + chunk : sees);
     if (PART && begin >= end) return;
 
     // queries, scaled by a power of two, as the narrow operand: row 8 nt + g, elements from t D/4 on
     uint32_t qf[NT][2 * T::KW][2];
     float fac[NT][2], m[NT][2], l[NT][2];
-    int64_t lim[NT][2];
+    int lim[NT][2];
     const float S = ld_f32(p.c.S_k) * p.scale * 1.4426950408889634f;
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
@@ -198,7 +246,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
         for (int c = 0; c < 2; c++) {                            // columns 2t, 2t + 1 of the MMA's result
             const int64_t rc = first + 8 * nt + 2 * t + c;
             fac[nt][c] = S * __shfl_sync(0xffffffffu, up, (2 * t + c) * 4);
-            lim[nt][c] = rc < rows ? (causal ? len - n + rc / p.group + 1 : len) : 0;
+            lim[nt][c] = rc < rows ? (int)(causal ? len - n + rc / p.group + 1 : len) : 0;
             m[nt][c] = neg_inf();
             l[nt][c] = 0.0f;
         }
@@ -210,7 +258,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
         for (int i = 0; i < D / 16; i++)
 #pragma unroll
             for (int c = 0; c < 4; c++) o[nt][i][c] = 0.0f;
-    int64_t least = end;                                         // keys that every row sees
+    int least = end;                                             // keys that every row sees
 #pragma unroll
     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
@@ -218,20 +266,19 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
             if (first + 8 * nt + 2 * t + c < rows && lim[nt][c] < least) least = lim[nt][c];
 #pragma unroll
     for (int i = 1; i < 4; i *= 2) {
-        const int64_t other = __shfl_xor_sync(0xffffffffu, least, i);
-        least = other < least ? other : least;
+        least = min(least, __shfl_xor_sync(0xffffffffu, least, i));
     }
 
     const int page_mask = (1 << p.c.page_log2) - 1;
     const int64_t head_codes = (int64_t)D << p.c.page_log2, part_codes = head_codes / 2;   // bytes of a page: a head's, K's
     const int64_t part_sf = (int64_t)(D / 16) << p.c.page_log2;
-    for (int64_t k0 = begin + warp * kWarpTokens; k0 < end; k0 += 4 * kWarpTokens) {
+    for (int k0 = begin + warp * kWarpTokens; k0 < end; k0 += 4 * kWarpTokens) {
         // pages of this lane's keys (16-token group g / 2) and values (group t); -1: hidden
         int64_t pages[2];
         int at[2];
 #pragma unroll
         for (int i = 0; i < 2; i++) {
-            const int64_t j = k0 + 16 * (i ? t : g >> 1);
+            const int j = k0 + 16 * (i ? t : g >> 1);
             int64_t pg = -1;
             if (j < end) {
                 pg = table[j >> p.c.page_log2];
@@ -241,7 +288,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
                 }
             }
             pages[i] = pg;
-            at[i] = (int)(j & page_mask);
+            at[i] = j & page_mask;
         }
         uint32_t kc[8][T::KW], ks[T::KB][4], vc[16][T::VW], vs[4];
         const bool kv_ok = pages[0] >= 0, vv_ok = pages[1] >= 0;
@@ -315,7 +362,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
                 for (int c = 0; c < 4; c++) {
                     float v = sc[nt][i][c] * fac[nt][c & 1];
                     if (!whole) {
-                        const int64_t j = k0 + 16 * (g >> 1) + 4 * i + (g & 1) + (c & 2);
+                        const int j = k0 + 16 * (g >> 1) + 4 * i + (g & 1) + (c & 2);
                         v = kv_ok && j < lim[nt][c & 1] && j < end ? v : neg_inf();
                     }
                     sc[nt][i][c] = v;
@@ -413,32 +460,52 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
                 for (int h = 0; h < 2; h++) s_o[warp][r][g * (D / 8) + 2 * i + h] = o[nt][i][2 * h + c] * w;
         }
     __syncthreads();
-    const float Sv = ld_f32(p.c.S_v);
-    for (int x = threadIdx.x; x < T::R * D; x += kThreads) {
-        const int r = x / D, d = x % D;
-        const int64_t row = first + r;
-        if (row >= rows) break;
+    // the block's sums, four neighbouring elements to a thread, into the first warp's place
+    for (int x = threadIdx.x; x < T::R * D / 4; x += kThreads) {
+        const int r = x / (D / 4), d = x % (D / 4) * 4;
+        float4 v = *reinterpret_cast<const float4*>(&s_o[0][r][d]);
+#pragma unroll
+        for (int w = 1; w < 4; w++) {
+            const float4 u = *reinterpret_cast<const float4*>(&s_o[w][r][d]);
+            v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+        }
         float top = neg_inf(), sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < 4; w++) top = max_nan(top, s_m[w][r]);
 #pragma unroll
         for (int w = 0; w < 4; w++) sum += s_m[w][r] == neg_inf() ? 0.0f : s_l[w][r] * ex2(s_m[w][r] - top);
-        const float v = (s_o[0][r][d] + s_o[1][r][d]) + (s_o[2][r][d] + s_o[3][r][d]);
-        const int64_t token = row0 + row / p.group, h = head * (int64_t)p.group + row % p.group;
-        if (PART) {
-            const int64_t at = ((part0 + part) * p.tokens + token) * p.q_heads + h;
-            static_cast<float*>(p.workspace)[at * D + d] = v;
-            if (d == 0)
-                reinterpret_cast<float2*>(static_cast<char*>(p.workspace) + p.plan.values)[at] = make_float2(top, sum);
-        } else {
-            const float out = top == neg_inf() ? 0.0f : v * (Sv / sum);
-            uint32_t bits;
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(bits) : "f"(0.0f), "f"(out));
-            static_cast<uint16_t*>(p.out.p)[token * p.out.token + h * p.out.head + d] = (uint16_t)bits;
-            if (p.lse && d == 0)
-                p.lse[token * p.q_heads + h] =
-                    top == neg_inf() ? neg_inf() : (top + log2f(sum) - kWeightBits) * 0.6931471805599453f;
+        if (JOIN == kCluster) {
+            *reinterpret_cast<float4*>(&s_o[0][r][d]) = v;
+            if (d == 0) s_top[r] = top, s_sum[r] = sum;
+        } else if (first + r < rows) {
+            write_row<D, PART>(p, part0 + part, row0, head, first + r, d, v, top, sum);
         }
+    }
+    if (JOIN == kCluster) {
+        cluster_arrive();
+        cluster_wait();
+        for (int x = (int)part * kThreads + threadIdx.x; x < T::R * D / 4; x += (int)parts * kThreads) {
+            const int r = x / (D / 4), d = x % (D / 4) * 4;
+            if (first + r >= rows) break;
+            float tops[kMaxCluster], top = neg_inf(), sum = 0.0f;
+#pragma unroll
+            for (uint32_t k = 0; k < kMaxCluster; k++) {
+                tops[k] = k < parts ? ld_cluster(cluster_addr(&s_top[r], k)) : neg_inf();
+                top = max_nan(top, tops[k]);
+            }
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (uint32_t k = 0; k < kMaxCluster; k++) {
+                if (k >= parts || tops[k] == neg_inf()) continue;
+                const float w = ex2(tops[k] - top);
+                const float4 u = ld_cluster4(cluster_addr(&s_o[0][r][d], k));
+                sum += ld_cluster(cluster_addr(&s_sum[r], k)) * w;
+                v.x += u.x * w, v.y += u.y * w, v.z += u.z * w, v.w += u.w * w;
+            }
+            write_row<D, false>(p, 0, row0, head, first + r, d, v, top, sum);
+        }
+        cluster_arrive();                                        // a block's memory stays until the others have read it
+        cluster_wait();
     }
 }
 
@@ -464,13 +531,17 @@ __global__ void __launch_bounds__(256) join_kernel(Attention p) {
     int64_t len = p.lens[b], most = p.width << p.c.page_log2;
     len = len < 0 ? 0 : len > most ? most : len;
     const int64_t sees = p.causal ? len - n + i + 1 : len;
-    const int64_t own = sees <= 0 ? 0 : (sees + p.plan.own.chunk - 1) / p.plan.own.chunk;
+    const int64_t chunk = part_tokens(len, p.plan.own.parts, p.plan.own.step());
+    const int64_t own = sees <= 0 ? 0 : (sees + chunk - 1) / chunk;
     int64_t shared = 0;
     if (p.prefix_len) {
         int64_t len2 = *p.prefix_len;
         most = p.prefix_width << p.c.page_log2;
         len2 = len2 < 0 ? 0 : len2 > most ? most : len2;
-        shared = p.plan.prefix.parts ? (len2 + p.plan.prefix.chunk - 1) / p.plan.prefix.chunk : 0;
+        if (p.plan.prefix.parts) {
+            const int64_t c2 = part_tokens(len2, p.plan.prefix.parts, p.plan.prefix.step());
+            shared = (len2 + c2 - 1) / c2;
+        }
     }
     // parts 0 .. own - 1 and those of the prefix, behind the most that a sequence has
     const float2* ml = reinterpret_cast<const float2*>(static_cast<const char*>(p.workspace) + p.plan.values);
@@ -523,36 +594,45 @@ __global__ void __launch_bounds__(256) join_kernel(Attention p) {
         p.lse[at] = top == neg_inf() ? neg_inf() : (top + log2f(sum) - kWeightBits) * 0.6931471805599453f;
 }
 
-cudaError_t launch_2d(void (*kernel)(Attention, Pass, int64_t), int64_t x, int y, cudaStream_t s, const Attention& p,
-                      const Pass& pass, int64_t part0) {
+template <int D, int NT, bool PREFIX, int JOIN>
+cudaError_t launch_rows(const Attention& p, const Pass& pass, int64_t part0, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)x, (unsigned)y);
+    cfg.gridDim = dim3((unsigned)((PREFIX ? 1 : p.batch) * pass.parts * pass.tiles), (unsigned)p.c.heads);
     cfg.blockDim = dim3(kThreads);
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)pass.parts;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, p, pass, part0);
+    cfg.numAttrs = JOIN == kCluster ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, rows_kernel<D, NT, PREFIX, JOIN>, p, pass, part0);
 }
 
-template <int D, bool PREFIX>
-cudaError_t launch_rows(const Attention& p, const Pass& pass, int64_t part0, cudaStream_t s) {
-    if (pass.rows > 16) return launch_tiles(p, pass, PREFIX, part0, s);
-    const int64_t x = (PREFIX ? 1 : p.batch) * pass.parts * pass.tiles;
-    const bool part = p.plan.parts() > 1;
-    if (pass.rows == 8)
-        return launch_2d(part ? rows_kernel<D, 1, PREFIX, true> : rows_kernel<D, 1, PREFIX, false>, x, p.c.heads, s, p, pass, part0);
-    return launch_2d(part ? rows_kernel<D, 2, PREFIX, true> : rows_kernel<D, 2, PREFIX, false>, x, p.c.heads, s, p, pass, part0);
+template <int D, int NT>
+cudaError_t dispatch(const Attention& p, const Pass& pass, bool prefix, int64_t part0, cudaStream_t s) {
+    if (prefix) return launch_rows<D, NT, true, kWorkspace>(p, pass, part0, s);
+    if (p.plan.through) return launch_rows<D, NT, false, kWorkspace>(p, pass, part0, s);
+    return pass.parts > 1 ? launch_rows<D, NT, false, kCluster>(p, pass, part0, s) : launch_rows<D, NT, false, kAlone>(p, pass, part0, s);
+}
+
+template <int D>
+cudaError_t launch_pass(const Attention& p, const Pass& pass, bool prefix, int64_t part0, cudaStream_t s) {
+    if (pass.rows == kTileRows) return launch_tiles(p, pass, prefix, part0, s);
+    return pass.rows == 8 ? dispatch<D, 1>(p, pass, prefix, part0, s) : dispatch<D, 2>(p, pass, prefix, part0, s);
 }
 
 template <int D>
 cudaError_t launch(const Attention& p, cudaStream_t s) {
-    cudaError_t e = launch_rows<D, false>(p, p.plan.own, 0, s);
-    if (e == cudaSuccess && p.plan.prefix.parts) e = launch_rows<D, true>(p, p.plan.prefix, p.plan.own.parts, s);
-    if (e == cudaSuccess && p.plan.parts() > 1)
-        e = launch_dependent(join_kernel<D>, (p.tokens * p.q_heads + 7) / 8, 256, s, p);
+    cudaError_t e = launch_pass<D>(p, p.plan.own, false, 0, s);
+    if (e == cudaSuccess && p.plan.prefix.parts) {
+        Attention q = p;
+        q.second = 1;
+        e = launch_pass<D>(q, p.plan.prefix, true, p.plan.own.parts, s);
+    }
+    if (e == cudaSuccess && p.plan.through) e = launch_dependent(join_kernel<D>, (p.tokens * p.q_heads + 7) / 8, 256, s, p);
     return e;
 }
 

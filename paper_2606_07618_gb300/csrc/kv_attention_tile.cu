@@ -186,8 +186,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     __shared__ Bars s_bars;
     __shared__ uint32_t s_tmem, s_hidden[4][4];
     __shared__ int s_abort;
-    grid_launch_dependents();
-    grid_dependency_wait();
+    if (!p.second) grid_dependency_wait();
+    grid_launch_dependents();                                    // behind the wait: the next pass counts on it
+    struct AtEnd {
+        int wait;
+        __device__ ~AtEnd() {
+            if (wait) grid_dependency_wait();
+        }
+    } at_end{p.second};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int head = blockIdx.y;
     // tiles from the last one on: with a causal mask it has the most keys
@@ -224,8 +230,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     if (first >= rows) return;
     const int64_t last = (first + 2 * kRows < rows ? first + 2 * kRows : rows) - 1;
     const int64_t sees = causal ? len - n + last / p.group + 1 : len;
-    const int64_t begin = part * pass.chunk;
-    const int64_t end = begin + pass.chunk < sees ? begin + pass.chunk : sees;
+    const int64_t chunk = part_tokens(len, pass.parts, kTileKeys), begin = part * chunk;
+    const int64_t end = begin + chunk < sees ? begin + chunk : sees;
     if (PART && begin >= end) return;
     const int tiles = end > begin ? (int)((end - begin + kKeys - 1) / kKeys) : 0;      // a part is less than 2^31 tokens
     const int both = rows - first > kRows;                       // the second tile has rows
@@ -580,8 +586,8 @@ cudaError_t launch(const Attention& p, const Pass& pass, int64_t part0, cudaStre
 
 template <int D>
 cudaError_t dispatch(const Attention& p, const Pass& pass, bool prefix, int64_t part0, cudaStream_t s) {
-    if (prefix) return p.plan.parts() > 1 ? launch<D, true, true>(p, pass, part0, s) : launch<D, true, false>(p, pass, part0, s);
-    return p.plan.parts() > 1 ? launch<D, false, true>(p, pass, part0, s) : launch<D, false, false>(p, pass, part0, s);
+    if (prefix) return launch<D, true, true>(p, pass, part0, s);
+    return p.plan.through ? launch<D, false, true>(p, pass, part0, s) : launch<D, false, false>(p, pass, part0, s);
 }
 
 }  // namespace

@@ -67,6 +67,10 @@ struct Attention {
     int* status;
     void* workspace;
     Plan plan;
+    // Set for the second pass of a call.  It is launched as a dependent of the first, whose blocks let it start only once
+    // they have waited for what came before the call themselves; it shares nothing with the first pass, so it does not wait
+    // for it before its end (which the join then waits for).
+    int second;
 };
 
 cudaError_t launch_rope(const Rope& p, int sms, cudaStream_t s);

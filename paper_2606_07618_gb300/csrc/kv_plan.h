@@ -6,13 +6,13 @@
 namespace nvfp4 {
 namespace kv {
 
-// Tokens of the cache that one warp takes at a time, and one block.
-constexpr int kWarpTokens = 64, kBlockTokens = 256;
-// Blocks that fill the GPU about twice: 152 SMs with four of them each.
-constexpr int64_t kBlocks = 152 * 4 * 2;
-// Rows of a block on tcgen05 (one block an SM), keys that it takes at a time.
+// Few rows (kv_attention.cu): a warp takes 64 tokens at a time, a block has four warps and an SM holds three
+// (dim 128) or four blocks.  Parts of one sequence and head join in a cluster of up to 8 blocks, more of them
+// through the workspace.
+constexpr int kWarpTokens = 64, kMaxCluster = 8;
+constexpr int64_t kSms = 152;
+// Many rows (kv_attention_tile.cu): rows of a block, one to an SM, and the keys that it takes at a time.
 constexpr int kTileRows = 256, kTileKeys = 128;
-constexpr int64_t kTileBlocks = 152;
 
 struct Sizes {
     int64_t tokens, batch, max_q;        // rows of q, sequences, the most queries of one
@@ -20,16 +20,30 @@ struct Sizes {
     int64_t length, prefix;              // the most cached tokens that the tables hold
 };
 
-// One pass over keys: rows of a key head in tiles of `rows`, keys in `parts` of `chunk` tokens.
+#ifdef __CUDACC__
+#define KV_BOTH __host__ __device__
+#else
+#define KV_BOTH
+#endif
+
+// One pass over keys: rows of a key head in tiles of `rows`, keys in `parts`.
 struct Pass {
     int rows;
-    int64_t tiles, parts, chunk;
+    int64_t tiles, parts;
+    KV_BOTH int64_t step() const { return rows == kTileRows ? kTileKeys : kWarpTokens; }
 };
+
+// Tokens of a part of a sequence of `length`: the parts are as even as whole steps allow.
+KV_BOTH inline int64_t part_tokens(int64_t length, int64_t parts, int64_t step) {
+    const int64_t n = (length + parts * step - 1) / (parts * step);
+    return (n < 1 ? 1 : n) * step;
+}
 
 struct Plan {
     Pass own, prefix;                    // prefix.parts is 0 without one
     int64_t parts() const { return own.parts + prefix.parts; }
-    // Sums of the parts, [parts][tokens][q_heads][dim] fp32, and their maxima and sums of weights.
+    // Whether the parts' sums go through the workspace: [parts][tokens][q_heads][dim] fp32, then maxima and sums of weights.
+    bool through = false;
     int64_t values = 0, bytes = 0;
     bool small = true;
     // Whether the launches' grids can hold it.
@@ -38,29 +52,53 @@ struct Plan {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-inline Pass plan_pass(int64_t sequences, int64_t heads, int64_t rows, int64_t length) {
+// Parts of a few rows' pass.  Blocks of equal work run in whole waves; of sequences between nothing and `length` tokens the
+// average is half of that, and the last block to start may be a longest one.  A block costs as much as
+// kBlockCost tokens before and after its loop.  The parts for which the two estimates together are least are taken.
+inline int64_t thin_parts(int64_t pairs, int64_t length, int64_t slots) {
+    constexpr int64_t kBlockCost = 384;
+    if (pairs * kMaxCluster <= slots) {  // few: all that there are, at 256 tokens a block or more
+        const int64_t most = ceil_div(length, 4 * kWarpTokens), all = slots / pairs;
+        if (most <= kMaxCluster) return ceil_div(length, 2 * kWarpTokens) < kMaxCluster ? ceil_div(length, 2 * kWarpTokens) : kMaxCluster;
+        return most < all ? most : all;
+    }
+    int64_t best = 1, least = INT64_MAX;
+    for (int64_t n = 1; n <= kMaxCluster; n++) {
+        if (n > 1 && (n - 1) * 2 * kWarpTokens >= length) break;
+        const int64_t block = kBlockCost + length / n, waves = ceil_div(pairs * n, slots);
+        const int64_t ragged = waves == 1 ? block : pairs * n * (kBlockCost + length / n / 2) / slots + block;
+        if (waves * block + ragged < least) least = waves * block + ragged, best = n;
+    }
+    return best;
+}
+
+inline Pass plan_pass(int64_t sequences, int64_t heads, int64_t dim, int64_t rows, int64_t length) {
     Pass p;
     p.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kTileRows;
     p.tiles = ceil_div(rows, p.rows);
-    const bool tile = p.rows == kTileRows;
-    const int64_t step = tile ? kTileKeys : kBlockTokens;
-    const int64_t most = length > step ? ceil_div(length, step) : 1;
-    int64_t parts = (tile ? kTileBlocks : kBlocks) / sequences / heads / p.tiles;
-    parts = parts < 1 ? 1 : parts > most ? most : parts;
-    p.chunk = ceil_div(length > 0 ? length : 1, parts * step) * step;
-    p.parts = length > 0 ? ceil_div(length, p.chunk) : 1;
+    p.parts = 1;
+    if (length <= 0 || sequences > kSms * 64 || p.tiles > kSms * 64) return p;      // (their product would be that, too)
+    const int64_t pairs = sequences * heads * p.tiles;
+    if (p.rows < kTileRows) {
+        p.parts = thin_parts(pairs, length, kSms * (dim == 128 ? (p.rows == 8 ? 3 : 2) : (p.rows == 8 ? 4 : 2)));
+    } else if (pairs < kSms) {
+        const int64_t most = ceil_div(length, kTileKeys);
+        p.parts = kSms / pairs < most ? kSms / pairs : most;
+    }
+    if (p.parts < 1) p.parts = 1;
     return p;
 }
 
 inline Plan make_plan(const Sizes& s) {
     const int64_t group = s.q_heads / s.heads;
     Plan p;
-    p.own = plan_pass(s.batch, s.heads, s.max_q * group, s.length);
-    p.prefix = Pass{0, 0, 0, 0};
-    if (s.prefix > 0) p.prefix = plan_pass(1, s.heads, s.tokens * group, s.prefix);
+    p.own = plan_pass(s.batch, s.heads, s.dim, s.max_q * group, s.length);
+    p.prefix = Pass{0, 0, 0};
+    if (s.prefix > 0) p.prefix = plan_pass(1, s.heads, s.dim, s.tokens * group, s.prefix);
     const int64_t blocks = (int64_t)1 << 31, rows = s.tokens * s.q_heads;
     p.small = p.own.tiles < blocks / p.own.parts / s.batch && p.prefix.tiles < blocks / (p.prefix.parts + 1) && rows < 8 * blocks;
-    if (p.small && p.parts() > 1) {
+    p.through = p.parts() > 1 && !(s.prefix <= 0 && p.own.rows < kTileRows && p.own.parts <= kMaxCluster);
+    if (p.small && p.through) {
         p.values = p.parts() * s.tokens * s.q_heads * s.dim * 4;
         p.values = (p.values + 255) / 256 * 256;
         p.bytes = p.values + (p.parts() * s.tokens * s.q_heads * 8 + 255) / 256 * 256;
