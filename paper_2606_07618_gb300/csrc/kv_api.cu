@@ -366,10 +366,10 @@ nvfp4_status attention(const nvfp4_kv_cache* cache, const void* q, int64_t q_tok
     p.lens = lens;
     p.offsets = offsets;
     p.table_ld = table_ld;
-    p.width = width;
+    p.width = p.c.pages > 0 ? width : 0;                         // an empty pool holds nothing
     p.prefix = prefix;
     p.prefix_len = shared ? prefix_len : nullptr;
-    p.prefix_width = prefix_width;
+    p.prefix_width = p.c.pages > 0 ? prefix_width : 0;
     p.scale = scale;
     p.lse = lse;
     p.status = status_dev;

@@ -149,7 +149,7 @@ __device__ __forceinline__ void write_row(const Attention& p, int64_t part, int6
 }
 
 template <int D, int NT, bool PREFIX, int JOIN>
-__global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, int64_t part0) {
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kernel(Attention p, Pass pass, int64_t part0) {
     constexpr bool PART = JOIN == kWorkspace;
     using T = Tile<D, NT>;
     __shared__ alignas(16) float s_o[4][T::R][D];
@@ -203,6 +203,49 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
     // tokens fit 31 bits from here on
     const int begin = (int)from, end = (int)(from + chunk < sees ? from + chunk : sees);
     if (PART && begin >= end) return;
+
+    // What the lane reads of a tile from token k0 on: keys of the 16-token group g / 2, values of group t.  A page that is
+    // not there (behind the end, outside the pool) is read as page 0 and hidden afterwards.
+    const int page_log2 = p.c.page_log2, page_mask = (1 << page_log2) - 1, pool = (int)p.c.pages;
+    const int64_t page_codes = (int64_t)p.c.heads * D << page_log2, page_sf = page_codes / 8;      // bytes of a page
+    const uint8_t *k_codes = p.c.codes + (((int64_t)head * D) << page_log2) + (g & 1) * (D / 2) + t * (D / 8);
+    const uint8_t *k_sf = p.c.sf + ((head * 2ll * (D / 16) + t * T::KB) << page_log2);
+    const uint8_t *v_codes = p.c.codes + (((int64_t)head * D + D / 2) << page_log2) + g * (D / 16);
+    const uint8_t *v_sf = p.c.sf + (((head * 2ll + 1) * (D / 16) + g * D / 128) << page_log2);
+    auto page_of = [&](int j) {
+        int pg = -1;
+        if (j < end) {
+            pg = table[j >> page_log2];
+            if ((unsigned)pg >= (unsigned)pool) outside = true, pg = -1;
+        }
+        return pg;
+    };
+    uint32_t kc[8][T::KW], ks[T::KB][4], vc[16][T::VW], vs[4];
+    auto load_keys = [&](int k0, int pg) {
+        const int64_t page = pg < 0 ? 0 : pg;
+        const int at = (k0 + 16 * (g >> 1)) & page_mask;
+        const uint8_t *c = k_codes + page * page_codes + at * (D / 2), *f = k_sf + page * page_sf + at;
+#pragma unroll
+        for (int i = 0; i < 8; i++) load_words<T::KW>(c + i * D, kc[i]);
+#pragma unroll
+        for (int i = 0; i < T::KB; i++) load_words<4>(f + (i << page_log2), ks[i]);
+    };
+    auto load_values = [&](int k0, int pg) {
+        const int64_t page = pg < 0 ? 0 : pg;
+        const int at = (k0 + 16 * t) & page_mask;
+        const uint8_t *c = v_codes + page * page_codes + at * (D / 2), *f = v_sf + page * page_sf + at;
+#pragma unroll
+        for (int i = 0; i < 16; i++) load_words<T::VW>(c + i * (D / 2), vc[i]);
+        load_words<4>(f, vs);
+    };
+    constexpr int kStride = 4 * kWarpTokens;
+    const int start = begin + warp * kWarpTokens;
+    int kpg = page_of(start + 16 * (g >> 1)), vpg = page_of(start + 16 * t);
+    if (start < end) {
+        load_keys(start, kpg);
+        load_values(start, vpg);
+    }
+    int kpg1 = page_of(start + kStride + 16 * (g >> 1)), vpg1 = page_of(start + kStride + 16 * t);
 
     // queries, scaled by a power of two, as the narrow operand: row 8 nt + g, elements from t D/4 on
     uint32_t qf[NT][2 * T::KW][2];
@@ -269,55 +312,10 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
         least = min(least, __shfl_xor_sync(0xffffffffu, least, i));
     }
 
-    const int page_mask = (1 << p.c.page_log2) - 1;
-    const int64_t head_codes = (int64_t)D << p.c.page_log2, part_codes = head_codes / 2;   // bytes of a page: a head's, K's
-    const int64_t part_sf = (int64_t)(D / 16) << p.c.page_log2;
-    for (int k0 = begin + warp * kWarpTokens; k0 < end; k0 += 4 * kWarpTokens) {
-        // pages of this lane's keys (16-token group g / 2) and values (group t); -1: hidden
-        int64_t pages[2];
-        int at[2];
-#pragma unroll
-        for (int i = 0; i < 2; i++) {
-            const int j = k0 + 16 * (i ? t : g >> 1);
-            int64_t pg = -1;
-            if (j < end) {
-                pg = table[j >> p.c.page_log2];
-                if (pg < 0 || pg >= p.c.pages) {
-                    outside = true;
-                    pg = -1;
-                }
-            }
-            pages[i] = pg;
-            at[i] = j & page_mask;
-        }
-        uint32_t kc[8][T::KW], ks[T::KB][4], vc[16][T::VW], vs[4];
-        const bool kv_ok = pages[0] >= 0, vv_ok = pages[1] >= 0;
-        const uint8_t* kp = p.c.codes + (pages[0] * p.c.heads + head) * head_codes + (at[0] + (g & 1)) * (D / 2) + t * (D / 8);
-        const uint8_t* kq = p.c.sf + (pages[0] * p.c.heads + head) * 2 * part_sf + ((int64_t)(t * T::KB) << p.c.page_log2) + at[0];
-        const uint8_t* vp = p.c.codes + (pages[1] * p.c.heads + head) * head_codes + part_codes + at[1] * (D / 2) + g * (D / 16);
-        const uint8_t* vq = p.c.sf + ((pages[1] * p.c.heads + head) * 2 + 1) * part_sf + ((int64_t)(g * D / 128) << p.c.page_log2) + at[1];
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-#pragma unroll
-            for (int j = 0; j < T::KW; j++) kc[i][j] = 0;
-            if (kv_ok) load_words<T::KW>(kp + i * D, kc[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < T::KB; i++) {
-#pragma unroll
-            for (int j = 0; j < 4; j++) ks[i][j] = 0;
-            if (kv_ok) load_words<4>(kq + ((int64_t)i << p.c.page_log2), ks[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-#pragma unroll
-            for (int j = 0; j < T::VW; j++) vc[i][j] = 0;
-            if (vv_ok) load_words<T::VW>(vp + i * (D / 2), vc[i]);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; j++) vs[j] = 0;
-        if (vv_ok) load_words<4>(vq, vs);
-
+    // a tile's keys are loaded over the last one's as soon as those are used, its values likewise, and its page numbers
+    // one tile earlier
+    for (int k0 = start; k0 < end; k0 += kStride) {
+        const bool kv_ok = kpg >= 0, vv_ok = vpg >= 0, more = k0 + kStride < end;
         float sc[NT][4][4];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)
@@ -348,6 +346,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
                 }
             }
         }
+        if (more) load_keys(k0 + kStride, kpg1);
         // weights
         const bool whole = __all_sync(0xffffffffu, k0 + kWarpTokens <= least && kv_ok);
         uint32_t pt[NT][4][2];
@@ -403,12 +402,12 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
                     for (int c = 0; c < 4; c++) o[nt][i][c] *= alpha[nt][c & 1];
         }
         // scale bytes behind the last token may be anything, NaN among it, and 0 NaN is no 0
-        if (k0 + 16 * t + 16 > end) {
+        if (!vv_ok || k0 + 16 * t + 16 > end) {
 #pragma unroll
             for (int j = 0; j < 4; j++)
 #pragma unroll
                 for (int c = 0; c < 4; c++)
-                    if (k0 + 16 * t + 4 * j + c >= end) vs[j] &= ~(0xFFu << (8 * c));
+                    if (!vv_ok || k0 + 16 * t + 4 * j + c >= end) vs[j] &= ~(0xFFu << (8 * c));
         }
 #pragma unroll
         for (int i = 0; i < 4; i++) {
@@ -430,6 +429,9 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Attention p, Pass pass, 
                 }
             }
         }
+        if (more) load_values(k0 + kStride, vpg1);
+        kpg = kpg1, vpg = vpg1;
+        kpg1 = page_of(k0 + 2 * kStride + 16 * (g >> 1)), vpg1 = page_of(k0 + 2 * kStride + 16 * t);
     }
     if (p.status && __any_sync(0xffffffffu, outside) && lane == 0) atomicOr(p.status, kStatusBounds);
 

@@ -11,6 +11,7 @@ namespace kv {
 // through the workspace.
 constexpr int kWarpTokens = 64, kMaxCluster = 8;
 constexpr int64_t kSms = 152;
+constexpr int blocks_per_sm(int64_t dim, int rows) { return dim == 128 ? (rows == 8 ? 3 : 2) : (rows == 8 ? 4 : 3); }
 // Many rows (kv_attention_tile.cu): rows of a block, one to an SM, and the keys that it takes at a time.
 constexpr int kTileRows = 256, kTileKeys = 128;
 
@@ -80,7 +81,7 @@ inline Pass plan_pass(int64_t sequences, int64_t heads, int64_t dim, int64_t row
     if (length <= 0 || sequences > kSms * 64 || p.tiles > kSms * 64) return p;      // (their product would be that, too)
     const int64_t pairs = sequences * heads * p.tiles;
     if (p.rows < kTileRows) {
-        p.parts = thin_parts(pairs, length, kSms * (dim == 128 ? (p.rows == 8 ? 3 : 2) : (p.rows == 8 ? 4 : 2)));
+        p.parts = thin_parts(pairs, length, kSms * blocks_per_sm(dim, p.rows));
     } else if (pairs < kSms) {
         const int64_t most = ceil_div(length, kTileKeys);
         p.parts = kSms / pairs < most ? kSms / pairs : most;
