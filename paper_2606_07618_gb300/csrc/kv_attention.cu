@@ -68,6 +68,12 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// The same onto nothing.
+__device__ __forceinline__ void mma16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
     uint32_t d;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
@@ -85,18 +91,28 @@ struct Tile {
     static constexpr int KW = D / 32;    // words of codes of a token that a lane reads: keys
     static constexpr int VW = D / 64;    // and values
     static constexpr int KB = D / 64;    // key blocks of a lane
+    // A warp's tile in shared memory, [word group][lane]: keys' codes and scales, values' codes and scales.
+    static constexpr int kKeys = 8 * 32 * KW * 4, kKeySf = kKeys + KB * 512, kValues = kKeySf + 16 * 32 * VW * 4, kWarp = kValues + 512;
+    static constexpr int kSums = 4 * R * D * 4;                  // the warps' sums, over the tiles
+    static constexpr int kSmem = 4 * kWarp > kSums ? 4 * kWarp : kSums;
 };
 
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const uint8_t* src) {
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 template <int W>
-__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[W]) {
-    if constexpr (W == 4) {
-        const uint4 v = ld_stream16<false>(p);
-        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-    } else if constexpr (W == 2) {
-        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-    } else {
-        asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
-    }
+__device__ __forceinline__ void ld_shared(uint32_t a, uint32_t (&w)[W]) {
+    if constexpr (W == 4)
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a) : "memory");
+    else if constexpr (W == 2)
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a) : "memory");
+    else
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(a) : "memory");
 }
 
 // Where a block's result goes: to out; to out together with the other blocks of its cluster, the parts of the
@@ -152,7 +168,8 @@ template <int D, int NT, bool PREFIX, int JOIN>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kernel(Attention p, Pass pass, int64_t part0) {
     constexpr bool PART = JOIN == kWorkspace;
     using T = Tile<D, NT>;
-    __shared__ alignas(16) float s_o[4][T::R][D];
+    __shared__ alignas(16) uint8_t s_mem[T::kSmem];
+    float(*s_o)[T::R][D] = reinterpret_cast<float(*)[T::R][D]>(s_mem);
     __shared__ float s_m[4][T::R], s_l[4][T::R], s_top[T::R], s_sum[T::R];
     if (!p.second) grid_dependency_wait();
     grid_launch_dependents();                                    // behind the wait: the next pass counts on it
@@ -220,31 +237,34 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
         }
         return pg;
     };
-    uint32_t kc[8][T::KW], ks[T::KB][4], vc[16][T::VW], vs[4];
+    // a lane copies what it reads itself
+    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(s_mem) + warp * T::kWarp;
+    const uint32_t m_kc = mine + lane * T::KW * 4, m_ks = mine + T::kKeys + lane * 16, m_vc = mine + T::kKeySf + lane * T::VW * 4,
+                   m_vs = mine + T::kValues + lane * 16;
     auto load_keys = [&](int k0, int pg) {
         const int64_t page = pg < 0 ? 0 : pg;
         const int at = (k0 + 16 * (g >> 1)) & page_mask;
         const uint8_t *c = k_codes + page * page_codes + at * (D / 2), *f = k_sf + page * page_sf + at;
 #pragma unroll
-        for (int i = 0; i < 8; i++) load_words<T::KW>(c + i * D, kc[i]);
+        for (int i = 0; i < 8; i++) copy_async<4 * T::KW>(m_kc + i * 32 * T::KW * 4, c + i * D);
 #pragma unroll
-        for (int i = 0; i < T::KB; i++) load_words<4>(f + (i << page_log2), ks[i]);
+        for (int i = 0; i < T::KB; i++) copy_async<16>(m_ks + i * 512, f + (i << page_log2));
     };
     auto load_values = [&](int k0, int pg) {
         const int64_t page = pg < 0 ? 0 : pg;
         const int at = (k0 + 16 * t) & page_mask;
         const uint8_t *c = v_codes + page * page_codes + at * (D / 2), *f = v_sf + page * page_sf + at;
 #pragma unroll
-        for (int i = 0; i < 16; i++) load_words<T::VW>(c + i * (D / 2), vc[i]);
-        load_words<4>(f, vs);
+        for (int i = 0; i < 16; i++) copy_async<4 * T::VW>(m_vc + i * 32 * T::VW * 4, c + i * (D / 2));
+        copy_async<16>(m_vs, f);
     };
     constexpr int kStride = 4 * kWarpTokens;
     const int start = begin + warp * kWarpTokens;
     int kpg = page_of(start + 16 * (g >> 1)), vpg = page_of(start + 16 * t);
-    if (start < end) {
-        load_keys(start, kpg);
-        load_values(start, vpg);
-    }
+    if (start < end) load_keys(start, kpg);
+    copy_commit();
+    if (start < end) load_values(start, vpg);
+    copy_commit();
     int kpg1 = page_of(start + kStride + 16 * (g >> 1)), vpg1 = page_of(start + kStride + 16 * t);
 
     // queries, scaled by a power of two, as the narrow operand: row 8 nt + g, elements from t D/4 on
@@ -312,17 +332,15 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
         least = min(least, __shfl_xor_sync(0xffffffffu, least, i));
     }
 
-    // a tile's keys are loaded over the last one's as soon as those are used, its values likewise, and its page numbers
-    // one tile earlier
+    // a tile's keys are copied over the last one's as soon as those are used, its values likewise (two groups of copies in
+    // flight, keys' and values'), and its page numbers come one tile earlier
     for (int k0 = start; k0 < end; k0 += kStride) {
         const bool kv_ok = kpg >= 0, vv_ok = vpg >= 0, more = k0 + kStride < end;
+        copy_wait<1>();
+        uint32_t ks[T::KB][4];
+#pragma unroll
+        for (int i = 0; i < T::KB; i++) ld_shared(m_ks + i * 512, ks[i]);
         float sc[NT][4][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int c = 0; c < 4; c++) sc[nt][i][c] = 0.0f;
         const uint32_t pick = g & 1 ? 0x3232u : 0x1010u;
 #pragma unroll
         for (int i = 0; i < 4; i++) {
@@ -332,21 +350,28 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
                 s0[k] = __byte_perm(e4m3x2_to_f16(ks[k][i] & 0xFFFF), 0, pick);
                 s1[k] = __byte_perm(e4m3x2_to_f16(ks[k][i] >> 16), 0, pick);
             }
+            uint32_t k0c[T::KW], k1c[T::KW];
+            ld_shared(m_kc + 2 * i * 32 * T::KW * 4, k0c);
+            ld_shared(m_kc + (2 * i + 1) * 32 * T::KW * 4, k1c);
 #pragma unroll
             for (int w = 0; w < T::KW; w++) {
                 uint32_t x[4], y[4];
-                e2m1x8_to_f16(kc[2 * i][w], x);
-                e2m1x8_to_f16(kc[2 * i + 1][w], y);
+                e2m1x8_to_f16(k0c[w], x);
+                e2m1x8_to_f16(k1c[w], y);
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
                     const uint32_t a[4] = {mul_h2(x[2 * h], s0[w / 2]), mul_h2(y[2 * h], s1[w / 2]),
                                            mul_h2(x[2 * h + 1], s0[w / 2]), mul_h2(y[2 * h + 1], s1[w / 2])};
 #pragma unroll
-                    for (int nt = 0; nt < NT; nt++) mma16(sc[nt][i], a, qf[nt][2 * w + h][0], qf[nt][2 * w + h][1]);
+                    for (int nt = 0; nt < NT; nt++) {
+                        if (w + h == 0) mma16_first(sc[nt][i], a, qf[nt][0][0], qf[nt][0][1]);
+                        else mma16(sc[nt][i], a, qf[nt][2 * w + h][0], qf[nt][2 * w + h][1]);
+                    }
                 }
             }
         }
         if (more) load_keys(k0 + kStride, kpg1);
+        copy_commit();
         // weights
         const bool whole = __all_sync(0xffffffffu, k0 + kWarpTokens <= least && kv_ok);
         uint32_t pt[NT][4][2];
@@ -401,6 +426,9 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
 #pragma unroll
                     for (int c = 0; c < 4; c++) o[nt][i][c] *= alpha[nt][c & 1];
         }
+        copy_wait<1>();
+        uint32_t vs[4];
+        ld_shared(m_vs, vs);
         // scale bytes behind the last token may be anything, NaN among it, and 0 NaN is no 0
         if (!vv_ok || k0 + 16 * t + 16 > end) {
 #pragma unroll
@@ -412,10 +440,13 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const uint32_t s01 = e4m3x2_to_f16(vs[i] & 0xFFFF), s23 = e4m3x2_to_f16(vs[i] >> 16);
+            uint32_t vc[4][T::VW];
+#pragma unroll
+            for (int c = 0; c < 4; c++) ld_shared(m_vc + (4 * i + c) * 32 * T::VW * 4, vc[c]);
 #pragma unroll
             for (int w = 0; w < T::VW; w++) {
                 constexpr uint32_t kLow = 0x0F0F0F0Fu;
-                const uint32_t a = vc[4 * i][w], b2 = vc[4 * i + 1][w], c = vc[4 * i + 2][w], d = vc[4 * i + 3][w];
+                const uint32_t a = vc[0][w], b2 = vc[1][w], c = vc[2][w], d = vc[3][w];
                 uint32_t lo01[4], hi01[4], lo23[4], hi23[4];
                 e2m1x8_to_f16((a & kLow) | ((b2 << 4) & ~kLow), lo01);
                 e2m1x8_to_f16(((a >> 4) & kLow) | (b2 & ~kLow), hi01);
@@ -430,6 +461,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
             }
         }
         if (more) load_values(k0 + kStride, vpg1);
+        copy_commit();
         kpg = kpg1, vpg = vpg1;
         kpg1 = page_of(k0 + 2 * kStride + 16 * (g >> 1)), vpg1 = page_of(k0 + 2 * kStride + 16 * t);
     }

@@ -11,7 +11,7 @@ namespace kv {
 // through the workspace.
 constexpr int kWarpTokens = 64, kMaxCluster = 8;
 constexpr int64_t kSms = 152;
-constexpr int blocks_per_sm(int64_t dim, int rows) { return dim == 128 ? (rows == 8 ? 3 : 2) : (rows == 8 ? 4 : 3); }
+constexpr int blocks_per_sm(int64_t dim, int rows) { return dim == 128 ? (rows == 8 ? 4 : 2) : (rows == 8 ? 5 : 4); }
 // Many rows (kv_attention_tile.cu): rows of a block, one to an SM, and the keys that it takes at a time.
 constexpr int kTileRows = 256, kTileKeys = 128;
 
