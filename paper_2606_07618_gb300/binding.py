@@ -572,20 +572,20 @@ _pack_cache = struct.Struct("4PqiiiP").pack                      # the last word
 
 def _cache(c):
     """(codes [pages, heads, 2, page, dim/2], sf [pages, heads, 2, dim/16, page], S_k, S_v) as the bytes of an
-    nvfp4_kv_cache, its heads, dim and page."""
+    nvfp4_kv_cache, its heads and dim."""
     codes, sf, S_k, S_v = c
     pages, heads, two, page, half = codes.shape
-    dim = 2 * half
-    if two != 2 or sf.shape != (pages, heads, 2, dim // 16, page):
+    if two != 2 or sf.shape != (pages, heads, 2, half >> 3, page):
         raise ValueError(f"cache: codes {tuple(codes.shape)} and scales {tuple(sf.shape)} do not belong together")
-    if not (codes.itemsize == sf.itemsize == 1):
+    if not (codes.dtype is sf.dtype is _U8 or codes.itemsize == sf.itemsize == 1):
         raise TypeError(f"cache: codes and scales in bytes are wanted, not {codes.dtype} and {sf.dtype}")
     if not (codes.is_contiguous() and sf.is_contiguous()):
         raise ValueError("cache: contiguous codes and scales are wanted")
-    for S in (S_k, S_v):
-        if S.dtype is not _F32 or S.numel() != 1:
-            raise TypeError(f"cache: one float32 as S is wanted, not {tuple(S.shape)} of {S.dtype}")
-    return _pack_cache(codes.data_ptr(), sf.data_ptr(), S_k.data_ptr(), S_v.data_ptr(), pages, page, heads, dim, 0), heads, dim, page
+    if not (S_k.dtype is S_v.dtype is _F32 and S_k.numel() == S_v.numel() == 1):
+        raise TypeError(f"cache: one float32 as S is wanted, not {tuple(S_k.shape)} of {S_k.dtype} and {tuple(S_v.shape)} of "
+                        f"{S_v.dtype}")
+    dim = 2 * half
+    return _pack_cache(codes.data_ptr(), sf.data_ptr(), S_k.data_ptr(), S_v.data_ptr(), pages, page, heads, dim, 0), heads, dim
 
 
 def _heads3(t, what: str):
@@ -593,13 +593,15 @@ def _heads3(t, what: str):
     if t.dim() != 3:
         raise ValueError(f"{what}: [tokens, heads, dim] is wanted, not {tuple(t.shape)}")
     token, head, one = t.stride()
+    if t.is_contiguous() and token and head:
+        return t.data_ptr(), token, head
     tokens, heads, dim = t.shape
     if one != 1 and dim > 1:
         raise ValueError(f"{what}: a contiguous innermost dimension is wanted")
-    if tokens <= 1:
-        token = max(token, heads * head, dim)
     if heads <= 1:
         head = max(head, dim)
+    if tokens <= 1:
+        token = max(token, heads * head, dim)
     return t.data_ptr(), token, head
 
 
@@ -607,7 +609,7 @@ def _list(t, n: int, dtype, what: str):
     """Pointer of n contiguous numbers of a type, on the device."""
     if t.dtype is not dtype:
         raise TypeError(f"{what}: {dtype} is wanted, not {t.dtype}")
-    if t.dim() != 1 or t.numel() < n or (t.numel() > 1 and t.stride(0) != 1):
+    if t.numel() < n or t.dim() != 1 or not t.is_contiguous():
         raise ValueError(f"{what}: {n} contiguous numbers are wanted, not {tuple(t.shape)}")
     return t.data_ptr()
 
@@ -616,9 +618,13 @@ def _pages(t, what: str):
     """Pointer, row stride, rows and width of a page table."""
     if t.dtype is not _I32:
         raise TypeError(f"{what}: {_I32} is wanted, not {t.dtype}")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: [sequences, pages] with contiguous rows is wanted, not {tuple(t.shape)}")
+    if t.dim() != 2:
+        raise ValueError(f"{what}: [sequences, pages] is wanted, not {tuple(t.shape)}")
     rows, width = t.shape
+    if t.is_contiguous():
+        return t.data_ptr(), width, rows, width
+    if width > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: contiguous rows are wanted")
     return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), width), rows, width
 
 
@@ -642,42 +648,36 @@ def nvfp4_rope(x, positions, turns, out=None, magnitude: float = 1.0, layout: in
         raise TypeError(f"out: {x.dtype} is wanted, not {out.dtype}")
     if out.shape != x.shape:
         raise ValueError(f"out: shape {tuple(x.shape)} is wanted, not {tuple(out.shape)}")
-    px, xt, xh = _heads3(x, "x")
-    po, ot, oh = _heads3(out, "out")
     tokens, heads, dim = x.shape
-    rot = 2 * turns.numel()
-    rc = (_lib or lib()).nvfp4_rope(px, xt, xh, po, ot, oh, _dtype(x), tokens, heads, dim, rot,
-                                    _list(positions, tokens, _I64, "positions"), _list(turns, rot // 2, _I64, "turns"),
-                                    magnitude, layout, 1 if inverse else 0, _stream(stream))
+    pairs = turns.numel()
+    rc = (_lib or lib()).nvfp4_rope(*_heads3(x, "x"), *_heads3(out, "out"), _dtype(x), tokens, heads, dim, 2 * pairs,
+                                    _list(positions, tokens, _I64, "positions"), _list(turns, pairs, _I64, "turns"), magnitude,
+                                    layout, 1 if inverse else 0, _stream(stream))
     _check("nvfp4_rope", rc)
     return out
 
 
-def _kv_pair(k, v, tokens, heads: int, dim: int, what: str):
-    """Pointers and strides of k and v (either None), their dtype code and rows."""
-    args, dt = [], None
-    for t, name in ((k, "k"), (v, "v")):
-        if t is None:
-            args += (None, 0, 0)
-            continue
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
-            raise ValueError(f"{name}: [tokens, {heads}, {dim}] is wanted, not {tuple(t.shape)}")
-        if tokens is None:
-            tokens, dt = t.shape[0], t.dtype
-        if t.shape[0] != tokens or t.dtype is not dt:
-            raise ValueError(f"{what}: k and v of one type and as many tokens are wanted")
-        args += _heads3(t, name)
-    if dt is None:
-        raise ValueError(f"{what}: k or v is wanted")
-    return args, NVFP4_IN_BF16 if dt is _BF16 else _dtype(k if k is not None else v), tokens
+def _kv_pair(k, v, heads: int, dim: int):
+    """Pointers and strides of k and v (either None), their dtype code and tokens."""
+    x = k if v is None else v
+    if x is None:
+        raise ValueError("k or v is wanted")
+    shape = x.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
+        raise ValueError(f"k, v: [tokens, {heads}, {dim}] is wanted, not {tuple(shape)}")
+    if x is not k and k is not None and (k.shape != shape or k.dtype is not x.dtype):
+        raise ValueError(f"k and v of one type and shape are wanted, not {tuple(k.shape)} and {tuple(shape)}")
+    a = (None, 0, 0) if k is None else _heads3(k, "k")
+    b = (None, 0, 0) if v is None else _heads3(v, "v")
+    return a, b, _dtype(x), shape[0]
 
 
 def nvfp4_kv_write(cache, k, v, slots, method: int = NVFP4_KV_SWEEP, status=None, stream=None):
     """Quantises k and v [tokens, heads, dim] (bf16 or fp32, either None) into the cache at slots [tokens] (page * size +
     offset; negative: skipped)."""
-    c, heads, dim, _ = _cache(cache)
-    args, dt, tokens = _kv_pair(k, v, None, heads, dim, "nvfp4_kv_write")
-    rc = (_lib or lib()).nvfp4_kv_write(c, *args, dt, tokens, _list(slots, tokens, _I64, "slots"), method, _status(status),
+    c, heads, dim = _cache(cache)
+    pk, pv, dt, tokens = _kv_pair(k, v, heads, dim)
+    rc = (_lib or lib()).nvfp4_kv_write(c, *pk, *pv, dt, tokens, _list(slots, tokens, _I64, "slots"), method, _status(status),
                                         _stream(stream))
     _check("nvfp4_kv_write", rc)
 
@@ -685,28 +685,31 @@ def nvfp4_kv_write(cache, k, v, slots, method: int = NVFP4_KV_SWEEP, status=None
 def nvfp4_kv_read(cache, table, starts, offsets, k=None, v=None, status=None, stream=None):
     """Rows offsets[b] .. offsets[b+1] of k and v [tokens, heads, dim] (bf16 or fp32, either None) = tokens starts[b] .. of
     sequence b (starts None: from 0)."""
-    c, heads, dim, _ = _cache(cache)
-    args, dt, tokens = _kv_pair(k, v, None, heads, dim, "nvfp4_kv_read")
+    c, heads, dim = _cache(cache)
+    pk, pv, dt, tokens = _kv_pair(k, v, heads, dim)
     pt, ld, batch, width = _pages(table, "table")
     rc = (_lib or lib()).nvfp4_kv_read(c, pt, ld, width, None if starts is None else _list(starts, batch, _I32, "starts"),
-                                       _list(offsets, batch + 1, _I32, "offsets"), batch, *args, dt, tokens, _status(status),
+                                       _list(offsets, batch + 1, _I32, "offsets"), batch, *pk, *pv, dt, tokens, _status(status),
                                        _stream(stream))
     _check("nvfp4_kv_read", rc)
 
 
 def nvfp4_kv_attention_workspace(cache, q, batch: int, width: int, max_q: int, prefix_width: int = 0) -> int:
     """Bytes of workspace of attention for queries q [tokens, q_heads, dim] and page tables of these widths."""
-    return (_lib or lib()).nvfp4_kv_attention_workspace(_cache(cache)[0], q.shape[0], q.shape[1], batch, width, max_q,
-                                                        prefix_width)
+    pages, heads, _, page, half = cache[0].shape
+    tokens, q_heads, _ = q.shape
+    return (_lib or lib()).nvfp4_kv_attention_workspace(_pack_cache(0, 0, 0, 0, pages, page, heads, 2 * half, 0), tokens, q_heads,
+                                                        batch, width, max_q, prefix_width)
 
 
 def _attention(fn: str, q, cache, prefix, table, lens, offsets, max_q, scale, out, causal, lse, workspace, status, stream):
-    c, heads, dim, _ = _cache(cache)
-    if q.dtype is not _BF16 or out.dtype is not _BF16:
+    c, heads, dim = _cache(cache)
+    if not q.dtype is out.dtype is _BF16:
         raise TypeError(f"{fn}: queries and results in bfloat16 are wanted, not {q.dtype} and {out.dtype}")
-    if q.dim() != 3 or q.shape[2] != dim or q.shape != out.shape:
-        raise ValueError(f"{fn}: q and out of [tokens, heads, {dim}] are wanted, not {tuple(q.shape)} and {tuple(out.shape)}")
-    tokens, q_heads, _ = q.shape
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != dim or out.shape != shape:
+        raise ValueError(f"{fn}: q and out of [tokens, heads, {dim}] are wanted, not {tuple(shape)} and {tuple(out.shape)}")
+    tokens, q_heads, _ = shape
     if q_heads < 1 or q_heads % heads:
         raise ValueError(f"{fn}: a multiple of {heads} query heads is wanted, not {q_heads}")
     if lse is not None:
@@ -714,12 +717,15 @@ def _attention(fn: str, q, cache, prefix, table, lens, offsets, max_q, scale, ou
             raise TypeError(f"lse: {_F32} is wanted, not {lse.dtype}")
         if lse.shape != (tokens, q_heads) or not lse.is_contiguous():
             raise ValueError(f"lse: contiguous, of shape {(tokens, q_heads)}, is wanted")
+        lse = lse.data_ptr()
+    if workspace is None:
+        ws, ws_bytes = None, 0
+    else:
+        ws, ws_bytes = _buffer(workspace, 0, "workspace"), workspace.nbytes
     pt, ld, batch, width = _pages(table, "table")
     rc = getattr(_lib or lib(), fn)(c, *_heads3(q, "q"), tokens, q_heads, *prefix, pt, ld, width, _list(lens, batch, _I32, "lens"),
                                     _list(offsets, batch + 1, _I32, "offsets"), batch, max_q, scale, 1 if causal else 0,
-                                    *_heads3(out, "out"), None if lse is None else lse.data_ptr(), _status(status),
-                                    _buffer(workspace, 0, "workspace"), workspace.nbytes if workspace is not None else 0,
-                                    _stream(stream))
+                                    *_heads3(out, "out"), lse, _status(status), ws, ws_bytes, _stream(stream))
     _check(fn, rc)
 
 

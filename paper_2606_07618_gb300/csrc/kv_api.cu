@@ -65,9 +65,10 @@ nvfp4_status check_tensor(const void* p, int64_t token, int64_t head, int64_t to
     if (tokens > 1 && token < across + dim && !(token >= dim && head >= all + dim)) return NVFP4_ERR_INVALID_ARG;
     if (across > kMaxBytes / 8 || all > kMaxBytes / 8) return NVFP4_ERR_RANGE;
     if (!aligned(p, (uintptr_t)esize)) return NVFP4_ERR_ALIGNMENT;
-    const int64_t step = 16 / esize;
-    x->t = kv::Tensor{const_cast<void*>(p), token, head,
-                      aligned(p, 16) && (token % step == 0 || tokens == 1) && (head % step == 0 || heads == 1)};
+    const auto whole = [&](int64_t n) {
+        return aligned(p, (uintptr_t)n) && (token % (n / esize) == 0 || tokens == 1) && (head % (n / esize) == 0 || heads == 1);
+    };
+    x->t = kv::Tensor{const_cast<void*>(p), token, head, whole(32) ? 2 : whole(16) ? 1 : 0};
     x->tokens = tokens;
     x->heads = heads;
     x->dim = dim;

@@ -11,25 +11,34 @@ namespace nvfp4 {
 namespace kv {
 namespace {
 
-// Place of a token's block in the pool: page, offset in it.
+// A column's block in the pool: byte offsets of page 0's token 0, and of a page.
 struct Place {
-    int64_t page;
-    int at;
+    uint8_t *codes, *sf;
+    int64_t page_codes, page_sf;
+    int row;                             // bytes of a token's codes
+    __device__ __forceinline__ Place(const Cache& c, int head, int part, int block) {
+        const int64_t at = (int64_t)(head * 2 + part) << c.page_log2;
+        row = c.dim / 2;
+        codes = c.codes + at * row + block * 8;
+        sf = c.sf + at * (c.dim / 16) + ((int64_t)block << c.page_log2);
+        page_sf = (int64_t)(c.heads * 2) * (c.dim / 16) << c.page_log2;
+        page_codes = 8 * page_sf;
+    }
+    __device__ __forceinline__ uint2* codes_of(int64_t page, int at) const {
+        return reinterpret_cast<uint2*>(codes + page * page_codes + at * row);
+    }
+    __device__ __forceinline__ uint8_t* sf_of(int64_t page, int at) const { return sf + page * page_sf + at; }
 };
-__device__ __forceinline__ int64_t row_of(const Cache& c, int64_t page, int head, int part) {
-    return (page * c.heads + head) * 2 + part;
-}
-__device__ __forceinline__ uint8_t* codes_at(const Cache& c, const Place& w, int head, int part, int block) {
-    return c.codes + ((row_of(c, w.page, head, part) << c.page_log2) + w.at) * (c.dim / 2) + block * 8;
-}
-__device__ __forceinline__ uint8_t* sf_at(const Cache& c, const Place& w, int head, int part, int block) {
-    return c.sf + ((row_of(c, w.page, head, part) * (c.dim / 16) + block) << c.page_log2) + w.at;
-}
 
 template <int DT>
 __device__ __forceinline__ void load_block(const Tensor& t, int64_t e, Raw& r) {
-    if (t.vec) {
-        const char* p = static_cast<const char*>(t.p) + e * (DT == 0 ? 2 : 4);
+    const char* p = static_cast<const char*>(t.p) + e * (DT == 0 ? 2 : 4);
+    if (t.vec == 2) {
+        ld_stream32<false>(p, r.a, r.b);
+        if (DT != 0) ld_stream32<false>(p + 32, r.c, r.d);
+        return;
+    }
+    if (t.vec == 1) {
         r.a = ld_stream16<false>(p);
         r.b = ld_stream16<false>(p + 16);
         if (DT != 0) {
@@ -54,65 +63,76 @@ __device__ __forceinline__ void load_block(const Tensor& t, int64_t e, Raw& r) {
     r.b = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
-// One warp's work: tokens 8 i .. 8 i + 7, blocks 4 j .. of a head of k or v.
-struct Item {
-    int64_t token;
+// A warp's column: four blocks of a head of k or v, of which it takes groups of 8 tokens, `step` groups apart.
+struct Column {
     int head, part, block;
+    int64_t group, step;
 };
-__device__ __forceinline__ Item item_of(int64_t w, int heads, int quads, int parts, int lane) {
-    const uint32_t per = (uint32_t)(heads * quads * parts);
-    const int64_t group = w / per;
-    uint32_t r = (uint32_t)(w - group * per);
-    Item it;
-    it.block = (int)(r % quads) * 4 + (lane & 3);
+struct Grid {
+    int columns;                         // of all heads and parts
+    int64_t groups, step;
+};
+__device__ __forceinline__ Column column_of(const Grid& grid, int heads, int quads, int lane) {
+    const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    Column c;
+    c.group = w / grid.columns;
+    int r = (int)(w - c.group * grid.columns);
+    c.block = r % quads * 4 + (lane & 3);
     r /= quads;
-    it.head = (int)(r % heads);
-    it.part = (int)(r / heads);
-    it.token = group * 8 + (lane >> 2);
-    return it;
+    c.head = r % heads;
+    c.part = r / heads;
+    c.step = grid.step;
+    if (c.group >= grid.step) c.group = grid.groups;            // warps that fill up the last block
+    return c;
 }
 
 template <int DT, int METHOD>
-__global__ void __launch_bounds__(256, METHOD == 0 ? 2 : 4) write_kernel(Write p, int64_t items) {
+__global__ void __launch_bounds__(256, METHOD == 0 ? 2 : DT == 0 ? 4 : 3) write_kernel(Write p, Grid grid) {
     __shared__ Cand tab[kTabN];
     grid_launch_dependents();
     build_table(tab);
     __syncthreads();
     grid_dependency_wait();
     const int lane = threadIdx.x & 31;
-    const int quads = p.c.dim / 64, only = p.in[0].p ? 0 : 1, parts = p.in[0].p && p.in[1].p ? 2 : 1;
-    float E[2];
-    bool usable[2];
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const float S = p.in[i].p ? ld_f32(i ? p.c.S_v : p.c.S_k) : 1.0f;
-        E[i] = __frcp_rn(S);
-        usable[i] = S > 0.0f && isfinite(S) && isfinite(E[i]);
-        if (!usable[i]) E[i] = 1.0f;
-    }
-    const int64_t slots = p.c.pages << p.c.page_log2;
+    const Column col = column_of(grid, p.c.heads, p.c.dim / 64, lane);
+    const int part = p.in[0].p ? col.part : 1;
+    const Tensor in = part ? p.in[1] : p.in[0];
+    const Place place(p.c, col.head, part, col.block);
+    const float S = ld_f32(part ? p.c.S_v : p.c.S_k);
+    float E = __frcp_rn(S);
+    const bool usable = S > 0.0f && isfinite(S) && isfinite(E);
+    if (!usable) E = 1.0f;
+    const u64 E2 = pack2(E, E);
+    const int64_t slots = p.c.pages << p.c.page_log2, from = (int64_t)col.head * in.head + col.block * 16;
     bool bad = false, outside = false;
-    for (int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); w < items; w += (int64_t)gridDim.x * 8) {
-        const Item it = item_of(w, p.c.heads, quads, parts, lane);
-        const int part = it.part + only;
-        bool valid = it.token < p.tokens;
-        int64_t slot = valid ? p.slots[it.token] : -1;
-        if (slot >= slots) outside = true;
-        valid = slot >= 0 && slot < slots;
+    // the next group's place and elements are on their way while this one is quantised
+    Raw next;
+    int64_t next_slot = -1;
+    auto fetch = [&](int64_t group) {
+        const int64_t token = group * 8 + (lane >> 2);
+        next_slot = -1;
+        if (group < grid.groups && token < p.tokens) {
+            next_slot = p.slots[token];
+            load_block<DT>(in, token * in.token + from, next);
+        }
+    };
+    fetch(col.group);
+    for (int64_t group = col.group; group < grid.groups; group += col.step) {
+        const int64_t slot = next_slot;
+        Raw raw = next;
+        fetch(group + col.step);
+        outside |= slot >= slots;
+        const bool valid = slot >= 0 && slot < slots;
         u64 y2[8];
         float m = 0.0f, ma = 0.0f, mb = 0.0f;
         if (valid) {
-            Raw raw;
-            const Tensor& t = p.in[part];
-            load_block<DT>(t, it.token * t.token + it.head * t.head + it.block * 16, raw);
-            const u64 E2 = part ? pack2(E[1], E[1]) : pack2(E[0], E[0]);
             m = METHOD == 0 ? raw_to_y_halves<DT>(raw, E2, y2, ma, mb) : raw_to_y<DT>(raw, E2, y2);
             bad |= !(m < __int_as_float(0x7f800000));
         } else {
 #pragma unroll
             for (int j = 0; j < 8; j++) y2[j] = 0ull;
         }
-        const bool zero = zero_block(usable[part], m);
+        const bool zero = zero_block(usable, m);
         int code;
         if (METHOD == 0) {
             const int I0 = e4m3_floor_code_of_sixth(m);
@@ -144,9 +164,10 @@ __global__ void __launch_bounds__(256, METHOD == 0 ? 2 : 4) write_kernel(Write p
                                    mul2(y2[4 * h + 3], r2));
         }
         if (valid) {
-            const Place at{slot >> p.c.page_log2, (int)(slot & ((1 << p.c.page_log2) - 1))};
-            *reinterpret_cast<uint2*>(codes_at(p.c, at, it.head, part, it.block)) = make_uint2(packed[0], packed[1]);
-            *sf_at(p.c, at, it.head, part, it.block) = (uint8_t)code;
+            const int64_t page = slot >> p.c.page_log2;
+            const int at = (int)(slot & ((1 << p.c.page_log2) - 1));
+            *place.codes_of(page, at) = make_uint2(packed[0], packed[1]);
+            *place.sf_of(page, at) = (uint8_t)code;
         }
     }
     if (p.status) {
@@ -156,58 +177,87 @@ __global__ void __launch_bounds__(256, METHOD == 0 ? 2 : 4) write_kernel(Write p
 }
 
 // Sequence of row r: the last b with offsets[b] <= r; batch where r is behind the last one.
-__device__ __forceinline__ int64_t sequence_of(const int32_t* offsets, int64_t batch, int64_t r) {
-    int64_t lo = 0, hi = batch + 1;
+__device__ __forceinline__ int sequence_of(const int32_t* offsets, int batch, int r) {
+    unsigned lo = 0, hi = (unsigned)batch + 1;
     while (hi > lo) {
-        const int64_t mid = (lo + hi) >> 1;
+        const unsigned mid = (lo + hi) >> 1;
         if (offsets[mid] > r) hi = mid;
         else lo = mid + 1;
     }
-    return lo - 1;
+    return (int)lo - 1;
 }
 
+// kGroups of a warp's groups at a time, their loads side by side.
+constexpr int kGroups = 4;
+
 template <int DT>
-__global__ void __launch_bounds__(256) read_kernel(Read p, int64_t items) {
+__global__ void __launch_bounds__(256) read_kernel(Read p, Grid grid) {
     grid_launch_dependents();
     grid_dependency_wait();
     const int lane = threadIdx.x & 31;
-    const int quads = p.c.dim / 64, only = p.out[0].p ? 0 : 1, parts = p.out[0].p && p.out[1].p ? 2 : 1;
+    const Column col = column_of(grid, p.c.heads, p.c.dim / 64, lane);
+    const int part = p.out[0].p ? col.part : 1;
+    const Tensor t = part ? p.out[1] : p.out[0];
+    const Place place(p.c, col.head, part, col.block);
+    const float S = ld_f32(part ? p.c.S_v : p.c.S_k);
+    const int64_t from = (int64_t)col.head * t.head + col.block * 16;
+    const int page_log2 = p.c.page_log2, page_mask = (1 << page_log2) - 1;
     bool outside = false;
-    for (int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); w < items; w += (int64_t)gridDim.x * 8) {
-        const Item it = item_of(w, p.c.heads, quads, parts, lane);
-        const int part = it.part + only;
-        if (it.token >= p.tokens) continue;
-        const int64_t b = sequence_of(p.offsets, p.batch, it.token);
-        if (b < 0 || b >= p.batch) continue;
-        const int64_t j = (p.starts ? p.starts[b] : 0) + (it.token - p.offsets[b]);
-        int64_t page = -1;
-        if (j >= 0 && (j >> p.c.page_log2) < p.width) page = p.table[b * p.table_ld + (j >> p.c.page_log2)];
-        const bool ok = page >= 0 && page < p.c.pages;
-        outside |= !ok;
-        uint2 q = make_uint2(0, 0);
-        uint32_t sf = 0;
-        if (ok) {
-            const Place at{page, (int)(j & ((1 << p.c.page_log2) - 1))};
-            q = *reinterpret_cast<const uint2*>(codes_at(p.c, at, it.head, part, it.block));
-            sf = *sf_at(p.c, at, it.head, part, it.block);
+    int b = -1, first = 0, past = 0, start = 0;                  // the last sequence found, its rows and first token
+    for (int64_t group = col.group; group < grid.groups; group += kGroups * col.step) {
+        int token[kGroups], page[kGroups], at[kGroups];          // tokens, pages and what they count fit 31 bits
+#pragma unroll
+        for (int k = 0; k < kGroups; k++) {
+            const int64_t row = (group + k * col.step) * 8 + (lane >> 2);
+            token[k] = group + k * col.step < grid.groups && row < p.tokens ? (int)row : -1;
+            page[k] = -1, at[k] = 0;
+            if (token[k] < 0) continue;
+            if (token[k] < first || token[k] >= past) {
+                b = sequence_of(p.offsets, (int)p.batch, token[k]);
+                const bool in = b >= 0 && b < p.batch;
+                first = in ? p.offsets[b] : 0, past = in ? p.offsets[b + 1] : 0;
+                if (!in) {
+                    token[k] = -1;                               // behind the last sequence
+                    continue;
+                }
+                start = p.starts ? p.starts[b] : 0;
+            }
+            const int64_t j = (int64_t)start + (token[k] - first);
+            if (j >= 0 && (j >> page_log2) < p.width) page[k] = p.table[b * p.table_ld + (j >> page_log2)];
+            at[k] = (int)j & page_mask;
         }
-        const float s = f16bits_to_f32(e4m3_to_f16bits(sf)), S = ld_f32(part ? p.c.S_v : p.c.S_k);
+        uint2 codes[kGroups];
+        uint32_t scale[kGroups];
+        bool there[kGroups];
+#pragma unroll
+        for (int k = 0; k < kGroups; k++) {
+            there[k] = page[k] >= 0 && page[k] < p.c.pages;
+            outside |= token[k] >= 0 && !there[k];
+            codes[k] = make_uint2(0, 0), scale[k] = 0;
+            if (there[k]) {
+                codes[k] = *place.codes_of(page[k], at[k]);
+                scale[k] = *place.sf_of(page[k], at[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kGroups; k++) {
+        if (token[k] < 0) continue;
+        const uint16_t s = e4m3_to_f16bits(scale[k]);
         float v[16];
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            uint32_t h;
-            const uint16_t byte = (uint16_t)(((i < 4 ? q.x : q.y) >> (8 * (i & 3))) & 0xFF);
-            asm("{\n\t.reg .b8 lo, hi;\n\tmov.b16 {lo, hi}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, lo;\n\t}" : "=r"(h) : "h"(byte));
             // q s is exact, q s S is rounded once
-            v[2 * i] = __fmul_rn(__fmul_rn(f16bits_to_f32((uint16_t)h), s), S);
-            v[2 * i + 1] = __fmul_rn(__fmul_rn(f16bits_to_f32((uint16_t)(h >> 16)), s), S);
+            const uint16_t byte = (uint16_t)(((i < 4 ? codes[k].x : codes[k].y) >> (8 * (i & 3))) & 0xFF);
+            asm("{\n\t.reg .b8 lo, hi;\n\t.reg .b32 h;\n\t.reg .b16 a, b;\n\tmov.b16 {lo, hi}, %2;\n\tcvt.rn.f16x2.e2m1x2 h, lo;\n\t"
+                "mov.b32 {a, b}, h;\n\tfma.rn.f32.f16 %0, a, %3, %4;\n\tfma.rn.f32.f16 %1, b, %3, %4;\n\t}"
+                : "=f"(v[2 * i]), "=f"(v[2 * i + 1]) : "h"(byte), "h"(s), "f"(-0.0f));
+            unpack2(mul2(pack2(v[2 * i], v[2 * i + 1]), pack2(S, S)), v[2 * i], v[2 * i + 1]);
         }
-        if (!ok) {
+        if (!there[k]) {
 #pragma unroll
             for (int i = 0; i < 16; i++) v[i] = 0.0f;
         }
-        const Tensor& t = p.out[part];
-        const int64_t e = it.token * t.token + it.head * t.head + it.block * 16;
+        const int64_t e = token[k] * t.token + from;
         uint32_t o[16];
 #pragma unroll
         for (int i = 0; i < 16; i++) o[i] = __float_as_uint(v[i]);
@@ -217,7 +267,13 @@ __global__ void __launch_bounds__(256) read_kernel(Read p, int64_t items) {
                 asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
         }
         constexpr int N = DT == 0 ? 8 : 16;                      // words
-        if (t.vec) {
+        if (t.vec == 2) {                                        // a sector at a time
+            char* d = static_cast<char*>(t.p) + e * (DT == 0 ? 2 : 4);
+#pragma unroll
+            for (int i = 0; i < N; i += 8)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(d + 4 * i), "r"(o[i]), "r"(o[i + 1]),
+                             "r"(o[i + 2]), "r"(o[i + 3]), "r"(o[i + 4]), "r"(o[i + 5]), "r"(o[i + 6]), "r"(o[i + 7]) : "memory");
+        } else if (t.vec == 1) {
             uint4* d = reinterpret_cast<uint4*>(static_cast<char*>(t.p) + e * (DT == 0 ? 2 : 4));
 #pragma unroll
             for (int i = 0; i < N / 4; i++) d[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
@@ -230,34 +286,41 @@ __global__ void __launch_bounds__(256) read_kernel(Read p, int64_t items) {
 #pragma unroll
             for (int i = 0; i < 16; i++) d[i] = o[i];
         }
+        }
     }
     if (p.status && __any_sync(0xffffffffu, outside) && lane == 0) atomicOr(p.status, kStatusBounds);
 }
 
-int64_t warps(int64_t tokens, const Cache& c, const Tensor (&t)[2]) {
-    return (tokens + 7) / 8 * c.heads * (c.dim / 64) * ((t[0].p != nullptr) + (t[1].p != nullptr));
+// Columns of all heads and parts, and as many warps to each as fill the GPU (at most one a group of tokens).
+Grid make_grid(int64_t tokens, const Cache& c, const Tensor (&t)[2], int64_t warps, int64_t* blocks) {
+    Grid g;
+    g.columns = c.heads * (c.dim / 64) * ((t[0].p != nullptr) + (t[1].p != nullptr));
+    g.groups = (tokens + 7) / 8;
+    g.step = warps / g.columns;
+    g.step = g.step < 1 ? 1 : g.step < g.groups ? g.step : g.groups;
+    *blocks = (g.step * g.columns + 7) / 8;
+    return g;
 }
 
 template <int DT, int METHOD>
-cudaError_t launch_write_one(const Write& p, int64_t items, int sms, cudaStream_t s) {
+cudaError_t launch_write_one(const Write& p, int sms, cudaStream_t s) {
     static std::atomic<int> occ[kOccDevices];
-    const int64_t cap = (int64_t)sms * occupancy_per_sm(occ, write_kernel<DT, METHOD>, 256), need = (items + 7) / 8;
-    return launch_dependent(write_kernel<DT, METHOD>, need < cap ? need : cap, 256, s, p, items);
+    int64_t blocks;
+    const Grid g = make_grid(p.tokens, p.c, p.in, (int64_t)sms * 8 * occupancy_per_sm(occ, write_kernel<DT, METHOD>, 256), &blocks);
+    return launch_dependent(write_kernel<DT, METHOD>, blocks, 256, s, p, g);
 }
 
 }  // namespace
 
 cudaError_t launch_write(const Write& p, int sms, cudaStream_t s) {
-    const int64_t items = warps(p.tokens, p.c, p.in);
-    if (p.dtype == 0) return p.method == 0 ? launch_write_one<0, 0>(p, items, sms, s) : launch_write_one<0, 1>(p, items, sms, s);
-    return p.method == 0 ? launch_write_one<1, 0>(p, items, sms, s) : launch_write_one<1, 1>(p, items, sms, s);
+    if (p.dtype == 0) return p.method == 0 ? launch_write_one<0, 0>(p, sms, s) : launch_write_one<0, 1>(p, sms, s);
+    return p.method == 0 ? launch_write_one<1, 0>(p, sms, s) : launch_write_one<1, 1>(p, sms, s);
 }
 
 cudaError_t launch_read(const Read& p, int sms, cudaStream_t s) {
-    const int64_t items = warps(p.tokens, p.c, p.out), need = (items + 7) / 8, cap = (int64_t)sms * 8;
-    const int64_t grid = need < cap ? need : cap;
-    return p.dtype == 0 ? launch_dependent(read_kernel<0>, grid, 256, s, p, items)
-                        : launch_dependent(read_kernel<1>, grid, 256, s, p, items);
+    int64_t blocks;
+    const Grid g = make_grid(p.tokens, p.c, p.out, (int64_t)sms * 8 * 6, &blocks);
+    return p.dtype == 0 ? launch_dependent(read_kernel<0>, blocks, 256, s, p, g) : launch_dependent(read_kernel<1>, blocks, 256, s, p, g);
 }
 
 }  // namespace kv

@@ -19,7 +19,7 @@ struct Cache {
     int page_log2, heads, dim;
 };
 
-// Strided tensor [tokens, heads, dim]; vec: base and strides are multiples of 16 bytes.
+// Strided tensor [tokens, heads, dim]; vec: base and strides are multiples of 16 bytes (1) or 32 (2).
 struct Tensor {
     void* p;
     int64_t token, head;

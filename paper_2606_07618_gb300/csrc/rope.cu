@@ -5,9 +5,9 @@
 // as a signed number of 2^-31 half-turns go to sincospif.  The conversion to fp32 rounds by up to 2^-25
 // of the angle's half-turns, the same order as the function's own error.
 //
-// A thread owns one unit of a head -- V pairs, 16 bytes of each of the pair's halves or 32
-// neighbouring bytes -- in up to four heads of one token: its V sines serve all of them, and their
-// loads are all in flight before the first is used.
+// A block takes a few tokens: its threads compute the sines of each pair once, into shared memory, while
+// the elements are on their way.  A thread owns one unit of a head -- V pairs, in two pieces of 16 bytes, either one
+// in each half of the pairs or of whole pairs, so that neighbouring threads' pieces are neighbours -- in up to kHeads heads.
 #include "kv_kernels.h"
 #include "nvfp4_device.cuh"
 
@@ -15,7 +15,7 @@ namespace nvfp4 {
 namespace kv {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kHeads = 2;
 
 // V elements of type DT: one 16-byte access, or single elements (V = 1).
 template <int DT, int V>
@@ -68,39 +68,60 @@ __device__ __forceinline__ void pack(const float (&v)[V], Words<DT, V>& r) {
 // Block (units of a head, heads, tokens); heads y, y + hl, ... of a thread.
 template <int DT, int V, int HALVES>
 __global__ void __launch_bounds__(kThreads) rope_kernel(Rope p, int hl, int copy) {
+    extern __shared__ float2 s_turn[];                           // [tokens][rot / 2]: magnitude times cosine and sine
     grid_launch_dependents();
     grid_dependency_wait();
-    const int64_t token = (int64_t)blockIdx.x * blockDim.z + threadIdx.z;
+    const int64_t token0 = (int64_t)blockIdx.x * blockDim.z, token = token0 + threadIdx.z;
     const int y = blockIdx.y * blockDim.y + threadIdx.y;
-    if (token >= p.tokens || y >= hl) return;
-    const int units = p.rot / (2 * V);
-    for (int u = threadIdx.x; u < units + copy; u += blockDim.x) {
+    const bool mine = token < p.tokens && y < hl;
+    const int half = p.rot / 2, units = half / V;
+    constexpr bool kSplit = HALVES || V > 1;                     // else a unit is one pair of neighbours
+    const int64_t xt = token * p.x.token, ot = token * p.out.token;
+    Words<DT, V> xa[kHeads], xb[kHeads];
+    // where a unit's pieces begin
+    auto first = [&](int u) { return u >= units ? p.rot + (u - units) * V : kSplit ? u * V : 2 * u; };
+    auto second = [&](int u) { return u >= units ? p.rot + (u - units + copy) * V : kSplit ? u * V + half : 2 * u + 1; };
+    auto read = [&](int u) {
+#pragma unroll
+        for (int k = 0; k < kHeads; k++) {
+            const int h = y + k * hl;
+            if (h < p.heads) {
+                xa[k] = load<DT, V>(p.x.p, xt + h * p.x.head + first(u));
+                xb[k] = load<DT, V>(p.x.p, xt + h * p.x.head + second(u));
+            }
+        }
+    };
+    int u = threadIdx.x;
+    const int last = units + copy;
+    if (mine && u < last) read(u);
+    const int tid = threadIdx.x + blockDim.x * (threadIdx.y + blockDim.y * threadIdx.z);
+    const int threads = blockDim.x * blockDim.y * blockDim.z;
+    for (int x = tid; x < half * (int)blockDim.z; x += threads) {
+        const int z = x / half;
+        if (token0 + z < p.tokens) {
+            const int hi = (int)(((uint64_t)p.positions[token0 + z] * p.turns[x - z * half]) >> 32);
+            float s, c;
+            sincospif(__fmul_rn((float)hi, 4.656612873077393e-10f), &s, &c);                // 2^-31
+            s_turn[x] = make_float2(c * p.magnitude, s * (p.inverse ? -p.magnitude : p.magnitude));
+        }
+    }
+    __syncthreads();
+    if (!mine) return;
+    for (; u < last; u += blockDim.x) {
+        if (u != (int)threadIdx.x) read(u);
         const bool rotate = u < units;
         float c[V], s[V];
         if (rotate) {
-            const uint64_t pos = (uint64_t)p.positions[token];
 #pragma unroll
             for (int i = 0; i < V; i++) {
-                const int hi = (int)((pos * p.turns[u * V + i]) >> 32);
-                sincospif(__fmul_rn((float)hi, 4.656612873077393e-10f), &s[i], &c[i]);      // 2^-31
-                c[i] *= p.magnitude;
-                s[i] *= p.inverse ? -p.magnitude : p.magnitude;
-            }
-        }
-        // elements: the pair's first halves at a, its second at b
-        const int a = rotate && HALVES ? u * V : u * 2 * V, b = rotate && HALVES ? a + p.rot / 2 : a + V;
-        Words<DT, V> xa[4], xb[4];
-        const int64_t xt = token * p.x.token, ot = token * p.out.token;
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-            const int h = y + k * hl;
-            if (h < p.heads) {
-                xa[k] = load<DT, V>(p.x.p, xt + h * p.x.head + a);
-                xb[k] = load<DT, V>(p.x.p, xt + h * p.x.head + b);
+                // whole pairs: V / 2 in each piece
+                const int pair = HALVES || V == 1 ? u * V + i : (i < V / 2 ? first(u) : second(u) - V) / 2 + i;
+                const float2 f = s_turn[threadIdx.z * half + pair];
+                c[i] = f.x, s[i] = f.y;
             }
         }
 #pragma unroll
-        for (int k = 0; k < 4; k++) {
+        for (int k = 0; k < kHeads; k++) {
             const int h = y + k * hl;
             if (h >= p.heads) break;
             if (rotate) {
@@ -112,7 +133,6 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(Rope p, int hl, int copy
                         fa[i] = __fmaf_rn(va, c[i], -__fmul_rn(vb, s[i]));
                         fb[i] = __fmaf_rn(va, s[i], __fmul_rn(vb, c[i]));
                     } else {
-                        // pair i lies at elements 2i, 2i + 1 of the unit's 2V
                         const Words<DT, V>& w = 2 * i < V ? xa[k] : xb[k];
                         const float va = get(w, 2 * i % V), vb = get(w, (2 * i + 1) % V);
                         float* f = 2 * i < V ? fa : fb;
@@ -123,8 +143,8 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(Rope p, int hl, int copy
                 pack<DT, V>(fa, xa[k]);
                 pack<DT, V>(fb, xb[k]);
             }
-            store<DT, V>(p.out.p, ot + h * p.out.head + a, xa[k]);
-            store<DT, V>(p.out.p, ot + h * p.out.head + b, xb[k]);
+            store<DT, V>(p.out.p, ot + h * p.out.head + first(u), xa[k]);
+            store<DT, V>(p.out.p, ot + h * p.out.head + second(u), xb[k]);
         }
     }
 }
@@ -134,20 +154,22 @@ cudaError_t launch(const Rope& p, int sms, cudaStream_t s) {
     const bool in_place = p.x.p == p.out.p;
     const int copy = in_place ? 0 : (p.dim - p.rot) / (2 * V);
     const int units = p.rot / (2 * V) + copy;
-    // four heads to a thread where that still fills the GPU (its sines are a thread's larger part)
+    // several heads to a thread where that still fills the GPU
     const bool many = p.tokens * units * p.heads >= (int64_t)sms * 2048;
-    const int hl = many ? (p.heads + 3) / 4 : p.heads;
+    const int hl = many ? (p.heads + kHeads - 1) / kHeads : p.heads;
     dim3 block, grid;
     block.x = units < kThreads ? units : kThreads;
     block.y = kThreads / block.x < (unsigned)hl ? kThreads / block.x : hl;
     block.z = kThreads / (block.x * block.y);
     if (block.z > 64) block.z = 64;
     if (!many) block.z = 1;
+    const size_t smem = (size_t)block.z * (p.rot / 2) * sizeof(float2);      // at most 64 tokens of 2 or 1 of 512 pairs
     grid.x = (unsigned)((p.tokens + block.z - 1) / block.z);
     grid.y = (hl + block.y - 1) / block.y;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
