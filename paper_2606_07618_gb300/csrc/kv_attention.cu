@@ -543,15 +543,16 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
     }
 }
 
-// A row's parts joined: a warp for each row.
+// A row's parts joined: a block of four warps for each row, every fourth part to a warp.
+constexpr int kJoinWarps = 4;
 template <int D>
-__global__ void __launch_bounds__(256) join_kernel(Attention p) {
+__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(Attention p) {
+    __shared__ float s_o[kJoinWarps][D], s_sum[kJoinWarps];
     grid_launch_dependents();
     grid_dependency_wait();
-    const int lane = threadIdx.x & 31;
-    const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t at = blockIdx.x;
     const int64_t token = at / p.q_heads, h = at - token * p.q_heads;
-    if (token >= p.tokens) return;
     int64_t lo = 0, hi = p.batch + 1;
     while (hi > lo) {
         const int64_t mid = (lo + hi) >> 1;
@@ -582,7 +583,7 @@ __global__ void __launch_bounds__(256) join_kernel(Attention p) {
     const float* vals = static_cast<const float*>(p.workspace);
     const int64_t stride = p.tokens * p.q_heads, parts = own + shared;
     float top = neg_inf();
-    for (int64_t k = lane; k < parts; k += 32) {
+    for (int64_t k = lane; k < parts; k += 32) {                 // every warp looks at all of them
         const float2 v = ml[(k < own ? k : p.plan.own.parts + k - own) * stride + at];
         top = max_nan(top, v.x);
     }
@@ -593,7 +594,7 @@ __global__ void __launch_bounds__(256) join_kernel(Attention p) {
 #pragma unroll
     for (int k = 0; k < N; k++) o[k] = 0.0f;
 #pragma unroll 4
-    for (int64_t k = 0; k < parts; k++) {
+    for (int64_t k = warp; k < parts; k += kJoinWarps) {
         const int64_t x = (k < own ? k : p.plan.own.parts + k - own) * stride + at;
         const float2 v = ml[x];
         const float w = v.x == neg_inf() ? 0.0f : ex2(v.x - top);
@@ -608,6 +609,17 @@ __global__ void __launch_bounds__(256) join_kernel(Attention p) {
         }
 #pragma unroll
         for (int c = 0; c < N; c++) o[c] += q[c] * w;
+    }
+#pragma unroll
+    for (int c = 0; c < N; c++) s_o[warp][lane * N + c] = o[c];
+    if (lane == 0) s_sum[warp] = sum;
+    __syncthreads();
+    if (warp != 0) return;
+#pragma unroll
+    for (int k = 1; k < kJoinWarps; k++) {
+        sum += s_sum[k];
+#pragma unroll
+        for (int c = 0; c < N; c++) o[c] += s_o[k][lane * N + c];
     }
     const float f = top == neg_inf() ? 0.0f : ld_f32(p.c.S_v) / sum;
     uint16_t* out = static_cast<uint16_t*>(p.out.p) + token * p.out.token + h * p.out.head + lane * N;
@@ -666,7 +678,7 @@ cudaError_t launch(const Attention& p, cudaStream_t s) {
         q.second = 1;
         e = launch_pass<D>(q, p.plan.prefix, true, p.plan.own.parts, s);
     }
-    if (e == cudaSuccess && p.plan.through) e = launch_dependent(join_kernel<D>, (p.tokens * p.q_heads + 7) / 8, 256, s, p);
+    if (e == cudaSuccess && p.plan.through) e = launch_dependent(join_kernel<D>, p.tokens * p.q_heads, 32 * kJoinWarps, s, p);
     return e;
 }
 

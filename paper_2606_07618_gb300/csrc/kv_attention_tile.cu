@@ -75,6 +75,11 @@ __device__ __forceinline__ uint4 e2m1x8_scaled(uint32_t w, uint32_t s) {
 __device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+// A whole sector.
+__device__ __forceinline__ void st_global32(void* p, const uint32_t* v) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
 // 32 columns of this thread's lane of tensor memory; the values are there after wait_ld32.
 __device__ __forceinline__ void tmem_ld32(uint32_t a, float (&v)[32]) {
     asm volatile(
@@ -413,90 +418,66 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
 #pragma unroll
             for (int c = 0; c < 4; c++) hid[c] = s_hidden[j & 3][c];
             const bool whole = __all_sync(0xffffffffu, left >= kKeys && !(hid[0] | hid[1] | hid[2] | hid[3]));
-            // the maximum over both halves of the scores; the first half stays in registers
-            float v[2][32], t4[4];
+            // Weights with the row's maximum so far, and the tile's maximum beside them; a warp in which that has
+            // grown too much takes the new one, scales O and forms its weights again (always at a row's first keys).
+            uint32_t w[4][16];
+            float sum;
+            for (bool again = true; again;) {
+                const float shift = m == neg_inf() ? 0.0f : kBits - m;
+                const u64 f2 = pack2(fac, fac), s2 = pack2(shift, shift), one2 = pack2(1.0f, 1.0f);
+                u64 sums[2] = {0ull, 0ull};
+                float v[2][32], top = neg_inf(), top1 = neg_inf();
+                tmem_ld32(ts, v[0]);
 #pragma unroll
-            for (int h = 1; h >= 0; h--) {
-                tmem_ld32(ts + 64 * h, v[0]);
-                tmem_ld32(ts + 64 * h + 32, v[1]);
-                wait_ld32(v[0]);
-                hold32(v[1]);
-                if (!whole) {
-#pragma unroll
-                    for (int c = 0; c < 2; c++)
-#pragma unroll
-                        for (int i = 0; i < 32; i++)
-                            if (64 * h + 32 * c + i >= left || (hid[2 * h + c] >> i & 1)) v[c][i] = neg_inf();
-                }
-#pragma unroll
-                for (int c = 0; c < 2; c++) {
-                    float x = max3_nan(v[c][0], v[c][1], v[c][2]), y = max3_nan(v[c][3], v[c][4], v[c][5]);
-#pragma unroll
-                    for (int i = 6; i < 30; i += 4) {
-                        x = max3_nan(x, v[c][i], v[c][i + 1]);
-                        y = max3_nan(y, v[c][i + 2], v[c][i + 3]);
-                    }
-                    t4[2 * h + c] = max3_nan(max3_nan(x, v[c][30], v[c][31]), y, y);
-                }
-            }
-            float top = max3_nan(max3_nan(t4[0], t4[1], t4[2]), t4[3], t4[3]);
-            top *= fac;
-            const bool grown = top > m + kGrowth;
-            if (__any_sync(0xffffffffu, grown)) {
-                const float alpha = !grown ? 1.0f : m == neg_inf() ? 0.0f : ex2(m - top);
-                if (grown) m = top;
-                l *= alpha;
-                if (j > 0) {
-#pragma unroll 1
-                    for (int c = 0; c < D; c += 16) {
-                        float o[16], z[16];
-                        tmem_ld16(to + c, o);
-                        tmem_wait_ld(o, z);
-                        uint32_t u[16];
-#pragma unroll
-                        for (int i = 0; i < 16; i++) u[i] = __float_as_uint(o[i] * alpha);
-                        tmem_st16(to + c, u);
-                    }
-                }
-            }
-            const float shift = m == neg_inf() ? 0.0f : kBits - m;
-            const u64 f2 = pack2(fac, fac), s2 = pack2(shift, shift);
-            const u64 one2 = pack2(1.0f, 1.0f);
-            u64 sum[2] = {0ull, 0ull};
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                if (h == 1) {
-                    tmem_ld32(ts + 64, v[0]);
-                    tmem_ld32(ts + 96, v[1]);
-                    wait_ld32(v[0]);
-                    hold32(v[1]);
+                for (int c = 0; c < 4; c++) {
+                    float(&x)[32] = v[c & 1];
+                    wait_ld32(x);
+                    if (c < 3) tmem_ld32(ts + 32 * (c + 1), v[(c + 1) & 1]);
                     if (!whole) {
 #pragma unroll
-                        for (int c = 0; c < 2; c++)
-#pragma unroll
-                            for (int i = 0; i < 32; i++)
-                                if (64 + 32 * c + i >= left || (hid[2 + c] >> i & 1)) v[c][i] = neg_inf();
+                        for (int i = 0; i < 32; i++)
+                            if (32 * c + i >= left || (hid[c] >> i & 1)) x[i] = neg_inf();
                     }
-                }
-#pragma unroll
-                for (int c = 0; c < 2; c++) {
-                    uint32_t w[16];
 #pragma unroll
                     for (int i = 0; i < 16; i++) {
-                        float a, bb;
-                        unpack2(fma2(pack2(v[c][2 * i], v[c][2 * i + 1]), f2, s2), a, bb);
+                        float& t = i & 1 ? top1 : top;
+                        t = max3_nan(t, x[2 * i], x[2 * i + 1]);
+                        float a, b2;
+                        unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), f2, s2), a, b2);
                         a = ex2(a);
-                        bb = ex2(bb);
-                        sum[i & 1] = fma2(pack2(a, bb), one2, sum[i & 1]);
-                        w[i] = f16x2(a, bb);
+                        b2 = ex2(b2);
+                        sums[i & 1] = fma2(pack2(a, b2), one2, sums[i & 1]);
+                        w[c][i] = f16x2(a, b2);
                     }
-                    tmem_st16(ts + 32 * h + 16 * c, w);
+                }
+                float a, b2, c2, d2;
+                unpack2(sums[0], a, b2);
+                unpack2(sums[1], c2, d2);
+                sum = (a + b2) + (c2 + d2);
+                top = max3_nan(top, top1, top1) * fac;
+                const bool grown = top > m + kGrowth;
+                again = __any_sync(0xffffffffu, grown);
+                if (again) {
+                    const float alpha = !grown ? 1.0f : m == neg_inf() ? 0.0f : ex2(m - top);
+                    if (grown) m = top;
+                    l *= alpha;
+                    if (j > 0) {
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 16) {
+                            float o[16], z[16];
+                            tmem_ld16(to + c, o);
+                            tmem_wait_ld(o, z);
+                            uint32_t u[16];
+#pragma unroll
+                            for (int i = 0; i < 16; i++) u[i] = __float_as_uint(o[i] * alpha);
+                            tmem_st16(to + c, u);
+                        }
+                    }
                 }
             }
-            float a, bb, c2, d2;
-            unpack2(sum[0], a, bb);
-            unpack2(sum[1], c2, d2);
-            l += (a + bb) + (c2 + d2);
+            l += sum;
+#pragma unroll
+            for (int c = 0; c < 4; c++) tmem_st16(ts + 16 * c, w[c]);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -521,18 +502,20 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                 for (int i = 0; i < 16; i++) o[i] = empty ? 0.0f : o[i] * f;
                 if (!valid) continue;
                 if (PART) {
-                    float4* d = reinterpret_cast<float4*>(static_cast<float*>(p.workspace) + at * D + c);
+                    float* d = static_cast<float*>(p.workspace) + at * D + c;
+                    uint32_t u[16];
 #pragma unroll
-                    for (int i = 0; i < 4; i++) d[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    for (int i = 0; i < 16; i++) u[i] = __float_as_uint(o[i]);
+                    st_global32(d, u);
+                    st_global32(d + 8, u + 8);
                 } else {
                     uint32_t w[8];
 #pragma unroll
                     for (int i = 0; i < 8; i++)
                         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(o[2 * i + 1]), "f"(o[2 * i]));
                     uint16_t* d = static_cast<uint16_t*>(p.out.p) + token * p.out.token + h * p.out.head + c;
-                    if (p.out.vec) {
-                        reinterpret_cast<uint4*>(d)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                        reinterpret_cast<uint4*>(d)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                    if (p.out.vec == 2) {
+                        st_global32(d, w);
                     } else {
 #pragma unroll
                         for (int i = 0; i < 16; i++) d[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));

@@ -97,7 +97,7 @@ inline Plan make_plan(const Sizes& s) {
     p.prefix = Pass{0, 0, 0};
     if (s.prefix > 0) p.prefix = plan_pass(1, s.heads, s.dim, s.tokens * group, s.prefix);
     const int64_t blocks = (int64_t)1 << 31, rows = s.tokens * s.q_heads;
-    p.small = p.own.tiles < blocks / p.own.parts / s.batch && p.prefix.tiles < blocks / (p.prefix.parts + 1) && rows < 8 * blocks;
+    p.small = p.own.tiles < blocks / p.own.parts / s.batch && p.prefix.tiles < blocks / (p.prefix.parts + 1) && rows < blocks;
     p.through = p.parts() > 1 && !(s.prefix <= 0 && p.own.rows < kTileRows && p.own.parts <= kMaxCluster);
     if (p.small && p.through) {
         p.values = p.parts() * s.tokens * s.q_heads * s.dim * 4;
