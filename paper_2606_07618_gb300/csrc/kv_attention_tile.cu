@@ -31,10 +31,10 @@ namespace {
 
 using namespace mm;
 
-constexpr int kSoftmaxWarps = 8, kLoadWarps = 8, kMmaWarp = kSoftmaxWarps + kLoadWarps;
-// Five warps to a quarter of the SM, three of the last four idle: of its 5 x 96 registers a thread, softmax takes 2 x 144, loads 2 x 72, MMAs 48.
+constexpr int kSoftmaxWarps = 8, kLoadWarps = 4, kMmaWarp = kSoftmaxWarps + kLoadWarps;
+// Four warps to a quarter of the SM, three of the last four idle: of its 4 x 128 registers a thread, softmax takes 2 x 176, loads 112, MMAs 48.
 constexpr int kTileThreads = 32 * (kMmaWarp + 4);
-constexpr int kSoftmaxRegs = 144, kLoadRegs = 72, kMmaRegs = 48;
+constexpr int kSoftmaxRegs = 176, kLoadRegs = 112, kMmaRegs = 48;
 constexpr int kKeys = 128, kRows = 128;
 constexpr float kBits = 7.0f, kGrowth = 8.0f, kJoinBits = 15.0f;
 
@@ -150,32 +150,18 @@ struct Bars {
 template <int D>
 struct Held {
     uint4 w[D / 32];
-    uint32_t s[D / 64];                                          // four scale codes each
-    __device__ __forceinline__ void load(const Cache& c, int64_t page, int at, int head, int part) {
-        if (page < 0) {
+    uint32_t s[D / 16];                                          // scale codes, not touched before they are used
+    __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* sf, int page_log2) {
 #pragma unroll
-            for (int i = 0; i < D / 32; i++) w[i] = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < D / 32; i++) w[i] = *reinterpret_cast<const uint4*>(codes + 16 * i);
 #pragma unroll
-            for (int i = 0; i < D / 64; i++) s[i] = 0;
-            return;
-        }
-        const int64_t row = (page * c.heads + head) * 2 + part;
-        const uint8_t* p = c.codes + ((row << c.page_log2) + at) * (D / 2);
-#pragma unroll
-        for (int i = 0; i < D / 32; i++) w[i] = *reinterpret_cast<const uint4*>(p + 16 * i);
-        const uint8_t* q = c.sf + ((row * (D / 16)) << c.page_log2) + at;
-#pragma unroll
-        for (int i = 0; i < D / 64; i++) {
-            s[i] = 0;
-#pragma unroll
-            for (int j = 0; j < 4; j++) s[i] |= (uint32_t)q[(int64_t)(4 * i + j) << c.page_log2] << (8 * j);
-        }
+        for (int i = 0; i < D / 16; i++) s[i] = sf[i << page_log2];
     }
     // into a row of an operand, whose address has the row's swizzle in its chunk bits (16 bytes: 8 elements)
     __device__ __forceinline__ void store(uint32_t row) const {
 #pragma unroll
         for (int b = 0; b < D / 16; b++) {
-            const uint32_t sc = scale_pair(__byte_perm(s[b / 4], 0, 0x1111 * (b & 3)));
+            const uint32_t sc = scale_pair(s[b] | s[b] << 8);
             const uint4& v = w[b / 2];
             const uint32_t at = (row ^ ((2 * b & 7) << 4)) + (b >> 2) * Shape<D>::kPanel;
             st_shared16(at, e2m1x8_scaled(b & 1 ? v.z : v.x, sc));
@@ -312,37 +298,55 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     bool ok = true;
     if (warp >= kSoftmaxWarps && warp < kMmaWarp) {
         regs_down<kLoadRegs>();
-        // four warps the keys, four the values; the next tile's bytes are on their way, and the page after it
-        const int t = tid & 127, part_kv = (warp - kSoftmaxWarps) >> 2;
-        auto page_of = [&](int j) -> int64_t {
-            const int64_t x = begin + (int64_t)j * kKeys + t;
-            if (j >= tiles || x >= end) return -1;
-            const int64_t page = table[x >> p.c.page_log2];
-            if (page >= 0 && page < p.c.pages) return page;
-            outside = true;
-            return -2;
+        // Items: keys of a tile, then its values.  The next two items' bytes are on their way, and the page number after
+        // them; nothing looks at a load's result before its item's turn.  A page that is not there (behind the end, outside
+        // the pool) is read as page 0: its keys are hidden, its values' scales zero (NaN times a weight of 0 is no 0).
+        const int t = tid & 127, page_log2 = p.c.page_log2, page_mask = (1 << page_log2) - 1, pool = (int)p.c.pages;
+        const int64_t page_codes = (int64_t)p.c.heads * D << page_log2, page_sf = page_codes / 8;  // bytes of a page
+        const uint8_t *codes = p.c.codes + ((int64_t)head * D << page_log2), *sf = p.c.sf + ((int64_t)head * (D / 8) << page_log2);
+        const int part_codes = (D / 2) << page_log2, part_sf = (D / 16) << page_log2;
+        const int token0 = (int)begin + t, stop = (int)end;
+        auto entry = [&](int j) {                                // page number of this thread's token of tile j, unchecked
+            const int64_t x = (int64_t)token0 + (int64_t)j * kKeys;
+            return x < stop ? table[x >> page_log2] : 0;
         };
-        const auto at = [&](int j) { return (int)((begin + (int64_t)j * kKeys + t) & ((1 << p.c.page_log2) - 1)); };
-        uint64_t *empty = part_kv ? s_bars.v_empty : s_bars.k_empty, *full = part_kv ? s_bars.v_full : s_bars.k_full;
-        const uint32_t row = (part_kv ? sv : sk) + t * 128 + ((t & 7) << 4);
-        Held<D> now;
-        int64_t page = page_of(0), page1 = page_of(1);
-        now.load(p.c, page, at(0), head, part_kv);
+        auto fetch = [&](Held<D>& h, int j, int part, int page) {
+            const int at = (token0 + j * kKeys) & page_mask;
+            const int64_t pg = (unsigned)page < (unsigned)pool ? page : 0;
+            h.load(codes + pg * page_codes + part * part_codes + at * (D / 2), sf + pg * page_sf + part * part_sf + at, page_log2);
+        };
+        const uint32_t row = t * 128 + ((t & 7) << 4);
+        Held<D> now, next;
+        int page = entry(0), page1 = entry(1);                   // of the items now and next, and after them
+        if (tiles > 0) {
+            fetch(now, 0, 0, page);
+            fetch(next, 0, 1, page);
+        }
 #pragma unroll 1
-        for (int j = 0; j < tiles; j++) {
-            const int st = j & 1;
-            if (j >= 2 && !mbar_wait_warp(smem_u32(empty + st), ((j >> 1) & 1) ^ 1)) { ok = false; break; }
-            if (part_kv == 0) {
-                const uint32_t mask = __ballot_sync(0xffffffffu, page == -2);
-                if (lane == 0) s_hidden[j & 3][warp - kSoftmaxWarps] = mask;
+        for (int i = 0; i < 2 * tiles; i++) {
+            const int j = i >> 1, part = i & 1, st = j & 1;
+            uint64_t *empty = (part ? s_bars.v_empty : s_bars.k_empty) + st, *full = (part ? s_bars.v_full : s_bars.k_full) + st;
+            const bool there = (int64_t)token0 + (int64_t)j * kKeys < stop, ok_page = (unsigned)page < (unsigned)pool;
+            if (part == 1 && !(there && ok_page)) {
+#pragma unroll
+                for (int k = 0; k < D / 16; k++) now.s[k] = 0;
             }
-            now.store(row + st * H::kOp);
+            if (j >= 2 && !mbar_wait_warp(smem_u32(empty), ((j >> 1) & 1) ^ 1)) { ok = false; break; }
+            if (part == 0) {
+                const uint32_t mask = __ballot_sync(0xffffffffu, there && !ok_page);
+                if (lane == 0) s_hidden[j & 3][warp - kSoftmaxWarps] = mask;
+                outside |= there && !ok_page;
+            }
+            now.store((part ? sv : sk) + st * H::kOp + row);
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(full + st));
-            page = page1;
-            page1 = page_of(j + 2);
-            now.load(p.c, page, at(j + 1), head, part_kv);
+            if (lane == 0) mbar_arrive(smem_u32(full));
+            now = next;
+            if (j + 1 < tiles) fetch(next, j + 1, part, page1);
+            if (part == 1) {
+                page = page1;
+                page1 = entry(j + 2);
+            }
         }
         if (p.status && __any_sync(0xffffffffu, outside) && lane == 0) atomicOr(p.status, kStatusBounds);
     } else if (warp >= kMmaWarp) {
@@ -418,66 +422,70 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
 #pragma unroll
             for (int c = 0; c < 4; c++) hid[c] = s_hidden[j & 3][c];
             const bool whole = __all_sync(0xffffffffu, left >= kKeys && !(hid[0] | hid[1] | hid[2] | hid[3]));
-            // Weights with the row's maximum so far, and the tile's maximum beside them; a warp in which that has
-            // grown too much takes the new one, scales O and forms its weights again (always at a row's first keys).
-            uint32_t w[4][16];
-            float sum;
-            for (bool again = true; again;) {
-                const float shift = m == neg_inf() ? 0.0f : kBits - m;
-                const u64 f2 = pack2(fac, fac), s2 = pack2(shift, shift), one2 = pack2(1.0f, 1.0f);
-                u64 sums[2] = {0ull, 0ull};
-                float v[2][32], top = neg_inf(), top1 = neg_inf();
-                tmem_ld32(ts, v[0]);
+            float v[4][32];
 #pragma unroll
-                for (int c = 0; c < 4; c++) {
-                    float(&x)[32] = v[c & 1];
-                    wait_ld32(x);
-                    if (c < 3) tmem_ld32(ts + 32 * (c + 1), v[(c + 1) & 1]);
-                    if (!whole) {
+            for (int c = 0; c < 4; c++) tmem_ld32(ts + 32 * c, v[c]);
+            wait_ld32(v[0]);
 #pragma unroll
-                        for (int i = 0; i < 32; i++)
-                            if (32 * c + i >= left || (hid[c] >> i & 1)) x[i] = neg_inf();
-                    }
+            for (int c = 1; c < 4; c++) hold32(v[c]);
+            if (!whole) {
 #pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        float& t = i & 1 ? top1 : top;
-                        t = max3_nan(t, x[2 * i], x[2 * i + 1]);
-                        float a, b2;
-                        unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), f2, s2), a, b2);
-                        a = ex2(a);
-                        b2 = ex2(b2);
-                        sums[i & 1] = fma2(pack2(a, b2), one2, sums[i & 1]);
-                        w[c][i] = f16x2(a, b2);
-                    }
+                for (int c = 0; c < 4; c++)
+#pragma unroll
+                    for (int i = 0; i < 32; i++)
+                        if (32 * c + i >= left || (hid[c] >> i & 1)) v[c][i] = neg_inf();
+            }
+            float tops[4];
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                float a = max3_nan(v[c][0], v[c][1], v[c][2]), b2 = max3_nan(v[c][3], v[c][4], v[c][5]);
+#pragma unroll
+                for (int i = 6; i < 30; i += 4) {
+                    a = max3_nan(a, v[c][i], v[c][i + 1]);
+                    b2 = max3_nan(b2, v[c][i + 2], v[c][i + 3]);
                 }
-                float a, b2, c2, d2;
-                unpack2(sums[0], a, b2);
-                unpack2(sums[1], c2, d2);
-                sum = (a + b2) + (c2 + d2);
-                top = max3_nan(top, top1, top1) * fac;
-                const bool grown = top > m + kGrowth;
-                again = __any_sync(0xffffffffu, grown);
-                if (again) {
-                    const float alpha = !grown ? 1.0f : m == neg_inf() ? 0.0f : ex2(m - top);
-                    if (grown) m = top;
-                    l *= alpha;
-                    if (j > 0) {
+                tops[c] = max3_nan(max3_nan(a, v[c][30], v[c][31]), b2, b2);
+            }
+            const float top = max3_nan(max3_nan(tops[0], tops[1], tops[2]), tops[3], tops[3]) * fac;
+            const bool grown = top > m + kGrowth;
+            if (__any_sync(0xffffffffu, grown)) {
+                const float alpha = !grown ? 1.0f : m == neg_inf() ? 0.0f : ex2(m - top);
+                if (grown) m = top;
+                l *= alpha;
+                if (j > 0) {
 #pragma unroll 1
-                        for (int c = 0; c < D; c += 16) {
-                            float o[16], z[16];
-                            tmem_ld16(to + c, o);
-                            tmem_wait_ld(o, z);
-                            uint32_t u[16];
+                    for (int c = 0; c < D; c += 16) {
+                        float o[16], z[16];
+                        tmem_ld16(to + c, o);
+                        tmem_wait_ld(o, z);
+                        uint32_t u[16];
 #pragma unroll
-                            for (int i = 0; i < 16; i++) u[i] = __float_as_uint(o[i] * alpha);
-                            tmem_st16(to + c, u);
-                        }
+                        for (int i = 0; i < 16; i++) u[i] = __float_as_uint(o[i] * alpha);
+                        tmem_st16(to + c, u);
                     }
                 }
             }
-            l += sum;
+            const float shift = m == neg_inf() ? 0.0f : kBits - m;
+            const u64 f2 = pack2(fac, fac), s2 = pack2(shift, shift), one2 = pack2(1.0f, 1.0f);
+            u64 sums[2] = {0ull, 0ull};
 #pragma unroll
-            for (int c = 0; c < 4; c++) tmem_st16(ts + 16 * c, w[c]);
+            for (int c = 0; c < 4; c++) {
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    float a, b2;
+                    unpack2(fma2(pack2(v[c][2 * i], v[c][2 * i + 1]), f2, s2), a, b2);
+                    a = ex2(a);
+                    b2 = ex2(b2);
+                    sums[i & 1] = fma2(pack2(a, b2), one2, sums[i & 1]);
+                    w[i] = f16x2(a, b2);
+                }
+                tmem_st16(ts + 16 * c, w);
+            }
+            float a, b2, c2, d2;
+            unpack2(sums[0], a, b2);
+            unpack2(sums[1], c2, d2);
+            l += (a + b2) + (c2 + d2);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
