@@ -20,9 +20,11 @@
 // Two tokens' codes of one dim are brought side by side as nibbles, so that one conversion gives the
 // pair of fp16 that the MMA wants.
 //
-// Softmax runs over the tiles of a warp with the running maximum and sum, weights scaled by 2^15 (the
-// smallest then keep fp16's full precision down to 2^-29 of the largest); warps, and the parts that a
-// long cache is split into, are joined by their maxima, in a fixed order.
+// Softmax runs over the tiles of a warp with a running maximum, which is followed only when it has grown by more than
+// 2^8: weights are held 2^7-fold, so that they stay below fp16's largest, and O is rarely scaled.  Warps, and the parts
+// that a long cache is split into, are joined by their maxima, in a fixed order.
+#include <climits>
+
 #include "kv_kernels.h"
 #include "nvfp4_device.cuh"
 
@@ -31,13 +33,18 @@ namespace kv {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr float kWeightBits = 15.0f;
+constexpr float kWeightBits = 7.0f, kGrowth = 8.0f;
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 // The larger one; NaN if either is, so that a query with NaN gives NaN.
 __device__ __forceinline__ float max_nan(float a, float b) {
     float d;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
 __device__ __forceinline__ float ex2(float x) {
@@ -139,9 +146,8 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 
 // Four elements of a row's result: top its largest logit (base 2), sum that of its weights, v weights times values.
 template <int D, bool PART>
-__device__ __forceinline__ void write_row(const Attention& p, int64_t part, int64_t row0, int head, int64_t row, int d,
-                                          const float4& v, float top, float sum) {
-    const int64_t token = row0 + row / p.group, h = head * (int64_t)p.group + row % p.group;
+__device__ __forceinline__ void write_row(const Attention& p, int64_t part, int64_t token, int64_t h, int d, const float4& v,
+                                          float top, float sum) {
     if (PART) {
         const int64_t at = (part * p.tokens + token) * p.q_heads + h;
         *reinterpret_cast<float4*>(static_cast<float*>(p.workspace) + at * D + d) = v;
@@ -169,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
     constexpr bool PART = JOIN == kWorkspace;
     using T = Tile<D, NT>;
     __shared__ alignas(16) uint8_t s_mem[T::kSmem];
-    float(*s_o)[T::R][D] = reinterpret_cast<float(*)[T::R][D]>(s_mem);
+    float* s_o = reinterpret_cast<float*>(s_mem);                // [warps][R][D], over the tiles
     __shared__ float s_m[4][T::R], s_l[4][T::R], s_top[T::R], s_sum[T::R];
     if (!p.second) grid_dependency_wait();
     grid_launch_dependents();                                    // behind the wait: the next pass counts on it
@@ -180,10 +186,10 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
         }
     } at_end{p.second};
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int head = blockIdx.y;
-    const uint32_t parts = (uint32_t)pass.parts, x = blockIdx.x / parts, part = blockIdx.x - x * parts;
-    const int64_t b = x / (uint32_t)pass.tiles, tile = x - b * pass.tiles;
+    const int head = blockIdx.y, group = p.group;
+    const uint32_t parts = (uint32_t)pass.parts, b = blockIdx.x / parts, part = blockIdx.x - b * parts;
 
+    const float S_k = ld_f32(p.c.S_k);
     int64_t row0 = 0, n, len;
     const int32_t* table;
     int64_t width;
@@ -209,17 +215,41 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
         len = len < 0 ? 0 : width << p.c.page_log2;
     }
     const bool causal = !PREFIX && p.causal;
-    const int64_t computed = PREFIX || n < p.max_q ? n : p.max_q;
-    const int64_t first = tile * T::R, rows = computed * p.group;
+    const int rows = (int)(PREFIX || n < p.max_q ? n : p.max_q) * group;     // at most 16
     if (p.status && outside && threadIdx.x == 0 && head == 0) atomicOr(p.status, kStatusBounds);
-    if (first >= rows) return;
-    // keys that the tile's last row sees
-    const int64_t last = (first + T::R < rows ? first + T::R : rows) - 1;
-    const int64_t sees = causal ? len - n + last / p.group + 1 : len;
-    const int64_t chunk = part_tokens(len, pass.parts, kWarpTokens), from = part * chunk;
-    // tokens fit 31 bits from here on
-    const int begin = (int)from, end = (int)(from + chunk < sees ? from + chunk : sees);
+    if (rows == 0) return;
+    // query and head of the group of row r < 16: r / group by a multiplication (group <= 16)
+    const uint32_t inverse = 65536u / (uint32_t)group + 1;
+    auto query_of = [&](int r) { return (int)(r * inverse >> 16); };
+    // keys that the last row sees; tokens fit 31 bits
+    const int shift = causal ? (int)(len - n) + 1 : (int)len, each = causal ? 1 : 0;      // row r sees shift + each query_of(r)
+    const int chunk = (int)part_tokens32((uint32_t)len, parts, kWarpTokens);
+    const int begin = (int)min((int64_t)part * chunk, (int64_t)INT_MAX), sees = shift + each * query_of(rows - 1);
+    const int end = sees - begin > chunk ? begin + chunk : sees;
     if (PART && begin >= end) return;
+
+    // the queries' elements: row 8 nt + g, from t D/4 on
+    uint32_t qw[NT][D / 8];
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        const int r = 8 * nt + g, i = query_of(r);
+#pragma unroll
+        for (int k = 0; k < D / 8; k++) qw[nt][k] = 0;
+        if (r < rows) {
+            const uint16_t* q = static_cast<const uint16_t*>(p.q.p) + (row0 + i) * p.q.token +
+                                ((int64_t)head * group + (r - i * group)) * p.q.head + t * (D / 4);
+            if (p.q.vec) {
+#pragma unroll
+                for (int k = 0; k < D / 32; k++) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(q + 8 * k);
+                    qw[nt][4 * k] = v.x, qw[nt][4 * k + 1] = v.y, qw[nt][4 * k + 2] = v.z, qw[nt][4 * k + 3] = v.w;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < D / 8; k++) qw[nt][k] = q[2 * k] | (uint32_t)q[2 * k + 1] << 16;
+            }
+        }
+    }
 
     // What the lane reads of a tile from token k0 on: keys of the 16-token group g / 2, values of group t.  A page that is
     // not there (behind the end, outside the pool) is read as page 0 and hidden afterwards.
@@ -261,40 +291,22 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
     constexpr int kStride = 4 * kWarpTokens;
     const int start = begin + warp * kWarpTokens;
     int kpg = page_of(start + 16 * (g >> 1)), vpg = page_of(start + 16 * t);
+    int kpg1 = page_of(start + kStride + 16 * (g >> 1)), vpg1 = page_of(start + kStride + 16 * t);
     if (start < end) load_keys(start, kpg);
     copy_commit();
     if (start < end) load_values(start, vpg);
     copy_commit();
-    int kpg1 = page_of(start + kStride + 16 * (g >> 1)), vpg1 = page_of(start + kStride + 16 * t);
 
-    // queries, scaled by a power of two, as the narrow operand: row 8 nt + g, elements from t D/4 on
+    // queries in fp16, scaled by a power of two a row, as the narrow operand
     uint32_t qf[NT][2 * T::KW][2];
     float fac[NT][2], m[NT][2], l[NT][2];
-    int lim[NT][2];
-    const float S = ld_f32(p.c.S_k) * p.scale * 1.4426950408889634f;
+    int lim[NT][2], least = end;                                 // keys that a column's row sees, that every row sees
+    const float S = S_k * p.scale * 1.4426950408889634f;
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
-        const int64_t r = first + 8 * nt + g;
-        uint32_t w[D / 8];
-#pragma unroll
-        for (int i = 0; i < D / 8; i++) w[i] = 0;
-        if (r < rows) {
-            const int64_t e = (row0 + r / p.group) * p.q.token + (head * (int64_t)p.group + r % p.group) * p.q.head + t * (D / 4);
-            const uint16_t* q = static_cast<const uint16_t*>(p.q.p) + e;
-            if (p.q.vec) {
-#pragma unroll
-                for (int i = 0; i < D / 32; i++) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(q + 8 * i);
-                    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < D / 8; i++) w[i] = q[2 * i] | (uint32_t)q[2 * i + 1] << 16;
-            }
-        }
         uint32_t top = 0;                                        // bf16 bits of the row's largest magnitude
 #pragma unroll
-        for (int i = 0; i < D / 8; i++) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+        for (int i = 0; i < D / 8; i++) top = max(top, max(qw[nt][i] & 0x7FFFu, (qw[nt][i] >> 16) & 0x7FFFu));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // 2^-e of the largest's exponent e, within fp32's normal powers; none for infinities and NaN
@@ -304,16 +316,20 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
         const float down = __int_as_float((127 - e) << 23), up = __int_as_float((127 + e) << 23);
 #pragma unroll
         for (int i = 0; i < D / 8; i++)
-            qf[nt][i / 2][i & 1] = f16x2(bf16lo(w[i]) * down, bf16hi(w[i]) * down);
+            qf[nt][i / 2][i & 1] = f16x2(bf16lo(qw[nt][i]) * down, bf16hi(qw[nt][i]) * down);
 #pragma unroll
         for (int c = 0; c < 2; c++) {                            // columns 2t, 2t + 1 of the MMA's result
-            const int64_t rc = first + 8 * nt + 2 * t + c;
+            const int r = 8 * nt + 2 * t + c;
             fac[nt][c] = S * __shfl_sync(0xffffffffu, up, (2 * t + c) * 4);
-            lim[nt][c] = rc < rows ? (int)(causal ? len - n + rc / p.group + 1 : len) : 0;
+            if (fac[nt][c] == 0.0f) fac[nt][c] = 1e-37f;         // hidden scores, -inf, stay that
+            lim[nt][c] = r < rows ? shift + each * query_of(r) : 0;
+            if (r < rows) least = min(least, lim[nt][c]);
             m[nt][c] = neg_inf();
             l[nt][c] = 0.0f;
         }
     }
+    least = min(least, __shfl_xor_sync(0xffffffffu, least, 1));
+    least = min(least, __shfl_xor_sync(0xffffffffu, least, 2));
     float o[NT][D / 16][4];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++)
@@ -321,16 +337,6 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
         for (int i = 0; i < D / 16; i++)
 #pragma unroll
             for (int c = 0; c < 4; c++) o[nt][i][c] = 0.0f;
-    int least = end;                                             // keys that every row sees
-#pragma unroll
-    for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-        for (int c = 0; c < 2; c++)
-            if (first + 8 * nt + 2 * t + c < rows && lim[nt][c] < least) least = lim[nt][c];
-#pragma unroll
-    for (int i = 1; i < 4; i *= 2) {
-        least = min(least, __shfl_xor_sync(0xffffffffu, least, i));
-    }
 
     // a tile's keys are copied over the last one's as soon as those are used, its values likewise (two groups of copies in
     // flight, keys' and values'), and its page numbers come one tile earlier
@@ -341,14 +347,14 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
 #pragma unroll
         for (int i = 0; i < T::KB; i++) ld_shared(m_ks + i * 512, ks[i]);
         float sc[NT][4][4];
-        const uint32_t pick = g & 1 ? 0x3232u : 0x1010u;
+        const uint32_t pick0 = g & 1 ? 0x11u : 0x00u, pick1 = g & 1 ? 0x33u : 0x22u;      // the token's byte, twice
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             uint32_t s0[T::KB], s1[T::KB];
 #pragma unroll
             for (int k = 0; k < T::KB; k++) {
-                s0[k] = __byte_perm(e4m3x2_to_f16(ks[k][i] & 0xFFFF), 0, pick);
-                s1[k] = __byte_perm(e4m3x2_to_f16(ks[k][i] >> 16), 0, pick);
+                s0[k] = e4m3x2_to_f16(__byte_perm(ks[k][i], 0, pick0));
+                s1[k] = e4m3x2_to_f16(__byte_perm(ks[k][i], 0, pick1));
             }
             uint32_t k0c[T::KW], k1c[T::KW];
             ld_shared(m_kc + 2 * i * 32 * T::KW * 4, k0c);
@@ -372,59 +378,62 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
         }
         if (more) load_keys(k0 + kStride, kpg1);
         copy_commit();
-        // weights
-        const bool whole = __all_sync(0xffffffffu, k0 + kWarpTokens <= least && kv_ok);
-        uint32_t pt[NT][4][2];
-        bool moved = false;
-        float alpha[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++) {
-            float top[2] = {neg_inf(), neg_inf()};
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int c = 0; c < 4; c++) {
-                    float v = sc[nt][i][c] * fac[nt][c & 1];
-                    if (!whole) {
-                        const int j = k0 + 16 * (g >> 1) + 4 * i + (g & 1) + (c & 2);
-                        v = kv_ok && j < lim[nt][c & 1] && j < end ? v : neg_inf();
-                    }
-                    sc[nt][i][c] = v;
-                    top[c & 1] = max_nan(top[c & 1], v);
-                }
-#pragma unroll
-            for (int c = 0; c < 2; c++) {
-#pragma unroll
-                for (int i = 4; i < 32; i *= 2) top[c] = max_nan(top[c], __shfl_xor_sync(0xffffffffu, top[c], i));
-                const float next = max_nan(m[nt][c], top[c]);
-                const float base = next == neg_inf() ? 0.0f : next - kWeightBits;
-                alpha[nt][c] = m[nt][c] == neg_inf() ? 0.0f : ex2(m[nt][c] - next);
-                moved |= next != m[nt][c];
-                m[nt][c] = next;
-                float sum = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-#pragma unroll
-                    for (int h = 0; h < 4; h += 2) {
-                        const float w = ex2(sc[nt][i][h + c] - base);
-                        sc[nt][i][h + c] = w;
-                        sum += w;
-                    }
-                l[nt][c] = l[nt][c] * alpha[nt][c] + sum;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                pt[nt][i][0] = transpose8x8(f16x2(sc[nt][i][0], sc[nt][i][1]));
-                pt[nt][i][1] = transpose8x8(f16x2(sc[nt][i][2], sc[nt][i][3]));
-            }
-        }
-        if (__any_sync(0xffffffffu, moved)) {
+        // Weights with the row's maximum so far; one that has grown by more than 2^kGrowth (always at the first keys) takes
+        // its place, and O and the sum are scaled.
+        if (!__all_sync(0xffffffffu, k0 + kWarpTokens <= least && kv_ok)) {
 #pragma unroll
             for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                for (int i = 0; i < D / 16; i++)
+                for (int i = 0; i < 4; i++)
 #pragma unroll
-                    for (int c = 0; c < 4; c++) o[nt][i][c] *= alpha[nt][c & 1];
+                    for (int c = 0; c < 4; c++) {
+                        const int j = k0 + 16 * (g >> 1) + 4 * i + (g & 1) + (c & 2);
+                        if (!kv_ok || j >= lim[nt][c & 1] || j >= end) sc[nt][i][c] = neg_inf();
+                    }
+        }
+        float top[NT][2];
+        bool grown = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+                float x = max3_nan(sc[nt][0][c], sc[nt][0][c + 2], sc[nt][1][c]);
+                x = max3_nan(x, sc[nt][1][c + 2], sc[nt][2][c]);
+                x = max3_nan(x, sc[nt][2][c + 2], sc[nt][3][c]);
+                x = max_nan(x, sc[nt][3][c + 2]);
+#pragma unroll
+                for (int i = 4; i < 32; i *= 2) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, i));
+                top[nt][c] = x * fac[nt][c];
+                grown |= !(top[nt][c] <= m[nt][c] + kGrowth);        // NaN: it becomes the maximum
+            }
+        if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                for (int c = 0; c < 2; c++) {
+                    const bool up = !(top[nt][c] <= m[nt][c] + kGrowth);
+                    const float alpha = !up ? 1.0f : m[nt][c] == neg_inf() ? 0.0f : ex2(m[nt][c] - top[nt][c]);
+                    if (up) m[nt][c] = top[nt][c];
+                    l[nt][c] *= alpha;
+#pragma unroll
+                    for (int i = 0; i < D / 16; i++) o[nt][i][c] *= alpha, o[nt][i][c + 2] *= alpha;
+                }
+        }
+        uint32_t pt[NT][4][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+            float base[2];
+#pragma unroll
+            for (int c = 0; c < 2; c++) base[c] = m[nt][c] == neg_inf() ? 0.0f : kWeightBits - m[nt][c];
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const float w0 = ex2(__fmaf_rn(sc[nt][i][2 * h], fac[nt][0], base[0]));
+                    const float w1 = ex2(__fmaf_rn(sc[nt][i][2 * h + 1], fac[nt][1], base[1]));
+                    l[nt][0] += w0, l[nt][1] += w1;
+                    pt[nt][i][h] = transpose8x8(f16x2(w0, w1));
+                }
         }
         copy_wait<1>();
         uint32_t vs[4];
@@ -471,15 +480,21 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
 #pragma unroll
     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-        for (int c = 0; c < 2; c++) {
+        for (int c = 0; c < 2; c++)
 #pragma unroll
             for (int i = 4; i < 32; i *= 2) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], i);
-            if (g == 0) {
+    if (g == 0) {
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
                 s_m[warp][8 * nt + 2 * t + c] = m[nt][c];
                 s_l[warp][8 * nt + 2 * t + c] = l[nt][c];
             }
-        }
+    }
     __syncthreads();
+    // 16 bytes d/4 of a row of sums; neighbouring rows' are apart in their banks
+    auto place = [](int w, int r, int q) { return ((w * T::R + r) * (D / 4) + (q ^ (r & 7))) * 4; };
 #pragma unroll
     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
@@ -489,38 +504,41 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
             const float w = m[nt][c] == neg_inf() ? 0.0f : ex2(m[nt][c] - top);
             // the lane's dims of this row: g D/8 + 0, 1, ..
 #pragma unroll
-            for (int i = 0; i < D / 16; i++)
-#pragma unroll
-                for (int h = 0; h < 2; h++) s_o[warp][r][g * (D / 8) + 2 * i + h] = o[nt][i][2 * h + c] * w;
+            for (int i = 0; i < D / 16; i += 2)
+                *reinterpret_cast<float4*>(s_o + place(warp, r, g * (D / 32) + i / 2)) =
+                    make_float4(o[nt][i][c] * w, o[nt][i][c + 2] * w, o[nt][i + 1][c] * w, o[nt][i + 1][c + 2] * w);
         }
-    __syncthreads();
-    // the block's sums, four neighbouring elements to a thread, into the first warp's place
-    for (int x = threadIdx.x; x < T::R * D / 4; x += kThreads) {
-        const int r = x / (D / 4), d = x % (D / 4) * 4;
-        float4 v = *reinterpret_cast<const float4*>(&s_o[0][r][d]);
-#pragma unroll
-        for (int w = 1; w < 4; w++) {
-            const float4 u = *reinterpret_cast<const float4*>(&s_o[w][r][d]);
-            v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
-        }
+    if (threadIdx.x < T::R) {
+        const int r = threadIdx.x;
         float top = neg_inf(), sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < 4; w++) top = max_nan(top, s_m[w][r]);
 #pragma unroll
         for (int w = 0; w < 4; w++) sum += s_m[w][r] == neg_inf() ? 0.0f : s_l[w][r] * ex2(s_m[w][r] - top);
+        s_top[r] = top, s_sum[r] = sum;
+    }
+    __syncthreads();
+    // the block's sums, four neighbouring elements to a thread, into the first warp's place
+    for (int x = threadIdx.x; x < rows * (D / 4); x += kThreads) {
+        const int r = x / (D / 4), q = x % (D / 4);
+        float4 v = *reinterpret_cast<const float4*>(s_o + place(0, r, q));
+#pragma unroll
+        for (int w = 1; w < 4; w++) {
+            const float4 u = *reinterpret_cast<const float4*>(s_o + place(w, r, q));
+            v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+        }
         if (JOIN == kCluster) {
-            *reinterpret_cast<float4*>(&s_o[0][r][d]) = v;
-            if (d == 0) s_top[r] = top, s_sum[r] = sum;
-        } else if (first + r < rows) {
-            write_row<D, PART>(p, part0 + part, row0, head, first + r, d, v, top, sum);
+            *reinterpret_cast<float4*>(s_o + place(0, r, q)) = v;
+        } else {
+            const int i = query_of(r);
+            write_row<D, PART>(p, part0 + part, row0 + i, (int64_t)head * group + (r - i * group), 4 * q, v, s_top[r], s_sum[r]);
         }
     }
     if (JOIN == kCluster) {
         cluster_arrive();
         cluster_wait();
-        for (int x = (int)part * kThreads + threadIdx.x; x < T::R * D / 4; x += (int)parts * kThreads) {
-            const int r = x / (D / 4), d = x % (D / 4) * 4;
-            if (first + r >= rows) break;
+        for (int x = (int)part * kThreads + threadIdx.x; x < rows * (D / 4); x += (int)parts * kThreads) {
+            const int r = x / (D / 4), q = x % (D / 4);
             float tops[kMaxCluster], top = neg_inf(), sum = 0.0f;
 #pragma unroll
             for (uint32_t k = 0; k < kMaxCluster; k++) {
@@ -532,11 +550,12 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
             for (uint32_t k = 0; k < kMaxCluster; k++) {
                 if (k >= parts || tops[k] == neg_inf()) continue;
                 const float w = ex2(tops[k] - top);
-                const float4 u = ld_cluster4(cluster_addr(&s_o[0][r][d], k));
+                const float4 u = ld_cluster4(cluster_addr(s_o + place(0, r, q), k));
                 sum += ld_cluster(cluster_addr(&s_sum[r], k)) * w;
                 v.x += u.x * w, v.y += u.y * w, v.z += u.z * w, v.w += u.w * w;
             }
-            write_row<D, false>(p, 0, row0, head, first + r, d, v, top, sum);
+            const int i = query_of(r);
+            write_row<D, false>(p, 0, row0 + i, (int64_t)head * group + (r - i * group), 4 * q, v, top, sum);
         }
         cluster_arrive();                                        // a block's memory stays until the others have read it
         cluster_wait();
@@ -643,7 +662,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(Attention p) {
 template <int D, int NT, bool PREFIX, int JOIN>
 cudaError_t launch_rows(const Attention& p, const Pass& pass, int64_t part0, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((PREFIX ? 1 : p.batch) * pass.parts * pass.tiles), (unsigned)p.c.heads);
+    cfg.gridDim = dim3((unsigned)((PREFIX ? 1 : p.batch) * pass.parts), (unsigned)p.c.heads);
     cfg.blockDim = dim3(kThreads);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];

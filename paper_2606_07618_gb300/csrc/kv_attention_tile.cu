@@ -36,7 +36,7 @@ constexpr int kSoftmaxWarps = 8, kLoadWarps = 4, kMmaWarp = kSoftmaxWarps + kLoa
 constexpr int kTileThreads = 32 * (kMmaWarp + 4);
 constexpr int kSoftmaxRegs = 176, kLoadRegs = 112, kMmaRegs = 48;
 constexpr int kKeys = 128, kRows = 128;
-constexpr float kBits = 7.0f, kGrowth = 8.0f, kJoinBits = 15.0f;
+constexpr float kBits = 7.0f, kGrowth = 8.0f;
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 __device__ __forceinline__ float ex2(float x) {
@@ -531,10 +531,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                 }
             }
             if (valid) {
-                // weights here are 2^kBits-fold of 2^m, those of the join 2^kJoinBits-fold; a NaN sum shows in both
+                // a NaN sum shows in both
                 if (PART)
                     reinterpret_cast<float2*>(static_cast<char*>(p.workspace) + p.plan.values)[at] =
-                        make_float2(l != l ? l : empty ? neg_inf() : m + (kJoinBits - kBits), l);
+                        make_float2(l != l ? l : empty ? neg_inf() : m, l);
                 else if (p.lse)
                     p.lse[at] = empty ? neg_inf() : (m + log2f(l) - kBits) * 0.6931471805599453f;
             }

@@ -40,6 +40,11 @@ KV_BOTH inline int64_t part_tokens(int64_t length, int64_t parts, int64_t step) 
     return (n < 1 ? 1 : n) * step;
 }
 
+KV_BOTH inline uint32_t part_tokens32(uint32_t length, uint32_t parts, uint32_t step) {      // length below 2^31
+    const uint32_t n = (length + parts * step - 1) / (parts * step);
+    return (n < 1 ? 1 : n) * step;
+}
+
 struct Plan {
     Pass own, prefix;                    // prefix.parts is 0 without one
     int64_t parts() const { return own.parts + prefix.parts; }
