@@ -143,7 +143,7 @@ struct Shape {
 };
 
 struct Bars {
-    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full;
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full, joined;
 };
 
 // A token's codes and scales of K or V on their way.
@@ -176,6 +176,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     extern __shared__ uint8_t smem_raw[];
     __shared__ Bars s_bars;
     __shared__ uint32_t s_tmem, s_hidden[4][4];
+    __shared__ float2 s_ml[kRows];
     __shared__ int s_abort;
     if (!p.second) grid_dependency_wait();
     grid_launch_dependents();                                    // behind the wait: the next pass counts on it
@@ -225,7 +226,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     const int64_t end = begin + chunk < sees ? begin + chunk : sees;
     if (PART && begin >= end) return;
     const int tiles = end > begin ? (int)((end - begin + kKeys - 1) / kKeys) : 0;      // a part is less than 2^31 tokens
-    const int both = rows - first > kRows;                       // the second tile has rows
+    // two streams of scores, weights and sums: of both tiles of rows; where there is only one (split), of its even and odd keys
+    const bool split = rows - first <= kRows && tiles > 1;
+    const int both = rows - first > kRows || split;
 
     const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;
     const uint32_t sq = base, sk = base + 2 * H::kOp, sv = base + 4 * H::kOp;
@@ -240,6 +243,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
             mbar_init(smem_u32(&s_bars.p_full[i]), 4);
         }
         mbar_init(smem_u32(&s_bars.o_full), 1);
+        mbar_init(smem_u32(&s_bars.joined), 4);
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -248,7 +252,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     float fac = 0.0f;
     int lim = 1 << 30;                                           // keys that the row sees of this part
     const int half = warp >> 2;                                  // tile of this warp's rows (softmax warps)
-    const int64_t row = first + tid;
+    const int64_t row = first + (split ? tid & 127 : tid);
     if (warp < kSoftmaxWarps) {
         uint32_t w[D / 2];
 #pragma unroll
@@ -370,40 +374,54 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
             if (elect_one()) mma_commit(smem_u32(bar));
             __syncwarp();
         };
-        if (tiles > 0) {
-            ok = mbar_wait_warp(smem_u32(&s_bars.k_full[0]), 0);
+        auto outputs = [&](int x, int st, bool first_keys) {
+            if (elect_one()) {
+                const uint64_t bd = smem_desc(sv + st * H::kOp, H::kPanel, 1024);
+#pragma unroll
+                for (int kk = 0; kk < kKeys / 16; kk++)
+                    mma_ts(tmem + H::kOut + x * D, tmem + H::kScores + x * 128 + kk * 8, bd + (kk * 16 * 128 >> 4), id_o,
+                           (uint32_t)(!first_keys | kk));
+            }
+            __syncwarp();
+        };
+        auto wait_for = [&](uint64_t* bar, int parity) {
+            ok = ok && mbar_wait_warp(smem_u32(bar), parity & 1);
             tc_fence_after();
-            if (ok) {
+            return ok;
+        };
+        if (split) {
+            for (int j = 0; j < 2 && wait_for(&s_bars.k_full[j], 0); j++) {
+                scores(j, j);
+                commit(&s_bars.k_empty[j]);
+            }
+            for (int j = 0; ok && j < tiles; j++) {
+                const int st = j & 1;
+                if (!wait_for(&s_bars.v_full[st], j >> 1) || !wait_for(&s_bars.p_full[st], j >> 1)) break;
+                outputs(st, st, j < 2);
+                commit(&s_bars.v_empty[st]);
+                if (j + 2 < tiles && wait_for(&s_bars.k_full[st], (j + 2) >> 1)) {
+                    scores(st, st);
+                    commit(&s_bars.k_empty[st]);
+                }
+            }
+        } else if (tiles > 0) {
+            if (wait_for(&s_bars.k_full[0], 0)) {
                 scores(0, 0);
                 if (both) scores(1, 0);
                 commit(&s_bars.k_empty[0]);
             }
-        }
-        for (int j = 0; ok && j < tiles; j++) {
-            const int st = j & 1, nx = (j + 1) & 1;
-            ok = mbar_wait_warp(smem_u32(&s_bars.v_full[st]), (j >> 1) & 1);
-            for (int x = 0; ok && x <= both; x++) {
-                ok = mbar_wait_warp(smem_u32(&s_bars.p_full[x]), j & 1);
+            for (int j = 0; ok && j < tiles; j++) {
+                const int st = j & 1, nx = (j + 1) & 1;
+                if (!wait_for(&s_bars.v_full[st], j >> 1)) break;
+                for (int x = 0; ok && x <= both; x++) {
+                    if (!wait_for(&s_bars.p_full[x], j)) break;
+                    outputs(x, st, j == 0);
+                    if (j + 1 < tiles && (x == 1 || wait_for(&s_bars.k_full[nx], (j + 1) >> 1))) scores(x, nx);
+                }
                 if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint64_t bd = smem_desc(sv + st * H::kOp, H::kPanel, 1024);
-#pragma unroll
-                    for (int kk = 0; kk < kKeys / 16; kk++)
-                        mma_ts(tmem + H::kOut + x * D, tmem + H::kScores + x * 128 + kk * 8, bd + (kk * 16 * 128 >> 4), id_o,
-                               (uint32_t)(j | kk));
-                }
-                __syncwarp();
-                if (j + 1 < tiles) {
-                    if (x == 0) ok = mbar_wait_warp(smem_u32(&s_bars.k_full[nx]), ((j + 1) >> 1) & 1);
-                    if (!ok) break;
-                    tc_fence_after();
-                    scores(x, nx);
-                }
+                commit(&s_bars.v_empty[st]);
+                if (j + 1 < tiles) commit(&s_bars.k_empty[nx]);
             }
-            if (!ok) break;
-            commit(&s_bars.v_empty[st]);
-            if (j + 1 < tiles) commit(&s_bars.k_empty[nx]);
         }
         commit(&s_bars.o_full);                                  // after every MMA issued, also on a timeout
         if (!mbar_wait_warp(smem_u32(&s_bars.o_full), 0)) ok = false;
@@ -414,8 +432,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);      // this warp's lanes
         const uint32_t ts = lanes + H::kScores + half * 128, to = lanes + H::kOut + half * D;
         float m = neg_inf(), l = 0.0f;
-        for (int j = 0; j < tiles; j++) {
-            if (!mbar_wait_warp(smem_u32(&s_bars.s_full[half]), j & 1)) { ok = false; break; }
+        const int step = split ? 2 : 1;
+        int turn = 0;
+        for (int j = split ? half : 0; j < tiles; j += step, turn++) {
+            if (!mbar_wait_warp(smem_u32(&s_bars.s_full[half]), turn & 1)) { ok = false; break; }
             tc_fence_after();
             const int left = lim - j * kKeys;                    // visible keys from this tile on
             uint32_t hid[4];
@@ -452,7 +472,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                 const float alpha = !grown ? 1.0f : m == neg_inf() ? 0.0f : ex2(m - top);
                 if (grown) m = top;
                 l *= alpha;
-                if (j > 0) {
+                if (turn > 0) {
 #pragma unroll 1
                     for (int c = 0; c < D; c += 16) {
                         float o[16], z[16];
@@ -493,7 +513,37 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
         }
         if (ok && !mbar_wait_warp(smem_u32(&s_bars.o_full), 0)) ok = false;
         tc_fence_after();
-        if (ok) {
+        // split: the second stream's maximum, sum and O through shared memory (the queries' place) to the first
+        float w0 = 1.0f, w1 = 0.0f;
+        const int r = tid & 127;
+        auto other = [&](int q) { return sq + (uint32_t)(r * D * 4) + ((q ^ (r & 7)) << 4); };      // 16 bytes of O
+        if (split && ok) {
+            if (half == 1) {
+                s_ml[r] = make_float2(m, l);
+#pragma unroll 1
+                for (int c = 0; c < D; c += 16) {
+                    float o[16], z[16];
+                    tmem_ld16(to + c, o);
+                    tmem_wait_ld(o, z);
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        st_shared16(other(c / 4 + i), make_uint4(__float_as_uint(o[4 * i]), __float_as_uint(o[4 * i + 1]),
+                                                                 __float_as_uint(o[4 * i + 2]), __float_as_uint(o[4 * i + 3])));
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&s_bars.joined));
+            } else if (!mbar_wait_warp(smem_u32(&s_bars.joined), 0)) {
+                ok = false;
+            } else {
+                const float2 v = s_ml[r];
+                const float top = fmaxf(m, v.x);
+                w0 = m == neg_inf() ? 0.0f : ex2(m - top);
+                w1 = v.x == neg_inf() ? 0.0f : ex2(v.x - top);
+                m = top;
+                l = l * w0 + v.y * w1;                           // a NaN sum stays one
+            }
+        }
+        if (ok && !(split && half == 1)) {
             const int64_t token = row0 + row / p.group, h = head * (int64_t)p.group + row % p.group;
             const int64_t at = PART ? ((part0 + part) * p.tokens + token) * p.q_heads + h : token * p.q_heads + h;
             const float f = PART ? 1.0f : ld_f32(p.c.S_v) / l;
@@ -505,6 +555,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                 if (tiles > 0) {
                     tmem_ld16(to + c, o);
                     tmem_wait_ld(o, z);
+                }
+                if (split) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        float4 u;
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(u.x), "=f"(u.y), "=f"(u.z), "=f"(u.w)
+                                     : "r"(other(c / 4 + i)) : "memory");
+                        o[4 * i] = o[4 * i] * w0 + u.x * w1, o[4 * i + 1] = o[4 * i + 1] * w0 + u.y * w1;
+                        o[4 * i + 2] = o[4 * i + 2] * w0 + u.z * w1, o[4 * i + 3] = o[4 * i + 3] * w0 + u.w * w1;
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < 16; i++) o[i] = empty ? 0.0f : o[i] * f;
