@@ -145,14 +145,35 @@ __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // Four elements of a row's result: top its largest logit (base 2), sum that of its weights, v weights times values.
+// merge: parts of the prefix in the workspace that are added.
 template <int D, bool PART>
-__device__ __forceinline__ void write_row(const Attention& p, int64_t part, int64_t token, int64_t h, int d, const float4& v,
-                                          float top, float sum) {
+__device__ __forceinline__ void write_row(const Attention& p, int64_t part, int64_t token, int64_t h, int d, float4 v, float top,
+                                          float sum, int merge) {
     if (PART) {
         const int64_t at = (part * p.tokens + token) * p.q_heads + h;
         *reinterpret_cast<float4*>(static_cast<float*>(p.workspace) + at * D + d) = v;
         if (d == 0) reinterpret_cast<float2*>(static_cast<char*>(p.workspace) + p.plan.values)[at] = make_float2(top, sum);
         return;
+    }
+    if (merge > 0) {
+        const int64_t at = token * p.q_heads + h, stride = p.tokens * p.q_heads;
+        const float2* ml = reinterpret_cast<const float2*>(static_cast<const char*>(p.workspace) + p.plan.values) + at;
+        const float* vals = static_cast<const float*>(p.workspace) + at * D + d;
+        float most = top;
+#pragma unroll 8
+        for (int k = 0; k < merge; k++) most = max_nan(most, ml[k * stride].x);
+        const float w = top == neg_inf() ? 0.0f : ex2(top - most);
+        v.x *= w, v.y *= w, v.z *= w, v.w *= w;
+        sum *= w;
+        top = most;
+#pragma unroll 8
+        for (int k = 0; k < merge; k++) {
+            const float2 m = ml[k * stride];
+            const float4 u = *reinterpret_cast<const float4*>(vals + k * stride * D);
+            const float x = m.x == neg_inf() ? 0.0f : ex2(m.x - top);
+            sum += m.y * x;
+            v.x += u.x * x, v.y += u.y * x, v.z += u.z * x, v.w += u.w * x;
+        }
     }
     const bool empty = top == neg_inf();
     const float f = empty ? 0.0f : ld_f32(p.c.S_v) / sum;
@@ -518,6 +539,16 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
         s_top[r] = top, s_sum[r] = sum;
     }
     __syncthreads();
+    // parts of the prefix to be added
+    int merge = 0;
+    if (JOIN != kWorkspace && p.plan.merge) {
+        const int64_t most = p.prefix_width << page_log2;
+        int64_t n2 = *p.prefix_len;
+        n2 = n2 < 0 ? 0 : n2 > most ? most : n2;
+        const uint32_t size = part_tokens32((uint32_t)n2, (uint32_t)p.plan.prefix.parts, (uint32_t)p.plan.prefix.step());
+        merge = (int)(((uint32_t)n2 + size - 1) / size);
+        grid_dependency_wait();                                  // its pass
+    }
     // the block's sums, four neighbouring elements to a thread, into the first warp's place
     for (int x = threadIdx.x; x < rows * (D / 4); x += kThreads) {
         const int r = x / (D / 4), q = x % (D / 4);
@@ -531,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
             *reinterpret_cast<float4*>(s_o + place(0, r, q)) = v;
         } else {
             const int i = query_of(r);
-            write_row<D, PART>(p, part0 + part, row0 + i, (int64_t)head * group + (r - i * group), 4 * q, v, s_top[r], s_sum[r]);
+            write_row<D, PART>(p, part0 + part, row0 + i, (int64_t)head * group + (r - i * group), 4 * q, v, s_top[r], s_sum[r], merge);
         }
     }
     if (JOIN == kCluster) {
@@ -555,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
                 v.x += u.x * w, v.y += u.y * w, v.z += u.z * w, v.w += u.w * w;
             }
             const int i = query_of(r);
-            write_row<D, false>(p, 0, row0 + i, (int64_t)head * group + (r - i * group), 4 * q, v, top, sum);
+            write_row<D, false>(p, 0, row0 + i, (int64_t)head * group + (r - i * group), 4 * q, v, top, sum, merge);
         }
         cluster_arrive();                                        // a block's memory stays until the others have read it
         cluster_wait();
@@ -679,7 +710,7 @@ cudaError_t launch_rows(const Attention& p, const Pass& pass, int64_t part0, cud
 template <int D, int NT>
 cudaError_t dispatch(const Attention& p, const Pass& pass, bool prefix, int64_t part0, cudaStream_t s) {
     if (prefix) return launch_rows<D, NT, true, kWorkspace>(p, pass, part0, s);
-    if (p.plan.through) return launch_rows<D, NT, false, kWorkspace>(p, pass, part0, s);
+    if (p.plan.through && !p.plan.merge) return launch_rows<D, NT, false, kWorkspace>(p, pass, part0, s);
     return pass.parts > 1 ? launch_rows<D, NT, false, kCluster>(p, pass, part0, s) : launch_rows<D, NT, false, kAlone>(p, pass, part0, s);
 }
 
@@ -691,13 +722,16 @@ cudaError_t launch_pass(const Attention& p, const Pass& pass, bool prefix, int64
 
 template <int D>
 cudaError_t launch(const Attention& p, cudaStream_t s) {
-    cudaError_t e = launch_pass<D>(p, p.plan.own, false, 0, s);
-    if (e == cudaSuccess && p.plan.prefix.parts) {
-        Attention q = p;
-        q.second = 1;
-        e = launch_pass<D>(q, p.plan.prefix, true, p.plan.own.parts, s);
+    const Plan& plan = p.plan;
+    if (!plan.prefix.parts) {
+        const cudaError_t e = launch_pass<D>(p, plan.own, false, 0, s);
+        return e != cudaSuccess || !plan.through ? e : launch_dependent(join_kernel<D>, p.tokens * p.q_heads, 32 * kJoinWarps, s, p);
     }
-    if (e == cudaSuccess && p.plan.through) e = launch_dependent(join_kernel<D>, p.tokens * p.q_heads, 32 * kJoinWarps, s, p);
+    Attention second = p;
+    second.second = 1;
+    cudaError_t e = launch_pass<D>(p, plan.prefix, true, plan.merge ? 0 : plan.own.parts, s);
+    if (e == cudaSuccess) e = launch_pass<D>(second, plan.own, false, 0, s);
+    if (e == cudaSuccess && !plan.merge) e = launch_dependent(join_kernel<D>, p.tokens * p.q_heads, 32 * kJoinWarps, s, p);
     return e;
 }
 

@@ -68,8 +68,8 @@ struct Attention {
     void* workspace;
     Plan plan;
     // Set for the second pass of a call.  It is launched as a dependent of the first, whose blocks let it start only once
-    // they have waited for what came before the call themselves; it shares nothing with the first pass, so it does not wait
-    // for it before its end (which the join then waits for).
+    // they have waited for what came before the call themselves; so it does not wait for the first before it merges
+    // its results, or before its end (which the join then waits for).
     int second;
 };
 

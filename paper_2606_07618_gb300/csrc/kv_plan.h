@@ -48,8 +48,10 @@ KV_BOTH inline uint32_t part_tokens32(uint32_t length, uint32_t parts, uint32_t 
 struct Plan {
     Pass own, prefix;                    // prefix.parts is 0 without one
     int64_t parts() const { return own.parts + prefix.parts; }
-    // Whether the parts' sums go through the workspace: [parts][tokens][q_heads][dim] fp32, then maxima and sums of weights.
-    bool through = false;
+    // Whether parts' sums go through the workspace: [parts][tokens][q_heads][dim] fp32, then maxima and sums of weights.  With
+    // `merge` those of the prefix alone, whose pass comes first: the pass over each sequence's own keys adds them to its results.
+    // Else the own parts, then the prefix's, and a launch of its own joins them.
+    bool through = false, merge = false;
     int64_t values = 0, bytes = 0;
     bool small = true;
     // Whether the launches' grids can hold it.
@@ -105,11 +107,14 @@ inline Plan make_plan(const Sizes& s) {
     if (s.prefix > 0) p.prefix = plan_pass(1, s.heads, s.dim, s.tokens * group, s.prefix);
     const int64_t blocks = (int64_t)1 << 31, rows = s.tokens * s.q_heads;
     p.small = p.own.tiles < blocks / p.own.parts / s.batch && p.prefix.tiles < blocks / (p.prefix.parts + 1) && rows < blocks;
-    p.through = p.parts() > 1 && !(s.prefix <= 0 && p.own.rows < kTileRows && p.own.parts <= kMaxCluster);
+    const bool alone = p.own.rows < kTileRows && p.own.parts <= kMaxCluster;       // the own pass needs no workspace
+    p.merge = s.prefix > 0 && alone;
+    p.through = p.parts() > 1 && !(s.prefix <= 0 && alone);
     if (p.small && p.through) {
-        p.values = p.parts() * s.tokens * s.q_heads * s.dim * 4;
+        const int64_t parts = p.merge ? p.prefix.parts : p.parts();
+        p.values = parts * s.tokens * s.q_heads * s.dim * 4;
         p.values = (p.values + 255) / 256 * 256;
-        p.bytes = p.values + (p.parts() * s.tokens * s.q_heads * 8 + 255) / 256 * 256;
+        p.bytes = p.values + (parts * s.tokens * s.q_heads * 8 + 255) / 256 * 256;
     }
     return p;
 }
