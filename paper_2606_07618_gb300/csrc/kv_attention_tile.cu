@@ -143,7 +143,7 @@ struct Shape {
 };
 
 struct Bars {
-    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full, joined;
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full, joined, q_full;
 };
 
 // A token's codes and scales of K or V on their way.
@@ -244,62 +244,19 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
         }
         mbar_init(smem_u32(&s_bars.o_full), 1);
         mbar_init(smem_u32(&s_bars.joined), 4);
+        mbar_init(smem_u32(&s_bars.q_full), kSoftmaxWarps);
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
 
-    // queries to fp16, scaled by a power of two a row
-    float fac = 0.0f;
-    int lim = 1 << 30;                                           // keys that the row sees of this part
-    const int half = warp >> 2;                                  // tile of this warp's rows (softmax warps)
-    const int64_t row = first + (split ? tid & 127 : tid);
-    if (warp < kSoftmaxWarps) {
-        uint32_t w[D / 2];
-#pragma unroll
-        for (int i = 0; i < D / 2; i++) w[i] = 0;
-        if (row < rows) {
-            const uint16_t* q = static_cast<const uint16_t*>(p.q.p) + (row0 + row / p.group) * p.q.token +
-                                (head * (int64_t)p.group + row % p.group) * p.q.head;
-            if (p.q.vec) {
-#pragma unroll
-                for (int i = 0; i < D / 8; i++) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(q + 8 * i);
-                    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < D / 2; i++) w[i] = q[2 * i] | (uint32_t)q[2 * i + 1] << 16;
-            }
-            const int64_t all = causal ? len - n + row / p.group + 1 : len;
-            const int64_t seen = (all < end ? all : end) - begin;
-            lim = seen < 0 ? 0 : (int)seen;
-        }
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < D / 2; i++) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
-        int e = (int)(top >> 7) - 127;
-        if (e == 128) e = 0;                                     // infinities and NaN stay what they are
-        e = e < -126 ? -126 : e > 126 ? 126 : e;
-        const float down = __int_as_float((127 - e) << 23), up = __int_as_float((127 + e) << 23);
-        fac = ld_f32(p.c.S_k) * p.scale * 1.4426950408889634f * up;
-        if (fac == 0.0f) fac = 1e-37f;                           // hidden scores, -inf, stay that
-#pragma unroll
-        for (int i = 0; i < D / 8; i++) {
-            uint32_t h[4];
-#pragma unroll
-            for (int j = 0; j < 4; j++) h[j] = f16x2(bf16lo(w[4 * i + j]) * down, bf16hi(w[4 * i + j]) * down);
-            const int r = tid & 127;
-            st_shared16(sq + half * H::kOp + (i >> 3) * H::kPanel + r * 128 + (((i & 7) ^ (r & 7)) << 4),
-                        make_uint4(h[0], h[1], h[2], h[3]));
-        }
-        fence_proxy_async();
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
 
     bool ok = true;
+    const int half = warp >> 2;                                  // tile of this warp's rows (softmax warps)
+    const int64_t row = first + (split ? tid & 127 : tid);
     if (warp >= kSoftmaxWarps && warp < kMmaWarp) {
         regs_down<kLoadRegs>();
         // Items: keys of a tile, then its values.  The next two items' bytes are on their way, and the page number after
@@ -389,6 +346,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
             tc_fence_after();
             return ok;
         };
+        wait_for(&s_bars.q_full, 0);
         if (split) {
             for (int j = 0; j < 2 && wait_for(&s_bars.k_full[j], 0); j++) {
                 scores(j, j);
@@ -428,6 +386,50 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
         }
     } else {
         regs_up<kSoftmaxRegs>();
+        // queries to fp16, scaled by a power of two a row
+        float fac = 0.0f;
+        int lim = 1 << 30;                                        // keys that the row sees of this part
+        uint32_t w[D / 2];
+#pragma unroll
+        for (int i = 0; i < D / 2; i++) w[i] = 0;
+        if (row < rows) {
+            const uint16_t* q = static_cast<const uint16_t*>(p.q.p) + (row0 + row / p.group) * p.q.token +
+                                (head * (int64_t)p.group + row % p.group) * p.q.head;
+            if (p.q.vec) {
+#pragma unroll
+                for (int i = 0; i < D / 8; i++) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(q + 8 * i);
+                    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 2; i++) w[i] = q[2 * i] | (uint32_t)q[2 * i + 1] << 16;
+            }
+            const int64_t all = causal ? len - n + row / p.group + 1 : len;
+            const int64_t seen = (all < end ? all : end) - begin;
+            lim = seen < 0 ? 0 : (int)seen;
+        }
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < D / 2; i++) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+        int e = (int)(top >> 7) - 127;
+        if (e == 128) e = 0;                                     // infinities and NaN stay what they are
+        e = e < -126 ? -126 : e > 126 ? 126 : e;
+        const float down = __int_as_float((127 - e) << 23), up = __int_as_float((127 + e) << 23);
+        fac = ld_f32(p.c.S_k) * p.scale * 1.4426950408889634f * up;
+        if (fac == 0.0f) fac = 1e-37f;                           // hidden scores, -inf, stay that
+#pragma unroll
+        for (int i = 0; i < D / 8; i++) {
+            uint32_t h[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) h[j] = f16x2(bf16lo(w[4 * i + j]) * down, bf16hi(w[4 * i + j]) * down);
+            const int r = tid & 127;
+            st_shared16(sq + half * H::kOp + (i >> 3) * H::kPanel + r * 128 + (((i & 7) ^ (r & 7)) << 4),
+                        make_uint4(h[0], h[1], h[2], h[3]));
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_bars.q_full));
         if (half == 0 || both) {
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);      // this warp's lanes
         const uint32_t ts = lanes + H::kScores + half * 128, to = lanes + H::kOut + half * D;
