@@ -143,7 +143,21 @@ nvfp4_status nvfp4_kv_attention(const nvfp4_kv_cache* cache, const void* q, int6
                                 void* workspace, size_t ws_bytes, void* stream);
 
 /*
- * The same for a batch that shares a prefix: every query also sees the first *prefix_len
+ * Self-test of the bounded waits (failure detection): nvfp4_kv_attention, of more than 16 rows a
+ * sequence and key head (max_q * q_heads / heads; fewer have no such waits: NVFP4_ERR_UNSUPPORTED),
+ * whose waits for keys are made to give up after their limit, by barriers that expect one arrival too
+ * many.  status_dev (required) gets bit 4 (16), out is not written by the blocks that gave up (what is
+ * joined from the workspace is undefined) and the CUDA context stays usable.
+ */
+nvfp4_status nvfp4_kv_selftest_wait_timeout(const nvfp4_kv_cache* cache, const void* q, int64_t q_token, int64_t q_head,
+                                            int64_t tokens, int q_heads, const int32_t* table, int64_t table_ld,
+                                            int64_t width, const int32_t* lens, const int32_t* offsets, int64_t batch,
+                                            int64_t max_q, float scale, int causal, void* out, int64_t out_token,
+                                            int64_t out_head, float* lse, int* status_dev, void* workspace,
+                                            size_t ws_bytes, void* stream);
+
+/*
+ * The same as nvfp4_kv_attention for a batch that shares a prefix: every query also sees the first *prefix_len
  * tokens of the pages prefix[0 .. prefix_width), before its own sequence's (table, lens,
  * offsets and the causal rule as above; a sequence may have no tokens of its own cached).
  * The prefix's keys and values are read once for all queries of the batch.

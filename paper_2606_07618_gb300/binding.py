@@ -126,10 +126,11 @@ def lib() -> ctypes.CDLL:
         L.nvfp4_kv_attention_workspace.argtypes = [p, i64, i32, i64, i64, i64, i64]
         L.nvfp4_kv_attention_workspace.restype = sz
         L.nvfp4_kv_attention.argtypes = [p, p, i64, i64, i64, i32, p, i64, i64, p, p, i64, i64, f, i, p, i64, i64, p, p, p, sz, p]
+        L.nvfp4_kv_selftest_wait_timeout.argtypes = L.nvfp4_kv_attention.argtypes
         L.nvfp4_kv_attention_prefix.argtypes = [p, p, i64, i64, i64, i32, p, i64, p, p, i64, i64, p, p, i64, i64, f, i, p, i64, i64,
                                                 p, p, p, sz, p]
         for fn in ("nvfp4_rope_turns", "nvfp4_rope", "nvfp4_kv_write", "nvfp4_kv_read", "nvfp4_kv_attention",
-                   "nvfp4_kv_attention_prefix"):
+                   "nvfp4_kv_selftest_wait_timeout", "nvfp4_kv_attention_prefix"):
             getattr(L, fn).restype = i
         for fn in ("mxfp4_quantize", "mxfp4_dequantize", "fp4_matmul", "fp4_selftest_wait_timeout", "fp4_matmul_backward",
                    "fp4_gated_ff", "fp4_gated_ff_backward"):
@@ -735,6 +736,13 @@ def nvfp4_kv_attention(q, cache, table, lens, offsets, max_q: int, scale: float,
     lens[b] cached tokens.  lse [tokens, q_heads] (fp32) optional."""
     _attention("nvfp4_kv_attention", q, cache, (), table, lens, offsets, max_q, scale, out, causal, lse, workspace, status,
                stream)
+
+
+def nvfp4_kv_selftest_wait_timeout(q, cache, table, lens, offsets, max_q: int, scale: float, out, status, workspace=None,
+                                   stream=None):
+    """nvfp4_kv_attention whose waits for keys run out (status bit 4).  See nvfp4kv.h."""
+    _attention("nvfp4_kv_selftest_wait_timeout", q, cache, (), table, lens, offsets, max_q, scale, out, True, None, workspace,
+               status, stream)
 
 
 def nvfp4_kv_attention_prefix(q, cache, prefix, prefix_len, table, lens, offsets, max_q: int, scale: float, out,

@@ -310,7 +310,7 @@ nvfp4_status attention(const nvfp4_kv_cache* cache, const void* q, int64_t q_tok
                        bool shared, const int32_t* prefix, int64_t prefix_width, const int32_t* prefix_len,
                        const int32_t* table, int64_t table_ld, int64_t width, const int32_t* lens, const int32_t* offsets,
                        int64_t batch, int64_t max_q, float scale, int causal, void* out, int64_t out_token, int64_t out_head,
-                       float* lse, int* status_dev, void* workspace, size_t ws_bytes, void* stream) {
+                       float* lse, int* status_dev, void* workspace, size_t ws_bytes, int starve, void* stream) {
     kv::Attention p = {};
     kv::Sizes s;
     int64_t codes, sf;
@@ -330,6 +330,7 @@ nvfp4_status attention(const nvfp4_kv_cache* cache, const void* q, int64_t q_tok
     if (!apart(a, b)) return NVFP4_ERR_INVALID_ARG;
     p.plan = kv::make_plan(s);
     if (!p.plan.fits()) return NVFP4_ERR_RANGE;
+    if (starve && p.plan.own.rows != kv::kTileRows) return NVFP4_ERR_UNSUPPORTED;
     if (p.plan.bytes > 0 && (!workspace || ws_bytes < (size_t)p.plan.bytes)) return NVFP4_ERR_INVALID_ARG;
     if (p.plan.bytes == 0) workspace = nullptr;
     if (!aligned(lens, 4) || !aligned(offsets, 4) || !aligned(prefix_len, 4) || !aligned(lse, 4) || !aligned(status_dev, 4) ||
@@ -375,6 +376,7 @@ nvfp4_status attention(const nvfp4_kv_cache* cache, const void* q, int64_t q_tok
     p.lse = lse;
     p.status = status_dev;
     p.workspace = workspace;
+    p.starve = starve;
     return result(kv::launch_attention(p, static_cast<cudaStream_t>(stream)));
 }
 
@@ -399,7 +401,17 @@ nvfp4_status nvfp4_kv_attention(const nvfp4_kv_cache* cache, const void* q, int6
                                 int causal, void* out, int64_t out_token, int64_t out_head, float* lse, int* status_dev,
                                 void* workspace, size_t ws_bytes, void* stream) {
     return attention(cache, q, q_token, q_head, tokens, q_heads, false, nullptr, 0, nullptr, table, table_ld, width, lens, offsets,
-                     batch, max_q, scale, causal, out, out_token, out_head, lse, status_dev, workspace, ws_bytes, stream);
+                     batch, max_q, scale, causal, out, out_token, out_head, lse, status_dev, workspace, ws_bytes, 0, stream);
+}
+
+nvfp4_status nvfp4_kv_selftest_wait_timeout(const nvfp4_kv_cache* cache, const void* q, int64_t q_token, int64_t q_head,
+                                            int64_t tokens, int q_heads, const int32_t* table, int64_t table_ld, int64_t width,
+                                            const int32_t* lens, const int32_t* offsets, int64_t batch, int64_t max_q,
+                                            float scale, int causal, void* out, int64_t out_token, int64_t out_head, float* lse,
+                                            int* status_dev, void* workspace, size_t ws_bytes, void* stream) {
+    if (!status_dev) return NVFP4_ERR_INVALID_ARG;
+    return attention(cache, q, q_token, q_head, tokens, q_heads, false, nullptr, 0, nullptr, table, table_ld, width, lens, offsets,
+                     batch, max_q, scale, causal, out, out_token, out_head, lse, status_dev, workspace, ws_bytes, 1, stream);
 }
 
 nvfp4_status nvfp4_kv_attention_prefix(const nvfp4_kv_cache* cache, const void* q, int64_t q_token, int64_t q_head,
@@ -410,7 +422,7 @@ nvfp4_status nvfp4_kv_attention_prefix(const nvfp4_kv_cache* cache, const void* 
                                        float* lse, int* status_dev, void* workspace, size_t ws_bytes, void* stream) {
     return attention(cache, q, q_token, q_head, tokens, q_heads, true, prefix, prefix_width, prefix_len, table, table_ld, width,
                      lens, offsets, batch, max_q, scale, causal, out, out_token, out_head, lse, status_dev, workspace, ws_bytes,
-                     stream);
+                     0, stream);
 }
 
 }  // extern "C"

@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     if (warp == kMmaWarp) tmem_alloc(smem_u32(&s_tmem), 512);
     if (tid == 0) {
         for (int i = 0; i < 2; i++) {
-            mbar_init(smem_u32(&s_bars.k_full[i]), 4);
+            mbar_init(smem_u32(&s_bars.k_full[i]), 4 + p.starve);
             mbar_init(smem_u32(&s_bars.v_full[i]), 4);
             mbar_init(smem_u32(&s_bars.k_empty[i]), 1);
             mbar_init(smem_u32(&s_bars.v_empty[i]), 1);

@@ -1,0 +1,158 @@
+"""Every path of attention over the cache -- few and many rows, parts alone, in clusters and through the workspace, with and
+without a prefix -- against 64 bits, at shapes that test_kv_plans.py shows to take them."""
+import time
+
+import pytest
+import torch
+
+import kv_reference as R
+
+pytestmark = pytest.mark.gpu
+
+# (lens, queries, heads, group, dim, page), further arguments -> rows of a block, how parts are joined, rows of the prefix's blocks
+PATHS = [
+    ((([100, 7], [1, 1], 2, 4, 64, 16), {}), (8, "alone", 0)),
+    ((([260, 7], [1, 1], 2, 4, 128, 16), {}), (8, "cluster", 0)),
+    ((([1100, 700], [2, 1], 1, 4, 64, 16), {}), (8, "cluster", 0)),
+    ((([1900, 64, 1], [1, 1, 1], 2, 8, 128, 64), {}), (8, "cluster", 0)),
+    ((([5000], [1], 2, 4, 128, 64), {}), (8, "workspace", 0)),
+    ((([100, 128], [2, 1], 2, 8, 128, 16), {}), (16, "alone", 0)),
+    ((([900, 70], [3, 2], 2, 4, 128, 16), {}), (16, "cluster", 0)),
+    ((([4000], [2], 1, 7, 64, 32), {}), (16, "workspace", 0)),
+    ((([40, 90], [30, 20], 38, 3, 64, 16), {}), (256, "alone", 0)),
+    ((([40, 90], [30, 20], 76, 2, 128, 16), {}), (256, "alone", 0)),
+    ((([700], [200], 1, 3, 128, 16), {}), (256, "workspace", 0)),
+    ((([300, 1000], [6, 9], 2, 4, 64, 16), {}), (256, "workspace", 0)),
+    ((([30], [1], 1, 4, 64, 16), {"prefix": 500}), (8, "merge", 8)),
+    ((([30, 300], [1, 1], 1, 8, 128, 16), {"prefix": 500}), (8, "merge", 16)),
+    ((([30, 9, 40], [1, 1, 1], 2, 8, 128, 16), {"prefix": 2000}), (8, "merge", 256)),
+    ((([30], [2], 1, 5, 128, 16), {"prefix": 300}), (16, "merge", 16)),
+    ((([30, 600], [2, 3], 2, 5, 64, 16), {"prefix": 900}), (16, "merge", 256)),
+    ((([9], [1], 1, 2, 128, 16), {"prefix": 64}), (8, "merge", 8)),
+    ((([50, 64], [9, 12], 2, 4, 128, 16), {"prefix": 333}), (256, "workspace", 256)),
+]
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2606_07618_gb300 import binding
+    binding.lib()
+    return binding
+
+
+@pytest.mark.parametrize("args,path", PATHS, ids=[f"{i}-{p[0]}-{p[1]}-{p[2]}" for i, (_, p) in enumerate(PATHS)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_paths(B, args, path, causal):
+    s = R.Setting(*args[0], **args[1], seed=7)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse = s.run(B, causal, extra=3, status=status)
+    R.check(out[:s.total], s.want(causal), lse[:s.total])
+    assert (out[s.total:] == 7.0).all() and status.item() == 0
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("queries", [[33, 64], [129, 1], [128], [43], [300, 90]])
+def test_one_and_two_tiles_of_rows(B, dim, queries):
+    """One tile's keys in two streams, two tiles, and a last tile alone, over odd numbers of key tiles."""
+    for extra in (0, 100, 400):
+        s = R.Setting([n + extra for n in queries], queries, 1, 3, dim, 32, seed=extra)
+        out, lse = s.run(B)
+        R.check(out, s.want(), lse)
+
+
+def test_prefix_alone(B):
+    """Sequences without tokens of their own, and a prefix of no tokens."""
+    s = R.Setting([0, 0], [1, 1], 2, 4, 128, 16, seed=3, prefix=700)
+    out, lse = s.run(B, causal=False)
+    R.check(out, s.want(False), lse)
+    for shape in (([30, 5], [1, 1], 2, 4, 128, 16), ([40, 50], [30, 20], 1, 4, 64, 16)):
+        s = R.Setting(*shape, seed=4, prefix=200)
+        dev = [t.cuda() for t in s.cache]
+        q, out = s.q.cuda(), torch.empty_like(s.q, device="cuda")
+        table, lens, offsets = s.table.cuda(), torch.tensor(s.lens, dtype=torch.int32, device="cuda"), s.offsets.cuda()
+        n = max(s.queries)
+        ws = torch.full((B.nvfp4_kv_attention_workspace(dev, q, 2, table.shape[1], n, s.common.numel()),), 255, dtype=torch.uint8, device="cuda")
+        B.nvfp4_kv_attention_prefix(q, dev, s.common.cuda(), torch.zeros(1, dtype=torch.int32, device="cuda"), table, lens, offsets, n,
+                                    s.scale, out, workspace=ws)
+        s.prefix = 0
+        s.common = s.common[:0]
+        R.check(out, s.want())
+
+
+def test_fewer_queries_than_max_q(B):
+    """max_q above the longest sequence's queries, and below it: those past it are not computed."""
+    s = R.Setting([90, 40], [3, 1], 2, 4, 64, 16, seed=5)
+    want = s.want()
+    for n in (3, 4, 100):
+        out, lse = s.run(B, max_q=n)
+        R.check(out, want, lse)
+    out, _ = s.run(B, max_q=2)
+    assert (out[2] == 7.0).all()
+    R.check(torch.cat((out[:2], out[3:])), [torch.cat((w[:2], w[3:])) for w in want])
+
+
+def test_pages_shared_and_out_of_order(B):
+    """Two sequences that hold the same pages, in another order each."""
+    s = R.Setting([64, 64], [1, 1], 1, 4, 128, 16, seed=6)
+    s.table[1] = s.table[0].flip(0)
+    out, lse = s.run(B)
+    R.check(out, s.want(), lse)
+
+
+def test_streams(B):
+    """Two calls at one time on two streams, each with a workspace of its own."""
+    sets = [R.Setting([3000 + i, 50], [1, 1], 2, 4, 128, 16, seed=i, prefix=600 * i) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in sets]
+    outs = []
+    torch.cuda.synchronize()
+    for s, stream in zip(sets, streams):
+        with torch.cuda.stream(stream):
+            outs.append(s.run(B))
+    torch.cuda.synchronize()
+    for s, (out, lse) in zip(sets, outs):
+        R.check(out, s.want(), lse)
+
+
+def test_two_graphs_share_a_workspace(B):
+    s = R.Setting([900, 80], [1, 1], 2, 4, 128, 16, seed=9, prefix=500)
+    t = R.Setting([4100], [1], 2, 4, 128, 16, seed=10)
+    calls, graphs = [], []
+    ws = None
+    for x in (s, t):
+        dev = [c.cuda() for c in x.cache]
+        q, out = x.q.cuda(), torch.empty_like(x.q, device="cuda")
+        table, lens, offsets = x.table.cuda(), torch.tensor(x.lens, dtype=torch.int32, device="cuda"), x.offsets.cuda()
+        common, plen = x.common.cuda(), torch.tensor([x.prefix], dtype=torch.int32, device="cuda")
+        need = B.nvfp4_kv_attention_workspace(dev, q, len(x.lens), table.shape[1], 1, common.numel())
+        calls.append((dev, q, out, table, lens, offsets, common, plen, need))
+    ws = torch.full((max(c[-1] for c in calls),), 255, dtype=torch.uint8, device="cuda")
+    for x, (dev, q, out, table, lens, offsets, common, plen, _) in zip((s, t), calls):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            if x.prefix:
+                B.nvfp4_kv_attention_prefix(q, dev, common, plen, table, lens, offsets, 1, x.scale, out, workspace=ws)
+            else:
+                B.nvfp4_kv_attention(q, dev, table, lens, offsets, 1, x.scale, out, workspace=ws)
+        graphs.append(g)
+    for _ in range(20):
+        for g in graphs:
+            g.replay()
+    for x, c in zip((s, t), calls):
+        R.check(c[2], x.want())
+
+
+def test_wait_runs_out_and_is_reported(B):
+    """The waits for keys give up after their limit, nothing is written, and the context stays usable."""
+    s = R.Setting([40, 90], [30, 20], 38, 3, 64, 16, seed=11)
+    dev = [t.cuda() for t in s.cache]
+    q, out = s.q.cuda(), torch.full_like(s.q, 7.0, device="cuda")
+    table, lens, offsets = s.table.cuda(), torch.tensor(s.lens, dtype=torch.int32, device="cuda"), s.offsets.cuda()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert B.nvfp4_kv_attention_workspace(dev, q, 2, table.shape[1], 30) == 0
+    torch.cuda.synchronize()
+    t0 = time.time()
+    B.nvfp4_kv_selftest_wait_timeout(q, dev, table, lens, offsets, 30, s.scale, out, status)
+    torch.cuda.synchronize()
+    assert 0.5 < time.time() - t0 < 60
+    assert status.item() == 16 and (out == 7.0).all()
+    out, lse = s.run(B)
+    R.check(out, s.want(), lse)

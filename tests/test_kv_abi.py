@@ -25,7 +25,8 @@ def test_header_and_exports(B):
     src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "nvfp4kv.h")).read(), flags=re.S)
     names = re.findall(r"^(?:nvfp4_status|size_t)\s+([a-z0-9_]+)\s*\(", src, re.M)
     assert sorted(names) == sorted(["nvfp4_rope_turns", "nvfp4_rope", "nvfp4_kv_write", "nvfp4_kv_read", "nvfp4_kv_attention",
-                                    "nvfp4_kv_attention_workspace", "nvfp4_kv_attention_prefix"])
+                                    "nvfp4_kv_attention_workspace", "nvfp4_kv_attention_prefix",
+                                    "nvfp4_kv_selftest_wait_timeout"])
     for n in names:
         assert hasattr(B.lib(), n), n
 
@@ -183,6 +184,14 @@ def test_attention_refusals(B, prefix):
         assert a(prefix=(prefix[0] + 2, 4, prefix[2])) == ALIGNMENT and a(prefix=(prefix[0], 4, prefix[2] + 2)) == ALIGNMENT
         assert a(ws=None) == INVALID and a(ws_bytes=100) == INVALID and a(ws=FAKE + 0x20000080) == ALIGNMENT
         assert a(ws=FAKE) == INVALID
+
+
+def test_selftest_refusals(B):
+    L = B.lib()
+    t = lambda heads=40, st=FAKE + 0x7000000: L.nvfp4_kv_selftest_wait_timeout(
+        cache(B), FAKE + 0x1000000, 64 * heads, 64, 8, heads, FAKE + 0x5000000, 8, 8, FAKE + 0x6000000, FAKE + 0x6100000, 2, 8, 0.1, 1,
+        FAKE + 0x2000000, 64 * heads, 64, None, st, FAKE + 0x20000000, 2 ** 40, None)
+    assert t(st=None) == INVALID and t(heads=4) == UNSUPPORTED     # 16 rows: no such waits
 
 
 # --------------------------------------------------------------------------- refusals of the binding
