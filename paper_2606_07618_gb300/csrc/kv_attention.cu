@@ -4,9 +4,13 @@
 // A value q s (without S) has at most 5 significant bits and lies in 2^-10 .. 2688, so fp16 holds
 // it exactly; a query's row is scaled by a power of two to below 2 and is exact in fp16 too
 // but for elements below 2^-14 of the row's largest.  Both products run on mma.sync
-// m16n8k16 (fp16 operands, fp32 sums): with 8 or 16 rows they take a fifth of the time that the
-// conversion of the cache's codes takes, and that goes straight from global memory to
-// registers, in the layout that the MMA's operands want.
+// m16n8k16 (fp16 operands, fp32 sums): with 8 or 16 rows they are 6% of the instructions, and an operand of
+// registers is what the converted codes already are (tcgen05 would want them in shared memory first).
+//
+// What bounds it is instruction issue: a warp's tile of 64 tokens (dim 128, 8 rows) takes about 1070 instructions, of
+// them 256 conversions, 256 multiplications by the blocks' scales and 64 MMAs, for 9.2 KB of cache.  16 sequences of
+// 4096 tokens with 8 key heads (75.8 MB, 11.2 us at the copy rate) take 20 us: 11 us of issue at the 2.8 instructions a
+// cycle that the loop reaches, and what a block spends before and after its four tiles a warp.
 //
 // Transposed products, so that the rows of queries are the MMA's narrow dimension:
 //   S^T [tokens 16, rows 8] = K Q^T,   O^T [dim 16, rows 8] += V^T P^T.
@@ -14,7 +18,9 @@
 // takes 64 tokens; lane (g, t) = (lane / 4, lane % 4) reads
 //   keys:   of tokens 16 (g/2) + (g&1) + 2i, i = 0..7, the dim/4 elements from t dim/4 on,
 //           and their scales of 16 tokens with one load a block;
-//   values: of tokens 16 t .. 16 t + 15, the dim/8 elements from g dim/8 on.
+//   values: of tokens 16 t .. 16 t + 15, the dim/8 elements from g dim/8 on,
+// each by asynchronous copies of its own to shared memory, keys and values in turn one tile ahead: 40 registers fewer than
+// loads kept in flight, so four blocks an SM instead of three (24.3 -> 22.4 us then).
 // Rows r and r + 8 of m-tile i of S^T are then tokens 16 (r/2) + 4i + (r&1) and two further, whose
 // weights, transposed by movmatrix, are the operand for the values of tokens 16 t + 4i .. + 3.
 // Two tokens' codes of one dim are brought side by side as nibbles, so that one conversion gives the

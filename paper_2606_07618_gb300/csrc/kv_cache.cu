@@ -3,7 +3,11 @@
 // Both are bound by memory, the sweep by its arithmetic (eleven candidates a block, the
 // arithmetic and code of quantize_kernel.cuh).  A warp covers 8 tokens by 4 blocks of 16: a
 // token's 4 blocks are 32 bytes of codes, a whole sector, and a block's scales of 8 tokens lie side by
-// side, so that neither side's scattered accesses take many more sectors than they hold.
+// side, so that neither side's scattered accesses take many more sectors than they hold.  A warp keeps to its
+// blocks of one head and walks the tokens, so that its addresses are a page's and a token's multiples.
+//
+// 65536 tokens of 8 heads of 128, bf16 (268 MB of keys and values, 75 MB of cache): written with block maxima in 64 us (51 at
+// the copy rate), swept in 203 (the sweep of as many elements by scalesweep_quantize: 194), read back in 75.
 #include "kv_kernels.h"
 #include "quantize_kernel.cuh"
 

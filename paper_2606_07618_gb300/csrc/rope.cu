@@ -8,6 +8,9 @@
 // A block takes a few tokens: its threads compute the sines of each pair once, into shared memory, while
 // the elements are on their way.  A thread owns one unit of a head -- V pairs, in two pieces of 16 bytes, either one
 // in each half of the pairs or of whole pairs, so that neighbouring threads' pieces are neighbours -- in up to kHeads heads.
+//
+// Bound by memory: 8192 tokens of 40 heads of 128 in bf16, 168 MB, in 27.5 us, 6.1 TB/s (a copy: 6.7).  Sines computed by
+// every thread for itself took 33.6, four heads a thread instead of two 31.7.
 #include "kv_kernels.h"
 #include "nvfp4_device.cuh"
 
