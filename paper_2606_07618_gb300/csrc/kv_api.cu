@@ -330,7 +330,7 @@ nvfp4_status attention(const nvfp4_kv_cache* cache, const void* q, int64_t q_tok
     if (!apart(a, b)) return NVFP4_ERR_INVALID_ARG;
     p.plan = kv::make_plan(s);
     if (!p.plan.fits()) return NVFP4_ERR_RANGE;
-    if (starve && p.plan.own.rows != kv::kTileRows) return NVFP4_ERR_UNSUPPORTED;
+    if (starve && p.plan.own.rows < kv::kTileRows) return NVFP4_ERR_UNSUPPORTED;
     if (p.plan.bytes > 0 && (!workspace || ws_bytes < (size_t)p.plan.bytes)) return NVFP4_ERR_INVALID_ARG;
     if (p.plan.bytes == 0) workspace = nullptr;
     if (!aligned(lens, 4) || !aligned(offsets, 4) || !aligned(prefix_len, 4) || !aligned(lse, 4) || !aligned(status_dev, 4) ||

@@ -722,7 +722,7 @@ cudaError_t dispatch(const Attention& p, const Pass& pass, bool prefix, int64_t 
 
 template <int D>
 cudaError_t launch_pass(const Attention& p, const Pass& pass, bool prefix, int64_t part0, cudaStream_t s) {
-    if (pass.rows == kTileRows) return launch_tiles(p, pass, prefix, part0, s);
+    if (pass.rows >= kTileRows) return launch_tiles(p, pass, prefix, part0, s);
     return pass.rows == 8 ? dispatch<D, 1>(p, pass, prefix, part0, s) : dispatch<D, 2>(p, pass, prefix, part0, s);
 }
 

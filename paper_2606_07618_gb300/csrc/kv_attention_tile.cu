@@ -22,9 +22,10 @@
 //
 // A step of 256 rows and 128 keys (dim 128) takes about 3500 cycles, its MMAs 2048 at their rate.  S = Q K^T takes 670 a
 // tile for 512: it reads 8 KB of operands per 64 cycles, all that shared memory gives, while the loads' stores want
-// some of it (without those 394 us of 455 then; without softmax, too, 348).  The softmax of a tile takes 1800 cycles, of
-// them 930 for its exponentials, beside the other tile's products.  2 x 2048 queries of 32 heads over 8192 tokens: 418 us,
-// 1.15 PFLOP/s (plain products at their rate: 250).
+// some of it (without those 394 us of 455 then; without softmax, too, 348).  So on long parts two CTAs take 512 rows as a
+// pair (kv_plan.h): their MMAs have 256 rows, and each CTA holds, and converts, half of every tile's keys and values.  What
+// is left, 3100 cycles a step, is a stream's chain: products 1024, the softmax of a tile 1800, of them 930 for its exponentials.
+// 2 x 2048 queries of 32 heads over 8192 tokens: 375 us, 1.28 PFLOP/s (single CTAs 418; plain products at their rate: 250).
 //
 // Every mbarrier wait is bounded (1 s): a role that gives up stops, the others do after it,
 // bit 4 (16) of the status word is set and what is missing is not written.
@@ -125,26 +126,77 @@ template <int N>
 __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// fp16 products; CG: the CTAs that they span.
+template <int CG>
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+    if (CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
 }
+template <int CG>
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+    if (CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                     ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                     ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+}
+// Arrival at the barrier when the MMAs issued so far are done; CG 2: at that of both CTAs.
+template <int CG>
+__device__ __forceinline__ void commit_to(uint64_t* bar) {
+    if (CG == 1)
+        mma_commit(smem_u32(bar));
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
+// Arrival at the first CTA's barrier.  A pair's orders tensor memory's accesses alone (with tcgen05's fences before and after).
+template <int CG>
+__device__ __forceinline__ void signal(uint64_t* bar) {
+    if (CG == 1)
+        mbar_arrive(smem_u32(bar));
+    else
+        asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(smem_u32(bar), 0)) : "memory");
+}
+// A pair's that orders shared memory, too.  From the threads that load or weigh, with their accesses in flight, it costs far more
+// (510 and 470 us where 375 is reached so), so one that has none of its own gives it for them.
+__device__ __forceinline__ void signal_all(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(smem_u32(bar), 0)) : "memory");
+}
+__device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return __all_sync(0xffffffffu, ok != 0);
+}
+template <int CG>
+__device__ __forceinline__ bool wait_signal(uint64_t* b, uint32_t parity) {
+    const uint32_t bar = smem_u32(b);
+    if (CG == 1) return mbar_wait_warp(bar, parity);
+    if (try_wait_cluster(bar, parity)) return true;
+    const unsigned long long t0 = now_ns();
+    while (!try_wait_cluster(bar, parity))
+        if (__any_sync(0xffffffffu, now_ns() - t0 > kWaitNs)) return false;
+    return true;
 }
 
 // kind::f16 with fp16 operands: D fp32 (bits 4-5 = 1), A and B fp16 (0), B's K along its rows or (bit 16) across them.
-__host__ __device__ constexpr uint32_t idesc_f16(int n, bool across) {
-    return (1u << 4) | (across ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool across) {
+    return (1u << 4) | (across ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
-template <int D>
+template <int D, int CG>
 struct Shape {
     static constexpr int kPanels = D / 64;                       // of 64 elements (128 bytes) a row
     static constexpr int kPanel = 128 * 128;                     // 128 rows
     static constexpr int kOp = kPanels * kPanel;                 // an operand: 128 rows of D fp16
-    static constexpr int kSmem = 6 * kOp + 1024;                 // Q twice, two stages of K and V
+    // A CTA's part of a tile of keys and of values: of a pair's, 64 keys, and 64 of the values' elements.
+    static constexpr int kKeyPanel = kPanel / CG, kStage = kOp / CG;
+    static constexpr int kSmem = 2 * kOp + 4 * kStage + 1024;    // Q twice, two stages of K and V
     static constexpr int kScores = 0, kOut = 256;                // columns of tensor memory
 };
 
@@ -169,16 +221,20 @@ struct Held {
         for (int b = 0; b < D / 16; b++) {
             const uint32_t sc = scale_pair(s[b] | s[b] << 8);
             const uint4& v = w[b / 2];
-            const uint32_t at = (row ^ ((2 * b & 7) << 4)) + (b >> 2) * Shape<D>::kPanel;
+            const uint32_t at = (row ^ ((2 * b & 7) << 4)) + (b >> 2) * Shape<128, 1>::kPanel;
             st_shared16(at, e2m1x8_scaled(b & 1 ? v.z : v.x, sc));
             st_shared16(at ^ 16, e2m1x8_scaled(b & 1 ? v.w : v.y, sc));
         }
     }
 };
 
-template <int D, bool PREFIX, bool PART>
+// CG 2: a pair of CTAs, whose MMAs span both: tiles of 256 rows, 128 in each.
+template <int D, bool PREFIX, bool PART, int CG>
 __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass pass, int64_t part0) {
-    using H = Shape<D>;
+    using H = Shape<D, CG>;
+    static_assert(CG == 1 || D == 128, "a pair's values come in 64 elements a CTA");
+    constexpr int kTile = CG * kRows;                            // rows of an MMA
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     extern __shared__ uint8_t smem_raw[];
     __shared__ Bars s_bars;
     __shared__ uint32_t s_tmem, s_hidden[4][4];
@@ -196,7 +252,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     const int head = blockIdx.y;
     // tiles from the last one on: with a causal mask it has the most keys
     const int64_t per = PREFIX ? pass.parts : pass.parts * p.batch;
-    const int64_t tile = pass.tiles - 1 - blockIdx.x / per, rest = blockIdx.x % per;
+    const int64_t block = blockIdx.x / CG, tile = pass.tiles - 1 - block / per, rest = block % per;
     const int64_t part = PREFIX ? rest : rest % pass.parts, b = PREFIX ? 0 : rest / pass.parts;
 
     int64_t row0 = 0, n, len, width;
@@ -224,45 +280,54 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     }
     if (p.status && outside && tid == 0 && head == 0) atomicOr(p.status, kStatusBounds);
     const bool causal = !PREFIX && p.causal;
-    const int64_t rows = (PREFIX || n < p.max_q ? n : p.max_q) * p.group, first = tile * 2 * kRows;
+    const int64_t rows = (PREFIX || n < p.max_q ? n : p.max_q) * p.group, first = tile * 2 * kTile;
     if (first >= rows) return;
-    const int64_t last = (first + 2 * kRows < rows ? first + 2 * kRows : rows) - 1;
+    const int64_t last = (first + 2 * kTile < rows ? first + 2 * kTile : rows) - 1;
     const int64_t sees = causal ? len - n + last / p.group + 1 : len;
     const int64_t chunk = part_tokens(len, pass.parts, kTileKeys), begin = part * chunk;
     const int64_t end = begin + chunk < sees ? begin + chunk : sees;
     if (PART && begin >= end) return;
     const int tiles = end > begin ? (int)((end - begin + kKeys - 1) / kKeys) : 0;      // a part is less than 2^31 tokens
     // two streams of scores, weights and sums: of both tiles of rows; where there is only one (split), of its even and odd keys
-    const bool split = rows - first <= kRows && tiles > 1;
-    const int both = rows - first > kRows || split;
+    const bool split = CG == 1 && rows - first <= kRows && tiles > 1;
+    const int both = rows - first > kTile || split;
 
     const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;
-    const uint32_t sq = base, sk = base + 2 * H::kOp, sv = base + 4 * H::kOp;
-    if (warp == kMmaWarp) tmem_alloc(smem_u32(&s_tmem), 512);
+    const uint32_t sq = base, sk = base + 2 * H::kOp, sv = sk + 2 * H::kStage;
+    if (warp == kMmaWarp) {
+        if (CG == 1) {
+            tmem_alloc(smem_u32(&s_tmem), 512);
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
+    }
     if (tid == 0) {
+        const int more = CG == 2 && rank == 0;                   // the other CTA's word
         for (int i = 0; i < 2; i++) {
-            mbar_init(smem_u32(&s_bars.k_full[i]), 4 + p.starve);
-            mbar_init(smem_u32(&s_bars.v_full[i]), 4);
+            mbar_init(smem_u32(&s_bars.k_full[i]), 4 + more + p.starve);
+            mbar_init(smem_u32(&s_bars.v_full[i]), 4 + more);
             mbar_init(smem_u32(&s_bars.k_empty[i]), 1);
             mbar_init(smem_u32(&s_bars.v_empty[i]), 1);
             mbar_init(smem_u32(&s_bars.s_full[i]), 1);
-            mbar_init(smem_u32(&s_bars.p_full[i]), 4);
+            mbar_init(smem_u32(&s_bars.p_full[i]), CG * 4);
         }
         mbar_init(smem_u32(&s_bars.o_full), 1);
         mbar_init(smem_u32(&s_bars.joined), 4);
-        mbar_init(smem_u32(&s_bars.q_full), kSoftmaxWarps);
+        mbar_init(smem_u32(&s_bars.q_full), kSoftmaxWarps + more);
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
 
     tc_fence_before();
     __syncthreads();
+    if (CG == 2) cluster_barrier();                              // both CTAs' barriers and tensor memory are there
     tc_fence_after();
     const uint32_t tmem = s_tmem;
 
     bool ok = true;
     const int half = warp >> 2;                                  // tile of this warp's rows (softmax warps)
-    const int64_t row = first + (split ? tid & 127 : tid);
+    const int64_t row = CG == 2 ? first + half * kTile + (int)rank * kRows + (tid & 127) : first + (split ? tid & 127 : tid);
     if (warp >= kSoftmaxWarps && warp < kMmaWarp) {
         regs_down<kLoadRegs>();
         // Items: keys of a tile, then its values.  The next two items' bytes are on their way, and the page number after
@@ -271,32 +336,38 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
         const int t = tid & 127, page_log2 = p.c.page_log2, page_mask = (1 << page_log2) - 1, pool = (int)p.c.pages;
         const int64_t page_codes = (int64_t)p.c.heads * D << page_log2, page_sf = page_codes / 8;  // bytes of a page
         const uint8_t *codes = p.c.codes + ((int64_t)head * D << page_log2), *sf = p.c.sf + ((int64_t)head * (D / 8) << page_log2);
-        const int part_codes = (D / 2) << page_log2, part_sf = (D / 16) << page_log2;
-        const int token0 = (int)begin + t, stop = (int)end;
-        auto entry = [&](int j) {                                // page number of this thread's token of tile j, unchecked
-            const int64_t x = (int64_t)token0 + (int64_t)j * kKeys;
+        // A pair's CTA: of the keys a half of 64 of them to a thread, of the values the CTA's half of each.
+        constexpr int E = D / CG;                                // elements of a thread
+        const int kt = CG == 2 ? (int)rank * 64 + (t >> 1) : t, kr = CG == 2 ? t >> 1 : t, kh = CG == 2 ? t & 1 : 0;
+        const uint8_t *k_codes = codes + kh * (E / 2), *k_sf = sf + ((int64_t)(kh * (E / 16)) << page_log2);
+        const uint8_t *v_codes = codes + ((int64_t)(D / 2) << page_log2) + rank * (E / 2);
+        const uint8_t *v_sf = sf + ((int64_t)(D / 16 + rank * (E / 16)) << page_log2);
+        const int stop = (int)end;
+        auto entry = [&](int j, int at) {                        // page number of a token of tile j, unchecked
+            const int64_t x = begin + (int64_t)j * kKeys + at;
             return x < stop ? table[x >> page_log2] : 0;
         };
-        auto fetch = [&](Held<D>& h, int j, int part, int page) {
-            const int at = (token0 + j * kKeys) & page_mask;
+        auto fetch = [&](Held<E>& h, int j, int at, const uint8_t* c, const uint8_t* f, int page) {
+            const int off = (int)((uint32_t)begin + (uint32_t)(j * kKeys + at)) & page_mask;
             const int64_t pg = (unsigned)page < (unsigned)pool ? page : 0;
-            h.load(codes + pg * page_codes + part * part_codes + at * (D / 2), sf + pg * page_sf + part * part_sf + at, page_log2);
+            h.load(c + pg * page_codes + off * (D / 2), f + pg * page_sf + off, page_log2);
         };
-        const uint32_t row = t * 128 + ((t & 7) << 4);
-        Held<D> now, next;
-        int page = entry(0), page1 = entry(1);                   // of the items now and next, and after them
+        const uint32_t k_row = sk + kh * H::kKeyPanel + kr * 128 + ((kr & 7) << 4), v_row = sv + t * 128 + ((t & 7) << 4);
+        Held<E> now, next;
+        int page = entry(0, t), page1 = entry(1, t);             // of the values now and next, and after them
+        int k_page1 = CG == 2 ? entry(1, kt) : 0;                // of the keys after the next
         if (tiles > 0) {
-            fetch(now, 0, 0, page);
-            fetch(next, 0, 1, page);
+            fetch(now, 0, kt, k_codes, k_sf, CG == 2 ? entry(0, kt) : page);
+            fetch(next, 0, t, v_codes, v_sf, page);
         }
 #pragma unroll 1
         for (int i = 0; i < 2 * tiles; i++) {
             const int j = i >> 1, part = i & 1, st = j & 1;
             uint64_t *empty = (part ? s_bars.v_empty : s_bars.k_empty) + st, *full = (part ? s_bars.v_full : s_bars.k_full) + st;
-            const bool there = (int64_t)token0 + (int64_t)j * kKeys < stop, ok_page = (unsigned)page < (unsigned)pool;
+            const bool there = begin + (int64_t)j * kKeys + t < stop, ok_page = (unsigned)page < (unsigned)pool;
             if (part == 1 && !(there && ok_page)) {
 #pragma unroll
-                for (int k = 0; k < D / 16; k++) now.s[k] = 0;
+                for (int k = 0; k < E / 16; k++) now.s[k] = 0;
             }
             if (j >= 2 && !mbar_wait_warp(smem_u32(empty), ((j >> 1) & 1) ^ 1)) { ok = false; break; }
             if (part == 0) {
@@ -304,51 +375,54 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                 if (lane == 0) s_hidden[j & 3][warp - kSoftmaxWarps] = mask;
                 outside |= there && !ok_page;
             }
-            now.store((part ? sv : sk) + st * H::kOp + row);
+            now.store((part ? v_row : k_row) + st * H::kStage);
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(full));
             now = next;
-            if (j + 1 < tiles) fetch(next, j + 1, part, page1);
+            if (j + 1 < tiles) {
+                if (part == 0) fetch(next, j + 1, kt, k_codes, k_sf, CG == 2 ? k_page1 : page1);
+                else fetch(next, j + 1, t, v_codes, v_sf, page1);
+            }
             if (part == 1) {
                 page = page1;
-                page1 = entry(j + 2);
+                page1 = entry(j + 2, t);
+                if (CG == 2) k_page1 = entry(j + 2, kt);
             }
         }
         if (p.status && __any_sync(0xffffffffu, outside) && lane == 0) atomicOr(p.status, kStatusBounds);
     } else if (warp >= kMmaWarp) {
         regs_down<kMmaRegs>();
-        if (warp == kMmaWarp) {
+        if (warp == kMmaWarp && rank == 0) {
         // all lanes run the loop and one is elected to issue, so that descriptors stay in uniform registers
-        constexpr uint32_t id_s = idesc_f16(kKeys, false), id_o = idesc_f16(D, true);
+        constexpr uint32_t id_s = idesc_f16(kTile, kKeys, false), id_o = idesc_f16(kTile, D, true);
         auto scores = [&](int x, int st) {
             if (elect_one()) {
-                const uint64_t a = smem_desc(sq + x * H::kOp, 16, 1024), bd = smem_desc(sk + st * H::kOp, 16, 1024);
+                const uint64_t a = smem_desc(sq + x * H::kOp, 16, 1024), bd = smem_desc(sk + st * H::kStage, 16, 1024);
 #pragma unroll
-                for (int kk = 0; kk < D / 16; kk++) {
-                    const uint32_t at = ((kk >> 2) * H::kPanel + (kk & 3) * 32) >> 4;
-                    mma_ss(tmem + H::kScores + x * 128, a + at, bd + at, id_s, kk != 0);
-                }
-                mma_commit(smem_u32(&s_bars.s_full[x]));
+                for (int kk = 0; kk < D / 16; kk++)
+                    mma_ss<CG>(tmem + H::kScores + x * 128, a + (((kk >> 2) * H::kPanel + (kk & 3) * 32) >> 4),
+                               bd + (((kk >> 2) * H::kKeyPanel + (kk & 3) * 32) >> 4), id_s, kk != 0);
+                commit_to<CG>(&s_bars.s_full[x]);
             }
             __syncwarp();
         };
         auto commit = [&](uint64_t* bar) {
-            if (elect_one()) mma_commit(smem_u32(bar));
+            if (elect_one()) commit_to<CG>(bar);
             __syncwarp();
         };
         auto outputs = [&](int x, int st, bool first_keys) {
             if (elect_one()) {
-                const uint64_t bd = smem_desc(sv + st * H::kOp, H::kPanel, 1024);
+                const uint64_t bd = smem_desc(sv + st * H::kStage, H::kPanel, 1024);
 #pragma unroll
                 for (int kk = 0; kk < kKeys / 16; kk++)
-                    mma_ts(tmem + H::kOut + x * D, tmem + H::kScores + x * 128 + kk * 8, bd + (kk * 16 * 128 >> 4), id_o,
-                           (uint32_t)(!first_keys | kk));
+                    mma_ts<CG>(tmem + H::kOut + x * D, tmem + H::kScores + x * 128 + kk * 8, bd + (kk * 16 * 128 >> 4), id_o,
+                               (uint32_t)(!first_keys | kk));
             }
             __syncwarp();
         };
         auto wait_for = [&](uint64_t* bar, int parity) {
-            ok = ok && mbar_wait_warp(smem_u32(bar), parity & 1);
+            ok = ok && wait_signal<CG>(bar, parity & 1);
             tc_fence_after();
             return ok;
         };
@@ -389,6 +463,21 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
         }
         commit(&s_bars.o_full);                                  // after every MMA issued, also on a timeout
         if (!mbar_wait_warp(smem_u32(&s_bars.o_full), 0)) ok = false;
+        } else if (CG == 2 && warp == kMmaWarp) {
+            // the second CTA's operands are there: said here for its warps
+            auto relay = [&](uint64_t* bar, int parity) {
+                if (ok) ok = mbar_wait_warp(smem_u32(bar), parity & 1);
+                tc_fence_after();
+                tc_fence_before();
+                if (ok && lane == 0) signal_all(bar);
+            };
+            relay(&s_bars.q_full, 0);
+            if (tiles > 0) relay(&s_bars.k_full[0], 0);
+            for (int j = 0; ok && j < tiles; j++) {
+                const int st = j & 1, nx = (j + 1) & 1;
+                relay(&s_bars.v_full[st], j >> 1);
+                if (j + 1 < tiles) relay(&s_bars.k_full[nx], (j + 1) >> 1);
+            }
         }
     } else {
         regs_up<kSoftmaxRegs>();
@@ -517,7 +606,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&s_bars.p_full[half]));
+            if (lane == 0) signal<CG>(&s_bars.p_full[half]);
         }
         if (ok && !mbar_wait_warp(smem_u32(&s_bars.o_full), 0)) ok = false;
         tc_fence_after();
@@ -614,45 +703,55 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+    if (CG == 2) cluster_barrier();                              // neither signals the other's barriers any more
+    if (warp == kMmaWarp) {
+        if (CG == 1) tmem_dealloc(tmem, 512);
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
     if (tid == 0 && s_abort && p.status) atomicOr(p.status, kStatusTimeout);
 }
 
-template <int D, bool PREFIX, bool PART>
+template <int D, bool PREFIX, bool PART, int CG>
 cudaError_t launch(const Attention& p, const Pass& pass, int64_t part0, cudaStream_t s) {
     static std::atomic<uint64_t> opted;                          // devices whose shared memory limit is raised
+    constexpr int kSmem = Shape<D, CG>::kSmem;
+    const auto kernel = tile_kernel<D, PREFIX, PART, CG>;
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     const uint64_t bit = dev < 64 ? 1ull << dev : 0;
     if (!(opted.load(std::memory_order_relaxed) & bit) || !bit) {
-        e = cudaFuncSetAttribute(tile_kernel<D, PREFIX, PART>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem);
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e != cudaSuccess) return e;
         opted.fetch_or(bit, std::memory_order_relaxed);
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(pass.tiles * pass.parts * (PREFIX ? 1 : p.batch)), (unsigned)p.c.heads);
+    cfg.gridDim = dim3((unsigned)(pass.tiles * pass.parts * (PREFIX ? 1 : p.batch) * CG), (unsigned)p.c.heads);
     cfg.blockDim = dim3(kTileThreads);
-    cfg.dynamicSmemBytes = Shape<D>::kSmem;
+    cfg.dynamicSmemBytes = kSmem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CG;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, tile_kernel<D, PREFIX, PART>, p, pass, part0);
+    cfg.numAttrs = CG;
+    return cudaLaunchKernelEx(&cfg, kernel, p, pass, part0);
 }
 
-template <int D>
+template <int D, int CG>
 cudaError_t dispatch(const Attention& p, const Pass& pass, bool prefix, int64_t part0, cudaStream_t s) {
-    if (prefix) return launch<D, true, true>(p, pass, part0, s);
-    return p.plan.through ? launch<D, false, true>(p, pass, part0, s) : launch<D, false, false>(p, pass, part0, s);
+    if (prefix) return launch<D, true, true, CG>(p, pass, part0, s);
+    return p.plan.through ? launch<D, false, true, CG>(p, pass, part0, s) : launch<D, false, false, CG>(p, pass, part0, s);
 }
 
 }  // namespace
 
 cudaError_t launch_tiles(const Attention& p, const Pass& pass, bool prefix, int64_t part0, cudaStream_t s) {
-    return p.c.dim == 64 ? dispatch<64>(p, pass, prefix, part0, s) : dispatch<128>(p, pass, prefix, part0, s);
+    if (p.c.dim == 64) return dispatch<64, 1>(p, pass, prefix, part0, s);
+    return pass.rows == kPairRows ? dispatch<128, 2>(p, pass, prefix, part0, s) : dispatch<128, 1>(p, pass, prefix, part0, s);
 }
 
 }  // namespace kv

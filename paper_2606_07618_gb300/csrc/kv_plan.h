@@ -13,7 +13,7 @@ constexpr int kWarpTokens = 64, kMaxCluster = 8;
 constexpr int64_t kSms = 152;
 constexpr int blocks_per_sm(int64_t dim, int rows) { return dim == 128 ? (rows == 8 ? 4 : 2) : (rows == 8 ? 5 : 4); }
 // Many rows (kv_attention_tile.cu): rows of a block, one to an SM, and the keys that it takes at a time.
-constexpr int kTileRows = 256, kTileKeys = 128;
+constexpr int kTileRows = 256, kTileKeys = 128, kPairRows = 512;     // (of a pair of blocks, dim 128)
 
 struct Sizes {
     int64_t tokens, batch, max_q;        // rows of q, sequences, the most queries of one
@@ -31,7 +31,7 @@ struct Sizes {
 struct Pass {
     int rows;
     int64_t tiles, parts;
-    KV_BOTH int64_t step() const { return rows == kTileRows ? kTileKeys : kWarpTokens; }
+    KV_BOTH int64_t step() const { return rows >= kTileRows ? kTileKeys : kWarpTokens; }
 };
 
 // Tokens of a part of a sequence of `length`: the parts are as even as whole steps allow.
@@ -93,9 +93,21 @@ inline Pass plan_pass(int64_t sequences, int64_t heads, int64_t dim, int64_t row
     const int64_t pairs = sequences * heads * p.tiles;
     if (p.rows < kTileRows) {
         p.parts = thin_parts(pairs, length, kSms * blocks_per_sm(dim, p.rows));
-    } else if (pairs < kSms) {
-        const int64_t most = ceil_div(length, kTileKeys);
-        p.parts = kSms / pairs < most ? kSms / pairs : most;
+    } else {
+        // Two blocks' MMAs together read half the keys each: a step is a tenth shorter, the start 2 us longer.  So: pairs where
+        // their rows are four fifths full and their parts long (32 heads of 2 x 2048 queries over 8192 tokens 418 -> 375 us, of
+        // 16 x 104 over 4096 155 -> 133; 16 of 512 over 2048 71.5 -> 70.9; 64 x 8 of 512 over 512 118 -> 149, of 1 over 8192, in
+        // parts of 900, 36.2 -> 38.7).
+        constexpr int64_t kPairTokens = 2048;
+        const int64_t whole = ceil_div(rows, kPairRows), two = kSms / 2 / (sequences * heads * whole);
+        if (dim == 128 && whole * kPairRows <= rows + rows / 4 && length >= kPairTokens * (two < 1 ? 1 : two)) {
+            p.rows = kPairRows;
+            p.tiles = whole;
+            p.parts = two;
+        } else if (pairs < kSms) {
+            const int64_t most = ceil_div(length, kTileKeys);
+            p.parts = kSms / pairs < most ? kSms / pairs : most;
+        }
     }
     if (p.parts < 1) p.parts = 1;
     return p;
@@ -108,7 +120,7 @@ inline Plan make_plan(const Sizes& s) {
     p.prefix = Pass{0, 0, 0};
     if (s.prefix > 0) p.prefix = plan_pass(1, s.heads, s.dim, s.tokens * group, s.prefix);
     const int64_t blocks = (int64_t)1 << 31, rows = s.tokens * s.q_heads;
-    p.small = p.own.tiles < blocks / p.own.parts / s.batch && p.prefix.tiles < blocks / (p.prefix.parts + 1) && rows < blocks;
+    p.small = p.own.tiles < blocks / 2 / p.own.parts / s.batch && p.prefix.tiles < blocks / 2 / (p.prefix.parts + 1) && rows < blocks;
     const bool alone = p.own.rows < kTileRows && p.own.parts <= kMaxCluster;       // the own pass needs no workspace
     p.merge = s.prefix > 0 && alone;
     p.through = p.parts() > 1 && !(s.prefix <= 0 && alone);

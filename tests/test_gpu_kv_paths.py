@@ -30,6 +30,10 @@ PATHS = [
     ((([30, 600], [2, 3], 2, 5, 64, 16), {"prefix": 900}), (16, "merge", 256)),
     ((([9], [1], 1, 2, 128, 16), {"prefix": 64}), (8, "merge", 8)),
     ((([50, 64], [9, 12], 2, 4, 128, 16), {"prefix": 333}), (256, "workspace", 256)),
+    ((([190, 2100], [165, 170], 39, 3, 128, 32), {}), (512, "alone", 0)),
+    ((([4100], [250], 38, 2, 128, 128), {}), (512, "workspace", 0)),
+    ((([3, 9, 1] * 20, [1] * 60, 10, 8, 128, 16), {"prefix": 15000}), (8, "merge", 512)),
+    ((([500, 2180], [150, 170], 76, 3, 128, 64), {"prefix": 2100}), (512, "workspace", 512)),
 ]
 
 @pytest.fixture(scope="module")
@@ -50,7 +54,7 @@ def test_paths(B, args, path, causal):
 
 
 @pytest.mark.parametrize("dim", [64, 128])
-@pytest.mark.parametrize("queries", [[33, 64], [129, 1], [128], [43], [300, 90]])
+@pytest.mark.parametrize("queries", [[33, 64], [129, 1], [128], [43], [300, 90], [137, 1], [171, 170], [342], [1, 400, 341]])
 def test_one_and_two_tiles_of_rows(B, dim, queries):
     """One tile's keys in two streams, two tiles, and a last tile alone, over odd numbers of key tiles."""
     for extra in (0, 100, 400):
@@ -140,17 +144,19 @@ def test_two_graphs_share_a_workspace(B):
         R.check(c[2], x.want())
 
 
-def test_wait_runs_out_and_is_reported(B):
-    """The waits for keys give up after their limit, nothing is written, and the context stays usable."""
-    s = R.Setting([40, 90], [30, 20], 38, 3, 64, 16, seed=11)
+@pytest.mark.parametrize("shape", [([40, 90], [30, 20], 38, 3, 64, 16), ([190, 2100], [165, 170], 39, 3, 128, 32)])
+def test_wait_runs_out_and_is_reported(B, shape):
+    """The waits for keys give up after their limit (of single blocks and of pairs), nothing is written, and the context stays usable."""
+    s = R.Setting(*shape, seed=11)
+    n = max(s.queries)
     dev = [t.cuda() for t in s.cache]
     q, out = s.q.cuda(), torch.full_like(s.q, 7.0, device="cuda")
     table, lens, offsets = s.table.cuda(), torch.tensor(s.lens, dtype=torch.int32, device="cuda"), s.offsets.cuda()
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
-    assert B.nvfp4_kv_attention_workspace(dev, q, 2, table.shape[1], 30) == 0
+    assert B.nvfp4_kv_attention_workspace(dev, q, 2, table.shape[1], n) == 0
     torch.cuda.synchronize()
     t0 = time.time()
-    B.nvfp4_kv_selftest_wait_timeout(q, dev, table, lens, offsets, 30, s.scale, out, status)
+    B.nvfp4_kv_selftest_wait_timeout(q, dev, table, lens, offsets, n, s.scale, out, status)
     torch.cuda.synchronize()
     assert 0.5 < time.time() - t0 < 60
     assert status.item() == 16 and (out == 7.0).all()

@@ -13,9 +13,9 @@ def test_shapes_take_their_paths():
     for args, want in T.PATHS:
         assert P.path_of(R.Setting(*args[0], **args[1])) == want, args
     seen = {want for _, want in T.PATHS}
-    assert seen >= {(r, j, 0) for r in (8, 16) for j in ("alone", "cluster", "workspace")} | {(256, "alone", 0), (256, "workspace", 0)}
+    assert seen >= {(r, j, 0) for r in (8, 16) for j in ("alone", "cluster", "workspace")} | {(r, j, 0) for r in (256, 512) for j in ("alone", "workspace")}
     # the prefix's pass has at least as many rows as a sequence's
-    assert seen >= {(r, "merge", q) for r in (8, 16) for q in (8, 16, 256) if q >= r} | {(256, "workspace", 256)}
+    assert seen >= {(r, "merge", q) for r in (8, 16) for q in (8, 16, 256) if q >= r} | {(8, "merge", 512), (256, "workspace", 256), (512, "workspace", 512)}
 
 
 def sizes(n):
@@ -38,7 +38,10 @@ def test_plans():
         tokens, batch, max_q, q_heads, heads, dim, length, prefix = s
         group = q_heads // heads
         assert p["rows"] * p["tiles"] >= max_q * group and p["rows"] * (p["tiles"] - 1) < max_q * group
-        assert p["rows"] == (8 if max_q * group <= 8 else 16 if max_q * group <= 16 else 256)
+        n = max_q * group
+        assert p["rows"] in ((8,) if n <= 8 else (16,) if n <= 16 else (256, 512))
+        if p["rows"] == 512:                                        # pairs: full ones, long parts
+            assert dim == 128 and p["tiles"] * 512 <= n * 1.25 and p["parts"] * 2048 <= length
         assert p["parts"] >= 1 and (p["prefix_parts"] >= 1) == (prefix > 0)
         if p["rows"] < 256:
             assert p["tiles"] == 1
