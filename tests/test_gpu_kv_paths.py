@@ -33,7 +33,7 @@ PATHS = [
     ((([190, 2100], [165, 170], 39, 3, 128, 32), {}), (512, "alone", 0)),
     ((([4100], [250], 38, 2, 128, 128), {}), (512, "workspace", 0)),
     ((([3, 9, 1] * 20, [1] * 60, 10, 8, 128, 16), {"prefix": 15000}), (8, "merge", 512)),
-    ((([500, 2180], [150, 170], 76, 3, 128, 64), {"prefix": 2100}), (512, "workspace", 512)),
+    ((([500, 2180], [150, 170], 38, 3, 128, 64), {"prefix": 2100}), (512, "workspace", 512)),
 ]
 
 @pytest.fixture(scope="module")
