@@ -1,5 +1,6 @@
 """Every path of attention over the cache -- few and many rows, parts alone, in clusters and through the workspace, with and
 without a prefix -- against 64 bits, at shapes that test_kv_plans.py shows to take them."""
+import math
 import time
 
 import pytest
@@ -31,6 +32,7 @@ PATHS = [
     ((([9], [1], 1, 2, 128, 16), {"prefix": 64}), (8, "merge", 8)),
     ((([50, 64], [9, 12], 2, 4, 128, 16), {"prefix": 333}), (256, "workspace", 256)),
     ((([190, 2100], [165, 170], 39, 3, 128, 32), {}), (512, "alone", 0)),
+    ((([0, 2100, 160], [165, 170, 169], 26, 3, 128, 32), {}), (512, "alone", 0)),
     ((([4100], [250], 38, 2, 128, 128), {}), (512, "workspace", 0)),
     ((([3, 9, 1] * 20, [1] * 60, 10, 8, 128, 16), {"prefix": 15000}), (8, "merge", 512)),
     ((([500, 2180], [150, 170], 38, 3, 128, 64), {"prefix": 2100}), (512, "workspace", 512)),
@@ -100,6 +102,77 @@ def test_pages_shared_and_out_of_order(B):
     s.table[1] = s.table[0].flip(0)
     out, lse = s.run(B)
     R.check(out, s.want(), lse)
+
+
+@pytest.mark.parametrize("shape", [([40], [1], 2, 4, 128, 16), ([40, 300], [3, 70], 2, 4, 128, 16), ([300, 40], [70, 40], 1, 3, 64, 16),
+                                   ([180, 2100], [165, 170], 38, 3, 128, 32)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_hidden_pages_and_queries_that_are_not_finite(B, shape, causal):
+    """Page numbers outside the pool hide their tokens of every kernel (page 0, which none holds, is NaN); a NaN and an infinity
+    stay in their rows."""
+    s = R.Setting(*shape, seed=21)
+    free = next(i for i in range(s.cache[0].shape[0]) if not (s.table == i).any())
+    s.table[s.table == 0] = free
+    for t in s.cache[:2]:
+        t[free] = t[0]
+    s.cache[1][0] = 0x7F
+    b, n, m = len(s.lens) - 1, s.lens[-1], s.queries[-1]
+    row, good = s.table[b].clone(), torch.ones(n, dtype=torch.bool)
+    for i, bad in ((0, -1), (2, s.cache[0].shape[0]), ((n - 1) // s.page, 2 ** 31 - 1)):
+        s.table[b, i] = bad
+        good[i * s.page:(i + 1) * s.page] = False
+    q, status = s.q.cuda(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    q[0, 1, 3], q[-1, -1, 9] = math.nan, math.inf
+    out, lse = s.run(B, causal, q=q, status=status)
+    assert status.item() == 4
+    k, v = (R.tokens_of(R.values(s.cache, i), row, n)[:, good] for i in (0, 1))
+    sees = good.long().cumsum(0)[(n - m + torch.arange(m)).clamp(min=0) if causal else torch.full((m,), n - 1)]
+    assert not causal or n >= m
+    last = R.attention(s.q[-m:].double().view(m, s.heads, s.group, s.dim), k, v, s.scale, sees)
+    rest = R.Setting(*shape, seed=21)
+    rest.table, rest.cache = s.table.clone(), s.cache
+    rest.table[b] = row
+    want = [torch.cat((w[:-m], x)) for w, x in zip(rest.want(causal), last)]
+    nan = torch.zeros(s.total, s.heads * s.group, dtype=torch.bool)
+    nan[0, 1] = nan[-1, -1] = True
+    assert torch.equal(torch.isnan(out.cpu()).all(-1), nan) and torch.equal(torch.isnan(out.cpu()).any(-1), nan)
+    want = [w.masked_fill(nan.view(s.total, s.heads, s.group, *[1] * (w.dim() - 3)), 0) for w in want]
+    R.check(out.masked_fill(nan.cuda()[..., None], 0), want)
+
+
+@pytest.mark.parametrize("queries", [1, 4, 20, 170])
+def test_a_pool_past_4_gb(B, queries):
+    """The same bits from pages at the end of a pool whose offsets pass 32 bits."""
+    s = R.Setting([2100], [queries], 38, 3, 128, 64, seed=22)
+    pages, heads = s.cache[0].shape[:2]
+    total = 2 ** 33 // (heads * 64 * 128) + 7
+    want = s.run(B)
+    codes = torch.empty(total, *s.cache[0].shape[1:], dtype=torch.uint8, device="cuda")
+    sf = torch.empty(total, *s.cache[1].shape[1:], dtype=torch.uint8, device="cuda")
+    codes[-pages:], sf[-pages:] = s.cache[0].cuda(), s.cache[1].cuda()
+    s.cache = (codes, sf, *s.cache[2:])
+    s.table += (total - pages)
+    for a, b in zip(s.run(B), want):
+        assert torch.equal(a, b)
+    # read back, and written again at the end
+    cache = (codes, sf, *(t.cuda() for t in s.cache[2:]))
+    k = torch.empty(2100, heads, 128, device="cuda")
+    v = torch.empty_like(k)
+    table, offsets = s.table.cuda(), torch.tensor([0, 2100], dtype=torch.int32, device="cuda")
+    B.nvfp4_kv_read(cache, table, None, offsets, k, v)
+    for i, x in enumerate((k, v)):
+        assert torch.equal(R.tokens_of(R.values((codes[-pages:].cpu(), sf[-pages:].cpu(), *s.cache[2:]), i), s.table[0] - (total - pages), 2100)
+                           .permute(1, 0, 2).float(), x.cpu())
+    slots = (s.table[0].long().repeat_interleave(64) * 64 + torch.arange(64).repeat(s.table.shape[1]))[:2100].cuda()
+    B.nvfp4_kv_write(cache, k, v, slots, B.NVFP4_KV_ABSMAX)
+    small = tuple(torch.zeros(pages, *t.shape[1:], dtype=torch.uint8, device="cuda") for t in (codes, sf)) + cache[2:]
+    B.nvfp4_kv_write(small, k, v, slots - (total - pages) * 64, B.NVFP4_KV_ABSMAX)
+    used = torch.zeros(pages * 64, dtype=torch.bool, device="cuda")
+    used[slots - (total - pages) * 64] = True
+    used = used.view(pages, 64)
+    for a, b, at in ((codes, small[0], 3), (sf, small[1], 4)):
+        a = a[-pages:].movedim(at, 1)[used]
+        assert torch.equal(a, b.movedim(at, 1)[used])
 
 
 def test_streams(B):
