@@ -84,6 +84,20 @@ def test_prefix_alone(B):
         R.check(out, s.want())
 
 
+@pytest.mark.parametrize("queries", [1, 40])
+def test_a_prefix_of_no_pages(B, queries):
+    """No prefix at all, by the call that takes one."""
+    s = R.Setting([300, 50], [queries, 1], 2, 4, 128, 16, seed=4)
+    want = s.run(B)
+    cache = tuple(t.cuda() for t in s.cache)
+    q, table, lens, offsets = s.q.cuda(), s.table.cuda(), torch.tensor(s.lens, dtype=torch.int32, device="cuda"), s.offsets.cuda()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    none, zero = torch.empty(0, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(B.nvfp4_kv_attention_workspace(cache, q, 2, table.shape[1], queries), dtype=torch.uint8, device="cuda")
+    B.nvfp4_kv_attention_prefix(q, cache, none, zero, table, lens, offsets, queries, s.scale, out, True, lse, ws)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
 def test_fewer_queries_than_max_q(B):
     """max_q above the longest sequence's queries, and below it: those past it are not computed."""
     s = R.Setting([90, 40], [3, 1], 2, 4, 64, 16, seed=5)
