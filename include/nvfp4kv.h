@@ -126,8 +126,8 @@ nvfp4_status nvfp4_kv_read(const nvfp4_kv_cache* cache, const int32_t* table, in
  *   q, out  [tokens, q_heads, dim] bf16, strides of a token and a head; q_heads a multiple of
  *           the cache's heads.  lse optional [tokens, q_heads] fp32.
  *   table   [batch] rows of `width` page numbers, table_ld apart; entries behind a
- *           sequence's last page are not read.  lens past width * page count as that and set bit 2; a page
- *           number outside the pool hides its tokens and sets bit 2.
+ *           sequence's last page are not read; width * page at most 2^31 - 2048.  lens past width * page
+ *           count as that and set bit 2; a page number outside the pool hides its tokens and sets bit 2.
  *   offsets [batch + 1], not falling, from 0 to at most `tokens`; no sequence has more than max_q queries (those past
  *           it are not computed).  Rows past offsets[batch] are left as they are.
  *   scale   finite and >= 0.
@@ -158,8 +158,8 @@ nvfp4_status nvfp4_kv_selftest_wait_timeout(const nvfp4_kv_cache* cache, const v
 
 /*
  * The same as nvfp4_kv_attention for a batch that shares a prefix: every query also sees the first *prefix_len
- * tokens of the pages prefix[0 .. prefix_width), before its own sequence's (table, lens,
- * offsets and the causal rule as above; a sequence may have no tokens of its own cached).
+ * tokens of the pages prefix[0 .. prefix_width), before its own sequence's (prefix_width * page at most 2^31 - 2048;
+ * table, lens, offsets and the causal rule as above; a sequence may have no tokens of its own cached).
  * The prefix's keys and values are read once for all queries of the batch.
  */
 nvfp4_status nvfp4_kv_attention_prefix(const nvfp4_kv_cache* cache, const void* q, int64_t q_token, int64_t q_head,

@@ -300,7 +300,7 @@ nvfp4_status attention_sizes(const nvfp4_kv_cache* c, int64_t tokens, int q_head
     if (tokens < 0 || batch < 0 || width < 0 || max_q < 0 || prefix_width < 0) return NVFP4_ERR_INVALID_ARG;
     if (q_heads < 1 || q_heads % c->heads) return NVFP4_ERR_INVALID_ARG;
     if (q_heads > kMaxHeads || tokens > kMaxTokens || batch > kMaxTokens || max_q > kMaxTokens) return NVFP4_ERR_RANGE;
-    if (width > INT_MAX / c->page || prefix_width > INT_MAX / c->page) return NVFP4_ERR_RANGE;
+    if (width > kv::kMaxLength / c->page || prefix_width > kv::kMaxLength / c->page) return NVFP4_ERR_RANGE;
     if (max_q > tokens) max_q = tokens;
     *s = kv::Sizes{tokens, batch, max_q, q_heads, c->heads, c->dim, width * c->page, prefix_width * c->page};
     return NVFP4_OK;

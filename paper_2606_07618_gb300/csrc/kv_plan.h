@@ -15,6 +15,10 @@ constexpr int blocks_per_sm(int64_t dim, int rows) { return dim == 128 ? (rows =
 // Many rows (kv_attention_tile.cu): rows of a block, one to an SM, and the keys that it takes at a time.
 constexpr int kTileRows = 256, kTileKeys = 128, kPairRows = 512;     // (of a pair of blocks, dim 128)
 
+// Most tokens that a table can hold: the kernels' token numbers are ints, which pass the last token by up to a block's start
+// (192), two tiles of 256 and 48 within one, and a part's tokens round up to a step.
+constexpr int64_t kMaxLength = ((int64_t)1 << 31) - 2048;
+
 struct Sizes {
     int64_t tokens, batch, max_q;        // rows of q, sequences, the most queries of one
     int q_heads, heads, dim;

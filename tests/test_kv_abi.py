@@ -186,6 +186,20 @@ def test_attention_refusals(B, prefix):
         assert a(ws=FAKE) == INVALID
 
 
+@pytest.mark.parametrize("page", [16, 64, 512, 1024])
+def test_longest_tables(B, page):
+    """width * page up to 2^31 - 2048 tokens, of a sequence's pages and of a prefix's: past that the kernels' token numbers, which look
+    ahead of the last one, would not fit 31 bits.  (What is accepted goes on to the check that looks the pointers up, and fails that.)"""
+    most = (2 ** 31 - 2048) // page
+    c, pre = cache(B, page=page), lambda n: (FAKE + 0x100000000, n, FAKE + 0x6300000)  # noqa: E731
+    far = dict(c=c, table=FAKE + 0x40000000, ws=FAKE + 0x200000000)
+    assert attend(B, batch=1, width=most, ld=most, **far) == INVALID
+    assert attend(B, batch=1, width=most + 1, ld=most + 1, **far) == RANGE
+    assert attend(B, prefix=pre(most), **far) == INVALID and attend(B, prefix=pre(most + 1), **far) == RANGE
+    size = lambda w, n: B.lib().nvfp4_kv_attention_workspace(c, 1, 4, 1, w, 1, n)  # noqa: E731
+    assert size(most, 0) > 0 and size(most + 1, 0) == 0 and size(8, most) > 0 and size(8, most + 1) == 0
+
+
 def test_selftest_refusals(B):
     L = B.lib()
     t = lambda heads=40, st=FAKE + 0x7000000: L.nvfp4_kv_selftest_wait_timeout(

@@ -64,6 +64,24 @@ def test_parts_cover_the_keys():
         assert L.tokens_of32(length, parts, step) == n
 
 
+def test_token_numbers_fit_31_bits():
+    """The kernels' numbers at the longest tables: where a warp of four starts, its next pages (two tiles of 256 tokens on, 48 within
+    one) and a part's tokens as an int, and the tile kernel's key numbers two tiles behind the last."""
+    most, L = 2 ** 31 - 2048, P.lib()
+    for length in (most, most - 1, most - 63, most - 5000, 2 ** 30 + 1):
+        for parts in list(range(1, 9)) + [19, 152, 608, 760]:
+            chunk = L.tokens_of32(length, parts, 64)
+            assert chunk < 2 ** 31 and chunk * parts >= length
+            # parts that join in a cluster all run; others return where they have no keys
+            last = parts - 1 if parts <= 8 else (length - 1) // chunk
+            assert last * chunk + 3 * 64 + 2 * 256 + 48 < 2 ** 31
+            assert length - 1 + 2 * 256 + 48 < 2 ** 31
+            tiles = -(-L.tokens_of(length, parts, 128) // 128)
+            assert (tiles + 1) * 128 + 127 < 2 ** 31
+    p = P.plan_of(1, 1, 1, 4, 1, 128, most)
+    assert p["fits"] and p["parts"] * P.lib().tokens_of32(most, p["parts"], 64) >= most
+
+
 def test_rows_divide_by_a_multiplication():
     """Row r of a block of few rows belongs to query r / group: r (65536 / group + 1) >> 16."""
     for group in range(1, 17):
