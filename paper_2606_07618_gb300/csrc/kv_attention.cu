@@ -370,6 +370,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
     for (int k0 = start; k0 < end; k0 += kStride) {
         const bool kv_ok = kpg >= 0, vv_ok = vpg >= 0, more = k0 + kStride < end;
         copy_wait<1>();
+        __syncwarp();                                            // lanes had page numbers of their own to fetch
         uint32_t ks[T::KB][4];
 #pragma unroll
         for (int i = 0; i < T::KB; i++) ld_shared(m_ks + i * 512, ks[i]);
@@ -445,6 +446,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
 #pragma unroll
                     for (int i = 0; i < D / 16; i++) o[nt][i][c] *= alpha, o[nt][i][c + 2] *= alpha;
                 }
+            __syncwarp();
         }
         uint32_t pt[NT][4][2];
 #pragma unroll
@@ -473,6 +475,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
                 for (int c = 0; c < 4; c++)
                     if (!vv_ok || k0 + 16 * t + 4 * j + c >= end) vs[j] &= ~(0xFFu << (8 * c));
         }
+        __syncwarp();
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const uint32_t s01 = e4m3x2_to_f16(vs[i] & 0xFFFF), s23 = e4m3x2_to_f16(vs[i] >> 16);
@@ -572,6 +575,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
         }
     }
     if (JOIN == kCluster) {
+        __syncwarp();                                            // half a warp may have had a row more
         cluster_arrive();
         cluster_wait();
         for (int x = (int)part * kThreads + threadIdx.x; x < rows * (D / 4); x += (int)parts * kThreads) {
@@ -594,6 +598,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
             const int i = query_of(r);
             write_row<D, false>(p, 0, row0 + i, (int64_t)head * group + (r - i * group), 4 * q, v, top, sum, merge);
         }
+        __syncwarp();
         cluster_arrive();                                        // a block's memory stays until the others have read it
         cluster_wait();
     }

@@ -551,6 +551,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
 #pragma unroll
                     for (int i = 0; i < 32; i++)
                         if (32 * c + i >= left || (hid[c] >> i & 1)) v[c][i] = neg_inf();
+                __syncwarp();
             }
             float tops[4];
 #pragma unroll
@@ -569,6 +570,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                 const float alpha = !grown ? 1.0f : m == neg_inf() ? 0.0f : ex2(m - top);
                 if (grown) m = top;
                 l *= alpha;
+                __syncwarp();                                    // the lanes together for tensor memory
                 if (turn > 0) {
 #pragma unroll 1
                     for (int c = 0; c < D; c += 16) {
@@ -646,6 +648,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
             const float f = PART ? 1.0f : ld_f32(p.c.S_v) / l;
             const bool empty = l == 0.0f;                        // saw nothing
             const bool valid = row < rows;
+            __syncwarp();
 #pragma unroll
             for (int c = 0; c < D; c += 16) {
                 float o[16], z[16];
@@ -665,15 +668,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                 }
 #pragma unroll
                 for (int i = 0; i < 16; i++) o[i] = empty ? 0.0f : o[i] * f;
-                if (!valid) continue;
-                if (PART) {
+                if (valid && PART) {
                     float* d = static_cast<float*>(p.workspace) + at * D + c;
                     uint32_t u[16];
 #pragma unroll
                     for (int i = 0; i < 16; i++) u[i] = __float_as_uint(o[i]);
                     st_global32(d, u);
                     st_global32(d + 8, u + 8);
-                } else {
+                } else if (valid) {
                     uint32_t w[8];
 #pragma unroll
                     for (int i = 0; i < 8; i++)
@@ -686,6 +688,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                         for (int i = 0; i < 16; i++) d[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
                     }
                 }
+                __syncwarp();                                    // lanes without a row stored nothing
             }
             if (valid) {
                 // a NaN sum shows in both
