@@ -121,8 +121,9 @@ nvfp4_status nvfp4_kv_read(const nvfp4_kv_cache* cache, const int32_t* table, in
  * query head h with the keys and values of head h / (q_heads / heads).  A query that sees
  * nothing gets out = 0 and lse = -inf.  Cached values and queries are exact in the products
  * (the queries up to 2^-25 of their row's largest), sums and softmax statistics in fp32; the weights are rounded to fp16
- * (by up to 2^-11, those below 2^-21 of the row's largest by up to 2^-32 of it) for the product
- * with the values, and the result once to bf16.
+ * (by up to 2^-11, those below 2^-21 of the row's largest by up to 2^-32 of it, 2^-25 where logits pass 2^22) for the
+ * product with the values, and the result once to bf16.  Logits (of base 2, scale q.k log2 e) are rounded to fp32 and may have any size
+ * that it holds: a key whose logit lies far above the others' takes all the weight, keys that tie share it.
  *   q, out  [tokens, q_heads, dim] bf16, strides of a token and a head; q_heads a multiple of
  *           the cache's heads.  lse optional [tokens, q_heads] fp32.
  *   table   [batch] rows of `width` page numbers, table_ld apart; entries behind a

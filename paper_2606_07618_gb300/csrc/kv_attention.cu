@@ -349,6 +349,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
             const int r = 8 * nt + 2 * t + c;
             fac[nt][c] = S * __shfl_sync(0xffffffffu, up, (2 * t + c) * 4);
             if (fac[nt][c] == 0.0f) fac[nt][c] = 1e-37f;         // hidden scores, -inf, stay that
+            if (fac[nt][c] > kWideFactor) least = INT_MIN;
             lim[nt][c] = r < rows ? shift + each * query_of(r) : 0;
             if (r < rows) least = min(least, lim[nt][c]);
             m[nt][c] = neg_inf();
@@ -357,6 +358,19 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
     }
     least = min(least, __shfl_xor_sync(0xffffffffu, least, 1));
     least = min(least, __shfl_xor_sync(0xffffffffu, least, 2));
+    // wide rows: every tile takes the masks' branch, which has the first factors
+    const bool wide = least == INT_MIN;
+    if (wide) {
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+                const bool first = fac[nt][c] > kWideFactor;
+                if (g == 0) s_m[warp][8 * nt + 2 * t + c] = first ? fac[nt][c] : 1.0f;
+                if (first) fac[nt][c] = 1.0f;
+            }
+        __syncwarp();
+    }
     float o[NT][D / 16][4];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++)
@@ -416,6 +430,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
 #pragma unroll
                     for (int c = 0; c < 4; c++) {
                         const int j = k0 + 16 * (g >> 1) + 4 * i + (g & 1) + (c & 2);
+                        if (wide) sc[nt][i][c] = __fmul_rn(sc[nt][i][c], s_m[warp][8 * nt + 2 * t + (c & 1)]);
                         if (!kv_ok || j >= lim[nt][c & 1] || j >= end) sc[nt][i][c] = neg_inf();
                     }
         }
@@ -432,15 +447,16 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
 #pragma unroll
                 for (int i = 4; i < 32; i *= 2) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, i));
                 top[nt][c] = x * fac[nt][c];
-                grown |= !(top[nt][c] <= m[nt][c] + kGrowth);        // NaN: it becomes the maximum
+                grown |= !(top[nt][c] <= __fadd_rd(m[nt][c], kGrowth));      // NaN: it becomes the maximum
             }
         if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
             for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                 for (int c = 0; c < 2; c++) {
-                    const bool up = !(top[nt][c] <= m[nt][c] + kGrowth);
-                    const float alpha = !up ? 1.0f : m[nt][c] == neg_inf() ? 0.0f : ex2(m[nt][c] - top[nt][c]);
+                    const bool up = !(top[nt][c] <= __fadd_rd(m[nt][c], kGrowth));
+                    const float alpha = !up ? 1.0f : m[nt][c] == neg_inf() ? 0.0f :
+                                        ex2(__fadd_rd(kWeightBits, -top[nt][c]) - __fadd_rd(kWeightBits, -m[nt][c]));
                     if (up) m[nt][c] = top[nt][c];
                     l[nt][c] *= alpha;
 #pragma unroll
@@ -453,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
         for (int nt = 0; nt < NT; nt++) {
             float base[2];
 #pragma unroll
-            for (int c = 0; c < 2; c++) base[c] = m[nt][c] == neg_inf() ? 0.0f : kWeightBits - m[nt][c];
+            for (int c = 0; c < 2; c++) base[c] = m[nt][c] == neg_inf() ? 0.0f : __fadd_rd(kWeightBits, -m[nt][c]);
 #pragma unroll
             for (int i = 0; i < 4; i++)
 #pragma unroll
@@ -505,6 +521,20 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(D, 8 * NT)) rows_kerne
         kpg1 = page_of(k0 + 2 * kStride + 16 * (g >> 1)), vpg1 = page_of(k0 + 2 * kStride + 16 * t);
     }
     if (p.status && __any_sync(0xffffffffu, outside) && lane == 0) atomicOr(p.status, kStatusBounds);
+
+    if (wide) {
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+                // what 7 - m lost
+                const float norm = m[nt][c] == neg_inf() ? 1.0f : ex2(kWeightBits - (m[nt][c] + __fadd_rd(kWeightBits, -m[nt][c])));
+                l[nt][c] *= norm;
+#pragma unroll
+                for (int i = 0; i < D / 16; i++) o[nt][i][c] *= norm, o[nt][i][c + 2] *= norm;
+            }
+        __syncwarp();                                            // done with the factors in s_m
+    }
 
     // join the four warps
 #pragma unroll

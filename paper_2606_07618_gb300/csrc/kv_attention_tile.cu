@@ -513,6 +513,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
         const float down = __int_as_float((127 - e) << 23), up = __int_as_float((127 + e) << 23);
         fac = ld_f32(p.c.S_k) * p.scale * 1.4426950408889634f * up;
         if (fac == 0.0f) fac = 1e-37f;                           // hidden scores, -inf, stay that
+        const float first_fac = fac > kWideFactor ? fac : 1.0f;
+        if (fac > kWideFactor) fac = 1.0f;
 #pragma unroll
         for (int i = 0; i < D / 8; i++) {
             uint32_t h[4];
@@ -538,7 +540,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
             uint32_t hid[4];
 #pragma unroll
             for (int c = 0; c < 4; c++) hid[c] = s_hidden[j & 3][c];
-            const bool whole = __all_sync(0xffffffffu, left >= kKeys && !(hid[0] | hid[1] | hid[2] | hid[3]));
+            const bool whole = __all_sync(0xffffffffu, left >= kKeys && first_fac == 1.0f && !(hid[0] | hid[1] | hid[2] | hid[3]));
             float v[4][32];
 #pragma unroll
             for (int c = 0; c < 4; c++) tmem_ld32(ts + 32 * c, v[c]);
@@ -550,7 +552,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                 for (int c = 0; c < 4; c++)
 #pragma unroll
                     for (int i = 0; i < 32; i++)
-                        if (32 * c + i >= left || (hid[c] >> i & 1)) v[c][i] = neg_inf();
+                        v[c][i] = 32 * c + i >= left || (hid[c] >> i & 1) ? neg_inf() : __fmul_rn(v[c][i], first_fac);
                 __syncwarp();
             }
             float tops[4];
@@ -565,9 +567,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                 tops[c] = max3_nan(max3_nan(a, v[c][30], v[c][31]), b2, b2);
             }
             const float top = max3_nan(max3_nan(tops[0], tops[1], tops[2]), tops[3], tops[3]) * fac;
-            const bool grown = top > m + kGrowth;
+            const bool grown = top > __fadd_rd(m, kGrowth);
             if (__any_sync(0xffffffffu, grown)) {
-                const float alpha = !grown ? 1.0f : m == neg_inf() ? 0.0f : ex2(m - top);
+                const float alpha = !grown ? 1.0f : m == neg_inf() ? 0.0f : ex2(__fadd_rd(kBits, -top) - __fadd_rd(kBits, -m));
                 if (grown) m = top;
                 l *= alpha;
                 __syncwarp();                                    // the lanes together for tensor memory
@@ -584,7 +586,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                     }
                 }
             }
-            const float shift = m == neg_inf() ? 0.0f : kBits - m;
+            const float shift = m == neg_inf() ? 0.0f : __fadd_rd(kBits, -m);
             const u64 f2 = pack2(fac, fac), s2 = pack2(shift, shift), one2 = pack2(1.0f, 1.0f);
             u64 sums[2] = {0ull, 0ull};
 #pragma unroll
@@ -612,8 +614,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
         }
         if (ok && !mbar_wait_warp(smem_u32(&s_bars.o_full), 0)) ok = false;
         tc_fence_after();
+        const float norm = m == neg_inf() ? 1.0f : ex2(kBits - (m + __fadd_rd(kBits, -m)));        // what 7 - m lost (kWideFactor)
+        l *= norm;
         // split: the second stream's maximum, sum and O through shared memory (the queries' place) to the first
-        float w0 = 1.0f, w1 = 0.0f;
+        float w0 = norm, w1 = 0.0f;
         const int r = tid & 127;
         auto other = [&](int q) { return sq + (uint32_t)(r * D * 4) + ((q ^ (r & 7)) << 4); };      // 16 bytes of O
         if (split && ok) {
@@ -626,8 +630,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                     tmem_wait_ld(o, z);
 #pragma unroll
                     for (int i = 0; i < 4; i++)
-                        st_shared16(other(c / 4 + i), make_uint4(__float_as_uint(o[4 * i]), __float_as_uint(o[4 * i + 1]),
-                                                                 __float_as_uint(o[4 * i + 2]), __float_as_uint(o[4 * i + 3])));
+                        st_shared16(other(c / 4 + i), make_uint4(__float_as_uint(o[4 * i] * norm), __float_as_uint(o[4 * i + 1] * norm),
+                                                                 __float_as_uint(o[4 * i + 2] * norm), __float_as_uint(o[4 * i + 3] * norm)));
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&s_bars.joined));
@@ -636,17 +640,18 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
             } else {
                 const float2 v = s_ml[r];
                 const float top = fmaxf(m, v.x);
-                w0 = m == neg_inf() ? 0.0f : ex2(m - top);
+                const float w = m == neg_inf() ? 0.0f : ex2(m - top);
+                w0 = w * norm;
                 w1 = v.x == neg_inf() ? 0.0f : ex2(v.x - top);
                 m = top;
-                l = l * w0 + v.y * w1;                           // a NaN sum stays one
+                l = l * w + v.y * w1;                            // a NaN sum stays one
             }
         }
         if (ok && !(split && half == 1)) {
             const int64_t token = row0 + row / p.group, h = head * (int64_t)p.group + row % p.group;
             const int64_t at = PART ? ((part0 + part) * p.tokens + token) * p.q_heads + h : token * p.q_heads + h;
-            const float f = PART ? 1.0f : ld_f32(p.c.S_v) / l;
-            const bool empty = l == 0.0f;                        // saw nothing
+            const float f = (PART ? 1.0f : ld_f32(p.c.S_v) / l) * (split ? 1.0f : norm);
+            const bool empty = m == neg_inf() && l == 0.0f;      // saw nothing (a NaN among its scores makes the sum NaN)
             const bool valid = row < rows;
             __syncwarp();
 #pragma unroll

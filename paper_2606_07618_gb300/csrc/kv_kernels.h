@@ -12,6 +12,14 @@ namespace kv {
 constexpr int kStatusNonFinite = 1;      // a token's x / S is not finite
 constexpr int kStatusBounds = 4;         // a length, slot or page number outside its bounds
 
+// A key's weight is 2^(x f + (7 - m)): x its score, f the factor that makes scores logits of base 2, m the row's largest logit so far, x f
+// rounded; one fused operation on a rounded 7 - m.  |x| < 2 * 128 * 2688 < 2^20, so with f <= kWideFactor logits are below 2^22
+// and the two roundings, the same for all of a row's weights, small.  With larger factors the weight of m's own key could be anywhere
+// (from 2^-64 to 2^64 at 2^30): there scores become rounded logits first, and f is 1, so that differences of close ones are exact.
+// 7 - m, and m + 8, past which a maximum is followed, are rounded down: weights stay within 2^15 however coarse fp32 is there.
+// What 7 - m lost, at most 7, is taken out of a wide row's sums at the end, where parts are joined by their m.
+constexpr float kWideFactor = 4.0f;
+
 struct Cache {
     uint8_t *codes, *sf;                 // [pages][heads][2][page][dim/2], [pages][heads][2][dim/16][page]
     const float *S_k, *S_v;
