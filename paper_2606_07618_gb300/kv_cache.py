@@ -31,7 +31,7 @@ from . import binding as B
 
 
 class Prefix:
-    """The pages and tokens of a prompt that several sequences share."""
+    """The pages and tokens of a prompt that several sequences share; pages is None once it is dropped."""
 
     def __init__(self, pages, length: int):
         self.pages, self.length, self.users = pages, length, 0
@@ -64,6 +64,8 @@ class Pages:
 
     def add(self, prefix: Prefix | None = None) -> int:
         """A new sequence without tokens (behind a prefix, if given); its number."""
+        if prefix is not None and prefix.pages is None:
+            raise ValueError("the prefix was dropped")
         self.next += 1
         self.sequences[self.next] = _Sequence(prefix)
         if prefix is not None:
@@ -90,10 +92,13 @@ class Pages:
             s.prefix.users -= 1
 
     def drop_prefix(self, prefix: Prefix) -> None:
+        """Ends a prefix that no sequence is behind; its pages are free again."""
+        if prefix.pages is None:
+            raise ValueError("the prefix was dropped before")
         if prefix.users:
             raise ValueError(f"{prefix.users} sequences are behind this prefix")
         self.free += prefix.pages
-        prefix.pages, prefix.length = [], 0
+        prefix.pages, prefix.length = None, 0
 
     def step(self, new) -> Step:
         """Makes room for new tokens, [(sequence, tokens), ..], each sequence once, all behind the same prefix or none of them

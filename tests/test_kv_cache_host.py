@@ -52,6 +52,22 @@ def test_prefix():
     assert len(p.free) == 10
 
 
+def test_a_dropped_prefix_is_refused():
+    """Sequences added behind it would attend without their prompt."""
+    p = pages()
+    a = p.add()
+    p.step([(a, 40)])
+    pre = p.share(a)
+    p.drop_prefix(pre)
+    with pytest.raises(ValueError):
+        p.add(pre)
+    with pytest.raises(ValueError):
+        p.drop_prefix(pre)
+    assert len(p.free) == 10 and not p.sequences and pre.users == 0
+    b = p.add()
+    assert p.step([(b, 3)]).positions.tolist() == [0, 1, 2]
+
+
 def test_refusals():
     for size in (8, 24, 2048, 0):
         with pytest.raises(ValueError):
