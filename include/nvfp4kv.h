@@ -147,9 +147,11 @@ nvfp4_status nvfp4_kv_attention(const nvfp4_kv_cache* cache, const void* q, int6
  * Self-test of the bounded waits (failure detection): nvfp4_kv_attention, of more than 16 rows a
  * sequence and key head (max_q * q_heads / heads; fewer have no such waits: NVFP4_ERR_UNSUPPORTED),
  * whose waits for keys are made to give up after their limit, by barriers that expect one arrival too
- * many.  status_dev (required) gets bit 4 (16), out is not written by the blocks that gave up (what is
- * joined from the workspace is undefined) and the CUDA context stays usable.
+ * many; with NVFP4_KV_STARVE_VALUES added to `causal` the waits for values instead.  status_dev (required) gets bit 4
+ * (16), out is not written by the blocks that gave up (what is joined from the workspace is undefined) and the CUDA
+ * context stays usable.
  */
+#define NVFP4_KV_STARVE_VALUES 2
 nvfp4_status nvfp4_kv_selftest_wait_timeout(const nvfp4_kv_cache* cache, const void* q, int64_t q_token, int64_t q_head,
                                             int64_t tokens, int q_heads, const int32_t* table, int64_t table_ld,
                                             int64_t width, const int32_t* lens, const int32_t* offsets, int64_t batch,

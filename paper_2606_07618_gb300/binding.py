@@ -27,6 +27,7 @@ FP4_ACT_SILU, FP4_ACT_GELU_TANH = 0, 1
 NVFP4_ROPE_NEIGHBOURS, NVFP4_ROPE_HALVES = 0, 1
 NVFP4_ROPE_PLAIN, NVFP4_ROPE_LINEAR, NVFP4_ROPE_BASE, NVFP4_ROPE_BANDS = 0, 1, 2, 3
 NVFP4_KV_ABSMAX, NVFP4_KV_SWEEP = 0, 1
+NVFP4_KV_STARVE_VALUES = 2
 
 STATUS = {0: "NVFP4_OK", 1: "NVFP4_ERR_INVALID_ARG", 2: "NVFP4_ERR_UNSUPPORTED", 3: "NVFP4_ERR_ALIGNMENT",
           4: "NVFP4_ERR_RANGE", 5: "NVFP4_ERR_CUDA"}
@@ -725,7 +726,7 @@ def _attention(fn: str, q, cache, prefix, table, lens, offsets, max_q, scale, ou
         ws, ws_bytes = _buffer(workspace, 0, "workspace"), workspace.nbytes
     pt, ld, batch, width = _pages(table, "table")
     rc = getattr(_lib or lib(), fn)(c, *_heads3(q, "q"), tokens, q_heads, *prefix, pt, ld, width, _list(lens, batch, _I32, "lens"),
-                                    _list(offsets, batch + 1, _I32, "offsets"), batch, max_q, scale, 1 if causal else 0,
+                                    _list(offsets, batch + 1, _I32, "offsets"), batch, max_q, scale, int(causal),
                                     *_heads3(out, "out"), lse, _status(status), ws, ws_bytes, _stream(stream))
     _check(fn, rc)
 
@@ -739,10 +740,10 @@ def nvfp4_kv_attention(q, cache, table, lens, offsets, max_q: int, scale: float,
 
 
 def nvfp4_kv_selftest_wait_timeout(q, cache, table, lens, offsets, max_q: int, scale: float, out, status, workspace=None,
-                                   stream=None):
-    """nvfp4_kv_attention whose waits for keys run out (status bit 4).  See nvfp4kv.h."""
-    _attention("nvfp4_kv_selftest_wait_timeout", q, cache, (), table, lens, offsets, max_q, scale, out, True, None, workspace,
-               status, stream)
+                                   stream=None, values: bool = False):
+    """nvfp4_kv_attention whose waits for keys, or for values, run out (status bit 4).  See nvfp4kv.h."""
+    _attention("nvfp4_kv_selftest_wait_timeout", q, cache, (), table, lens, offsets, max_q, scale, out,
+               1 + (NVFP4_KV_STARVE_VALUES if values else 0), None, workspace, status, stream)
 
 
 def nvfp4_kv_attention_prefix(q, cache, prefix, prefix_len, table, lens, offsets, max_q: int, scale: float, out,

@@ -411,7 +411,8 @@ nvfp4_status nvfp4_kv_selftest_wait_timeout(const nvfp4_kv_cache* cache, const v
                                             int* status_dev, void* workspace, size_t ws_bytes, void* stream) {
     if (!status_dev) return NVFP4_ERR_INVALID_ARG;
     return attention(cache, q, q_token, q_head, tokens, q_heads, false, nullptr, 0, nullptr, table, table_ld, width, lens, offsets,
-                     batch, max_q, scale, causal, out, out_token, out_head, lse, status_dev, workspace, ws_bytes, 1, stream);
+                     batch, max_q, scale, causal & ~NVFP4_KV_STARVE_VALUES, out, out_token, out_head, lse, status_dev, workspace, ws_bytes,
+                     causal & NVFP4_KV_STARVE_VALUES ? 2 : 1, stream);
 }
 
 nvfp4_status nvfp4_kv_attention_prefix(const nvfp4_kv_cache* cache, const void* q, int64_t q_token, int64_t q_head,

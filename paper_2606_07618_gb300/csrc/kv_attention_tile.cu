@@ -201,7 +201,7 @@ struct Shape {
 };
 
 struct Bars {
-    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full, joined, q_full;
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full, drained, joined, q_full;
 };
 
 // A token's codes and scales of K or V on their way.
@@ -305,14 +305,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
     if (tid == 0) {
         const int more = CG == 2 && rank == 0;                   // the other CTA's word
         for (int i = 0; i < 2; i++) {
-            mbar_init(smem_u32(&s_bars.k_full[i]), 4 + more + p.starve);
-            mbar_init(smem_u32(&s_bars.v_full[i]), 4 + more);
+            mbar_init(smem_u32(&s_bars.k_full[i]), 4 + more + (p.starve == 1));
+            mbar_init(smem_u32(&s_bars.v_full[i]), 4 + more + (p.starve == 2));
             mbar_init(smem_u32(&s_bars.k_empty[i]), 1);
             mbar_init(smem_u32(&s_bars.v_empty[i]), 1);
             mbar_init(smem_u32(&s_bars.s_full[i]), 1);
             mbar_init(smem_u32(&s_bars.p_full[i]), CG * 4);
         }
         mbar_init(smem_u32(&s_bars.o_full), 1);
+        mbar_init(smem_u32(&s_bars.drained), 1);
         mbar_init(smem_u32(&s_bars.joined), 4);
         mbar_init(smem_u32(&s_bars.q_full), kSoftmaxWarps + more);
         s_abort = 0;
@@ -461,8 +462,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(Attention p, Pass
                 if (j + 1 < tiles) commit(&s_bars.k_empty[nx]);
             }
         }
-        commit(&s_bars.o_full);                                  // after every MMA issued, also on a timeout
-        if (!mbar_wait_warp(smem_u32(&s_bars.o_full), 0)) ok = false;
+        // after every MMA issued: to the softmax warps, too, where none is missing
+        uint64_t* done = ok ? &s_bars.o_full : &s_bars.drained;
+        commit(done);
+        if (!mbar_wait_warp(smem_u32(done), 0)) ok = false;
         } else if (CG == 2 && warp == kMmaWarp) {
             // the second CTA's operands are there: said here for its warps
             auto relay = [&](uint64_t* bar, int parity) {

@@ -79,7 +79,7 @@ struct Attention {
     // they have waited for what came before the call themselves; so it does not wait for the first before it merges
     // its results, or before its end (which the join then waits for).
     int second;
-    int starve;                          // 1: the waits for keys run out (self-test)
+    int starve;                          // 1: the waits for keys run out, 2: those for values (self-test)
 };
 
 cudaError_t launch_rope(const Rope& p, int sms, cudaStream_t s);
