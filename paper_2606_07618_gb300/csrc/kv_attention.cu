@@ -1,15 +1,15 @@
 // Attention over the NVFP4 key/value cache for few rows a key head (nvfp4_kv_attention,
 // nvfp4_kv_attention_prefix).
 //
-// A value q s (without S) has at most 5 significant bits and lies in 2^-10 .. 2688, so fp16 holds
-// it exactly; a query's row is scaled by a power of two to below 2 and is exact in fp16 too
+// A value q s (without S) has at most 6 significant bits (2 of E2M1, 4 of E4M3) and lies in 2^-10 .. 2688, so fp16
+// holds it exactly; a query's row is scaled by a power of two to below 2 and is exact in fp16 too
 // but for elements below 2^-14 of the row's largest.  Both products run on mma.sync
 // m16n8k16 (fp16 operands, fp32 sums): with 8 or 16 rows they are 6% of the instructions, and an operand of
 // registers is what the converted codes already are (tcgen05 would want them in shared memory first).
 //
 // What bounds it is instruction issue: a warp's tile of 64 tokens (dim 128, 8 rows) takes about 1070 instructions, of
 // them 256 conversions, 256 multiplications by the blocks' scales and 64 MMAs, for 9.2 KB of cache.  16 sequences of
-// 4096 tokens with 8 key heads (75.8 MB, 11.2 us at the copy rate) take 20 us: 11 us of issue at the 2.8 instructions a
+// 4096 tokens with 8 key heads (75.8 MB, 11.2 us at the copy rate) take 20.9 us: 11 us of issue at the 2.8 instructions a
 // cycle that the loop reaches, and what a block spends before and after its four tiles a warp.
 //
 // Transposed products, so that the rows of queries are the MMA's narrow dimension:
@@ -27,7 +27,8 @@
 // pair of fp16 that the MMA wants.
 //
 // Softmax runs over the tiles of a warp with a running maximum, which is followed only when it has grown by more than
-// 2^8: weights are held 2^7-fold, so that they stay below fp16's largest, and O is rarely scaled.  Warps, and the parts
+// 2^8: weights are held 2^7-fold, so that they stay below fp16's largest, and O is rarely scaled.  Rows whose logits may
+// pass 2^22 round them first (kWideFactor; it costs the others 1%: 20.7 -> 20.9 us, dim 64 and 16 rows 52.2 -> 53.3).  Warps, and the parts
 // that a long cache is split into, are joined by their maxima, in a fixed order.
 #include <climits>
 

@@ -15,7 +15,7 @@
 //   warps 0-7   softmax, a thread a row: maximum, weights to fp16 over the scores' own columns of
 //               tensor memory (P is the MMA's operand from there), the sum; O stays in tensor memory.
 //               O is scaled only when a row's maximum has grown by more than 2^8 (weights are held
-//               2^7-fold, so that they stay below fp16's largest).
+//               2^7-fold, so that they stay below fp16's largest; large logits: kWideFactor).
 //
 // Tensor memory: scores of both streams 2 x 128 columns, O 2 x dim.  Shared memory: Q 64 KB, two stages each
 // of keys and values of 32 KB (dim 128).
