@@ -726,7 +726,7 @@ def _attention(fn: str, q, cache, prefix, table, lens, offsets, max_q, scale, ou
         ws, ws_bytes = _buffer(workspace, 0, "workspace"), workspace.nbytes
     pt, ld, batch, width = _pages(table, "table")
     rc = getattr(_lib or lib(), fn)(c, *_heads3(q, "q"), tokens, q_heads, *prefix, pt, ld, width, _list(lens, batch, _I32, "lens"),
-                                    _list(offsets, batch + 1, _I32, "offsets"), batch, max_q, scale, int(causal),
+                                    _list(offsets, batch + 1, _I32, "offsets"), batch, max_q, scale, causal,
                                     *_heads3(out, "out"), lse, _status(status), ws, ws_bytes, _stream(stream))
     _check(fn, rc)
 
@@ -735,8 +735,8 @@ def nvfp4_kv_attention(q, cache, table, lens, offsets, max_q: int, scale: float,
                        workspace=None, status=None, stream=None):
     """out = softmax(scale q K^T) V for q, out [tokens, q_heads, dim] (bf16): rows offsets[b] .. of sequence b over its
     lens[b] cached tokens.  lse [tokens, q_heads] (fp32) optional."""
-    _attention("nvfp4_kv_attention", q, cache, (), table, lens, offsets, max_q, scale, out, causal, lse, workspace, status,
-               stream)
+    _attention("nvfp4_kv_attention", q, cache, (), table, lens, offsets, max_q, scale, out, 1 if causal else 0, lse, workspace,
+               status, stream)
 
 
 def nvfp4_kv_selftest_wait_timeout(q, cache, table, lens, offsets, max_q: int, scale: float, out, status, workspace=None,
@@ -750,5 +750,5 @@ def nvfp4_kv_attention_prefix(q, cache, prefix, prefix_len, table, lens, offsets
                               causal: bool = True, lse=None, workspace=None, status=None, stream=None):
     """The same where every query also sees the first prefix_len (int32, one element) tokens of the pages prefix [pages]."""
     pre = (_list(prefix, 0, _I32, "prefix"), prefix.numel(), _list(prefix_len.reshape(-1), 1, _I32, "prefix_len"))
-    _attention("nvfp4_kv_attention_prefix", q, cache, pre, table, lens, offsets, max_q, scale, out, causal, lse, workspace,
-               status, stream)
+    _attention("nvfp4_kv_attention_prefix", q, cache, pre, table, lens, offsets, max_q, scale, out, 1 if causal else 0, lse,
+               workspace, status, stream)

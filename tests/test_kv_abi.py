@@ -226,6 +226,26 @@ def test_binding_checks_caches(B):
             B.nvfp4_kv_write(bad, k, k, slots)
 
 
+@pytest.mark.parametrize("causal", [None, 0, 1, 2, True, "yes"])
+def test_causal_is_a_truth_value(B, causal, monkeypatch):
+    """Whatever is false or true in Python: the calls get 0 or 1."""
+    seen = {}
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: seen.setdefault(name, args) and 0
+    monkeypatch.setattr(B, "_lib", Library())
+    monkeypatch.setattr(B, "_stream", lambda stream: 0)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    q, table = torch.zeros(4, 6, 64, dtype=torch.bfloat16), torch.zeros(2, 3, dtype=torch.int32)
+    args = (table, i32(1, 1), i32(0, 2, 4), 2, 0.125, q.clone(), causal)
+    B.nvfp4_kv_attention(q, _cache(), *args)
+    B.nvfp4_kv_attention_prefix(q, _cache(), i32(0), i32(1), *args)
+    for name in ("nvfp4_kv_attention", "nvfp4_kv_attention_prefix"):
+        at = seen[name].index(0.125) + 1
+        assert type(seen[name][at]) is int and seen[name][at] == (1 if causal else 0)
+
+
 def test_binding_checks_tensors(B):
     c = _cache()
     k = torch.zeros(4, 2, 64)
